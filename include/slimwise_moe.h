@@ -363,6 +363,107 @@ int slimwise_moe_noalloc_device_status(void *stream, int32_t *flags);
 int slimwise_moe_device_status(const void *workspace, void *stream,
                                int32_t *flags);
 
+/*
+ * Operators over rows of vocabulary logits: what the optional distillation of
+ * the pruned decoder trains on (Sec. 3.3, Eq. 3) and what a decode step
+ * answers with.  Shared by the three entry points:
+ *
+ *   logits      bf16 or fp32 [rows, vocab], row t at logits + t * row_stride
+ *               elements; any start, stride and vocabulary (rows need only
+ *               their elements' alignment)
+ *   dtype       SLIMWISE_DTYPE_BF16 or SLIMWISE_DTYPE_FP32 (others:
+ *               SLIMWISE_ERR_UNSUPPORTED_SHAPE)
+ *   rows        0 <= rows <= 2^20 (0: a no-op); vocab 1 <= vocab <= 393216
+ *               (else UNSUPPORTED_SHAPE); row_stride >= vocab
+ *   other arrays are 4-byte aligned, [rows] or [rows, k] row-major
+ *
+ * They need no workspace, keep no state, and do not synchronise.  What only
+ * the device can see (a NaN logit, an id outside the vocabulary) is reported
+ * in that row's results, as each entry point says.  The results of a row do
+ * not depend on the other rows of the call.
+ */
+enum { SLIMWISE_DTYPE_BF16 = 0, SLIMWISE_DTYPE_FP32 = 1 };
+
+/*
+ * The k largest logits of each row as log-probabilities at a temperature: the
+ * targets that a teacher (the full-pool layer's model) leaves for distillation.
+ *   k            1 <= k <= min(256, vocab)
+ *   temperature  in [1e-6, 1e6]
+ *   ids          int32 [rows, k]  larger logit first, ties to the lower id
+ *   logp         fp32 [rows, k]   z / temperature - logsumexp(z / temperature)
+ *   log_rest     fp32 [rows]      log of the mass of all other elements
+ *                                 (-inf: none)
+ * A row with NaN or +inf, or of -inf alone, has NaN in logp and log_rest; ids
+ * are then the largest of the other elements, padded with -1.
+ */
+int slimwise_top_logits(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
+                        int64_t row_stride, int32_t k, float temperature, int32_t *ids,
+                        float *logp, float *log_rest, void *stream);
+
+/*
+ * The distillation loss and, where grad is given, its gradient:
+ *   L_t  = alpha CE_t + (1 - alpha) temperature^2 KL_t
+ *   CE_t = -log softmax(z_t)[label_t]
+ *   KL_t = sum_j P_j (log P_j - log q_j) + r (log r - log Q), with
+ *          P_j = exp top_logp[t, j], r = exp log_rest[t],
+ *          q = softmax(z_t / temperature), q_j at top_ids[t, j], and Q the
+ *          mass of q outside the list (terms with P_j = 0 or r = 0 are 0)
+ *   loss = sum_t row_weight[t] L_t,   grad[t] = row_weight[t] dL_t / dz_t
+ *
+ *   labels       int32 [rows]; a negative label leaves its row out: L_t = 0
+ *                and a gradient row of zeros, whatever the row holds
+ *   top_ids      int32 [rows, k], distinct within a row (else the row's
+ *                results are undefined); negative: the entry is absent
+ *   top_logp, log_rest  fp32, as slimwise_top_logits writes them
+ *   k            1 <= k <= min(256, vocab)
+ *   alpha        in [0, 1];  temperature in [1e-6, 1e6]
+ *   row_weight   fp32 [rows], NULL: 1 each
+ *   row_loss     fp32 [rows]   L_t, without its weight
+ *   loss         fp32 [1], NULL to skip; the same bits on every run
+ *   grad         dtype [rows, vocab] at grad_stride >= vocab, NULL to skip.
+ *                It may be `logits` itself (same stride) and may not overlap
+ *                it otherwise (SLIMWISE_ERR_INVALID_ARG).  Rows that start at
+ *                the same offset from a 16-byte boundary as the logits' are
+ *                written fastest.
+ * A label or id >= vocab gives its row NaN loss and gradient; NaN and +inf
+ * logits spread over their row as they do in the formulas.  Where Q is 0 with
+ * r > 0 the loss is +inf and the residual's share of the gradient is left out.
+ */
+int slimwise_distill_loss(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
+                          int64_t row_stride, const int32_t *labels, const int32_t *top_ids,
+                          const float *top_logp, const float *log_rest, int32_t k, float alpha,
+                          float temperature, const float *row_weight, float *row_loss,
+                          float *loss, void *grad, int64_t grad_stride, void *stream);
+
+/*
+ * One token of each row, drawn with a given random number.  With m the row's
+ * largest logit, e_i = exp((z_i - m) / T) and whole-number weights
+ * w_i = floor(2^40 e_i), in order of value (ties: lower id first):
+ *   top-k   the first top_k elements (top_k <= 0 or >= vocab: all), mass M
+ *   top-p   of these, those before which a mass under top_p M lies, the first
+ *           always (top_p >= 1: all)
+ *   min-p   of these, those with e_i >= min_p (min_p <= 0: all)
+ * and the token is the first id, ascending, at which the kept mass exceeds
+ * uniform times its total.  Sums of whole numbers do not depend on their
+ * order: a row's token is the same whatever the batch.  top_p and uniform
+ * count to 24 bits.
+ *   temperature  fp32 [rows], NULL: 1; 0 (or below FLT_MIN): the largest
+ *                element, logprob 0
+ *   top_k        int32 [rows], NULL: all;  top_p fp32 [rows], NULL: 1;
+ *   min_p        fp32 [rows], NULL: 0
+ *   uniform      fp32 [rows] in [0, 1)
+ *   tokens       int32 [rows]
+ *   logprob      fp32 [rows]  log of the token's share of the kept mass
+ * A row whose request is out of range (temperature negative or not finite,
+ * top_p negative, min_p above 1, uniform outside [0, 1), any of them NaN) or
+ * whose logits have no distribution (NaN, +inf, or -inf alone) gets token -1
+ * and logprob NaN.
+ */
+int slimwise_sample(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
+                    int64_t row_stride, const float *temperature, const int32_t *top_k,
+                    const float *top_p, const float *min_p, const float *uniform,
+                    int32_t *tokens, float *logprob, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,6 +9,7 @@ from .binding import (  # noqa: F401
     SlimwiseError,
     alloc_workspace,
     load,
+    slimwise_distill_loss,
     slimwise_moe_compact_layer,
     slimwise_moe_decode,
     slimwise_moe_decode_ex,
@@ -21,4 +22,6 @@ from .binding import (  # noqa: F401
     slimwise_moe_select_retained,
     slimwise_moe_shared_workspace_size,
     slimwise_moe_workspace_size,
+    slimwise_sample,
+    slimwise_top_logits,
 )

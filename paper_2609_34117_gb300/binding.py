@@ -36,6 +36,7 @@ EXPORTED = (
     "slimwise_moe_shared_workspace_size", "slimwise_moe_decode_shared",
     "slimwise_moe_decode_shared_ex", "slimwise_moe_expert_stats", "slimwise_moe_select_retained",
     "slimwise_moe_noalloc_device_status", "slimwise_moe_compact_layer",
+    "slimwise_top_logits", "slimwise_distill_loss", "slimwise_sample",
 )
 
 
@@ -98,6 +99,11 @@ def load(path: str | None = None) -> ctypes.CDLL:
             lib.slimwise_moe_expert_stats.argtypes = [P, P, P, P, i32, P, P, P, SP, P, sz]
             lib.slimwise_moe_select_retained.argtypes = [P, i32, i32, i32, P, P]
             lib.slimwise_moe_compact_layer.argtypes = [P, P, P, P, i32, SP, P, P, P, P, P]
+            i64, f32 = ctypes.c_int64, ctypes.c_float
+            rows = [P, i32, i32, i32, i64]
+            lib.slimwise_top_logits.argtypes = rows + [i32, f32, P, P, P, P]
+            lib.slimwise_distill_loss.argtypes = rows + [P, P, P, P, i32, f32, f32, P, P, P, P, i64, P]
+            lib.slimwise_sample.argtypes = rows + [P] * 8
             for name in EXPORTED[1:]:
                 getattr(lib, name).restype = ctypes.c_int
             _lib = lib
@@ -419,3 +425,124 @@ def slimwise_moe_noalloc_device_status(stream=None) -> int:
     if rc not in (0, 5):
         _check(rc, "slimwise_moe_noalloc_device_status")
     return int(flags.value)
+
+
+_DTYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _logits(t, name="logits"):
+    """(pointer, dtype code, rows, vocab, row stride) of a row-major matrix whose
+    rows may be further apart than they are long."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be torch.bfloat16 or torch.float32, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    rows, vocab = t.shape
+    # a dimension of one element has no stride of its own
+    if vocab > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), code, rows, vocab, t.stride(0) if rows > 1 else vocab
+
+
+def _vec(t, dtype, shape, name, device):
+    """Pointer of an optional contiguous array of the call's rows (None: NULL)."""
+    if t is None:
+        return None
+    _dev(t, dtype, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    return t.data_ptr()
+
+
+def slimwise_top_logits(logits, k, temperature=1.0, ids=None, logp=None, log_rest=None,
+                        stream=None):
+    """A teacher's distillation targets: the k largest logits of each row as
+    log-probabilities at a temperature, and the log of the others' mass.
+    Returns (ids int32 [rows, k], logp fp32 [rows, k], log_rest fp32 [rows])."""
+    row_args = _logits(logits)
+    rows, k, dev = row_args[2], int(k), logits.device
+    if ids is None:
+        ids = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
+    if logp is None:
+        logp = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=dev)
+    if log_rest is None:
+        log_rest = torch.empty(rows, dtype=torch.float32, device=dev)
+    _check(load().slimwise_top_logits(
+        *row_args, k, temperature, _vec(ids, torch.int32, (rows, k), "ids", dev),
+        _vec(logp, torch.float32, (rows, k), "logp", dev),
+        _vec(log_rest, torch.float32, (rows,), "log_rest", dev), _stream(stream)),
+        "slimwise_top_logits")
+    return ids, logp, log_rest
+
+
+def slimwise_distill_loss(logits, labels, top_ids, top_logp, log_rest, alpha=0.1, temperature=1.0,
+                          row_weight=None, grad=True, row_loss=None, loss=None, stream=None):
+    """Distillation loss of a student's logits against a teacher's targets
+    (Sec. 3.3, Eq. 3) and its gradient.  grad: True to allocate the gradient (in
+    the logits' type and row stride), False for the loss alone, or the tensor to
+    write (`logits` itself: in place).  row_weight: fp32 [rows], e.g. 1 / the
+    number of labelled rows; None: 1 each.  Returns (loss fp32 [1], row losses
+    fp32 [rows], gradient or None)."""
+    row_args = _logits(logits)
+    _, _, rows, vocab, stride = row_args
+    dev, f32 = logits.device, torch.float32
+    if not isinstance(top_ids, torch.Tensor) or top_ids.dim() != 2:
+        raise ValueError("top_ids must have two dimensions")
+    k = top_ids.shape[1]
+    g_ptr, g_stride = None, 0
+    if grad is True:
+        grad = torch.empty((rows, stride), dtype=logits.dtype, device=dev)[:, :vocab]
+        g_ptr, g_stride = grad.data_ptr(), stride
+    elif grad is False or grad is None:
+        grad = None
+    else:
+        g_ptr, code, g_rows, g_vocab, g_stride = _logits(grad, "grad")
+        if code != row_args[1] or (g_rows, g_vocab) != (rows, vocab) or grad.device != dev:
+            raise ValueError("grad must have the logits' type, shape and device")
+    if row_loss is None:
+        row_loss = torch.empty(rows, dtype=f32, device=dev)
+    if loss is None:
+        # the sum over no rows is not computed by a kernel
+        loss = torch.empty(1, dtype=f32, device=dev) if rows else torch.zeros(1, dtype=f32, device=dev)
+    for t, name in ((labels, "labels"), (top_ids, "top_ids"), (top_logp, "top_logp"),
+                    (log_rest, "log_rest")):
+        if t is None:
+            raise TypeError(f"{name} must be a CUDA tensor")
+    _check(load().slimwise_distill_loss(
+        *row_args, _vec(labels, torch.int32, (rows,), "labels", dev),
+        _vec(top_ids, torch.int32, (rows, k), "top_ids", dev),
+        _vec(top_logp, f32, (rows, k), "top_logp", dev),
+        _vec(log_rest, f32, (rows,), "log_rest", dev), k, alpha, temperature,
+        _vec(row_weight, f32, (rows,), "row_weight", dev),
+        _vec(row_loss, f32, (rows,), "row_loss", dev), _vec(loss, f32, (1,), "loss", dev),
+        g_ptr, g_stride, _stream(stream)), "slimwise_distill_loss")
+    return loss, row_loss, grad
+
+
+def slimwise_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None,
+                    tokens=None, logprob=None, stream=None):
+    """One token of each row with the given random numbers uniform fp32 [rows] in
+    [0, 1).  temperature, top_p, min_p (fp32 [rows]) and top_k (int32 [rows]) are
+    the rows' requests; None: 1, 1, 0 and all.  Temperature 0 takes the largest
+    logit.  Returns (tokens int32 [rows], log of each token's share fp32 [rows])."""
+    row_args = _logits(logits)
+    rows, dev, f32 = row_args[2], logits.device, torch.float32
+    if uniform is None:
+        raise TypeError("uniform must be a CUDA tensor")
+    if tokens is None:
+        tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+    if logprob is None:
+        logprob = torch.empty(rows, dtype=f32, device=dev)
+    shape = (rows,)
+    _check(load().slimwise_sample(
+        *row_args, _vec(temperature, f32, shape, "temperature", dev),
+        _vec(top_k, torch.int32, shape, "top_k", dev), _vec(top_p, f32, shape, "top_p", dev),
+        _vec(min_p, f32, shape, "min_p", dev), _vec(uniform, f32, shape, "uniform", dev),
+        _vec(tokens, torch.int32, shape, "tokens", dev), _vec(logprob, f32, shape, "logprob", dev),
+        _stream(stream)), "slimwise_sample")
+    return tokens, logprob

@@ -1,0 +1,449 @@
+// sample.cu -- one token per row of logits, drawn with a given random number
+// under the row's temperature, top-k, top-p and min-p.
+//
+// With z' = z / T and m the largest logit, an element's weight is the whole
+// number w = floor(2^40 exp((z - m) / T)).  Masses are then sums of whole
+// numbers, so that no result depends on how a row was split or in which order
+// it was summed, and a draw is the same on every batch size.  In order of
+// value (ties: lower id):
+//   top-k  the first k elements, of mass M
+//   top-p  those of them before which less than p M lies (the first always)
+//   min-p  those of them with exp((z - m) / T) >= min_p
+// and the token is the first id, ascending, at which the kept mass exceeds
+// u times its total.  p and u are taken in 24 bits.
+//
+// Nearly every row is decided by its best few elements, which the scan of
+// vocab.cuh finds in the one read that bounds this kernel.  The mass of the
+// whole row, which a nucleus without top-k needs, comes from the same read as a
+// float; it decides except where the nucleus would end within that sum's error
+// bound, and then the leader sums the exact mass in a second pass.  Rows that
+// keep more than the listed elements (a wide nucleus, no filter at all) are
+// left to the end and then searched by the whole cluster: thresholds that split
+// the remaining range of values in eight, a pass over the row each.
+#include "vocab.cuh"
+
+namespace slimwise {
+
+constexpr int kSampleCtas = 3;    // CTAs of an SM
+constexpr int kNucleus = 64;      // elements looked at for a nucleus or min-p without top-k
+constexpr int kTopKListed = kTopMax;  // largest top-k that is decided from the list
+constexpr int32_t kLeftOver = -2; // a token that is still to be searched (its logprob: the maximum)
+constexpr float kWeightOne = 1099511627776.0f;  // 2^40, the largest element's weight
+// Bound of the relative difference between the scan's float mass and the sum of
+// the weights.  Elements at 2^-x of the largest hold a share of at most
+// V 2^-x, so exponents beyond 19 do not count; to there, an exponent rounded
+// three times in each of the two and a logarithm's base rounded twice make
+// 19 (1.5 2^-23 + 2^-23) ln 2 < 2^-18.3; exp2's and exp's own 2^-22, and sums
+// of 19 roundings (8 in a window, 2 of the compensated sum, 8 + 1 over threads
+// and CTAs) 2^-19.7; the weights' truncation V 2^-40.
+constexpr double kMassError = 1.0 / 131072.0;
+
+enum SampleMode { kDone = 0, kExactMass = 1, kSearch = 2 };
+
+struct SampleShared {
+  uint64_t weight[kTopMax];
+  uint64_t slot[2][kClusterMax][8];  // each CTA's sums of a pass
+  uint64_t red[kScanWarps][8];
+};
+
+__device__ __forceinline__ uint64_t fraction(uint64_t mass, uint64_t f24) {
+  return ((mass >> 32) * f24 << 8) + ((mass & 0xFFFFFFFFull) * f24 >> 24);
+}
+
+struct Draw {  // one row's request
+  float inv;   // 1 / T
+  float min_p;
+  int top_k;   // 1 .. vocab
+  uint64_t p24, u24;
+  bool limited, nucleus;  // whether top-k, top-p leave anything out
+};
+__device__ __forceinline__ float element_exp(float z, float m, float inv) {
+  return expf(__fmul_rn(__fsub_rn(z, m), inv));
+}
+__device__ __forceinline__ uint64_t element_weight(float e) {
+  return (uint64_t)__float2ull_rz(e * kWeightOne);
+}
+
+// Sums of N whole numbers over the cluster; slot[parity] keeps each CTA's.
+template <int N>
+__device__ __forceinline__ void cluster_sum(uint64_t (&v)[N], int &parity, SampleShared &sh) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+    if ((tid & 31) == 0) sh.red[tid >> 5][i] = v[i];
+  }
+  __syncthreads();
+  if (tid < N * C) {
+    const int i = tid % N;
+    uint64_t s = 0;
+    for (int w = 0; w < kScanWarps; ++w) s += sh.red[w][i];
+    *cluster.map_shared_rank(&sh.slot[parity][rank][i], tid / N) = s;
+  }
+  cluster.sync();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = 0;
+    for (int r = 0; r < C; ++r) v[i] += sh.slot[parity][r][i];
+  }
+  parity ^= 1;
+}
+
+// The part of a row that this CTA passes over, and what a pass counts.
+template <typename T>
+struct Part {
+  Row<T> row;
+  int lo, hi;
+  float m, inv;
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    constexpr int E = Row<T>::E;
+    for (int i = lo + (int)threadIdx.x; i < hi; i += kScanThreads) {
+      float z[E];
+      unpack<T>(load_window(row, i), z);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int id = i * E - row.mis + e;
+        if (id >= 0 && id < row.vocab) f(z[e], id);
+      }
+    }
+  }
+};
+
+// A prefix of the order: values above `o`, and of those equal to it the ids up
+// to `id`.
+struct Limit {
+  uint32_t o;
+  int id;
+  __device__ __forceinline__ bool has(uint32_t v, int i) const { return v > o || (v == o && i <= id); }
+};
+
+// The largest v with amount(values >= v within `in`) >= want, and in `above`
+// the amount of the values > v.  `mass`: amounts are weights, else counts.
+// start: a value for which the amount is known to suffice; top: the largest.
+template <typename T>
+__device__ __noinline__ uint32_t search_value(const Part<T> &part, Limit in, bool mass,
+                                              uint64_t want, uint32_t start, uint32_t top,
+                                              uint64_t &above, int &parity, SampleShared &sh) {
+  uint64_t a = start, b = (uint64_t)top + 1;
+  above = 0;
+  while (b - a > 1) {
+    const uint64_t span = b - a;
+    uint64_t v[7] = {0, 0, 0, 0, 0, 0, 0};
+    part.each([&](float z, int id) {
+      const uint32_t o = ordered(z);
+      if (!in.has(o, id)) return;
+      const uint64_t w = mass ? element_weight(element_exp(z, part.m, part.inv)) : 1;
+#pragma unroll
+      for (int i = 0; i < 7; ++i) v[i] += o >= a + span * (i + 1) / 8 ? w : 0;
+    });
+    cluster_sum(v, parity, sh);
+    uint64_t na = a, nb = b;
+    for (int i = 0; i < 7; ++i) {
+      const uint64_t t = a + span * (i + 1) / 8;
+      if (v[i] >= want) {
+        na = t;
+      } else if (t < nb) {
+        nb = t;
+        above = v[i];
+      }
+    }
+    a = na;
+    b = nb;
+  }
+  return (uint32_t)a;
+}
+
+// The smallest id such that `want` elements of value o have ids up to it.
+template <typename T>
+__device__ __noinline__ int search_id(const Part<T> &part, uint32_t o, uint64_t want, int &parity,
+                                      SampleShared &sh) {
+  int a = -1, b = part.row.vocab - 1;  // too few up to a, enough up to b
+  while (b - a > 1) {
+    const int64_t span = b - a;
+    uint64_t v[7] = {0, 0, 0, 0, 0, 0, 0};
+    part.each([&](float z, int id) {
+      if (ordered(z) != o) return;
+#pragma unroll
+      for (int i = 0; i < 7; ++i) v[i] += id <= a + span * (i + 1) / 8 ? 1 : 0;
+    });
+    cluster_sum(v, parity, sh);
+    int na = a, nb = b;
+    for (int i = 6; i >= 0; --i) {
+      const int t = a + (int)(span * (i + 1) / 8);
+      if (v[i] >= want) nb = t;
+      else if (t > na) na = t;
+    }
+    a = na;
+    b = nb;
+  }
+  return b;
+}
+
+// The whole request over the whole row, by all CTAs of the cluster.
+template <typename T>
+__device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int &parity,
+                                        int32_t *token, float *logprob, SampleShared &sh) {
+  constexpr int E = Row<T>::E;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t top = ordered(part.m);
+  Limit keep = {0, part.row.vocab};
+  uint64_t above;
+  if (d.limited) {
+    keep.o = search_value(part, keep, false, (uint64_t)d.top_k, 0, top, above, parity, sh);
+    keep.id = search_id(part, keep.o, (uint64_t)d.top_k - above, parity, sh);
+  }
+  if (d.nucleus) {
+    uint64_t mass[1] = {0};
+    part.each([&](float z, int id) {
+      if (keep.has(ordered(z), id)) mass[0] += element_weight(element_exp(z, part.m, part.inv));
+    });
+    cluster_sum(mass, parity, sh);
+    const uint64_t f = fraction(mass[0], d.p24), cut = f > 1 ? f : 1;
+    const uint32_t o = search_value(part, keep, true, cut, keep.o, top, above, parity, sh);
+    const uint64_t w = element_weight(element_exp(unordered(o), part.m, part.inv));
+    // of the elements of value o (each of weight w > 0), those before which
+    // less than the cut lies; top-k's limit already holds among them
+    const int id = search_id(part, o, (cut - above + w - 1) / w, parity, sh);
+    keep.id = o == keep.o ? min(id, keep.id) : id;
+    keep.o = o;
+  }
+  auto kept = [&](float z, int id) -> uint64_t {
+    const float e = element_exp(z, part.m, part.inv);
+    return keep.has(ordered(z), id) && e >= d.min_p ? element_weight(e) : 0;
+  };
+  // this CTA's warps take consecutive runs of windows, so that the running sum
+  // over ids is one over CTAs, warps, steps of 32 windows, lanes and elements
+  const int per = (part.hi - part.lo + kScanWarps - 1) / (kScanWarps);
+  const int wlo = min(part.lo + warp * per, part.hi), whi = min(wlo + per, part.hi);
+  auto window = [&](int i) -> uint64_t {
+    uint64_t s = 0;
+    if (i < whi) {
+      float z[E];
+      unpack<T>(load_window(part.row, i), z);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int id = i * E - part.row.mis + e;
+        if (id >= 0 && id < part.row.vocab) s += kept(z[e], id);
+      }
+    }
+    return s;
+  };
+  uint64_t mine = 0;
+  for (int i = wlo + lane; i < whi; i += 32) mine += window(i);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+  if (lane == 0) sh.weight[warp] = mine;
+  uint64_t total[1] = {lane == 0 ? mine : 0};
+  const int at = parity;
+  cluster_sum(total, parity, sh);
+  const uint64_t target = fraction(total[0], d.u24);
+  uint64_t before = 0;
+  for (int r = 0; r < rank; ++r) before += sh.slot[at][r][0];
+  for (int w = 0; w < warp; ++w) before += sh.weight[w];
+  if (target < before || target >= before + mine) return;
+  for (int i = wlo; i < whi; i += 32) {
+    const uint64_t s = window(i + lane);
+    uint64_t incl = s;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    const uint64_t step = __shfl_sync(0xFFFFFFFFu, incl, 31);
+    if (target < before + step) {
+      uint64_t b = before + incl - s;
+      if (target >= b && target < b + s) {
+        float z[E];
+        unpack<T>(load_window(part.row, i + lane), z);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int id = (i + lane) * E - part.row.mis + e;
+          const uint64_t w = id >= 0 && id < part.row.vocab ? kept(z[e], id) : 0;
+          if (target >= b && target < b + w) {
+            *token = id;
+            *logprob = logf((float)w / (float)total[0]);
+          }
+          b += w;
+        }
+      }
+      return;
+    }
+    before += step;
+  }
+}
+
+// The request decided at a row's leader from its n largest elements, sh.cand.
+// `mass`: the mass of the whole row if known exactly, else 0; rest: the sum of
+// 2^((z - ref) c) over all other elements.  m: the row's maximum.
+__device__ __forceinline__ int decide(const Draw &d, int n, float rest, float ref, float c, float m,
+                                      uint64_t mass, int32_t *token, float *logprob,
+                                      ScanShared &sh, SampleShared &sm) {
+  const int tid = threadIdx.x;
+  const uint64_t key = tid < n ? sh.cand[tid] : 0;
+  const float e = key ? element_exp(key_value(key), m, d.inv) : 0.0f;
+  uint64_t w = element_weight(e);
+  sm.weight[tid] = w;
+  __syncthreads();
+  int rank = 0;
+  uint64_t before = 0;
+  for (int i = 0; i < n; ++i)
+    if (sh.cand[i] > key) {
+      ++rank;
+      before += sm.weight[i];
+    }
+  const bool in = key && rank < d.top_k;
+  const uint64_t listed = block_reduce<kScanThreads>(in ? w : 0, sh.red64, OpAdd());
+  uint64_t cut = ~0ull;
+  if (n >= d.top_k) {
+    if (d.nucleus) cut = fraction(listed, d.p24);
+  } else {
+    // the elements that are not listed come after these; with both limits, the
+    // nucleus is one of a mass that is not known here
+    if (d.limited && d.nucleus) return kSearch;
+    const float last = -block_reduce<kScanThreads>(key ? -e : -INFINITY, sh.redf, OpMax());
+    uint64_t low = ~0ull;
+    if (d.nucleus && mass) {
+      low = cut = fraction(mass, d.p24);
+    } else if (d.nucleus) {
+      if (key) sh.by_rank[rank] = e;
+      __syncthreads();
+      const float cand = block_reduce<kScanThreads>(tid < n ? sh.by_rank[tid] : 0.0f, sh.redf, OpAdd());
+      const double about = ((double)cand + (double)rest * exp2((double)((ref - m) * c))) * kWeightOne *
+                           (double)d.p24 * (1.0 / 16777216.0);
+      low = (uint64_t)fmax(about * (1.0 - kMassError) - 2.0, 0.0);
+      cut = (uint64_t)(about * (1.0 + kMassError)) + 2;
+    }
+    if (!(last < d.min_p) && (!d.nucleus || listed < cut)) return kSearch;
+    if (__syncthreads_or(key && rank > 0 && before >= low && before < cut)) return kExactMass;
+  }
+  if (cut < 1) cut = 1;
+  if (!(in && before < cut && e >= d.min_p)) w = 0;
+  sm.weight[tid] = w;
+  const uint64_t total = block_reduce<kScanThreads>(w, sh.red64, OpAdd());
+  const uint64_t target = fraction(total, d.u24);
+  uint64_t id_before = 0;
+  for (int i = 0; i < n; ++i)  // (the key's low half is the complement of the id)
+    if ((uint32_t)sh.cand[i] > (uint32_t)key) id_before += sm.weight[i];
+  if (w && target >= id_before && target < id_before + w) {
+    *token = (int32_t)key_index(key);
+    *logprob = logf((float)w / (float)total);
+  }
+  return kDone;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kScanThreads, kSampleCtas)
+    sample_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int cap,
+                  const float *__restrict__ temperature, const int32_t *__restrict__ top_k,
+                  const float *__restrict__ top_p, const float *__restrict__ min_p,
+                  const float *__restrict__ uniform, int32_t *tokens, float *logprob) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  SampleShared &sm = *reinterpret_cast<SampleShared *>(smem);
+  ScanShared &sh = *reinterpret_cast<ScanShared *>(smem + sizeof(SampleShared));
+  const int tid = threadIdx.x;
+  Scan<T> scan(sh, cap, logits, stride, vocab, rows);
+  const int first = blockIdx.x / scan.C;
+  // the row's request; false if it is out of range
+  auto request = [&](int t, Draw &d, int &K) {
+    const float temp = temperature ? temperature[t] : 1.0f;
+    const int tk = top_k ? top_k[t] : 0;
+    const float tp = top_p ? top_p[t] : 1.0f;
+    const float mp = min_p ? min_p[t] : 0.0f;
+    const float u = uniform[t];
+    const bool good = temp >= 0.0f && temp < INFINITY && tp >= 0.0f && mp <= 1.0f && u >= 0.0f && u < 1.0f;
+    const bool greedy = !good || temp < FLT_MIN;
+    d.inv = greedy ? 1.0f : 1.0f / temp;
+    d.min_p = mp;
+    d.top_k = greedy ? 1 : (tk > 0 && tk < vocab) ? tk : vocab;
+    d.limited = d.top_k < vocab;
+    d.nucleus = tp < 1.0f;
+    d.p24 = (uint64_t)(fminf(tp, 1.0f) * 16777216.0f);
+    d.u24 = (uint64_t)(u * 16777216.0f);
+    // elements to look at: all that top-k leaves, else a guess of what a nucleus
+    // or min-p keeps; without any filter only the largest
+    K = d.top_k <= kTopKListed ? d.top_k : (d.nucleus || mp > 0.0f) ? min(kNucleus, vocab) : 1;
+    return good;
+  };
+  int turn = 0;
+  for (int t = first; t < rows; t += scan.clusters, ++turn) {
+    Draw d;
+    int K, n;
+    const bool good = request(t, d, K);
+    const float c = kLog2e * d.inv;
+    scan.scan(t, K, c);
+    if (!scan.gather(t, turn, n)) continue;
+    uint64_t best = 0;
+    for (int i = 0; i < n; ++i) best = sh.cand[i] > best ? sh.cand[i] : best;
+    const float m = n > 0 ? key_value(best) : -INFINITY;
+    const float rest = block_reduce<kScanThreads>(scan.s, sh.redf, OpAdd());
+    if (!good || !(rest < INFINITY) || !(m > -INFINITY) || !(m < INFINITY)) {
+      // NaN or +inf in the row, or nothing but -inf: no distribution
+      if (tid == 0) {
+        tokens[t] = -1;
+        logprob[t] = NAN;
+      }
+      continue;
+    }
+    int mode = decide(d, n, rest, scan.ref, c, m, 0, tokens + t, logprob + t, sh, sm);
+    if (mode == kExactMass) {
+      const Row<T> row = scan.row_of(t);
+      const Part<T> all = {row, 0, row.windows, m, d.inv};
+      uint64_t mass = 0;
+      all.each([&](float z, int) { mass += element_weight(element_exp(z, m, d.inv)); });
+      mass = block_reduce<kScanThreads>(mass, sh.red64, OpAdd());
+      mode = decide(d, n, rest, scan.ref, c, m, mass, tokens + t, logprob + t, sh, sm);
+    }
+    if (mode == kSearch && tid == 0) {
+      tokens[t] = kLeftOver;
+      logprob[t] = m;
+    }
+  }
+  scan.finish();
+  cg::this_cluster().sync();
+  int parity = 0;
+  for (int t = first; t < rows; t += scan.clusters) {
+    // (the row's own search writes these after a barrier that all CTAs reach)
+    if (__ldcg(tokens + t) != kLeftOver) continue;
+    Draw d;
+    int K;
+    request(t, d, K);
+    Part<T> part = {scan.row_of(t), 0, 0, __ldcg(logprob + t), d.inv};
+    scan.slice(part.row, part.lo, part.hi);
+    search_row(part, d, parity, tokens + t, logprob + t, sm);
+  }
+  cg::this_cluster().sync();  // no CTA ends while its sums can still be read or written
+}
+
+template <typename T>
+static cudaError_t launch(const void *logits, int rows, int vocab, int64_t stride,
+                          const float *temperature, const int32_t *top_k, const float *top_p,
+                          const float *min_p, const float *uniform, int32_t *tokens,
+                          float *logprob, cudaStream_t stream) {
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleCtas);
+  const int cap = candidate_cap(top_k ? kTopKListed : kNucleus);
+  const size_t base = sizeof(SampleShared) + sizeof(ScanShared);
+  return launch_clusters(sample_kernel<T>, g.clusters, g.C, kScanThreads,
+                         base + (g.C > 1 ? (size_t)g.C * cap * 8 : 0),
+                         base + kClusterMax * candidate_cap(kTopKListed) * 8, stream,
+                         static_cast<const T *>(logits), stride, rows, vocab, cap, temperature,
+                         top_k, top_p, min_p, uniform, tokens, logprob);
+}
+
+cudaError_t launch_sample(const void *logits, int dtype, int rows, int vocab, int64_t stride,
+                          const float *temperature, const int32_t *top_k, const float *top_p,
+                          const float *min_p, const float *uniform, int32_t *tokens,
+                          float *logprob, cudaStream_t stream) {
+  return dtype == SLIMWISE_DTYPE_BF16
+             ? launch<__nv_bfloat16>(logits, rows, vocab, stride, temperature, top_k, top_p, min_p,
+                                     uniform, tokens, logprob, stream)
+             : launch<float>(logits, rows, vocab, stride, temperature, top_k, top_p, min_p,
+                             uniform, tokens, logprob, stream);
+}
+
+}  // namespace slimwise

@@ -1,0 +1,113 @@
+// top_logits.cu -- a teacher's targets for distillation: the K largest logits
+// of each row as log-probabilities, and the log of the mass that the others
+// hold (SlimWise Sec. 3.3, Eq. 3: top-K of the teacher plus a residual bucket).
+//
+//   S    = ids of the K largest z (larger value first, then the lower id)
+//   logp = z_S / tau - log sum_i exp(z_i / tau)
+//   log_rest = log (sum_{i not in S} exp(z_i / tau)) - log sum_i exp(z_i / tau)
+//
+// The mass of the others is summed over them, not taken as 1 - the list's: a
+// teacher that is nearly sure leaves 1e-6, which the difference would not hold.
+// Bound by the one read of the logits (vocab.cuh has the scan).
+#include "vocab.cuh"
+
+namespace slimwise {
+
+constexpr int kTopCtas = 3;  // CTAs of an SM
+
+template <typename T>
+__global__ void __launch_bounds__(kScanThreads, kTopCtas)
+    top_logits_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int K,
+                      float c, int32_t *__restrict__ ids, float *__restrict__ logp,
+                      float *__restrict__ log_rest) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  ScanShared &sh = *reinterpret_cast<ScanShared *>(smem);
+  const int tid = threadIdx.x;
+  Scan<T> scan(sh, candidate_cap(K), logits, stride, vocab, rows);
+  int turn = 0;
+  for (int t = blockIdx.x / scan.C; t < rows; t += scan.clusters, ++turn) {
+    scan.scan(t, K, c);
+    int n;
+    if (!scan.gather(t, turn, n)) continue;
+    // one candidate a thread: its place in the order
+    const uint64_t key = tid < n ? sh.cand[tid] : 0;
+    int rank = 0;
+    uint64_t best = 0;
+    for (int i = 0; i < n; ++i) {
+      const uint64_t o = sh.cand[i];
+      rank += o > key;
+      best = o > best ? o : best;
+    }
+    const float m = fmaxf(n > 0 ? key_value(best) : -INFINITY, kFloorRef);
+    const float x = (key_value(key) - m) * c;
+    // sums in the order of the ranks
+    if (key) sh.by_rank[rank] = key_value(key);
+    __syncthreads();
+    // the rest relative to the last of the list, which it does not exceed
+    const float last = n >= K ? fmaxf(sh.by_rank[K - 1], kFloorRef) : scan.ref;
+    float rest = scan.s * exp_from(scan.ref, last, c), e = 0.0f;
+    if (tid < n) {
+      if (tid < K) e = exp_from(sh.by_rank[tid], m, c);
+      else rest += exp_from(sh.by_rank[tid], last, c);
+    }
+    const float from_ref = (last - m) * c;  // log2 of the rest's scale
+    rest = block_reduce<kScanThreads>(rest, sh.redf, OpAdd());
+    const float top = block_reduce<kScanThreads>(e, sh.redf, OpAdd());
+    const float log_total = log2f(fmaf(rest, ex2(from_ref), top));
+    const int64_t at = (int64_t)t * K;
+    if (key && rank < K) {
+      ids[at + rank] = (int32_t)key_index(key);
+      logp[at + rank] = (x - log_total) * kLn2;
+    }
+    // a row with NaN can have fewer candidates than K
+    if (tid >= n && tid < K) {
+      ids[at + tid] = -1;
+      logp[at + tid] = NAN;
+    }
+    if (tid == 0) log_rest[t] = ((log2f(rest) + from_ref) - log_total) * kLn2;
+  }
+  scan.finish();
+}
+
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int ctas_per_sm) {
+  const int windows = (int)(((int64_t)vocab * element_bytes + 15) / 16) + 1;
+  const int slots = 152 * ctas_per_sm;
+  ScanGrid best = {1, 1};
+  double best_use = 0.0;
+  for (int C = 1; C <= kClusterMax; C *= 2) {
+    if (C > 1 && windows < C * kScanStep / 2) break;
+    const int at_once = slots / C, clusters = rows < at_once ? rows : at_once;
+    const int rounds = (rows + clusters - 1) / clusters;
+    // share of the CTAs' time that has work: the larger cluster has to be worth it
+    const double use = (double)rows * C / ((double)rounds * slots);
+    if (use > 1.05 * best_use) {
+      best = {C, clusters};
+      best_use = use;
+    }
+  }
+  return best;
+}
+
+template <typename T>
+static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t stride, int k,
+                              float temperature, int32_t *ids, float *logp, float *log_rest,
+                              cudaStream_t stream) {
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kTopCtas);
+  const size_t smem = sizeof(ScanShared) + (g.C > 1 ? (size_t)g.C * candidate_cap(k) * 8 : 0);
+  return launch_clusters(top_logits_kernel<T>, g.clusters, g.C, kScanThreads, smem,
+                         sizeof(ScanShared) + kClusterMax * kTopMax * 8, stream,
+                         static_cast<const T *>(logits), stride, rows, vocab, k,
+                         kLog2e / temperature, ids, logp, log_rest);
+}
+
+cudaError_t launch_top_logits(const void *logits, int dtype, int rows, int vocab, int64_t stride,
+                              int k, float temperature, int32_t *ids, float *logp, float *log_rest,
+                              cudaStream_t stream) {
+  return dtype == SLIMWISE_DTYPE_BF16
+             ? launch_top<__nv_bfloat16>(logits, rows, vocab, stride, k, temperature, ids, logp,
+                                         log_rest, stream)
+             : launch_top<float>(logits, rows, vocab, stride, k, temperature, ids, logp, log_rest,
+                                 stream);
+}
+
+}  // namespace slimwise
