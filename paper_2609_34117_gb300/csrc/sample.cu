@@ -26,7 +26,7 @@ namespace slimwise {
 
 constexpr int kSampleCtas = 3;    // CTAs of an SM
 constexpr int kNucleus = 64;      // elements looked at for a nucleus or min-p without top-k
-constexpr int kTopKListed = kTopMax;  // largest top-k that is decided from the list
+constexpr int kTopKListed = 128;  // largest top-k that is decided from the list
 constexpr int32_t kLeftOver = -2; // a token that is still to be searched (its logprob: the maximum)
 constexpr float kWeightOne = 1099511627776.0f;  // 2^40, the largest element's weight
 // Bound of the relative difference between the scan's float mass and the sum of
@@ -292,11 +292,12 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
   __syncthreads();
   int rank = 0;
   uint64_t before = 0;
-  for (int i = 0; i < n; ++i)
-    if (sh.cand[i] > key) {
-      ++rank;
-      before += sm.weight[i];
-    }
+  if (key)
+    for (int i = 0; i < n; ++i)
+      if (sh.cand[i] > key) {
+        ++rank;
+        before += sm.weight[i];
+      }
   const bool in = key && rank < d.top_k;
   const uint64_t listed = block_reduce<kScanThreads>(in ? w : 0, sh.red64, OpAdd());
   uint64_t cut = ~0ull;
@@ -328,7 +329,7 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
   const uint64_t total = block_reduce<kScanThreads>(w, sh.red64, OpAdd());
   const uint64_t target = fraction(total, d.u24);
   uint64_t id_before = 0;
-  for (int i = 0; i < n; ++i)  // (the key's low half is the complement of the id)
+  for (int i = 0; w && i < n; ++i)  // (the key's low half is the complement of the id)
     if ((uint32_t)sh.cand[i] > (uint32_t)key) id_before += sm.weight[i];
   if (w && target >= id_before && target < id_before + w) {
     *token = (int32_t)key_index(key);
@@ -339,7 +340,7 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
 
 template <typename T>
 __global__ void __launch_bounds__(kScanThreads, kSampleCtas)
-    sample_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int cap,
+    sample_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int K_most,
                   const float *__restrict__ temperature, const int32_t *__restrict__ top_k,
                   const float *__restrict__ top_p, const float *__restrict__ min_p,
                   const float *__restrict__ uniform, int32_t *tokens, float *logprob) {
@@ -347,10 +348,9 @@ __global__ void __launch_bounds__(kScanThreads, kSampleCtas)
   SampleShared &sm = *reinterpret_cast<SampleShared *>(smem);
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem + sizeof(SampleShared));
   const int tid = threadIdx.x;
-  Scan<T> scan(sh, cap, logits, stride, vocab, rows);
-  const int first = blockIdx.x / scan.C;
+  Scan<T> scan(sh, K_most, logits, stride, vocab, rows);
   // the row's request; false if it is out of range
-  auto request = [&](int t, Draw &d, int &K) {
+  auto request_of = [&](int t, Draw &d, int &K) {
     const float temp = temperature ? temperature[t] : 1.0f;
     const int tk = top_k ? top_k[t] : 0;
     const float tp = top_p ? top_p[t] : 1.0f;
@@ -370,17 +370,17 @@ __global__ void __launch_bounds__(kScanThreads, kSampleCtas)
     K = d.top_k <= kTopKListed ? d.top_k : (d.nucleus || mp > 0.0f) ? min(kNucleus, vocab) : 1;
     return good;
   };
-  int turn = 0;
-  for (int t = first; t < rows; t += scan.clusters, ++turn) {
+  auto request = [&](int t, int &K, float &c) {
     Draw d;
-    int K, n;
-    const bool good = request(t, d, K);
-    const float c = kLog2e * d.inv;
-    scan.scan(t, K, c);
-    if (!scan.gather(t, turn, n)) continue;
-    uint64_t best = 0;
-    for (int i = 0; i < n; ++i) best = sh.cand[i] > best ? sh.cand[i] : best;
-    const float m = n > 0 ? key_value(best) : -INFINITY;
+    request_of(t, d, K);
+    c = kLog2e * d.inv;
+  };
+  scan.rows_of_cluster(request, [&](int t, int n) {
+    Draw d;
+    int K;
+    const bool good = request_of(t, d, K);
+    const float c = scan.c;
+    const float m = block_reduce<kScanThreads>(tid < n ? key_value(sh.cand[tid]) : -INFINITY, sh.redf, OpMax());
     const float rest = block_reduce<kScanThreads>(scan.s, sh.redf, OpAdd());
     if (!good || !(rest < INFINITY) || !(m > -INFINITY) || !(m < INFINITY)) {
       // NaN or +inf in the row, or nothing but -inf: no distribution
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(kScanThreads, kSampleCtas)
         tokens[t] = -1;
         logprob[t] = NAN;
       }
-      continue;
+      return;
     }
     int mode = decide(d, n, rest, scan.ref, c, m, 0, tokens + t, logprob + t, sh, sm);
     if (mode == kExactMass) {
@@ -403,16 +403,15 @@ __global__ void __launch_bounds__(kScanThreads, kSampleCtas)
       tokens[t] = kLeftOver;
       logprob[t] = m;
     }
-  }
-  scan.finish();
+  });
   cg::this_cluster().sync();
   int parity = 0;
-  for (int t = first; t < rows; t += scan.clusters) {
+  for (int t = blockIdx.x / scan.C; t < rows; t += scan.clusters) {
     // (the row's own search writes these after a barrier that all CTAs reach)
     if (__ldcg(tokens + t) != kLeftOver) continue;
     Draw d;
     int K;
-    request(t, d, K);
+    request_of(t, d, K);
     Part<T> part = {scan.row_of(t), 0, 0, __ldcg(logprob + t), d.inv};
     scan.slice(part.row, part.lo, part.hi);
     search_row(part, d, parity, tokens + t, logprob + t, sm);
@@ -426,12 +425,11 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
                           const float *min_p, const float *uniform, int32_t *tokens,
                           float *logprob, cudaStream_t stream) {
   const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleCtas);
-  const int cap = candidate_cap(top_k ? kTopKListed : kNucleus);
-  const size_t base = sizeof(SampleShared) + sizeof(ScanShared);
+  const int K_most = top_k ? kTopKListed : kNucleus;
   return launch_clusters(sample_kernel<T>, g.clusters, g.C, kScanThreads,
-                         base + (g.C > 1 ? (size_t)g.C * cap * 8 : 0),
-                         base + kClusterMax * candidate_cap(kTopKListed) * 8, stream,
-                         static_cast<const T *>(logits), stride, rows, vocab, cap, temperature,
+                         sizeof(SampleShared) + scan_smem(K_most, g.C),
+                         sizeof(SampleShared) + scan_smem(kTopKListed, kClusterMax), stream,
+                         static_cast<const T *>(logits), stride, rows, vocab, K_most, temperature,
                          top_k, top_p, min_p, uniform, tokens, logprob);
 }
 

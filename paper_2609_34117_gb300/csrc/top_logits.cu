@@ -23,26 +23,23 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   extern __shared__ __align__(128) unsigned char smem[];
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem);
   const int tid = threadIdx.x;
-  Scan<T> scan(sh, candidate_cap(K), logits, stride, vocab, rows);
-  int turn = 0;
-  for (int t = blockIdx.x / scan.C; t < rows; t += scan.clusters, ++turn) {
-    scan.scan(t, K, c);
-    int n;
-    if (!scan.gather(t, turn, n)) continue;
+  Scan<T> scan(sh, K, logits, stride, vocab, rows);
+  auto request = [&](int, int &k, float &cc) {
+    k = K;
+    cc = c;
+  };
+  scan.rows_of_cluster(request, [&](int t, int n) {
     // one candidate a thread: its place in the order
     const uint64_t key = tid < n ? sh.cand[tid] : 0;
     int rank = 0;
-    uint64_t best = 0;
-    for (int i = 0; i < n; ++i) {
-      const uint64_t o = sh.cand[i];
-      rank += o > key;
-      best = o > best ? o : best;
+    if (key) {
+      for (int i = 0; i < n; ++i) rank += sh.cand[i] > key;
+      sh.by_rank[rank] = key_value(key);
     }
-    const float m = fmaxf(n > 0 ? key_value(best) : -INFINITY, kFloorRef);
-    const float x = (key_value(key) - m) * c;
-    // sums in the order of the ranks
-    if (key) sh.by_rank[rank] = key_value(key);
     __syncthreads();
+    // sums in the order of the ranks
+    const float m = fmaxf(n > 0 ? sh.by_rank[0] : -INFINITY, kFloorRef);
+    const float x = (key_value(key) - m) * c;
     // the rest relative to the last of the list, which it does not exceed
     const float last = n >= K ? fmaxf(sh.by_rank[K - 1], kFloorRef) : scan.ref;
     float rest = scan.s * exp_from(scan.ref, last, c), e = 0.0f;
@@ -65,8 +62,7 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
       logp[at + tid] = NAN;
     }
     if (tid == 0) log_rest[t] = ((log2f(rest) + from_ref) - log_total) * kLn2;
-  }
-  scan.finish();
+  });
 }
 
 ScanGrid scan_grid(int rows, int vocab, int element_bytes, int ctas_per_sm) {
@@ -75,7 +71,7 @@ ScanGrid scan_grid(int rows, int vocab, int element_bytes, int ctas_per_sm) {
   ScanGrid best = {1, 1};
   double best_use = 0.0;
   for (int C = 1; C <= kClusterMax; C *= 2) {
-    if (C > 1 && windows < C * kScanStep / 2) break;
+    if (C > 1 && windows < C * kScanWarps * kWarpStep / 2) break;
     const int at_once = slots / C, clusters = rows < at_once ? rows : at_once;
     const int rounds = (rows + clusters - 1) / clusters;
     // share of the CTAs' time that has work: the larger cluster has to be worth it
@@ -93,9 +89,8 @@ static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t s
                               float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
   const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kTopCtas);
-  const size_t smem = sizeof(ScanShared) + (g.C > 1 ? (size_t)g.C * candidate_cap(k) * 8 : 0);
-  return launch_clusters(top_logits_kernel<T>, g.clusters, g.C, kScanThreads, smem,
-                         sizeof(ScanShared) + kClusterMax * kTopMax * 8, stream,
+  return launch_clusters(top_logits_kernel<T>, g.clusters, g.C, kScanThreads, scan_smem(k, g.C),
+                         scan_smem(kTopMax, kClusterMax), stream,
                          static_cast<const T *>(logits), stride, rows, vocab, k,
                          kLog2e / temperature, ids, logp, log_rest);
 }

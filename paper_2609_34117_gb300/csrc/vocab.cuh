@@ -105,15 +105,16 @@ struct Row {
   const T *p;      // first element
   const uint4 *w;  // window 0 (the 16-byte boundary at or before p)
   int vocab, mis, windows;
+  int whole_lo, whole_n;  // the windows that lie in the row: from, number
   __device__ __forceinline__ Row(const T *row, int V) : p(row), vocab(V) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(row);
     mis = (int)((a & 15) / sizeof(T));
     w = reinterpret_cast<const uint4 *>(a & ~(uintptr_t)15);
     windows = (mis + V + E - 1) / E;
+    whole_lo = mis > 0;
+    whole_n = max((mis + V) / E - whole_lo, 0);
   }
-  __device__ __forceinline__ bool whole(int i) const {
-    return i * E >= mis && (i + 1) * E <= mis + vocab;
-  }
+  __device__ __forceinline__ bool whole(int i) const { return (unsigned)(i - whole_lo) < (unsigned)whole_n; }
 };
 
 __device__ __forceinline__ uint32_t neg_inf_bits(const __nv_bfloat16 *) { return 0xFF80FF80u; }
@@ -148,6 +149,9 @@ __device__ __forceinline__ uint4 load_window(const Row<T> &r, int i) {
   return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+
 template <typename T>
 __device__ __forceinline__ void unpack(const uint4 &v, float (&f)[16 / sizeof(T)]) {
   const uint32_t u[4] = {v.x, v.y, v.z, v.w};
@@ -174,6 +178,21 @@ __device__ __forceinline__ float window_max(const uint4 &v) {
     asm("max.bf16x2 %0, %1, %2;" : "=r"(n) : "r"(v.z), "r"(v.w));
     asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(n));
     return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  }
+}
+
+// Of two windows.
+template <typename T>
+__device__ __forceinline__ float window_max(const uint4 &v, const uint4 &w) {
+  if constexpr (sizeof(T) == 4) {
+    return fmaxf(window_max<T>(v), window_max<T>(w));
+  } else {
+    uint4 m;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(m.x) : "r"(v.x), "r"(w.x));
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(m.y) : "r"(v.y), "r"(w.y));
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(m.z) : "r"(v.z), "r"(w.z));
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(m.w) : "r"(v.w), "r"(w.w));
+    return window_max<T>(m);
   }
 }
 
@@ -236,22 +255,36 @@ __device__ __forceinline__ void unpack_pairs(const uint4 &v, uint64_t (&p)[8 / s
   }
 }
 
-// Sum over the window of 2^((z - ref) c).
+// Sum over N windows of 2^((z - ref) c).
+template <typename T, int N>
+__device__ __forceinline__ float windows_sum(const uint4 (&v)[N], float c, float ref) {
+  constexpr int P = 8 / (int)sizeof(T);
+  const uint64_t mr = pair(-ref, -ref), cc = pair(c, c);
+  uint64_t sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint64_t p[P];
+    unpack_pairs<T>(v[i], p);
+#pragma unroll
+    for (int q = 0; q < P; ++q) p[q] = exp2_pair(p[q], mr, cc);
+#pragma unroll
+    for (int d = 1; d < P; d *= 2)
+#pragma unroll
+      for (int q = 0; q < P; q += 2 * d) p[q] = add2(p[q], p[q + d]);
+    sum[i] = p[0];
+  }
+#pragma unroll
+  for (int d = 1; d < N; d *= 2)
+#pragma unroll
+    for (int i = 0; i + d < N; i += 2 * d) sum[i] = add2(sum[i], sum[i + d]);
+  float a, b;
+  split(sum[0], a, b);
+  return a + b;
+}
 template <typename T>
 __device__ __forceinline__ float window_sum(const uint4 &v, float c, float ref) {
-  constexpr int P = 8 / (int)sizeof(T);
-  uint64_t p[P];
-  unpack_pairs<T>(v, p);
-  const uint64_t mr = pair(-ref, -ref), cc = pair(c, c);
-#pragma unroll
-  for (int q = 0; q < P; ++q) p[q] = exp2_pair(p[q], mr, cc);
-#pragma unroll
-  for (int d = 1; d < P; d *= 2)
-#pragma unroll
-    for (int q = 0; q < P; q += 2 * d) p[q] = add2(p[q], p[q + d]);
-  float a, b;
-  split(p[0], a, b);
-  return a + b;
+  const uint4 one[1] = {v};
+  return windows_sum<T, 1>(one, c, ref);
 }
 
 // Block reductions over NT threads; every thread gets the result.  `buf` has
@@ -281,51 +314,45 @@ struct OpMax {
 // threshold under which fewer than K of the row's elements cannot lie, and (b)
 // the sum of the exponentials of all others.
 //
-// The threshold: each thread keeps the largest element of two groups of
-// windows.  If K groups reach a value, K elements do, so the K-th largest group
-// maximum bounds the K-th largest element from below, and with many more groups
-// than K it is near it, however long the row: of 512 groups, about
-// -512 ln(1 - K / 512) elements lie above it (68 for K = 64).  It is found by
-// bisection with block-wide counts, after the 1st, 2nd, 4th, ... step, so that
-// each doubling of what was read lists that many windows again and no more.  A
-// window whose maximum reaches the threshold is listed with its sum; any other
+// The row is cut into one run for each warp of the cluster, and a run into units
+// of four windows (64 bytes), one a lane in each step.  Each thread keeps the
+// largest element of two groups of its windows.  If m = K / 8 groups of each
+// warp of a CTA reach a value, K elements do, so the least over the warps of
+// each one's m-th largest group bounds the K-th largest element from below.
+// With many more groups than K it is near it, however long the row: about 100
+// elements lie above it for K = 64.  It costs a warp a bisection with ballots
+// and the CTA one barrier, after the 1st, 4th, 16th, ... step and the last.  A
+// unit whose maximum reaches the threshold is listed with its sum; any other
 // only adds its sum to the thread's.
 //
-// The K largest elements of a row lie in the K windows of largest maximum (ties:
+// The K largest elements of a run lie in its K units of largest maximum (ties:
 // lower index), since each of those holds an element that goes before every
-// element of the others.  So a list that fills (many equal values, or rows in
-// rising order) is cut to its K best windows by a radix selection, and nothing
-// that matters is lost.
+// element of the others.  So a warp whose list fills (many equal values, or rows
+// in rising order) cuts it to its K best units, and nothing that matters is lost.
 //
 // Sums are relative to the threshold, not to the maximum: what lies below the
 // list keeps its precision however far the list rises above it.  Which thread
 // adds what never depends on timing, so that results are the same on every run.
 //
-// Each warp streams its windows through a ring of its own with bulk copies; a
-// stage is copied again as soon as its windows are in registers, and the copies
-// of the next row are under way while a row is finished.
+// Each warp streams its run through a ring of its own with bulk copies; a stage
+// is copied again as soon as its windows are in registers, and the copies of the
+// next row are under way while a row is finished.
 constexpr int kScanThreads = 256;
 constexpr int kScanWarps = kScanThreads / 32;
-constexpr int kScanUnroll = 4;                          // windows of a lane in a step
-constexpr int kWarpStep = 32 * kScanUnroll;             // windows of a warp in a step
-constexpr int kScanStep = kScanThreads * kScanUnroll;   // windows of a CTA in a step
+constexpr int kUnit = 4;                      // windows of a unit
+constexpr int kWarpStep = 32 * kUnit;         // windows of a warp in a step
 constexpr int kScanStages = 2;
-constexpr int kListWarp = 192;                          // listed windows of a warp
-constexpr int kListSlots = kScanWarps * kListWarp / kScanThreads;  // of a thread
 constexpr int kClusterMax = 8;
-static_assert(kTopMax <= kScanThreads, "a thread for each kept window and candidate");
-static_assert(kTopMax / kScanWarps + kWarpStep <= kListWarp, "room for a step after a cut");
+static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
 
 // Candidates that a CTA passes on: the K best and others, if there are no more
-// than this (else the K best alone).
-__host__ __device__ inline int candidate_cap(int K) {
-  return K >= 128 ? kTopMax : K <= 32 ? 64 : 2 * K;
-}
+// than this (else the K best alone).  A power of two.
+__host__ __device__ inline int candidate_cap(int K) { return K <= 32 ? 64 : K <= 64 ? 128 : kTopMax; }
+// Units that a warp's list has room for: K (64 at least) and two steps'.
+__host__ __device__ inline int list_room(int K) { return (K <= 64 ? 64 : (K + 31) / 32 * 32) + 64; }
 
 struct ScanShared {
   uint4 ring[kScanWarps][kScanStages][kWarpStep];
-  uint64_t key[kScanWarps][kListWarp];
-  float sum[kScanWarps][kListWarp];  // of 2^((z - the window's maximum) c)
   uint64_t cand[kTopMax];
   uint64_t bar[kScanWarps][kScanStages];
   uint64_t red64[kScanWarps];
@@ -333,13 +360,22 @@ struct ScanShared {
   float by_rank[kTopMax];
   float redf[kScanWarps];
   uint32_t redu[2][kScanWarps];
+  float reach[2][kScanWarps], known[2][kScanWarps];  // by refresh, in turn
+  int part[2][kScanWarps];
   int count[kScanWarps];
   int sel_digit, sel_above, sel_bin;
-  int late;                                  // a wait for a copy gave up
-  float part_sum[kClusterMax], part_thr[kClusterMax];  // at a row's leader: each CTA's
-  int part_exact[kClusterMax];
-  // then, in clusters: uint64_t [cluster][cap], each CTA's candidates at a row's leader
+  int late;                                          // a wait for a copy gave up
+  float part_sum[2][kClusterMax], part_thr[2][kClusterMax];  // at a row's leader: each CTA's
+  int part_exact[2][kClusterMax];
+  // then  uint64_t [warps][room]   listed units' keys (maximum, index of the first window)
+  //       float [warps][room]      and their sums of 2^((z - maximum) c)
+  //       uint64_t [cluster][cap]  in clusters, at a row's leader: each CTA's
+  //                                candidates (in clusters of two, two of these)
 };
+inline size_t scan_smem(int K, int C) {
+  return sizeof(ScanShared) + (size_t)kScanWarps * list_room(K) * 12 +
+         (C > 1 ? (size_t)(C > 4 ? C : 4) * candidate_cap(K) * 8 : 0);
+}
 
 // The bits of v from bit `from` (up to 64) up.
 __device__ __forceinline__ uint64_t high_bits(uint64_t v, int from) {
@@ -445,39 +481,84 @@ __device__ __forceinline__ int block_prefix(int v, int &total, ScanShared &sh) {
   return before + incl - v;
 }
 
+// A value that at least m of the warp's 2 x 32 values a, b reach, and few more;
+// -inf if fewer than m are above -inf.  `low`: a value that is known to be
+// reached by as many, or -inf.  Bisection over the order of the values' bits,
+// which masked logits of the type's lowest value do not stretch as they would
+// the range of the values, down to steps of `grain` bits.
+__device__ __forceinline__ float warp_reach(float a, float b, int m, float low, uint32_t grain) {
+  const uint32_t all = 0xFFFFFFFFu;
+  const uint32_t oa = ordered(a), ob = ordered(b), none = ordered(-INFINITY);
+  auto count = [&](uint32_t x) { return __popc(__ballot_sync(all, oa >= x)) + __popc(__ballot_sync(all, ob >= x)); };
+  uint32_t lo, hi = __reduce_max_sync(all, max(oa, ob));
+  if (low > -INFINITY) {
+    lo = ordered(low);
+  } else {
+    lo = __reduce_min_sync(all, min(oa > none ? oa : all, ob > none ? ob : all));
+    if (lo == all) return -INFINITY;
+  }
+  if (count(lo) < m) return low;
+  while (hi > lo + grain) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    const int n = count(mid);
+    if (n >= m) {
+      lo = mid;
+      if (n <= m + m / 4) break;
+    } else {
+      hi = mid;
+    }
+  }
+  return unordered(lo);
+}
+
 template <typename T>
 struct Scan {
   static constexpr int E = Row<T>::E;
+  static constexpr uint32_t kGrain = sizeof(T) == 2 ? 0xFFFFu : 0x1FFFu;  // a bf16's step; 2^-10 of an fp32
   ScanShared &sh;
-  uint64_t *recv;  // behind sh
-  int recv_cap;    // candidates of a CTA that recv has room for
+  uint64_t *list_key;  // this warp's
+  float *list_sum;
+  uint64_t *recv;
+  int room, recv_cap;  // of a warp's list; of a CTA's part of recv
   const T *logits;
   int64_t stride;
   int vocab, rows;
+  int log_parts;                // warps of a cluster
   int C, rank, clusters;        // CTAs of a cluster, this CTA's place, clusters of the grid
   int lane, warp;
-  // the copies under way: step next_k of row next_t
-  int next_t, next_k;
+  // the copies under way: step next_k of row next_t, whose run is at next_src
+  // with windows [next_a, next_b) to copy
+  int next_t, next_k, next_steps, next_a, next_b;
+  const uint4 *next_src;
   uint32_t issued, used;        // stages copied, and read
   // the row at hand
-  int lo, hi, K;
+  int K;
   float c, thr;                 // scale of the exponents (log2 e / temperature); threshold
-  float list_thr;               // maximum at which a window is listed: thr, or just above it
+  float list_thr;               // maximum at which a window is listed: thr, or more
   float ref, s, lost;           // s, with its low part: sum of 2^((z - ref) c) of what is not listed
-  bool exact;                   // the K best alone are known to be complete
-  bool dead;                    // a copy did not arrive: this warp waits for none any more
   float top0, top1;             // maxima of this thread's groups
   int listed;                   // windows in this warp's list
+  int turn;                     // of reach and known
+  bool exact;                   // the K best alone are known to be complete
+  bool dead;                    // a copy did not arrive: this warp waits for none any more
 
-  __device__ __forceinline__ Scan(ScanShared &shared, int cap, const T *z, int64_t st, int V, int n)
-      : sh(shared), recv(reinterpret_cast<uint64_t *>(&shared + 1)), recv_cap(cap), logits(z),
-        stride(st), vocab(V), rows(n), dead(false) {
+  // K_most: the largest K of all rows
+  __device__ __forceinline__ Scan(ScanShared &shared, int K_most, const T *z, int64_t st, int V, int n)
+      : sh(shared), logits(z), stride(st), vocab(V), rows(n), dead(false) {
     cg::cluster_group cluster = cg::this_cluster();
     C = (int)cluster.num_blocks();
     rank = (int)cluster.block_rank();
     clusters = (int)gridDim.x / C;
+    log_parts = 31 - __clz(C * kScanWarps);
     lane = threadIdx.x & 31;
     warp = threadIdx.x >> 5;
+    room = list_room(K_most);
+    recv_cap = candidate_cap(K_most);
+    uint64_t *const keys = reinterpret_cast<uint64_t *>(&sh + 1);
+    float *const sums = reinterpret_cast<float *>(keys + kScanWarps * room);
+    list_key = keys + warp * room;
+    list_sum = sums + warp * room;
+    recv = reinterpret_cast<uint64_t *>(sums + kScanWarps * room);
     if (threadIdx.x == 0) {
       for (int w = 0; w < kScanWarps; ++w)
         for (int i = 0; i < kScanStages; ++i) mbar_init(smem_u32(&sh.bar[w][i]), 1);
@@ -485,45 +566,66 @@ struct Scan {
       sh.late = 0;
     }
     __syncthreads();
-    next_t = (int)(blockIdx.x / C);
-    next_k = 0;
     issued = used = 0;
+    turn = 0;
+    next_t = (int)(blockIdx.x / C);
+    next_row();
     for (int i = 0; i < kScanStages; ++i) issue();
     if (C > 1) cluster_arrive();  // every CTA runs before another writes to its shared memory
-    waited = C == 1;
   }
   __device__ __forceinline__ Row<T> row_of(int t) const {
     return Row<T>(logits + (int64_t)t * stride, vocab);
   }
-  __device__ __forceinline__ void slice(const Row<T> &row, int &a, int &b) const {
-    const int per = (row.windows + C - 1) / C;
-    a = min(rank * per, row.windows);
-    b = min(a + per, row.windows);
+  // Windows of a run: whole units.
+  __device__ __forceinline__ int run_windows(const Row<T> &row) const {
+    return (((row.windows + (1 << log_parts) - 1) >> log_parts) + kUnit - 1) & ~(kUnit - 1);
+  }
+  // Run of this warp: its first window, their number (returns), and the steps
+  // that every warp of the cluster takes.
+  __device__ __forceinline__ int run(const Row<T> &row, int &first, int &steps) const {
+    const int per = run_windows(row);
+    steps = (per + kWarpStep - 1) / kWarpStep;
+    first = min((rank * kScanWarps + warp) * per, row.windows);
+    return min(per, row.windows - first);
+  }
+  // This CTA's windows.
+  __device__ __forceinline__ void slice(const Row<T> &row, int &lo, int &hi) const {
+    const int per = run_windows(row);
+    lo = min(rank * kScanWarps * per, row.windows);
+    hi = min(lo + kScanWarps * per, row.windows);
+  }
+  // [a, b): the windows of the run that lie whole in the row.
+  __device__ __forceinline__ void whole_part(const Row<T> &row, int first, int n, int &a, int &b) const {
+    a = max(row.whole_lo - first, 0);
+    b = min(row.whole_lo + row.whole_n - first, n);
   }
 
-  // Starts the copy of this warp's windows of the next step; the row's partial
-  // windows at its ends are left out.
+  __device__ __forceinline__ void next_row() {
+    next_k = 0;
+    if (next_t >= rows) return;
+    const Row<T> row = row_of(next_t);
+    int first;
+    const int n = run(row, first, next_steps);
+    whole_part(row, first, n, next_a, next_b);
+    next_src = row.w + first;
+  }
+  // Starts the copy of this warp's windows of the next step.
   __device__ __forceinline__ void issue() {
     if (next_t >= rows || dead) return;
-    const Row<T> row = row_of(next_t);
-    int a, b;
-    slice(row, a, b);
     const int stage = (int)(issued % kScanStages);
-    const int i0 = a + next_k * kScanStep + warp * kWarpStep;
-    int first = i0, end = min(i0 + kWarpStep, b);
-    if (first == 0 && !row.whole(0)) ++first;
-    if (end == row.windows && end > first && !row.whole(end - 1)) --end;
+    const int at = next_k * kWarpStep;
+    const int from = max(at, next_a), to = min(at + kWarpStep, next_b);
     const uint32_t bar = smem_u32(&sh.bar[warp][stage]);
     __syncwarp();
     if (elect_one()) {
-      const uint32_t bytes = end > first ? (uint32_t)(end - first) * 16 : 0;
+      const uint32_t bytes = to > from ? (uint32_t)(to - from) * 16 : 0;
       mbar_arrive_expect_tx(bar, bytes);
-      if (bytes) bulk_load(smem_u32(&sh.ring[warp][stage][first - i0]), row.w + first, bytes, bar);
+      if (bytes) bulk_load(smem_u32(&sh.ring[warp][stage][from - at]), next_src + from, bytes, bar);
     }
     ++issued;
-    if (a + (++next_k) * kScanStep >= b) {
-      next_k = 0;
+    if (++next_k >= next_steps) {
       next_t += clusters;
+      next_row();
     }
   }
   // Waits for the oldest copy; a wait that gives up marks the CTA's results.
@@ -541,70 +643,55 @@ struct Scan {
     return stage;
   }
 
-  __device__ __forceinline__ int groups_at(float x) const {
-    return __syncthreads_count(top0 >= x) + __syncthreads_count(top1 >= x);
-  }
-  // Raises the threshold to what the groups show, and drops the listed windows
-  // below it.
+  // Raises the threshold to what the groups of all warps show, and drops the
+  // listed windows below it.
   __device__ __forceinline__ void refresh() {
-    // bounds to search between: the groups' largest, and the threshold at hand
-    // or (the first time) the groups' least
-    const float least = fminf(top0 > -INFINITY ? top0 : INFINITY, top1 > -INFINITY ? top1 : INFINITY);
-    const uint32_t h = __reduce_max_sync(0xFFFFFFFFu, ordered(fmaxf(top0, top1)));
-    const uint32_t l = __reduce_min_sync(0xFFFFFFFFu, ordered(least));
+    const float reach = warp_reach(top0, top1, (K + kScanWarps - 1) / kScanWarps, thr, kGrain);
+    turn ^= 1;
     if (lane == 0) {
-      sh.redu[0][warp] = h;
-      sh.redu[1][warp] = l;
+      sh.reach[turn][warp] = reach;
+      sh.known[turn][warp] = thr;
+      sh.part[turn][warp] = exact;
     }
     __syncthreads();
-    uint32_t high = 0, low = 0xFFFFFFFFu;
+    float low = INFINITY, known = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kScanWarps; ++w) {
-      high = max(high, sh.redu[0][w]);
-      low = min(low, sh.redu[1][w]);
+      low = fminf(low, sh.reach[turn][w]);
+      known = fmaxf(known, sh.known[turn][w]);
+      exact |= sh.part[turn][w] != 0;
     }
-    bool known = true;  // K groups reach `low`
-    if (thr > -INFINITY) low = ordered(thr);
-    else known = low <= high && groups_at(unordered(low)) >= K;
-    if (known) {
-      while (high - low > 1) {
-        const uint32_t mid = low + (high - low) / 2;
-        const int n = groups_at(unordered(mid));
-        if (n >= K) {
-          low = mid;
-          if (n <= K + K / 8) break;
-        } else {
-          high = mid;
-        }
-      }
-      if (unordered(low) > thr) {
-        raise(unordered(low));
-        list_thr = thr;
-      }
+    low = fmaxf(low, known);
+    if (low > thr) {
+      raise(low);
+      list_thr = fmaxf(list_thr, thr);
     }
-    __syncthreads();
     int out = 0;
     for (int base = 0; base < listed; base += 32) {
       const int i = base + lane;
       uint64_t k = 0;
       float ws = 0.0f;
       if (i < listed) {
-        k = sh.key[warp][i];
-        ws = sh.sum[warp][i];
+        k = list_key[i];
+        ws = list_sum[i];
       }
-      const bool keep = k && key_value(k) >= thr;
-      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, keep);
-      if (keep) {
-        const int at = out + __popc(mask & ((1u << lane) - 1u));
-        sh.key[warp][at] = k;
-        sh.sum[warp][at] = ws;
-      } else if (k) {
-        drop(k, ws);
-      }
-      out += __popc(mask);
-      __syncwarp();
+      out = keep(k, ws, k && key_value(k) >= thr, out);
     }
     listed = out;
+  }
+  // Moves the entries (a lane each) that are kept to place `out` and on, in
+  // order, and drops the others; returns the next place.
+  __device__ __forceinline__ int keep(uint64_t k, float ws, bool yes, int out) {
+    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+    if (yes) {
+      const int at = out + __popc(mask & ((1u << lane) - 1u));
+      list_key[at] = k;
+      list_sum[at] = ws;
+    } else if (k) {
+      drop(k, ws);
+    }
+    __syncwarp();
+    return out + __popc(mask);
   }
   __device__ __forceinline__ void raise(float low) {
     thr = low;
@@ -617,61 +704,46 @@ struct Scan {
     s += ws * exp_from(fmaxf(key_value(k), kFloorRef), ref, c);
   }
 
-  // Cuts the lists to the CTA's K best windows, spread evenly over the warps.
+  // Cuts this warp's list to its K best windows: the windows that it reads from
+  // now on come after those of equal maximum.
   __device__ __forceinline__ void cut() {
-    if (lane == 0) sh.count[warp] = listed;
-    __syncthreads();
-    uint64_t k[kListSlots];
-    float ws[kListSlots];
-    int have = 0;
-#pragma unroll
-    for (int j = 0; j < kListSlots; ++j) {
-      const int f = j * kScanThreads + (int)threadIdx.x, w = f / kListWarp, i = f % kListWarp;
-      const bool in = i < sh.count[w];
-      k[j] = in ? sh.key[w][i] : 0;
-      ws[j] = in ? sh.sum[w][i] : 0.0f;
-      have += in;
+    uint64_t low = 0, high = ~0ull;  // at least K keys reach low, fewer reach high
+    while (high - low > 1) {
+      const uint64_t mid = low + (high - low) / 2;
+      int n = 0;
+      for (int i = lane; i < listed; i += 32) n += list_key[i] >= mid;
+      n = __reduce_add_sync(0xFFFFFFFFu, n);
+      if (n >= K) low = mid;
+      else high = mid;
+      if (n == K) break;
     }
-    int total;
-    block_prefix(have, total, sh);
-    const uint64_t t = total > K ? select_kth(k, K, sh) : 1;
-    int keep = 0;
     uint32_t least = 0xFFFFFFFFu;
-#pragma unroll
-    for (int j = 0; j < kListSlots; ++j)
-      if (k[j] >= t) {
-        ++keep;
-        least = min(least, (uint32_t)(k[j] >> 32));
-      }
+    for (int i = lane; i < listed; i += 32)
+      if (list_key[i] >= low) least = min(least, (uint32_t)(list_key[i] >> 32));
     least = __reduce_min_sync(0xFFFFFFFFu, least);
-    if (lane == 0) sh.redu[1][warp] = least;
-    int at = block_prefix(keep, total, sh);
-#pragma unroll
-    for (int w = 0; w < kScanWarps; ++w) least = min(least, sh.redu[1][w]);
-    if (total >= K) {
-      // windows that are read from now on come after those of equal maximum
-      if (unordered(least) > thr) raise(unordered(least));
-      list_thr = unordered(ordered(thr) + 1);
-      exact = true;
-    }
-#pragma unroll
-    for (int j = 0; j < kListSlots; ++j) {
-      if (k[j] >= t) {
-        sh.key[at % kScanWarps][at / kScanWarps] = k[j];
-        sh.sum[at % kScanWarps][at / kScanWarps] = ws[j];
-        ++at;
-      } else if (k[j]) {
-        drop(k[j], ws[j]);
+    if (unordered(least) > thr) raise(unordered(least));
+    list_thr = unordered(ordered(thr) + 1);
+    exact = true;
+    int out = 0;
+    for (int base = 0; base < listed; base += 32) {
+      const int i = base + lane;
+      uint64_t k = 0;
+      float ws = 0.0f;
+      if (i < listed) {
+        k = list_key[i];
+        ws = list_sum[i];
       }
+      out = keep(k, ws, k && k >= low, out);
     }
-    listed = (total - warp + kScanWarps - 1) / kScanWarps;
-    __syncthreads();
+    listed = out;
   }
 
   // Scans this CTA's part of row t for the k largest at 2^(z cc).
   __device__ __forceinline__ void scan(int t, int k, float cc) {
     const Row<T> row = row_of(t);
-    slice(row, lo, hi);
+    int first, steps, a, b;
+    const int n = run(row, first, steps);
+    whole_part(row, first, n, a, b);
     K = k;
     c = cc;
     thr = list_thr = top0 = top1 = -INFINITY;
@@ -680,102 +752,259 @@ struct Scan {
     s = lost = 0.0f;
     listed = 0;
     int refresh_at = 0;
-    const int steps = max((hi - lo + kScanStep - 1) / kScanStep, 1);
+    // a lane's windows are read in an order that keeps 8 lanes off each other's banks
+    const int turned = lane >> 1;
     for (int step = 0; step < steps; ++step) {
       const int stage = wait();
-      const int i0 = lo + step * kScanStep + warp * kWarpStep + lane;
-      uint4 v[kScanUnroll];
-      float wm[kScanUnroll];
+      const int at = step * kWarpStep + lane * kUnit;
+      uint4 v[kUnit];
+      if (step * kWarpStep >= a && (step + 1) * kWarpStep <= b) {
 #pragma unroll
-      for (int u = 0; u < kScanUnroll; ++u) {
-        const int i = i0 + 32 * u;
-        const uint32_t none = neg_inf_bits(row.p);
-        v[u] = make_uint4(none, none, none, none);
-        if (i < hi) v[u] = row.whole(i) ? sh.ring[warp][stage][lane + 32 * u] : load_window(row, i);
-        wm[u] = window_max<T>(v[u]);
+        for (int u = 0; u < kUnit; ++u) v[u] = sh.ring[warp][stage][lane * kUnit + ((u + turned) & (kUnit - 1))];
+      } else {
+#pragma unroll
+        for (int u = 0; u < kUnit; ++u) {
+          const int i = at + ((u + turned) & (kUnit - 1));
+          const uint32_t none = neg_inf_bits(row.p);
+          v[u] = make_uint4(none, none, none, none);
+          if (i < n) v[u] = i >= a && i < b ? sh.ring[warp][stage][i - step * kWarpStep] : load_window(row, first + i);
+        }
       }
-      top0 = fmaxf(top0, fmaxf(wm[0], wm[1]));
-      top1 = fmaxf(top1, fmaxf(wm[2], wm[3]));
+      const float m0 = window_max<T>(v[0], v[1]), m1 = window_max<T>(v[2], v[3]);
+      top0 = fmaxf(top0, m0);
+      top1 = fmaxf(top1, m1);
       issue();
       if (step == refresh_at || step + 1 == steps) {
         refresh();
-        refresh_at = 2 * step + 1;
+        refresh_at = 4 * step + 3;
       }
-      float sums = 0.0f;
-#pragma unroll
-      for (int u = 0; u < kScanUnroll; ++u) {
-        const int i = i0 + 32 * u;
-        const bool list = i < hi && wm[u] >= list_thr;
-        const float r = list ? fmaxf(wm[u], kFloorRef) : ref;
-        const float ws = window_sum<T>(v[u], c, r);
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, list);
-        if (mask) {
-          if (list) {
-            const int at = listed + __popc(mask & ((1u << lane) - 1u));
-            sh.key[warp][at] = make_key(wm[u], (uint32_t)i);
-            sh.sum[warp][at] = ws;
-          }
-          listed += __popc(mask);
-        }
-        sums += list ? 0.0f : ws;
-      }
-      // s + sums with the rounding kept (a row's thread adds hundreds of these)
-      const float y = sums - lost, z = s + y;
+      const float m = fmaxf(m0, m1);
+      const bool list = m >= list_thr && at < n;
+      const float from = list ? fmaxf(m, kFloorRef) : ref;
+      const float sum = windows_sum<T, kUnit>(v, c, from);
+      // s + sum with the rounding kept (a row's thread adds hundreds of these)
+      const float y = (list ? 0.0f : sum) - lost, z = s + y;
       lost = (z - s) - y;
       s = z;
-      __syncwarp();
-      if (step + 1 < steps && __syncthreads_or(listed > kListWarp - kWarpStep)) {
-        refresh();
-        if (__syncthreads_or(listed > kListWarp - kWarpStep)) cut();
+      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, list);
+      if (mask) {
+        if (list) {
+          const int to = listed + __popc(mask & ((1u << lane) - 1u));
+          list_key[to] = make_key(m, (uint32_t)(first + at));
+          list_sum[to] = sum;
+        }
+        listed += __popc(mask);
+        __syncwarp();
+        if (listed > room - 32 && step + 1 < steps) cut();
       }
     }
-    __syncthreads();
-    if (lane == 0) sh.count[warp] = listed;
-    __syncthreads();
     if (sh.late) s = NAN;
-    int total = 0;
+  }
+
+  // The elements of the listed units that reach the threshold, as keys (value,
+  // id): written to dst in a fixed order, followed by zeros up to `fill`.
+  // Returns their number, at most `cap`; if there were more, the K largest
+  // alone.  All others go into s.
+  __device__ __forceinline__ int candidates(int t, uint64_t *dst, int cap, int fill) {
+    const Row<T> row = row_of(t);
+    const int most = exact ? K : cap;
+    // a lane for each window of this warp's units: how many elements reach, then
+    // (the windows now in L1) where they go
+    const int windows = listed * kUnit;
+    int mine = 0;
+    for (int i = lane; i < windows; i += 32) {
+      const int at = (int)key_index(list_key[i / kUnit]) + i % kUnit;
+      if (at < row.windows) mine += reaching(row, at, load_window(row, at));
+    }
+    const int warp_n = __reduce_add_sync(0xFFFFFFFFu, mine);
+    turn ^= 1;
+    if (lane == 0) {
+      sh.part[turn][warp] = warp_n;
+      sh.count[warp] = listed;
+    }
+    __syncthreads();
+    int before = 0, total = 0, units = 0;
 #pragma unroll
-    for (int w = 0; w < kScanWarps; ++w) total += sh.count[w];
-    if (total > kScanThreads) {
-      __syncthreads();
-      cut();
+    for (int w = 0; w < kScanWarps; ++w) {
+      if (w < warp) before += sh.part[turn][w];
+      total += sh.part[turn][w];
+      units += sh.count[w];
+    }
+    if (total > most) return most_of_many(row, dst, most, fill, units);
+    for (int base = 0; base < windows; base += 32) {
+      const int i = base + lane;
+      const int at = i < windows ? (int)key_index(list_key[i / kUnit]) + i % kUnit : row.windows;
+      const bool in = at < row.windows;
+      const uint32_t none = neg_inf_bits(row.p);
+      const uint4 v = in ? load_window(row, at) : make_uint4(none, none, none, none);
+      const int n = in ? reaching(row, at, v) : 0;
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += u;
+      }
+      if (n == 0) {
+        s += window_sum<T>(v, c, ref);
+      } else {
+        uint64_t *to = dst + before + incl - n;
+        each(row, at, v, [&](float z, int id) {
+          if (z >= thr) *to++ = make_key(z, (uint32_t)id);
+          else s += exp_from(z, ref, c);
+        });
+      }
+      before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+    }
+    for (int i = total + (int)threadIdx.x; i < fill; i += kScanThreads) dst[i] = 0;
+    return total;
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(const Row<T> &row, int at, const uint4 &v, F f) const {
+    float z[E];
+    unpack<T>(v, z);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int id = at * E - row.mis + e;
+      if (id >= 0 && id < vocab) f(z[e], id);
+    }
+  }
+  // Elements of window `at` that reach the threshold.
+  __device__ __forceinline__ int reaching(const Row<T> &row, int at, const uint4 &v) const {
+    int n = 0;
+    if (window_max<T>(v) >= thr) each(row, at, v, [&](float z, int) { n += z >= thr; });
+    return n;
+  }
+
+  // candidates() where there are more than may be passed on (many equal values,
+  // or a short row): the units are cut to the K best of the CTA, their windows
+  // to the K best, and the elements of those to the K largest.
+  __device__ __forceinline__ int most_of_many(const Row<T> &row, uint64_t *dst, int most, int fill,
+                                              int units) {
+    const int tid = threadIdx.x;
+    const uint64_t *const keys = list_key - warp * room;
+    if (units > kScanThreads) {
+      constexpr int kSlots = kScanWarps * (kTopMax + 64) / kScanThreads;
+      uint64_t k[kSlots];
+#pragma unroll
+      for (int j = 0; j < kSlots; ++j) {
+        const int f = j * kScanThreads + tid, of = f / room, i = f - of * room;
+        k[j] = of < kScanWarps && i < sh.count[of] ? keys[of * room + i] : 0;
+      }
+      const uint64_t low = select_kth(k, K, sh);
+      exact = true;
+      raise_to_least(k, low);
+      int out = 0;
+      for (int base = 0; base < listed; base += 32) {
+        const int i = base + lane;
+        const uint64_t key = i < listed ? list_key[i] : 0;
+        const float ws = i < listed ? list_sum[i] : 0.0f;
+        out = keep(key, ws, key && key >= low, out);
+      }
+      listed = out;
       if (lane == 0) sh.count[warp] = listed;
       __syncthreads();
     }
-  }
-
-  // The elements of the listed windows that reach the threshold, as keys (value,
-  // id): written to dst in a fixed order, followed by zeros up to `fill`.
-  // Returns their number, at most candidate_cap(K); if there were more, the K
-  // largest alone.  All others go into s.
-  __device__ __forceinline__ int candidates(int t, uint64_t *dst, int fill) {
-    const Row<T> row = row_of(t);
-    const int tid = threadIdx.x;
-    uint64_t k[E] = {};
-    int i = -1, left = tid, n = 0;
+    // a unit each thread
+    int unit = -1, left = tid;
 #pragma unroll
     for (int w = 0; w < kScanWarps; ++w) {
-      if (left >= 0 && left < sh.count[w]) i = (int)key_index(sh.key[w][left]);
+      if (left >= 0 && left < sh.count[w]) unit = (int)key_index(keys[w * room + left]);
       left -= sh.count[w];
     }
-    if (i >= 0) {
-      float f[E];
-      unpack<T>(load_window(row, i), f);
+    uint64_t k[kUnit];
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < kUnit; ++u) {
+      k[u] = 0;
+      if (unit >= 0 && unit + u < row.windows) {
+        const uint4 v = load_window(row, unit + u);
+        const float m = window_max<T>(v);
+        if (m >= thr) {
+          k[u] = make_key(m, (uint32_t)(unit + u));
+          ++n;
+        } else {
+          s += window_sum<T>(v, c, ref);
+        }
+      }
+    }
+    int total;
+    int at = block_prefix(n, total, sh);
+    if (total > kScanThreads) {
+      const uint64_t low = select_kth(k, K, sh);
+      exact = true;
+      raise_to_least(k, low);
+      n = 0;
+#pragma unroll
+      for (int u = 0; u < kUnit; ++u) {
+        if (k[u] >= low) {
+          ++n;
+        } else if (k[u]) {
+          s += window_sum<T>(load_window(row, unit + u), c, ref);
+          k[u] = 0;
+        }
+      }
+      at = block_prefix(n, total, sh);
+    }
+    // a window each thread
+#pragma unroll
+    for (int u = 0; u < kUnit; ++u)
+      if (k[u]) sh.hist[at++] = key_index(k[u]);
+    __syncthreads();
+    const int window = tid < total ? (int)sh.hist[tid] : -1;
+    __syncthreads();
+    uint64_t key[E] = {};
+    n = 0;
+    if (window >= 0) {
+      const uint4 v = load_window(row, window);
+      float z[E];
+      unpack<T>(v, z);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int id = i * E - row.mis + e;
+        const int id = window * E - row.mis + e;
         if (id >= 0 && id < vocab) {
-          if (f[e] >= thr) {
-            k[e] = make_key(f[e], (uint32_t)id);
+          if (z[e] >= thr) {
+            key[e] = make_key(z[e], (uint32_t)id);
             ++n;
           } else {
-            s += exp_from(f[e], ref, c);
+            s += exp_from(z[e], ref, c);
           }
         }
       }
     }
-    return emit(k, n, exact ? K : candidate_cap(K), dst, fill);
+    return emit(key, n, exact ? K : most, dst, fill);
   }
+  // Raises the threshold to the least value of the block's keys from `low` up.
+  template <int N>
+  __device__ __forceinline__ void raise_to_least(const uint64_t (&k)[N], uint64_t low) {
+    uint32_t least = 0xFFFFFFFFu;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (k[j] >= low) least = min(least, (uint32_t)(k[j] >> 32));
+    least = __reduce_min_sync(0xFFFFFFFFu, least);
+    if (lane == 0) sh.redu[1][warp] = least;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kScanWarps; ++w) least = min(least, sh.redu[1][w]);
+    __syncthreads();
+    if (unordered(least) > thr) raise(unordered(least));
+  }
+  // Leaves the keys from t up and adds the others to s; returns how many are left.
+  template <int N>
+  __device__ __forceinline__ int drop_below(uint64_t t, uint64_t (&k)[N]) {
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if (k[e] >= t) {
+        n += k[e] != 0;
+      } else if (k[e]) {
+        s += exp_from(key_value(k[e]), ref, c);
+        k[e] = 0;
+      }
+    }
+    return n;
+  }
+  // Writes the threads' keys (n of this thread are not 0) to dst, in the
+  // threads' order; if they are more than `most`, the K largest alone.
   template <int N>
   __device__ __forceinline__ int emit(uint64_t (&k)[N], int n, int most, uint64_t *dst, int fill) {
     int total;
@@ -783,26 +1012,9 @@ struct Scan {
     if (total > most) {
       exact = true;
       const uint64_t t = select_kth(k, K, sh);
-      n = 0;
-      uint32_t least = 0xFFFFFFFFu;
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (k[e] >= t) {
-          ++n;
-          least = min(least, (uint32_t)(k[e] >> 32));
-        }
-      least = __reduce_min_sync(0xFFFFFFFFu, least);
-      if (lane == 0) sh.redu[1][warp] = least;
+      raise_to_least(k, t);
+      n = drop_below(t, k);
       at = block_prefix(n, total, sh);
-#pragma unroll
-      for (int w = 0; w < kScanWarps; ++w) least = min(least, sh.redu[1][w]);
-      if (unordered(least) > thr) raise(unordered(least));
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (k[e] && k[e] < t) {
-          s += exp_from(key_value(k[e]), ref, c);
-          k[e] = 0;
-        }
     }
 #pragma unroll
     for (int e = 0; e < N; ++e)
@@ -811,66 +1023,105 @@ struct Scan {
     return total;
   }
 
-  // After scan(): gathers the cluster's candidates at the row's leader, which
-  // changes from row to row (`turn`).  True there: then sh.cand holds n
-  // candidates, the n largest elements of the row (n >= K unless the row has
-  // fewer or NaN), and s (this thread's part), ref and thr are the row's.
-  //
-  // The barrier's phase of a row ends when all its parts are written.  A CTA
-  // writes the next row's after that phase; a leader reads its row's before it
-  // arrives at the next, and leads again a row later at the earliest, so that
-  // one buffer is enough.
-  __device__ __forceinline__ bool gather(int t, int turn, int &n) {
-    if (C == 1) {
-      n = candidates(t, sh.cand, 0);
-      __syncthreads();
-      return true;
-    }
+  // In a cluster, a row's parts are gathered at its leader, which changes from
+  // row to row, and the leader joins them once it has scanned and passed on its
+  // part of the next row, so that it waits for no one.  A phase of the cluster's
+  // barrier ends when all parts of a row are written; a CTA writes the next
+  // row's after that.  A leader reads its row's parts before it arrives at the
+  // second next phase, and leads again after C rows: in clusters of two, whose
+  // CTAs may then write a second row's parts too early, they go to a second
+  // buffer.
+  __device__ __forceinline__ int leader_of(int row_turn) const { return row_turn & (C - 1); }
+  __device__ __forceinline__ int half_of(int row_turn) const { return C == 2 ? row_turn >> 1 & 1 : 0; }
+  // After scan(): passes on this CTA's part of row t.
+  __device__ __forceinline__ void push(int t, int row_turn) {
     cg::cluster_group cluster = cg::this_cluster();
-    const int tid = threadIdx.x, leader = turn % C, cap = candidate_cap(K);
-    if (!waited) cluster_wait();
-    candidates(t, cluster.map_shared_rank(recv, leader) + rank * recv_cap, cap);
+    const int leader = leader_of(row_turn), half = half_of(row_turn), cap = candidate_cap(K);
+    cluster_wait();
+    candidates(t, cluster.map_shared_rank(recv, leader) + (half * C + rank) * recv_cap, cap, cap);
     const float total = block_reduce<kScanThreads>(s, sh.redf, OpAdd());
-    if (tid == 0) {
-      *cluster.map_shared_rank(&sh.part_sum[rank], leader) = total;
-      *cluster.map_shared_rank(&sh.part_thr[rank], leader) = thr;
-      *cluster.map_shared_rank(&sh.part_exact[rank], leader) = exact;
+    if (threadIdx.x == 0) {
+      *cluster.map_shared_rank(&sh.part_sum[half][rank], leader) = total;
+      *cluster.map_shared_rank(&sh.part_thr[half][rank], leader) = thr;
+      *cluster.map_shared_rank(&sh.part_exact[half][rank], leader) = exact;
     }
     cluster_arrive();
-    waited = rank == leader;
-    if (!waited) return false;
-    cluster_wait();
+  }
+  // At the leader, after the phase of its row: as candidates() in a cluster of
+  // one, sh.cand then holds the n largest elements of the row (n >= K unless the
+  // row has fewer or NaN), and s (this thread's part), ref and thr are the row's.
+  __device__ __forceinline__ int merge(int row_turn, int k_, float cc) {
+    const int tid = threadIdx.x, half = half_of(row_turn);
+    K = k_;
+    c = cc;
+    const int cap = candidate_cap(K);
+    thr = -INFINITY;
+    exact = false;
     for (int i = 0; i < C; ++i) {
-      thr = fmaxf(thr, sh.part_thr[i]);
-      exact |= sh.part_exact[i] != 0;
+      thr = fmaxf(thr, sh.part_thr[half][i]);
+      exact |= sh.part_exact[half][i] != 0;
     }
     ref = fmaxf(thr, kFloorRef);
-    s = tid < C ? sh.part_sum[tid] * exp_from(fmaxf(sh.part_thr[tid], kFloorRef), ref, c) : 0.0f;
-    uint64_t k[kTopMax * kClusterMax / kScanThreads];
-    int mine = 0;
+    s = tid < C ? sh.part_sum[half][tid] * exp_from(fmaxf(sh.part_thr[half][tid], kFloorRef), ref, c) : 0.0f;
+    constexpr int kKeys = kTopMax * kClusterMax / kScanThreads;
+    uint64_t k[kKeys];
+    float most = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kTopMax * kClusterMax / kScanThreads; ++j) {
-      const int i = j * kScanThreads + tid, r = i / cap;
-      k[j] = r < C ? recv[r * recv_cap + i % cap] : 0;
-      if (k[j] && key_value(k[j]) < thr) {
-        s += exp_from(key_value(k[j]), ref, c);
-        k[j] = 0;
-      }
-      mine += k[j] != 0;
+    for (int j = 0; j < kKeys; ++j) {
+      const int i = j * kScanThreads + tid, r = i >> (31 - __clz(cap));
+      k[j] = r < C ? recv[(half * C + r) * recv_cap + (i & (cap - 1))] : 0;
+      if (k[j]) most = fmaxf(most, key_value(k[j]));
     }
-    n = emit(k, mine, exact ? K : cap, sh.cand, 0);
+    // the threads' largest show a threshold too
+    const float reach = warp_reach(most, -INFINITY, (K + kScanWarps - 1) / kScanWarps, -INFINITY, kGrain);
+    turn ^= 1;
+    if (lane == 0) sh.reach[turn][warp] = reach;
     __syncthreads();
-    return true;
+    float low = INFINITY;
+#pragma unroll
+    for (int w = 0; w < kScanWarps; ++w) low = fminf(low, sh.reach[turn][w]);
+    if (low > thr) raise(low);
+    const int mine = drop_below(thr > -INFINITY ? (uint64_t)ordered(thr) << 32 : 1, k);
+    const int n = emit(k, mine, exact ? K : cap, sh.cand, 0);
+    __syncthreads();
+    return n;
   }
-  // No CTA ends while another may write to its shared memory, or a copy to its own.
-  __device__ __forceinline__ void finish() {
-    if (!waited) cluster_wait();
-    waited = true;
+  // The loop over this cluster's rows.  request(t, K, c) says what row t is
+  // scanned for; done(t, n) is called by all threads of a row's leader.
+  template <typename R, typename D>
+  __device__ __forceinline__ void rows_of_cluster(R request, D done) {
+    int t = (int)(blockIdx.x / C);
+    for (int row_turn = 0;; ++row_turn, t += clusters) {
+      const bool more = t < rows;
+      int at = -1, n = 0, k;
+      float cc;
+      if (more) {
+        request(t, k, cc);
+        scan(t, k, cc);
+      }
+      if (C == 1) {
+        if (more) {
+          n = candidates(t, sh.cand, candidate_cap(K), 0);
+          __syncthreads();
+          at = t;
+        }
+      } else {
+        if (more) push(t, row_turn);
+        else cluster_wait();
+        if (row_turn > 0 && leader_of(row_turn - 1) == rank) {
+          at = t - clusters;
+          request(at, k, cc);
+          n = merge(row_turn - 1, k, cc);
+        }
+      }
+      if (at >= 0) done(at, n);
+      if (!more) break;
+    }
+    // a copy that did not come in time may still come: not after this CTA's end
     if (dead)
       for (; used != issued; ++used)
         wait_copy(smem_u32(&sh.bar[warp][used % kScanStages]), (used / kScanStages) & 1);
   }
-  bool waited;  // this thread has passed the last phase that it arrived at
   static __device__ __forceinline__ void cluster_arrive() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   }
