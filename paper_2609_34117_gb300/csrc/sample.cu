@@ -285,19 +285,29 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
                                       uint64_t mass, int32_t *token, float *logprob,
                                       ScanShared &sh, SampleShared &sm) {
   const int tid = threadIdx.x;
-  const uint64_t key = tid < n ? sh.cand[tid] : 0;
-  const float e = key ? element_exp(key_value(key), m, d.inv) : 0.0f;
-  uint64_t w = element_weight(e);
-  sm.weight[tid] = w;
+  // a few lanes for each candidate; the first of them holds it
+  const int lanes = candidate_lanes(n), at = tid / lanes, sub = tid % lanes;
+  if (tid < n) sm.weight[tid] = element_weight(element_exp(key_value(sh.cand[tid]), m, d.inv));
+  uint64_t key = at < n ? sh.cand[at] : 0;
   __syncthreads();
   int rank = 0;
   uint64_t before = 0;
-  if (key)
-    for (int i = 0; i < n; ++i)
+  if (key) {
+#pragma unroll 4
+    for (int i = sub; i < n; i += lanes)
       if (sh.cand[i] > key) {
         ++rank;
         before += sm.weight[i];
       }
+  }
+  for (int o = 1; o < lanes; o *= 2) {
+    rank += __shfl_xor_sync(0xFFFFFFFFu, rank, o);
+    before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
+  }
+  const uint64_t shared_key = key;
+  if (sub) key = 0;
+  const float e = key ? element_exp(key_value(key), m, d.inv) : 0.0f;
+  uint64_t w = key ? sm.weight[at] : 0;
   const bool in = key && rank < d.top_k;
   const uint64_t listed = block_reduce<kScanThreads>(in ? w : 0, sh.red64, OpAdd());
   uint64_t cut = ~0ull;
@@ -325,12 +335,17 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
   }
   if (cut < 1) cut = 1;
   if (!(in && before < cut && e >= d.min_p)) w = 0;
-  sm.weight[tid] = w;
+  __syncthreads();
+  if (key) sm.weight[at] = w;
   const uint64_t total = block_reduce<kScanThreads>(w, sh.red64, OpAdd());
   const uint64_t target = fraction(total, d.u24);
   uint64_t id_before = 0;
-  for (int i = 0; w && i < n; ++i)  // (the key's low half is the complement of the id)
-    if ((uint32_t)sh.cand[i] > (uint32_t)key) id_before += sm.weight[i];
+  if (shared_key) {
+#pragma unroll 4
+    for (int i = sub; i < n; i += lanes)  // (the key's low half is the complement of the id)
+      if ((uint32_t)sh.cand[i] > (uint32_t)shared_key) id_before += sm.weight[i];
+  }
+  for (int o = 1; o < lanes; o *= 2) id_before += __shfl_xor_sync(0xFFFFFFFFu, id_before, o);
   if (w && target >= id_before && target < id_before + w) {
     *token = (int32_t)key_index(key);
     *logprob = logf((float)w / (float)total);

@@ -29,13 +29,17 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
     cc = c;
   };
   scan.rows_of_cluster(request, [&](int t, int n) {
-    // one candidate a thread: its place in the order
-    const uint64_t key = tid < n ? sh.cand[tid] : 0;
+    // a candidate's place in the order, by a few lanes
+    const int lanes = candidate_lanes(n), at_cand = tid / lanes, sub = tid % lanes;
+    uint64_t key = at_cand < n ? sh.cand[at_cand] : 0;
     int rank = 0;
     if (key) {
-      for (int i = 0; i < n; ++i) rank += sh.cand[i] > key;
-      sh.by_rank[rank] = key_value(key);
+#pragma unroll 4
+      for (int i = sub; i < n; i += lanes) rank += sh.cand[i] > key;
     }
+    for (int o = 1; o < lanes; o *= 2) rank += __shfl_xor_sync(0xFFFFFFFFu, rank, o);
+    if (sub) key = 0;
+    if (key) sh.by_rank[rank] = key_value(key);
     __syncthreads();
     // sums in the order of the ranks
     const float m = fmaxf(n > 0 ? sh.by_rank[0] : -INFINITY, kFloorRef);

@@ -343,17 +343,19 @@ constexpr int kUnit = 4;                      // windows of a unit
 constexpr int kWarpStep = 32 * kUnit;         // windows of a warp in a step
 constexpr int kScanStages = 2;
 constexpr int kClusterMax = 8;
+constexpr int kStage = 32;
 static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
 
 // Candidates that a CTA passes on: the K best and others, if there are no more
 // than this (else the K best alone).  A power of two.
-__host__ __device__ inline int candidate_cap(int K) { return K <= 32 ? 64 : K <= 64 ? 128 : kTopMax; }
+__host__ __device__ inline int candidate_cap(int K) { return K <= 8 ? 64 : K <= 32 ? 128 : kTopMax; }
 // Units that a warp's list has room for: K (64 at least) and two steps'.
 __host__ __device__ inline int list_room(int K) { return (K <= 64 ? 64 : (K + 31) / 32 * 32) + 64; }
 
 struct ScanShared {
   uint4 ring[kScanWarps][kScanStages][kWarpStep];
   uint64_t cand[kTopMax];
+  uint64_t stage[kScanWarps][kStage];  // a warp's candidates before their place is known
   uint64_t bar[kScanWarps][kScanStages];
   uint64_t red64[kScanWarps];
   uint32_t hist[256];
@@ -483,13 +485,27 @@ __device__ __forceinline__ int block_prefix(int v, int &total, ScanShared &sh) {
 
 // A value that at least m of the warp's 2 x 32 values a, b reach, and few more;
 // -inf if fewer than m are above -inf.  `low`: a value that is known to be
-// reached by as many, or -inf.  Bisection over the order of the values' bits,
+// reached by as many, or -inf.  For larger m, bisection over the order of the values' bits,
 // which masked logits of the type's lowest value do not stretch as they would
 // the range of the values, down to steps of `grain` bits.
 __device__ __forceinline__ float warp_reach(float a, float b, int m, float low, uint32_t grain) {
   const uint32_t all = 0xFFFFFFFFu;
   const uint32_t oa = ordered(a), ob = ordered(b), none = ordered(-INFINITY);
   auto count = [&](uint32_t x) { return __popc(__ballot_sync(all, oa >= x)) + __popc(__ballot_sync(all, ob >= x)); };
+  if (m <= 12) {
+    // the m-th largest itself, taking away the largest in turn
+    uint32_t first = max(oa, ob), second = min(oa, ob);
+    while (true) {
+      const uint32_t h = __reduce_max_sync(all, first);
+      if (h <= none) return low;
+      m -= __popc(__ballot_sync(all, first == h)) + __popc(__ballot_sync(all, second == h));
+      if (m <= 0) return fmaxf(low, unordered(h));
+      if (first == h) {
+        first = second == h ? 0 : second;
+        second = 0;
+      }
+    }
+  }
   uint32_t lo, hi = __reduce_max_sync(all, max(oa, ob));
   if (low > -INFINITY) {
     lo = ordered(low);
@@ -509,6 +525,11 @@ __device__ __forceinline__ float warp_reach(float a, float b, int m, float low, 
     }
   }
   return unordered(lo);
+}
+
+// Lanes that share a candidate in a pass over all n of them (a power of two).
+__device__ __forceinline__ int candidate_lanes(int n) {
+  return n <= 32 ? 8 : n <= 64 ? 4 : n <= 128 ? 2 : 1;
 }
 
 template <typename T>
@@ -808,18 +829,42 @@ struct Scan {
   __device__ __forceinline__ int candidates(int t, uint64_t *dst, int cap, int fill) {
     const Row<T> row = row_of(t);
     const int most = exact ? K : cap;
-    // a lane for each window of this warp's units: how many elements reach, then
-    // (the windows now in L1) where they go
+    // a lane for each window of this warp's units; a warp's candidates are held
+    // until it is known where they go (if they are too many to hold, the windows
+    // are read again, from L1)
     const int windows = listed * kUnit;
-    int mine = 0;
-    for (int i = lane; i < windows; i += 32) {
-      const int at = (int)key_index(list_key[i / kUnit]) + i % kUnit;
-      if (at < row.windows) mine += reaching(row, at, load_window(row, at));
-    }
-    const int warp_n = __reduce_add_sync(0xFFFFFFFFu, mine);
+    float add = 0.0f;
+    int held = 0;
+    auto pass = [&](auto put, float &sum) {
+#pragma unroll 2
+      for (int base = 0; base < windows; base += 32) {
+        const int i = base + lane;
+        const int at = i < windows ? (int)key_index(list_key[i / kUnit]) + i % kUnit : row.windows;
+        const uint32_t none = neg_inf_bits(row.p);
+        const uint4 v = at < row.windows ? load_window(row, at) : make_uint4(none, none, none, none);
+        const bool hit = at < row.windows && window_max<T>(v) >= thr;
+        if (!hit) sum += window_sum<T>(v, c, ref);
+        if (!__any_sync(0xFFFFFFFFu, hit)) continue;
+        float z[E];
+        unpack<T>(v, z);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int id = at * E - row.mis + e;
+          const bool in = hit && id >= 0 && id < vocab, yes = in && z[e] >= thr;
+          put(yes, z[e], id);
+          if (in && !yes) sum += exp_from(z[e], ref, c);
+        }
+      }
+    };
+    pass([&](bool yes, float z, int id) {
+      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+      const int at = held + __popc(mask & ((1u << lane) - 1u));
+      if (yes && at < kStage) sh.stage[warp][at] = make_key(z, (uint32_t)id);
+      held += __popc(mask);
+    }, add);
     turn ^= 1;
     if (lane == 0) {
-      sh.part[turn][warp] = warp_n;
+      sh.part[turn][warp] = held;
       sh.count[warp] = listed;
     }
     __syncthreads();
@@ -831,48 +876,18 @@ struct Scan {
       units += sh.count[w];
     }
     if (total > most) return most_of_many(row, dst, most, fill, units);
-    for (int base = 0; base < windows; base += 32) {
-      const int i = base + lane;
-      const int at = i < windows ? (int)key_index(list_key[i / kUnit]) + i % kUnit : row.windows;
-      const bool in = at < row.windows;
-      const uint32_t none = neg_inf_bits(row.p);
-      const uint4 v = in ? load_window(row, at) : make_uint4(none, none, none, none);
-      const int n = in ? reaching(row, at, v) : 0;
-      int incl = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if (lane >= o) incl += u;
-      }
-      if (n == 0) {
-        s += window_sum<T>(v, c, ref);
-      } else {
-        uint64_t *to = dst + before + incl - n;
-        each(row, at, v, [&](float z, int id) {
-          if (z >= thr) *to++ = make_key(z, (uint32_t)id);
-          else s += exp_from(z, ref, c);
-        });
-      }
-      before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+    if (held <= kStage) {
+      s += add;
+      if (lane < held) dst[before + lane] = sh.stage[warp][lane];
+    } else {
+      pass([&](bool yes, float z, int id) {
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+        if (yes) dst[before + __popc(mask & ((1u << lane) - 1u))] = make_key(z, (uint32_t)id);
+        before += __popc(mask);
+      }, s);
     }
     for (int i = total + (int)threadIdx.x; i < fill; i += kScanThreads) dst[i] = 0;
     return total;
-  }
-  template <typename F>
-  __device__ __forceinline__ void each(const Row<T> &row, int at, const uint4 &v, F f) const {
-    float z[E];
-    unpack<T>(v, z);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int id = at * E - row.mis + e;
-      if (id >= 0 && id < vocab) f(z[e], id);
-    }
-  }
-  // Elements of window `at` that reach the threshold.
-  __device__ __forceinline__ int reaching(const Row<T> &row, int at, const uint4 &v) const {
-    int n = 0;
-    if (window_max<T>(v) >= thr) each(row, at, v, [&](float z, int) { n += z >= thr; });
-    return n;
   }
 
   // candidates() where there are more than may be passed on (many equal values,
