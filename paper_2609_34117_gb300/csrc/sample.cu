@@ -24,7 +24,7 @@
 
 namespace slimwise {
 
-constexpr int kSampleCtas = 3;    // CTAs of an SM
+constexpr int kSampleCtas = 4;    // CTAs of an SM
 constexpr int kNucleus = 64;      // elements looked at for a nucleus or min-p without top-k
 constexpr int kTopKListed = 128;  // largest top-k that is decided from the list
 constexpr int32_t kLeftOver = -2; // a token that is still to be searched (its logprob: the maximum)

@@ -13,7 +13,10 @@
 
 namespace slimwise {
 
-constexpr int kTopCtas = 3;  // CTAs of an SM
+constexpr int kTopCtas = 4;  // CTAs of an SM
+// A CTA's time for a row, in cycles: for each of its windows, and besides (the
+// thresholds, the candidates, the row's end).
+constexpr double kWindowCycles = 2.0, kRowCycles = 20000.0;
 
 template <typename T>
 __global__ void __launch_bounds__(kScanThreads, kTopCtas)
@@ -73,16 +76,14 @@ ScanGrid scan_grid(int rows, int vocab, int element_bytes, int ctas_per_sm) {
   const int windows = (int)(((int64_t)vocab * element_bytes + 15) / 16) + 1;
   const int slots = 152 * ctas_per_sm;
   ScanGrid best = {1, 1};
-  double best_use = 0.0;
+  double least = 0.0;
   for (int C = 1; C <= kClusterMax; C *= 2) {
-    if (C > 1 && windows < C * kScanWarps * kWarpStep / 2) break;
     const int at_once = slots / C, clusters = rows < at_once ? rows : at_once;
     const int rounds = (rows + clusters - 1) / clusters;
-    // share of the CTAs' time that has work: the larger cluster has to be worth it
-    const double use = (double)rows * C / ((double)rounds * slots);
-    if (use > 1.05 * best_use) {
+    const double time = rounds * (kWindowCycles * windows / C + kRowCycles);
+    if (C == 1 || time < least) {
       best = {C, clusters};
-      best_use = use;
+      least = time;
     }
   }
   return best;

@@ -334,14 +334,17 @@ struct OpMax {
 // list keeps its precision however far the list rises above it.  Which thread
 // adds what never depends on timing, so that results are the same on every run.
 //
-// Each warp streams its run through a ring of its own with bulk copies; a stage
-// is copied again as soon as its windows are in registers, and the copies of the
-// next row are under way while a row is finished.
+// Each warp streams its run through a ring of its own with asynchronous copies; a
+// stage is copied again as soon as its windows are in registers, and the copies
+// of the next row are under way while a row is finished.  (Bulk copies counted on
+// mbarriers cost about 80 instructions a step to issue and await, these 20, and
+// the scan is bound by its instructions.)
 constexpr int kScanThreads = 256;
 constexpr int kScanWarps = kScanThreads / 32;
 constexpr int kUnit = 4;                      // windows of a unit
 constexpr int kWarpStep = 32 * kUnit;         // windows of a warp in a step
 constexpr int kScanStages = 2;
+static_assert(kScanStages == 2, "a stage's number is one bit");
 constexpr int kClusterMax = 8;
 constexpr int kStage = 32;
 static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
@@ -349,24 +352,28 @@ static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
 // Candidates that a CTA passes on: the K best and others, if there are no more
 // than this (else the K best alone).  A power of two.
 __host__ __device__ inline int candidate_cap(int K) { return K <= 8 ? 64 : K <= 32 ? 128 : kTopMax; }
-// Units that a warp's list has room for: K (64 at least) and two steps'.
-__host__ __device__ inline int list_room(int K) { return (K <= 64 ? 64 : (K + 31) / 32 * 32) + 64; }
+// Units that a warp's list has room for: K (64 at least), and what a threshold
+// of the 4th step lists until the 16th.
+constexpr int kListSpare = 112;
+__host__ __device__ inline int list_room(int K) { return (K <= 64 ? 64 : (K + 31) / 32 * 32) + kListSpare; }
 
 struct ScanShared {
   uint4 ring[kScanWarps][kScanStages][kWarpStep];
   uint64_t cand[kTopMax];
-  uint64_t stage[kScanWarps][kStage];  // a warp's candidates before their place is known
-  uint64_t bar[kScanWarps][kScanStages];
   uint64_t red64[kScanWarps];
-  uint32_t hist[256];
-  float by_rank[kTopMax];
+  union {
+    uint64_t stage[kScanWarps][kStage];  // a warp's candidates before their place is known
+    struct {
+      uint32_t hist[256];
+      float by_rank[kTopMax];
+    };
+  };
   float redf[kScanWarps];
   uint32_t redu[2][kScanWarps];
-  float reach[2][kScanWarps], known[2][kScanWarps];  // by refresh, in turn
+  alignas(16) float reach[2][kScanWarps], known[2][kScanWarps];  // by refresh, in turn
   int part[2][kScanWarps];
   int count[kScanWarps];
   int sel_digit, sel_above, sel_bin;
-  int late;                                          // a wait for a copy gave up
   float part_sum[2][kClusterMax], part_thr[2][kClusterMax];  // at a row's leader: each CTA's
   int part_exact[2][kClusterMax];
   // then  uint64_t [warps][room]   listed units' keys (maximum, index of the first window)
@@ -547,11 +554,12 @@ struct Scan {
   int log_parts;                // warps of a cluster
   int C, rank, clusters;        // CTAs of a cluster, this CTA's place, clusters of the grid
   int lane, warp;
-  // the copies under way: step next_k of row next_t, whose run is at next_src
-  // with windows [next_a, next_b) to copy
-  int next_t, next_k, next_steps, next_a, next_b;
+  // the next copy: of row next_t, with next_left steps to go; this lane's first
+  // window is the next_i-th of next_n to copy
+  int next_t, next_left, next_i, next_n;
   const uint4 *next_src;
-  uint32_t issued, used;        // stages copied, and read
+  uint32_t ring;                // this lane's place in the ring's first stage
+  int issue_stage, stage;       // that is copied and read next
   // the row at hand
   int K;
   float c, thr;                 // scale of the exponents (log2 e / temperature); threshold
@@ -561,11 +569,10 @@ struct Scan {
   int listed;                   // windows in this warp's list
   int turn;                     // of reach and known
   bool exact;                   // the K best alone are known to be complete
-  bool dead;                    // a copy did not arrive: this warp waits for none any more
 
   // K_most: the largest K of all rows
   __device__ __forceinline__ Scan(ScanShared &shared, int K_most, const T *z, int64_t st, int V, int n)
-      : sh(shared), logits(z), stride(st), vocab(V), rows(n), dead(false) {
+      : sh(shared), logits(z), stride(st), vocab(V), rows(n) {
     cg::cluster_group cluster = cg::this_cluster();
     C = (int)cluster.num_blocks();
     rank = (int)cluster.block_rank();
@@ -580,14 +587,8 @@ struct Scan {
     list_key = keys + warp * room;
     list_sum = sums + warp * room;
     recv = reinterpret_cast<uint64_t *>(sums + kScanWarps * room);
-    if (threadIdx.x == 0) {
-      for (int w = 0; w < kScanWarps; ++w)
-        for (int i = 0; i < kScanStages; ++i) mbar_init(smem_u32(&sh.bar[w][i]), 1);
-      mbar_fence_init();
-      sh.late = 0;
-    }
-    __syncthreads();
-    issued = used = 0;
+    ring = smem_u32(&sh.ring[warp][0][lane]);
+    issue_stage = stage = 0;
     turn = 0;
     next_t = (int)(blockIdx.x / C);
     next_row();
@@ -622,48 +623,47 @@ struct Scan {
   }
 
   __device__ __forceinline__ void next_row() {
-    next_k = 0;
-    if (next_t >= rows) return;
-    const Row<T> row = row_of(next_t);
-    int first;
-    const int n = run(row, first, next_steps);
-    whole_part(row, first, n, next_a, next_b);
-    next_src = row.w + first;
-  }
-  // Starts the copy of this warp's windows of the next step.
-  __device__ __forceinline__ void issue() {
-    if (next_t >= rows || dead) return;
-    const int stage = (int)(issued % kScanStages);
-    const int at = next_k * kWarpStep;
-    const int from = max(at, next_a), to = min(at + kWarpStep, next_b);
-    const uint32_t bar = smem_u32(&sh.bar[warp][stage]);
-    __syncwarp();
-    if (elect_one()) {
-      const uint32_t bytes = to > from ? (uint32_t)(to - from) * 16 : 0;
-      mbar_arrive_expect_tx(bar, bytes);
-      if (bytes) bulk_load(smem_u32(&sh.ring[warp][stage][from - at]), next_src + from, bytes, bar);
+    if (next_t >= rows) {
+      next_left = 1 << 30;
+      next_n = 0;
+      return;
     }
-    ++issued;
-    if (++next_k >= next_steps) {
+    const Row<T> row = row_of(next_t);
+    int first, a, b;
+    const int n = run(row, first, next_left);
+    whole_part(row, first, n, a, b);
+    next_src = row.w + first + lane;
+    next_i = lane - a;
+    next_n = max(b - a, 0);
+  }
+  // Starts the copy of this warp's windows of the next step, the row's partial
+  // windows left out.  The stage's windows have been read by all lanes.
+  __device__ __forceinline__ void issue() {
+    const uint32_t to = ring + issue_stage * (kWarpStep * 16);
+#pragma unroll
+    for (int u = 0; u < kUnit; ++u)
+      if ((unsigned)(next_i + 32 * u) < (unsigned)next_n)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + u * 512), "l"(next_src + 32 * u)
+                     : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    issue_stage ^= 1;
+    next_i += kWarpStep;
+    next_src += kWarpStep;
+    if (--next_left == 0) {
       next_t += clusters;
       next_row();
     }
   }
-  // Waits for the oldest copy; a wait that gives up marks the CTA's results.
-  __device__ __forceinline__ int wait() {
-    const int stage = (int)(used % kScanStages);
-    if (!dead) {
-      const bool ok = wait_copy(smem_u32(&sh.bar[warp][stage]), (used / kScanStages) & 1);
-      if (!__all_sync(0xFFFFFFFFu, ok)) {
-        dead = true;
-        sh.late = 1;
-      } else {
-        ++used;
-      }
-    }
-    return stage;
+  // Waits for the oldest copy, of all lanes.
+  __device__ __forceinline__ void wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kScanStages - 1) : "memory");
+    __syncwarp();
   }
 
+  static __device__ __forceinline__ float least_of(const float (&x)[kScanWarps]) {
+    const float4 a = *reinterpret_cast<const float4 *>(x), b = *reinterpret_cast<const float4 *>(x + 4);
+    return fminf(fminf(fminf(a.x, a.y), fminf(a.z, a.w)), fminf(fminf(b.x, b.y), fminf(b.z, b.w)));
+  }
   // Raises the threshold to what the groups of all warps show, and drops the
   // listed windows below it.
   __device__ __forceinline__ void refresh() {
@@ -672,15 +672,14 @@ struct Scan {
     if (lane == 0) {
       sh.reach[turn][warp] = reach;
       sh.known[turn][warp] = thr;
-      sh.part[turn][warp] = exact;
     }
-    __syncthreads();
-    float low = INFINITY, known = -INFINITY;
+    // (a warp that cut its list knows more than the others)
+    const bool cuts = __syncthreads_or(exact);
+    float low = least_of(sh.reach[turn]), known = thr;
+    if (cuts) {
+      exact = true;
 #pragma unroll
-    for (int w = 0; w < kScanWarps; ++w) {
-      low = fminf(low, sh.reach[turn][w]);
-      known = fmaxf(known, sh.known[turn][w]);
-      exact |= sh.part[turn][w] != 0;
+      for (int w = 0; w < kScanWarps; ++w) known = fmaxf(known, sh.known[turn][w]);
     }
     low = fmaxf(low, known);
     if (low > thr) {
@@ -776,7 +775,7 @@ struct Scan {
     // a lane's windows are read in an order that keeps 8 lanes off each other's banks
     const int turned = lane >> 1;
     for (int step = 0; step < steps; ++step) {
-      const int stage = wait();
+      wait();
       const int at = step * kWarpStep + lane * kUnit;
       uint4 v[kUnit];
       if (step * kWarpStep >= a && (step + 1) * kWarpStep <= b) {
@@ -794,6 +793,8 @@ struct Scan {
       const float m0 = window_max<T>(v[0], v[1]), m1 = window_max<T>(v[2], v[3]);
       top0 = fmaxf(top0, m0);
       top1 = fmaxf(top1, m1);
+      stage ^= 1;
+      __syncwarp();
       issue();
       if (step == refresh_at || step + 1 == steps) {
         refresh();
@@ -819,7 +820,6 @@ struct Scan {
         if (listed > room - 32 && step + 1 < steps) cut();
       }
     }
-    if (sh.late) s = NAN;
   }
 
   // The elements of the listed units that reach the threshold, as keys (value,
@@ -841,23 +841,24 @@ struct Scan {
         const int i = base + lane;
         const int at = i < windows ? (int)key_index(list_key[i / kUnit]) + i % kUnit : row.windows;
         const uint32_t none = neg_inf_bits(row.p);
-        const uint4 v = at < row.windows ? load_window(row, at) : make_uint4(none, none, none, none);
-        const bool hit = at < row.windows && window_max<T>(v) >= thr;
-        if (!hit) sum += window_sum<T>(v, c, ref);
-        if (!__any_sync(0xFFFFFFFFu, hit)) continue;
+        uint4 v = make_uint4(none, none, none, none);
+        if (at < row.windows) v = load_window(row, at);
         float z[E];
         unpack<T>(v, z);
+        const int id0 = at * E - row.mis;
+        float sums = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const int id = at * E - row.mis + e;
-          const bool in = hit && id >= 0 && id < vocab, yes = in && z[e] >= thr;
-          put(yes, z[e], id);
-          if (in && !yes) sum += exp_from(z[e], ref, c);
+          // what lies outside the row is -inf, and no candidate below a threshold of -inf
+          const bool yes = z[e] >= thr && (thr > -INFINITY || (id0 + e >= 0 && id0 + e < vocab && at < row.windows));
+          const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+          if (mask) put(mask, yes, z[e], id0 + e);
+          sums += exp_from(yes ? -INFINITY : z[e], ref, c);
         }
+        sum += sums;
       }
     };
-    pass([&](bool yes, float z, int id) {
-      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+    pass([&](uint32_t mask, bool yes, float z, int id) {
       const int at = held + __popc(mask & ((1u << lane) - 1u));
       if (yes && at < kStage) sh.stage[warp][at] = make_key(z, (uint32_t)id);
       held += __popc(mask);
@@ -880,8 +881,7 @@ struct Scan {
       s += add;
       if (lane < held) dst[before + lane] = sh.stage[warp][lane];
     } else {
-      pass([&](bool yes, float z, int id) {
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+      pass([&](uint32_t mask, bool yes, float z, int id) {
         if (yes) dst[before + __popc(mask & ((1u << lane) - 1u))] = make_key(z, (uint32_t)id);
         before += __popc(mask);
       }, s);
@@ -898,7 +898,7 @@ struct Scan {
     const int tid = threadIdx.x;
     const uint64_t *const keys = list_key - warp * room;
     if (units > kScanThreads) {
-      constexpr int kSlots = kScanWarps * (kTopMax + 64) / kScanThreads;
+      constexpr int kSlots = (kScanWarps * (kTopMax + kListSpare) + kScanThreads - 1) / kScanThreads;
       uint64_t k[kSlots];
 #pragma unroll
       for (int j = 0; j < kSlots; ++j) {
@@ -1092,9 +1092,7 @@ struct Scan {
     turn ^= 1;
     if (lane == 0) sh.reach[turn][warp] = reach;
     __syncthreads();
-    float low = INFINITY;
-#pragma unroll
-    for (int w = 0; w < kScanWarps; ++w) low = fminf(low, sh.reach[turn][w]);
+    const float low = least_of(sh.reach[turn]);
     if (low > thr) raise(low);
     const int mine = drop_below(thr > -INFINITY ? (uint64_t)ordered(thr) << 32 : 1, k);
     const int n = emit(k, mine, exact ? K : cap, sh.cand, 0);
@@ -1132,10 +1130,6 @@ struct Scan {
       if (at >= 0) done(at, n);
       if (!more) break;
     }
-    // a copy that did not come in time may still come: not after this CTA's end
-    if (dead)
-      for (; used != issued; ++used)
-        wait_copy(smem_u32(&sh.bar[warp][used % kScanStages]), (used / kScanStages) & 1);
   }
   static __device__ __forceinline__ void cluster_arrive() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
