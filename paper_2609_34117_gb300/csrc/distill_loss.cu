@@ -13,21 +13,26 @@
 // element, set in shared memory before the row is read, takes the list's
 // elements out of the sums.
 //
-// A cluster handles a row.  Each CTA has its part copied into shared memory, in
-// chunks that are all asked for at once, and sums exponentials against a
-// running maximum as they come; one exchange over the cluster gives every CTA
-// the row's sums, and the gradient is computed from shared memory: one read and
-// one write of the row, which bound the kernel.
+// A cluster handles a row.  For the gradient each CTA has its part copied into
+// shared memory, in chunks that are all asked for at once, and sums exponentials
+// against a running maximum as they come; for the loss alone the part passes
+// through registers.  Each warp hands its sums to every CTA of the cluster, by
+// stores that the receivers' mbarriers count (a cluster barrier would wait for
+// the CTA's other memory operations too), each warp then joins all of them with
+// the list by itself, and the gradient is computed from shared memory: one read
+// and one write of the row, which bound the kernel.
 #include "vocab.cuh"
 
 namespace slimwise {
 
 constexpr int kLossThreads = 256;
-constexpr int kLossUnroll = 2;
-constexpr int kChunk = kLossThreads * kLossUnroll;  // windows of a copy (8 KB)
+constexpr int kLossWarps = kLossThreads / 32;
+constexpr int kLossUnroll = 4;
+constexpr int kChunk = kLossThreads * kLossUnroll;  // windows of a step, and of a copy (16 KB)
 constexpr int kSliceMax = 200 * 1024;               // bytes of a row that one CTA may hold
-constexpr int kChunksMax = kSliceMax / (kChunk * 16);
+constexpr int kChunksMax = kSliceMax / (kChunk * 16) + 1;
 static_assert(kTopMax <= kLossThreads, "one thread per list entry");
+static_assert(kClusterMax * kLossWarps <= 64, "two of the cluster's warps a lane");
 
 struct LossArgs {
   const int32_t *labels, *top_ids;
@@ -38,26 +43,22 @@ struct LossArgs {
 };
 
 struct LossShared {
+  float4 part[kClusterMax * kLossWarps];  // each warp's reference, sum for p, sum for q
+  int id[kTopMax];                        // the list: ids (-1: absent), logits, log P and P
+  float z[kTopMax], lp[kTopMax], p[kTopMax];
   uint64_t bar[kChunksMax];
-  float part[kClusterMax][3];  // each CTA's: reference, sum for p, sum for q
-  float red[kLossThreads / 32][5];
+  uint64_t parts;                         // counts the bytes of part
 };
 
-template <int N>
-__device__ __forceinline__ void block_sums(float (&v)[N], LossShared &sh) {
+__device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
+  for (int o = 16; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
-    if ((threadIdx.x & 31) == 0) sh.red[threadIdx.x >> 5][i] = v[i];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v[i] = 0.0f;
-    for (int w = 0; w < kLossThreads / 32; ++w) v[i] += sh.red[w][i];
-  }
-  __syncthreads();
+  for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  return v;
 }
 
 __device__ __forceinline__ void store(float *p, float v) { *p = v; }
@@ -80,23 +81,26 @@ __device__ __forceinline__ uint4 without(uint4 v, uint32_t bits) {
 }
 
 template <typename T>
+__device__ __forceinline__ uint4 packed(const float (&f)[16 / sizeof(T)]) {
+  if constexpr (sizeof(T) == 4) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                      __float_as_uint(f[3]));
+  } else {
+    uint32_t u[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[q]) : "f"(f[2 * q + 1]), "f"(f[2 * q]));
+    return make_uint4(u[0], u[1], u[2], u[3]);
+  }
+}
+
+template <typename T>
 __device__ __forceinline__ void store_window(T *g, const Row<T> &row, int i,
                                              const float (&f)[Row<T>::E]) {
   constexpr int E = Row<T>::E;
   const int id0 = i * E - row.mis;
   if (row.whole(i)) {
-    uint4 v;
-    if constexpr (sizeof(T) == 4) {
-      v = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
-                     __float_as_uint(f[3]));
-    } else {
-      uint32_t u[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[q]) : "f"(f[2 * q + 1]), "f"(f[2 * q]));
-      v = make_uint4(u[0], u[1], u[2], u[3]);
-    }
-    *reinterpret_cast<uint4 *>(g + id0) = v;
+    *reinterpret_cast<uint4 *>(g + id0) = packed<T>(f);
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e)
@@ -106,15 +110,17 @@ __device__ __forceinline__ void store_window(T *g, const Row<T> &row, int i,
 
 // kTemp: tau is not 1, so that p and q are two softmaxes.
 template <typename T, bool kGrad, bool kTemp>
-__global__ void __launch_bounds__(kLossThreads, 4)
+__global__ void __launch_bounds__(kLossThreads, kGrad ? 5 : 6)
     distill_loss_kernel(const T *logits, int64_t stride, LossArgs a, T *grad, int64_t grad_stride) {
   constexpr int E = Row<T>::E;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ LossShared sh;
+  pdl_launch_dependents();
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const int tid = threadIdx.x, V = a.vocab;
+  const int tid = threadIdx.x, lane = tid & 31, V = a.vocab;
   const int64_t t = blockIdx.x / C;
+  const int label = a.labels[t];
   const Row<T> row(logits + t * stride, V);
   const int per = (row.windows + C - 1) / C;
   const int lo = min(rank * per, row.windows), hi = min(lo + per, row.windows);
@@ -122,7 +128,6 @@ __global__ void __launch_bounds__(kLossThreads, 4)
   T *const g = kGrad ? grad + t * grad_stride : nullptr;
   // gradient rows that start like the logits' are written in whole windows
   const bool alike = kGrad && ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(row.p)) & 15) == 0;
-  const int label = a.labels[t];
   if (label < 0) {  // not trained on
     if (rank == 0 && tid == 0) a.row_loss[t] = 0.0f;
     if constexpr (kGrad) {
@@ -135,119 +140,151 @@ __global__ void __launch_bounds__(kLossThreads, 4)
     return;
   }
 
+  // a word of bits for each thread and step: 8 for each of its windows
   uint4 *const slice = reinterpret_cast<uint4 *>(smem);
-  uint32_t *const bits = reinterpret_cast<uint32_t *>(smem + (size_t)per * 16);
+  uint32_t *const bits = reinterpret_cast<uint32_t *>(smem + (kGrad ? (size_t)per * 16 : 0));
   const int chunks = (hi - lo + kChunk - 1) / kChunk;
   if (tid == 0) {
-    for (int i = 0; i < chunks; ++i) mbar_init(smem_u32(&sh.bar[i]), 1);
+    mbar_init(smem_u32(&sh.parts), 1);
+    if constexpr (kGrad)
+      for (int i = 0; i < chunks; ++i) mbar_init(smem_u32(&sh.bar[i]), 1);
     mbar_fence_init();
-    for (int i = 0; i < chunks; ++i) {
-      // the row's partial windows at its ends are left out
-      int first = lo + i * kChunk, end = min(first + kChunk, hi);
-      uint4 *dst = slice + i * kChunk;
-      if (first == 0 && !row.whole(0)) {
-        ++first;
-        ++dst;
+    mbar_arrive_expect_tx(smem_u32(&sh.parts), (uint32_t)(C * kLossWarps * sizeof(float4)));
+    if constexpr (kGrad)
+      for (int i = 0; i < chunks; ++i) {
+        // the row's partial windows at its ends are left out
+        const int at = lo + i * kChunk, from = max(at, row.whole_lo);
+        const int to = min(min(at + kChunk, hi), row.whole_lo + row.whole_n);
+        const uint32_t bytes = to > from ? (uint32_t)(to - from) * 16 : 0;
+        mbar_arrive_expect_tx(smem_u32(&sh.bar[i]), bytes);
+        if (bytes) bulk_load(smem_u32(slice + (from - lo)), row.w + from, bytes, smem_u32(&sh.bar[i]));
       }
-      if (end == row.windows && end > first && !row.whole(end - 1)) --end;
-      const uint32_t bytes = end > first ? (uint32_t)(end - first) * 16 : 0;
-      mbar_arrive_expect_tx(smem_u32(&sh.bar[i]), bytes);
-      if (bytes) bulk_load(smem_u32(dst), row.w + first, bytes, smem_u32(&sh.bar[i]));
-    }
   }
-  for (int i = tid; i < (hi - lo + 3) / 4; i += kLossThreads) bits[i] = 0;
-  const int id = tid < a.K ? a.top_ids[t * a.K + tid] : -1;
-  const float lp = tid < a.K ? a.top_logp[t * a.K + tid] : 0.0f;
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // its mbarrier can be used
+  int id = -1;
+  float lp = 0.0f;
+  if (tid < a.K) {
+    id = a.top_ids[t * a.K + tid];
+    lp = a.top_logp[t * a.K + tid];
+  }
+  for (int i = 0; i < chunks; ++i) bits[i * kLossThreads + tid] = 0;
+  if constexpr (kGrad)
+    for (int i = tid; i < 2; i += kLossThreads) {
+      const int at = i ? row.windows - 1 : 0;
+      if (at >= lo && at < hi && !row.whole(at)) slice[at - lo] = load_window(row, at);
+    }
   const bool bad = __syncthreads_or(id >= V) || label >= V;
-  const bool listed = id >= 0 && !bad;
-  const float z = listed ? to_float(row.p[id]) : -INFINITY;
-  const float zy = to_float(row.p[bad ? 0 : label]);
-  if (listed && id >= id_lo && id < id_hi) {
+  if (bad) id = -1;
+  float z = -INFINITY, zy = 0.0f;
+  if (id >= 0) z = to_float(row.p[id]);
+  if (!bad) zy = to_float(row.p[label]);
+  if (id >= id_lo && id < id_hi) {
     const int i = (id + row.mis) / E - lo;
-    atomicOr(&bits[i >> 2], 1u << ((i & 3) * 8 + (id + row.mis) % E));
+    atomicOr(&bits[i / kChunk * kLossThreads + i % kLossThreads],
+             1u << (i % kChunk / kLossThreads * 8 + (id + row.mis) % E));
   }
   __syncthreads();
 
   // sums of the exponentials outside the list, against the largest so far: s1
   // of 2^((z - ref) c1), and with a temperature s2 of 2^((z - ref) c2)
   const float c1 = kLog2e, c2 = kTemp ? kLog2e / a.tau : kLog2e;
-  const unsigned char *const byte = reinterpret_cast<const unsigned char *>(bits);
   float s1 = 0.0f, s2 = 0.0f, ref = kFloorRef;
   bool came = true;
   for (int b = 0; b < chunks; ++b) {
-    came = came && wait_copy(smem_u32(&sh.bar[b]), 0);
+    if constexpr (kGrad) came = came && wait_copy(smem_u32(&sh.bar[b]), 0);
+    const uint32_t mask = bits[b * kLossThreads + tid];
+    const int i0 = b * kChunk + tid;
     uint4 v[kLossUnroll];
-    float m = -INFINITY;
+    if ((b + 1) * kChunk <= hi - lo) {
 #pragma unroll
-    for (int u = 0; u < kLossUnroll; ++u) {
-      const int i = b * kChunk + u * kLossThreads + tid;
-      const uint32_t none = neg_inf_bits(row.p);
-      v[u] = make_uint4(none, none, none, none);
-      if (lo + i < hi) {
-        if (row.whole(lo + i)) {
-          v[u] = slice[i];
-        } else {
-          v[u] = load_window(row, lo + i);
-          slice[i] = v[u];
-        }
-        const uint32_t mk = byte[i];
-        if (mk) v[u] = without<T>(v[u], mk);
+      for (int u = 0; u < kLossUnroll; ++u)
+        v[u] = kGrad ? slice[i0 + u * kLossThreads] : load_window(row, lo + i0 + u * kLossThreads);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kLossUnroll; ++u) {
+        const int i = i0 + u * kLossThreads;
+        const uint32_t none = neg_inf_bits(row.p);
+        v[u] = make_uint4(none, none, none, none);
+        if (lo + i < hi) v[u] = kGrad ? slice[i] : load_window(row, lo + i);
       }
-      m = fmaxf(m, window_max<T>(v[u]));
     }
-    const float n = fmaxf(ref, m);
-    s1 *= exp_from(ref, n, c1);
-    if constexpr (kTemp) s2 *= exp_from(ref, n, c2);
-    ref = n;
+    if (mask) {
 #pragma unroll
-    for (int u = 0; u < kLossUnroll; ++u) {
-      s1 += window_sum<T>(v[u], c1, ref);
-      if constexpr (kTemp) s2 += window_sum<T>(v[u], c2, ref);
+      for (int u = 0; u < kLossUnroll; ++u) v[u] = without<T>(v[u], mask >> (8 * u) & 0xFFu);
     }
+    const float n = fmaxf(ref, fmaxf(window_max<T>(v[0], v[1]), window_max<T>(v[2], v[3])));
+    s1 = fmaf(s1, exp_from(ref, n, c1), windows_sum<T, kLossUnroll>(v, c1, n));
+    if constexpr (kTemp) s2 = fmaf(s2, exp_from(ref, n, c2), windows_sum<T, kLossUnroll>(v, c2, n));
+    ref = n;
   }
   if (!came) s1 = s2 = NAN;
-  // over the block, then over the cluster
+  // over the warp, then to every CTA of the cluster
   {
-    const float top = block_reduce<kLossThreads>(ref, &sh.red[0][0], OpMax());
-    s1 = block_reduce<kLossThreads>(s1 * exp_from(ref, top, c1), &sh.red[0][0], OpAdd());
-    if constexpr (kTemp)
-      s2 = block_reduce<kLossThreads>(s2 * exp_from(ref, top, c2), &sh.red[0][0], OpAdd());
+    const float top = warp_max(ref);
+    s1 = warp_sum(s1 * exp_from(ref, top, c1));
+    if constexpr (kTemp) s2 = warp_sum(s2 * exp_from(ref, top, c2));
     ref = top;
   }
-  cluster.sync();  // every CTA of the cluster runs
-  if (tid < C) {
-    float *const p = cluster.map_shared_rank(&sh.part[rank][0], tid);
-    p[0] = ref;
-    p[1] = s1;
-    p[2] = s2;
+  if (tid < a.K) {
+    sh.id[tid] = id;
+    sh.z[tid] = z;
+    sh.lp[tid] = lp;
+    sh.p[tid] = id >= 0 ? expf(lp) : 0.0f;
   }
-  const float z_top = block_reduce<kLossThreads>(z, &sh.red[0][0], OpMax());
-  cluster.sync();
-  ref = fmaxf(z_top, kFloorRef);
-  for (int r = 0; r < C; ++r) ref = fmaxf(ref, sh.part[r][0]);
-  float rest1 = 0.0f, rest2 = 0.0f;
-  for (int r = 0; r < C; ++r) {
-    rest1 += sh.part[r][1] * exp_from(sh.part[r][0], ref, c1);
-    if constexpr (kTemp) rest2 += sh.part[r][2] * exp_from(sh.part[r][0], ref, c2);
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (lane < C) {
+    const uint32_t to = mapa_shared(smem_u32(&sh.part[rank * kLossWarps + (tid >> 5)]), lane);
+    asm volatile(
+        "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
+        "f"(ref), "f"(s1), "f"(s2), "f"(0.0f), "r"(mapa_shared(smem_u32(&sh.parts), lane))
+        : "memory");
   }
-  if constexpr (!kTemp) rest2 = rest1;
-  const float e1 = exp_from(z, ref, c1), e2 = kTemp ? exp_from(z, ref, c2) : e1;
-  const float P = listed ? expf(lp) : 0.0f;
-  float sums[3] = {listed ? e1 : 0.0f, listed ? e2 : 0.0f, P};
-  block_sums(sums, sh);
+  __syncthreads();  // the list
+  if (!mbar_wait_cluster_bounded(smem_u32(&sh.parts), 0, nullptr, kDefaultWaitLimitNs)) came = false;
+  const bool lost = !__all_sync(0xFFFFFFFFu, came);
+
+  // the row's sums, by each warp for itself: the parts, and the list
+  float4 part[2];
+  float z_top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int i = lane + 32 * j;
+    part[j] = i < C * kLossWarps ? sh.part[i] : make_float4(kFloorRef, 0.0f, 0.0f, 0.0f);
+    z_top = fmaxf(z_top, part[j].x);
+  }
+  for (int i = lane; i < a.K; i += 32) z_top = fmaxf(z_top, sh.z[i]);
+  ref = fmaxf(warp_max(z_top), kFloorRef);
+  float rest1 = warp_sum(part[0].y * exp_from(part[0].x, ref, c1) + part[1].y * exp_from(part[1].x, ref, c1));
+  float rest2 = rest1;
+  if constexpr (kTemp)
+    rest2 = warp_sum(part[0].z * exp_from(part[0].x, ref, c2) + part[1].z * exp_from(part[1].x, ref, c2));
+  float list1 = 0.0f, list2 = 0.0f, M = 0.0f;
+  bool y_listed = false;
+  for (int i = lane; i < a.K; i += 32) {
+    list1 += exp_from(sh.z[i], ref, c1);
+    if constexpr (kTemp) list2 += exp_from(sh.z[i], ref, c2);
+    M += sh.p[i];
+    y_listed |= sh.id[i] == label;
+  }
+  y_listed = __any_sync(0xFFFFFFFFu, y_listed);
   const float lr = a.log_rest[t], r = expf(lr);
-  const float total1 = bad ? NAN : rest1 + sums[0], total2 = bad ? NAN : kTemp ? rest2 + sums[1] : total1;
-  const float M = sums[2] + r;
+  const float total1 = bad || lost ? NAN : rest1 + warp_sum(list1);
+  const float total2 = kTemp ? (bad || lost ? NAN : rest2 + warp_sum(list2)) : total1;
+  M = warp_sum(M) + r;
   const float w = a.row_weight ? a.row_weight[t] : 1.0f;
   const float beta = (1.0f - a.alpha) * a.tau;
-  if (rank == 0) {
+  if (rank == 0 && tid < 32) {
     const float l2 = log2f(total2);
-    float kl[1] = {P > 0.0f ? P * (lp - ((z - ref) * c2 - l2) * kLn2) : 0.0f};
-    block_sums(kl, sh);
-    if (tid == 0) {
+    float kl = 0.0f;
+    for (int i = lane; i < a.K; i += 32) {
+      const float P = sh.p[i];
+      if (P > 0.0f) kl += P * (sh.lp[i] - ((sh.z[i] - ref) * c2 - l2) * kLn2);
+    }
+    kl = warp_sum(kl);
+    if (lane == 0) {
       const float ce = (log2f(total1) - (zy - ref) * c1) * kLn2;
       const float kr = r > 0.0f ? r * (lr - (log2f(rest2) - l2) * kLn2) : 0.0f;
-      a.row_loss[t] = a.alpha * ce + beta * a.tau * (kl[0] + kr);
+      a.row_loss[t] = a.alpha * ce + beta * a.tau * (kl + kr);
     }
   }
   if constexpr (kGrad) {
@@ -262,37 +299,49 @@ __global__ void __launch_bounds__(kLossThreads, 4)
       return v;
     };
     if (alike) {
-      for (int i = lo + tid; i < hi; i += kLossThreads) {
+      const uint64_t mr = pair(-ref, -ref), cc1 = pair(c1, c1), cc2 = pair(c2, c2);
+      const uint64_t AA = pair(A, A), BB = pair(B, B);
+      auto window = [&](int i, auto put) {
         constexpr int P = E / 2;
         uint64_t p[P];
         unpack_pairs<T>(slice[i - lo], p);
         float f[E];
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-          const uint64_t mr = pair(-ref, -ref);
-          uint64_t v = mul2(pair(A, A), exp2_pair(p[q], mr, pair(c1, c1)));
-          if constexpr (kTemp) v = add2(v, mul2(pair(B, B), exp2_pair(p[q], mr, pair(c2, c2))));
+          uint64_t v = mul2(AA, exp2_pair(p[q], mr, cc1));
+          if constexpr (kTemp) v = add2(v, mul2(BB, exp2_pair(p[q], mr, cc2)));
           split(v, f[2 * q], f[2 * q + 1]);
         }
-        store_window(g, row, i, f);
+        put(f);
+      };
+      const int from = max(lo, row.whole_lo), to = min(hi, row.whole_lo + row.whole_n);
+      uint4 *const gw = reinterpret_cast<uint4 *>(g - row.mis);
+#pragma unroll 4
+      for (int i = from + tid; i < to; i += kLossThreads)
+        window(i, [&](const float (&f)[E]) { gw[i] = packed<T>(f); });
+      // the row's partial windows
+      for (int i = tid; i < 2; i += kLossThreads) {
+        const int at = i ? row.windows - 1 : 0;
+        if (at >= lo && at < hi && !row.whole(at))
+          window(at, [&](const float (&f)[E]) { store_window(g, row, at, f); });
       }
     } else {
-      __syncthreads();
-      const T *const part = reinterpret_cast<const T *>(slice) + row.mis - lo * E;
-      for (int i = id_lo + tid; i < id_hi; i += kLossThreads) store(g + i, outside(to_float(part[i])));
+      const T *const from = reinterpret_cast<const T *>(slice) + row.mis - lo * E;
+      for (int i = id_lo + tid; i < id_hi; i += kLossThreads) store(g + i, outside(to_float(from[i])));
     }
     // then the list's elements and the label
-    const bool y_listed = __syncthreads_or(listed && id == label);
-    if (!bad && listed && id >= id_lo && id < id_hi) {
+    __syncthreads();
+    if (!bad && id >= id_lo && id < id_hi) {
       const float on = id == label ? a.alpha : 0.0f;
-      store(g + id, w * (a.alpha * (e1 / total1) - on + beta * (M * (e2 / total2) - P)));
+      const float e1 = exp_from(z, ref, c1), e2 = kTemp ? exp_from(z, ref, c2) : e1;
+      store(g + id, w * (a.alpha * (e1 / total1) - on + beta * (M * (e2 / total2) - sh.p[tid])));
     }
     if (!bad && tid == 0 && !y_listed && label >= id_lo && label < id_hi)
       store(g + label, outside(zy) - w * a.alpha);
+    // a copy that did not come in time may still come: not after this CTA's end
+    if (lost)
+      for (int b = 0; b < chunks; ++b) wait_copy(smem_u32(&sh.bar[b]), 0);
   }
-  // a copy that did not come in time may still come: not after this CTA's end
-  if (!came)
-    for (int b = 0; b < chunks; ++b) wait_copy(smem_u32(&sh.bar[b]), 0);
 }
 
 // loss = sum of weight x row loss: thread i adds its rows i, i + 1024, ... in
@@ -301,6 +350,7 @@ __global__ void __launch_bounds__(1024)
     loss_sum_kernel(const float *__restrict__ row_loss, const float *__restrict__ row_weight,
                     int rows, float *__restrict__ loss) {
   __shared__ double part[32];
+  pdl_wait_primary();
   double s = 0.0;
   for (int t = threadIdx.x; t < rows; t += 1024)
     s += (double)row_loss[t] * (row_weight ? (double)row_weight[t] : 1.0);
@@ -314,17 +364,28 @@ __global__ void __launch_bounds__(1024)
   }
 }
 
+// CTAs of a row.
+static int grad_ctas(int rows, int windows) {
+  int C = 1;
+  while (C < kClusterMax && (windows > C * 40 * 64 || (rows * C < 608 && windows >= 2 * C * kLossThreads))) C *= 2;
+  return C;
+}
+static int loss_ctas(int rows, int windows) {
+  int C = 1;
+  while (C < kClusterMax && rows * C < 6 * 912 && windows >= 2 * C * kLossThreads) C *= 2;
+  return C;
+}
+
 template <typename T, bool kGrad, bool kTemp>
 static cudaError_t launch(const void *logits, int rows, int64_t stride, const LossArgs &a,
                           void *grad, int64_t grad_stride, cudaStream_t stream) {
   constexpr int E = Row<T>::E;
   const int windows = (a.vocab + 2 * E - 2) / E;  // the most that a row can cover
-  int C = 1;
-  while (C < kClusterMax && (windows > C * 40 * 64 || (rows * C < 608 && windows >= 2 * C * kChunk))) C *= 2;
+  const int C = kGrad ? grad_ctas(rows, windows) : loss_ctas(rows, windows);
   const size_t per = (size_t)(windows + C - 1) / C;
-  const size_t smem = per * 16 + (per + 3) / 4 * 4;
+  const size_t smem = (kGrad ? per * 16 : 0) + (per + kChunk - 1) / kChunk * kLossThreads * 4;
   return launch_clusters(distill_loss_kernel<T, kGrad, kTemp>, rows, C, kLossThreads, smem,
-                         kSliceMax + kSliceMax / 16, stream, static_cast<const T *>(logits),
+                         kSliceMax + (kSliceMax / 16 + kChunk - 1) / kChunk * kLossThreads * 4, stream, static_cast<const T *>(logits),
                          stride, a, static_cast<T *>(grad), grad_stride);
 }
 
@@ -349,8 +410,16 @@ cudaError_t launch_distill_loss(const void *logits, int dtype, int rows, int voc
                         ? launch<__nv_bfloat16>(logits, rows, stride, a, grad, grad_stride, stream)
                         : launch<float>(logits, rows, stride, a, grad, grad_stride, stream);
   if (err != cudaSuccess || !loss) return err;
-  loss_sum_kernel<<<1, 1024, 0, stream>>>(row_loss, row_weight, rows, loss);
-  return cudaGetLastError();
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(1);
+  cfg.blockDim = dim3(1024);
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, loss_sum_kernel, (const float *)row_loss, row_weight, rows, loss);
 }
 
 }  // namespace slimwise
