@@ -29,10 +29,11 @@ constexpr int kLossThreads = 256;
 constexpr int kLossWarps = kLossThreads / 32;
 constexpr int kLossUnroll = 4;
 constexpr int kChunk = kLossThreads * kLossUnroll;  // windows of a step, and of a copy (16 KB)
+constexpr int kGradCtas = 4, kLossCtas = 5;            // CTAs of an SM, with and without gradient
 constexpr int kSliceMax = 200 * 1024;               // bytes of a row that one CTA may hold
 constexpr int kChunksMax = kSliceMax / (kChunk * 16) + 1;
 static_assert(kTopMax <= kLossThreads, "one thread per list entry");
-static_assert(kClusterMax * kLossWarps <= 64, "two of the cluster's warps a lane");
+constexpr int kLaneParts = kClusterMax * kLossWarps / 32;  // of the cluster's warps, a lane's
 
 struct LossArgs {
   const int32_t *labels, *top_ids;
@@ -110,7 +111,7 @@ __device__ __forceinline__ void store_window(T *g, const Row<T> &row, int i,
 
 // kTemp: tau is not 1, so that p and q are two softmaxes.
 template <typename T, bool kGrad, bool kTemp>
-__global__ void __launch_bounds__(kLossThreads, kGrad ? 5 : 6)
+__global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
     distill_loss_kernel(const T *logits, int64_t stride, LossArgs a, T *grad, int64_t grad_stride) {
   constexpr int E = Row<T>::E;
   extern __shared__ __align__(16) unsigned char smem[];
@@ -244,20 +245,24 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? 5 : 6)
   const bool lost = !__all_sync(0xFFFFFFFFu, came);
 
   // the row's sums, by each warp for itself: the parts, and the list
-  float4 part[2];
+  float4 part[kLaneParts];
   float z_top = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < kLaneParts; ++j) {
     const int i = lane + 32 * j;
     part[j] = i < C * kLossWarps ? sh.part[i] : make_float4(kFloorRef, 0.0f, 0.0f, 0.0f);
     z_top = fmaxf(z_top, part[j].x);
   }
   for (int i = lane; i < a.K; i += 32) z_top = fmaxf(z_top, sh.z[i]);
   ref = fmaxf(warp_max(z_top), kFloorRef);
-  float rest1 = warp_sum(part[0].y * exp_from(part[0].x, ref, c1) + part[1].y * exp_from(part[1].x, ref, c1));
-  float rest2 = rest1;
-  if constexpr (kTemp)
-    rest2 = warp_sum(part[0].z * exp_from(part[0].x, ref, c2) + part[1].z * exp_from(part[1].x, ref, c2));
+  float rest1 = 0.0f, rest2 = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kLaneParts; ++j) {
+    rest1 += part[j].y * exp_from(part[j].x, ref, c1);
+    if constexpr (kTemp) rest2 += part[j].z * exp_from(part[j].x, ref, c2);
+  }
+  rest1 = warp_sum(rest1);
+  rest2 = kTemp ? warp_sum(rest2) : rest1;
   float list1 = 0.0f, list2 = 0.0f, M = 0.0f;
   bool y_listed = false;
   for (int i = lane; i < a.K; i += 32) {
@@ -364,16 +369,32 @@ __global__ void __launch_bounds__(1024)
   }
 }
 
-// CTAs of a row.
-static int grad_ctas(int rows, int windows) {
-  int C = 1;
-  while (C < kClusterMax && (windows > C * 40 * 64 || (rows * C < 608 && windows >= 2 * C * kLossThreads))) C *= 2;
-  return C;
+// Shared memory of a CTA that takes `per` windows.
+static size_t loss_smem(int per, bool grad) {
+  return (grad ? (size_t)per * 16 : 0) + (size_t)(per + kChunk - 1) / kChunk * kLossThreads * 4;
 }
-static int loss_ctas(int rows, int windows) {
-  int C = 1;
-  while (C < kClusterMax && rows * C < 6 * 912 && windows >= 2 * C * kLossThreads) C *= 2;
-  return C;
+// CTAs of a row.  With the gradient, the number that lets the CTAs of an SM hold
+// the most of their rows at once: at 131072 bf16, parts of 65 KB three to an SM
+// took 363 us for 4096 rows, 44 KB four 385, 33 KB five 392, 87 KB two 413.  Each
+// CTA also costs its row's exchange: the fewest that come within a few percent.
+// Where few rows leave SMs idle, more.
+static int loss_ctas(int rows, int windows, bool grad) {
+  int best = 1;
+  if (grad) {
+    size_t most = 0;
+    for (int C = 1; C <= kClusterMax; ++C) {
+      const int per = (windows + C - 1) / C;
+      if (per * 16 > kSliceMax) continue;
+      const int ctas = (int)(228 * 1024 / (loss_smem(per, true) + sizeof(LossShared) + 1024));
+      const size_t held = (size_t)(ctas < kGradCtas ? ctas : kGradCtas) * per;
+      if (held > most + most / 32) {
+        most = held;
+        best = C;
+      }
+    }
+  }
+  while (best <= kClusterMax / 2 && rows * best <= 152 && windows >= 2 * best * kLossThreads) best *= 2;
+  return best;
 }
 
 template <typename T, bool kGrad, bool kTemp>
@@ -381,11 +402,10 @@ static cudaError_t launch(const void *logits, int rows, int64_t stride, const Lo
                           void *grad, int64_t grad_stride, cudaStream_t stream) {
   constexpr int E = Row<T>::E;
   const int windows = (a.vocab + 2 * E - 2) / E;  // the most that a row can cover
-  const int C = kGrad ? grad_ctas(rows, windows) : loss_ctas(rows, windows);
-  const size_t per = (size_t)(windows + C - 1) / C;
-  const size_t smem = (kGrad ? per * 16 : 0) + (per + kChunk - 1) / kChunk * kLossThreads * 4;
-  return launch_clusters(distill_loss_kernel<T, kGrad, kTemp>, rows, C, kLossThreads, smem,
-                         kSliceMax + (kSliceMax / 16 + kChunk - 1) / kChunk * kLossThreads * 4, stream, static_cast<const T *>(logits),
+  const int C = loss_ctas(rows, windows, kGrad);
+  return launch_clusters(distill_loss_kernel<T, kGrad, kTemp>, rows, C, kLossThreads,
+                         loss_smem((windows + C - 1) / C, kGrad),
+                         loss_smem(kSliceMax / 16, true), stream, static_cast<const T *>(logits),
                          stride, a, static_cast<T *>(grad), grad_stride);
 }
 
