@@ -428,6 +428,7 @@ def slimwise_moe_noalloc_device_status(stream=None) -> int:
 
 
 _DTYPES = {torch.bfloat16: 0, torch.float32: 1}
+_I32, _F32 = torch.int32, torch.float32
 
 
 def _logits(t, name="logits"):
@@ -441,22 +442,23 @@ def _logits(t, name="logits"):
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
     rows, vocab = t.shape
+    stride, step = t.stride()
     # a dimension of one element has no stride of its own
-    if vocab > 1 and t.stride(1) != 1:
+    if step != 1 and vocab > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return t.data_ptr(), code, rows, vocab, t.stride(0) if rows > 1 else vocab
+    return t.data_ptr(), code, rows, vocab, stride if rows > 1 else vocab
 
 
-def _vec(t, dtype, shape, name, device):
-    """Pointer of an optional contiguous array of the call's rows (None: NULL)."""
-    if t is None:
-        return None
+def _vec(t, dtype, shape, name, index):
+    """Pointer of a contiguous array of the call's rows on device `index`."""
+    # (one pass over a good tensor: these checks are most of a small call's time)
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.get_device() == index and t.is_contiguous()):
+        return t.data_ptr()
     _dev(t, dtype, name)
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be on cuda:{index}")
 
 
 def slimwise_top_logits(logits, k, temperature=1.0, ids=None, logp=None, log_rest=None,
@@ -465,18 +467,17 @@ def slimwise_top_logits(logits, k, temperature=1.0, ids=None, logp=None, log_res
     log-probabilities at a temperature, and the log of the others' mass.
     Returns (ids int32 [rows, k], logp fp32 [rows, k], log_rest fp32 [rows])."""
     row_args = _logits(logits)
-    rows, k, dev = row_args[2], int(k), logits.device
+    rows, k, dev = row_args[2], int(k), logits.get_device()
     if ids is None:
-        ids = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
+        ids = torch.empty((rows, max(k, 0)), dtype=_I32, device=logits.device)
     if logp is None:
-        logp = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=dev)
+        logp = torch.empty((rows, max(k, 0)), dtype=_F32, device=logits.device)
     if log_rest is None:
-        log_rest = torch.empty(rows, dtype=torch.float32, device=dev)
+        log_rest = torch.empty(rows, dtype=_F32, device=logits.device)
     _check(load().slimwise_top_logits(
-        *row_args, k, temperature, _vec(ids, torch.int32, (rows, k), "ids", dev),
-        _vec(logp, torch.float32, (rows, k), "logp", dev),
-        _vec(log_rest, torch.float32, (rows,), "log_rest", dev), _stream(stream)),
-        "slimwise_top_logits")
+        *row_args, k, temperature, _vec(ids, _I32, (rows, k), "ids", dev),
+        _vec(logp, _F32, (rows, k), "logp", dev), _vec(log_rest, _F32, (rows,), "log_rest", dev),
+        _stream(stream)), "slimwise_top_logits")
     return ids, logp, log_rest
 
 
@@ -489,37 +490,35 @@ def slimwise_distill_loss(logits, labels, top_ids, top_logp, log_rest, alpha=0.1
     number of labelled rows; None: 1 each.  Returns (loss fp32 [1], row losses
     fp32 [rows], gradient or None)."""
     row_args = _logits(logits)
-    _, _, rows, vocab, stride = row_args
-    dev, f32 = logits.device, torch.float32
+    _, code, rows, vocab, stride = row_args
+    dev = logits.get_device()
     if not isinstance(top_ids, torch.Tensor) or top_ids.dim() != 2:
         raise ValueError("top_ids must have two dimensions")
     k = top_ids.shape[1]
-    g_ptr, g_stride = None, 0
+    one, many = (rows,), (rows, k)
+    p_labels = _vec(labels, _I32, one, "labels", dev)
+    p_ids = _vec(top_ids, _I32, many, "top_ids", dev)
+    p_logp = _vec(top_logp, _F32, many, "top_logp", dev)
+    p_rest = _vec(log_rest, _F32, one, "log_rest", dev)
+    p_weight = None if row_weight is None else _vec(row_weight, _F32, one, "row_weight", dev)
     if grad is True:
-        grad = torch.empty((rows, stride), dtype=logits.dtype, device=dev)[:, :vocab]
+        grad = torch.empty_strided((rows, vocab), (stride, 1), dtype=logits.dtype,
+                                   device=logits.device)
         g_ptr, g_stride = grad.data_ptr(), stride
     elif grad is False or grad is None:
-        grad = None
+        grad, g_ptr, g_stride = None, None, 0
     else:
-        g_ptr, code, g_rows, g_vocab, g_stride = _logits(grad, "grad")
-        if code != row_args[1] or (g_rows, g_vocab) != (rows, vocab) or grad.device != dev:
+        g_ptr, g_code, g_rows, g_vocab, g_stride = _logits(grad, "grad")
+        if g_code != code or (g_rows, g_vocab) != (rows, vocab) or grad.get_device() != dev:
             raise ValueError("grad must have the logits' type, shape and device")
     if row_loss is None:
-        row_loss = torch.empty(rows, dtype=f32, device=dev)
+        row_loss = torch.empty(rows, dtype=_F32, device=logits.device)
     if loss is None:
         # the sum over no rows is not computed by a kernel
-        loss = torch.empty(1, dtype=f32, device=dev) if rows else torch.zeros(1, dtype=f32, device=dev)
-    for t, name in ((labels, "labels"), (top_ids, "top_ids"), (top_logp, "top_logp"),
-                    (log_rest, "log_rest")):
-        if t is None:
-            raise TypeError(f"{name} must be a CUDA tensor")
+        loss = (torch.empty if rows else torch.zeros)(1, dtype=_F32, device=logits.device)
     _check(load().slimwise_distill_loss(
-        *row_args, _vec(labels, torch.int32, (rows,), "labels", dev),
-        _vec(top_ids, torch.int32, (rows, k), "top_ids", dev),
-        _vec(top_logp, f32, (rows, k), "top_logp", dev),
-        _vec(log_rest, f32, (rows,), "log_rest", dev), k, alpha, temperature,
-        _vec(row_weight, f32, (rows,), "row_weight", dev),
-        _vec(row_loss, f32, (rows,), "row_loss", dev), _vec(loss, f32, (1,), "loss", dev),
+        *row_args, p_labels, p_ids, p_logp, p_rest, k, alpha, temperature, p_weight,
+        _vec(row_loss, _F32, one, "row_loss", dev), _vec(loss, _F32, (1,), "loss", dev),
         g_ptr, g_stride, _stream(stream)), "slimwise_distill_loss")
     return loss, row_loss, grad
 
@@ -531,18 +530,17 @@ def slimwise_sample(logits, uniform, temperature=None, top_k=None, top_p=None, m
     the rows' requests; None: 1, 1, 0 and all.  Temperature 0 takes the largest
     logit.  Returns (tokens int32 [rows], log of each token's share fp32 [rows])."""
     row_args = _logits(logits)
-    rows, dev, f32 = row_args[2], logits.device, torch.float32
-    if uniform is None:
-        raise TypeError("uniform must be a CUDA tensor")
+    rows, dev = row_args[2], logits.get_device()
+    one = (rows,)
     if tokens is None:
-        tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+        tokens = torch.empty(rows, dtype=_I32, device=logits.device)
     if logprob is None:
-        logprob = torch.empty(rows, dtype=f32, device=dev)
-    shape = (rows,)
+        logprob = torch.empty(rows, dtype=_F32, device=logits.device)
     _check(load().slimwise_sample(
-        *row_args, _vec(temperature, f32, shape, "temperature", dev),
-        _vec(top_k, torch.int32, shape, "top_k", dev), _vec(top_p, f32, shape, "top_p", dev),
-        _vec(min_p, f32, shape, "min_p", dev), _vec(uniform, f32, shape, "uniform", dev),
-        _vec(tokens, torch.int32, shape, "tokens", dev), _vec(logprob, f32, shape, "logprob", dev),
-        _stream(stream)), "slimwise_sample")
+        *row_args, None if temperature is None else _vec(temperature, _F32, one, "temperature", dev),
+        None if top_k is None else _vec(top_k, _I32, one, "top_k", dev),
+        None if top_p is None else _vec(top_p, _F32, one, "top_p", dev),
+        None if min_p is None else _vec(min_p, _F32, one, "min_p", dev),
+        _vec(uniform, _F32, one, "uniform", dev), _vec(tokens, _I32, one, "tokens", dev),
+        _vec(logprob, _F32, one, "logprob", dev), _stream(stream)), "slimwise_sample")
     return tokens, logprob

@@ -403,7 +403,7 @@ static cudaError_t launch(const void *logits, int rows, int64_t stride, const Lo
   constexpr int E = Row<T>::E;
   const int windows = (a.vocab + 2 * E - 2) / E;  // the most that a row can cover
   const int C = loss_ctas(rows, windows, kGrad);
-  return launch_clusters(distill_loss_kernel<T, kGrad, kTemp>, rows, C, kLossThreads,
+  return launch_clusters<distill_loss_kernel<T, kGrad, kTemp>>(rows, C, kLossThreads,
                          loss_smem((windows + C - 1) / C, kGrad),
                          loss_smem(kSliceMax / 16, true), stream, static_cast<const T *>(logits),
                          stride, a, static_cast<T *>(grad), grad_stride);

@@ -441,7 +441,7 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
                           float *logprob, cudaStream_t stream) {
   const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleCtas);
   const int K_most = top_k ? kTopKListed : kNucleus;
-  return launch_clusters(sample_kernel<T>, g.clusters, g.C, kScanThreads,
+  return launch_clusters<sample_kernel<T>>(g.clusters, g.C, kScanThreads,
                          sizeof(SampleShared) + scan_smem(K_most, g.C),
                          sizeof(SampleShared) + scan_smem(kTopKListed, kClusterMax), stream,
                          static_cast<const T *>(logits), stride, rows, vocab, K_most, temperature,

@@ -94,7 +94,7 @@ static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t s
                               float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
   const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kTopCtas);
-  return launch_clusters(top_logits_kernel<T>, g.clusters, g.C, kScanThreads, scan_smem(k, g.C),
+  return launch_clusters<top_logits_kernel<T>>(g.clusters, g.C, kScanThreads, scan_smem(k, g.C),
                          scan_smem(kTopMax, kClusterMax), stream,
                          static_cast<const T *>(logits), stride, rows, vocab, k,
                          kLog2e / temperature, ids, logp, log_rest);

@@ -11,6 +11,8 @@
 // maximum nor a sum of exponentials sees.
 #pragma once
 
+#include <atomic>
+
 #include <cooperative_groups.h>
 #include <float.h>
 #include <cuda_bf16.h>
@@ -30,14 +32,23 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFloorRef = -FLT_MAX;
 
 // Launches `clusters` clusters of C CTAs.  smem_max: the kernel's shared-memory
-// attribute, one value per kernel; smem: this launch's.
-template <typename K, typename... A>
-inline cudaError_t launch_clusters(K kernel, int clusters, int C, int threads, size_t smem,
-                                   size_t smem_max, cudaStream_t stream, A... args) {
-  cudaError_t err = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel),
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)smem_max);
+// attribute, one value per kernel, set on its first launch on a device and again
+// after a launch that failed (a context that was reset has lost it); smem: this
+// launch's.
+template <auto kKernel, typename... A>
+inline cudaError_t launch_clusters(int clusters, int C, int threads, size_t smem, size_t smem_max,
+                                   cudaStream_t stream, A... args) {
+  static std::atomic<uint64_t> ready{0};  // a bit for each device
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
   if (err != cudaSuccess) return err;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(ready.load(std::memory_order_acquire) & bit)) {
+    err = cudaFuncSetAttribute(reinterpret_cast<const void *>(kKernel),
+                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
+    if (err != cudaSuccess) return err;
+    ready.fetch_or(bit, std::memory_order_release);
+  }
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)C;
@@ -50,7 +61,9 @@ inline cudaError_t launch_clusters(K kernel, int clusters, int C, int threads, s
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
+  err = cudaLaunchKernelEx(&cfg, kKernel, args...);
+  if (err != cudaSuccess) ready.fetch_and(~bit, std::memory_order_release);
+  return err;
 }
 
 cudaError_t launch_top_logits(const void *logits, int dtype, int rows, int vocab, int64_t stride,
