@@ -24,7 +24,7 @@
 
 namespace slimwise {
 
-constexpr int kSampleCtas = 4;    // CTAs of an SM
+constexpr int kSampleCtas = 3;    // CTAs of an SM
 constexpr int kNucleus = 64;      // elements looked at for a nucleus or min-p without top-k
 constexpr int kTopKListed = 128;  // largest top-k that is decided from the list
 constexpr int32_t kLeftOver = -2; // a token that is still to be searched (its logprob: the maximum)
@@ -353,7 +353,7 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
   return kDone;
 }
 
-template <typename T>
+template <typename T, bool kCluster>
 __global__ void __launch_bounds__(kScanThreads, kSampleCtas)
     sample_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int K_most,
                   const float *__restrict__ temperature, const int32_t *__restrict__ top_k,
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kScanThreads, kSampleCtas)
   SampleShared &sm = *reinterpret_cast<SampleShared *>(smem);
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem + sizeof(SampleShared));
   const int tid = threadIdx.x;
-  Scan<T> scan(sh, K_most, logits, stride, vocab, rows);
+  Scan<T, kCluster> scan(sh, K_most, logits, stride, vocab, rows);
   // the row's request; false if it is out of range
   auto request_of = [&](int t, Draw &d, int &K) {
     const float temp = temperature ? temperature[t] : 1.0f;
@@ -439,13 +439,18 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
                           const float *temperature, const int32_t *top_k, const float *top_p,
                           const float *min_p, const float *uniform, int32_t *tokens,
                           float *logprob, cudaStream_t stream) {
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleCtas);
   const int K_most = top_k ? kTopKListed : kNucleus;
-  return launch_clusters<sample_kernel<T>>(g.clusters, g.C, kScanThreads,
-                         sizeof(SampleShared) + scan_smem(K_most, g.C),
-                         sizeof(SampleShared) + scan_smem(kTopKListed, kClusterMax), stream,
-                         static_cast<const T *>(logits), stride, rows, vocab, K_most, temperature,
-                         top_k, top_p, min_p, uniform, tokens, logprob);
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), K_most, kSampleCtas, sizeof(SampleShared));
+  const auto launch = g.C > 1 ? launch_clusters<sample_kernel<T, true>, const T *, int64_t, int, int, int,
+                                                const float *, const int32_t *, const float *,
+                                                const float *, const float *, int32_t *, float *>
+                              : launch_clusters<sample_kernel<T, false>, const T *, int64_t, int, int, int,
+                                                const float *, const int32_t *, const float *,
+                                                const float *, const float *, int32_t *, float *>;
+  return launch(g.clusters, g.C, kScanThreads, sizeof(SampleShared) + scan_smem(K_most, g.C),
+                sizeof(SampleShared) + scan_smem(kTopKListed, kClusterMax), stream,
+                static_cast<const T *>(logits), stride, rows, vocab, K_most, temperature, top_k,
+                top_p, min_p, uniform, tokens, logprob);
 }
 
 cudaError_t launch_sample(const void *logits, int dtype, int rows, int vocab, int64_t stride,

@@ -14,11 +14,7 @@
 namespace slimwise {
 
 constexpr int kTopCtas = 4;  // CTAs of an SM
-// A CTA's time for a row, in cycles: for each of its windows, and besides (the
-// thresholds, the candidates, the row's end).
-constexpr double kWindowCycles = 2.0, kRowCycles = 20000.0;
-
-template <typename T>
+template <typename T, bool kCluster>
 __global__ void __launch_bounds__(kScanThreads, kTopCtas)
     top_logits_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int K,
                       float c, int32_t *__restrict__ ids, float *__restrict__ logp,
@@ -26,7 +22,7 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   extern __shared__ __align__(128) unsigned char smem[];
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem);
   const int tid = threadIdx.x;
-  Scan<T> scan(sh, K, logits, stride, vocab, rows);
+  Scan<T, kCluster> scan(sh, K, logits, stride, vocab, rows);
   auto request = [&](int, int &k, float &cc) {
     k = K;
     cc = c;
@@ -72,32 +68,28 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   });
 }
 
-ScanGrid scan_grid(int rows, int vocab, int element_bytes, int ctas_per_sm) {
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int K, int ctas_per_sm,
+                   size_t more_smem) {
   const int windows = (int)(((int64_t)vocab * element_bytes + 15) / 16) + 1;
-  const int slots = 152 * ctas_per_sm;
-  ScanGrid best = {1, 1};
-  double least = 0.0;
-  for (int C = 1; C <= kClusterMax; C *= 2) {
-    const int at_once = slots / C, clusters = rows < at_once ? rows : at_once;
-    const int rounds = (rows + clusters - 1) / clusters;
-    const double time = rounds * (kWindowCycles * windows / C + kRowCycles);
-    if (C == 1 || time < least) {
-      best = {C, clusters};
-      least = time;
-    }
-  }
-  return best;
+  int C = 1;
+  while (C < kClusterMax && rows * C <= 128 && windows >= 2 * C * 2 * kScanWarps * kWarpStep) C *= 2;
+  const int fit = (int)(228 * 1024 / (scan_smem(K, C) + more_smem + 1024));
+  const int at_once = 152 * (fit < ctas_per_sm ? fit : ctas_per_sm) / C;
+  return {C, rows < at_once ? rows : at_once};
 }
 
 template <typename T>
 static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t stride, int k,
                               float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kTopCtas);
-  return launch_clusters<top_logits_kernel<T>>(g.clusters, g.C, kScanThreads, scan_smem(k, g.C),
-                         scan_smem(kTopMax, kClusterMax), stream,
-                         static_cast<const T *>(logits), stride, rows, vocab, k,
-                         kLog2e / temperature, ids, logp, log_rest);
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), k, kTopCtas, 0);
+  const auto launch = g.C > 1 ? launch_clusters<top_logits_kernel<T, true>, const T *, int64_t, int, int, int,
+                                                float, int32_t *, float *, float *>
+                              : launch_clusters<top_logits_kernel<T, false>, const T *, int64_t, int, int, int,
+                                                float, int32_t *, float *, float *>;
+  return launch(g.clusters, g.C, kScanThreads, scan_smem(k, g.C), scan_smem(kTopMax, kClusterMax),
+                stream, static_cast<const T *>(logits), stride, rows, vocab, k,
+                kLog2e / temperature, ids, logp, log_rest);
 }
 
 cudaError_t launch_top_logits(const void *logits, int dtype, int rows, int vocab, int64_t stride,

@@ -79,12 +79,14 @@ cudaError_t launch_distill_loss(const void *logits, int dtype, int rows, int voc
                                 float temperature, const float *row_weight, float *row_loss,
                                 float *loss, void *grad, int64_t grad_stride, cudaStream_t stream);
 
-// How a scan is launched: CTAs of a cluster (a row is split over them), and
-// clusters, each of which takes every clusters-th row.
+// How a scan for the K largest is launched: CTAs of a cluster (a row is split
+// over them), and clusters, each of which takes every clusters-th row.
+// ctas_per_sm: what the kernel's registers allow; more_smem: the kernel's shared
+// memory besides the scan's.
 struct ScanGrid {
   int C, clusters;
 };
-ScanGrid scan_grid(int rows, int vocab, int element_bytes, int ctas_per_sm);
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int K, int ctas_per_sm, size_t more_smem);
 
 #if defined(__CUDACC__)
 namespace cg = cooperative_groups;
@@ -329,12 +331,12 @@ struct OpMax {
 //
 // The row is cut into one run for each warp of the cluster, and a run into units
 // of four windows (64 bytes), one a lane in each step.  Each thread keeps the
-// largest element of two groups of its windows.  If m = K / 8 groups of each
-// warp of a CTA reach a value, K elements do, so the least over the warps of
-// each one's m-th largest group bounds the K-th largest element from below.
-// With many more groups than K it is near it, however long the row: about 100
-// elements lie above it for K = 64.  It costs a warp a bisection with ballots
-// and the CTA one barrier, after the 1st, 4th, 16th, ... step and the last.  A
+// largest element of its windows (for K > 96, of two groups of them).  If m =
+// K / 8 groups of each warp of a CTA reach a value, K elements do, so the least
+// over the warps of each one's m-th largest group bounds the K-th largest
+// element from below.  With many more groups than K it is near it, however long
+// the row: about 100 elements lie above it for K = 64.  It costs a warp m
+// reductions and the CTA one barrier, after the 2nd, 8th, 32nd, ... step and the last.  A
 // unit whose maximum reaches the threshold is listed with its sum; any other
 // only adds its sum to the thread's.
 //
@@ -366,7 +368,7 @@ static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
 // than this (else the K best alone).  A power of two.
 __host__ __device__ inline int candidate_cap(int K) { return K <= 8 ? 64 : K <= 32 ? 128 : kTopMax; }
 // Units that a warp's list has room for: K (64 at least), and what a threshold
-// of the 4th step lists until the 16th.
+// of the 8th step lists until the 32nd.
 constexpr int kListSpare = 112;
 __host__ __device__ inline int list_room(int K) { return (K <= 64 ? 64 : (K + 31) / 32 * 32) + kListSpare; }
 
@@ -503,29 +505,29 @@ __device__ __forceinline__ int block_prefix(int v, int &total, ScanShared &sh) {
   return before + incl - v;
 }
 
+// The m-th largest of the warp's values, for small m: the largest taken away in
+// turn.  At least `low` (a value known to be reached by as many, or -inf).
+__device__ __forceinline__ float warp_mth(float a, int m, float low) {
+  uint32_t o = ordered(a);
+  while (true) {
+    const uint32_t h = __reduce_max_sync(0xFFFFFFFFu, o);
+    const bool top = o == h;
+    m -= __popc(__ballot_sync(0xFFFFFFFFu, top));
+    if (m <= 0) return fmaxf(low, unordered(h));
+    if (h <= ordered(-INFINITY)) return low;
+    if (top) o = 0;
+  }
+}
+
 // A value that at least m of the warp's 2 x 32 values a, b reach, and few more;
 // -inf if fewer than m are above -inf.  `low`: a value that is known to be
-// reached by as many, or -inf.  For larger m, bisection over the order of the values' bits,
+// reached by as many, or -inf.  Bisection over the order of the values' bits,
 // which masked logits of the type's lowest value do not stretch as they would
 // the range of the values, down to steps of `grain` bits.
 __device__ __forceinline__ float warp_reach(float a, float b, int m, float low, uint32_t grain) {
   const uint32_t all = 0xFFFFFFFFu;
   const uint32_t oa = ordered(a), ob = ordered(b), none = ordered(-INFINITY);
   auto count = [&](uint32_t x) { return __popc(__ballot_sync(all, oa >= x)) + __popc(__ballot_sync(all, ob >= x)); };
-  if (m <= 12) {
-    // the m-th largest itself, taking away the largest in turn
-    uint32_t first = max(oa, ob), second = min(oa, ob);
-    while (true) {
-      const uint32_t h = __reduce_max_sync(all, first);
-      if (h <= none) return low;
-      m -= __popc(__ballot_sync(all, first == h)) + __popc(__ballot_sync(all, second == h));
-      if (m <= 0) return fmaxf(low, unordered(h));
-      if (first == h) {
-        first = second == h ? 0 : second;
-        second = 0;
-      }
-    }
-  }
   uint32_t lo, hi = __reduce_max_sync(all, max(oa, ob));
   if (low > -INFINITY) {
     lo = ordered(low);
@@ -552,7 +554,8 @@ __device__ __forceinline__ int candidate_lanes(int n) {
   return n <= 32 ? 8 : n <= 64 ? 4 : n <= 128 ? 2 : 1;
 }
 
-template <typename T>
+// kCluster: rows are split over the CTAs of a cluster (else the cluster is one CTA).
+template <typename T, bool kCluster>
 struct Scan {
   static constexpr int E = Row<T>::E;
   static constexpr uint32_t kGrain = sizeof(T) == 2 ? 0xFFFFu : 0x1FFFu;  // a bf16's step; 2^-10 of an fp32
@@ -586,9 +589,14 @@ struct Scan {
   // K_most: the largest K of all rows
   __device__ __forceinline__ Scan(ScanShared &shared, int K_most, const T *z, int64_t st, int V, int n)
       : sh(shared), logits(z), stride(st), vocab(V), rows(n) {
-    cg::cluster_group cluster = cg::this_cluster();
-    C = (int)cluster.num_blocks();
-    rank = (int)cluster.block_rank();
+    if constexpr (kCluster) {
+      cg::cluster_group cluster = cg::this_cluster();
+      C = (int)cluster.num_blocks();
+      rank = (int)cluster.block_rank();
+    } else {
+      C = 1;
+      rank = 0;
+    }
     clusters = (int)gridDim.x / C;
     log_parts = 31 - __clz(C * kScanWarps);
     lane = threadIdx.x & 31;
@@ -606,7 +614,7 @@ struct Scan {
     next_t = (int)(blockIdx.x / C);
     next_row();
     for (int i = 0; i < kScanStages; ++i) issue();
-    if (C > 1) cluster_arrive();  // every CTA runs before another writes to its shared memory
+    if constexpr (kCluster) cluster_arrive();  // every CTA runs before another writes to its shared memory
   }
   __device__ __forceinline__ Row<T> row_of(int t) const {
     return Row<T>(logits + (int64_t)t * stride, vocab);
@@ -680,7 +688,8 @@ struct Scan {
   // Raises the threshold to what the groups of all warps show, and drops the
   // listed windows below it.
   __device__ __forceinline__ void refresh() {
-    const float reach = warp_reach(top0, top1, (K + kScanWarps - 1) / kScanWarps, thr, kGrain);
+    const int m = (K + kScanWarps - 1) / kScanWarps;
+    const float reach = m <= 12 ? warp_mth(fmaxf(top0, top1), m, thr) : warp_reach(top0, top1, m, thr, kGrain);
     turn ^= 1;
     if (lane == 0) {
       sh.reach[turn][warp] = reach;
@@ -784,7 +793,7 @@ struct Scan {
     ref = kFloorRef;
     s = lost = 0.0f;
     listed = 0;
-    int refresh_at = 0;
+    int refresh_at = 1;
     // a lane's windows are read in an order that keeps 8 lanes off each other's banks
     const int turned = lane >> 1;
     for (int step = 0; step < steps; ++step) {
@@ -842,40 +851,48 @@ struct Scan {
   __device__ __forceinline__ int candidates(int t, uint64_t *dst, int cap, int fill) {
     const Row<T> row = row_of(t);
     const int most = exact ? K : cap;
-    // a lane for each window of this warp's units; a warp's candidates are held
-    // until it is known where they go (if they are too many to hold, the windows
-    // are read again, from L1)
+    // The windows of this warp's units that reach, a lane each, noted where the
+    // units' sums were, which are not needed any more; then the elements of those
+    // windows, a lane each.  A warp's candidates are held until it is known where
+    // they go (if they are too many to hold, the elements are read again).
+    int *const hit_list = reinterpret_cast<int *>(list_sum);
     const int windows = listed * kUnit;
     float add = 0.0f;
-    int held = 0;
-    auto pass = [&](auto put, float &sum) {
+    int hits = 0, held = 0;
 #pragma unroll 2
-      for (int base = 0; base < windows; base += 32) {
+    for (int base = 0; base < windows; base += 32) {
+      const int i = base + lane;
+      const int at = i < windows ? (int)key_index(list_key[i / kUnit]) + i % kUnit : row.windows;
+      const uint32_t none = neg_inf_bits(row.p);
+      uint4 v = make_uint4(none, none, none, none);
+      if (at < row.windows) v = load_window(row, at);
+      const bool hit = at < row.windows && window_max<T>(v) >= thr;
+      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, hit);
+      const int to = hits + __popc(mask & ((1u << lane) - 1u));
+      if (hit && to < room) hit_list[to] = at;
+      if (!hit) add += window_sum<T>(v, c, ref);
+      hits += __popc(mask);
+    }
+    __syncwarp();
+    auto pass = [&](auto put, float &sum) {
+      const int elements = hits <= room ? hits * E : 0;
+#pragma unroll 2
+      for (int base = 0; base < elements; base += 32) {
         const int i = base + lane;
-        const int at = i < windows ? (int)key_index(list_key[i / kUnit]) + i % kUnit : row.windows;
-        const uint32_t none = neg_inf_bits(row.p);
-        uint4 v = make_uint4(none, none, none, none);
-        if (at < row.windows) v = load_window(row, at);
-        float z[E];
-        unpack<T>(v, z);
-        const int id0 = at * E - row.mis;
-        float sums = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          // what lies outside the row is -inf, and no candidate below a threshold of -inf
-          const bool yes = z[e] >= thr && (thr > -INFINITY || (id0 + e >= 0 && id0 + e < vocab && at < row.windows));
-          const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
-          if (mask) put(mask, yes, z[e], id0 + e);
-          sums += exp_from(yes ? -INFINITY : z[e], ref, c);
-        }
-        sum += sums;
+        const int id = i < elements ? hit_list[i / E] * E - row.mis + i % E : -1;
+        const bool in = id >= 0 && id < vocab;
+        const float z = in ? to_float(row.p[id]) : 0.0f;
+        const bool yes = in && z >= thr;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+        if (yes) put(__popc(mask & ((1u << lane) - 1u)), z, id);
+        else if (in) sum += exp_from(z, ref, c);
+        held += __popc(mask);
       }
     };
-    pass([&](uint32_t mask, bool yes, float z, int id) {
-      const int at = held + __popc(mask & ((1u << lane) - 1u));
-      if (yes && at < kStage) sh.stage[warp][at] = make_key(z, (uint32_t)id);
-      held += __popc(mask);
+    pass([&](int at, float z, int id) {
+      if (held + at < kStage) sh.stage[warp][held + at] = make_key(z, (uint32_t)id);
     }, add);
+    if (hits > room) held = 1 << 20;  // too many to note: too many in all
     turn ^= 1;
     if (lane == 0) {
       sh.part[turn][warp] = held;
@@ -890,14 +907,13 @@ struct Scan {
       units += sh.count[w];
     }
     if (total > most) return most_of_many(row, dst, most, fill, units);
+    s += add;
     if (held <= kStage) {
-      s += add;
       if (lane < held) dst[before + lane] = sh.stage[warp][lane];
     } else {
-      pass([&](uint32_t mask, bool yes, float z, int id) {
-        if (yes) dst[before + __popc(mask & ((1u << lane) - 1u))] = make_key(z, (uint32_t)id);
-        before += __popc(mask);
-      }, s);
+      held = 0;
+      float again = 0.0f;
+      pass([&](int at, float z, int id) { dst[before + held + at] = make_key(z, (uint32_t)id); }, again);
     }
     for (int i = total + (int)threadIdx.x; i < fill; i += kScanThreads) dst[i] = 0;
     return total;
@@ -925,8 +941,11 @@ struct Scan {
       for (int base = 0; base < listed; base += 32) {
         const int i = base + lane;
         const uint64_t key = i < listed ? list_key[i] : 0;
-        const float ws = i < listed ? list_sum[i] : 0.0f;
-        out = keep(key, ws, key && key >= low, out);
+        if (key && key < low)
+          for (int u = 0; u < kUnit; ++u)
+            if ((int)key_index(key) + u < row.windows)
+              s += window_sum<T>(load_window(row, (int)key_index(key) + u), c, ref);
+        out = keep(key, 0.0f, key && key >= low, out);
       }
       listed = out;
       if (lane == 0) sh.count[warp] = listed;
@@ -1101,7 +1120,9 @@ struct Scan {
       if (k[j]) most = fmaxf(most, key_value(k[j]));
     }
     // the threads' largest show a threshold too
-    const float reach = warp_reach(most, -INFINITY, (K + kScanWarps - 1) / kScanWarps, -INFINITY, kGrain);
+    const float reach = (K + kScanWarps - 1) / kScanWarps <= 12
+                            ? warp_mth(most, (K + kScanWarps - 1) / kScanWarps, -INFINITY)
+                            : warp_reach(most, -INFINITY, (K + kScanWarps - 1) / kScanWarps, -INFINITY, kGrain);
     turn ^= 1;
     if (lane == 0) sh.reach[turn][warp] = reach;
     __syncthreads();
@@ -1125,7 +1146,7 @@ struct Scan {
         request(t, k, cc);
         scan(t, k, cc);
       }
-      if (C == 1) {
+      if constexpr (!kCluster) {
         if (more) {
           n = candidates(t, sh.cand, candidate_cap(K), 0);
           __syncthreads();
