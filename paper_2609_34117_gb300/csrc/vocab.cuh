@@ -359,7 +359,8 @@ constexpr int kScanWarps = kScanThreads / 32;
 constexpr int kUnit = 4;                      // windows of a unit
 constexpr int kWarpStep = 32 * kUnit;         // windows of a warp in a step
 constexpr int kScanStages = 2;
-static_assert(kScanStages == 2, "a stage's number is one bit");
+constexpr uint32_t kStageBytes = kWarpStep * 16;
+static_assert(kScanStages == 2, "the stage at hand is the one or the other");
 constexpr int kClusterMax = 8;
 constexpr int kStage = 32;
 static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
@@ -369,10 +370,18 @@ static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
 __host__ __device__ inline int candidate_cap(int K) { return K <= 8 ? 64 : K <= 32 ? 128 : kTopMax; }
 // Units that a warp's list has room for: K (64 at least), and what a threshold
 // of the 8th step lists until the 32nd.
-constexpr int kListSpare = 112;
+constexpr int kListSpare = 80;
 __host__ __device__ inline int list_room(int K) { return (K <= 64 ? 64 : (K + 31) / 32 * 32) + kListSpare; }
+// A listed unit: its key (maximum, index of its first window), its sum of
+// 2^((z - maximum) c), and, by the time its sum is not needed any more, a window
+// that reaches the threshold (not necessarily its own).
+struct alignas(16) Listed {
+  uint64_t key;
+  float sum;
+  int window;
+};
 
-struct ScanShared {
+struct alignas(128) ScanShared {
   uint4 ring[kScanWarps][kScanStages][kWarpStep];
   uint64_t cand[kTopMax];
   uint64_t red64[kScanWarps];
@@ -391,13 +400,12 @@ struct ScanShared {
   int sel_digit, sel_above, sel_bin;
   float part_sum[2][kClusterMax], part_thr[2][kClusterMax];  // at a row's leader: each CTA's
   int part_exact[2][kClusterMax];
-  // then  uint64_t [warps][room]   listed units' keys (maximum, index of the first window)
-  //       float [warps][room]      and their sums of 2^((z - maximum) c)
+  // then  Listed [warps][room]
   //       uint64_t [cluster][cap]  in clusters, at a row's leader: each CTA's
   //                                candidates (in clusters of two, two of these)
 };
 inline size_t scan_smem(int K, int C) {
-  return sizeof(ScanShared) + (size_t)kScanWarps * list_room(K) * 12 +
+  return sizeof(ScanShared) + (size_t)kScanWarps * list_room(K) * sizeof(Listed) +
          (C > 1 ? (size_t)(C > 4 ? C : 4) * candidate_cap(K) * 8 : 0);
 }
 
@@ -560,8 +568,7 @@ struct Scan {
   static constexpr int E = Row<T>::E;
   static constexpr uint32_t kGrain = sizeof(T) == 2 ? 0xFFFFu : 0x1FFFu;  // a bf16's step; 2^-10 of an fp32
   ScanShared &sh;
-  uint64_t *list_key;  // this warp's
-  float *list_sum;
+  Listed *list;        // this warp's
   uint64_t *recv;
   int room, recv_cap;  // of a warp's list; of a CTA's part of recv
   const T *logits;
@@ -574,8 +581,8 @@ struct Scan {
   // window is the next_i-th of next_n to copy
   int next_t, next_left, next_i, next_n;
   const uint4 *next_src;
-  uint32_t ring;                // this lane's place in the ring's first stage
-  int issue_stage, stage;       // that is copied and read next
+  uint32_t put_at, get_at;      // this lane's places in the ring's first stage
+  uint32_t stage;               // offset of the stage that is read next, and then copied
   // the row at hand
   int K;
   float c, thr;                 // scale of the exponents (log2 e / temperature); threshold
@@ -603,13 +610,13 @@ struct Scan {
     warp = threadIdx.x >> 5;
     room = list_room(K_most);
     recv_cap = candidate_cap(K_most);
-    uint64_t *const keys = reinterpret_cast<uint64_t *>(&sh + 1);
-    float *const sums = reinterpret_cast<float *>(keys + kScanWarps * room);
-    list_key = keys + warp * room;
-    list_sum = sums + warp * room;
-    recv = reinterpret_cast<uint64_t *>(sums + kScanWarps * room);
-    ring = smem_u32(&sh.ring[warp][0][lane]);
-    issue_stage = stage = 0;
+    Listed *const lists = reinterpret_cast<Listed *>(&sh + 1);
+    list = lists + warp * room;
+    recv = reinterpret_cast<uint64_t *>(lists + kScanWarps * room);
+    put_at = smem_u32(&sh.ring[warp][0][lane]);
+    stage = 0;
+    // a lane's windows are read in an order that keeps 8 lanes off each other's banks
+    get_at = smem_u32(&sh.ring[warp][0][lane * kUnit]) + ((lane >> 1) & (kUnit - 1)) * 16;
     turn = 0;
     next_t = (int)(blockIdx.x / C);
     next_row();
@@ -660,20 +667,26 @@ struct Scan {
   // Starts the copy of this warp's windows of the next step, the row's partial
   // windows left out.  The stage's windows have been read by all lanes.
   __device__ __forceinline__ void issue() {
-    const uint32_t to = ring + issue_stage * (kWarpStep * 16);
+    if (next_i - lane >= 0 && next_i - lane + kWarpStep <= next_n) {
 #pragma unroll
-    for (int u = 0; u < kUnit; ++u)
-      if ((unsigned)(next_i + 32 * u) < (unsigned)next_n)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + u * 512), "l"(next_src + 32 * u)
-                     : "memory");
+      for (int u = 0; u < kUnit; ++u) copy_window(u);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kUnit; ++u)
+        if ((unsigned)(next_i + 32 * u) < (unsigned)next_n) copy_window(u);
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    issue_stage ^= 1;
+    stage ^= kStageBytes;
     next_i += kWarpStep;
     next_src += kWarpStep;
     if (--next_left == 0) {
       next_t += clusters;
       next_row();
     }
+  }
+  __device__ __forceinline__ void copy_window(int u) const {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(put_at + stage + u * 512), "l"(next_src + 32 * u)
+                 : "memory");
   }
   // Waits for the oldest copy, of all lanes.
   __device__ __forceinline__ void wait() {
@@ -686,8 +699,8 @@ struct Scan {
     return fminf(fminf(fminf(a.x, a.y), fminf(a.z, a.w)), fminf(fminf(b.x, b.y), fminf(b.z, b.w)));
   }
   // Raises the threshold to what the groups of all warps show, and drops the
-  // listed windows below it.
-  __device__ __forceinline__ void refresh() {
+  // listed units below it (unless it is not the last time and they are few).
+  __device__ __forceinline__ void refresh(bool last) {
     const int m = (K + kScanWarps - 1) / kScanWarps;
     const float reach = m <= 12 ? warp_mth(fmaxf(top0, top1), m, thr) : warp_reach(top0, top1, m, thr, kGrain);
     turn ^= 1;
@@ -708,32 +721,24 @@ struct Scan {
       raise(low);
       list_thr = fmaxf(list_thr, thr);
     }
+    if (last || listed > 24) keep_from(thr > -INFINITY ? (uint64_t)ordered(thr) << 32 : 1);
+  }
+  // Keeps the units of this warp's list whose keys are at least t, in order, and
+  // drops the others.
+  __device__ __forceinline__ void keep_from(uint64_t t) {
     int out = 0;
     for (int base = 0; base < listed; base += 32) {
       const int i = base + lane;
-      uint64_t k = 0;
-      float ws = 0.0f;
-      if (i < listed) {
-        k = list_key[i];
-        ws = list_sum[i];
-      }
-      out = keep(k, ws, k && key_value(k) >= thr, out);
+      Listed e = {0, 0.0f, 0};
+      if (i < listed) e = list[i];
+      const bool yes = e.key >= t;
+      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+      if (yes) list[out + __popc(mask & ((1u << lane) - 1u))] = e;
+      else if (e.key) s += e.sum * exp_from(fmaxf(key_value(e.key), kFloorRef), ref, c);
+      out += __popc(mask);
+      __syncwarp();
     }
     listed = out;
-  }
-  // Moves the entries (a lane each) that are kept to place `out` and on, in
-  // order, and drops the others; returns the next place.
-  __device__ __forceinline__ int keep(uint64_t k, float ws, bool yes, int out) {
-    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
-    if (yes) {
-      const int at = out + __popc(mask & ((1u << lane) - 1u));
-      list_key[at] = k;
-      list_sum[at] = ws;
-    } else if (k) {
-      drop(k, ws);
-    }
-    __syncwarp();
-    return out + __popc(mask);
   }
   __device__ __forceinline__ void raise(float low) {
     thr = low;
@@ -741,9 +746,6 @@ struct Scan {
     s *= f;
     lost *= f;
     ref = r;
-  }
-  __device__ __forceinline__ void drop(uint64_t k, float ws) {
-    s += ws * exp_from(fmaxf(key_value(k), kFloorRef), ref, c);
   }
 
   // Cuts this warp's list to its K best windows: the windows that it reads from
@@ -753,7 +755,7 @@ struct Scan {
     while (high - low > 1) {
       const uint64_t mid = low + (high - low) / 2;
       int n = 0;
-      for (int i = lane; i < listed; i += 32) n += list_key[i] >= mid;
+      for (int i = lane; i < listed; i += 32) n += list[i].key >= mid;
       n = __reduce_add_sync(0xFFFFFFFFu, n);
       if (n >= K) low = mid;
       else high = mid;
@@ -761,23 +763,12 @@ struct Scan {
     }
     uint32_t least = 0xFFFFFFFFu;
     for (int i = lane; i < listed; i += 32)
-      if (list_key[i] >= low) least = min(least, (uint32_t)(list_key[i] >> 32));
+      if (list[i].key >= low) least = min(least, (uint32_t)(list[i].key >> 32));
     least = __reduce_min_sync(0xFFFFFFFFu, least);
     if (unordered(least) > thr) raise(unordered(least));
     list_thr = unordered(ordered(thr) + 1);
     exact = true;
-    int out = 0;
-    for (int base = 0; base < listed; base += 32) {
-      const int i = base + lane;
-      uint64_t k = 0;
-      float ws = 0.0f;
-      if (i < listed) {
-        k = list_key[i];
-        ws = list_sum[i];
-      }
-      out = keep(k, ws, k && k >= low, out);
-    }
-    listed = out;
+    keep_from(low);
   }
 
   // Scans this CTA's part of row t for the k largest at 2^(z cc).
@@ -794,48 +785,45 @@ struct Scan {
     s = lost = 0.0f;
     listed = 0;
     int refresh_at = 1;
-    // a lane's windows are read in an order that keeps 8 lanes off each other's banks
-    const int turned = lane >> 1;
+    const int full_from = (a + kWarpStep - 1) / kWarpStep, full_to = b / kWarpStep;
     for (int step = 0; step < steps; ++step) {
       wait();
       const int at = step * kWarpStep + lane * kUnit;
       uint4 v[kUnit];
-      if (step * kWarpStep >= a && (step + 1) * kWarpStep <= b) {
+      if (step >= full_from && step < full_to) {
 #pragma unroll
-        for (int u = 0; u < kUnit; ++u) v[u] = sh.ring[warp][stage][lane * kUnit + ((u + turned) & (kUnit - 1))];
+        for (int u = 0; u < kUnit; ++u) v[u] = ld_shared_v4((get_at ^ (u * 16)) + stage);
       } else {
 #pragma unroll
         for (int u = 0; u < kUnit; ++u) {
-          const int i = at + ((u + turned) & (kUnit - 1));
+          const int i = at + (((get_at >> 4) ^ u) & (kUnit - 1));
           const uint32_t none = neg_inf_bits(row.p);
           v[u] = make_uint4(none, none, none, none);
-          if (i < n) v[u] = i >= a && i < b ? sh.ring[warp][stage][i - step * kWarpStep] : load_window(row, first + i);
+          if (i < n) v[u] = i >= a && i < b ? ld_shared_v4((get_at ^ (u * 16)) + stage) : load_window(row, first + i);
         }
       }
       const float m0 = window_max<T>(v[0], v[1]), m1 = window_max<T>(v[2], v[3]);
       top0 = fmaxf(top0, m0);
       top1 = fmaxf(top1, m1);
-      stage ^= 1;
       __syncwarp();
       issue();
       if (step == refresh_at || step + 1 == steps) {
-        refresh();
+        refresh(step + 1 == steps);
         refresh_at = 4 * step + 3;
       }
       const float m = fmaxf(m0, m1);
-      const bool list = m >= list_thr && at < n;
-      const float from = list ? fmaxf(m, kFloorRef) : ref;
+      const bool yes = m >= list_thr && at < n;
+      const float from = yes ? fmaxf(m, kFloorRef) : ref;
       const float sum = windows_sum<T, kUnit>(v, c, from);
       // s + sum with the rounding kept (a row's thread adds hundreds of these)
-      const float y = (list ? 0.0f : sum) - lost, z = s + y;
+      const float y = (yes ? 0.0f : sum) - lost, z = s + y;
       lost = (z - s) - y;
       s = z;
-      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, list);
+      const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
       if (mask) {
-        if (list) {
+        if (yes) {
           const int to = listed + __popc(mask & ((1u << lane) - 1u));
-          list_key[to] = make_key(m, (uint32_t)(first + at));
-          list_sum[to] = sum;
+          list[to] = {make_key(m, (uint32_t)(first + at)), sum, 0};
         }
         listed += __popc(mask);
         __syncwarp();
@@ -851,25 +839,24 @@ struct Scan {
   __device__ __forceinline__ int candidates(int t, uint64_t *dst, int cap, int fill) {
     const Row<T> row = row_of(t);
     const int most = exact ? K : cap;
-    // The windows of this warp's units that reach, a lane each, noted where the
-    // units' sums were, which are not needed any more; then the elements of those
+    // The windows of this warp's units that reach, a lane each, noted with
+    // the listed units; then the elements of those
     // windows, a lane each.  A warp's candidates are held until it is known where
     // they go (if they are too many to hold, the elements are read again).
-    int *const hit_list = reinterpret_cast<int *>(list_sum);
     const int windows = listed * kUnit;
     float add = 0.0f;
     int hits = 0, held = 0;
 #pragma unroll 2
     for (int base = 0; base < windows; base += 32) {
       const int i = base + lane;
-      const int at = i < windows ? (int)key_index(list_key[i / kUnit]) + i % kUnit : row.windows;
+      const int at = i < windows ? (int)key_index(list[i / kUnit].key) + i % kUnit : row.windows;
       const uint32_t none = neg_inf_bits(row.p);
       uint4 v = make_uint4(none, none, none, none);
       if (at < row.windows) v = load_window(row, at);
       const bool hit = at < row.windows && window_max<T>(v) >= thr;
       const uint32_t mask = __ballot_sync(0xFFFFFFFFu, hit);
       const int to = hits + __popc(mask & ((1u << lane) - 1u));
-      if (hit && to < room) hit_list[to] = at;
+      if (hit && to < room) list[to].window = at;
       if (!hit) add += window_sum<T>(v, c, ref);
       hits += __popc(mask);
     }
@@ -879,7 +866,7 @@ struct Scan {
 #pragma unroll 2
       for (int base = 0; base < elements; base += 32) {
         const int i = base + lane;
-        const int id = i < elements ? hit_list[i / E] * E - row.mis + i % E : -1;
+        const int id = i < elements ? list[i / E].window * E - row.mis + i % E : -1;
         const bool in = id >= 0 && id < vocab;
         const float z = in ? to_float(row.p[id]) : 0.0f;
         const bool yes = in && z >= thr;
@@ -925,29 +912,19 @@ struct Scan {
   __device__ __forceinline__ int most_of_many(const Row<T> &row, uint64_t *dst, int most, int fill,
                                               int units) {
     const int tid = threadIdx.x;
-    const uint64_t *const keys = list_key - warp * room;
+    const Listed *const lists = list - warp * room;
     if (units > kScanThreads) {
       constexpr int kSlots = (kScanWarps * (kTopMax + kListSpare) + kScanThreads - 1) / kScanThreads;
       uint64_t k[kSlots];
 #pragma unroll
       for (int j = 0; j < kSlots; ++j) {
         const int f = j * kScanThreads + tid, of = f / room, i = f - of * room;
-        k[j] = of < kScanWarps && i < sh.count[of] ? keys[of * room + i] : 0;
+        k[j] = of < kScanWarps && i < sh.count[of] ? lists[of * room + i].key : 0;
       }
       const uint64_t low = select_kth(k, K, sh);
       exact = true;
       raise_to_least(k, low);
-      int out = 0;
-      for (int base = 0; base < listed; base += 32) {
-        const int i = base + lane;
-        const uint64_t key = i < listed ? list_key[i] : 0;
-        if (key && key < low)
-          for (int u = 0; u < kUnit; ++u)
-            if ((int)key_index(key) + u < row.windows)
-              s += window_sum<T>(load_window(row, (int)key_index(key) + u), c, ref);
-        out = keep(key, 0.0f, key && key >= low, out);
-      }
-      listed = out;
+      keep_from(low);
       if (lane == 0) sh.count[warp] = listed;
       __syncthreads();
     }
@@ -955,7 +932,7 @@ struct Scan {
     int unit = -1, left = tid;
 #pragma unroll
     for (int w = 0; w < kScanWarps; ++w) {
-      if (left >= 0 && left < sh.count[w]) unit = (int)key_index(keys[w * room + left]);
+      if (left >= 0 && left < sh.count[w]) unit = (int)key_index(lists[w * room + left].key);
       left -= sh.count[w];
     }
     uint64_t k[kUnit];
