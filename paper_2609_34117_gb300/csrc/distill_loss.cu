@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
 #pragma unroll
       for (int u = 0; u < kLossUnroll; ++u) v[u] = without<T>(v[u], mask >> (8 * u) & 0xFFu);
     }
-    const float n = fmaxf(ref, fmaxf(window_max<T>(v[0], v[1]), window_max<T>(v[2], v[3])));
+    const float n = fmaxf(ref, fmaxf(window_max<T, false>(v[0], v[1]), window_max<T, false>(v[2], v[3])));
     s1 = fmaf(s1, exp_from(ref, n, c1), windows_sum<T, kLossUnroll>(v, c1, n));
     if constexpr (kTemp) s2 = fmaf(s2, exp_from(ref, n, c2), windows_sum<T, kLossUnroll>(v, c2, n));
     ref = n;

@@ -18,15 +18,22 @@
 // float; it decides except where the nucleus would end within that sum's error
 // bound, and then the leader sums the exact mass in a second pass.  Rows that
 // keep more than the listed elements (a wide nucleus, no filter at all) are
-// left to the end and then searched by the whole cluster: thresholds that split
-// the remaining range of values in eight, a pass over the row each.
+// left to the end and then searched by a whole cluster: thresholds that split
+// the remaining range of values in eight, a pass over the row each.  Where
+// clusters scan the rows, the same kernel does that; where single CTAs do, a
+// second kernel, so that a left-over row still gets a cluster and the first
+// keeps four CTAs on an SM.
 #include "vocab.cuh"
 
 namespace slimwise {
 
-constexpr int kSampleCtas = 3;    // CTAs of an SM
-constexpr int kNucleus = 64;      // elements looked at for a nucleus or min-p without top-k
-constexpr int kTopKListed = 128;  // largest top-k that is decided from the list
+// CTAs of an SM: three leave the scan all its registers, four hold more rows at
+// once.  256 rows of 150001 fp32 take 38 us with three and 46 with four, 512 of
+// 262144 bf16 73 and 67: three as long as they hold all rows.
+constexpr int kFewCtas = 3, kManyCtas = 4;
+constexpr int kNucleus = 32;      // elements looked at for a nucleus or min-p without top-k
+constexpr int kSampleRoom = 128;  // of a warp's list
+constexpr int kTopKListed = kSampleRoom - 32;  // largest top-k that is decided from the list
 constexpr int32_t kLeftOver = -2; // a token that is still to be searched (its logprob: the maximum)
 constexpr float kWeightOne = 1099511627776.0f;  // 2^40, the largest element's weight
 // Bound of the relative difference between the scan's float mass and the sum of
@@ -36,14 +43,27 @@ constexpr float kWeightOne = 1099511627776.0f;  // 2^40, the largest element's w
 // 19 (1.5 2^-23 + 2^-23) ln 2 < 2^-18.3; exp2's and exp's own 2^-22, and sums
 // of 19 roundings (8 in a window, 2 of the compensated sum, 8 + 1 over threads
 // and CTAs) 2^-19.7; the weights' truncation V 2^-40.
-constexpr double kMassError = 1.0 / 131072.0;
+constexpr uint64_t kMassError = 1 << 17;  // one part in
 
 enum SampleMode { kDone = 0, kExactMass = 1, kSearch = 2 };
 
-struct SampleShared {
-  uint64_t weight[kTopMax];
+// What a search uses of shared memory, where the ring was.
+struct SearchShared {
   uint64_t slot[2][kClusterMax][8];  // each CTA's sums of a pass
   uint64_t red[kScanWarps][8];
+  uint64_t mass[kScanWarps];
+  uint32_t left[kScanWarps];         // rows that are left over, a bit each
+};
+static_assert(sizeof(SearchShared) <= sizeof(ScanShared::ring), "the search fits the ring");
+struct SampleShared {
+  uint64_t weight[kTopMax];
+};
+struct SampleArgs {
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p, *uniform;
+  int32_t *tokens;
+  float *logprob;
 };
 
 __device__ __forceinline__ uint64_t fraction(uint64_t mass, uint64_t f24) {
@@ -66,7 +86,7 @@ __device__ __forceinline__ uint64_t element_weight(float e) {
 
 // Sums of N whole numbers over the cluster; slot[parity] keeps each CTA's.
 template <int N>
-__device__ __forceinline__ void cluster_sum(uint64_t (&v)[N], int &parity, SampleShared &sh) {
+__device__ __forceinline__ void cluster_sum(uint64_t (&v)[N], int &parity, SearchShared &sh) {
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x;
@@ -127,7 +147,7 @@ struct Limit {
 template <typename T>
 __device__ __noinline__ uint32_t search_value(const Part<T> &part, Limit in, bool mass,
                                               uint64_t want, uint32_t start, uint32_t top,
-                                              uint64_t &above, int &parity, SampleShared &sh) {
+                                              uint64_t &above, int &parity, SearchShared &sh) {
   uint64_t a = start, b = (uint64_t)top + 1;
   above = 0;
   while (b - a > 1) {
@@ -160,7 +180,7 @@ __device__ __noinline__ uint32_t search_value(const Part<T> &part, Limit in, boo
 // The smallest id such that `want` elements of value o have ids up to it.
 template <typename T>
 __device__ __noinline__ int search_id(const Part<T> &part, uint32_t o, uint64_t want, int &parity,
-                                      SampleShared &sh) {
+                                      SearchShared &sh) {
   int a = -1, b = part.row.vocab - 1;  // too few up to a, enough up to b
   while (b - a > 1) {
     const int64_t span = b - a;
@@ -186,7 +206,7 @@ __device__ __noinline__ int search_id(const Part<T> &part, uint32_t o, uint64_t 
 // The whole request over the whole row, by all CTAs of the cluster.
 template <typename T>
 __device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int &parity,
-                                        int32_t *token, float *logprob, SampleShared &sh) {
+                                        int32_t *token, float *logprob, SearchShared &sh) {
   constexpr int E = Row<T>::E;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank();
@@ -238,14 +258,14 @@ __device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int 
   for (int i = wlo + lane; i < whi; i += 32) mine += window(i);
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
-  if (lane == 0) sh.weight[warp] = mine;
+  if (lane == 0) sh.mass[warp] = mine;
   uint64_t total[1] = {lane == 0 ? mine : 0};
   const int at = parity;
   cluster_sum(total, parity, sh);
   const uint64_t target = fraction(total[0], d.u24);
   uint64_t before = 0;
   for (int r = 0; r < rank; ++r) before += sh.slot[at][r][0];
-  for (int w = 0; w < warp; ++w) before += sh.weight[w];
+  for (int w = 0; w < warp; ++w) before += sh.mass[w];
   if (target < before || target >= before + mine) return;
   for (int i = wlo; i < whi; i += 32) {
     const uint64_t s = window(i + lane);
@@ -294,11 +314,11 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
   uint64_t before = 0;
   if (key) {
 #pragma unroll 4
-    for (int i = sub; i < n; i += lanes)
-      if (sh.cand[i] > key) {
-        ++rank;
-        before += sm.weight[i];
-      }
+    for (int i = sub; i < n; i += lanes) {
+      const bool first = sh.cand[i] > key;
+      rank += first;
+      before += first ? sm.weight[i] : 0;
+    }
   }
   for (int o = 1; o < lanes; o *= 2) {
     rank += __shfl_xor_sync(0xFFFFFFFFu, rank, o);
@@ -325,10 +345,10 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
       if (key) sh.by_rank[rank] = e;
       __syncthreads();
       const float cand = block_reduce<kScanThreads>(tid < n ? sh.by_rank[tid] : 0.0f, sh.redf, OpAdd());
-      const double about = ((double)cand + (double)rest * exp2((double)((ref - m) * c))) * kWeightOne *
-                           (double)d.p24 * (1.0 / 16777216.0);
-      low = (uint64_t)fmax(about * (1.0 - kMassError) - 2.0, 0.0);
-      cut = (uint64_t)(about * (1.0 + kMassError)) + 2;
+      // the share in whole numbers, and the error bound around it
+      const uint64_t about = fraction(__float2ull_rz(fmaf(rest, ex2((ref - m) * c), cand) * kWeightOne), d.p24);
+      low = about - about / kMassError;
+      cut = about + about / kMassError + 2;
     }
     if (!(last < d.min_p) && (!d.nucleus || listed < cut)) return kSearch;
     if (__syncthreads_or(key && rank > 0 && before >= low && before < cut)) return kExactMass;
@@ -343,7 +363,7 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
   if (shared_key) {
 #pragma unroll 4
     for (int i = sub; i < n; i += lanes)  // (the key's low half is the complement of the id)
-      if ((uint32_t)sh.cand[i] > (uint32_t)shared_key) id_before += sm.weight[i];
+      id_before += (uint32_t)sh.cand[i] > (uint32_t)shared_key ? sm.weight[i] : 0;
   }
   for (int o = 1; o < lanes; o *= 2) id_before += __shfl_xor_sync(0xFFFFFFFFu, id_before, o);
   if (w && target >= id_before && target < id_before + w) {
@@ -353,85 +373,125 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
   return kDone;
 }
 
-template <typename T, bool kCluster>
-__global__ void __launch_bounds__(kScanThreads, kSampleCtas)
+// The request of row t, and how many elements to look at: all that top-k leaves,
+// else a guess of what a nucleus or min-p keeps; without any filter only the
+// largest.  False if the request is out of range.
+__device__ __forceinline__ bool request_of(const SampleArgs &a, int t, int vocab, Draw &d, int &K) {
+  const float temp = a.temperature ? a.temperature[t] : 1.0f;
+  const int tk = a.top_k ? a.top_k[t] : 0;
+  const float tp = a.top_p ? a.top_p[t] : 1.0f;
+  const float mp = a.min_p ? a.min_p[t] : 0.0f;
+  const float u = a.uniform[t];
+  const bool good = temp >= 0.0f && temp < INFINITY && tp >= 0.0f && mp <= 1.0f && u >= 0.0f && u < 1.0f;
+  const bool greedy = !good || temp < FLT_MIN;
+  d.inv = greedy ? 1.0f : 1.0f / temp;
+  d.min_p = mp;
+  d.top_k = greedy ? 1 : (tk > 0 && tk < vocab) ? tk : vocab;
+  d.limited = d.top_k < vocab;
+  d.nucleus = tp < 1.0f;
+  d.p24 = (uint64_t)(fminf(tp, 1.0f) * 16777216.0f);
+  d.u24 = (uint64_t)(u * 16777216.0f);
+  K = d.top_k <= kTopKListed ? d.top_k : (d.nucleus || mp > 0.0f) ? min(kNucleus, vocab) : 1;
+  return good;
+}
+
+// Row t's token, by its leader's threads, from its n largest elements in sh.cand
+// and s, this thread's part of the sum of all others.  Not inlined: the scan's
+// loop keeps its registers.
+template <typename T>
+__device__ __noinline__ void finish_row(const SampleArgs &a, const Row<T> row, int t, int n, float s,
+                                        float ref, ScanShared &sh, SampleShared &sm) {
+  const int tid = threadIdx.x;
+  Draw d;
+  int K;
+  const bool good = request_of(a, t, row.vocab, d, K);
+  const float c = kLog2e * d.inv;
+  const float m = block_reduce<kScanThreads>(tid < n ? key_value(sh.cand[tid]) : -INFINITY, sh.redf, OpMax());
+  const float rest = block_reduce<kScanThreads>(s, sh.redf, OpAdd());
+  if (!good || !(rest < INFINITY) || !(m > -INFINITY) || !(m < INFINITY)) {
+    // NaN or +inf in the row, or nothing but -inf: no distribution
+    if (tid == 0) {
+      a.tokens[t] = -1;
+      a.logprob[t] = NAN;
+    }
+    return;
+  }
+  uint64_t mass = 0;
+  int mode;
+  while ((mode = decide(d, n, rest, ref, c, m, mass, a.tokens + t, a.logprob + t, sh, sm)) == kExactMass) {
+    const Part<T> all = {row, 0, row.windows, m, d.inv};
+    all.each([&](float z, int) { mass += element_weight(element_exp(z, m, d.inv)); });
+    mass = block_reduce<kScanThreads>(mass, sh.red64, OpAdd());
+  }
+  if (mode == kSearch && tid == 0) {
+    a.tokens[t] = kLeftOver;
+    a.logprob[t] = m;
+  }
+}
+
+// The rows of this cluster that were left over, searched by all its CTAs.
+template <typename T>
+__device__ __forceinline__ void search_rows(const T *logits, int64_t stride, int rows, int vocab,
+                                            const SampleArgs &a, SearchShared &sh) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int tid = threadIdx.x, first = (int)(blockIdx.x / C), clusters = (int)(gridDim.x / C);
+  int parity = 0;
+  for (int base = first; base < rows; base += kScanThreads * clusters) {
+    // (a row's own search writes its token after a barrier that all CTAs reach)
+    const int mine = base + tid * clusters;
+    const bool left = mine < rows && __ldcg(a.tokens + mine) == kLeftOver;
+    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, left);
+    if ((tid & 31) == 0) sh.left[tid >> 5] = mask;
+    if (!__syncthreads_or(left)) continue;
+    for (int w = 0; w < kScanWarps; ++w)
+      for (uint32_t bits = sh.left[w]; bits; bits &= bits - 1) {
+        const int t = base + (32 * w + __ffs((int)bits) - 1) * clusters;
+        Draw d;
+        int K;
+        request_of(a, t, vocab, d, K);
+        Part<T> part = {Row<T>(logits + (int64_t)t * stride, vocab), 0, 0, __ldcg(a.logprob + t), d.inv};
+        const int per = (part.row.windows + C - 1) / C;
+        part.lo = min(rank * per, part.row.windows);
+        part.hi = min(part.lo + per, part.row.windows);
+        search_row(part, d, parity, a.tokens + t, a.logprob + t, sh);
+      }
+    __syncthreads();
+  }
+  cluster.sync();  // no CTA ends while its sums can still be read or written
+}
+
+template <typename T, bool kCluster, int kCtas>
+__global__ void __launch_bounds__(kScanThreads, kCtas)
     sample_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int K_most,
-                  const float *__restrict__ temperature, const int32_t *__restrict__ top_k,
-                  const float *__restrict__ top_p, const float *__restrict__ min_p,
-                  const float *__restrict__ uniform, int32_t *tokens, float *logprob) {
+                  const __grid_constant__ SampleArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   SampleShared &sm = *reinterpret_cast<SampleShared *>(smem);
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem + sizeof(SampleShared));
-  const int tid = threadIdx.x;
-  Scan<T, kCluster> scan(sh, K_most, logits, stride, vocab, rows);
-  // the row's request; false if it is out of range
-  auto request_of = [&](int t, Draw &d, int &K) {
-    const float temp = temperature ? temperature[t] : 1.0f;
-    const int tk = top_k ? top_k[t] : 0;
-    const float tp = top_p ? top_p[t] : 1.0f;
-    const float mp = min_p ? min_p[t] : 0.0f;
-    const float u = uniform[t];
-    const bool good = temp >= 0.0f && temp < INFINITY && tp >= 0.0f && mp <= 1.0f && u >= 0.0f && u < 1.0f;
-    const bool greedy = !good || temp < FLT_MIN;
-    d.inv = greedy ? 1.0f : 1.0f / temp;
-    d.min_p = mp;
-    d.top_k = greedy ? 1 : (tk > 0 && tk < vocab) ? tk : vocab;
-    d.limited = d.top_k < vocab;
-    d.nucleus = tp < 1.0f;
-    d.p24 = (uint64_t)(fminf(tp, 1.0f) * 16777216.0f);
-    d.u24 = (uint64_t)(u * 16777216.0f);
-    // elements to look at: all that top-k leaves, else a guess of what a nucleus
-    // or min-p keeps; without any filter only the largest
-    K = d.top_k <= kTopKListed ? d.top_k : (d.nucleus || mp > 0.0f) ? min(kNucleus, vocab) : 1;
-    return good;
-  };
-  auto request = [&](int t, int &K, float &c) {
+  pdl_launch_dependents();
+  Scan<T, kCluster, true> scan(sh, kSampleRoom, K_most, logits, stride, vocab, rows);
+  auto request = [&](int t, int &K, float &c, bool &sums) {
     Draw d;
-    request_of(t, d, K);
+    request_of(a, t, vocab, d, K);
     c = kLog2e * d.inv;
+    sums = d.nucleus && !d.limited;  // only such a nucleus is one of the row's whole mass
   };
   scan.rows_of_cluster(request, [&](int t, int n) {
-    Draw d;
-    int K;
-    const bool good = request_of(t, d, K);
-    const float c = scan.c;
-    const float m = block_reduce<kScanThreads>(tid < n ? key_value(sh.cand[tid]) : -INFINITY, sh.redf, OpMax());
-    const float rest = block_reduce<kScanThreads>(scan.s, sh.redf, OpAdd());
-    if (!good || !(rest < INFINITY) || !(m > -INFINITY) || !(m < INFINITY)) {
-      // NaN or +inf in the row, or nothing but -inf: no distribution
-      if (tid == 0) {
-        tokens[t] = -1;
-        logprob[t] = NAN;
-      }
-      return;
-    }
-    int mode = decide(d, n, rest, scan.ref, c, m, 0, tokens + t, logprob + t, sh, sm);
-    if (mode == kExactMass) {
-      const Row<T> row = scan.row_of(t);
-      const Part<T> all = {row, 0, row.windows, m, d.inv};
-      uint64_t mass = 0;
-      all.each([&](float z, int) { mass += element_weight(element_exp(z, m, d.inv)); });
-      mass = block_reduce<kScanThreads>(mass, sh.red64, OpAdd());
-      mode = decide(d, n, rest, scan.ref, c, m, mass, tokens + t, logprob + t, sh, sm);
-    }
-    if (mode == kSearch && tid == 0) {
-      tokens[t] = kLeftOver;
-      logprob[t] = m;
-    }
+    finish_row(a, scan.row_of(t), t, n, scan.s, scan.ref, sh, sm);
   });
-  cg::this_cluster().sync();
-  int parity = 0;
-  for (int t = blockIdx.x / scan.C; t < rows; t += scan.clusters) {
-    // (the row's own search writes these after a barrier that all CTAs reach)
-    if (__ldcg(tokens + t) != kLeftOver) continue;
-    Draw d;
-    int K;
-    request_of(t, d, K);
-    Part<T> part = {scan.row_of(t), 0, 0, __ldcg(logprob + t), d.inv};
-    scan.slice(part.row, part.lo, part.hi);
-    search_row(part, d, parity, tokens + t, logprob + t, sm);
+  if constexpr (kCluster) {
+    cg::this_cluster().sync();
+    search_rows(logits, stride, rows, vocab, a, *reinterpret_cast<SearchShared *>(sh.ring));
   }
-  cg::this_cluster().sync();  // no CTA ends while its sums can still be read or written
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kScanThreads)
+    sample_search_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab,
+                         const __grid_constant__ SampleArgs a) {
+  __shared__ SearchShared search;
+  pdl_wait_primary();
+  search_rows(logits, stride, rows, vocab, a, search);
 }
 
 template <typename T>
@@ -440,17 +500,35 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
                           const float *min_p, const float *uniform, int32_t *tokens,
                           float *logprob, cudaStream_t stream) {
   const int K_most = top_k ? kTopKListed : kNucleus;
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), K_most, kSampleCtas, sizeof(SampleShared));
-  const auto launch = g.C > 1 ? launch_clusters<sample_kernel<T, true>, const T *, int64_t, int, int, int,
-                                                const float *, const int32_t *, const float *,
-                                                const float *, const float *, int32_t *, float *>
-                              : launch_clusters<sample_kernel<T, false>, const T *, int64_t, int, int, int,
-                                                const float *, const int32_t *, const float *,
-                                                const float *, const float *, int32_t *, float *>;
-  return launch(g.clusters, g.C, kScanThreads, sizeof(SampleShared) + scan_smem(K_most, g.C),
-                sizeof(SampleShared) + scan_smem(kTopKListed, kClusterMax), stream,
-                static_cast<const T *>(logits), stride, rows, vocab, K_most, temperature, top_k,
-                top_p, min_p, uniform, tokens, logprob);
+  const bool many = rows > 152 * kFewCtas;
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleRoom, K_most,
+                               many ? kManyCtas : kFewCtas, sizeof(SampleShared));
+  const SampleArgs a = {temperature, top_k, top_p, min_p, uniform, tokens, logprob};
+  const T *const z = static_cast<const T *>(logits);
+  const auto launch =
+      g.C > 1 ? launch_clusters<sample_kernel<T, true, kFewCtas>, const T *, int64_t, int, int, int, SampleArgs>
+      : many  ? launch_clusters<sample_kernel<T, false, kManyCtas>, const T *, int64_t, int, int, int, SampleArgs>
+              : launch_clusters<sample_kernel<T, false, kFewCtas>, const T *, int64_t, int, int, int, SampleArgs>;
+  cudaError_t err = launch(g.clusters, g.C, kScanThreads,
+                           sizeof(SampleShared) + scan_smem(kSampleRoom, K_most, g.C),
+                           sizeof(SampleShared) + scan_smem(kSampleRoom, kTopKListed, kClusterMax),
+                           stream, z, stride, rows, vocab, K_most, a);
+  if (err != cudaSuccess || g.C > 1) return err;
+  const int clusters = 152 / kClusterMax;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kClusterMax;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((rows < clusters ? rows : clusters) * kClusterMax));
+  cfg.blockDim = dim3(kScanThreads);
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, sample_search_kernel<T>, z, stride, rows, vocab, a);
 }
 
 cudaError_t launch_sample(const void *logits, int dtype, int rows, int vocab, int64_t stride,

@@ -22,10 +22,11 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   extern __shared__ __align__(128) unsigned char smem[];
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem);
   const int tid = threadIdx.x;
-  Scan<T, kCluster> scan(sh, K, logits, stride, vocab, rows);
-  auto request = [&](int, int &k, float &cc) {
+  Scan<T, kCluster, false> scan(sh, list_room(K), K, logits, stride, vocab, rows);
+  auto request = [&](int, int &k, float &cc, bool &sums) {
     k = K;
     cc = c;
+    sums = true;
   };
   scan.rows_of_cluster(request, [&](int t, int n) {
     // a candidate's place in the order, by a few lanes
@@ -68,12 +69,12 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   });
 }
 
-ScanGrid scan_grid(int rows, int vocab, int element_bytes, int K, int ctas_per_sm,
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, int ctas_per_sm,
                    size_t more_smem) {
   const int windows = (int)(((int64_t)vocab * element_bytes + 15) / 16) + 1;
   int C = 1;
   while (C < kClusterMax && rows * C <= 128 && windows >= 2 * C * 2 * kScanWarps * kWarpStep) C *= 2;
-  const int fit = (int)(228 * 1024 / (scan_smem(K, C) + more_smem + 1024));
+  const int fit = (int)(228 * 1024 / (scan_smem(room, K, C) + more_smem + 1024));
   const int at_once = 152 * (fit < ctas_per_sm ? fit : ctas_per_sm) / C;
   return {C, rows < at_once ? rows : at_once};
 }
@@ -82,13 +83,13 @@ template <typename T>
 static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t stride, int k,
                               float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), k, kTopCtas, 0);
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), list_room(k), k, kTopCtas, 0);
   const auto launch = g.C > 1 ? launch_clusters<top_logits_kernel<T, true>, const T *, int64_t, int, int, int,
                                                 float, int32_t *, float *, float *>
                               : launch_clusters<top_logits_kernel<T, false>, const T *, int64_t, int, int, int,
                                                 float, int32_t *, float *, float *>;
-  return launch(g.clusters, g.C, kScanThreads, scan_smem(k, g.C), scan_smem(kTopMax, kClusterMax),
-                stream, static_cast<const T *>(logits), stride, rows, vocab, k,
+  return launch(g.clusters, g.C, kScanThreads, scan_smem(list_room(k), k, g.C),
+                scan_smem(list_room(kTopMax), kTopMax, kClusterMax), stream, static_cast<const T *>(logits), stride, rows, vocab, k,
                 kLog2e / temperature, ids, logp, log_rest);
 }
 

@@ -86,7 +86,8 @@ cudaError_t launch_distill_loss(const void *logits, int dtype, int rows, int voc
 struct ScanGrid {
   int C, clusters;
 };
-ScanGrid scan_grid(int rows, int vocab, int element_bytes, int K, int ctas_per_sm, size_t more_smem);
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, int ctas_per_sm,
+                   size_t more_smem);
 
 #if defined(__CUDACC__)
 namespace cg = cooperative_groups;
@@ -196,10 +197,30 @@ __device__ __forceinline__ float window_max(const uint4 &v) {
   }
 }
 
-// Of two windows.
-template <typename T>
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Of two windows (kNan: NaN if any is).
+template <typename T, bool kNan>
 __device__ __forceinline__ float window_max(const uint4 &v, const uint4 &w) {
-  if constexpr (sizeof(T) == 4) {
+  if constexpr (kNan && sizeof(T) == 4) {
+    const uint32_t a[8] = {v.x, v.y, v.z, v.w, w.x, w.y, w.z, w.w};
+    float m = __uint_as_float(a[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = max_nan(m, __uint_as_float(a[i]));
+    return m;
+  } else if constexpr (kNan) {
+    const uint32_t m = max2_nan(max2_nan(max2_nan(v.x, w.x), max2_nan(v.y, w.y)),
+                                max2_nan(max2_nan(v.z, w.z), max2_nan(v.w, w.w)));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  } else if constexpr (sizeof(T) == 4) {
     return fmaxf(window_max<T>(v), window_max<T>(w));
   } else {
     uint4 m;
@@ -404,8 +425,9 @@ struct alignas(128) ScanShared {
   //       uint64_t [cluster][cap]  in clusters, at a row's leader: each CTA's
   //                                candidates (in clusters of two, two of these)
 };
-inline size_t scan_smem(int K, int C) {
-  return sizeof(ScanShared) + (size_t)kScanWarps * list_room(K) * sizeof(Listed) +
+// room: of a warp's list; K: the largest number of candidates asked for.
+inline size_t scan_smem(int room, int K, int C) {
+  return sizeof(ScanShared) + (size_t)kScanWarps * room * sizeof(Listed) +
          (C > 1 ? (size_t)(C > 4 ? C : 4) * candidate_cap(K) * 8 : 0);
 }
 
@@ -563,7 +585,9 @@ __device__ __forceinline__ int candidate_lanes(int n) {
 }
 
 // kCluster: rows are split over the CTAs of a cluster (else the cluster is one CTA).
-template <typename T, bool kCluster>
+// kSumless: scan() can leave out the sums (of the 400 instructions of a step,
+// 120); s is then 0, or NaN where the row has NaN.
+template <typename T, bool kCluster, bool kSumless>
 struct Scan {
   static constexpr int E = Row<T>::E;
   static constexpr uint32_t kGrain = sizeof(T) == 2 ? 0xFFFFu : 0x1FFFu;  // a bf16's step; 2^-10 of an fp32
@@ -593,8 +617,10 @@ struct Scan {
   int turn;                     // of reach and known
   bool exact;                   // the K best alone are known to be complete
 
-  // K_most: the largest K of all rows
-  __device__ __forceinline__ Scan(ScanShared &shared, int K_most, const T *z, int64_t st, int V, int n)
+  // list_rooms: units that a warp's list has room for (at least K + 32), K_most: the
+  // largest K of all rows
+  __device__ __forceinline__ Scan(ScanShared &shared, int list_rooms, int K_most, const T *z, int64_t st,
+                                  int V, int n)
       : sh(shared), logits(z), stride(st), vocab(V), rows(n) {
     if constexpr (kCluster) {
       cg::cluster_group cluster = cg::this_cluster();
@@ -608,7 +634,7 @@ struct Scan {
     log_parts = 31 - __clz(C * kScanWarps);
     lane = threadIdx.x & 31;
     warp = threadIdx.x >> 5;
-    room = list_room(K_most);
+    room = list_rooms;
     recv_cap = candidate_cap(K_most);
     Listed *const lists = reinterpret_cast<Listed *>(&sh + 1);
     list = lists + warp * room;
@@ -637,12 +663,6 @@ struct Scan {
     steps = (per + kWarpStep - 1) / kWarpStep;
     first = min((rank * kScanWarps + warp) * per, row.windows);
     return min(per, row.windows - first);
-  }
-  // This CTA's windows.
-  __device__ __forceinline__ void slice(const Row<T> &row, int &lo, int &hi) const {
-    const int per = run_windows(row);
-    lo = min(rank * kScanWarps * per, row.windows);
-    hi = min(lo + kScanWarps * per, row.windows);
   }
   // [a, b): the windows of the run that lie whole in the row.
   __device__ __forceinline__ void whole_part(const Row<T> &row, int first, int n, int &a, int &b) const {
@@ -772,7 +792,7 @@ struct Scan {
   }
 
   // Scans this CTA's part of row t for the k largest at 2^(z cc).
-  __device__ __forceinline__ void scan(int t, int k, float cc) {
+  __device__ __forceinline__ void scan(int t, int k, float cc, bool sums) {
     const Row<T> row = row_of(t);
     int first, steps, a, b;
     const int n = run(row, first, steps);
@@ -785,6 +805,7 @@ struct Scan {
     s = lost = 0.0f;
     listed = 0;
     int refresh_at = 1;
+    bool nan = false;
     const int full_from = (a + kWarpStep - 1) / kWarpStep, full_to = b / kWarpStep;
     for (int step = 0; step < steps; ++step) {
       wait();
@@ -802,7 +823,8 @@ struct Scan {
           if (i < n) v[u] = i >= a && i < b ? ld_shared_v4((get_at ^ (u * 16)) + stage) : load_window(row, first + i);
         }
       }
-      const float m0 = window_max<T>(v[0], v[1]), m1 = window_max<T>(v[2], v[3]);
+      const float m0 = window_max<T, kSumless>(v[0], v[1]), m1 = window_max<T, kSumless>(v[2], v[3]);
+      if constexpr (kSumless) nan |= m0 != m0 || m1 != m1;
       top0 = fmaxf(top0, m0);
       top1 = fmaxf(top1, m1);
       __syncwarp();
@@ -813,12 +835,15 @@ struct Scan {
       }
       const float m = fmaxf(m0, m1);
       const bool yes = m >= list_thr && at < n;
-      const float from = yes ? fmaxf(m, kFloorRef) : ref;
-      const float sum = windows_sum<T, kUnit>(v, c, from);
-      // s + sum with the rounding kept (a row's thread adds hundreds of these)
-      const float y = (yes ? 0.0f : sum) - lost, z = s + y;
-      lost = (z - s) - y;
-      s = z;
+      float sum = 0.0f;
+      if (!kSumless || sums) {
+        const float from = yes ? fmaxf(m, kFloorRef) : ref;
+        sum = windows_sum<T, kUnit>(v, c, from);
+        // s + sum with the rounding kept (a row's thread adds hundreds of these)
+        const float y = (yes ? 0.0f : sum) - lost, z = s + y;
+        lost = (z - s) - y;
+        s = z;
+      }
       const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
       if (mask) {
         if (yes) {
@@ -830,6 +855,7 @@ struct Scan {
         if (listed > room - 32 && step + 1 < steps) cut();
       }
     }
+    if (kSumless && nan) s = NAN;
   }
 
   // The elements of the listed units that reach the threshold, as keys (value,
@@ -1110,7 +1136,7 @@ struct Scan {
     __syncthreads();
     return n;
   }
-  // The loop over this cluster's rows.  request(t, K, c) says what row t is
+  // The loop over this cluster's rows.  request(t, K, c, sums) says what row t is
   // scanned for; done(t, n) is called by all threads of a row's leader.
   template <typename R, typename D>
   __device__ __forceinline__ void rows_of_cluster(R request, D done) {
@@ -1120,8 +1146,9 @@ struct Scan {
       int at = -1, n = 0, k;
       float cc;
       if (more) {
-        request(t, k, cc);
-        scan(t, k, cc);
+        bool sums;
+        request(t, k, cc, sums);
+        scan(t, k, cc, sums);
       }
       if constexpr (!kCluster) {
         if (more) {
@@ -1134,7 +1161,8 @@ struct Scan {
         else cluster_wait();
         if (row_turn > 0 && leader_of(row_turn - 1) == rank) {
           at = t - clusters;
-          request(at, k, cc);
+          bool sums;
+          request(at, k, cc, sums);
           n = merge(row_turn - 1, k, cc);
         }
       }
