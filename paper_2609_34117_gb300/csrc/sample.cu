@@ -18,11 +18,12 @@
 // float; it decides except where the nucleus would end within that sum's error
 // bound, and then the leader sums the exact mass in a second pass.  Rows that
 // keep more than the listed elements (a wide nucleus, no filter at all) are
-// left to the end and then searched by a whole cluster: thresholds that split
-// the remaining range of values in eight, a pass over the row each.  Where
-// clusters scan the rows, the same kernel does that; where single CTAs do, a
-// second kernel, so that a left-over row still gets a cluster and the first
-// keeps four CTAs on an SM.
+// left to the end and then searched by a whole cluster: the limits of top-k and
+// top-p by a radix selection of 11 bits a pass over the row, from histograms of
+// masses and counts, then the token by a running sum over ids.  Where clusters
+// scan the rows, the same kernel does that; where single CTAs do, a second
+// kernel, so that a left-over row still gets a cluster and the first keeps four
+// CTAs on an SM.
 #include "vocab.cuh"
 
 namespace slimwise {
@@ -47,14 +48,17 @@ constexpr uint64_t kMassError = 1 << 17;  // one part in
 
 enum SampleMode { kDone = 0, kExactMass = 1, kSearch = 2 };
 
-// What a search uses of shared memory, where the ring was.
+// What a search uses of shared memory, where the scan's was.
+constexpr int kBins = 2048;
 struct SearchShared {
-  uint64_t slot[2][kClusterMax][8];  // each CTA's sums of a pass
-  uint64_t red[kScanWarps][8];
-  uint64_t mass[kScanWarps];
+  uint32_t hist[4][kBins];           // of a pass: weights in three parts of 14 bits, counts
+  uint64_t slot[2][kClusterMax];     // each CTA's sum
+  uint64_t red[kScanWarps];
+  uint64_t above;                    // result of a pass, written by the CTA that found it
+  int bin;
   uint32_t left[kScanWarps];         // rows that are left over, a bit each
 };
-static_assert(sizeof(SearchShared) <= sizeof(ScanShared::ring), "the search fits the ring");
+static_assert(sizeof(SearchShared) <= sizeof(ScanShared), "the search fits the scan's memory");
 struct SampleShared {
   uint64_t weight[kTopMax];
 };
@@ -84,52 +88,52 @@ __device__ __forceinline__ uint64_t element_weight(float e) {
   return (uint64_t)__float2ull_rz(e * kWeightOne);
 }
 
-// Sums of N whole numbers over the cluster; slot[parity] keeps each CTA's.
-template <int N>
-__device__ __forceinline__ void cluster_sum(uint64_t (&v)[N], int &parity, SearchShared &sh) {
+// Sum of a whole number over the cluster; slot[parity] keeps each CTA's.
+__device__ __forceinline__ uint64_t cluster_sum(uint64_t v, int &parity, SearchShared &sh) {
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
-    if ((tid & 31) == 0) sh.red[tid >> 5][i] = v[i];
-  }
-  __syncthreads();
-  if (tid < N * C) {
-    const int i = tid % N;
-    uint64_t s = 0;
-    for (int w = 0; w < kScanWarps; ++w) s += sh.red[w][i];
-    *cluster.map_shared_rank(&sh.slot[parity][rank][i], tid / N) = s;
-  }
+  v = block_reduce<kScanThreads>(v, sh.red, OpAdd());
+  if (tid < C) *cluster.map_shared_rank(&sh.slot[parity][rank], tid) = v;
   cluster.sync();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v[i] = 0;
-    for (int r = 0; r < C; ++r) v[i] += sh.slot[parity][r][i];
-  }
+  v = 0;
+  for (int r = 0; r < C; ++r) v += sh.slot[parity][r];
   parity ^= 1;
+  return v;
 }
 
-// The part of a row that this CTA passes over, and what a pass counts.
+// The part of a row that this CTA passes over.
 template <typename T>
 struct Part {
   Row<T> row;
   int lo, hi;
   float m, inv;
-  template <typename F>
-  __device__ __forceinline__ void each(F f) const {
+  // f(element, id) of windows from, from + step, ... below end, by this thread,
+  // U loads at a time.
+  template <int U = 4, typename F>
+  __device__ __forceinline__ void each(int from, int end, int step, F f) const {
     constexpr int E = Row<T>::E;
-    for (int i = lo + (int)threadIdx.x; i < hi; i += kScanThreads) {
-      float z[E];
-      unpack<T>(load_window(row, i), z);
+    for (int i = from; i < end; i += U * step) {
+      uint4 v[U];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int id = i * E - row.mis + e;
-        if (id >= 0 && id < row.vocab) f(z[e], id);
+      for (int u = 0; u < U; ++u)
+        if (i + u * step < end) v[u] = load_window(row, i + u * step);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i + u * step >= end) break;
+        float z[E];
+        unpack<T>(v[u], z);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int id = (i + u * step) * E - row.mis + e;
+          if (id >= 0 && id < row.vocab) f(z[e], id);
+        }
       }
     }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    each(lo + (int)threadIdx.x, hi, kScanThreads, f);
   }
 };
 
@@ -141,134 +145,136 @@ struct Limit {
   __device__ __forceinline__ bool has(uint32_t v, int i) const { return v > o || (v == o && i <= id); }
 };
 
-// The largest v with amount(values >= v within `in`) >= want, and in `above`
-// the amount of the values > v.  `mass`: amounts are weights, else counts.
-// start: a value for which the amount is known to suffice; top: the largest.
+// The largest value v (as ordered()) with amount(values >= v within `in`) at
+// least `want`, and in `above` the amount of the values > v.  Amounts are weights
+// (`mass`) or counts.  want 0: the share p24 of the whole amount; cut: that wanted.
 template <typename T>
-__device__ __noinline__ uint32_t search_value(const Part<T> &part, Limit in, bool mass,
-                                              uint64_t want, uint32_t start, uint32_t top,
-                                              uint64_t &above, int &parity, SearchShared &sh) {
-  uint64_t a = start, b = (uint64_t)top + 1;
+__device__ __noinline__ uint32_t search_value(const Part<T> &part, Limit in, bool mass, uint64_t want,
+                                              uint64_t p24, uint64_t &above, uint64_t &cut, int &parity,
+                                              SearchShared &sh) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = kBins / C, mine = per / kScanThreads;  // bins of a CTA, of a thread
+  uint32_t prefix = 0;
   above = 0;
-  while (b - a > 1) {
-    const uint64_t span = b - a;
-    uint64_t v[7] = {0, 0, 0, 0, 0, 0, 0};
+  for (int known = 32; known > (sizeof(T) == 2 ? 16 : 0);) {
+    const int shift = max(known - 11, sizeof(T) == 2 ? 16 : 0);  // (a bf16 has 16 bits)
+    for (int i = tid; i < 4 * kBins; i += kScanThreads) (&sh.hist[0][0])[i] = 0;
+    __syncthreads();
     part.each([&](float z, int id) {
       const uint32_t o = ordered(z);
-      if (!in.has(o, id)) return;
-      const uint64_t w = mass ? element_weight(element_exp(z, part.m, part.inv)) : 1;
-#pragma unroll
-      for (int i = 0; i < 7; ++i) v[i] += o >= a + span * (i + 1) / 8 ? w : 0;
-    });
-    cluster_sum(v, parity, sh);
-    uint64_t na = a, nb = b;
-    for (int i = 0; i < 7; ++i) {
-      const uint64_t t = a + span * (i + 1) / 8;
-      if (v[i] >= want) {
-        na = t;
-      } else if (t < nb) {
-        nb = t;
-        above = v[i];
+      if (!in.has(o, id) || (known < 32 && (o ^ prefix) >> known)) return;
+      const uint32_t bin = (o >> shift) & ((1u << (known - shift)) - 1u);
+      if (mass) {
+        const uint64_t w = element_weight(element_exp(z, part.m, part.inv));
+        if (w & 0x3FFF) atomicAdd(&sh.hist[0][bin], (uint32_t)(w & 0x3FFF));
+        if (w >> 14) {
+          atomicAdd(&sh.hist[1][bin], (uint32_t)(w >> 14 & 0x3FFF));
+          atomicAdd(&sh.hist[2][bin], (uint32_t)(w >> 28));
+        }
+      } else {
+        atomicAdd(&sh.hist[3][bin], 1u);
       }
-    }
-    a = na;
-    b = nb;
-  }
-  return (uint32_t)a;
-}
-
-// The smallest id such that `want` elements of value o have ids up to it.
-template <typename T>
-__device__ __noinline__ int search_id(const Part<T> &part, uint32_t o, uint64_t want, int &parity,
-                                      SearchShared &sh) {
-  int a = -1, b = part.row.vocab - 1;  // too few up to a, enough up to b
-  while (b - a > 1) {
-    const int64_t span = b - a;
-    uint64_t v[7] = {0, 0, 0, 0, 0, 0, 0};
-    part.each([&](float z, int id) {
-      if (ordered(z) != o) return;
-#pragma unroll
-      for (int i = 0; i < 7; ++i) v[i] += id <= a + span * (i + 1) / 8 ? 1 : 0;
     });
-    cluster_sum(v, parity, sh);
-    int na = a, nb = b;
-    for (int i = 6; i >= 0; --i) {
-      const int t = a + (int)(span * (i + 1) / 8);
-      if (v[i] >= want) nb = t;
-      else if (t > na) na = t;
+    cluster.sync();
+    // CTA r joins bins r per .. of all CTAs, each thread `mine` of them
+    const int first = rank * per + tid * mine;
+    uint64_t amount[kBins / kScanThreads], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kBins / kScanThreads; ++j) {
+      amount[j] = 0;
+      if (j < mine)
+        for (int r = 0; r < C; ++r) {
+          const uint32_t *const h = cluster.map_shared_rank(&sh.hist[0][first + j], r);
+          amount[j] += mass ? (uint64_t)h[0] + ((uint64_t)h[kBins] << 14) + ((uint64_t)h[2 * kBins] << 28)
+                            : (uint64_t)h[3 * kBins];
+        }
+      sum += amount[j];
     }
-    a = na;
-    b = nb;
+    // this thread's higher bins' amount within the CTA, then the cluster
+    uint64_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t v = __shfl_down_sync(0xFFFFFFFFu, incl, o);
+      if (lane + o < 32) incl += v;
+    }
+    if (lane == 0) sh.red[warp] = incl;
+    __syncthreads();
+    uint64_t over = incl - sum, total = 0;
+    for (int w = 0; w < kScanWarps; ++w) {
+      if (w > warp) over += sh.red[w];
+      total += sh.red[w];
+    }
+    if (tid < C) *cluster.map_shared_rank(&sh.slot[parity][rank], tid) = total;
+    cluster.sync();
+    uint64_t all = 0;
+    for (int r = 0; r < C; ++r) {
+      if (r > rank) over += sh.slot[parity][r];
+      all += sh.slot[parity][r];
+    }
+    parity ^= 1;
+    if (want == 0) {
+      want = fraction(all, p24);
+      if (want < 1) want = 1;
+    }
+    if (known == 32) cut = want;
+#pragma unroll
+    for (int j = kBins / kScanThreads - 1; j >= 0; --j) {
+      if (j >= mine) continue;
+      if (over < want && want <= over + amount[j])
+        for (int r = 0; r < C; ++r) {
+          *cluster.map_shared_rank(&sh.above, r) = over;
+          *cluster.map_shared_rank(&sh.bin, r) = first + j;
+        }
+      over += amount[j];
+    }
+    cluster.sync();
+    prefix |= (uint32_t)sh.bin << shift;
+    above += sh.above;
+    want -= sh.above;
+    known = shift;
   }
-  return b;
+  // the other bits of a bf16: its own are inverted below zero
+  return sizeof(T) == 2 && !(prefix >> 31) ? prefix | 0xFFFFu : prefix;
 }
 
-// The whole request over the whole row, by all CTAs of the cluster.
-template <typename T>
-__device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int &parity,
-                                        int32_t *token, float *logprob, SearchShared &sh) {
+// The first id at which the running sum over ids of f(element, id) exceeds
+// target(the sum over all), by the thread that has it: found(id, f there, sum).
+// CTAs' warps take consecutive runs of windows, so that the running sum is one
+// over CTAs, warps, steps of 32 windows, lanes and elements.
+template <typename T, typename F, typename G, typename H>
+__device__ __forceinline__ void search_sum(const Part<T> &part, F f, G target_of, H found, int &parity,
+                                           SearchShared &sh) {
   constexpr int E = Row<T>::E;
-  cg::cluster_group cluster = cg::this_cluster();
-  const int rank = (int)cluster.block_rank();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t top = ordered(part.m);
-  Limit keep = {0, part.row.vocab};
-  uint64_t above;
-  if (d.limited) {
-    keep.o = search_value(part, keep, false, (uint64_t)d.top_k, 0, top, above, parity, sh);
-    keep.id = search_id(part, keep.o, (uint64_t)d.top_k - above, parity, sh);
-  }
-  if (d.nucleus) {
-    uint64_t mass[1] = {0};
-    part.each([&](float z, int id) {
-      if (keep.has(ordered(z), id)) mass[0] += element_weight(element_exp(z, part.m, part.inv));
-    });
-    cluster_sum(mass, parity, sh);
-    const uint64_t f = fraction(mass[0], d.p24), cut = f > 1 ? f : 1;
-    const uint32_t o = search_value(part, keep, true, cut, keep.o, top, above, parity, sh);
-    const uint64_t w = element_weight(element_exp(unordered(o), part.m, part.inv));
-    // of the elements of value o (each of weight w > 0), those before which
-    // less than the cut lies; top-k's limit already holds among them
-    const int id = search_id(part, o, (cut - above + w - 1) / w, parity, sh);
-    keep.id = o == keep.o ? min(id, keep.id) : id;
-    keep.o = o;
-  }
-  auto kept = [&](float z, int id) -> uint64_t {
-    const float e = element_exp(z, part.m, part.inv);
-    return keep.has(ordered(z), id) && e >= d.min_p ? element_weight(e) : 0;
-  };
-  // this CTA's warps take consecutive runs of windows, so that the running sum
-  // over ids is one over CTAs, warps, steps of 32 windows, lanes and elements
-  const int per = (part.hi - part.lo + kScanWarps - 1) / (kScanWarps);
-  const int wlo = min(part.lo + warp * per, part.hi), whi = min(wlo + per, part.hi);
-  auto window = [&](int i) -> uint64_t {
-    uint64_t s = 0;
-    if (i < whi) {
-      float z[E];
-      unpack<T>(load_window(part.row, i), z);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int id = i * E - part.row.mis + e;
-        if (id >= 0 && id < part.row.vocab) s += kept(z[e], id);
-      }
-    }
-    return s;
-  };
+  const int rank = (int)cg::this_cluster().block_rank();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per = (part.hi - part.lo + kScanWarps - 1) / kScanWarps;
+  const int lo = min(part.lo + warp * per, part.hi), hi = min(lo + per, part.hi);
   uint64_t mine = 0;
-  for (int i = wlo + lane; i < whi; i += 32) mine += window(i);
+  part.each(lo + lane, hi, 32, [&](float z, int id) { mine += f(z, id); });
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
-  if (lane == 0) sh.mass[warp] = mine;
-  uint64_t total[1] = {lane == 0 ? mine : 0};
   const int at = parity;
-  cluster_sum(total, parity, sh);
-  const uint64_t target = fraction(total[0], d.u24);
+  const uint64_t total = cluster_sum(lane == 0 ? mine : 0, parity, sh);
+  const uint64_t target = target_of(total);
+  if (lane == 0) sh.red[warp] = mine;
+  __syncthreads();
   uint64_t before = 0;
-  for (int r = 0; r < rank; ++r) before += sh.slot[at][r][0];
-  for (int w = 0; w < warp; ++w) before += sh.mass[w];
+  for (int r = 0; r < rank; ++r) before += sh.slot[at][r];
+  for (int w = 0; w < warp; ++w) before += sh.red[w];
   if (target < before || target >= before + mine) return;
-  for (int i = wlo; i < whi; i += 32) {
-    const uint64_t s = window(i + lane);
+  for (int i = lo; i < hi; i += 32) {
+    float z[E];
+    uint64_t s = 0;
+    if (i + lane < hi) {
+      unpack<T>(load_window(part.row, i + lane), z);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int id = (i + lane) * E - part.row.mis + e;
+        if (id >= 0 && id < part.row.vocab) s += f(z[e], id);
+      }
+    }
     uint64_t incl = s;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -279,16 +285,11 @@ __device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int 
     if (target < before + step) {
       uint64_t b = before + incl - s;
       if (target >= b && target < b + s) {
-        float z[E];
-        unpack<T>(load_window(part.row, i + lane), z);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const int id = (i + lane) * E - part.row.mis + e;
-          const uint64_t w = id >= 0 && id < part.row.vocab ? kept(z[e], id) : 0;
-          if (target >= b && target < b + w) {
-            *token = id;
-            *logprob = logf((float)w / (float)total[0]);
-          }
+          const uint64_t w = id >= 0 && id < part.row.vocab ? f(z[e], id) : 0;
+          if (target >= b && target < b + w) found(id, w, total);
           b += w;
         }
       }
@@ -296,6 +297,55 @@ __device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int 
     }
     before += step;
   }
+}
+
+// The id up to which there are `want` elements of value o.
+template <typename T>
+__device__ __noinline__ int search_id(const Part<T> &part, uint32_t o, uint64_t want, int &parity,
+                                      SearchShared &sh) {
+  cg::cluster_group cluster = cg::this_cluster();
+  search_sum(
+      part, [&](float z, int) -> uint64_t { return ordered(z) == o; },
+      [&](uint64_t) { return want - 1; },
+      [&](int id, uint64_t, uint64_t) {
+        for (int r = 0; r < (int)cluster.num_blocks(); ++r) *cluster.map_shared_rank(&sh.bin, r) = id;
+      },
+      parity, sh);
+  cluster.sync();
+  return sh.bin;
+}
+
+// The whole request over the whole row, by all CTAs of the cluster.
+template <typename T>
+__device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int &parity,
+                                        int32_t *token, float *logprob, SearchShared &sh) {
+  Limit keep = {0, part.row.vocab};
+  uint64_t above, cut;
+  if (d.limited) {
+    keep.o = search_value(part, keep, false, (uint64_t)d.top_k, 0, above, cut, parity, sh);
+    keep.id = search_id(part, keep.o, (uint64_t)d.top_k - above, parity, sh);
+  }
+  if (d.nucleus) {
+    // of the elements of value o (each of weight w > 0), those before which less
+    // than the cut lies; top-k's limit already holds among them
+    const uint32_t o = search_value(part, keep, true, 0, d.p24, above, cut, parity, sh);
+    const uint64_t w = element_weight(element_exp(unordered(o), part.m, part.inv));
+    const int id = search_id(part, o, (cut - above + w - 1) / w, parity, sh);
+    keep.id = o == keep.o ? min(id, keep.id) : id;
+    keep.o = o;
+  }
+  search_sum(
+      part,
+      [&](float z, int id) -> uint64_t {
+        const float e = element_exp(z, part.m, part.inv);
+        return keep.has(ordered(z), id) && e >= d.min_p ? element_weight(e) : 0;
+      },
+      [&](uint64_t total) { return fraction(total, d.u24); },
+      [&](int id, uint64_t w, uint64_t total) {
+        *token = id;
+        *logprob = logf((float)w / (float)total);
+      },
+      parity, sh);
 }
 
 // The request decided at a row's leader from its n largest elements, sh.cand.
@@ -420,7 +470,7 @@ __device__ __noinline__ void finish_row(const SampleArgs &a, const Row<T> row, i
   int mode;
   while ((mode = decide(d, n, rest, ref, c, m, mass, a.tokens + t, a.logprob + t, sh, sm)) == kExactMass) {
     const Part<T> all = {row, 0, row.windows, m, d.inv};
-    all.each([&](float z, int) { mass += element_weight(element_exp(z, m, d.inv)); });
+    all.template each<1>(tid, row.windows, kScanThreads, [&](float z, int) { mass += element_weight(element_exp(z, m, d.inv)); });
     mass = block_reduce<kScanThreads>(mass, sh.red64, OpAdd());
   }
   if (mode == kSearch && tid == 0) {
@@ -481,7 +531,7 @@ __global__ void __launch_bounds__(kScanThreads, kCtas)
   });
   if constexpr (kCluster) {
     cg::this_cluster().sync();
-    search_rows(logits, stride, rows, vocab, a, *reinterpret_cast<SearchShared *>(sh.ring));
+    search_rows(logits, stride, rows, vocab, a, *reinterpret_cast<SearchShared *>(&sh));
   }
 }
 
@@ -514,7 +564,7 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
                            sizeof(SampleShared) + scan_smem(kSampleRoom, kTopKListed, kClusterMax),
                            stream, z, stride, rows, vocab, K_most, a);
   if (err != cudaSuccess || g.C > 1) return err;
-  const int clusters = 152 / kClusterMax;
+  const int clusters = 2 * 152 / kClusterMax;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = kClusterMax;
