@@ -50,6 +50,8 @@ enum SampleMode { kDone = 0, kExactMass = 1, kSearch = 2 };
 
 // What a search uses of shared memory, where the scan's was.
 constexpr int kBins = 2048;
+// Steps of 32 windows of a warp, in clusters of two and more.
+constexpr int kStepsMax = (kVocabMax / 4 / 2 / kScanWarps + 31) / 32 + 4;
 struct SearchShared {
   uint32_t hist[4][kBins];           // of a pass: weights in three parts of 14 bits, counts
   uint64_t slot[2][kClusterMax];     // each CTA's sum
@@ -59,6 +61,7 @@ struct SearchShared {
   uint32_t left[kScanWarps];         // rows that are left over, a bit each
 };
 static_assert(sizeof(SearchShared) <= sizeof(ScanShared), "the search fits the scan's memory");
+static_assert(kScanWarps * kStepsMax * 8 <= sizeof(SearchShared::hist), "the steps' sums fit the bins");
 struct SampleShared {
   uint64_t weight[kTopMax];
 };
@@ -84,8 +87,12 @@ struct Draw {  // one row's request
 __device__ __forceinline__ float element_exp(float z, float m, float inv) {
   return expf(__fmul_rn(__fsub_rn(z, m), inv));
 }
+// floor(2^40 e) of an e in [0, 1], by shifting its mantissa (a conversion to 64
+// bits takes many times as long); what lies under 2^-40 shifts out.
 __device__ __forceinline__ uint64_t element_weight(float e) {
-  return (uint64_t)__float2ull_rz(e * kWeightOne);
+  const uint32_t b = __float_as_uint(e), mantissa = (b & 0x7FFFFFu) | 0x800000u;
+  const int shift = (int)(b >> 23) - (127 + 23 - 40);
+  return shift >= 0 ? (uint64_t)mantissa << shift : (uint64_t)(mantissa >> min(-shift, 31));
 }
 
 // Sum of a whole number over the cluster; slot[parity] keeps each CTA's.
@@ -251,10 +258,35 @@ __device__ __forceinline__ void search_sum(const Part<T> &part, F f, G target_of
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = (part.hi - part.lo + kScanWarps - 1) / kScanWarps;
   const int lo = min(part.lo + warp * per, part.hi), hi = min(lo + per, part.hi);
-  uint64_t mine = 0;
-  part.each(lo + lane, hi, 32, [&](float z, int id) { mine += f(z, id); });
+  // each step's sum is kept, so that only the step of the target is read again
+  uint64_t *const steps = reinterpret_cast<uint64_t *>(sh.hist) + warp * kStepsMax;
+  auto step_sum = [&](const uint4 &v, int i) {
+    float z[E];
+    unpack<T>(v, z);
+    uint64_t s = 0;
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+    for (int e = 0; e < E; ++e) {
+      const int id = i * E - part.row.mis + e;
+      s += id >= 0 && id < part.row.vocab && i < hi ? f(z[e], id) : 0;
+    }
+    return s;
+  };
+  uint64_t mine = 0;
+  constexpr int U = 4;
+  for (int i = lo, k = 0; i < hi; i += 32 * U, k += U) {
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[u] = i + 32 * u + lane < hi ? load_window(part.row, i + 32 * u + lane) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint64_t s = step_sum(v[u], i + 32 * u + lane);
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+      if (lane == 0 && k + u < kStepsMax) steps[k + u] = s;
+      mine += s;
+    }
+  }
   const int at = parity;
   const uint64_t total = cluster_sum(lane == 0 ? mine : 0, parity, sh);
   const uint64_t target = target_of(total);
@@ -264,38 +296,26 @@ __device__ __forceinline__ void search_sum(const Part<T> &part, F f, G target_of
   for (int r = 0; r < rank; ++r) before += sh.slot[at][r];
   for (int w = 0; w < warp; ++w) before += sh.red[w];
   if (target < before || target >= before + mine) return;
-  for (int i = lo; i < hi; i += 32) {
+  int i = lo;
+  for (int k = 0; before + steps[k] <= target; ++k, i += 32) before += steps[k];
+  const uint64_t s = step_sum(i + lane < hi ? load_window(part.row, i + lane) : make_uint4(0, 0, 0, 0), i + lane);
+  uint64_t incl = s;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  uint64_t b = before + incl - s;
+  if (target >= b && target < b + s) {
     float z[E];
-    uint64_t s = 0;
-    if (i + lane < hi) {
-      unpack<T>(load_window(part.row, i + lane), z);
+    unpack<T>(load_window(part.row, i + lane), z);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int id = (i + lane) * E - part.row.mis + e;
-        if (id >= 0 && id < part.row.vocab) s += f(z[e], id);
-      }
+    for (int e = 0; e < E; ++e) {
+      const int id = (i + lane) * E - part.row.mis + e;
+      const uint64_t w = id >= 0 && id < part.row.vocab ? f(z[e], id) : 0;
+      if (target >= b && target < b + w) found(id, w, total);
+      b += w;
     }
-    uint64_t incl = s;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint64_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    const uint64_t step = __shfl_sync(0xFFFFFFFFu, incl, 31);
-    if (target < before + step) {
-      uint64_t b = before + incl - s;
-      if (target >= b && target < b + s) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int id = (i + lane) * E - part.row.mis + e;
-          const uint64_t w = id >= 0 && id < part.row.vocab ? f(z[e], id) : 0;
-          if (target >= b && target < b + w) found(id, w, total);
-          b += w;
-        }
-      }
-      return;
-    }
-    before += step;
   }
 }
 
