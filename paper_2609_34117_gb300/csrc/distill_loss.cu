@@ -41,6 +41,7 @@ struct LossArgs {
   float *row_loss;
   int vocab, K;
   float alpha, tau;
+  bool summed;  // the kernel that sums the row losses follows
 };
 
 struct LossShared {
@@ -116,7 +117,7 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   constexpr int E = Row<T>::E;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ LossShared sh;
-  pdl_launch_dependents();
+  if (a.summed) pdl_launch_dependents();
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, V = a.vocab;
@@ -425,7 +426,7 @@ cudaError_t launch_distill_loss(const void *logits, int dtype, int rows, int voc
                                 float temperature, const float *row_weight, float *row_loss,
                                 float *loss, void *grad, int64_t grad_stride, cudaStream_t stream) {
   const LossArgs a = {labels, top_ids, top_logp, log_rest, row_weight, row_loss,
-                      vocab, k, alpha, temperature};
+                      vocab, k, alpha, temperature, loss != nullptr};
   cudaError_t err = dtype == SLIMWISE_DTYPE_BF16
                         ? launch<__nv_bfloat16>(logits, rows, stride, a, grad, grad_stride, stream)
                         : launch<float>(logits, rows, stride, a, grad, grad_stride, stream);

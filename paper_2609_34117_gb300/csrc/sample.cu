@@ -15,10 +15,9 @@
 // Nearly every row is decided by its best few elements, which the scan of
 // vocab.cuh finds in the one read that bounds this kernel.  The mass of the
 // whole row, which a nucleus without top-k needs, comes from the same read as a
-// float; it decides except where the nucleus would end within that sum's error
-// bound, and then the leader sums the exact mass in a second pass.  Rows that
-// keep more than the listed elements (a wide nucleus, no filter at all) are
-// left to the end and then searched by a whole cluster: the limits of top-k and
+// float.  Rows that keep more than the listed elements (a wide nucleus, no filter
+// at all), and those few whose nucleus would end within that float's error bound,
+// are left to the end and then searched by a whole cluster: the limits of top-k and
 // top-p by a radix selection of 11 bits a pass over the row, from histograms of
 // masses and counts, then the token by a running sum over ids.  Where clusters
 // scan the rows, the same kernel does that; where single CTAs do, a second
@@ -45,8 +44,6 @@ constexpr float kWeightOne = 1099511627776.0f;  // 2^40, the largest element's w
 // of 19 roundings (8 in a window, 2 of the compensated sum, 8 + 1 over threads
 // and CTAs) 2^-19.7; the weights' truncation V 2^-40.
 constexpr uint64_t kMassError = 1 << 17;  // one part in
-
-enum SampleMode { kDone = 0, kExactMass = 1, kSearch = 2 };
 
 // What a search uses of shared memory, where the scan's was.
 constexpr int kBins = 2048;
@@ -368,12 +365,12 @@ __device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int 
       parity, sh);
 }
 
-// The request decided at a row's leader from its n largest elements, sh.cand.
-// `mass`: the mass of the whole row if known exactly, else 0; rest: the sum of
-// 2^((z - ref) c) over all other elements.  m: the row's maximum.
-__device__ __forceinline__ int decide(const Draw &d, int n, float rest, float ref, float c, float m,
-                                      uint64_t mass, int32_t *token, float *logprob,
-                                      ScanShared &sh, SampleShared &sm) {
+// The request decided at a row's leader from its n largest elements, sh.cand;
+// false if they do not decide it.  rest: the sum of 2^((z - ref) c) over all
+// other elements; m: the row's maximum.
+__device__ __forceinline__ bool decide(const Draw &d, int n, float rest, float ref, float c, float m,
+                                       int32_t *token, float *logprob, ScanShared &sh,
+                                       SampleShared &sm) {
   const int tid = threadIdx.x;
   // a few lanes for each candidate; the first of them holds it
   const int lanes = candidate_lanes(n), at = tid / lanes, sub = tid % lanes;
@@ -406,12 +403,10 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
   } else {
     // the elements that are not listed come after these; with both limits, the
     // nucleus is one of a mass that is not known here
-    if (d.limited && d.nucleus) return kSearch;
+    if (d.limited && d.nucleus) return false;
     const float last = -block_reduce<kScanThreads>(key ? -e : -INFINITY, sh.redf, OpMax());
     uint64_t low = ~0ull;
-    if (d.nucleus && mass) {
-      low = cut = fraction(mass, d.p24);
-    } else if (d.nucleus) {
+    if (d.nucleus) {
       if (key) sh.by_rank[rank] = e;
       __syncthreads();
       const float cand = block_reduce<kScanThreads>(tid < n ? sh.by_rank[tid] : 0.0f, sh.redf, OpAdd());
@@ -420,8 +415,8 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
       low = about - about / kMassError;
       cut = about + about / kMassError + 2;
     }
-    if (!(last < d.min_p) && (!d.nucleus || listed < cut)) return kSearch;
-    if (__syncthreads_or(key && rank > 0 && before >= low && before < cut)) return kExactMass;
+    if (!(last < d.min_p) && (!d.nucleus || listed < cut)) return false;
+    if (__syncthreads_or(key && rank > 0 && before >= low && before < cut)) return false;
   }
   if (cut < 1) cut = 1;
   if (!(in && before < cut && e >= d.min_p)) w = 0;
@@ -440,7 +435,7 @@ __device__ __forceinline__ int decide(const Draw &d, int n, float rest, float re
     *token = (int32_t)key_index(key);
     *logprob = logf((float)w / (float)total);
   }
-  return kDone;
+  return true;
 }
 
 // The request of row t, and how many elements to look at: all that top-k leaves,
@@ -486,14 +481,7 @@ __device__ __noinline__ void finish_row(const SampleArgs &a, const Row<T> row, i
     }
     return;
   }
-  uint64_t mass = 0;
-  int mode;
-  while ((mode = decide(d, n, rest, ref, c, m, mass, a.tokens + t, a.logprob + t, sh, sm)) == kExactMass) {
-    const Part<T> all = {row, 0, row.windows, m, d.inv};
-    all.template each<1>(tid, row.windows, kScanThreads, [&](float z, int) { mass += element_weight(element_exp(z, m, d.inv)); });
-    mass = block_reduce<kScanThreads>(mass, sh.red64, OpAdd());
-  }
-  if (mode == kSearch && tid == 0) {
+  if (!decide(d, n, rest, ref, c, m, a.tokens + t, a.logprob + t, sh, sm) && tid == 0) {
     a.tokens[t] = kLeftOver;
     a.logprob[t] = m;
   }
@@ -538,7 +526,7 @@ __global__ void __launch_bounds__(kScanThreads, kCtas)
   extern __shared__ __align__(128) unsigned char smem[];
   SampleShared &sm = *reinterpret_cast<SampleShared *>(smem);
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem + sizeof(SampleShared));
-  pdl_launch_dependents();
+  if constexpr (!kCluster) pdl_launch_dependents();  // the search kernel, which waits
   Scan<T, kCluster, true> scan(sh, kSampleRoom, K_most, logits, stride, vocab, rows);
   auto request = [&](int t, int &K, float &c, bool &sums) {
     Draw d;
