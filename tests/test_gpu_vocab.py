@@ -634,3 +634,67 @@ def test_offsets_past_32_bits():
     want = sw.slimwise_distill_loss(near, labels, *b)
     got = sw.slimwise_distill_loss(z, labels, *b, grad=z)
     assert torch.equal(got[1], want[1]) and torch.equal(z, want[2])
+
+
+def test_the_same_bits_on_every_run():
+    # rows whose lists overflow among them; many rows and few, so that single CTAs and clusters scan
+    for rows in (3, 400):
+        z = _rows(rows, 50021, torch.bfloat16, seed=44)
+        z[0] = 0.0
+        z[1] = torch.linspace(-20.0, 20.0, 50021, device=DEV).to(torch.bfloat16)
+        top = sw.slimwise_top_logits(z, 64)
+        loss = sw.slimwise_distill_loss(z, _labels(z, 1), *top)
+        for _ in range(5):
+            assert all(torch.equal(a, b) for a, b in zip(top, sw.slimwise_top_logits(z, 64)))
+            assert all(torch.equal(a, b) for a, b in
+                       zip(loss, sw.slimwise_distill_loss(z, _labels(z, 1), *top)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_top_logits_clustered(dtype):
+    # the largest elements side by side, in one warp's run or across two, over many more than fit a list
+    z = _rows(6, 131072, dtype, seed=45, scale=1.0)
+    bump = torch.linspace(20.0, 10.0, 400, device=DEV).to(dtype)
+    for t, at in enumerate((0, 131072 - 400, 16384 - 200, 65536 - 3, 4096, 77777)):
+        z[t, at:at + 400] = bump
+    for k in (8, 64, 256):
+        _check_top(z, k, 1.0)
+    _check_top(z.repeat(60, 1), 64, 1.0)
+
+
+def test_outputs_keep_their_bounds():
+    # guards around every output, at a row count that fills no block
+    rows, vocab, k = 5, 20011, 33
+    z = _rows(rows, vocab, torch.bfloat16, seed=46)
+
+    def guarded(n, dtype):
+        flat = torch.full((n + 64,), 77, dtype=dtype, device=DEV)
+        return flat, flat[32:32 + n]
+
+    made = [guarded(rows * k, torch.int32), guarded(rows * k, torch.float32), guarded(rows, torch.float32),
+            guarded(rows, torch.int32), guarded(rows, torch.float32), guarded(rows, torch.float32),
+            guarded(1, torch.float32)]
+    ids, logp, rest, tokens, lp, row, loss = [m[1] for m in made]
+    sw.slimwise_top_logits(z, k, ids=ids.view(rows, k), logp=logp.view(rows, k), log_rest=rest)
+    sw.slimwise_sample(z, torch.rand(rows, device=DEV), tokens=tokens, logprob=lp)
+    sw.slimwise_sample(z, torch.rand(rows, device=DEV), top_p=torch.full((rows,), 0.9, device=DEV),
+                       tokens=tokens, logprob=lp)
+    sw.slimwise_distill_loss(z, _labels(z, 1), ids.view(rows, k), logp.view(rows, k), rest, row_loss=row,
+                             loss=loss)
+    for flat, view in made:
+        n = view.numel()
+        assert bool((flat[:32] == 77).all()) and bool((flat[32 + n:] == 77).all())
+
+
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_sample_wide_sets_in_any_batch(rows):
+    # left-over rows are searched by clusters of another size where other numbers of rows are scanned
+    z = _rows(8, 30011, torch.bfloat16, seed=47)
+    u = torch.rand(8, generator=_gen(48), device=DEV)
+    p = torch.tensor([1.0, 0.9, 0.99, 0.5, 1.0, 0.9, 0.3, 0.95], device=DEV)
+    k = torch.tensor([0, 0, 5000, 700, 20, 0, 0, 97], dtype=torch.int32, device=DEV)
+    one = [sw.slimwise_sample(z[i:i + 1], u[i:i + 1], top_p=p[i:i + 1], top_k=k[i:i + 1]) for i in range(8)]
+    pick = torch.arange(rows, device=DEV) % 8
+    tokens, lp = sw.slimwise_sample(z[pick], u[pick], top_p=p[pick], top_k=k[pick])
+    for i in range(rows):
+        assert torch.equal(tokens[i:i + 1], one[i % 8][0]) and torch.equal(lp[i:i + 1], one[i % 8][1]), i
