@@ -239,6 +239,10 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
       "l"(src), "r"(bytes), "r"(bar)
       : "memory");
 }
+// Bulk copy of whole windows into L2.
+__device__ __forceinline__ void bulk_prefetch(const void *src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
+}
 // Waits for a copy; false after a second without it.
 __device__ __forceinline__ bool wait_copy(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
