@@ -31,6 +31,9 @@ namespace slimwise {
 // once.  256 rows of 150001 fp32 take 38 us with three and 46 with four, 512 of
 // 262144 bf16 73 and 67: three as long as they hold all rows.
 constexpr int kFewCtas = 3, kManyCtas = 4;
+// Of the search: with all of 512 rows of 131072 bf16 left over (a nucleus of 0.9
+// of nearly flat rows), two took 2.0 ms, three 1.7, four 1.3.
+constexpr int kSearchCtas = 4;
 constexpr int kNucleus = 32;      // elements looked at for a nucleus or min-p without top-k
 constexpr int kSampleRoom = 128;  // of a warp's list
 constexpr int kTopKListed = kSampleRoom - 32;  // largest top-k that is decided from the list
@@ -544,7 +547,7 @@ __global__ void __launch_bounds__(kScanThreads, kCtas)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kScanThreads)
+__global__ void __launch_bounds__(kScanThreads, kSearchCtas)
     sample_search_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab,
                          const __grid_constant__ SampleArgs a) {
   __shared__ SearchShared search;
@@ -572,7 +575,7 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
                            sizeof(SampleShared) + scan_smem(kSampleRoom, kTopKListed, kClusterMax),
                            stream, z, stride, rows, vocab, K_most, a);
   if (err != cudaSuccess || g.C > 1) return err;
-  const int clusters = 2 * 152 / kClusterMax;
+  const int clusters = kSearchCtas * 152 / kClusterMax;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = kClusterMax;
