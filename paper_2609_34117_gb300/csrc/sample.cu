@@ -39,14 +39,17 @@ constexpr int kSampleRoom = 128;  // of a warp's list
 constexpr int kTopKListed = kSampleRoom - 32;  // largest top-k that is decided from the list
 constexpr int32_t kLeftOver = -2; // a token that is still to be searched (its logprob: the maximum)
 constexpr float kWeightOne = 1099511627776.0f;  // 2^40, the largest element's weight
-// Bound of the relative difference between the scan's float mass and the sum of
-// the weights.  Elements at 2^-x of the largest hold a share of at most
-// V 2^-x, so exponents beyond 19 do not count; to there, an exponent rounded
-// three times in each of the two and a logarithm's base rounded twice make
-// 19 (1.5 2^-23 + 2^-23) ln 2 < 2^-18.3; exp2's and exp's own 2^-22, and sums
-// of 19 roundings (8 in a window, 2 of the compensated sum, 8 + 1 over threads
-// and CTAs) 2^-19.7; the weights' truncation V 2^-40.
-constexpr uint64_t kMassError = 1 << 17;  // one part in
+// Bound of the relative difference between the scan's float sum of the elements
+// that are not listed and the sum of their weights (but for the weights'
+// truncation, one part in 2^40 each).  An element at 2^-x of the largest weighs
+// less than its truncation beyond x = 40, and elements there or at lesser depths
+// have exponents that are rounded three times in the one and twice in the other,
+// logarithm's base and quotient included: 40 (1.5 2^-23 + 2^-23) ln 2 < 2^-16.8;
+// exp2's and exp's own 2^-22, and sums of 19 roundings (8 in a unit, 2 of the
+// compensated sum, 8 + 1 over threads and CTAs) 2^-19.7; and 2^-22 more each time
+// that a warp's reference is raised, at most 5 + 48 times (48 cuts of a list: 3072
+// units of a warp, 64 between two cuts): 2^-15.3 in all.
+constexpr uint64_t kMassError = 1 << 15;  // one part in
 
 // What a search uses of shared memory, where the scan's was.
 constexpr int kBins = 2048;
@@ -372,7 +375,7 @@ __device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int 
 // false if they do not decide it.  rest: the sum of 2^((z - ref) c) over all
 // other elements; m: the row's maximum.
 __device__ __forceinline__ bool decide(const Draw &d, int n, float rest, float ref, float c, float m,
-                                       int32_t *token, float *logprob, ScanShared &sh,
+                                       int vocab, int32_t *token, float *logprob, ScanShared &sh,
                                        SampleShared &sm) {
   const int tid = threadIdx.x;
   // a few lanes for each candidate; the first of them holds it
@@ -410,13 +413,11 @@ __device__ __forceinline__ bool decide(const Draw &d, int n, float rest, float r
     const float last = -block_reduce<kScanThreads>(key ? -e : -INFINITY, sh.redf, OpMax());
     uint64_t low = ~0ull;
     if (d.nucleus) {
-      if (key) sh.by_rank[rank] = e;
-      __syncthreads();
-      const float cand = block_reduce<kScanThreads>(tid < n ? sh.by_rank[tid] : 0.0f, sh.redf, OpAdd());
-      // the share in whole numbers, and the error bound around it
-      const uint64_t about = fraction(__float2ull_rz(fmaf(rest, ex2((ref - m) * c), cand) * kWeightOne), d.p24);
-      low = about - about / kMassError;
-      cut = about + about / kMassError + 2;
+      // the mass: the listed elements', which are all the largest, and about the rest's
+      const uint64_t about = __float2ull_rz(rest * ex2((ref - m) * c) * kWeightOne);
+      const uint64_t error = about / kMassError + (uint64_t)vocab + 2;
+      low = fraction(listed + about - min(about, error), d.p24);
+      cut = fraction(listed + about + error, d.p24) + 1;
     }
     if (!(last < d.min_p) && (!d.nucleus || listed < cut)) return false;
     if (__syncthreads_or(key && rank > 0 && before >= low && before < cut)) return false;
@@ -484,7 +485,7 @@ __device__ __noinline__ void finish_row(const SampleArgs &a, const Row<T> row, i
     }
     return;
   }
-  if (!decide(d, n, rest, ref, c, m, a.tokens + t, a.logprob + t, sh, sm) && tid == 0) {
+  if (!decide(d, n, rest, ref, c, m, row.vocab, a.tokens + t, a.logprob + t, sh, sm) && tid == 0) {
     a.tokens[t] = kLeftOver;
     a.logprob[t] = m;
   }
@@ -530,7 +531,7 @@ __global__ void __launch_bounds__(kScanThreads, kCtas)
   SampleShared &sm = *reinterpret_cast<SampleShared *>(smem);
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem + sizeof(SampleShared));
   if constexpr (!kCluster) pdl_launch_dependents();  // the search kernel, which waits
-  Scan<T, kCluster, true> scan(sh, kSampleRoom, K_most, logits, stride, vocab, rows);
+  Scan<T, kCluster, true, false> scan(sh, kSampleRoom, K_most, logits, stride, vocab, rows);
   auto request = [&](int t, int &K, float &c, bool &sums) {
     Draw d;
     request_of(a, t, vocab, d, K);
