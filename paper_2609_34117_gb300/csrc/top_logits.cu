@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   extern __shared__ __align__(128) unsigned char smem[];
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem);
   const int tid = threadIdx.x;
-  Scan<T, kCluster, false> scan(sh, list_room(K), K, logits, stride, vocab, rows);
+  Scan<T, kCluster, false, true> scan(sh, list_room(K), K, logits, stride, vocab, rows);
   auto request = [&](int, int &k, float &cc, bool &sums) {
     k = K;
     cc = c;
@@ -83,14 +83,15 @@ template <typename T>
 static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t stride, int k,
                               float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), list_room(k), k, kTopCtas, 0);
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), list_room(k), k, kTopCtas, wide_smem(k));
   const auto launch = g.C > 1 ? launch_clusters<top_logits_kernel<T, true>, const T *, int64_t, int, int, int,
                                                 float, int32_t *, float *, float *>
                               : launch_clusters<top_logits_kernel<T, false>, const T *, int64_t, int, int, int,
                                                 float, int32_t *, float *, float *>;
-  return launch(g.clusters, g.C, kScanThreads, scan_smem(list_room(k), k, g.C),
-                scan_smem(list_room(kTopMax), kTopMax, kClusterMax), stream, static_cast<const T *>(logits), stride, rows, vocab, k,
-                kLog2e / temperature, ids, logp, log_rest);
+  return launch(g.clusters, g.C, kScanThreads, scan_smem(list_room(k), k, g.C) + wide_smem(k),
+                scan_smem(list_room(kTopMax), kTopMax, kClusterMax) + wide_smem(kTopMax), stream,
+                static_cast<const T *>(logits), stride, rows, vocab, k, kLog2e / temperature, ids, logp,
+                log_rest);
 }
 
 cudaError_t launch_top_logits(const void *logits, int dtype, int rows, int vocab, int64_t stride,

@@ -388,6 +388,11 @@ constexpr uint32_t kStageBytes = kWarpStep * 16;
 static_assert(kScanStages == 2, "the stage at hand is the one or the other");
 constexpr int kClusterMax = 8;
 constexpr int kStage = 32;
+// Candidates that a CTA holds to pick from if they are more than it passes on (K
+// above 64: the groups are then no more than twice the K wanted, and a threshold
+// lets 1.5 to 2 K through on most rows; picked from where they lie, the 1181 rows
+// of 22705 bf16 at K = 256 take 108 us, through most_of_many() 151).
+constexpr int kWide = 3 * kTopMax;
 static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
 
 // Candidates that a CTA passes on: the K best and others, if there are no more
@@ -434,6 +439,8 @@ inline size_t scan_smem(int room, int K, int C) {
   return sizeof(ScanShared) + (size_t)kScanWarps * room * sizeof(Listed) +
          (C > 1 ? (size_t)(C > 4 ? C : 4) * candidate_cap(K) * 8 : 0);
 }
+// What follows that: the candidates that are too many to pass on.
+inline size_t wide_smem(int K) { return K > 64 ? kWide * 8 : 0; }
 
 // The bits of v from bit `from` (up to 64) up.
 __device__ __forceinline__ uint64_t high_bits(uint64_t v, int from) {
@@ -591,13 +598,15 @@ __device__ __forceinline__ int candidate_lanes(int n) {
 // kCluster: rows are split over the CTAs of a cluster (else the cluster is one CTA).
 // kSumless: scan() can leave out the sums (of the 400 instructions of a step,
 // 120); s is then 0, or NaN where the row has NaN.
-template <typename T, bool kCluster, bool kSumless>
+// kHoldWide: wide_smem(K_most) bytes follow the lists.
+template <typename T, bool kCluster, bool kSumless, bool kHoldWide>
 struct Scan {
   static constexpr int E = Row<T>::E;
   static constexpr uint32_t kGrain = sizeof(T) == 2 ? 0xFFFFu : 0x1FFFu;  // a bf16's step; 2^-10 of an fp32
   ScanShared &sh;
   Listed *list;        // this warp's
   uint64_t *recv;
+  uint64_t *wide;
   int room, recv_cap;  // of a warp's list; of a CTA's part of recv
   const T *logits;
   int64_t stride;
@@ -643,6 +652,7 @@ struct Scan {
     Listed *const lists = reinterpret_cast<Listed *>(&sh + 1);
     list = lists + warp * room;
     recv = reinterpret_cast<uint64_t *>(lists + kScanWarps * room);
+    wide = kHoldWide && K_most > 64 ? recv + (kCluster ? max(C, 4) * recv_cap : 0) : nullptr;
     put_at = smem_u32(&sh.ring[warp][0][lane]);
     stage = 0;
     // a lane's windows are read in an order that keeps 8 lanes off each other's banks
@@ -923,14 +933,29 @@ struct Scan {
       total += sh.part[turn][w];
       units += sh.count[w];
     }
-    if (total > most) return most_of_many(row, dst, most, fill, units);
+    const bool many = total > most;
+    if (many && (!kHoldWide || !wide || total > kWide)) return most_of_many(row, dst, most, fill, units);
     s += add;
+    uint64_t *const to = kHoldWide && many ? wide : dst;
     if (held <= kStage) {
-      if (lane < held) dst[before + lane] = sh.stage[warp][lane];
+      if (lane < held) to[before + lane] = sh.stage[warp][lane];
     } else {
       held = 0;
       float again = 0.0f;
-      pass([&](int at, float z, int id) { dst[before + held + at] = make_key(z, (uint32_t)id); }, again);
+      pass([&](int at, float z, int id) { to[before + held + at] = make_key(z, (uint32_t)id); }, again);
+    }
+    if (kHoldWide && many) {
+      __syncthreads();
+      constexpr int kKeys = kWide / kScanThreads;
+      uint64_t k[kKeys];
+      int mine = 0;
+#pragma unroll
+      for (int j = 0; j < kKeys; ++j) {
+        const int i = j * kScanThreads + (int)threadIdx.x;
+        k[j] = i < total ? wide[i] : 0;
+        mine += i < total;
+      }
+      return emit(k, mine, most, dst, fill);
     }
     for (int i = total + (int)threadIdx.x; i < fill; i += kScanThreads) dst[i] = 0;
     return total;
