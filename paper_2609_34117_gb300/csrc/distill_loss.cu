@@ -34,7 +34,8 @@ constexpr int kSliceMax = 200 * 1024;               // bytes of a row that one C
 constexpr int kAhead = 2;                            // steps that the loss alone prefetches
 constexpr int kChunksMax = kSliceMax / (kChunk * 16) + 1;
 static_assert(kTopMax <= kLossThreads, "one thread per list entry");
-constexpr int kLaneParts = kClusterMax * kLossWarps / 32;  // of the cluster's warps, a lane's
+constexpr int kLossCluster = 16;                     // most CTAs of a row
+constexpr int kLaneParts = kLossCluster * kLossWarps / 32;  // of the cluster's warps, a lane's
 
 struct LossArgs {
   const int32_t *labels, *top_ids;
@@ -46,11 +47,10 @@ struct LossArgs {
 };
 
 struct LossShared {
-  float4 part[kClusterMax * kLossWarps];  // each warp's reference, sum for p, sum for q
   int id[kTopMax];                        // the list: ids (-1: absent), logits, log P and P
   float z[kTopMax], lp[kTopMax], p[kTopMax];
   uint64_t bar[kChunksMax];
-  uint64_t parts;                         // counts the bytes of part
+  uint64_t parts;                         // counts the bytes of the cluster's warps' sums
 };
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -111,6 +111,23 @@ __device__ __forceinline__ void store_window(T *g, const Row<T> &row, int i,
   }
 }
 
+// The 16 bytes that start `at` bytes into two neighbouring windows, 0 < at < 16
+// and a multiple of the element's size; `at` is the same for all threads.
+template <typename T>
+__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int at) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (at & 8)
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+  if (at & 4)
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  if (sizeof(T) == 2 && at & 2)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // kTemp: tau is not 1, so that p and q are two softmaxes.
 template <typename T, bool kGrad, bool kTemp>
 __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
@@ -146,6 +163,8 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   // a word of bits for each thread and step: 8 for each of its windows
   uint4 *const slice = reinterpret_cast<uint4 *>(smem);
   uint32_t *const bits = reinterpret_cast<uint32_t *>(smem + (kGrad ? (size_t)per * 16 : 0));
+  // each warp's reference, sum for p, sum for q, of the cluster's warps
+  float4 *const parts = reinterpret_cast<float4 *>(bits + (per + kChunk - 1) / kChunk * kLossThreads);
   const int chunks = (hi - lo + kChunk - 1) / kChunk;
   if (tid == 0) {
     mbar_init(smem_u32(&sh.parts), 1);
@@ -245,7 +264,7 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   }
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (lane < C) {
-    const uint32_t to = mapa_shared(smem_u32(&sh.part[rank * kLossWarps + (tid >> 5)]), lane);
+    const uint32_t to = mapa_shared(smem_u32(&parts[rank * kLossWarps + (tid >> 5)]), lane);
     asm volatile(
         "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
         "f"(ref), "f"(s1), "f"(s2), "f"(0.0f), "r"(mapa_shared(smem_u32(&sh.parts), lane))
@@ -261,7 +280,8 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
 #pragma unroll
   for (int j = 0; j < kLaneParts; ++j) {
     const int i = lane + 32 * j;
-    part[j] = i < C * kLossWarps ? sh.part[i] : make_float4(kFloorRef, 0.0f, 0.0f, 0.0f);
+    part[j] = make_float4(kFloorRef, 0.0f, 0.0f, 0.0f);
+    if (i < C * kLossWarps) part[j] = parts[i];
     z_top = fmaxf(z_top, part[j].x);
   }
   for (int i = lane; i < a.K; i += 32) z_top = fmaxf(z_top, sh.z[i]);
@@ -269,6 +289,7 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   float rest1 = 0.0f, rest2 = 0.0f;
 #pragma unroll
   for (int j = 0; j < kLaneParts; ++j) {
+    if (32 * j >= C * kLossWarps) break;
     rest1 += part[j].y * exp_from(part[j].x, ref, c1);
     if constexpr (kTemp) rest2 += part[j].z * exp_from(part[j].x, ref, c2);
   }
@@ -314,36 +335,50 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
       if constexpr (kTemp) v = fmaf(B, exp_from(x, ref, c2), v);
       return v;
     };
-    if (alike) {
-      const uint64_t mr = pair(-ref, -ref), cc1 = pair(c1, c1), cc2 = pair(c2, c2);
-      const uint64_t AA = pair(A, A), BB = pair(B, B);
-      auto window = [&](int i, auto put) {
-        constexpr int P = E / 2;
-        uint64_t p[P];
-        unpack_pairs<T>(slice[i - lo], p);
-        float f[E];
+    const uint64_t mr = pair(-ref, -ref), cc1 = pair(c1, c1), cc2 = pair(c2, c2);
+    const uint64_t AA = pair(A, A), BB = pair(B, B);
+    auto window = [&](uint4 v, auto put) {
+      constexpr int P = E / 2;
+      uint64_t p[P];
+      unpack_pairs<T>(v, p);
+      float f[E];
 #pragma unroll
-        for (int q = 0; q < P; ++q) {
-          uint64_t v = mul2(AA, exp2_pair(p[q], mr, cc1));
-          if constexpr (kTemp) v = add2(v, mul2(BB, exp2_pair(p[q], mr, cc2)));
-          split(v, f[2 * q], f[2 * q + 1]);
-        }
-        put(f);
-      };
+      for (int q = 0; q < P; ++q) {
+        uint64_t v = mul2(AA, exp2_pair(p[q], mr, cc1));
+        if constexpr (kTemp) v = add2(v, mul2(BB, exp2_pair(p[q], mr, cc2)));
+        split(v, f[2 * q], f[2 * q + 1]);
+      }
+      put(f);
+    };
+    if (alike) {
       const int from = max(lo, row.whole_lo), to = min(hi, row.whole_lo + row.whole_n);
       uint4 *const gw = reinterpret_cast<uint4 *>(g - row.mis);
 #pragma unroll 4
       for (int i = from + tid; i < to; i += kLossThreads)
-        window(i, [&](const float (&f)[E]) { gw[i] = packed<T>(f); });
+        window(slice[i - lo], [&](const float (&f)[E]) { gw[i] = packed<T>(f); });
       // the row's partial windows
       for (int i = tid; i < 2; i += kLossThreads) {
         const int at = i ? row.windows - 1 : 0;
         if (at >= lo && at < hi && !row.whole(at))
-          window(at, [&](const float (&f)[E]) { store_window(g, row, at, f); });
+          window(slice[at - lo], [&](const float (&f)[E]) { store_window(g, row, at, f); });
       }
     } else {
-      const T *const from = reinterpret_cast<const T *>(slice) + row.mis - lo * E;
-      for (int i = id_lo + tid; i < id_hi; i += kLossThreads) store(g + i, outside(to_float(from[i])));
+      // windows of the gradient, each from two of the logits', and the elements
+      // before and after them (4096 rows of 131072 bf16: 373 us, an element at a
+      // time 402; gradients of the same alignment 350)
+      const int before = min((int)((16 - (reinterpret_cast<uintptr_t>(g + id_lo) & 15)) & 15) / (int)sizeof(T),
+                             max(id_hi - id_lo, 0));
+      const int from = id_lo + before, n = max(id_hi - from, 0) / E;
+      const int first = from + row.mis - lo * E, at = first % E * (int)sizeof(T);
+      const uint4 *const src = slice + first / E;
+      uint4 *const gw = reinterpret_cast<uint4 *>(g + from);
+#pragma unroll 2
+      for (int i = tid; i < n; i += kLossThreads)
+        window(shifted<T>(src[i], src[i + 1], at), [&](const float (&f)[E]) { gw[i] = packed<T>(f); });
+      const T *const part = reinterpret_cast<const T *>(slice) + row.mis - lo * E;
+      const int after = max(id_hi - from, 0) - n * E;
+      if (tid < before) store(g + id_lo + tid, outside(to_float(part[id_lo + tid])));
+      if (tid < after) store(g + from + n * E + tid, outside(to_float(part[from + n * E + tid])));
     }
     // then the list's elements and the label
     __syncthreads();
@@ -380,24 +415,30 @@ __global__ void __launch_bounds__(1024)
   }
 }
 
-// Shared memory of a CTA that takes `per` windows.
-static size_t loss_smem(int per, bool grad) {
-  return (grad ? (size_t)per * 16 : 0) + (size_t)(per + kChunk - 1) / kChunk * kLossThreads * 4;
+// Shared memory of a CTA that takes `per` windows, one of C of a row.
+static size_t loss_smem(int per, int C, bool grad) {
+  return (grad ? (size_t)per * 16 : 0) + (size_t)(per + kChunk - 1) / kChunk * kLossThreads * 4 +
+         (size_t)C * kLossWarps * sizeof(float4);
 }
 // CTAs of a row.  With the gradient, the number that lets the CTAs of an SM hold
 // the most of their rows at once: at 131072 bf16, parts of 65 KB three to an SM
-// took 363 us for 4096 rows, 44 KB four 385, 33 KB five 392, 87 KB two 413.  Each
-// CTA also costs its row's exchange: the fewest that come within a few percent.
+// took 363 us for 4096 rows, 44 KB four 385, 33 KB five 392, 87 KB two 413.  One
+// CTA alone on an SM does not read while it writes (380000 bf16, 512 rows: parts
+// of 190 KB 179 us, of 95 KB 152), and two less than three (1000 rows of 128256
+// fp32: 2 x 100 KB 177, 3 x 63 KB 168): they count for 9/10.  Each CTA also costs
+// its row's exchange: the fewest that come within a few percent.
 // Where few rows leave SMs idle, more.
 static int loss_ctas(int rows, int windows, bool grad) {
   int best = 1;
   if (grad) {
     size_t most = 0;
-    for (int C = 1; C <= kClusterMax; ++C) {
+    for (int C = 1; C <= kLossCluster; ++C) {
       const int per = (windows + C - 1) / C;
       if (per * 16 > kSliceMax) continue;
-      const int ctas = (int)(228 * 1024 / (loss_smem(per, true) + sizeof(LossShared) + 1024));
-      const size_t held = (size_t)(ctas < kGradCtas ? ctas : kGradCtas) * per;
+      const int ctas = (int)(228 * 1024 / (loss_smem(per, C, true) + sizeof(LossShared) + 1024));
+      if (ctas < 2) continue;
+      size_t held = (size_t)(ctas < kGradCtas ? ctas : kGradCtas) * per;
+      if (ctas == 2) held -= held / 10;
       if (held > most + most / 32) {
         most = held;
         best = C;
@@ -416,9 +457,9 @@ static cudaError_t launch(const void *logits, int rows, int64_t stride, const Lo
   constexpr int E = Row<T>::E;
   const int windows = (a.vocab + 2 * E - 2) / E;  // the most that a row can cover
   const int C = loss_ctas(rows, windows, kGrad);
-  return launch_clusters<distill_loss_kernel<T, kGrad, kTemp>>(rows, C, kLossThreads,
-                         loss_smem((windows + C - 1) / C, kGrad),
-                         loss_smem(kSliceMax / 16, true), stream, static_cast<const T *>(logits),
+  return launch_clusters<distill_loss_kernel<T, kGrad, kTemp>, kGrad>(rows, C, kLossThreads,
+                         loss_smem((windows + C - 1) / C, C, kGrad),
+                         loss_smem(kSliceMax / 16, kLossCluster, true), stream, static_cast<const T *>(logits),
                          stride, a, static_cast<T *>(grad), grad_stride);
 }
 

@@ -568,9 +568,9 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
   const SampleArgs a = {temperature, top_k, top_p, min_p, uniform, tokens, logprob};
   const T *const z = static_cast<const T *>(logits);
   const auto launch =
-      g.C > 1 ? launch_clusters<sample_kernel<T, true, kFewCtas>, const T *, int64_t, int, int, int, SampleArgs>
-      : many  ? launch_clusters<sample_kernel<T, false, kManyCtas>, const T *, int64_t, int, int, int, SampleArgs>
-              : launch_clusters<sample_kernel<T, false, kFewCtas>, const T *, int64_t, int, int, int, SampleArgs>;
+      g.C > 1 ? launch_clusters<sample_kernel<T, true, kFewCtas>, false, const T *, int64_t, int, int, int, SampleArgs>
+      : many  ? launch_clusters<sample_kernel<T, false, kManyCtas>, false, const T *, int64_t, int, int, int, SampleArgs>
+              : launch_clusters<sample_kernel<T, false, kFewCtas>, false, const T *, int64_t, int, int, int, SampleArgs>;
   cudaError_t err = launch(g.clusters, g.C, kScanThreads,
                            sizeof(SampleShared) + scan_smem(kSampleRoom, K_most, g.C),
                            sizeof(SampleShared) + scan_smem(kSampleRoom, kTopKListed, kClusterMax),

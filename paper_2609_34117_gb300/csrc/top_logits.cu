@@ -84,9 +84,9 @@ static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t s
                               float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
   const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), list_room(k), k, kTopCtas, wide_smem(k));
-  const auto launch = g.C > 1 ? launch_clusters<top_logits_kernel<T, true>, const T *, int64_t, int, int, int,
+  const auto launch = g.C > 1 ? launch_clusters<top_logits_kernel<T, true>, false, const T *, int64_t, int, int, int,
                                                 float, int32_t *, float *, float *>
-                              : launch_clusters<top_logits_kernel<T, false>, const T *, int64_t, int, int, int,
+                              : launch_clusters<top_logits_kernel<T, false>, false, const T *, int64_t, int, int, int,
                                                 float, int32_t *, float *, float *>;
   return launch(g.clusters, g.C, kScanThreads, scan_smem(list_room(k), k, g.C) + wide_smem(k),
                 scan_smem(list_room(kTopMax), kTopMax, kClusterMax) + wide_smem(kTopMax), stream,

@@ -35,7 +35,8 @@ constexpr float kFloorRef = -FLT_MAX;
 // attribute, one value per kernel, set on its first launch on a device and again
 // after a launch that failed (a context that was reset has lost it); smem: this
 // launch's.
-template <auto kKernel, typename... A>
+// Clusters of more than 8 CTAs are asked for with kWideClusters.
+template <auto kKernel, bool kWideClusters = false, typename... A>
 inline cudaError_t launch_clusters(int clusters, int C, int threads, size_t smem, size_t smem_max,
                                    cudaStream_t stream, A... args) {
   static std::atomic<uint64_t> ready{0};  // a bit for each device
@@ -46,6 +47,9 @@ inline cudaError_t launch_clusters(int clusters, int C, int threads, size_t smem
   if (!(ready.load(std::memory_order_acquire) & bit)) {
     err = cudaFuncSetAttribute(reinterpret_cast<const void *>(kKernel),
                                cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
+    if (err == cudaSuccess && kWideClusters)
+      err = cudaFuncSetAttribute(reinterpret_cast<const void *>(kKernel),
+                                 cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (err != cudaSuccess) return err;
     ready.fetch_or(bit, std::memory_order_release);
   }

@@ -238,6 +238,30 @@ def test_distill_loss_rows_that_start_anywhere(pad, start, gpad, gstart, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+@pytest.mark.parametrize("vocab,gpad,gstart", [(3, 2, 1), (17, 0, 3), (70001, 3, 1), (262147, 7, 5), (393216, 1, 0)])
+def test_distill_loss_gradient_rows_of_another_alignment(vocab, gpad, gstart, tau, dtype):
+    rows = 3
+    z = _rows(rows, vocab, dtype, seed=15)
+    args = (_labels(z, 3),) + _targets(z, min(64, vocab - 1), tau, 4)
+    want = sw.slimwise_distill_loss(z, *args, alpha=0.1, temperature=tau)
+    flat = torch.full((gstart + rows * (vocab + gpad) + 64,), 7.0, dtype=dtype, device=DEV)
+    g = flat[gstart:gstart + rows * (vocab + gpad)].view(rows, vocab + gpad)
+    got = _check_loss(z, *args, alpha=0.1, tau=tau, grad=g[:, :vocab])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert bool((flat[:gstart] == 7.0).all()) and bool((flat[gstart + rows * (vocab + gpad):] == 7.0).all())
+    assert bool((g[:, vocab:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [20000, 236985, 300007, 393216])
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+def test_distill_loss_long_rows_over_many_ctas(vocab, tau, dtype):
+    z = _rows(160, vocab, dtype, seed=16)
+    _check_loss(z, _labels(z, 3), *_targets(z, 64, tau, 4), alpha=0.1, tau=tau)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("vocab", [1000, 70001])
 @pytest.mark.parametrize("tau", [1.0, 2.0])
 def test_distill_loss_in_place(vocab, dtype, tau):
