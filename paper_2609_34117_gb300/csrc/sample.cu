@@ -53,8 +53,8 @@ constexpr uint64_t kMassError = 1 << 15;  // one part in
 
 // What a search uses of shared memory, where the scan's was.
 constexpr int kBins = 2048;
-// Steps of 32 windows of a warp, in clusters of two and more.
-constexpr int kStepsMax = (kVocabMax / 4 / 2 / kScanWarps + 31) / 32 + 4;
+// Steps of 4 x 32 windows of a warp, in clusters of two and more.
+constexpr int kStepsMax = (kVocabMax / 4 / 2 / kScanWarps + 127) / 128 + 1;
 struct SearchShared {
   uint32_t hist[4][kBins];           // of a pass: weights in three parts of 14 bits, counts
   uint64_t slot[2][kClusterMax];     // each CTA's sum
@@ -133,11 +133,11 @@ struct Part {
         if (i + u * step >= end) break;
         float z[E];
         unpack<T>(v[u], z);
+        const int id0 = (i + u * step) * E - row.mis;
+        const bool whole = row.whole(i + u * step);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int id = (i + u * step) * E - row.mis + e;
-          if (id >= 0 && id < row.vocab) f(z[e], id);
-        }
+        for (int e = 0; e < E; ++e)
+          if (whole || (id0 + e >= 0 && id0 + e < row.vocab)) f(z[e], id0 + e);
       }
     }
   }
@@ -155,11 +155,52 @@ struct Limit {
   __device__ __forceinline__ bool has(uint32_t v, int i) const { return v > o || (v == o && i <= id); }
 };
 
+// What the elements of a row count for in a running sum: (z, id), and a whole
+// window's from id0 on.
+struct EqualTo {  // one if they are o, as ordered()
+  uint32_t o;
+  __device__ __forceinline__ uint64_t operator()(float z, int) const { return ordered(z) == o; }
+  template <int E>
+  __device__ __forceinline__ uint64_t window(const float (&z)[E], int) const {
+    uint32_t n = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) n += ordered(z[e]) == o;
+    return n;
+  }
+};
+struct KeptWeight {  // their weights, if they are kept
+  Limit keep;
+  bool limited;  // keep leaves any out
+  float m, inv, min_p;
+  __device__ __forceinline__ float kept(float z, int id) const {
+    const float e = element_exp(z, m, inv);
+    return (!limited || keep.has(ordered(z), id)) && e >= min_p ? e : 0.0f;
+  }
+  __device__ __forceinline__ uint64_t operator()(float z, int id) const { return element_weight(kept(z, id)); }
+  // floor(2^40 e) as two whole numbers of 20 bits, which a sum with 2^23, rounded
+  // down, leaves in a float's low bits: floor(2^20 e), and that of the remainder,
+  // which is exact.  Half as many instructions as the shift to 64 bits takes.
+  template <int E>
+  __device__ __forceinline__ uint64_t window(const float (&z)[E], int id0) const {
+    constexpr float kUnit = 1048576.0f, kOnes = 8388608.0f;
+    uint32_t high = 0, low = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float k = kept(z[e], id0 + e), h = __fmaf_rd(k, kUnit, kOnes);
+      const float l = __fmaf_rd(__fmaf_rn(k, kUnit, kOnes - h), kUnit, kOnes);
+      high += __float_as_uint(h);
+      low += __float_as_uint(l);
+    }
+    constexpr uint32_t kBias = 0x4B000000u * E;  // (modulo 2^32)
+    return ((uint64_t)(high - kBias) << 20) + (low - kBias);
+  }
+};
+
 // The largest value v (as ordered()) with amount(values >= v within `in`) at
 // least `want`, and in `above` the amount of the values > v.  Amounts are weights
 // (`mass`) or counts.  want 0: the share p24 of the whole amount; cut: that wanted.
 template <typename T>
-__device__ __noinline__ uint32_t search_value(const Part<T> &part, Limit in, bool mass, uint64_t want,
+__device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, bool mass, uint64_t want,
                                               uint64_t p24, uint64_t &above, uint64_t &cut, int &parity,
                                               SearchShared &sh) {
   cg::cluster_group cluster = cg::this_cluster();
@@ -252,10 +293,10 @@ __device__ __noinline__ uint32_t search_value(const Part<T> &part, Limit in, boo
 // The first id at which the running sum over ids of f(element, id) exceeds
 // target(the sum over all), by the thread that has it: found(id, f there, sum).
 // CTAs' warps take consecutive runs of windows, so that the running sum is one
-// over CTAs, warps, steps of 32 windows, lanes and elements.
+// over CTAs, warps, steps of 4 x 32 windows, those 4, lanes and elements.
 template <typename T, typename F, typename G, typename H>
-__device__ __forceinline__ void search_sum(const Part<T> &part, F f, G target_of, H found, int &parity,
-                                           SearchShared &sh) {
+__device__ __forceinline__ void search_sum(const Part<T> &part, const F f, G target_of, H found,
+                                           int &parity, SearchShared &sh) {
   constexpr int E = Row<T>::E;
   const int rank = (int)cg::this_cluster().block_rank();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -263,32 +304,31 @@ __device__ __forceinline__ void search_sum(const Part<T> &part, F f, G target_of
   const int lo = min(part.lo + warp * per, part.hi), hi = min(lo + per, part.hi);
   // each step's sum is kept, so that only the step of the target is read again
   uint64_t *const steps = reinterpret_cast<uint64_t *>(sh.hist) + warp * kStepsMax;
-  auto step_sum = [&](const uint4 &v, int i) {
+  auto window_sum = [&](const uint4 &v, int i) {
     float z[E];
     unpack<T>(v, z);
+    const int id0 = i * E - part.row.mis;
+    if (i < hi && part.row.whole(i)) return f.window(z, id0);
     uint64_t s = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int id = i * E - part.row.mis + e;
-      s += id >= 0 && id < part.row.vocab && i < hi ? f(z[e], id) : 0;
-    }
+    for (int e = 0; e < E; ++e)
+      s += id0 + e >= 0 && id0 + e < part.row.vocab && i < hi ? f(z[e], id0 + e) : 0;
     return s;
   };
+  auto load = [&](int i) { return i < hi ? load_window(part.row, i) : make_uint4(0, 0, 0, 0); };
   uint64_t mine = 0;
   constexpr int U = 4;
-  for (int i = lo, k = 0; i < hi; i += 32 * U, k += U) {
+  for (int i = lo, k = 0; i < hi; i += 32 * U, ++k) {
     uint4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      v[u] = i + 32 * u + lane < hi ? load_window(part.row, i + 32 * u + lane) : make_uint4(0, 0, 0, 0);
+    for (int u = 0; u < U; ++u) v[u] = load(i + 32 * u + lane);
+    uint64_t s = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      uint64_t s = step_sum(v[u], i + 32 * u + lane);
+    for (int u = 0; u < U; ++u) s += window_sum(v[u], i + 32 * u + lane);
 #pragma unroll
-      for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-      if (lane == 0 && k + u < kStepsMax) steps[k + u] = s;
-      mine += s;
-    }
+    for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (lane == 0) steps[k] = s;
+    mine += s;
   }
   const int at = parity;
   const uint64_t total = cluster_sum(lane == 0 ? mine : 0, parity, sh);
@@ -300,35 +340,39 @@ __device__ __forceinline__ void search_sum(const Part<T> &part, F f, G target_of
   for (int w = 0; w < warp; ++w) before += sh.red[w];
   if (target < before || target >= before + mine) return;
   int i = lo;
-  for (int k = 0; before + steps[k] <= target; ++k, i += 32) before += steps[k];
-  const uint64_t s = step_sum(i + lane < hi ? load_window(part.row, i + lane) : make_uint4(0, 0, 0, 0), i + lane);
-  uint64_t incl = s;
+  for (int k = 0; before + steps[k] <= target; ++k, i += 32 * U) before += steps[k];
+  for (int u = 0; u < U; ++u, i += 32) {
+    const uint4 v = load(i + lane);
+    const uint64_t s = window_sum(v, i + lane);
+    uint64_t incl = s;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint64_t v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-    if (lane >= o) incl += v;
-  }
-  uint64_t b = before + incl - s;
-  if (target >= b && target < b + s) {
-    float z[E];
-    unpack<T>(load_window(part.row, i + lane), z);
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t more = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += more;
+    }
+    uint64_t b = before + incl - s;
+    before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+    if (target >= b && target < b + s) {
+      float z[E];
+      unpack<T>(v, z);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int id = (i + lane) * E - part.row.mis + e;
-      const uint64_t w = id >= 0 && id < part.row.vocab ? f(z[e], id) : 0;
-      if (target >= b && target < b + w) found(id, w, total);
-      b += w;
+      for (int e = 0; e < E; ++e) {
+        const int id = (i + lane) * E - part.row.mis + e;
+        const uint64_t w = id >= 0 && id < part.row.vocab ? f(z[e], id) : 0;
+        if (target >= b && target < b + w) found(id, w, total);
+        b += w;
+      }
     }
   }
 }
 
 // The id up to which there are `want` elements of value o.
 template <typename T>
-__device__ __noinline__ int search_id(const Part<T> &part, uint32_t o, uint64_t want, int &parity,
+__device__ __noinline__ int search_id(const Part<T> part, uint32_t o, uint64_t want, int &parity,
                                       SearchShared &sh) {
   cg::cluster_group cluster = cg::this_cluster();
   search_sum(
-      part, [&](float z, int) -> uint64_t { return ordered(z) == o; },
+      part, EqualTo{o},
       [&](uint64_t) { return want - 1; },
       [&](int id, uint64_t, uint64_t) {
         for (int r = 0; r < (int)cluster.num_blocks(); ++r) *cluster.map_shared_rank(&sh.bin, r) = id;
@@ -340,7 +384,7 @@ __device__ __noinline__ int search_id(const Part<T> &part, uint32_t o, uint64_t 
 
 // The whole request over the whole row, by all CTAs of the cluster.
 template <typename T>
-__device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int &parity,
+__device__ __noinline__ void search_row(const Part<T> part, const Draw d, int &parity,
                                         int32_t *token, float *logprob, SearchShared &sh) {
   Limit keep = {0, part.row.vocab};
   uint64_t above, cut;
@@ -358,11 +402,7 @@ __device__ __noinline__ void search_row(const Part<T> &part, const Draw &d, int 
     keep.o = o;
   }
   search_sum(
-      part,
-      [&](float z, int id) -> uint64_t {
-        const float e = element_exp(z, part.m, part.inv);
-        return keep.has(ordered(z), id) && e >= d.min_p ? element_weight(e) : 0;
-      },
+      part, KeptWeight{keep, d.limited || d.nucleus, part.m, part.inv, d.min_p},
       [&](uint64_t total) { return fraction(total, d.u24); },
       [&](int id, uint64_t w, uint64_t total) {
         *token = id;
