@@ -17,12 +17,12 @@
 // whole row, which a nucleus without top-k needs, comes from the same read as a
 // float.  Rows that keep more than the listed elements (a wide nucleus, no filter
 // at all), and those few whose nucleus would end within that float's error bound,
-// are left to the end and then searched by a whole cluster: the limits of top-k and
-// top-p by a radix selection of 11 bits a pass over the row, from histograms of
-// masses and counts, then the token by a running sum over ids.  Where clusters
-// scan the rows, the same kernel does that; where single CTAs do, a second
-// kernel, so that a left-over row still gets a cluster and the first keeps four
-// CTAs on an SM.
+// are left to the end and then searched by a whole cluster, or by a CTA each where
+// they are many: the limits of top-k and top-p by a radix selection of 11 bits a
+// pass over the row, from histograms of masses and counts, then the token by a
+// running sum over ids.  Where clusters scan the rows, the same kernel does that;
+// where single CTAs do, a second kernel, so that a left-over row still gets a
+// cluster and the first keeps four CTAs on an SM.
 #include "vocab.cuh"
 
 namespace slimwise {
@@ -31,8 +31,9 @@ namespace slimwise {
 // once.  256 rows of 150001 fp32 take 38 us with three and 46 with four, 512 of
 // 262144 bf16 73 and 67: three as long as they hold all rows.
 constexpr int kFewCtas = 3, kManyCtas = 4;
-// Of the search: with all of 512 rows of 131072 bf16 left over (a nucleus of 0.9
-// of nearly flat rows), two took 2.0 ms, three 1.7, four 1.3.
+// Of the search: with all of 512 rows of 131072 bf16 left over, no filter takes 242
+// us with two, 284 with three, 176 with four and 253 with five; a nucleus of 0.9
+// of nearly flat rows 1320, 1585, 1037 and 1587.
 constexpr int kSearchCtas = 4;
 constexpr int kNucleus = 32;      // elements looked at for a nucleus or min-p without top-k
 constexpr int kSampleRoom = 128;  // of a warp's list
@@ -53,10 +54,15 @@ constexpr uint64_t kMassError = 1 << 15;  // one part in
 
 // What a search uses of shared memory, where the scan's was.
 constexpr int kBins = 2048;
-// Steps of 4 x 32 windows of a warp, in clusters of two and more.
-constexpr int kStepsMax = (kVocabMax / 4 / 2 / kScanWarps + 127) / 128 + 1;
+// Rows left over in a cluster's share from which each is searched by one CTA: 608
+// rows of 32000 fp32 without a filter (8 a cluster) take 102 us so and 220 by
+// clusters, 512 of 131072 bf16 (6 or 7) 234 and 263; 380 of 131072 fp32 (5) 241
+// and 224.
+constexpr int kAloneFrom = 6;
+// Steps of 4 x 32 windows of a warp.
+constexpr int kStepsMax = (kVocabMax / 4 / kScanWarps + 127) / 128 + 1;
 struct SearchShared {
-  uint32_t hist[4][kBins];           // of a pass: weights in three parts of 14 bits, counts
+  uint32_t hist[2][kBins];           // of a pass: counts, or sums of weights in two halves
   uint64_t slot[2][kClusterMax];     // each CTA's sum
   uint64_t red[kScanWarps];
   uint64_t above;                    // result of a pass, written by the CTA that found it
@@ -98,16 +104,27 @@ __device__ __forceinline__ uint64_t element_weight(float e) {
   return shift >= 0 ? (uint64_t)mantissa << shift : (uint64_t)(mantissa >> min(-shift, 31));
 }
 
-// Sum of a whole number over the cluster; slot[parity] keeps each CTA's.
-__device__ __forceinline__ uint64_t cluster_sum(uint64_t v, int &parity, SearchShared &sh) {
-  cg::cluster_group cluster = cg::this_cluster();
-  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+// The CTAs that search a row: all of a cluster, or one of it.
+struct Team {
+  int C, rank;  // CTAs, this one's place
+  __device__ __forceinline__ void sync() const {
+    if (C > 1) cg::this_cluster().sync();
+    else __syncthreads();
+  }
+  template <typename V>
+  __device__ __forceinline__ V *of(V *p, int r) const {
+    return C > 1 ? cg::this_cluster().map_shared_rank(p, r) : p;
+  }
+};
+
+// Sum of a whole number over the team; slot[parity] keeps each CTA's.
+__device__ __forceinline__ uint64_t team_sum(const Team team, uint64_t v, int &parity, SearchShared &sh) {
   const int tid = threadIdx.x;
   v = block_reduce<kScanThreads>(v, sh.red, OpAdd());
-  if (tid < C) *cluster.map_shared_rank(&sh.slot[parity][rank], tid) = v;
-  cluster.sync();
+  if (tid < team.C) *team.of(&sh.slot[parity][team.rank], tid) = v;
+  team.sync();
   v = 0;
-  for (int r = 0; r < C; ++r) v += sh.slot[parity][r];
+  for (int r = 0; r < team.C; ++r) v += sh.slot[parity][r];
   parity ^= 1;
   return v;
 }
@@ -116,34 +133,50 @@ __device__ __forceinline__ uint64_t cluster_sum(uint64_t v, int &parity, SearchS
 template <typename T>
 struct Part {
   Row<T> row;
+  Team team;
   int lo, hi;
   float m, inv;
-  // f(element, id) of windows from, from + step, ... below end, by this thread,
-  // U loads at a time.
-  template <int U = 4, typename F>
-  __device__ __forceinline__ void each(int from, int end, int step, F f) const {
-    constexpr int E = Row<T>::E;
-    for (int i = from; i < end; i += U * step) {
-      uint4 v[U];
+  // f(window, its number) of windows i, i + step, ... of U (none beyond end: of
+  // -inf), all loaded before the first f; f's code is there once.
+  static constexpr int U = 4;
+  template <typename F>
+  __device__ __forceinline__ void batch(int i, int step, int end, F f) const {
+    uint4 v[U];
+    const uint32_t none = neg_inf_bits(row.p);
+    if (i >= row.whole_lo && i + (U - 1) * step < min(end, row.whole_lo + row.whole_n)) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i + u * step < end) v[u] = load_window(row, i + u * step);
+      for (int u = 0; u < U; ++u) v[u] = ld_global_v4(row.w + i + u * step);
+    } else {
 #pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = make_uint4(none, none, none, none);
+#pragma unroll 1
       for (int u = 0; u < U; ++u) {
-        if (i + u * step >= end) break;
-        float z[E];
-        unpack<T>(v[u], z);
-        const int id0 = (i + u * step) * E - row.mis;
-        const bool whole = row.whole(i + u * step);
+        const uint4 w = i + u * step < end ? load_window(row, i + u * step) : make_uint4(none, none, none, none);
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (whole || (id0 + e >= 0 && id0 + e < row.vocab)) f(z[e], id0 + e);
+        for (int x = 0; x < U; ++x)
+          if (x == u) v[x] = w;
       }
     }
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) {
+      f(v[0], i + u * step);
+#pragma unroll
+      for (int x = 0; x + 1 < U; ++x) v[x] = v[x + 1];
+    }
   }
+  // f(element, id) of all elements of this CTA's part.  (Elements beside the row
+  // are -inf: they weigh nothing, and come with ids outside the row.)
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    each(lo + (int)threadIdx.x, hi, kScanThreads, f);
+    constexpr int E = Row<T>::E;
+    for (int i = lo + (int)threadIdx.x; i < hi; i += U * kScanThreads)
+      batch(i, kScanThreads, hi, [&](const uint4 &v, int at) {
+        float z[E];
+        unpack<T>(v, z);
+        const int id0 = at * E - row.mis;
+#pragma unroll
+        for (int e = 0; e < E; ++e) f(z[e], id0 + e);
+      });
   }
 };
 
@@ -157,14 +190,17 @@ struct Limit {
 
 // What the elements of a row count for in a running sum: (z, id), and a whole
 // window's from id0 on.
-struct EqualTo {  // one if they are o, as ordered()
+struct EqualTo {  // one if they are o, as ordered(), and in the row
   uint32_t o;
-  __device__ __forceinline__ uint64_t operator()(float z, int) const { return ordered(z) == o; }
+  int vocab;
+  __device__ __forceinline__ uint64_t operator()(float z, int id) const {
+    return ordered(z) == o && (unsigned)id < (unsigned)vocab;
+  }
   template <int E>
-  __device__ __forceinline__ uint64_t window(const float (&z)[E], int) const {
+  __device__ __forceinline__ uint64_t window(const float (&z)[E], int id0) const {
     uint32_t n = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) n += ordered(z[e]) == o;
+    for (int e = 0; e < E; ++e) n += (*this)(z[e], id0 + e) ? 1 : 0;
     return n;
   }
 };
@@ -203,32 +239,31 @@ template <typename T>
 __device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, bool mass, uint64_t want,
                                               uint64_t p24, uint64_t &above, uint64_t &cut, int &parity,
                                               SearchShared &sh) {
-  cg::cluster_group cluster = cg::this_cluster();
-  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const Team team = part.team;
+  const int C = team.C, rank = team.rank;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = kBins / C, mine = per / kScanThreads;  // bins of a CTA, of a thread
   uint32_t prefix = 0;
   above = 0;
   for (int known = 32; known > (sizeof(T) == 2 ? 16 : 0);) {
     const int shift = max(known - 11, sizeof(T) == 2 ? 16 : 0);  // (a bf16 has 16 bits)
-    for (int i = tid; i < 4 * kBins; i += kScanThreads) (&sh.hist[0][0])[i] = 0;
+    for (int i = tid; i < 2 * kBins; i += kScanThreads) (&sh.hist[0][0])[i] = 0;
     __syncthreads();
     part.each([&](float z, int id) {
       const uint32_t o = ordered(z);
-      if (!in.has(o, id) || (known < 32 && (o ^ prefix) >> known)) return;
+      if (!in.has(o, id) || (known < 32 && (o ^ prefix) >> known) || (unsigned)id >= (unsigned)part.row.vocab) return;
       const uint32_t bin = (o >> shift) & ((1u << (known - shift)) - 1u);
       if (mass) {
         const uint64_t w = element_weight(element_exp(z, part.m, part.inv));
-        if (w & 0x3FFF) atomicAdd(&sh.hist[0][bin], (uint32_t)(w & 0x3FFF));
-        if (w >> 14) {
-          atomicAdd(&sh.hist[1][bin], (uint32_t)(w >> 14 & 0x3FFF));
-          atomicAdd(&sh.hist[2][bin], (uint32_t)(w >> 28));
-        }
+        // a sum of 64 bits in two, by hand: few weights have a high half
+        const uint32_t low = (uint32_t)w, was = low ? atomicAdd(&sh.hist[0][bin], low) : 0;
+        const uint32_t high = (uint32_t)(w >> 32) + (was + low < was);
+        if (high) atomicAdd(&sh.hist[1][bin], high);
       } else {
-        atomicAdd(&sh.hist[3][bin], 1u);
+        atomicAdd(&sh.hist[0][bin], 1u);
       }
     });
-    cluster.sync();
+    team.sync();
     // CTA r joins bins r per .. of all CTAs, each thread `mine` of them
     const int first = rank * per + tid * mine;
     uint64_t amount[kBins / kScanThreads], sum = 0;
@@ -237,9 +272,8 @@ __device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, bool
       amount[j] = 0;
       if (j < mine)
         for (int r = 0; r < C; ++r) {
-          const uint32_t *const h = cluster.map_shared_rank(&sh.hist[0][first + j], r);
-          amount[j] += mass ? (uint64_t)h[0] + ((uint64_t)h[kBins] << 14) + ((uint64_t)h[2 * kBins] << 28)
-                            : (uint64_t)h[3 * kBins];
+          const uint32_t *const h = team.of(&sh.hist[0][first + j], r);
+          amount[j] += h[0] + ((uint64_t)h[kBins] << 32);
         }
       sum += amount[j];
     }
@@ -257,8 +291,8 @@ __device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, bool
       if (w > warp) over += sh.red[w];
       total += sh.red[w];
     }
-    if (tid < C) *cluster.map_shared_rank(&sh.slot[parity][rank], tid) = total;
-    cluster.sync();
+    if (tid < C) *team.of(&sh.slot[parity][rank], tid) = total;
+    team.sync();
     uint64_t all = 0;
     for (int r = 0; r < C; ++r) {
       if (r > rank) over += sh.slot[parity][r];
@@ -275,12 +309,12 @@ __device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, bool
       if (j >= mine) continue;
       if (over < want && want <= over + amount[j])
         for (int r = 0; r < C; ++r) {
-          *cluster.map_shared_rank(&sh.above, r) = over;
-          *cluster.map_shared_rank(&sh.bin, r) = first + j;
+          *team.of(&sh.above, r) = over;
+          *team.of(&sh.bin, r) = first + j;
         }
       over += amount[j];
     }
-    cluster.sync();
+    team.sync();
     prefix |= (uint32_t)sh.bin << shift;
     above += sh.above;
     want -= sh.above;
@@ -298,7 +332,7 @@ template <typename T, typename F, typename G, typename H>
 __device__ __forceinline__ void search_sum(const Part<T> &part, const F f, G target_of, H found,
                                            int &parity, SearchShared &sh) {
   constexpr int E = Row<T>::E;
-  const int rank = (int)cg::this_cluster().block_rank();
+  const int rank = part.team.rank;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = (part.hi - part.lo + kScanWarps - 1) / kScanWarps;
   const int lo = min(part.lo + warp * per, part.hi), hi = min(lo + per, part.hi);
@@ -307,31 +341,20 @@ __device__ __forceinline__ void search_sum(const Part<T> &part, const F f, G tar
   auto window_sum = [&](const uint4 &v, int i) {
     float z[E];
     unpack<T>(v, z);
-    const int id0 = i * E - part.row.mis;
-    if (i < hi && part.row.whole(i)) return f.window(z, id0);
-    uint64_t s = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      s += id0 + e >= 0 && id0 + e < part.row.vocab && i < hi ? f(z[e], id0 + e) : 0;
-    return s;
+    return f.window(z, i * E - part.row.mis);
   };
-  auto load = [&](int i) { return i < hi ? load_window(part.row, i) : make_uint4(0, 0, 0, 0); };
   uint64_t mine = 0;
-  constexpr int U = 4;
+  constexpr int U = Part<T>::U;
   for (int i = lo, k = 0; i < hi; i += 32 * U, ++k) {
-    uint4 v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load(i + 32 * u + lane);
     uint64_t s = 0;
-#pragma unroll
-    for (int u = 0; u < U; ++u) s += window_sum(v[u], i + 32 * u + lane);
+    part.batch(i + lane, 32, hi, [&](const uint4 &v, int at) { s += window_sum(v, at); });
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
     if (lane == 0) steps[k] = s;
     mine += s;
   }
   const int at = parity;
-  const uint64_t total = cluster_sum(lane == 0 ? mine : 0, parity, sh);
+  const uint64_t total = team_sum(part.team, lane == 0 ? mine : 0, parity, sh);
   const uint64_t target = target_of(total);
   if (lane == 0) sh.red[warp] = mine;
   __syncthreads();
@@ -341,9 +364,8 @@ __device__ __forceinline__ void search_sum(const Part<T> &part, const F f, G tar
   if (target < before || target >= before + mine) return;
   int i = lo;
   for (int k = 0; before + steps[k] <= target; ++k, i += 32 * U) before += steps[k];
-  for (int u = 0; u < U; ++u, i += 32) {
-    const uint4 v = load(i + lane);
-    const uint64_t s = window_sum(v, i + lane);
+  part.batch(i + lane, 32, hi, [&](const uint4 &v, int at) {
+    const uint64_t s = window_sum(v, at);
     uint64_t incl = s;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -357,32 +379,31 @@ __device__ __forceinline__ void search_sum(const Part<T> &part, const F f, G tar
       unpack<T>(v, z);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int id = (i + lane) * E - part.row.mis + e;
-        const uint64_t w = id >= 0 && id < part.row.vocab ? f(z[e], id) : 0;
-        if (target >= b && target < b + w) found(id, w, total);
+        const uint64_t w = f(z[e], at * E - part.row.mis + e);
+        if (target >= b && target < b + w) found(at * E - part.row.mis + e, w, total);
         b += w;
       }
     }
-  }
+  });
 }
 
 // The id up to which there are `want` elements of value o.
 template <typename T>
 __device__ __noinline__ int search_id(const Part<T> part, uint32_t o, uint64_t want, int &parity,
                                       SearchShared &sh) {
-  cg::cluster_group cluster = cg::this_cluster();
+  const Team team = part.team;
   search_sum(
-      part, EqualTo{o},
+      part, EqualTo{o, part.row.vocab},
       [&](uint64_t) { return want - 1; },
       [&](int id, uint64_t, uint64_t) {
-        for (int r = 0; r < (int)cluster.num_blocks(); ++r) *cluster.map_shared_rank(&sh.bin, r) = id;
+        for (int r = 0; r < team.C; ++r) *team.of(&sh.bin, r) = id;
       },
       parity, sh);
-  cluster.sync();
+  team.sync();
   return sh.bin;
 }
 
-// The whole request over the whole row, by all CTAs of the cluster.
+// The whole request over the whole row, by all CTAs of the team.
 template <typename T>
 __device__ __noinline__ void search_row(const Part<T> part, const Draw d, int &parity,
                                         int32_t *token, float *logprob, SearchShared &sh) {
@@ -531,8 +552,9 @@ __device__ __noinline__ void finish_row(const SampleArgs &a, const Row<T> row, i
   }
 }
 
-// The rows of this cluster that were left over, searched by all its CTAs.
-template <typename T>
+// The rows of this cluster that were left over: a few are searched by all its
+// CTAs, one after the other; if they are many (kAlone), by a CTA each.
+template <typename T, bool kAlone>
 __device__ __forceinline__ void search_rows(const T *logits, int64_t stride, int rows, int vocab,
                                             const SampleArgs &a, SearchShared &sh) {
   cg::cluster_group cluster = cg::this_cluster();
@@ -545,20 +567,27 @@ __device__ __forceinline__ void search_rows(const T *logits, int64_t stride, int
     const bool left = mine < rows && __ldcg(a.tokens + mine) == kLeftOver;
     const uint32_t mask = __ballot_sync(0xFFFFFFFFu, left);
     if ((tid & 31) == 0) sh.left[tid >> 5] = mask;
-    if (!__syncthreads_or(left)) continue;
+    const int n = __syncthreads_count(left);
+    if (n == 0) continue;
+    const bool alone = kAlone && n >= kAloneFrom;
+    const Team team = {alone ? 1 : C, alone ? 0 : rank};
+    if (alone) cluster.sync();
+    int turn = 0;
     for (int w = 0; w < kScanWarps; ++w)
       for (uint32_t bits = sh.left[w]; bits; bits &= bits - 1) {
+        if (alone && turn++ % C != rank) continue;
         const int t = base + (32 * w + __ffs((int)bits) - 1) * clusters;
         Draw d;
         int K;
         request_of(a, t, vocab, d, K);
-        Part<T> part = {Row<T>(logits + (int64_t)t * stride, vocab), 0, 0, __ldcg(a.logprob + t), d.inv};
-        const int per = (part.row.windows + C - 1) / C;
-        part.lo = min(rank * per, part.row.windows);
+        Part<T> part = {Row<T>(logits + (int64_t)t * stride, vocab), team, 0, 0, __ldcg(a.logprob + t), d.inv};
+        const int per = (part.row.windows + team.C - 1) / team.C;
+        part.lo = min(team.rank * per, part.row.windows);
         part.hi = min(part.lo + per, part.row.windows);
         search_row(part, d, parity, a.tokens + t, a.logprob + t, sh);
+        __syncthreads();  // the next row's bins lie where this one's steps are read
       }
-    __syncthreads();
+    if (alone) cluster.sync();  // before others write here again
   }
   cluster.sync();  // no CTA ends while its sums can still be read or written
 }
@@ -583,7 +612,7 @@ __global__ void __launch_bounds__(kScanThreads, kCtas)
   });
   if constexpr (kCluster) {
     cg::this_cluster().sync();
-    search_rows(logits, stride, rows, vocab, a, *reinterpret_cast<SearchShared *>(&sh));
+    search_rows<T, false>(logits, stride, rows, vocab, a, *reinterpret_cast<SearchShared *>(&sh));
   }
 }
 
@@ -593,7 +622,7 @@ __global__ void __launch_bounds__(kScanThreads, kSearchCtas)
                          const __grid_constant__ SampleArgs a) {
   __shared__ SearchShared search;
   pdl_wait_primary();
-  search_rows(logits, stride, rows, vocab, a, search);
+  search_rows<T, true>(logits, stride, rows, vocab, a, search);
 }
 
 template <typename T>

@@ -140,16 +140,15 @@ struct Row {
 __device__ __forceinline__ uint32_t neg_inf_bits(const __nv_bfloat16 *) { return 0xFF80FF80u; }
 __device__ __forceinline__ uint32_t neg_inf_bits(const float *) { return 0xFF800000u; }
 
+__device__ __forceinline__ uint4 ld_global_v4(const uint4 *p) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
 // Window i of the row, -inf outside the row.
 template <typename T>
 __device__ __forceinline__ uint4 load_window(const Row<T> &r, int i) {
-  if (r.whole(i)) {
-    uint4 v;
-    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "l"(r.w + i));
-    return v;
-  }
+  if (r.whole(i)) return ld_global_v4(r.w + i);
   constexpr int E = Row<T>::E;
   uint32_t u[4];
 #pragma unroll

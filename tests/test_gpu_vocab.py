@@ -722,3 +722,35 @@ def test_sample_wide_sets_in_any_batch(rows):
     tokens, lp = sw.slimwise_sample(z[pick], u[pick], top_p=p[pick], top_k=k[pick])
     for i in range(rows):
         assert torch.equal(tokens[i:i + 1], one[i % 8][0]) and torch.equal(lp[i:i + 1], one[i % 8][1]), i
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [3001, 30011])
+def test_sample_many_rows_that_are_left_over(vocab, dtype):
+    # many of them are searched by a CTA each, a few by a cluster, and none of it shows
+    z = _rows(8, vocab, dtype, seed=49)
+    u = torch.rand(8, generator=_gen(50), device=DEV)
+    p = torch.tensor([1.0, 0.9, 0.99, 0.5, 1.0, 0.9, 0.3, 0.95], device=DEV)
+    k = torch.tensor([0, 0, 1500, 700, 0, 1000, 0, 97], dtype=torch.int32, device=DEV)
+    one = [sw.slimwise_sample(z[i:i + 1], u[i:i + 1], top_p=p[i:i + 1], top_k=k[i:i + 1]) for i in range(8)]
+    want = [torch.cat([o[j] for o in one]) for j in range(2)]
+    for rows in (500, 1300):
+        pick = torch.arange(rows, device=DEV) * 5 % 8
+        for _ in range(3):
+            tokens, lp = sw.slimwise_sample(z[pick], u[pick], top_p=p[pick], top_k=k[pick])
+            assert torch.equal(tokens, want[0][pick]) and torch.equal(lp, want[1][pick])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,rows", [(393216, 1), (393216, 500), (1025, 700)])
+def test_sample_equal_logits(vocab, rows, dtype):
+    # every weight is 2^40: the first ids up to the share p, each as likely
+    z = torch.full((rows, vocab), 2.5, dtype=dtype, device=DEV)
+    u = torch.rand(rows, generator=_gen(51), device=DEV)
+    p = torch.rand(rows, generator=_gen(52), device=DEV)
+    tokens, lp = sw.slimwise_sample(z, u, top_p=p)
+    part = lambda mass, f: mass * int(float(f) * 2 ** 24) >> 24
+    for i, (got, a, b, l) in enumerate(zip(tokens.tolist(), u.tolist(), p.tolist(), lp.tolist())):
+        kept = max(-(-part(vocab << 40, b) // (1 << 40)), 1)
+        assert got == part(kept << 40, a) >> 40, i
+        assert abs(l + math.log(kept)) <= 2.0 ** -20 * (1 + math.log(kept)), i
