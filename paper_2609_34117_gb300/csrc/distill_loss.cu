@@ -128,8 +128,9 @@ __device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int at) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// kTemp: tau is not 1, so that p and q are two softmaxes.
-template <typename T, bool kGrad, bool kTemp>
+// kTemp: tau is not 1, so that p and q are two softmaxes.  kAlike: the gradient's
+// rows are aligned as the logits' (the code for others costs 1% beside them).
+template <typename T, bool kGrad, bool kTemp, bool kAlike>
 __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
     distill_loss_kernel(const T *logits, int64_t stride, LossArgs a, T *grad, int64_t grad_stride) {
   constexpr int E = Row<T>::E;
@@ -146,8 +147,8 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   const int lo = min(rank * per, row.windows), hi = min(lo + per, row.windows);
   const int id_lo = max(lo * E - row.mis, 0), id_hi = min(hi * E - row.mis, V);
   T *const g = kGrad ? grad + t * grad_stride : nullptr;
-  // gradient rows that start like the logits' are written in whole windows
-  const bool alike = kGrad && ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(row.p)) & 15) == 0;
+  // gradient rows that start like the logits' are written in the same windows
+  const bool alike = kAlike || ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(row.p)) & 15) == 0;
   if (label < 0) {  // not trained on
     if (rank == 0 && tid == 0) a.row_loss[t] = 0.0f;
     if constexpr (kGrad) {
@@ -451,13 +452,13 @@ static int loss_ctas(int rows, int windows, bool grad) {
   return best;
 }
 
-template <typename T, bool kGrad, bool kTemp>
+template <typename T, bool kGrad, bool kTemp, bool kAlike>
 static cudaError_t launch(const void *logits, int rows, int64_t stride, const LossArgs &a,
                           void *grad, int64_t grad_stride, cudaStream_t stream) {
   constexpr int E = Row<T>::E;
   const int windows = (a.vocab + 2 * E - 2) / E;  // the most that a row can cover
   const int C = loss_ctas(rows, windows, kGrad);
-  return launch_clusters<distill_loss_kernel<T, kGrad, kTemp>, kGrad>(rows, C, kLossThreads,
+  return launch_clusters<distill_loss_kernel<T, kGrad, kTemp, kAlike>, kGrad>(rows, C, kLossThreads,
                          loss_smem((windows + C - 1) / C, C, kGrad),
                          loss_smem(kSliceMax / 16, kLossCluster, true), stream, static_cast<const T *>(logits),
                          stride, a, static_cast<T *>(grad), grad_stride);
@@ -467,10 +468,16 @@ template <typename T>
 static cudaError_t launch(const void *logits, int rows, int64_t stride, const LossArgs &a,
                           void *grad, int64_t grad_stride, cudaStream_t stream) {
   const bool temp = a.tau != 1.0f;
-  return grad ? temp ? launch<T, true, true>(logits, rows, stride, a, grad, grad_stride, stream)
-                     : launch<T, true, false>(logits, rows, stride, a, grad, grad_stride, stream)
-         : temp ? launch<T, false, true>(logits, rows, stride, a, grad, grad_stride, stream)
-                : launch<T, false, false>(logits, rows, stride, a, grad, grad_stride, stream);
+  if (!grad)
+    return temp ? launch<T, false, true, true>(logits, rows, stride, a, grad, grad_stride, stream)
+                : launch<T, false, false, true>(logits, rows, stride, a, grad, grad_stride, stream);
+  const bool alike = (reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(grad)) % 16 == 0 &&
+                     (stride - grad_stride) * (int64_t)sizeof(T) % 16 == 0;
+  if (alike)
+    return temp ? launch<T, true, true, true>(logits, rows, stride, a, grad, grad_stride, stream)
+                : launch<T, true, false, true>(logits, rows, stride, a, grad, grad_stride, stream);
+  return temp ? launch<T, true, true, false>(logits, rows, stride, a, grad, grad_stride, stream)
+              : launch<T, true, false, false>(logits, rows, stride, a, grad, grad_stride, stream);
 }
 
 cudaError_t launch_distill_loss(const void *logits, int dtype, int rows, int vocab, int64_t stride,
