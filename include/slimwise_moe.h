@@ -380,7 +380,9 @@ int slimwise_moe_device_status(const void *workspace, void *stream,
  * They need no workspace, keep no state, and do not synchronise.  What only
  * the device can see (a NaN logit, an id outside the vocabulary) is reported
  * in that row's results, as each entry point says.  The results of a row do
- * not depend on the other rows of the call.
+ * not depend on what the other rows hold.  How many they are decides how a row
+ * is split, and so the last bits of a sum in floats; a sampled token and its
+ * log-probability are the same in any batch.
  */
 enum { SLIMWISE_DTYPE_BF16 = 0, SLIMWISE_DTYPE_FP32 = 1 };
 

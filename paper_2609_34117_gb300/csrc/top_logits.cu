@@ -8,7 +8,17 @@
 //
 // The mass of the others is summed over them, not taken as 1 - the list's: a
 // teacher that is nearly sure leaves 1e-6, which the difference would not hold.
-// Bound by the one read of the logits (vocab.cuh has the scan).
+//
+// One read of the logits (vocab.cuh has the scan), a few hundred bytes written a
+// row.  4096 rows of 131072 bf16, K = 64: 223 us, 4.8 TB/s (0.71 of a copy), with
+// the schedulers issuing in 79 % of the cycles: bound by its instructions, 12.5 a
+// warp and 32 elements, of which a step's exponentials and sums are 3.6 and the
+// rest the maxima, copies, lists, thresholds and a row's end.  511 rows of 150001
+// fp32: 70 us, 4.3 TB/s; 511 rows on 152 SMs leave some with four and some with
+// three, which alone takes 54.  One row of 131072 bf16: 13 us, the latency of a
+// launch, 8 CTAs' scan and the leader's join.  Above K = 64 the lists of K units a
+// warp leave room for three CTAs on an SM, from about 160 for two (1181 rows of
+// 22705 bf16, K = 256: 108 us).
 #include "vocab.cuh"
 
 namespace slimwise {
