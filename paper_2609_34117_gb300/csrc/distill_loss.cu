@@ -271,11 +271,13 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
     sh.p[tid] = id >= 0 ? expf(lp) : 0.0f;
   }
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  // (with zy, so that it has been read when another CTA may write over it in place;
+  // the list's logits are in shared memory by now)
   if (lane < C) {
     const uint32_t to = mapa_shared(smem_u32(&parts[rank * kLossWarps + (tid >> 5)]), lane);
     asm volatile(
         "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
-        "f"(ref), "f"(s1), "f"(s2), "f"(0.0f), "r"(mapa_shared(smem_u32(&sh.parts), lane))
+        "f"(ref), "f"(s1), "f"(s2), "f"(zy), "r"(mapa_shared(smem_u32(&sh.parts), lane))
         : "memory");
   }
   __syncthreads();  // the list
