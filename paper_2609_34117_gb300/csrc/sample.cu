@@ -640,7 +640,7 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
                           float *logprob, cudaStream_t stream) {
   const int K_most = top_k ? kTopKListed : kNucleus;
   const bool many = rows > 152 * kFewCtas;
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleRoom, K_most,
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleRoom, K_most, false,
                                many ? kManyCtas : kFewCtas, sizeof(SampleShared));
   const SampleArgs a = {temperature, top_k, top_p, min_p, uniform, tokens, logprob};
   const T *const z = static_cast<const T *>(logits);
@@ -649,8 +649,8 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
       : many  ? launch_clusters<sample_kernel<T, false, kManyCtas>, false, const T *, int64_t, int, int, int, SampleArgs>
               : launch_clusters<sample_kernel<T, false, kFewCtas>, false, const T *, int64_t, int, int, int, SampleArgs>;
   cudaError_t err = launch(g.clusters, g.C, kScanThreads,
-                           sizeof(SampleShared) + scan_smem(kSampleRoom, K_most, g.C),
-                           sizeof(SampleShared) + scan_smem(kSampleRoom, kTopKListed, kClusterMax),
+                           sizeof(SampleShared) + scan_smem(kSampleRoom, K_most, g.C, false),
+                           sizeof(SampleShared) + scan_smem(kSampleRoom, kTopKListed, kClusterMax, false),
                            stream, z, stride, rows, vocab, K_most, a);
   if (err != cudaSuccess || g.C > 1) return err;
   const int clusters = kSearchCtas * 152 / kClusterMax;

@@ -16,15 +16,16 @@
 // rest the maxima, copies, lists, thresholds and a row's end.  511 rows of 150001
 // fp32: 70 us, 4.3 TB/s; 511 rows on 152 SMs leave some with four and some with
 // three, which alone takes 54.  One row of 131072 bf16: 13 us, the latency of a
-// launch, 8 CTAs' scan and the leader's join.  Above K = 64 the lists of K units a
-// warp leave room for three CTAs on an SM, from about 160 for two (1181 rows of
-// 22705 bf16, K = 256: 108 us).
+// launch, 8 CTAs' scan and the leader's join.  Above K = 64 a kernel of its own
+// holds long lists and candidates, and leaves room for three CTAs on an SM: 4096
+// rows of 131072 bf16 at K = 100 281 us, at K = 256 428 (selecting and ranking 256 of about
+// 450 candidates a row); 1181 of 22705 bf16 at K = 256 89 us.
 #include "vocab.cuh"
 
 namespace slimwise {
 
 constexpr int kTopCtas = 4;  // CTAs of an SM
-template <typename T, bool kCluster>
+template <typename T, bool kCluster, bool kLong>
 __global__ void __launch_bounds__(kScanThreads, kTopCtas)
     top_logits_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int K,
                       float c, int32_t *__restrict__ ids, float *__restrict__ logp,
@@ -32,7 +33,7 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   extern __shared__ __align__(128) unsigned char smem[];
   ScanShared &sh = *reinterpret_cast<ScanShared *>(smem);
   const int tid = threadIdx.x;
-  Scan<T, kCluster, false, true> scan(sh, list_room(K), K, logits, stride, vocab, rows);
+  Scan<T, kCluster, false, kLong> scan(sh, list_room(K), K, logits, stride, vocab, rows);
   auto request = [&](int, int &k, float &cc, bool &sums) {
     k = K;
     cc = c;
@@ -79,29 +80,36 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   });
 }
 
-ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, int ctas_per_sm,
-                   size_t more_smem) {
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, bool long_lists,
+                   int ctas_per_sm, size_t more_smem) {
   const int windows = (int)(((int64_t)vocab * element_bytes + 15) / 16) + 1;
   int C = 1;
   while (C < kClusterMax && rows * C <= 128 && windows >= 2 * C * 2 * kScanWarps * kWarpStep) C *= 2;
-  const int fit = (int)(228 * 1024 / (scan_smem(room, K, C) + more_smem + 1024));
+  const int fit = (int)(228 * 1024 / (scan_smem(room, K, C, long_lists) + more_smem + 1024));
   const int at_once = 152 * (fit < ctas_per_sm ? fit : ctas_per_sm) / C;
   return {C, rows < at_once ? rows : at_once};
+}
+
+template <typename T, bool kCluster, bool kLong>
+static cudaError_t launch_top(const ScanGrid &g, const void *logits, int rows, int vocab, int64_t stride,
+                              int k, float temperature, int32_t *ids, float *logp, float *log_rest,
+                              cudaStream_t stream) {
+  const int most = kLong ? kTopMax : 64;
+  return launch_clusters<top_logits_kernel<T, kCluster, kLong>>(
+      g.clusters, g.C, kScanThreads, scan_smem(list_room(k), k, g.C, kLong),
+      scan_smem(list_room(most), most, kCluster ? kClusterMax : 1, kLong), stream,
+      static_cast<const T *>(logits), stride, rows, vocab, k, kLog2e / temperature, ids, logp, log_rest);
 }
 
 template <typename T>
 static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t stride, int k,
                               float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), list_room(k), k, kTopCtas, wide_smem(k));
-  const auto launch = g.C > 1 ? launch_clusters<top_logits_kernel<T, true>, false, const T *, int64_t, int, int, int,
-                                                float, int32_t *, float *, float *>
-                              : launch_clusters<top_logits_kernel<T, false>, false, const T *, int64_t, int, int, int,
-                                                float, int32_t *, float *, float *>;
-  return launch(g.clusters, g.C, kScanThreads, scan_smem(list_room(k), k, g.C) + wide_smem(k),
-                scan_smem(list_room(kTopMax), kTopMax, kClusterMax) + wide_smem(kTopMax), stream,
-                static_cast<const T *>(logits), stride, rows, vocab, k, kLog2e / temperature, ids, logp,
-                log_rest);
+  const bool l = k > 64;
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), list_room(k), k, l, kTopCtas, 0);
+  const auto launch = g.C > 1 ? l ? launch_top<T, true, true> : launch_top<T, true, false>
+                              : l ? launch_top<T, false, true> : launch_top<T, false, false>;
+  return launch(g, logits, rows, vocab, stride, k, temperature, ids, logp, log_rest, stream);
 }
 
 cudaError_t launch_top_logits(const void *logits, int dtype, int rows, int vocab, int64_t stride,

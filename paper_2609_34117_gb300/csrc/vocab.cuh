@@ -90,8 +90,8 @@ cudaError_t launch_distill_loss(const void *logits, int dtype, int rows, int voc
 struct ScanGrid {
   int C, clusters;
 };
-ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, int ctas_per_sm,
-                   size_t more_smem);
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, bool long_lists,
+                   int ctas_per_sm, size_t more_smem);
 
 #if defined(__CUDACC__)
 namespace cg = cooperative_groups;
@@ -393,8 +393,9 @@ constexpr int kClusterMax = 8;
 constexpr int kStage = 32;
 // Candidates that a CTA holds to pick from if they are more than it passes on (K
 // above 64: the groups are then no more than twice the K wanted, and a threshold
-// lets 1.5 to 2 K through on most rows; picked from where they lie, the 1181 rows
-// of 22705 bf16 at K = 256 take 108 us, through most_of_many() 151).
+// lets 1.5 to 2 K through on most rows).  1181 rows of 22705 bf16 at K = 256 took
+// 151 us through most_of_many(), 120 held, and take 89 with a window a lane, the
+// warps' candidates behind their lists, and three CTAs on an SM.
 constexpr int kWide = 3 * kTopMax;
 static_assert(kTopMax <= kScanThreads, "a thread for each candidate");
 
@@ -412,6 +413,30 @@ struct alignas(16) Listed {
   uint64_t key;
   float sum;
   int window;
+};
+// A warp's list.  kLong: for long lists, without the window and in 12 bytes, keys
+// and then sums (with K = 256 three CTAs fit an SM, not two).
+template <bool kLong>
+struct UnitList {
+  static constexpr int kBytes = kLong ? 12 : sizeof(Listed);
+  unsigned char *p;
+  int room;
+  __device__ __forceinline__ Listed *entry(int i) const { return reinterpret_cast<Listed *>(p) + i; }
+  __device__ __forceinline__ uint64_t *keys() const { return reinterpret_cast<uint64_t *>(p); }
+  __device__ __forceinline__ float *sums() const { return reinterpret_cast<float *>(p + room * 8); }
+  __device__ __forceinline__ uint64_t key(int i) const { return kLong ? keys()[i] : entry(i)->key; }
+  __device__ __forceinline__ Listed get(int i) const {
+    if constexpr (kLong) return {keys()[i], sums()[i], 0};
+    else return *entry(i);
+  }
+  __device__ __forceinline__ void put(int i, const Listed &e) const {
+    if constexpr (kLong) {
+      keys()[i] = e.key;
+      sums()[i] = e.sum;
+    } else {
+      *entry(i) = e;
+    }
+  }
 };
 
 struct alignas(128) ScanShared {
@@ -433,17 +458,18 @@ struct alignas(128) ScanShared {
   int sel_digit, sel_above, sel_bin;
   float part_sum[2][kClusterMax], part_thr[2][kClusterMax];  // at a row's leader: each CTA's
   int part_exact[2][kClusterMax];
-  // then  Listed [warps][room]
+  // then  UnitList [warps], of `room` units
   //       uint64_t [cluster][cap]  in clusters, at a row's leader: each CTA's
   //                                candidates (in clusters of two, two of these)
 };
 // room: of a warp's list; K: the largest number of candidates asked for.
-inline size_t scan_smem(int room, int K, int C) {
-  return sizeof(ScanShared) + (size_t)kScanWarps * room * sizeof(Listed) +
-         (C > 1 ? (size_t)(C > 4 ? C : 4) * candidate_cap(K) * 8 : 0);
+// long_lists: those of a Scan with kLong, and after all that what it holds of
+// candidates that are too many to pass on.
+inline size_t scan_smem(int room, int K, int C, bool long_lists) {
+  return sizeof(ScanShared) +
+         (size_t)kScanWarps * room * (long_lists ? UnitList<true>::kBytes : UnitList<false>::kBytes) +
+         (C > 1 ? (size_t)(C > 4 ? C : 4) * candidate_cap(K) * 8 : 0) + (long_lists ? kWide * 8 : 0);
 }
-// What follows that: the candidates that are too many to pass on.
-inline size_t wide_smem(int K) { return K > 64 ? kWide * 8 : 0; }
 
 // The bits of v from bit `from` (up to 64) up.
 __device__ __forceinline__ uint64_t high_bits(uint64_t v, int from) {
@@ -601,13 +627,13 @@ __device__ __forceinline__ int candidate_lanes(int n) {
 // kCluster: rows are split over the CTAs of a cluster (else the cluster is one CTA).
 // kSumless: scan() can leave out the sums (of the 400 instructions of a step,
 // 120); s is then 0, or NaN where the row has NaN.
-// kHoldWide: wide_smem(K_most) bytes follow the lists.
-template <typename T, bool kCluster, bool kSumless, bool kHoldWide>
+// kLong: for K above 64, whose lists and candidates are long.
+template <typename T, bool kCluster, bool kSumless, bool kLong>
 struct Scan {
   static constexpr int E = Row<T>::E;
   static constexpr uint32_t kGrain = sizeof(T) == 2 ? 0xFFFFu : 0x1FFFu;  // a bf16's step; 2^-10 of an fp32
   ScanShared &sh;
-  Listed *list;        // this warp's
+  UnitList<kLong> list;  // this warp's
   uint64_t *recv;
   uint64_t *wide;
   int room, recv_cap;  // of a warp's list; of a CTA's part of recv
@@ -652,10 +678,9 @@ struct Scan {
     warp = threadIdx.x >> 5;
     room = list_rooms;
     recv_cap = candidate_cap(K_most);
-    Listed *const lists = reinterpret_cast<Listed *>(&sh + 1);
-    list = lists + warp * room;
-    recv = reinterpret_cast<uint64_t *>(lists + kScanWarps * room);
-    wide = kHoldWide && K_most > 64 ? recv + (kCluster ? max(C, 4) * recv_cap : 0) : nullptr;
+    list = list_of(warp);
+    recv = reinterpret_cast<uint64_t *>(list_of(kScanWarps).p);
+    wide = kLong ? recv + (kCluster ? max(C, 4) * recv_cap : 0) : nullptr;
     put_at = smem_u32(&sh.ring[warp][0][lane]);
     stage = 0;
     // a lane's windows are read in an order that keeps 8 lanes off each other's banks
@@ -665,6 +690,9 @@ struct Scan {
     next_row();
     for (int i = 0; i < kScanStages; ++i) issue();
     if constexpr (kCluster) cluster_arrive();  // every CTA runs before another writes to its shared memory
+  }
+  __device__ __forceinline__ UnitList<kLong> list_of(int w) const {
+    return {reinterpret_cast<unsigned char *>(&sh + 1) + w * room * UnitList<kLong>::kBytes, room};
   }
   __device__ __forceinline__ Row<T> row_of(int t) const {
     return Row<T>(logits + (int64_t)t * stride, vocab);
@@ -767,10 +795,10 @@ struct Scan {
     for (int base = 0; base < listed; base += 32) {
       const int i = base + lane;
       Listed e = {0, 0.0f, 0};
-      if (i < listed) e = list[i];
+      if (i < listed) e = list.get(i);
       const bool yes = e.key >= t;
       const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
-      if (yes) list[out + __popc(mask & ((1u << lane) - 1u))] = e;
+      if (yes) list.put(out + __popc(mask & ((1u << lane) - 1u)), e);
       else if (e.key) s += e.sum * exp_from(fmaxf(key_value(e.key), kFloorRef), ref, c);
       out += __popc(mask);
       __syncwarp();
@@ -792,7 +820,7 @@ struct Scan {
     while (high - low > 1) {
       const uint64_t mid = low + (high - low) / 2;
       int n = 0;
-      for (int i = lane; i < listed; i += 32) n += list[i].key >= mid;
+      for (int i = lane; i < listed; i += 32) n += list.key(i) >= mid;
       n = __reduce_add_sync(0xFFFFFFFFu, n);
       if (n >= K) low = mid;
       else high = mid;
@@ -800,7 +828,7 @@ struct Scan {
     }
     uint32_t least = 0xFFFFFFFFu;
     for (int i = lane; i < listed; i += 32)
-      if (list[i].key >= low) least = min(least, (uint32_t)(list[i].key >> 32));
+      if (list.key(i) >= low) least = min(least, (uint32_t)(list.key(i) >> 32));
     least = __reduce_min_sync(0xFFFFFFFFu, least);
     if (unordered(least) > thr) raise(unordered(least));
     list_thr = unordered(ordered(thr) + 1);
@@ -865,7 +893,7 @@ struct Scan {
       if (mask) {
         if (yes) {
           const int to = listed + __popc(mask & ((1u << lane) - 1u));
-          list[to] = {make_key(m, (uint32_t)(first + at)), sum, 0};
+          list.put(to, {make_key(m, (uint32_t)(first + at)), sum, 0});
         }
         listed += __popc(mask);
         __syncwarp();
@@ -880,6 +908,7 @@ struct Scan {
   // Returns their number, at most `cap`; if there were more, the K largest
   // alone.  All others go into s.
   __device__ __forceinline__ int candidates(int t, uint64_t *dst, int cap, int fill) {
+    if constexpr (kLong) return long_candidates(t, dst, cap, fill);
     const Row<T> row = row_of(t);
     const int most = exact ? K : cap;
     // The windows of this warp's units that reach, a lane each, noted with
@@ -892,14 +921,14 @@ struct Scan {
 #pragma unroll 2
     for (int base = 0; base < windows; base += 32) {
       const int i = base + lane;
-      const int at = i < windows ? (int)key_index(list[i / kUnit].key) + i % kUnit : row.windows;
+      const int at = i < windows ? (int)key_index(list.key(i / kUnit)) + i % kUnit : row.windows;
       const uint32_t none = neg_inf_bits(row.p);
       uint4 v = make_uint4(none, none, none, none);
       if (at < row.windows) v = load_window(row, at);
       const bool hit = at < row.windows && window_max<T>(v) >= thr;
       const uint32_t mask = __ballot_sync(0xFFFFFFFFu, hit);
       const int to = hits + __popc(mask & ((1u << lane) - 1u));
-      if (hit && to < room) list[to].window = at;
+      if (hit && to < room) list.entry(to)->window = at;
       if (!hit) add += window_sum<T>(v, c, ref);
       hits += __popc(mask);
     }
@@ -909,7 +938,7 @@ struct Scan {
 #pragma unroll 2
       for (int base = 0; base < elements; base += 32) {
         const int i = base + lane;
-        const int id = i < elements ? list[i / E].window * E - row.mis + i % E : -1;
+        const int id = i < elements ? list.entry(i / E)->window * E - row.mis + i % E : -1;
         const bool in = id >= 0 && id < vocab;
         const float z = in ? to_float(row.p[id]) : 0.0f;
         const bool yes = in && z >= thr;
@@ -936,32 +965,84 @@ struct Scan {
       total += sh.part[turn][w];
       units += sh.count[w];
     }
-    const bool many = total > most;
-    if (many && (!kHoldWide || !wide || total > kWide)) return most_of_many(row, dst, most, fill, units);
+    if (total > most) return most_of_many(row, dst, most, fill, units);
     s += add;
-    uint64_t *const to = kHoldWide && many ? wide : dst;
     if (held <= kStage) {
-      if (lane < held) to[before + lane] = sh.stage[warp][lane];
+      if (lane < held) dst[before + lane] = sh.stage[warp][lane];
     } else {
       held = 0;
       float again = 0.0f;
-      pass([&](int at, float z, int id) { to[before + held + at] = make_key(z, (uint32_t)id); }, again);
-    }
-    if (kHoldWide && many) {
-      __syncthreads();
-      constexpr int kKeys = kWide / kScanThreads;
-      uint64_t k[kKeys];
-      int mine = 0;
-#pragma unroll
-      for (int j = 0; j < kKeys; ++j) {
-        const int i = j * kScanThreads + (int)threadIdx.x;
-        k[j] = i < total ? wide[i] : 0;
-        mine += i < total;
-      }
-      return emit(k, mine, most, dst, fill);
+      pass([&](int at, float z, int id) { dst[before + held + at] = make_key(z, (uint32_t)id); }, again);
     }
     for (int i = total + (int)threadIdx.x; i < fill; i += kScanThreads) dst[i] = 0;
     return total;
+  }
+
+  // candidates() for long lists, most of whose windows hold some: a window a lane,
+  // and a warp's candidates held behind its list.
+  __device__ __forceinline__ int long_candidates(int t, uint64_t *dst, int cap, int fill) {
+    const Row<T> row = row_of(t);
+    const int most = exact ? K : cap;
+    const int windows = listed * kUnit, hold = room - listed;
+    uint64_t *const keys = list.keys() + listed;
+    float add = 0.0f;
+    int held = 0;
+    for (int base = 0; base < windows; base += 32) {
+      const int i = base + lane;
+      const int at = i < windows ? (int)key_index(list.key(i / kUnit)) + i % kUnit : row.windows;
+      const uint32_t none = neg_inf_bits(row.p);
+      uint4 v = make_uint4(none, none, none, none);
+      if (at < row.windows) v = load_window(row, at);
+      const bool hit = at < row.windows && window_max<T>(v) >= thr;
+      if (!hit) add += window_sum<T>(v, c, ref);
+      if (!__any_sync(0xFFFFFFFFu, hit)) continue;
+      float z[E];
+      unpack<T>(v, z);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int id = at * E - row.mis + e;
+        const bool in = hit && (unsigned)id < (unsigned)vocab, yes = in && z[e] >= thr;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, yes);
+        const int to = held + __popc(mask & ((1u << lane) - 1u));
+        if (yes && to < hold) keys[to] = make_key(z[e], (uint32_t)id);
+        if (in && !yes) add += exp_from(z[e], ref, c);
+        held += __popc(mask);
+      }
+    }
+    if (held > hold) held = 1 << 20;  // too many to hold: too many in all
+    turn ^= 1;
+    if (lane == 0) {
+      sh.part[turn][warp] = held;
+      sh.count[warp] = listed;
+    }
+    __syncthreads();
+    int before = 0, total = 0, units = 0;
+#pragma unroll
+    for (int w = 0; w < kScanWarps; ++w) {
+      if (w < warp) before += sh.part[turn][w];
+      total += sh.part[turn][w];
+      units += sh.count[w];
+    }
+    const bool many = total > most;
+    if (total > kWide) return most_of_many(row, dst, most, fill, units);
+    s += add;
+    uint64_t *const to = many ? wide : dst;
+    for (int i = lane; i < held; i += 32) to[before + i] = keys[i];
+    if (!many) {
+      for (int i = total + (int)threadIdx.x; i < fill; i += kScanThreads) dst[i] = 0;
+      return total;
+    }
+    __syncthreads();
+    constexpr int kKeys = kWide / kScanThreads;
+    uint64_t k[kKeys];
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) {
+      const int i = j * kScanThreads + (int)threadIdx.x;
+      k[j] = i < total ? wide[i] : 0;
+      mine += i < total;
+    }
+    return emit(k, mine, most, dst, fill);
   }
 
   // candidates() where there are more than may be passed on (many equal values,
@@ -970,14 +1051,13 @@ struct Scan {
   __device__ __forceinline__ int most_of_many(const Row<T> &row, uint64_t *dst, int most, int fill,
                                               int units) {
     const int tid = threadIdx.x;
-    const Listed *const lists = list - warp * room;
     if (units > kScanThreads) {
       constexpr int kSlots = (kScanWarps * (kTopMax + kListSpare) + kScanThreads - 1) / kScanThreads;
       uint64_t k[kSlots];
 #pragma unroll
       for (int j = 0; j < kSlots; ++j) {
         const int f = j * kScanThreads + tid, of = f / room, i = f - of * room;
-        k[j] = of < kScanWarps && i < sh.count[of] ? lists[of * room + i].key : 0;
+        k[j] = of < kScanWarps && i < sh.count[of] ? list_of(of).key(i) : 0;
       }
       const uint64_t low = select_kth(k, K, sh);
       exact = true;
@@ -990,7 +1070,7 @@ struct Scan {
     int unit = -1, left = tid;
 #pragma unroll
     for (int w = 0; w < kScanWarps; ++w) {
-      if (left >= 0 && left < sh.count[w]) unit = (int)key_index(lists[w * room + left].key);
+      if (left >= 0 && left < sh.count[w]) unit = (int)key_index(list_of(w).key(left));
       left -= sh.count[w];
     }
     uint64_t k[kUnit];
