@@ -27,7 +27,7 @@
 // 512 rows of 262144 bf16 under mixed requests: 70 us, 3.8 TB/s, four rows on some
 // SMs and three on others (47 us at the least); 256 of 150001 fp32 43 us, 3.6 TB/s,
 // one or two rows on an SM, whose copies in flight do not fill the memory's latency;
-// 64 of 131072 fp32 with top-p 22.5 us; one row 15 us, latency.  A search costs
+// 64 of 131072 fp32 with top-p 22.5 us; one row 14.5 us, latency.  A search costs
 // more: 512 rows of 131072 bf16 without any filter 176 us (by its instructions: 0.57
 // of the issue slots, and block barriers), with a nucleus of 0.9 of nearly flat
 // rows 1.04 ms (the histograms' atomics in shared memory).
@@ -35,10 +35,11 @@
 
 namespace slimwise {
 
-// CTAs of an SM: three leave the scan all its registers, four hold more rows at
-// once.  256 rows of 150001 fp32 take 38 us with three and 46 with four, 512 of
-// 262144 bf16 73 and 67: three as long as they hold all rows.
-constexpr int kFewCtas = 3, kManyCtas = 4;
+// Three stages of the rings, as top logits have for few rows, gain nothing here
+// (200 rows of 150001 bf16 29.8 us against 28.0).  256 rows of 150001 fp32 take 38
+// us with three CTAs on an SM, which leave the scan its registers, and 46 with
+// four; 512 of 262144 bf16, which four hold at once, 73 and 67.
+constexpr int kSampleStages = kManyStages;
 // Of the search: with all of 512 rows of 131072 bf16 left over, no filter takes 242
 // us with two, 284 with three, 176 with four and 253 with five; a nucleus of 0.9
 // of nearly flat rows 1320, 1585, 1037 and 1587.
@@ -77,7 +78,7 @@ struct SearchShared {
   int bin;
   uint32_t left[kScanWarps];         // rows that are left over, a bit each
 };
-static_assert(sizeof(SearchShared) <= sizeof(ScanShared), "the search fits the scan's memory");
+static_assert(sizeof(SearchShared) <= sizeof(ScanShared<kSampleStages>), "the search fits the scan's memory");
 static_assert(kScanWarps * kStepsMax * 8 <= sizeof(SearchShared::hist), "the steps' sums fit the bins");
 struct SampleShared {
   uint64_t weight[kTopMax];
@@ -443,9 +444,9 @@ __device__ __noinline__ void search_row(const Part<T> part, const Draw d, int &p
 // The request decided at a row's leader from its n largest elements, sh.cand;
 // false if they do not decide it.  rest: the sum of 2^((z - ref) c) over all
 // other elements; m: the row's maximum.
+template <typename S>
 __device__ __forceinline__ bool decide(const Draw &d, int n, float rest, float ref, float c, float m,
-                                       int vocab, int32_t *token, float *logprob, ScanShared &sh,
-                                       SampleShared &sm) {
+                                       int vocab, int32_t *token, float *logprob, S &sh, SampleShared &sm) {
   const int tid = threadIdx.x;
   // a few lanes for each candidate; the first of them holds it
   const int lanes = candidate_lanes(n), at = tid / lanes, sub = tid % lanes;
@@ -536,9 +537,9 @@ __device__ __forceinline__ bool request_of(const SampleArgs &a, int t, int vocab
 // Row t's token, by its leader's threads, from its n largest elements in sh.cand
 // and s, this thread's part of the sum of all others.  Not inlined: the scan's
 // loop keeps its registers.
-template <typename T>
+template <typename T, typename S>
 __device__ __noinline__ void finish_row(const SampleArgs &a, const Row<T> row, int t, int n, float s,
-                                        float ref, ScanShared &sh, SampleShared &sm) {
+                                        float ref, S &sh, SampleShared &sm) {
   const int tid = threadIdx.x;
   Draw d;
   int K;
@@ -606,9 +607,9 @@ __global__ void __launch_bounds__(kScanThreads, kCtas)
                   const __grid_constant__ SampleArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   SampleShared &sm = *reinterpret_cast<SampleShared *>(smem);
-  ScanShared &sh = *reinterpret_cast<ScanShared *>(smem + sizeof(SampleShared));
+  auto &sh = *reinterpret_cast<ScanShared<kSampleStages> *>(smem + sizeof(SampleShared));
   if constexpr (!kCluster) pdl_launch_dependents();  // the search kernel, which waits
-  Scan<T, kCluster, true, false> scan(sh, kSampleRoom, K_most, logits, stride, vocab, rows);
+  Scan<T, kCluster, true, false, kSampleStages> scan(sh, kSampleRoom, K_most, logits, stride, vocab, rows);
   auto request = [&](int t, int &K, float &c, bool &sums) {
     Draw d;
     request_of(a, t, vocab, d, K);
@@ -633,25 +634,30 @@ __global__ void __launch_bounds__(kScanThreads, kSearchCtas)
   search_rows<T, true>(logits, stride, rows, vocab, a, search);
 }
 
+template <typename T, bool kCluster, int kCtas>
+static cudaError_t launch_scan(const ScanGrid &g, const T *z, int64_t stride, int rows, int vocab, int K_most,
+                               const SampleArgs &a, cudaStream_t stream) {
+  return launch_clusters<sample_kernel<T, kCluster, kCtas>>(
+      g.clusters, g.C, kScanThreads, g.smem,
+      sizeof(SampleShared) + scan_smem(kSampleStages, kSampleRoom, kTopKListed, kCluster ? kClusterMax : 1, false),
+      stream, z, stride, rows, vocab, K_most, a);
+}
+
 template <typename T>
 static cudaError_t launch(const void *logits, int rows, int vocab, int64_t stride,
                           const float *temperature, const int32_t *top_k, const float *top_p,
                           const float *min_p, const float *uniform, int32_t *tokens,
                           float *logprob, cudaStream_t stream) {
   const int K_most = top_k ? kTopKListed : kNucleus;
-  const bool many = rows > 152 * kFewCtas;
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleRoom, K_most, false,
-                               many ? kManyCtas : kFewCtas, sizeof(SampleShared));
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), kSampleRoom, K_most, false, kSampleStages,
+                               sizeof(SampleShared));
   const SampleArgs a = {temperature, top_k, top_p, min_p, uniform, tokens, logprob};
   const T *const z = static_cast<const T *>(logits);
   const auto launch =
-      g.C > 1 ? launch_clusters<sample_kernel<T, true, kFewCtas>, false, const T *, int64_t, int, int, int, SampleArgs>
-      : many  ? launch_clusters<sample_kernel<T, false, kManyCtas>, false, const T *, int64_t, int, int, int, SampleArgs>
-              : launch_clusters<sample_kernel<T, false, kFewCtas>, false, const T *, int64_t, int, int, int, SampleArgs>;
-  cudaError_t err = launch(g.clusters, g.C, kScanThreads,
-                           sizeof(SampleShared) + scan_smem(kSampleRoom, K_most, g.C, false),
-                           sizeof(SampleShared) + scan_smem(kSampleRoom, kTopKListed, kClusterMax, false),
-                           stream, z, stride, rows, vocab, K_most, a);
+      g.C > 1 ? launch_scan<T, true, kFewCtas>
+      : g.few ? launch_scan<T, false, kFewCtas>
+              : launch_scan<T, false, kManyCtas>;
+  cudaError_t err = launch(g, z, stride, rows, vocab, K_most, a, stream);
   if (err != cudaSuccess || g.C > 1) return err;
   const int clusters = kSearchCtas * 152 / kClusterMax;
   cudaLaunchAttribute attr[2];

@@ -24,16 +24,22 @@
 
 namespace slimwise {
 
-constexpr int kTopCtas = 4;  // CTAs of an SM
-template <typename T, bool kCluster, bool kLong>
-__global__ void __launch_bounds__(kScanThreads, kTopCtas)
+// Stages of the rings where the rows are few: 152 rows of 150001 fp32 take 23.5 us
+// with three and 26.3 with two, 304 of 131072 bf16 24.6 and 26.5, 16 rows in
+// clusters 17.0 and 18.1.
+constexpr int kFewStages = 3;
+__host__ __device__ constexpr int top_stages(int ctas) { return ctas == kFewCtas ? kFewStages : kManyStages; }
+
+template <typename T, bool kCluster, bool kLong, int kCtas>
+__global__ void __launch_bounds__(kScanThreads, kCtas)
     top_logits_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int K,
                       float c, int32_t *__restrict__ ids, float *__restrict__ logp,
                       float *__restrict__ log_rest) {
   extern __shared__ __align__(128) unsigned char smem[];
-  ScanShared &sh = *reinterpret_cast<ScanShared *>(smem);
+  constexpr int kStages = top_stages(kCtas);
+  auto &sh = *reinterpret_cast<ScanShared<kStages> *>(smem);
   const int tid = threadIdx.x;
-  Scan<T, kCluster, false, kLong> scan(sh, list_room(K), K, logits, stride, vocab, rows);
+  Scan<T, kCluster, false, kLong, kStages> scan(sh, list_room(K), K, logits, stride, vocab, rows);
   auto request = [&](int, int &k, float &cc, bool &sums) {
     k = K;
     cc = c;
@@ -80,36 +86,47 @@ __global__ void __launch_bounds__(kScanThreads, kTopCtas)
   });
 }
 
-ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, bool long_lists,
-                   int ctas_per_sm, size_t more_smem) {
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, bool long_lists, int few_stages,
+                   size_t more_smem) {
   const int windows = (int)(((int64_t)vocab * element_bytes + 15) / 16) + 1;
   int C = 1;
   while (C < kClusterMax && rows * C <= 128 && windows >= 2 * C * 2 * kScanWarps * kWarpStep) C *= 2;
-  const int fit = (int)(228 * 1024 / (scan_smem(room, K, C, long_lists) + more_smem + 1024));
-  const int at_once = 152 * (fit < ctas_per_sm ? fit : ctas_per_sm) / C;
-  return {C, rows < at_once ? rows : at_once};
+  const auto with = [&](int ctas) {
+    const int stages = ctas == kFewCtas ? few_stages : kManyStages;
+    const size_t smem = scan_smem(stages, room, K, C, long_lists) + more_smem;
+    const int fit = (int)(228 * 1024 / (smem + 1024)), at_once = 152 * (fit < ctas ? fit : ctas) / C;
+    return ScanGrid{C, rows < at_once ? rows : at_once, ctas == kFewCtas, smem};
+  };
+  const ScanGrid few = with(kFewCtas);
+  return few.clusters == rows || C > 1 ? few : with(kManyCtas);
 }
 
-template <typename T, bool kCluster, bool kLong>
+template <typename T, bool kCluster, bool kLong, int kCtas>
 static cudaError_t launch_top(const ScanGrid &g, const void *logits, int rows, int vocab, int64_t stride,
                               int k, float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
   const int most = kLong ? kTopMax : 64;
-  return launch_clusters<top_logits_kernel<T, kCluster, kLong>>(
-      g.clusters, g.C, kScanThreads, scan_smem(list_room(k), k, g.C, kLong),
-      scan_smem(list_room(most), most, kCluster ? kClusterMax : 1, kLong), stream,
+  return launch_clusters<top_logits_kernel<T, kCluster, kLong, kCtas>>(
+      g.clusters, g.C, kScanThreads, g.smem,
+      scan_smem(top_stages(kCtas), list_room(most), most, kCluster ? kClusterMax : 1, kLong), stream,
       static_cast<const T *>(logits), stride, rows, vocab, k, kLog2e / temperature, ids, logp, log_rest);
 }
-
+template <typename T, bool kLong>
+static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t stride, int k,
+                              float temperature, int32_t *ids, float *logp, float *log_rest,
+                              cudaStream_t stream) {
+  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), list_room(k), k, kLong, kFewStages, 0);
+  const auto launch = g.C > 1 ? launch_top<T, true, kLong, kFewCtas>
+                      : g.few ? launch_top<T, false, kLong, kFewCtas>
+                              : launch_top<T, false, kLong, kManyCtas>;
+  return launch(g, logits, rows, vocab, stride, k, temperature, ids, logp, log_rest, stream);
+}
 template <typename T>
 static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t stride, int k,
                               float temperature, int32_t *ids, float *logp, float *log_rest,
                               cudaStream_t stream) {
-  const bool l = k > 64;
-  const ScanGrid g = scan_grid(rows, vocab, (int)sizeof(T), list_room(k), k, l, kTopCtas, 0);
-  const auto launch = g.C > 1 ? l ? launch_top<T, true, true> : launch_top<T, true, false>
-                              : l ? launch_top<T, false, true> : launch_top<T, false, false>;
-  return launch(g, logits, rows, vocab, stride, k, temperature, ids, logp, log_rest, stream);
+  return k > 64 ? launch_top<T, true>(logits, rows, vocab, stride, k, temperature, ids, logp, log_rest, stream)
+                : launch_top<T, false>(logits, rows, vocab, stride, k, temperature, ids, logp, log_rest, stream);
 }
 
 cudaError_t launch_top_logits(const void *logits, int dtype, int rows, int vocab, int64_t stride,

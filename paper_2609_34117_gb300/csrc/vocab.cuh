@@ -84,14 +84,18 @@ cudaError_t launch_distill_loss(const void *logits, int dtype, int rows, int voc
                                 float *loss, void *grad, int64_t grad_stride, cudaStream_t stream);
 
 // How a scan for the K largest is launched: CTAs of a cluster (a row is split
-// over them), and clusters, each of which takes every clusters-th row.
-// ctas_per_sm: what the kernel's registers allow; more_smem: the kernel's shared
-// memory besides the scan's.
+// over them), clusters, each of which takes every clusters-th row, and which
+// kernel: for kFewCtas CTAs of an SM if those hold all rows, else for kManyCtas.
+// few_stages: of the few's rings; more_smem: the kernel's shared memory besides
+// the scan's.
+constexpr int kManyCtas = 4, kFewCtas = 3, kManyStages = 2;
 struct ScanGrid {
   int C, clusters;
+  bool few;
+  size_t smem;
 };
-ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, bool long_lists,
-                   int ctas_per_sm, size_t more_smem);
+ScanGrid scan_grid(int rows, int vocab, int element_bytes, int room, int K, bool long_lists, int few_stages,
+                   size_t more_smem);
 
 #if defined(__CUDACC__)
 namespace cg = cooperative_groups;
@@ -386,9 +390,7 @@ constexpr int kScanThreads = 256;
 constexpr int kScanWarps = kScanThreads / 32;
 constexpr int kUnit = 4;                      // windows of a unit
 constexpr int kWarpStep = 32 * kUnit;         // windows of a warp in a step
-constexpr int kScanStages = 2;
 constexpr uint32_t kStageBytes = kWarpStep * 16;
-static_assert(kScanStages == 2, "the stage at hand is the one or the other");
 constexpr int kClusterMax = 8;
 constexpr int kStage = 32;
 // Candidates that a CTA holds to pick from if they are more than it passes on (K
@@ -439,8 +441,9 @@ struct UnitList {
   }
 };
 
+template <int kStages>
 struct alignas(128) ScanShared {
-  uint4 ring[kScanWarps][kScanStages][kWarpStep];
+  uint4 ring[kScanWarps][kStages][kWarpStep];
   uint64_t cand[kTopMax];
   uint64_t red64[kScanWarps];
   union {
@@ -465,8 +468,8 @@ struct alignas(128) ScanShared {
 // room: of a warp's list; K: the largest number of candidates asked for.
 // long_lists: those of a Scan with kLong, and after all that what it holds of
 // candidates that are too many to pass on.
-inline size_t scan_smem(int room, int K, int C, bool long_lists) {
-  return sizeof(ScanShared) +
+inline size_t scan_smem(int stages, int room, int K, int C, bool long_lists) {
+  return sizeof(ScanShared<1>) + (size_t)(stages - 1) * kScanWarps * kStageBytes +
          (size_t)kScanWarps * room * (long_lists ? UnitList<true>::kBytes : UnitList<false>::kBytes) +
          (C > 1 ? (size_t)(C > 4 ? C : 4) * candidate_cap(K) * 8 : 0) + (long_lists ? kWide * 8 : 0);
 }
@@ -479,8 +482,8 @@ __device__ __forceinline__ uint64_t high_bits(uint64_t v, int from) {
 // Threshold such that exactly K of the keys in the block's registers (0: none)
 // are at least it; more than K are not 0.  A radix selection from the highest
 // bit in which they differ, 8 bits a pass, that ends when a whole bin is taken.
-template <int N>
-__device__ __forceinline__ uint64_t select_kth(const uint64_t (&k)[N], int K, ScanShared &sh) {
+template <int N, typename S>
+__device__ __forceinline__ uint64_t select_kth(const uint64_t (&k)[N], int K, S &sh) {
   const int tid = threadIdx.x;
   uint32_t hi_or = 0, hi_and = 0xFFFFFFFFu;
 #pragma unroll
@@ -554,7 +557,8 @@ __device__ __forceinline__ uint64_t select_kth(const uint64_t (&k)[N], int K, Sc
 }
 
 // Exclusive prefix sum of v over the block; `total` the sum.
-__device__ __forceinline__ int block_prefix(int v, int &total, ScanShared &sh) {
+template <typename S>
+__device__ __forceinline__ int block_prefix(int v, int &total, S &sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int incl = v;
 #pragma unroll
@@ -627,12 +631,13 @@ __device__ __forceinline__ int candidate_lanes(int n) {
 // kCluster: rows are split over the CTAs of a cluster (else the cluster is one CTA).
 // kSumless: scan() can leave out the sums (of the 400 instructions of a step,
 // 120); s is then 0, or NaN where the row has NaN.
-// kLong: for K above 64, whose lists and candidates are long.
-template <typename T, bool kCluster, bool kSumless, bool kLong>
+// kLong: for K above 64, whose lists and candidates are long.  kStages: of a ring.
+template <typename T, bool kCluster, bool kSumless, bool kLong, int kStages>
 struct Scan {
   static constexpr int E = Row<T>::E;
   static constexpr uint32_t kGrain = sizeof(T) == 2 ? 0xFFFFu : 0x1FFFu;  // a bf16's step; 2^-10 of an fp32
-  ScanShared &sh;
+  using Shared = ScanShared<kStages>;
+  Shared &sh;
   UnitList<kLong> list;  // this warp's
   uint64_t *recv;
   uint64_t *wide;
@@ -661,7 +666,7 @@ struct Scan {
 
   // list_rooms: units that a warp's list has room for (at least K + 32), K_most: the
   // largest K of all rows
-  __device__ __forceinline__ Scan(ScanShared &shared, int list_rooms, int K_most, const T *z, int64_t st,
+  __device__ __forceinline__ Scan(Shared &shared, int list_rooms, int K_most, const T *z, int64_t st,
                                   int V, int n)
       : sh(shared), logits(z), stride(st), vocab(V), rows(n) {
     if constexpr (kCluster) {
@@ -688,7 +693,7 @@ struct Scan {
     turn = 0;
     next_t = (int)(blockIdx.x / C);
     next_row();
-    for (int i = 0; i < kScanStages; ++i) issue();
+    for (int i = 0; i < kStages; ++i) issue();
     if constexpr (kCluster) cluster_arrive();  // every CTA runs before another writes to its shared memory
   }
   __device__ __forceinline__ UnitList<kLong> list_of(int w) const {
@@ -741,7 +746,8 @@ struct Scan {
         if ((unsigned)(next_i + 32 * u) < (unsigned)next_n) copy_window(u);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    stage ^= kStageBytes;
+    if constexpr (kStages == 2) stage ^= kStageBytes;
+    else stage = stage == (kStages - 1) * kStageBytes ? 0 : stage + kStageBytes;
     next_i += kWarpStep;
     next_src += kWarpStep;
     if (--next_left == 0) {
@@ -755,7 +761,7 @@ struct Scan {
   }
   // Waits for the oldest copy, of all lanes.
   __device__ __forceinline__ void wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kScanStages - 1) : "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
     __syncwarp();
   }
 
