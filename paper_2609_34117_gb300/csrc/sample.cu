@@ -213,13 +213,13 @@ struct EqualTo {  // one if they are o, as ordered(), and in the row
     return n;
   }
 };
-struct KeptWeight {  // their weights, if they are kept
+template <bool kAll>
+struct KeptWeight {  // their weights, if they are kept (kAll: all are)
   Limit keep;
-  bool limited;  // keep leaves any out
   float m, inv, min_p;
   __device__ __forceinline__ float kept(float z, int id) const {
     const float e = element_exp(z, m, inv);
-    return (!limited || keep.has(ordered(z), id)) && e >= min_p ? e : 0.0f;
+    return kAll || (keep.has(ordered(z), id) && e >= min_p) ? e : 0.0f;
   }
   __device__ __forceinline__ uint64_t operator()(float z, int id) const { return element_weight(kept(z, id)); }
   // floor(2^40 e) as two whole numbers of 20 bits, which a sum with 2^23, rounded
@@ -412,6 +412,19 @@ __device__ __noinline__ int search_id(const Part<T> part, uint32_t o, uint64_t w
   return sh.bin;
 }
 
+// The token among the elements that are kept.
+template <typename T, typename F>
+__device__ __noinline__ void search_token(const Part<T> part, const F f, uint64_t u24, int &parity,
+                                          int32_t *token, float *logprob, SearchShared &sh) {
+  search_sum(
+      part, f, [&](uint64_t total) { return fraction(total, u24); },
+      [&](int id, uint64_t w, uint64_t total) {
+        *token = id;
+        *logprob = logf((float)w / (float)total);
+      },
+      parity, sh);
+}
+
 // The whole request over the whole row, by all CTAs of the team.
 template <typename T>
 __device__ __noinline__ void search_row(const Part<T> part, const Draw d, int &parity,
@@ -431,14 +444,10 @@ __device__ __noinline__ void search_row(const Part<T> part, const Draw d, int &p
     keep.id = o == keep.o ? min(id, keep.id) : id;
     keep.o = o;
   }
-  search_sum(
-      part, KeptWeight{keep, d.limited || d.nucleus, part.m, part.inv, d.min_p},
-      [&](uint64_t total) { return fraction(total, d.u24); },
-      [&](int id, uint64_t w, uint64_t total) {
-        *token = id;
-        *logprob = logf((float)w / (float)total);
-      },
-      parity, sh);
+  if (d.limited || d.nucleus || d.min_p > 0.0f)
+    search_token(part, KeptWeight<false>{keep, part.m, part.inv, d.min_p}, d.u24, parity, token, logprob, sh);
+  else
+    search_token(part, KeptWeight<true>{keep, part.m, part.inv, d.min_p}, d.u24, parity, token, logprob, sh);
 }
 
 // The request decided at a row's leader from its n largest elements, sh.cand;
