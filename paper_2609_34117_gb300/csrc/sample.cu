@@ -71,7 +71,7 @@ constexpr int kAloneFrom = 6;
 // Steps of 4 x 32 windows of a warp.
 constexpr int kStepsMax = (kVocabMax / 4 / kScanWarps + 127) / 128 + 1;
 struct SearchShared {
-  uint32_t hist[2][kBins];           // of a pass: counts, or sums of weights in two halves
+  uint32_t hist[2][kBins];           // of a pass: two copies of counts, or sums of weights in two halves
   uint64_t slot[2][kClusterMax];     // each CTA's sum
   uint64_t red[kScanWarps];
   uint64_t above;                    // result of a pass, written by the CTA that found it
@@ -243,9 +243,9 @@ struct KeptWeight {  // their weights, if they are kept (kAll: all are)
 
 // The largest value v (as ordered()) with amount(values >= v within `in`) at
 // least `want`, and in `above` the amount of the values > v.  Amounts are weights
-// (`mass`) or counts.  want 0: the share p24 of the whole amount; cut: that wanted.
-template <typename T>
-__device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, bool mass, uint64_t want,
+// (kMass) or counts.  want 0: the share p24 of the whole amount; cut: that wanted.
+template <bool kMass, typename T>
+__device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, uint64_t want,
                                               uint64_t p24, uint64_t &above, uint64_t &cut, int &parity,
                                               SearchShared &sh) {
   const Team team = part.team;
@@ -262,14 +262,14 @@ __device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, bool
       const uint32_t o = ordered(z);
       if (!in.has(o, id) || (known < 32 && (o ^ prefix) >> known) || (unsigned)id >= (unsigned)part.row.vocab) return;
       const uint32_t bin = (o >> shift) & ((1u << (known - shift)) - 1u);
-      if (mass) {
+      if constexpr (kMass) {
         const uint64_t w = element_weight(element_exp(z, part.m, part.inv));
         // a sum of 64 bits in two, by hand: few weights have a high half
         const uint32_t low = (uint32_t)w, was = low ? atomicAdd(&sh.hist[0][bin], low) : 0;
         const uint32_t high = (uint32_t)(w >> 32) + (was + low < was);
         if (high) atomicAdd(&sh.hist[1][bin], high);
       } else {
-        atomicAdd(&sh.hist[0][bin], 1u);
+        atomicAdd(&sh.hist[lane & 1][bin], 1u);  // (two copies: fewer lanes meet)
       }
     });
     team.sync();
@@ -282,7 +282,7 @@ __device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, bool
       if (j < mine)
         for (int r = 0; r < C; ++r) {
           const uint32_t *const h = team.of(&sh.hist[0][first + j], r);
-          amount[j] += h[0] + ((uint64_t)h[kBins] << 32);
+          amount[j] += h[0] + ((uint64_t)h[kBins] << (kMass ? 32 : 0));
         }
       sum += amount[j];
     }
@@ -432,13 +432,13 @@ __device__ __noinline__ void search_row(const Part<T> part, const Draw d, int &p
   Limit keep = {0, part.row.vocab};
   uint64_t above, cut;
   if (d.limited) {
-    keep.o = search_value(part, keep, false, (uint64_t)d.top_k, 0, above, cut, parity, sh);
+    keep.o = search_value<false>(part, keep, (uint64_t)d.top_k, 0, above, cut, parity, sh);
     keep.id = search_id(part, keep.o, (uint64_t)d.top_k - above, parity, sh);
   }
   if (d.nucleus) {
     // of the elements of value o (each of weight w > 0), those before which less
     // than the cut lies; top-k's limit already holds among them
-    const uint32_t o = search_value(part, keep, true, 0, d.p24, above, cut, parity, sh);
+    const uint32_t o = search_value<true>(part, keep, 0, d.p24, above, cut, parity, sh);
     const uint64_t w = element_weight(element_exp(unordered(o), part.m, part.inv));
     const int id = search_id(part, o, (cut - above + w - 1) / w, parity, sh);
     keep.id = o == keep.o ? min(id, keep.id) : id;
