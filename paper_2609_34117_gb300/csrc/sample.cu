@@ -241,6 +241,32 @@ struct KeptWeight {  // their weights, if they are kept (kAll: all are)
   }
 };
 
+// Bins of a pass: counts, or masses (kMass), of the elements within `in` whose bits
+// from `known` up are the prefix's, by their bits from `shift` to there.  A
+// function of its own for the registers.
+template <bool kMass, typename T>
+__device__ __noinline__ void histogram(const Part<T> part, const Limit in, int known, int shift,
+                                       uint32_t prefix, SearchShared &sh) {
+  const int tid = threadIdx.x, copy = tid & 1;
+  for (int i = tid; i < 2 * kBins; i += kScanThreads) (&sh.hist[0][0])[i] = 0;
+  __syncthreads();
+  const uint32_t mask = (1u << (known - shift)) - 1u, others = known < 32 ? ~0u << known : 0;
+  part.each([&](float z, int id) {
+    const uint32_t o = ordered(z);
+    if (!in.has(o, id) || ((o ^ prefix) & others) || (unsigned)id >= (unsigned)part.row.vocab) return;
+    const uint32_t bin = o >> shift & mask;
+    if constexpr (kMass) {
+      const uint64_t w = element_weight(element_exp(z, part.m, part.inv));
+      // a sum of 64 bits in two, by hand: few weights have a high half
+      const uint32_t low = (uint32_t)w, was = low ? atomicAdd(&sh.hist[0][bin], low) : 0;
+      const uint32_t high = (uint32_t)(w >> 32) + (was + low < was);
+      if (high) atomicAdd(&sh.hist[1][bin], high);
+    } else {
+      atomicAdd(&sh.hist[copy][bin], 1u);  // (two copies: fewer lanes meet)
+    }
+  });
+}
+
 // The largest value v (as ordered()) with amount(values >= v within `in`) at
 // least `want`, and in `above` the amount of the values > v.  Amounts are weights
 // (kMass) or counts.  want 0: the share p24 of the whole amount; cut: that wanted.
@@ -256,22 +282,7 @@ __device__ __noinline__ uint32_t search_value(const Part<T> part, Limit in, uint
   above = 0;
   for (int known = 32; known > (sizeof(T) == 2 ? 16 : 0);) {
     const int shift = max(known - 11, sizeof(T) == 2 ? 16 : 0);  // (a bf16 has 16 bits)
-    for (int i = tid; i < 2 * kBins; i += kScanThreads) (&sh.hist[0][0])[i] = 0;
-    __syncthreads();
-    part.each([&](float z, int id) {
-      const uint32_t o = ordered(z);
-      if (!in.has(o, id) || (known < 32 && (o ^ prefix) >> known) || (unsigned)id >= (unsigned)part.row.vocab) return;
-      const uint32_t bin = (o >> shift) & ((1u << (known - shift)) - 1u);
-      if constexpr (kMass) {
-        const uint64_t w = element_weight(element_exp(z, part.m, part.inv));
-        // a sum of 64 bits in two, by hand: few weights have a high half
-        const uint32_t low = (uint32_t)w, was = low ? atomicAdd(&sh.hist[0][bin], low) : 0;
-        const uint32_t high = (uint32_t)(w >> 32) + (was + low < was);
-        if (high) atomicAdd(&sh.hist[1][bin], high);
-      } else {
-        atomicAdd(&sh.hist[lane & 1][bin], 1u);  // (two copies: fewer lanes meet)
-      }
-    });
+    histogram<kMass>(part, in, known, shift, prefix, sh);
     team.sync();
     // CTA r joins bins r per .. of all CTAs, each thread `mine` of them
     const int first = rank * per + tid * mine;
