@@ -28,9 +28,9 @@
 // SMs and three on others (47 us at the least); 256 of 150001 fp32 43 us, 3.6 TB/s,
 // one or two rows on an SM, whose copies in flight do not fill the memory's latency;
 // 64 of 131072 fp32 with top-p 22.5 us; one row 14.5 us, latency.  A search costs
-// more: 512 rows of 131072 bf16 without any filter 176 us (by its instructions: 0.57
-// of the issue slots, and block barriers), with a nucleus of 0.9 of nearly flat
-// rows 1.04 ms (the histograms' atomics in shared memory).
+// more: 512 rows of 131072 bf16 without any filter 128 us (by its instructions), with
+// top-k 1000 475, with a nucleus of 0.9 of nearly flat rows 0.9 ms (the
+// histograms' atomics in shared memory).
 #include "vocab.cuh"
 
 namespace slimwise {
@@ -40,10 +40,11 @@ namespace slimwise {
 // us with three CTAs on an SM, which leave the scan its registers, and 46 with
 // four; 512 of 262144 bf16, which four hold at once, 73 and 67.
 constexpr int kSampleStages = kManyStages;
-// Of the search: with all of 512 rows of 131072 bf16 left over, no filter takes 242
-// us with two, 284 with three, 176 with four and 253 with five; a nucleus of 0.9
-// of nearly flat rows 1320, 1585, 1037 and 1587.
-constexpr int kSearchCtas = 4;
+// The search goes by the same rule.  With all rows left over, 512 of 131072 bf16
+// take 128 us without a filter and 900 with a nucleus of 0.9 of nearly flat rows
+// with four CTAs on an SM, 195 and 1390 with three, 163 and 1560 with five; 380 of
+// 131072 fp32, which three hold at once, 142 and 836 with three, 162 and 976 with
+// four, 150 and 1260 with five.
 constexpr int kNucleus = 32;      // elements looked at for a nucleus or min-p without top-k
 constexpr int kSampleRoom = 128;  // of a warp's list
 constexpr int kTopKListed = kSampleRoom - 32;  // largest top-k that is decided from the list
@@ -64,9 +65,9 @@ constexpr uint64_t kMassError = 1 << 15;  // one part in
 // What a search uses of shared memory, where the scan's was.
 constexpr int kBins = 2048;
 // Rows left over in a cluster's share from which each is searched by one CTA: 608
-// rows of 32000 fp32 without a filter (8 a cluster) take 102 us so and 220 by
-// clusters, 512 of 131072 bf16 (6 or 7) 234 and 263; 380 of 131072 fp32 (5) 241
-// and 224.
+// rows of 32000 fp32 without a filter (8 a cluster) take 73 us so and 156 by
+// clusters, 512 of 131072 bf16 (6 or 7) 128 and 182; with a nucleus of 0.9, 304
+// of 131072 bf16 (4) 723 and 610.
 constexpr int kAloneFrom = 6;
 // Steps of 4 x 32 windows of a warp.
 constexpr int kStepsMax = (kVocabMax / 4 / kScanWarps + 127) / 128 + 1;
@@ -645,8 +646,8 @@ __global__ void __launch_bounds__(kScanThreads, kCtas)
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kScanThreads, kSearchCtas)
+template <typename T, int kCtas>
+__global__ void __launch_bounds__(kScanThreads, kCtas)
     sample_search_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab,
                          const __grid_constant__ SampleArgs a) {
   __shared__ SearchShared search;
@@ -679,7 +680,7 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
               : launch_scan<T, false, kManyCtas>;
   cudaError_t err = launch(g, z, stride, rows, vocab, K_most, a, stream);
   if (err != cudaSuccess || g.C > 1) return err;
-  const int clusters = kSearchCtas * 152 / kClusterMax;
+  const int clusters = (g.few ? kFewCtas : kManyCtas) * 152 / kClusterMax;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = kClusterMax;
@@ -693,7 +694,8 @@ static cudaError_t launch(const void *logits, int rows, int vocab, int64_t strid
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, sample_search_kernel<T>, z, stride, rows, vocab, a);
+  return cudaLaunchKernelEx(&cfg, g.few ? sample_search_kernel<T, kFewCtas> : sample_search_kernel<T, kManyCtas>,
+                            z, stride, rows, vocab, a);
 }
 
 cudaError_t launch_sample(const void *logits, int dtype, int rows, int vocab, int64_t stride,
