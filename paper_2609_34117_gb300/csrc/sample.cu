@@ -24,7 +24,7 @@
 // where single CTAs do, a second kernel, so that a left-over row still gets a
 // cluster and the first keeps four CTAs on an SM.
 //
-// 512 rows of 262144 bf16 under mixed requests: 70 us, 3.8 TB/s, four rows on some
+// 512 rows of 262144 bf16 under mixed requests: 68 us, 3.9 TB/s, four rows on some
 // SMs and three on others (47 us at the least); 256 of 150001 fp32 43 us, 3.6 TB/s,
 // one or two rows on an SM, whose copies in flight do not fill the memory's latency;
 // 64 of 131072 fp32 with top-p 22.5 us; one row 14.5 us, latency.  A search costs
