@@ -618,6 +618,7 @@ __device__ __forceinline__ void search_rows(const T *logits, int64_t stride, int
         __syncthreads();  // the next row's bins lie where this one's steps are read
       }
     if (alone) cluster.sync();  // before others write here again
+    else __syncthreads();       // every warp has read sh.left to its end
   }
   cluster.sync();  // no CTA ends while its sums can still be read or written
 }

@@ -1,0 +1,53 @@
+"""The operators over vocabulary logits at the ends of their ranges: more rows
+than one pass of the search takes, masses far below the largest logit, targets
+and weights without a value.  Tokens are exact; the other tolerances are those of
+test_gpu_vocab.py, or derived at the test."""
+import pytest
+import torch
+
+import paper_2609_34117_gb300 as sw
+
+from tests.test_gpu_vocab import DEV, TYPES, _gen, _rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    sw.build.build()
+
+
+# ---------------------------------------------------------------------------
+# sampling: more rows than the search takes in one pass
+# ---------------------------------------------------------------------------
+# (76 clusters take every 76th row, 256 of theirs in a pass)
+CLUSTERS = 76
+PASS = 256 * CLUSTERS
+# requests that the listed elements of a nearly flat row do not decide, and that they do
+WIDE = [(1.0, 0, 1.0), (1.0, 300, 1.0), (1.0, 0, 0.9), (1.0, 300, 0.8)]
+LISTED = [(0.0, 0, 1.0), (0.7, 20, 0.8)]
+
+
+def _check_batch(z, u, kinds, step=1000):
+    """The tokens of all rows in one call are those of `step` rows at a time;
+    kinds: index of each row's request in WIDE + LISTED."""
+    t, k, p = torch.tensor(WIDE + LISTED, device=DEV)[kinds].unbind(1)
+    t, k, p = t.contiguous(), k.to(torch.int32).contiguous(), p.contiguous()
+    tokens, logprob = sw.slimwise_sample(z, u, temperature=t, top_k=k, top_p=p)
+    for a in range(0, z.shape[0], step):
+        b = slice(a, a + step)
+        want = sw.slimwise_sample(z[b], u[b], temperature=t[b], top_k=k[b], top_p=p[b])
+        assert torch.equal(tokens[b], want[0]) and torch.equal(logprob[b], want[1]), a
+    assert bool((tokens >= 0).all()) and bool((logprob <= 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sample_passes_with_few_rows_left_over(dtype):
+    # four rows of each cluster are left over in every pass: the cluster's CTAs search them together
+    rows = 2 * PASS + 6000
+    z = _rows(rows, 301, dtype, seed=61, scale=1.0)
+    at = torch.arange(rows, device=DEV) // CLUSTERS
+    kinds = torch.where(at % 64 == 5, 0, len(WIDE))
+    _check_batch(z, torch.rand(rows, generator=_gen(62), device=DEV), kinds)
