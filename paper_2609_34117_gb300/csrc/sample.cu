@@ -617,8 +617,12 @@ __device__ __forceinline__ void search_rows(const T *logits, int64_t stride, int
         search_row(part, d, parity, a.tokens + t, a.logprob + t, sh);
         __syncthreads();  // the next row's bins lie where this one's steps are read
       }
-    if (alone) cluster.sync();  // before others write here again
-    else __syncthreads();       // every warp has read sh.left to its end
+    if (alone) {
+      cluster.sync();  // before others write here again
+      parity = 0;      // (each CTA's rows took another number of sums)
+    } else {
+      __syncthreads();  // every warp has read sh.left to its end
+    }
   }
   cluster.sync();  // no CTA ends while its sums can still be read or written
 }

@@ -51,3 +51,16 @@ def test_sample_passes_with_few_rows_left_over(dtype):
     at = torch.arange(rows, device=DEV) // CLUSTERS
     kinds = torch.where(at % 64 == 5, 0, len(WIDE))
     _check_batch(z, torch.rand(rows, generator=_gen(62), device=DEV), kinds)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [PASS + 44, 20000, 22000, 2 * PASS + 1500])
+def test_sample_passes_searched_in_either_way(rows, dtype):
+    # a tenth of the rows are left over, under requests that take unlike numbers of sums: in a full
+    # pass a CTA each searches them, in the last all of a cluster
+    z = _rows(rows, 1000, dtype, seed=63, scale=1.0)
+    g = _gen(64)
+    wide = torch.rand(rows, generator=g, device=DEV) < 0.1
+    kinds = torch.where(wide, torch.randint(0, len(WIDE), (rows,), generator=g, device=DEV),
+                        torch.randint(len(WIDE), len(WIDE + LISTED), (rows,), generator=g, device=DEV))
+    _check_batch(z, torch.rand(rows, generator=g, device=DEV), kinds)
