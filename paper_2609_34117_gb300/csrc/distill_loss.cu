@@ -11,7 +11,9 @@
 // Q is summed over the elements outside S, not taken as 1 - the list's mass,
 // which a student that is nearly sure would cancel to nothing: a bit per
 // element, set in shared memory before the row is read, takes the list's
-// elements out of the sums.
+// elements out of the sums.  Where the list lies far above all of them, they keep
+// a reference of their own, so that Q and the residual's share r q_i / Q hold
+// however small Q is.
 //
 // A cluster handles a row.  For the gradient each CTA has its part copied into
 // shared memory, in chunks that are all asked for at once, and sums exponentials
@@ -42,6 +44,10 @@ constexpr int kAhead = 2;                            // steps that the loss alon
 constexpr int kChunksMax = kSliceMax / (kChunk * 16) + 1;
 static_assert(kTopMax <= kLossThreads, "one thread per list entry");
 constexpr int kLossCluster = 16;                     // most CTAs of a row
+// Bits of the exponent between the row's largest logit and the largest outside the
+// list from which on those outside have a reference of their own: they then add next
+// to nothing to the row's sum, and below it the largest of them is far from underflow.
+constexpr float kFarBits = 40.0f;
 constexpr int kLaneParts = kLossCluster * kLossWarps / 32;  // of the cluster's warps, a lane's
 
 struct LossArgs {
@@ -286,22 +292,24 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
 
   // the row's sums, by each warp for itself: the parts, and the list
   float4 part[kLaneParts];
-  float z_top = -INFINITY;
+  float top = kFloorRef;
 #pragma unroll
   for (int j = 0; j < kLaneParts; ++j) {
     const int i = lane + 32 * j;
     part[j] = make_float4(kFloorRef, 0.0f, 0.0f, 0.0f);
     if (i < C * kLossWarps) part[j] = parts[i];
-    z_top = fmaxf(z_top, part[j].x);
+    top = fmaxf(top, part[j].x);
   }
-  for (int i = lane; i < a.K; i += 32) z_top = fmaxf(z_top, sh.z[i]);
-  ref = fmaxf(warp_max(z_top), kFloorRef);
+  const float rest_top = warp_max(top);
+  for (int i = lane; i < a.K; i += 32) top = fmaxf(top, sh.z[i]);
+  ref = warp_max(top);
+  const float rest_ref = (ref - rest_top) * c2 > kFarBits ? rest_top : ref;
   float rest1 = 0.0f, rest2 = 0.0f;
 #pragma unroll
   for (int j = 0; j < kLaneParts; ++j) {
     if (32 * j >= C * kLossWarps) break;
-    rest1 += part[j].y * exp_from(part[j].x, ref, c1);
-    if constexpr (kTemp) rest2 += part[j].z * exp_from(part[j].x, ref, c2);
+    rest1 += part[j].y * exp_from(part[j].x, rest_ref, c1);
+    if constexpr (kTemp) rest2 += part[j].z * exp_from(part[j].x, rest_ref, c2);
   }
   rest1 = warp_sum(rest1);
   rest2 = kTemp ? warp_sum(rest2) : rest1;
@@ -315,8 +323,11 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   }
   y_listed = __any_sync(0xFFFFFFFFu, y_listed);
   const float lr = a.log_rest[t], r = expf(lr);
-  const float total1 = bad || lost ? NAN : rest1 + warp_sum(list1);
-  const float total2 = kTemp ? (bad || lost ? NAN : rest2 + warp_sum(list2)) : total1;
+  // totals against ref: the elements outside the list count for scale1, scale2 (1
+  // where their reference is the row's)
+  const float scale1 = exp_from(rest_ref, ref, c1), scale2 = kTemp ? exp_from(rest_ref, ref, c2) : scale1;
+  const float total1 = bad || lost ? NAN : fmaf(rest1, scale1, warp_sum(list1));
+  const float total2 = kTemp ? (bad || lost ? NAN : fmaf(rest2, scale2, warp_sum(list2))) : total1;
   M = warp_sum(M) + r;
   const float w = a.row_weight ? a.row_weight[t] : 1.0f;
   const float beta = (1.0f - a.alpha) * a.tau;
@@ -330,22 +341,23 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
     kl = warp_sum(kl);
     if (lane == 0) {
       const float ce = (log2f(total1) - (zy - ref) * c1) * kLn2;
-      const float kr = r > 0.0f ? r * (lr - (log2f(rest2) - l2) * kLn2) : 0.0f;
+      const float kr = r > 0.0f ? r * (lr - (log2f(rest2) - l2 + (rest_ref - ref) * c2) * kLn2) : 0.0f;
       a.row_loss[t] = a.alpha * ce + beta * a.tau * (kl + kr);
     }
   }
   if constexpr (kGrad) {
-    // outside the list: A e1 + B e2 (B into A when there is one softmax)
+    // outside the list: A e1 + B e2, exponentials against rest_ref (B into A when
+    // there is one softmax).  A listed element's may overflow; it is written again.
     const float share = rest2 > 0.0f ? r / rest2 : 0.0f;
-    float A = w * a.alpha / total1;
-    float B = w * beta * (M / total2 - share);
+    float A = w * a.alpha * scale1 / total1;
+    float B = w * beta * (M * scale2 / total2 - share);
     if constexpr (!kTemp) A += B;
     auto outside = [&](float x) {
-      float v = A * exp_from(x, ref, c1);
-      if constexpr (kTemp) v = fmaf(B, exp_from(x, ref, c2), v);
+      float v = A * exp_from(x, rest_ref, c1);
+      if constexpr (kTemp) v = fmaf(B, exp_from(x, rest_ref, c2), v);
       return v;
     };
-    const uint64_t mr = pair(-ref, -ref), cc1 = pair(c1, c1), cc2 = pair(c2, c2);
+    const uint64_t mr = pair(-rest_ref, -rest_ref), cc1 = pair(c1, c1), cc2 = pair(c2, c2);
     const uint64_t AA = pair(A, A), BB = pair(B, B);
     auto window = [&](uint4 v, auto put) {
       constexpr int P = E / 2;

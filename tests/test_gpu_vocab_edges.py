@@ -7,7 +7,7 @@ import torch
 
 import paper_2609_34117_gb300 as sw
 
-from tests.test_gpu_vocab import DEV, TYPES, _gen, _rows
+from tests.test_gpu_vocab import DEV, MASS, TYPES, _check_loss, _gen, _loss64, _rows
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,25 @@ def test_sample_passes_searched_in_either_way(rows, dtype):
     kinds = torch.where(wide, torch.randint(0, len(WIDE), (rows,), generator=g, device=DEV),
                         torch.randint(len(WIDE), len(WIDE + LISTED), (rows,), generator=g, device=DEV))
     _check_batch(z, torch.rand(rows, generator=g, device=DEV), kinds)
+
+
+# ---------------------------------------------------------------------------
+# distillation loss
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gap,tau", [(60, 1.0), (87, 1.0), (90, 1.0), (104, 1.0), (150, 1.0), (200, 1.0),
+                                     (200, 2.0), (9, 0.1), (14, 0.15), (16, 0.2), (30, 0.05)])
+def test_distill_loss_mass_outside_the_list_far_below_it(gap, tau, dtype):
+    # the student's mass outside the list is e^(-gap / tau), and the teacher's any
+    z = _rows(6, 20000, dtype, seed=65, scale=0.5)
+    ids = torch.arange(5, 20000, 1000, device=DEV)
+    z[:, ids] += gap
+    rest = torch.tensor([-0.7, -10.0, -40.0, -90.0, -100.0, -0.01], device=DEV)
+    logp = torch.log(-torch.expm1(rest) / 20)[:, None].expand(6, 20).contiguous()
+    labels = torch.tensor([5, 6, 1005, 2005, 5, 19999], dtype=torch.int32, device=DEV)
+    top = ids.to(torch.int32).expand(6, 20).contiguous()
+    weight = torch.tensor([1.0, 8.0, 0.5, 1.0, 8.0, 8.0], device=DEV)
+    _check_loss(z, labels, top, logp, rest, alpha=0.1, tau=tau, weight=weight)
+    row = sw.slimwise_distill_loss(z, labels, top, logp, rest, temperature=tau, grad=False)[1]
+    want = _loss64(z.double(), labels, top, logp, rest, 0.1, tau)[0]
+    assert bool(((row.double() - want).abs() <= 4 * MASS * (1 + tau * tau) + 2.0 ** -20 * want.abs()).all())
