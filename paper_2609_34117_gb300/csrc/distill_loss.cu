@@ -332,17 +332,19 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   const float w = a.row_weight ? a.row_weight[t] : 1.0f;
   const float beta = (1.0f - a.alpha) * a.tau;
   if (rank == 0 && tid < 32) {
-    const float l2 = log2f(total2);
+    // CE and tau KL from differences of logits as they are: those from a logit of the
+    // type's lowest value are finite, and not so times log2 e or over a small tau
+    const float l1 = logf(total1), l2 = kTemp ? a.tau * logf(total2) : l1;
     float kl = 0.0f;
     for (int i = lane; i < a.K; i += 32) {
       const float P = sh.p[i];
-      if (P > 0.0f) kl += P * (sh.lp[i] - ((sh.z[i] - ref) * c2 - l2) * kLn2);
+      if (P > 0.0f) kl += P * (a.tau * sh.lp[i] + l2 - (sh.z[i] - ref));
     }
     kl = warp_sum(kl);
     if (lane == 0) {
-      const float ce = (log2f(total1) - (zy - ref) * c1) * kLn2;
-      const float kr = r > 0.0f ? r * (lr - (log2f(rest2) - l2 + (rest_ref - ref) * c2) * kLn2) : 0.0f;
-      a.row_loss[t] = a.alpha * ce + beta * a.tau * (kl + kr);
+      const float ce = l1 - (zy - ref);
+      const float kr = r > 0.0f ? r * (a.tau * (lr - logf(rest2 / total2)) - (rest_ref - ref)) : 0.0f;
+      a.row_loss[t] = a.alpha * ce + beta * (kl + kr);
     }
   }
   if constexpr (kGrad) {

@@ -7,7 +7,7 @@ import torch
 
 import paper_2609_34117_gb300 as sw
 
-from tests.test_gpu_vocab import DEV, MASS, TYPES, _check_loss, _gen, _loss64, _rows
+from tests.test_gpu_vocab import DEV, INF, MASS, TYPES, _check_loss, _gen, _loss64, _rows, _targets
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,37 @@ def test_distill_loss_mass_outside_the_list_far_below_it(gap, tau, dtype):
     row = sw.slimwise_distill_loss(z, labels, top, logp, rest, temperature=tau, grad=False)[1]
     want = _loss64(z.double(), labels, top, logp, rest, 0.1, tau)[0]
     assert bool(((row.double() - want).abs() <= 4 * MASS * (1 + tau * tau) + 2.0 ** -20 * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0])
+def test_distill_loss_of_lowest_values(tau, dtype):
+    # the label, a listed token, all that is not listed at the type's lowest value: losses of 1e34
+    # to 1e37, not infinite
+    low = torch.finfo(dtype).min
+    z = _rows(3, 9001, dtype, seed=66)
+    ids, logp, rest = _targets(z, 20, tau, 4)
+    labels = torch.tensor([4000, int(ids[1, 0]), int(ids[2, 1])], dtype=torch.int32, device=DEV)
+    z[0, 4000] = low
+    z[1, int(ids[1, 5])] = low
+    keep = torch.zeros(9001, dtype=torch.bool, device=DEV)
+    keep[ids[2].long()] = True
+    z[2] = torch.where(keep, z[2], low)
+    loss, row, grad = sw.slimwise_distill_loss(z, labels, ids, logp, rest, alpha=0.1, temperature=tau)
+    z64 = z.double()
+    want, mark, P, r, _ = _loss64(z64, labels, ids, logp, rest, 0.1, tau)
+    # (in the loss's type: 0.9 tau r 3.4e38 of the last row passes its range at tau 2)
+    assert torch.equal(torch.isfinite(row), torch.isfinite(want.float()))
+    fin = torch.isfinite(row)
+    assert bool(((row.double() - want).abs() <= 2.0 ** -20 * want.abs())[fin].all()) and bool((want > 1e30).all())
+    # the gradient by its formula, the shares of the rest among themselves: logsumexp's own gradient
+    # does not hold at -3e38, where 64 bits do not tell the log of a sum of 8981 from that of one
+    p, q = torch.softmax(z64, 1), torch.softmax(z64 / tau, 1)
+    onehot = torch.zeros_like(p).scatter_(1, labels.long()[:, None], 1.0)
+    listed = torch.zeros_like(p).scatter_(1, ids.long(), P)
+    share = torch.softmax((z64 / tau).masked_fill(mark, -INF), 1) * r[:, None] + listed
+    M, beta = (P.sum(1) + r)[:, None], 0.9 * tau
+    g = 0.1 * (p - onehot) + beta * (M * q - share)
+    tol = 2 * MASS * (0.1 * (p + onehot) + beta * (M * q + share)) + 1e-38
+    tol = tol + (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -22) * g.abs()
+    assert bool(((grad.double() - g).abs() <= tol).all())
