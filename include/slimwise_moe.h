@@ -427,7 +427,8 @@ int slimwise_top_logits(const void *logits, int32_t dtype, int32_t rows, int32_t
  *                it otherwise (SLIMWISE_ERR_INVALID_ARG).  Rows that start at
  *                the same offset from a 16-byte boundary as the logits' are
  *                written fastest.
- * A label or id >= vocab gives its row NaN loss and gradient; NaN and +inf
+ * A label or id >= vocab gives its row NaN loss and gradient, and so does a NaN
+ * among its targets (a teacher's row without a distribution); NaN and +inf
  * logits spread over their row as they do in the formulas.  Where Q is 0 with
  * r > 0 the loss is +inf and the residual's share of the gradient is left out.
  */

@@ -334,16 +334,17 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   if (rank == 0 && tid < 32) {
     // CE and tau KL from differences of logits as they are: those from a logit of the
     // type's lowest value are finite, and not so times log2 e or over a small tau
+    // (a target that is not a number is not 0: it makes the loss NaN, as the gradient)
     const float l1 = logf(total1), l2 = kTemp ? a.tau * logf(total2) : l1;
     float kl = 0.0f;
     for (int i = lane; i < a.K; i += 32) {
       const float P = sh.p[i];
-      if (P > 0.0f) kl += P * (a.tau * sh.lp[i] + l2 - (sh.z[i] - ref));
+      if (P != 0.0f) kl += P * (a.tau * sh.lp[i] + l2 - (sh.z[i] - ref));
     }
     kl = warp_sum(kl);
     if (lane == 0) {
       const float ce = l1 - (zy - ref);
-      const float kr = r > 0.0f ? r * (a.tau * (lr - logf(rest2 / total2)) - (rest_ref - ref)) : 0.0f;
+      const float kr = r != 0.0f ? r * (a.tau * (lr - logf(rest2 / total2)) - (rest_ref - ref)) : 0.0f;
       a.row_loss[t] = a.alpha * ce + beta * (kl + kr);
     }
   }

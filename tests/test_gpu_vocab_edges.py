@@ -2,6 +2,8 @@
 than one pass of the search takes, masses far below the largest logit, targets
 and weights without a value.  Tokens are exact; the other tolerances are those of
 test_gpu_vocab.py, or derived at the test."""
+import math
+
 import pytest
 import torch
 
@@ -120,3 +122,22 @@ def test_distill_loss_of_lowest_values(tau, dtype):
     tol = 2 * MASS * (0.1 * (p + onehot) + beta * (M * q + share)) + 1e-38
     tol = tol + (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -22) * g.abs()
     assert bool(((grad.double() - g).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("alpha", [0.0, 0.1, 1.0])
+def test_distill_loss_of_targets_without_a_distribution(alpha, dtype):
+    teacher = _rows(6, 9001, dtype, seed=68)
+    z = _rows(6, 9001, dtype, seed=69)
+    labels = torch.tensor([3, 4, 5, 6, 7, 8], dtype=torch.int32, device=DEV)
+    clean = sw.slimwise_top_logits(teacher, 64)
+    want = sw.slimwise_distill_loss(z, labels, *clean, alpha=alpha)
+    teacher[1, 7] = math.nan
+    teacher[2, 9] = INF
+    ids, logp, rest = sw.slimwise_top_logits(teacher, 64)
+    logp[3, 5] = math.nan
+    rest[4] = math.nan
+    loss, row, grad = sw.slimwise_distill_loss(z, labels, ids, logp, rest, alpha=alpha)
+    assert math.isnan(float(loss)) and bool(torch.isnan(row[1:5]).all()) and bool(torch.isnan(grad[1:5]).all())
+    for t in (0, 5):
+        assert torch.equal(row[t], want[1][t]) and torch.equal(grad[t], want[2][t])
