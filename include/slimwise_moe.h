@@ -409,7 +409,8 @@ int slimwise_top_logits(const void *logits, int32_t dtype, int32_t rows, int32_t
  *   KL_t = sum_j P_j (log P_j - log q_j) + r (log r - log Q), with
  *          P_j = exp top_logp[t, j], r = exp log_rest[t],
  *          q = softmax(z_t / temperature), q_j at top_ids[t, j], and Q the
- *          mass of q outside the list (terms with P_j = 0 or r = 0 are 0)
+ *          mass of q outside the list (terms with P_j = 0 or r = 0 are 0, and
+ *          so is an infinite CE or KL whose factor is 0)
  *   loss = sum_t row_weight[t] L_t,   grad[t] = row_weight[t] dL_t / dz_t
  *
  *   labels       int32 [rows]; a negative label leaves its row out: L_t = 0

@@ -345,7 +345,9 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
     if (lane == 0) {
       const float ce = l1 - (zy - ref);
       const float kr = r != 0.0f ? r * (a.tau * (lr - logf(rest2 / total2)) - (rest_ref - ref)) : 0.0f;
-      a.row_loss[t] = a.alpha * ce + beta * (kl + kr);
+      // an infinite term without weight is 0, as it is in the gradient
+      auto weighted = [](float by, float x) { return by == 0.0f && x == INFINITY ? 0.0f : by * x; };
+      a.row_loss[t] = weighted(a.alpha, ce) + weighted(beta, kl + kr);
     }
   }
   if constexpr (kGrad) {

@@ -141,3 +141,28 @@ def test_distill_loss_of_targets_without_a_distribution(alpha, dtype):
     assert math.isnan(float(loss)) and bool(torch.isnan(row[1:5]).all()) and bool(torch.isnan(grad[1:5]).all())
     for t in (0, 5):
         assert torch.equal(row[t], want[1][t]) and torch.equal(grad[t], want[2][t])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+def test_distill_loss_terms_without_weight(tau, dtype):
+    z = _rows(2, 9001, dtype, seed=67)
+    ids, logp, rest = _targets(z, 20, tau, 4)
+    labels = torch.tensor([40, 41], dtype=torch.int32, device=DEV)
+    z[0, 40] = -INF
+    # alpha 0: the label's infinite cross entropy does not count
+    row, grad = sw.slimwise_distill_loss(z, labels, ids, logp, rest, alpha=0.0, temperature=tau)[1:]
+    want = sw.slimwise_distill_loss(z, labels + 3, ids, logp, rest, alpha=0.0, temperature=tau)[1:]
+    assert bool(torch.isfinite(row).all()) and torch.equal(row, want[0]) and torch.equal(grad, want[1])
+    # alpha 1: nor does an infinite divergence
+    z[1, int(ids[1, 3])] = -INF
+    labels = torch.tensor([42, 43], dtype=torch.int32, device=DEV)
+    row, grad = sw.slimwise_distill_loss(z, labels, ids, logp, rest, alpha=1.0, temperature=tau)[1:]
+    ce = -torch.log_softmax(z.double(), 1).gather(1, labels.long()[:, None])[:, 0]
+    assert bool(((row.double() - ce).abs() <= 2 * MASS + 2.0 ** -20 * ce.abs()).all())
+    assert bool(torch.isfinite(grad).all())
+    # what is not a number still shows
+    z[0, 7] = math.nan
+    for alpha in (0.0, 1.0):
+        row = sw.slimwise_distill_loss(z, labels, ids, logp, rest, alpha=alpha, temperature=tau)[1]
+        assert bool(torch.isnan(row[0])) and bool(torch.isfinite(row[1])) == (alpha == 1.0)
