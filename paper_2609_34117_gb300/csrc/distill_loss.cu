@@ -424,9 +424,9 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
 
 // loss = sum of weight x row loss: thread i adds its rows i, i + 1024, ... in
 // order, in fp64, then a butterfly and the warps in turn: the same every time.
+// (row_loss is still written when this kernel starts: no __restrict__)
 __global__ void __launch_bounds__(1024)
-    loss_sum_kernel(const float *__restrict__ row_loss, const float *__restrict__ row_weight,
-                    int rows, float *__restrict__ loss) {
+    loss_sum_kernel(const float *row_loss, const float *__restrict__ row_weight, int rows, float *loss) {
   __shared__ double part[32];
   pdl_wait_primary();
   double s = 0.0;
