@@ -414,7 +414,8 @@ int slimwise_top_logits(const void *logits, int32_t dtype, int32_t rows, int32_t
  *   loss = sum_t row_weight[t] L_t,   grad[t] = row_weight[t] dL_t / dz_t
  *
  *   labels       int32 [rows]; a negative label leaves its row out: L_t = 0
- *                and a gradient row of zeros, whatever the row holds
+ *                and a gradient row of zeros, whatever the row, its targets
+ *                and its weight hold
  *   top_ids      int32 [rows, k], distinct within a row (else the row's
  *                results are undefined); negative: the entry is absent
  *   top_logp, log_rest  fp32, as slimwise_top_logits writes them

@@ -422,16 +422,21 @@ __global__ void __launch_bounds__(kLossThreads, kGrad ? kGradCtas : kLossCtas)
   }
 }
 
-// loss = sum of weight x row loss: thread i adds its rows i, i + 1024, ... in
-// order, in fp64, then a butterfly and the warps in turn: the same every time.
+// loss = sum of weight x row loss over the rows with a label, whatever the others'
+// weights (1 / the number of labelled rows may be 1 / 0): thread i adds its rows i,
+// i + 1024, ... in order, in fp64, then a butterfly and the warps in turn: the same
+// every time.
 // (row_loss is still written when this kernel starts: no __restrict__)
 __global__ void __launch_bounds__(1024)
-    loss_sum_kernel(const float *row_loss, const float *__restrict__ row_weight, int rows, float *loss) {
+    loss_sum_kernel(const float *row_loss, const int32_t *__restrict__ labels,
+                    const float *__restrict__ row_weight, int rows, float *loss) {
   __shared__ double part[32];
   pdl_wait_primary();
   double s = 0.0;
-  for (int t = threadIdx.x; t < rows; t += 1024)
-    s += (double)row_loss[t] * (row_weight ? (double)row_weight[t] : 1.0);
+  for (int t = threadIdx.x; t < rows; t += 1024) {
+    const double l = (double)row_loss[t] * (row_weight ? (double)row_weight[t] : 1.0);
+    s += labels[t] >= 0 ? l : 0.0;
+  }
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
@@ -526,7 +531,7 @@ cudaError_t launch_distill_loss(const void *logits, int dtype, int rows, int voc
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, loss_sum_kernel, (const float *)row_loss, row_weight, rows, loss);
+  return cudaLaunchKernelEx(&cfg, loss_sum_kernel, (const float *)row_loss, labels, row_weight, rows, loss);
 }
 
 }  // namespace slimwise

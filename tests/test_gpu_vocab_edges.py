@@ -166,3 +166,20 @@ def test_distill_loss_terms_without_weight(tau, dtype):
     for alpha in (0.0, 1.0):
         row = sw.slimwise_distill_loss(z, labels, ids, logp, rest, alpha=alpha, temperature=tau)[1]
         assert bool(torch.isnan(row[0])) and bool(torch.isfinite(row[1])) == (alpha == 1.0)
+
+
+def test_distill_loss_rows_left_out_whatever_their_weight():
+    # 1 / the number of labelled rows, where there are none, is no number
+    z = _rows(5, 2001, torch.float32, seed=70)
+    args = _targets(z, 20, 1.0, 4)
+    labels = torch.tensor([3, -100, 5, -1, -100], dtype=torch.int32, device=DEV)
+    w = torch.tensor([0.25, math.nan, 0.75, INF, -INF], device=DEV)
+    want = sw.slimwise_distill_loss(z, labels, *args, row_weight=torch.nan_to_num(w, 0.0, 0.0, 0.0))
+    loss, row, grad = sw.slimwise_distill_loss(z, labels, *args, row_weight=w)
+    assert all(torch.equal(a, b) for a, b in zip((loss, row, grad), want))
+    none = torch.full_like(labels, -100)
+    loss, row, grad = sw.slimwise_distill_loss(z, none, *args, row_weight=(none >= 0).float() / (none >= 0).sum())
+    assert float(loss) == 0.0 and not bool(row.any()) and not bool(grad.any())
+    # a row that is trained on shows such a weight
+    w[0] = math.nan
+    assert math.isnan(float(sw.slimwise_distill_loss(z, labels, *args, row_weight=w)[0]))
