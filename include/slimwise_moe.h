@@ -423,7 +423,8 @@ int slimwise_top_logits(const void *logits, int32_t dtype, int32_t rows, int32_t
  *   alpha        in [0, 1];  temperature in [1e-6, 1e6]
  *   row_weight   fp32 [rows], NULL: 1 each
  *   row_loss     fp32 [rows]   L_t, without its weight
- *   loss         fp32 [1], NULL to skip; the same bits on every run
+ *   loss         fp32 [1], NULL to skip; the same bits on every run (not
+ *                written where there are no rows)
  *   grad         dtype [rows, vocab] at grad_stride >= vocab, NULL to skip.
  *                It may be `logits` itself (same stride) and may not overlap
  *                it otherwise (SLIMWISE_ERR_INVALID_ARG).  Rows that start at

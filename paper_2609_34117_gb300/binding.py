@@ -514,12 +514,14 @@ def slimwise_distill_loss(logits, labels, top_ids, top_logp, log_rest, alpha=0.1
     if row_loss is None:
         row_loss = torch.empty(rows, dtype=_F32, device=logits.device)
     if loss is None:
-        # the sum over no rows is not computed by a kernel
-        loss = (torch.empty if rows else torch.zeros)(1, dtype=_F32, device=logits.device)
+        loss = torch.empty(1, dtype=_F32, device=logits.device)
     _check(load().slimwise_distill_loss(
         *row_args, p_labels, p_ids, p_logp, p_rest, k, alpha, temperature, p_weight,
         _vec(row_loss, _F32, one, "row_loss", dev), _vec(loss, _F32, (1,), "loss", dev),
         g_ptr, g_stride, _stream(stream)), "slimwise_distill_loss")
+    if rows == 0:  # the sum over no rows is not computed by a kernel
+        with torch.cuda.stream(stream):
+            loss.zero_()
     return loss, row_loss, grad
 
 

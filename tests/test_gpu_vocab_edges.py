@@ -183,3 +183,17 @@ def test_distill_loss_rows_left_out_whatever_their_weight():
     # a row that is trained on shows such a weight
     w[0] = math.nan
     assert math.isnan(float(sw.slimwise_distill_loss(z, labels, *args, row_weight=w)[0]))
+
+
+def test_distill_loss_of_no_rows_writes_the_loss_it_was_given():
+    loss = torch.full((1,), 7.0, device=DEV)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        loss.fill_(7.0)
+        torch.cuda.synchronize()
+        out = sw.slimwise_distill_loss(torch.empty((0, 100), device=DEV), torch.empty(0, **i32),
+                                       torch.empty((0, 8), **i32), torch.empty((0, 8), device=DEV),
+                                       torch.empty(0, device=DEV), loss=loss, stream=stream)[0]
+        torch.cuda.synchronize()
+        assert out is loss and float(loss) == 0.0
