@@ -461,6 +461,17 @@ def _vec(t, dtype, shape, name, index):
     raise ValueError(f"{name} must be on cuda:{index}")
 
 
+def _new(stream, shape, dtype, device, strides=None):
+    """An output of a call on `stream`, in that stream's memory: a block that the
+    current stream gave back may still be in use there."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _new(None, shape, dtype, device, strides)
+    if strides is not None:
+        return torch.empty_strided(shape, strides, dtype=dtype, device=device)
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def slimwise_top_logits(logits, k, temperature=1.0, ids=None, logp=None, log_rest=None,
                         stream=None):
     """A teacher's distillation targets: the k largest logits of each row as
@@ -469,11 +480,11 @@ def slimwise_top_logits(logits, k, temperature=1.0, ids=None, logp=None, log_res
     row_args = _logits(logits)
     rows, k, dev = row_args[2], int(k), logits.get_device()
     if ids is None:
-        ids = torch.empty((rows, max(k, 0)), dtype=_I32, device=logits.device)
+        ids = _new(stream, (rows, max(k, 0)), _I32, logits.device)
     if logp is None:
-        logp = torch.empty((rows, max(k, 0)), dtype=_F32, device=logits.device)
+        logp = _new(stream, (rows, max(k, 0)), _F32, logits.device)
     if log_rest is None:
-        log_rest = torch.empty(rows, dtype=_F32, device=logits.device)
+        log_rest = _new(stream, (rows,), _F32, logits.device)
     _check(load().slimwise_top_logits(
         *row_args, k, temperature, _vec(ids, _I32, (rows, k), "ids", dev),
         _vec(logp, _F32, (rows, k), "logp", dev), _vec(log_rest, _F32, (rows,), "log_rest", dev),
@@ -502,8 +513,7 @@ def slimwise_distill_loss(logits, labels, top_ids, top_logp, log_rest, alpha=0.1
     p_rest = _vec(log_rest, _F32, one, "log_rest", dev)
     p_weight = None if row_weight is None else _vec(row_weight, _F32, one, "row_weight", dev)
     if grad is True:
-        grad = torch.empty_strided((rows, vocab), (stride, 1), dtype=logits.dtype,
-                                   device=logits.device)
+        grad = _new(stream, (rows, vocab), logits.dtype, logits.device, (stride, 1))
         g_ptr, g_stride = grad.data_ptr(), stride
     elif grad is False or grad is None:
         grad, g_ptr, g_stride = None, None, 0
@@ -512,9 +522,9 @@ def slimwise_distill_loss(logits, labels, top_ids, top_logp, log_rest, alpha=0.1
         if g_code != code or (g_rows, g_vocab) != (rows, vocab) or grad.get_device() != dev:
             raise ValueError("grad must have the logits' type, shape and device")
     if row_loss is None:
-        row_loss = torch.empty(rows, dtype=_F32, device=logits.device)
+        row_loss = _new(stream, one, _F32, logits.device)
     if loss is None:
-        loss = torch.empty(1, dtype=_F32, device=logits.device)
+        loss = _new(stream, (1,), _F32, logits.device)
     _check(load().slimwise_distill_loss(
         *row_args, p_labels, p_ids, p_logp, p_rest, k, alpha, temperature, p_weight,
         _vec(row_loss, _F32, one, "row_loss", dev), _vec(loss, _F32, (1,), "loss", dev),
@@ -535,9 +545,9 @@ def slimwise_sample(logits, uniform, temperature=None, top_k=None, top_p=None, m
     rows, dev = row_args[2], logits.get_device()
     one = (rows,)
     if tokens is None:
-        tokens = torch.empty(rows, dtype=_I32, device=logits.device)
+        tokens = _new(stream, one, _I32, logits.device)
     if logprob is None:
-        logprob = torch.empty(rows, dtype=_F32, device=logits.device)
+        logprob = _new(stream, one, _F32, logits.device)
     _check(load().slimwise_sample(
         *row_args, None if temperature is None else _vec(temperature, _F32, one, "temperature", dev),
         None if top_k is None else _vec(top_k, _I32, one, "top_k", dev),

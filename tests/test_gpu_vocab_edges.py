@@ -197,3 +197,28 @@ def test_distill_loss_of_no_rows_writes_the_loss_it_was_given():
                                        torch.empty(0, device=DEV), loss=loss, stream=stream)[0]
         torch.cuda.synchronize()
         assert out is loss and float(loss) == 0.0
+
+
+# ---------------------------------------------------------------------------
+# all three
+# ---------------------------------------------------------------------------
+def test_outputs_are_memory_of_the_stream_that_writes_them():
+    # a block that the current stream has just given back may still be in use there
+    rows, vocab, k = 256, 4001, 64
+    z = _rows(rows, vocab, torch.float32, seed=71)
+    top = sw.slimwise_top_logits(z, k)
+    labels, u = top[0][:, 0].contiguous(), torch.rand(rows, generator=_gen(72), device=DEV)
+    side = torch.cuda.Stream()
+    calls = [lambda: sw.slimwise_top_logits(z, k, stream=side),
+             lambda: sw.slimwise_distill_loss(z, labels, *top, stream=side),
+             lambda: sw.slimwise_sample(z, u, stream=side)]
+    for call in calls:
+        torch.cuda.synchronize()
+        shapes = [(t.shape, t.dtype) for t in call()]
+        side.synchronize()
+        given_back = [torch.empty(s, dtype=d, device=DEV) for s, d in shapes * 4]
+        at = {t.data_ptr() for t in given_back}
+        del given_back
+        out = call()
+        side.synchronize()
+        assert not at & {t.data_ptr() for t in out}
