@@ -496,8 +496,9 @@ def slimwise_distill_loss(logits, labels, top_ids, top_logp, log_rest, alpha=0.1
                           row_weight=None, grad=True, row_loss=None, loss=None, stream=None):
     """Distillation loss of a student's logits against a teacher's targets
     (Sec. 3.3, Eq. 3) and its gradient.  grad: True to allocate the gradient (in
-    the logits' type and row stride), False for the loss alone, or the tensor to
-    write (`logits` itself: in place).  row_weight: fp32 [rows], e.g. 1 / the
+    the logits' type and row stride; rows next to each other where the logits' are
+    more than twice their length apart), False for the loss alone, or the tensor
+    to write (`logits` itself: in place).  row_weight: fp32 [rows], e.g. 1 / the
     number of labelled rows; None: 1 each.  Returns (loss fp32 [1], row losses
     fp32 [rows], gradient or None)."""
     row_args = _logits(logits)
@@ -513,8 +514,11 @@ def slimwise_distill_loss(logits, labels, top_ids, top_logp, log_rest, alpha=0.1
     p_rest = _vec(log_rest, _F32, one, "log_rest", dev)
     p_weight = None if row_weight is None else _vec(row_weight, _F32, one, "row_weight", dev)
     if grad is True:
-        grad = _new(stream, (rows, vocab), logits.dtype, logits.device, (stride, 1))
-        g_ptr, g_stride = grad.data_ptr(), stride
+        # rows far apart (one position of many) are not worth their distance in memory;
+        # what a 16-byte boundary leaves of it stays, for which rows are written fastest
+        g_stride = stride if stride <= 2 * vocab else vocab + (stride - vocab) % 8
+        grad = _new(stream, (rows, vocab), logits.dtype, logits.device, (g_stride, 1))
+        g_ptr = grad.data_ptr()
     elif grad is False or grad is None:
         grad, g_ptr, g_stride = None, None, 0
     else:

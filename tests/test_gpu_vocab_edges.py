@@ -199,6 +199,23 @@ def test_distill_loss_of_no_rows_writes_the_loss_it_was_given():
         assert out is loss and float(loss) == 0.0
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("between", [1, 8, 63, 4001])
+def test_distill_gradient_of_rows_far_apart_takes_rows_of_its_own(between, dtype):
+    # the last of 16 positions: 15 rows and more lie between two of the logits'
+    rows, vocab = 6, 4001
+    every = _rows(rows, 16 * vocab + between, dtype, seed=74)
+    z = every[:, 15 * vocab:16 * vocab]
+    args = (torch.arange(rows, dtype=torch.int32, device=DEV),) + _targets(z, 20, 1.0, 4)
+    loss, row, grad = sw.slimwise_distill_loss(z, *args)
+    want = sw.slimwise_distill_loss(z, *args, grad=torch.empty_strided(z.shape, z.stride(), dtype=dtype, device=DEV))
+    assert torch.equal(row, want[1]) and torch.equal(grad, want[2])
+    assert grad.untyped_storage().nbytes() <= rows * (vocab + 8) * grad.element_size()
+    # rows that are nearly next to each other keep their stride
+    z = _rows(rows, vocab, dtype, seed=75, pad=between % 64)
+    assert sw.slimwise_distill_loss(z, *args)[2].stride() == z.stride()
+
+
 # ---------------------------------------------------------------------------
 # all three
 # ---------------------------------------------------------------------------
