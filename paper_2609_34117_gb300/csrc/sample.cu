@@ -53,14 +53,22 @@ constexpr float kWeightOne = 1099511627776.0f;  // 2^40, the largest element's w
 // Bound of the relative difference between the scan's float sum of the elements
 // that are not listed and the sum of their weights (but for the weights'
 // truncation, one part in 2^40 each).  An element at 2^-x of the largest weighs
-// less than its truncation beyond x = 40, and elements there or at lesser depths
-// have exponents that are rounded three times in the one and twice in the other,
-// logarithm's base and quotient included: 40 (1.5 2^-23 + 2^-23) ln 2 < 2^-16.8;
-// exp2's and exp's own 2^-22, and sums of 19 roundings (8 in a unit, 2 of the
-// compensated sum, 8 + 1 over threads and CTAs) 2^-19.7; and 2^-22 more each time
-// that a warp's reference is raised, at most 5 + 48 times (48 cuts of a list: 3072
-// units of a warp, 64 between two cuts): 2^-15.3 in all.
-constexpr uint64_t kMassError = 1 << 15;  // one part in
+// less than its truncation beyond x = 40.  In units of 2^-24, along the longest way
+// that an element's share can take:
+//   145  exponents of 40 bits: of the scan rounded three times, and the logarithm's
+//        base; of the weights twice (the quotient 1 / T is the same in both)
+//     8  exp2's and exp's own
+//   290  58 changes of a sum's reference, a factor of exp2 and a product: 4 at
+//        refreshes, 48 at cuts of a warp's list (3072 units of it, 64 between two
+//        cuts), 6 in most_of_many() and the join
+//   217  additions of units that are dropped from the list: their factor, and four to
+//        a lane at each refresh and cut and at the row's end
+//    32  additions of windows, elements and keys in most_of_many() and the join
+//    52  of the row's end: windows and elements of the listed units to a lane
+//    32  sums of a unit, over steps (compensated), threads and CTAs
+//     5  the reference's factor
+// which are 781 or less than 2^-14 in all.
+constexpr uint64_t kMassError = 1 << 14;  // one part in
 
 // What a search uses of shared memory, where the scan's was.
 constexpr int kBins = 2048;
