@@ -69,6 +69,38 @@ def test_sample_passes_searched_in_either_way(rows, dtype):
 
 
 # ---------------------------------------------------------------------------
+# top logits
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab,k", [(9, 20011, 64), (3, 131072, 256), (700, 4097, 20)])
+@pytest.mark.parametrize("tau", [1.0, 4.0, 30.0])
+def test_top_logits_rest_near_the_whole_mass(tau, rows, vocab, k, dtype):
+    # log_rest = -log(1 + list / rest): what the ratio of the two sums is off by, times the list's
+    # share, and two roundings.  A sum is off by at most 2^-16 (exponents of at most 40 bits of three
+    # roundings each, 83 parts in 2^24; exp2's 4; 40 additions; 5 changes of reference of 5)
+    z = _rows(rows, vocab, dtype, seed=73)
+    ids, logp, rest = sw.slimwise_top_logits(z, k, temperature=tau)
+    lp = torch.log_softmax(z.double() / tau, 1)
+    want = torch.logsumexp(lp.scatter(1, ids.long(), -INF), 1)
+    share = -torch.expm1(want)
+    assert bool(((rest.double() - want).abs() <= 2.0 ** -15 * share + 2.0 ** -22 * want.abs()).all())
+    want = lp.gather(1, ids.long())
+    assert bool(((logp.double() - want).abs() <= 2.0 ** -16 + 2.0 ** -22 * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_top_logits_of_lowest_values(dtype):
+    # a listed element at the type's lowest value has a finite log-probability, as its quotient has
+    z = torch.full((2, 5003), -INF, dtype=dtype, device=DEV)
+    z[:, 100:140] = torch.finfo(dtype).min
+    z[:, 7] = 1.5
+    for tau in (1.0, 2.0):
+        ids, logp, rest = sw.slimwise_top_logits(z, 20, temperature=tau)
+        want = torch.log_softmax(z.double() / tau, 1).gather(1, ids.long())
+        assert bool(((logp.double() - want).abs() <= 2.0 ** -22 * want.abs() + 2.0 ** -16).all())
+
+
+# ---------------------------------------------------------------------------
 # distillation loss
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", TYPES)
