@@ -30,19 +30,10 @@ namespace slimwise {
 constexpr int kFewStages = 3;
 __host__ __device__ constexpr int top_stages(int ctas) { return ctas == kFewCtas ? kFewStages : kManyStages; }
 
-// The log of the others' mass as a share of the whole: of `rest` times e^scale beside
-// `top`.  A difference of two logarithms would cancel where they hold most of it, and
-// where they hold next to nothing the product underflow.
-__device__ __noinline__ float log_share(float rest, float scale, float top) {
-  const float mass = rest * expf(scale);
-  if (mass >= top) return -log1pf(top / mass);
-  return mass > 0x1p-60f ? logf(mass / (mass + top)) : logf(rest) + scale - logf(mass + top);
-}
-
 template <typename T, bool kCluster, bool kLong, int kCtas>
 __global__ void __launch_bounds__(kScanThreads, kCtas)
     top_logits_kernel(const T *__restrict__ logits, int64_t stride, int rows, int vocab, int K,
-                      float c, float tau, int32_t *__restrict__ ids, float *__restrict__ logp,
+                      float c, float inv, int32_t *__restrict__ ids, float *__restrict__ logp,
                       float *__restrict__ log_rest) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int kStages = top_stages(kCtas);
@@ -76,21 +67,26 @@ __global__ void __launch_bounds__(kScanThreads, kCtas)
       if (tid < K) e = exp_from(sh.by_rank[tid], m, c);
       else rest += exp_from(sh.by_rank[tid], last, c);
     }
-    const float scale = (last - m) / tau;  // log of the rest's scale
+    const float scale = (last - m) * inv;  // log of the rest's scale
     rest = block_reduce<kScanThreads>(rest, sh.redf, OpAdd());
     const float top = block_reduce<kScanThreads>(e, sh.redf, OpAdd());
-    const float log_total = logf(fmaf(rest, expf(scale), top));
+    const float mass = rest * expf(scale), total = mass + top, log_total = logf(total);
     const int64_t at = (int64_t)t * K;
     if (key && rank < K) {
       ids[at + rank] = (int32_t)key_index(key);
-      logp[at + rank] = (key_value(key) - m) / tau - log_total;
+      logp[at + rank] = (key_value(key) - m) * inv - log_total;
     }
     // a row with NaN can have fewer candidates than K
     if (tid >= n && tid < K) {
       ids[at + tid] = -1;
       logp[at + tid] = NAN;
     }
-    if (tid == 0) log_rest[t] = log_share(rest, scale, top);
+    // of the rest's share, not a difference of two logarithms, which cancels where
+    // the rest is most of the row; but so where the rest's mass underflows
+    if (tid == 0)
+      log_rest[t] = mass >= top        ? -log1pf(__fdividef(top, mass))
+                    : mass > 0x1p-60f ? logf(__fdividef(mass, total))
+                                      : logf(rest) + scale - log_total;
   });
 }
 
@@ -117,7 +113,7 @@ static cudaError_t launch_top(const ScanGrid &g, const void *logits, int rows, i
   return launch_clusters<top_logits_kernel<T, kCluster, kLong, kCtas>>(
       g.clusters, g.C, kScanThreads, g.smem,
       scan_smem(top_stages(kCtas), list_room(most), most, kCluster ? kClusterMax : 1, kLong), stream,
-      static_cast<const T *>(logits), stride, rows, vocab, k, kLog2e / temperature, temperature, ids, logp, log_rest);
+      static_cast<const T *>(logits), stride, rows, vocab, k, kLog2e / temperature, 1.0f / temperature, ids, logp, log_rest);
 }
 template <typename T, bool kLong>
 static cudaError_t launch_top(const void *logits, int rows, int vocab, int64_t stride, int k,
