@@ -66,11 +66,7 @@ struct LossShared {
   uint64_t parts;                         // counts the bytes of the cluster's warps' sums
 };
 
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-  return v;
-}
+__device__ __forceinline__ float warp_max(float v) { return unordered(__reduce_max_sync(0xFFFFFFFFu, ordered(v))); }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
