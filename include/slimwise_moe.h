@@ -380,9 +380,9 @@ int slimwise_moe_device_status(const void *workspace, void *stream,
  * They need no workspace, keep no state, and do not synchronise.  What only
  * the device can see (a NaN logit, an id outside the vocabulary) is reported
  * in that row's results, as each entry point says.  The results of a row do
- * not depend on what the other rows hold.  How many they are decides how a row
- * is split, and so the last bits of a sum in floats; a sampled token and its
- * log-probability are the same in any batch.
+ * not depend on what the other rows hold.  How many they are, and how far from a
+ * 16-byte boundary it starts, decide how a row is split, and so the last bits of a
+ * sum in floats; a sampled token and its log-probability are the same in any batch.
  */
 enum { SLIMWISE_DTYPE_BF16 = 0, SLIMWISE_DTYPE_FP32 = 1 };
 
@@ -427,7 +427,8 @@ int slimwise_top_logits(const void *logits, int32_t dtype, int32_t rows, int32_t
  *                written where there are no rows)
  *   grad         dtype [rows, vocab] at grad_stride >= vocab, NULL to skip.
  *                It may be `logits` itself (same stride) and may not overlap
- *                it otherwise (SLIMWISE_ERR_INVALID_ARG).  Rows that start at
+ *                it otherwise (SLIMWISE_ERR_INVALID_ARG); with the same stride
+ *                its rows may lie between the logits'.  Rows that start at
  *                the same offset from a 16-byte boundary as the logits' are
  *                written fastest.
  * A label or id >= vocab gives its row NaN loss and gradient, and so does a NaN

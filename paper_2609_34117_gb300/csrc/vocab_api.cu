@@ -68,7 +68,11 @@ int slimwise_distill_loss(const void *logits, int32_t dtype, int32_t rows, int32
     const uintptr_t a = reinterpret_cast<uintptr_t>(logits), b = reinterpret_cast<uintptr_t>(grad);
     const uintptr_t an = (uintptr_t)size * ((uintptr_t)(rows - 1) * row_stride + vocab);
     const uintptr_t bn = (uintptr_t)size * ((uintptr_t)(rows - 1) * grad_stride + vocab);
-    if (a < b + bn && b < a + an) return SLIMWISE_ERR_INVALID_ARG;
+    // (rows of one buffer beside each other do not overlap: the same stride, columns apart)
+    const int64_t step = size * row_stride, row = size * (int64_t)vocab;
+    const int64_t apart = ((int64_t)(b - a) % step + step) % step;
+    const bool beside = grad_stride == row_stride && apart >= row && apart + row <= step;
+    if (a < b + bn && b < a + an && !beside) return SLIMWISE_ERR_INVALID_ARG;
   }
   return status(launch_distill_loss(logits, dtype, rows, vocab, row_stride, labels, top_ids,
                                     top_logp, log_rest, k, alpha, temperature, row_weight,

@@ -248,6 +248,29 @@ def test_distill_gradient_of_rows_far_apart_takes_rows_of_its_own(between, dtype
     assert sw.slimwise_distill_loss(z, *args)[2].stride() == z.stride()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("first,then", [(0, 2001), (0, 2008), (2016, 0), (2003, 1)])
+def test_distill_gradient_beside_the_logits_in_one_buffer(first, then, dtype):
+    rows, vocab = 5, 2001
+    z = _rows(rows, vocab, dtype, seed=76)
+    args = (torch.arange(rows, dtype=torch.int32, device=DEV),) + _targets(z, 20, 1.0, 4)
+    both = torch.full((rows, 4020), 7.0, dtype=dtype, device=DEV)
+    own, grad = both[:, first:first + vocab], both[:, then:then + vocab]
+    own.copy_(z)
+    # the same gradient apart, whose rows start where these do
+    want = sw.slimwise_distill_loss(own, *args, grad=torch.zeros_like(both)[:, then:then + vocab])
+    got = sw.slimwise_distill_loss(own, *args, grad=grad)
+    assert torch.equal(own, z) and all(torch.equal(a, b) for a, b in zip(got, want))
+    keep = torch.ones(4020, dtype=torch.bool, device=DEV)
+    keep[first:first + vocab] = keep[then:then + vocab] = False
+    assert bool((both[:, keep] == 7.0).all())
+    # a column that both have is refused
+    for at in (first + vocab - 1, first + 1, first - 1):
+        if 0 <= at <= 4020 - vocab:
+            with pytest.raises(sw.SlimwiseError):
+                sw.slimwise_distill_loss(own, *args, grad=both[:, at:at + vocab])
+
+
 # ---------------------------------------------------------------------------
 # all three
 # ---------------------------------------------------------------------------
