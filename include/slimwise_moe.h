@@ -394,9 +394,10 @@ enum { SLIMWISE_DTYPE_BF16 = 0, SLIMWISE_DTYPE_FP32 = 1 };
  *   ids          int32 [rows, k]  larger logit first, ties to the lower id
  *   logp         fp32 [rows, k]   z / temperature - logsumexp(z / temperature)
  *   log_rest     fp32 [rows]      log of the mass of all other elements
- *                                 (-inf: none)
+ *                                 (-inf: none; one below 2^-126 of the list's
+ *                                 last element counts as none)
  * A row with NaN or +inf, or of -inf alone, has NaN in logp and log_rest; ids
- * are then the largest of the other elements, padded with -1.
+ * are then the largest of the elements that are not NaN, padded with -1.
  */
 int slimwise_top_logits(const void *logits, int32_t dtype, int32_t rows, int32_t vocab,
                         int64_t row_stride, int32_t k, float temperature, int32_t *ids,

@@ -24,8 +24,8 @@
 // the list by itself, and the gradient is computed from shared memory: one read
 // and one write of the row, which bound the kernel.
 //
-// 4096 rows of 131072 bf16 with the gradient: 346 us, 5.9 TB/s (0.87 of a copy);
-// 1021 rows of 65537 fp32 at a temperature 98 us, 5.2 TB/s, with two exponentials
+// 4096 rows of 131072 bf16 with the gradient: 350 us, 5.8 TB/s (0.86 of a copy);
+// 1021 rows of 65537 fp32 at a temperature 97 us, 5.3 TB/s, with two exponentials
 // an element in each direction; the loss alone of 2048 rows of 150001 bf16 103 us,
 // 5.4 TB/s.  What is left is the CTAs' turns: a part is read, summed, exchanged
 // and written, and with three parts on an SM reads do not always overlap writes.
@@ -38,7 +38,10 @@ constexpr int kLossThreads = 256;
 constexpr int kLossWarps = kLossThreads / 32;
 constexpr int kLossUnroll = 4;
 constexpr int kChunk = kLossThreads * kLossUnroll;  // windows of a step, and of a copy (16 KB)
-constexpr int kGradCtas = 4, kLossCtas = 5;            // CTAs of an SM, with and without gradient
+// CTAs of an SM, with and without gradient.  The loss alone of 2048 x 150001 bf16
+// takes 8 us longer with four; at a temperature, where five spill 64 bytes a thread,
+// it takes the same with both (147 to 149 us, around the whole call).
+constexpr int kGradCtas = 4, kLossCtas = 5;
 constexpr int kSliceMax = 200 * 1024;               // bytes of a row that one CTA may hold
 constexpr int kAhead = 2;                            // steps that the loss alone prefetches
 constexpr int kChunksMax = kSliceMax / (kChunk * 16) + 1;

@@ -26,11 +26,14 @@
 //
 // 512 rows of 262144 bf16 under mixed requests: 68 us, 3.9 TB/s, four rows on some
 // SMs and three on others (47 us at the least); 256 of 150001 fp32 43 us, 3.6 TB/s,
-// one or two rows on an SM, whose copies in flight do not fill the memory's latency;
-// 64 of 131072 fp32 with top-p 22.5 us; one row 14.5 us, latency.  A search costs
-// more: 512 rows of 131072 bf16 without any filter 128 us (by its instructions), with
-// top-k 1000 475, with a nucleus of 0.9 of nearly flat rows 0.9 ms (the
-// histograms' atomics in shared memory).
+// one or two rows on an SM.  What takes the rest of both is not established: issue
+// slots are 36 and 64 % busy, DRAM 52 and 53 %, and more copies in flight (a third
+// stage of the rings) gain nothing.  64 rows of 131072 fp32 with top-p 22.5 us, one
+// row 15 us: one after the other a launch, the scan, the join and the decision.  A
+// search costs more: 512 rows of 131072 bf16 without any filter 128 us (by its
+// instructions), with top-k 1000 475, with a nucleus of 0.9 of nearly flat rows 0.9
+// ms (the histograms' atomics in shared memory); its functions spill up to 164 bytes
+// a thread.
 #include "vocab.cuh"
 
 namespace slimwise {
@@ -252,7 +255,7 @@ struct KeptWeight {  // their weights, if they are kept (kAll: all are)
 
 // Bins of a pass: counts, or masses (kMass), of the elements within `in` whose bits
 // from `known` up are the prefix's, by their bits from `shift` to there.  A
-// function of its own for the registers.
+// function of its own (inlined, top-k 1000 of 512 x 131072 bf16 took 531 us, not 475).
 template <bool kMass, typename T>
 __device__ __noinline__ void histogram(const Part<T> part, const Limit in, int known, int shift,
                                        uint32_t prefix, SearchShared &sh) {

@@ -10,13 +10,13 @@
 // teacher that is nearly sure leaves 1e-6, which the difference would not hold.
 //
 // One read of the logits (vocab.cuh has the scan), a few hundred bytes written a
-// row.  4096 rows of 131072 bf16, K = 64: 222 us, 4.8 TB/s (0.71 of a copy), with
+// row.  4096 rows of 131072 bf16, K = 64: 223 us, 4.8 TB/s (0.71 of a copy), with
 // the schedulers issuing in 79 % of the cycles: bound by its instructions, 12.5 a
 // warp and 32 elements, of which a step's exponentials and sums are 3.6 and the
 // rest the maxima, copies, lists, thresholds and a row's end.  511 rows of 150001
 // fp32: 70 us, 4.3 TB/s; 511 rows on 152 SMs leave some with four and some with
-// three, which alone takes 54.  One row of 131072 bf16: 13 us, the latency of a
-// launch, 8 CTAs' scan and the leader's join.  Above K = 64 a kernel of its own
+// three, which alone takes 54.  One row of 131072 bf16: 13 us, one after the other a
+// launch, 8 CTAs' scan and the leader's join (their shares are not measured).  Above K = 64 a kernel of its own
 // holds long lists and candidates, and leaves room for three CTAs on an SM: 4096
 // rows of 131072 bf16 at K = 100 281 us, at K = 256 428 (selecting and ranking 256
 // of about 450 candidates a row); 1181 of 22705 bf16 at K = 256 89 us.
