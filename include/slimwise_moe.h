@@ -472,6 +472,111 @@ int slimwise_sample(const void *logits, int32_t dtype, int32_t rows, int32_t voc
                     const float *top_p, const float *min_p, const float *uniform,
                     int32_t *tokens, float *logprob, void *stream);
 
+/*
+ * Operators around the layer: the ends of the model whose middle it is, for
+ * training and for serving.  The embedding's lookup, the norm and the head's cross
+ * entropy, each with its gradient.  Shared by them:
+ *
+ *   - Rows are bf16 or fp32 (dtype) of any start, length and stride, in elements,
+ *     unless an entry point says otherwise (they need their elements' alignment;
+ *     rows that start on 16-byte boundaries are fastest); other arrays are 4-byte
+ *     aligned.  0 <= rows <= 2^20 and strides of at least a row (else
+ *     SLIMWISE_ERR_INVALID_ARG); 1 <= hidden <= 16384 (else UNSUPPORTED_SHAPE).
+ *   - Outputs may overlap neither inputs, nor each other, nor the workspace
+ *     (INVALID_ARG); of two matrices of one stride the rows may lie between each
+ *     other's.  Nothing outside the rows is written.
+ *   - 0 rows are a no-op (the table's gradient without accumulate is still zeroed).
+ *   - A workspace needs no initialisation and may be reused by ordered calls.
+ *   - Results do not depend on timing: sums are made in an order that sizes,
+ *     alignment, labels and ids decide, in fp32 (the loss's in fp64), and rounded
+ *     once to the output's type.
+ */
+
+/*
+ * out[i] = scale table[ids[i]] (0 <= ids[i] < vocab); ids[i] < 0 (padding): zeros;
+ * ids[i] >= vocab: NaN.
+ *   table  dtype [vocab, hidden] at row_stride, 1 <= vocab <= 2^20
+ *   ids    int32 [rows];  scale finite;  out  dtype [rows, hidden] at out_stride
+ */
+int slimwise_embed(const void *table, int32_t dtype, int32_t vocab, int32_t hidden,
+                   int64_t row_stride, const int32_t *ids, int32_t rows, float scale, void *out,
+                   int64_t out_stride, void *stream);
+
+/*
+ * The table's gradient: out[v] = scale sum over i with ids[i] = v of grad[i];
+ * tokens that do not occur get zeros, or, with accumulate, all rows are added to
+ * what `out` holds (a tied head's gradient, an earlier batch).  Ids outside
+ * [0, vocab) take part in nothing.
+ *   grad  dtype [rows, hidden] at row_stride
+ *   out   out_dtype [vocab, hidden] at out_stride, either type
+ *   workspace  256-byte aligned, slimwise_embed_grad_workspace_size() bytes
+ */
+int slimwise_embed_grad_workspace_size(int32_t rows, int32_t hidden, size_t *bytes);
+int slimwise_embed_grad(const void *grad, int32_t dtype, int32_t rows, int32_t hidden,
+                        int64_t row_stride, const int32_t *ids, float scale, void *out,
+                        int32_t out_dtype, int32_t vocab, int64_t out_stride, int32_t accumulate,
+                        void *stream, void *workspace, size_t workspace_bytes);
+
+/*
+ * Layer norm (layer != 0) or RMS norm of rows:
+ *   mu = mean x (RMS: 0),  r = 1 / sqrt(mean (x - mu)^2 + eps)
+ *   y  = (x - mu) r weight + bias
+ *   x, y    dtype [rows, hidden] at row_stride, y_stride
+ *   weight  fp32 [hidden];  bias  fp32 [hidden], NULL: 0;  0 <= eps <= 1e30
+ *   mean    fp32 [rows] mu: given for layer norm, NULL for RMS norm
+ *   rstd    fp32 [rows] r
+ */
+int slimwise_norm(const void *x, int32_t dtype, int32_t rows, int32_t hidden, int64_t row_stride,
+                  const float *weight, const float *bias, int32_t layer, float eps, void *y,
+                  int64_t y_stride, float *mean, float *rstd, void *stream);
+
+/*
+ * Its gradient, with n = (x - mean) rstd and g = dy weight:
+ *   dx = rstd (g - mean g - n mean(n g))   (RMS norm, mean NULL: without mean g)
+ *   dweight = sum over rows of dy n,  dbias = sum over rows of dy
+ *   dy, x, dx  dtype [rows, hidden];  mean, rstd as slimwise_norm wrote them
+ *   dweight    fp32 [hidden];  dbias  fp32 [hidden], NULL to skip (and for RMS norm)
+ *   workspace  slimwise_norm_grad_workspace_size() bytes
+ */
+int slimwise_norm_grad_workspace_size(int32_t rows, int32_t hidden, size_t *bytes);
+int slimwise_norm_grad(const void *dy, int64_t dy_stride, const void *x, int32_t dtype, int32_t rows,
+                       int32_t hidden, int64_t row_stride, const float *weight, const float *mean,
+                       const float *rstd, void *dx, int64_t dx_stride, float *dweight, float *dbias,
+                       void *stream, void *workspace, size_t workspace_bytes);
+
+/*
+ * Cross entropy of the logits z = hidden weight^T, which are not kept, and its
+ * gradients:
+ *   L_t  = log sum_v exp z_tv - z_t[label_t],   loss = sum_t row_weight[t] L_t
+ *   grad_hidden = dz weight,  grad_weight = dz^T hidden,
+ *   dz_tv = row_weight[t] (softmax(z_t)_v - [v = label_t])
+ *   hidden       bf16 [rows, width] at hidden_stride
+ *   weight       bf16 [vocab, width] at weight_stride (the head)
+ *                width a multiple of 8; 1 <= vocab <= 393216; these and the
+ *                gradients have rows on 16-byte boundaries (else UNSUPPORTED_SHAPE)
+ *   labels       int32 [rows]; a negative label leaves its row out: L_t = 0 and
+ *                a gradient row of zeros, whatever the row and its weight hold
+ *   row_weight   fp32 [rows], NULL: 1 each
+ *   row_loss     fp32 [rows];  loss  fp32 [1], NULL to skip
+ *   grad_hidden  bf16 [rows, width], NULL to skip
+ *   grad_weight  grad_weight_dtype [vocab, width], NULL to skip
+ *   workspace    256-byte aligned, slimwise_linear_loss_workspace_size() bytes for
+ *                the gradients asked for: 2 bytes for each row and token, at most
+ *                2^31 of them, and less beside
+ * A row with a label >= vocab, a NaN or a logit of +inf has NaN loss and gradient,
+ * and grad_weight is then NaN where the formula has it.  dz's numerators (which the
+ * products take) and the rows scaled by their weights are rounded to bf16.  A device
+ * wait that gave up is reported by slimwise_moe_device_status(workspace, ...).
+ */
+int slimwise_linear_loss_workspace_size(int32_t rows, int32_t width, int32_t vocab,
+                                        int32_t grad_hidden, int32_t grad_weight, size_t *bytes);
+int slimwise_linear_loss(const void *hidden, int64_t hidden_stride, const void *weight,
+                         int64_t weight_stride, int32_t rows, int32_t width, int32_t vocab,
+                         const int32_t *labels, const float *row_weight, float *row_loss, float *loss,
+                         void *grad_hidden, int64_t grad_hidden_stride, void *grad_weight,
+                         int32_t grad_weight_dtype, int64_t grad_weight_stride, void *stream,
+                         void *workspace, size_t workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,6 +10,11 @@ from .binding import (  # noqa: F401
     alloc_workspace,
     load,
     slimwise_distill_loss,
+    slimwise_embed,
+    slimwise_embed_grad,
+    slimwise_embed_grad_workspace_size,
+    slimwise_linear_loss,
+    slimwise_linear_loss_workspace_size,
     slimwise_moe_compact_layer,
     slimwise_moe_decode,
     slimwise_moe_decode_ex,
@@ -22,6 +27,9 @@ from .binding import (  # noqa: F401
     slimwise_moe_select_retained,
     slimwise_moe_shared_workspace_size,
     slimwise_moe_workspace_size,
+    slimwise_norm,
+    slimwise_norm_grad,
+    slimwise_norm_grad_workspace_size,
     slimwise_sample,
     slimwise_top_logits,
 )

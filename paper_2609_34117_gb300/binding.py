@@ -37,6 +37,9 @@ EXPORTED = (
     "slimwise_moe_decode_shared_ex", "slimwise_moe_expert_stats", "slimwise_moe_select_retained",
     "slimwise_moe_noalloc_device_status", "slimwise_moe_compact_layer",
     "slimwise_top_logits", "slimwise_distill_loss", "slimwise_sample",
+    "slimwise_embed", "slimwise_embed_grad_workspace_size", "slimwise_embed_grad",
+    "slimwise_norm", "slimwise_norm_grad_workspace_size", "slimwise_norm_grad",
+    "slimwise_linear_loss_workspace_size", "slimwise_linear_loss",
 )
 
 
@@ -104,6 +107,15 @@ def load(path: str | None = None) -> ctypes.CDLL:
             lib.slimwise_top_logits.argtypes = rows + [i32, f32, P, P, P, P]
             lib.slimwise_distill_loss.argtypes = rows + [P, P, P, P, i32, f32, f32, P, P, P, P, i64, P]
             lib.slimwise_sample.argtypes = rows + [P] * 8
+            lib.slimwise_embed.argtypes = [P, i32, i32, i32, i64, P, i32, f32, P, i64, P]
+            lib.slimwise_embed_grad_workspace_size.argtypes = [i32, i32, ctypes.POINTER(sz)]
+            lib.slimwise_embed_grad.argtypes = [P, i32, i32, i32, i64, P, f32, P, i32, i32, i64, i32, P, P, sz]
+            lib.slimwise_norm.argtypes = [P, i32, i32, i32, i64, P, P, i32, f32, P, i64, P, P, P]
+            lib.slimwise_norm_grad_workspace_size.argtypes = [i32, i32, ctypes.POINTER(sz)]
+            lib.slimwise_norm_grad.argtypes = [P, i64, P, i32, i32, i32, i64, P, P, P, P, i64, P, P, P, P, sz]
+            lib.slimwise_linear_loss_workspace_size.argtypes = [i32] * 5 + [ctypes.POINTER(sz)]
+            lib.slimwise_linear_loss.argtypes = [P, i64, P, i64, i32, i32, i32, P, P, P, P, P, i64, P, i32,
+                                                 i64, P, P, sz]
             for name in EXPORTED[1:]:
                 getattr(lib, name).restype = ctypes.c_int
             _lib = lib
@@ -560,3 +572,203 @@ def slimwise_sample(logits, uniform, temperature=None, top_k=None, top_p=None, m
         _vec(uniform, _F32, one, "uniform", dev), _vec(tokens, _I32, one, "tokens", dev),
         _vec(logprob, _F32, one, "logprob", dev), _stream(stream)), "slimwise_sample")
     return tokens, logprob
+
+
+_U8 = torch.uint8
+
+
+def _matrix(t, name, dtype=None, shape=None, index=None):
+    """_logits of a matrix, of the given type, shape and device where these are given."""
+    args = _logits(t, name)
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if index is not None and t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index}")
+    return args
+
+
+def _scratch(workspace, size, args, what, stream, device):
+    """(workspace, pointer, bytes): the given one, or a new one in the stream's memory."""
+    n = ctypes.c_size_t(0)
+    _check(size(*args, ctypes.byref(n)), what)
+    if workspace is None:
+        workspace = _new(stream, (n.value,), _U8, device)
+    else:
+        _dev(workspace, _U8, "workspace")
+        if workspace.device != device:
+            raise ValueError(f"workspace must be on {device}")
+    return workspace, workspace.data_ptr(), workspace.numel()
+
+
+def slimwise_embed(table, ids, scale=1.0, out=None, stream=None):
+    """Rows of an embedding table by token id (int32 [rows]), times scale; zeros for
+    ids below 0, NaN for ids outside the table.  Returns out [rows, hidden]."""
+    ptr, code, vocab, hidden, stride = _matrix(table, "table")
+    dev = table.get_device()
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise ValueError("ids must have one dimension")
+    rows = ids.shape[0]
+    p_ids = _vec(ids, _I32, (rows,), "ids", dev)
+    if out is None:
+        out = _new(stream, (rows, hidden), table.dtype, table.device)
+    o = _matrix(out, "out", table.dtype, (rows, hidden), dev)
+    _check(load().slimwise_embed(ptr, code, vocab, hidden, stride, p_ids, rows, scale, o[0], o[4],
+                                 _stream(stream)), "slimwise_embed")
+    return out
+
+
+def slimwise_embed_grad_workspace_size(rows: int, hidden: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().slimwise_embed_grad_workspace_size(rows, hidden, ctypes.byref(n)),
+           "slimwise_embed_grad_workspace_size")
+    return int(n.value)
+
+
+def slimwise_embed_grad(grad, ids, out, scale=1.0, accumulate=False, workspace=None, stream=None):
+    """The table's gradient, into out [vocab, hidden] (bf16 or fp32): each token's
+    rows of grad [rows, hidden] summed, times scale; all other rows zero, or, with
+    accumulate, added to what out holds.  Ids outside the table take part in
+    nothing.  Returns out."""
+    ptr, code, rows, hidden, stride = _matrix(grad, "grad")
+    dev = grad.get_device()
+    o_ptr, o_code, vocab, o_hidden, o_stride = _matrix(out, "out", index=dev)
+    if o_hidden != hidden:
+        raise ValueError(f"out must have rows of {hidden}, got {o_hidden}")
+    p_ids = _vec(ids, _I32, (rows,), "ids", dev)
+    lib = load()
+    workspace, w, n = _scratch(workspace, lib.slimwise_embed_grad_workspace_size, (rows, hidden),
+                               "slimwise_embed_grad", stream, grad.device)
+    _check(lib.slimwise_embed_grad(ptr, code, rows, hidden, stride, p_ids, scale, o_ptr, o_code, vocab,
+                                   o_stride, int(accumulate), _stream(stream), w, n), "slimwise_embed_grad")
+    return out
+
+
+def slimwise_norm(x, weight, bias=None, layer=False, eps=1e-5, y=None, mean=None, rstd=None, stream=None):
+    """Layer norm (layer=True) or RMS norm of the rows of x, with weight fp32
+    [hidden] and, where given, bias fp32 [hidden].  Returns (y, mean fp32 [rows] or
+    None for RMS norm, rstd fp32 [rows]); the last two are what the gradient needs."""
+    ptr, code, rows, hidden, stride = _matrix(x, "x")
+    dev, one, width = x.get_device(), (rows,), (hidden,)
+    if y is None:
+        y = _new(stream, (rows, hidden), x.dtype, x.device)
+    o = _matrix(y, "y", x.dtype, (rows, hidden), dev)
+    if rstd is None:
+        rstd = _new(stream, one, _F32, x.device)
+    if not layer:
+        if mean is not None:
+            raise ValueError("mean is layer norm's")
+    elif mean is None:
+        mean = _new(stream, one, _F32, x.device)
+    _check(load().slimwise_norm(
+        ptr, code, rows, hidden, stride, _vec(weight, _F32, width, "weight", dev),
+        None if bias is None else _vec(bias, _F32, width, "bias", dev), int(bool(layer)), eps, o[0], o[4],
+        None if mean is None else _vec(mean, _F32, one, "mean", dev), _vec(rstd, _F32, one, "rstd", dev),
+        _stream(stream)), "slimwise_norm")
+    return y, mean, rstd
+
+
+def slimwise_norm_grad_workspace_size(rows: int, hidden: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().slimwise_norm_grad_workspace_size(rows, hidden, ctypes.byref(n)),
+           "slimwise_norm_grad_workspace_size")
+    return int(n.value)
+
+
+def slimwise_norm_grad(dy, x, weight, rstd, mean=None, grad_bias=None, dx=None, dweight=None, dbias=None,
+                       workspace=None, stream=None):
+    """The norm's gradient from dy [rows, hidden], its input, weight and statistics
+    (mean: layer norm's; None: RMS norm).  grad_bias: whether the bias's gradient is
+    wanted (None: for layer norm).  Returns (dx, dweight fp32 [hidden], dbias fp32
+    [hidden] or None)."""
+    ptr, code, rows, hidden, stride = _matrix(x, "x")
+    dev, one, width = x.get_device(), (rows,), (hidden,)
+    d = _matrix(dy, "dy", x.dtype, (rows, hidden), dev)
+    if grad_bias is None:
+        grad_bias = mean is not None
+    if grad_bias and mean is None:
+        raise ValueError("the bias has a gradient in layer norm alone")
+    if dbias is not None and not grad_bias:
+        raise ValueError("dbias is given, but not wanted")
+    if dx is None:
+        dx = _new(stream, (rows, hidden), x.dtype, x.device)
+    o = _matrix(dx, "dx", x.dtype, (rows, hidden), dev)
+    if dweight is None:
+        dweight = _new(stream, width, _F32, x.device)
+    if grad_bias and dbias is None:
+        dbias = _new(stream, width, _F32, x.device)
+    lib = load()
+    workspace, w, n = _scratch(workspace, lib.slimwise_norm_grad_workspace_size, (rows, hidden),
+                               "slimwise_norm_grad", stream, x.device)
+    _check(lib.slimwise_norm_grad(
+        d[0], d[4], ptr, code, rows, hidden, stride, _vec(weight, _F32, width, "weight", dev),
+        None if mean is None else _vec(mean, _F32, one, "mean", dev), _vec(rstd, _F32, one, "rstd", dev),
+        o[0], o[4], _vec(dweight, _F32, width, "dweight", dev),
+        None if dbias is None else _vec(dbias, _F32, width, "dbias", dev), _stream(stream), w, n),
+        "slimwise_norm_grad")
+    if rows == 0:  # the sums over no rows are not computed by a kernel
+        with torch.cuda.stream(stream):
+            dweight.zero_()
+            if dbias is not None:
+                dbias.zero_()
+    return dx, dweight, dbias
+
+
+def slimwise_linear_loss_workspace_size(rows: int, hidden: int, vocab: int, grad_hidden=True,
+                                        grad_weight=True) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().slimwise_linear_loss_workspace_size(rows, hidden, vocab, int(bool(grad_hidden)),
+                                                      int(bool(grad_weight)), ctypes.byref(n)),
+           "slimwise_linear_loss_workspace_size")
+    return int(n.value)
+
+
+def slimwise_linear_loss(hidden, weight, labels, row_weight=None, grad_hidden=True, grad_weight=True,
+                         row_loss=None, loss=None, workspace=None, stream=None):
+    """Cross entropy of the head's logits hidden @ weight.T (bf16 [rows, width] and
+    [vocab, width]) at labels int32 [rows] (negative: the row is left out), without
+    keeping the logits, and its gradients.  row_weight fp32 [rows], e.g. 1 / the
+    number of labelled rows; None: 1 each.  grad_hidden, grad_weight: True to
+    allocate that gradient, False to leave it out, or the tensor to write (the
+    weight's in bf16 or fp32).  Returns (loss fp32 [1], row losses fp32 [rows],
+    gradient of hidden or None, gradient of weight or None)."""
+    bf16 = torch.bfloat16
+    h_ptr, _, rows, width, h_stride = _matrix(hidden, "hidden", bf16)
+    dev = hidden.get_device()
+    w_ptr, _, vocab, w_width, w_stride = _matrix(weight, "weight", bf16, index=dev)
+    if w_width != width:
+        raise ValueError(f"weight must have rows of {width}, got {w_width}")
+    one = (rows,)
+    p_labels = _vec(labels, _I32, one, "labels", dev)
+    p_weight = None if row_weight is None else _vec(row_weight, _F32, one, "row_weight", dev)
+
+    def gradient(g, shape, name, dtype):
+        if g is False or g is None:
+            return None, None, 0, 0
+        if g is True:
+            g = _new(stream, shape, bf16, hidden.device)
+            return g, g.data_ptr(), 0, width
+        ptr, code, _, _, stride = _matrix(g, name, dtype, shape, dev)
+        return g, ptr, code, stride
+
+    dh, dh_ptr, _, dh_stride = gradient(grad_hidden, (rows, width), "grad_hidden", bf16)
+    dw, dw_ptr, dw_code, dw_stride = gradient(grad_weight, (vocab, width), "grad_weight", None)
+    if row_loss is None:
+        row_loss = _new(stream, one, _F32, hidden.device)
+    if loss is None:
+        loss = _new(stream, (1,), _F32, hidden.device)
+    lib = load()
+    workspace, ws, n = _scratch(workspace, lib.slimwise_linear_loss_workspace_size,
+                                (rows, width, vocab, int(dh is not None), int(dw is not None)),
+                                "slimwise_linear_loss", stream, hidden.device)
+    _check(lib.slimwise_linear_loss(
+        h_ptr, h_stride, w_ptr, w_stride, rows, width, vocab, p_labels, p_weight,
+        _vec(row_loss, _F32, one, "row_loss", dev), _vec(loss, _F32, (1,), "loss", dev), dh_ptr, dh_stride,
+        dw_ptr, dw_code, dw_stride, _stream(stream), ws, n), "slimwise_linear_loss")
+    if rows == 0:  # the sums over no rows are not computed by a kernel
+        with torch.cuda.stream(stream):
+            loss.zero_()
+            if dw is not None:
+                dw.zero_()
+    return loss, row_loss, dh, dw

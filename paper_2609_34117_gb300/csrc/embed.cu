@@ -1,0 +1,435 @@
+// embed.cu -- rows of an embedding table by token id, and the table's gradient.
+//
+//   out[i]    = scale table[id_i]           (id < 0: zeros; id >= vocab: NaN)
+//   dtable[v] = scale sum over i with id_i = v of dout[i]
+//
+// Both move bytes: the lookup reads the rows asked for and writes them; the
+// gradient reads dout once and writes the whole table, most of it zeros.
+//
+// The gradient's order of summation must not depend on timing, so there are no
+// atomics on it.  One cluster sorts the positions by token (a stable radix sort
+// in two or three passes, histograms in shared memory) while the other CTAs
+// write the zeros of the tokens that do not occur; each of those finds its
+// tokens' presence by reading all ids.  The next kernel sums the sorted rows in
+// pieces of kPiece positions: a token that lies inside a piece is written, one
+// that crosses its border leaves fp32 sums, which a third kernel adds in order.
+// A token that occurs thousands of times is so spread over hundreds of CTAs.
+#include "train.cuh"
+
+namespace slimwise {
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// lookup
+// ---------------------------------------------------------------------------
+constexpr int kLookupThreads = 256, kLookupLoads = 8;
+
+// A warp copies strips of kLookupLoads accesses a lane.
+template <typename T, int V>
+__global__ void __launch_bounds__(kLookupThreads)
+    embed_kernel(const T *__restrict__ table, int vocab, int hidden, int64_t stride,
+                 const int32_t *__restrict__ ids, int rows, float scale, T *__restrict__ out,
+                 int64_t out_stride) {
+  constexpr int E = V == 1 && sizeof(T) == 2 ? 2 * kLookupLoads : V * kLookupLoads;
+  using Part = RowPart<T, V, E>;
+  constexpr int kStrip = 32 * E;
+  const int lane = threadIdx.x & 31;
+  const int strips = (hidden + kStrip - 1) / kStrip;
+  const int64_t all = (int64_t)rows * strips;
+  const int64_t warps = (int64_t)gridDim.x * (kLookupThreads / 32);
+  for (int64_t u = (int64_t)blockIdx.x * (kLookupThreads / 32) + (threadIdx.x >> 5); u < all; u += warps) {
+    const int i = (int)(u / strips), c = (int)(u % strips) * kStrip;
+    const int id = __ldg(ids + i);
+    Part p;
+    if (id >= 0 && id < vocab) {
+      p.load(table + (int64_t)id * stride + c, lane, 32, hidden - c);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) p.set2(e, p.get(e) * scale, p.get(e + 1) * scale);
+    } else {
+      const float v = id < 0 ? 0.0f : __int_as_float(0x7FC00000);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) p.set2(e, v, v);
+    }
+    p.store(out + (int64_t)i * out_stride + c, lane, 32, hidden - c);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// gradient
+// ---------------------------------------------------------------------------
+constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int kPiece = 32;        // sorted positions that a group sums
+constexpr int kSumThreads = 256;
+
+struct SortShared {
+  uint32_t count[kSortWarps][kDigits];  // of a warp's items, then where its next item goes
+  uint32_t total[kDigits];              // of the CTA's items
+  uint32_t scan[kSortWarps];
+};
+// Bits of the largest key: vocab itself, the key of ids outside the table.
+__host__ __device__ inline int key_bits(int vocab) {
+  int b = 1;
+  while (vocab >> b) ++b;
+  return b;
+}
+
+// An item: x = key, y = position.  The last pass leaves them in a.
+struct SortArgs {
+  const int32_t *ids;
+  int n, vocab;
+  uint2 *a, *b;
+};
+
+__device__ __forceinline__ uint32_t cluster_load(const uint32_t *p, uint32_t rank) {
+  return ld_shared_cluster(mapa_shared(smem_u32(p), rank));
+}
+
+// Stable sort by key, one cluster.  A warp holds a run of the items; the digits
+// of its items are counted (pass 1 of the data), counts become the warps' first
+// places, digit by digit, and the items are moved in order (pass 2).
+__device__ void sort_by_id(const SortArgs &s, SortShared &sh) {
+  const int cta = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int bits = key_bits(s.vocab), passes = (bits + kDigitBits - 1) / kDigitBits;
+  const int width = (bits + passes - 1) / passes;
+  // items of a warp, a multiple of 32
+  const int per = ((s.n + kSortCtas * kSortWarps - 1) / (kSortCtas * kSortWarps) + 31) / 32 * 32;
+  const int64_t first = (int64_t)(cta * kSortWarps + warp) * per;
+  const int lo = (int)(first < s.n ? first : s.n), hi = (int)(first + per < s.n ? first + per : s.n);
+  for (int pass = 0; pass < passes; ++pass) {
+    // the last pass writes s.a
+    const uint2 *src = (passes - pass) & 1 ? s.b : s.a;
+    uint2 *dst = (passes - pass) & 1 ? s.a : s.b;
+    const int shift = pass * width;
+    auto item = [&](int i) {
+      if (pass > 0) return __ldcg(src + i);
+      const int id = __ldg(s.ids + i);
+      return make_uint2(id >= 0 && id < s.vocab ? (uint32_t)id : (uint32_t)s.vocab, (uint32_t)i);
+    };
+    for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0u;
+    __syncthreads();
+    for (int i = lo; i < hi; i += 32) {
+      const bool in = i + lane < hi;
+      const uint32_t d = in ? (item(i + lane).x >> shift) & (kDigits - 1) : kDigits;
+      const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
+      if (in && (same & ((1u << lane) - 1)) == 0) sh.count[warp][d] += __popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    if (threadIdx.x < kDigits) {
+      uint32_t sum = 0;
+      for (int w = 0; w < kSortWarps; ++w) {
+        const uint32_t c = sh.count[w][threadIdx.x];
+        sh.count[w][threadIdx.x] = sum;
+        sum += c;
+      }
+      sh.total[threadIdx.x] = sum;
+    }
+    cluster_sync_all();
+    uint32_t before = 0, all = 0;  // this digit's items in earlier CTAs, in all
+    if (threadIdx.x < kDigits)
+      for (int c = 0; c < kSortCtas; ++c) {
+        const uint32_t v = cluster_load(&sh.total[threadIdx.x], (uint32_t)c);
+        before += c < cta ? v : 0u;
+        all += v;
+      }
+    // exclusive scan of `all` over the digits
+    uint32_t inc = all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    if (lane == 31) sh.scan[warp] = inc;
+    __syncthreads();
+    if (threadIdx.x < kDigits) {
+      uint32_t base = before + inc - all;
+      for (int w = 0; w < warp; ++w) base += sh.scan[w];
+      for (int w = 0; w < kSortWarps; ++w) sh.count[w][threadIdx.x] += base;
+    }
+    __syncthreads();
+    for (int i = lo; i < hi; i += 32) {
+      const bool in = i + lane < hi;
+      const uint2 v = in ? item(i + lane) : make_uint2(0, 0);
+      const uint32_t d = in ? (v.x >> shift) & (kDigits - 1) : kDigits;
+      const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
+      const uint32_t rank = __popc(same & ((1u << lane) - 1));
+      const uint32_t place = in ? sh.count[warp][d] + rank : 0u;
+      __syncwarp();
+      if (in) {
+        dst[place] = v;
+        if (rank == 0) sh.count[warp][d] += __popc(same);
+      }
+      __syncwarp();
+    }
+    // the pass's items, written by all CTAs, are read by the next; totals are read no more
+    __threadfence();
+    cluster_sync_all();
+  }
+}
+
+// Cluster 0 sorts; the CTAs of the others share the table's rows and write the
+// zeros of those without a token (`zero`: else there are no others).
+template <typename O, int V>
+__global__ void __launch_bounds__(kSortThreads)
+    embed_sort_kernel(SortArgs s, O *__restrict__ out, int hidden, int64_t out_stride) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  if (blockIdx.x < kSortCtas) {
+    sort_by_id(s, *reinterpret_cast<SortShared *>(smem));
+    return;
+  }
+  uint32_t *present = reinterpret_cast<uint32_t *>(smem);
+  const int ctas = gridDim.x - kSortCtas, per = (s.vocab + ctas - 1) / ctas;
+  const int64_t first = (int64_t)(blockIdx.x - kSortCtas) * per;
+  const int lo = (int)(first < s.vocab ? first : s.vocab);
+  const int rows = min(per, s.vocab - lo);
+  for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) present[i] = 0u;
+  __syncthreads();
+#pragma unroll 8
+  for (int i = threadIdx.x; i < s.n; i += kSortThreads) {
+    const int r = __ldg(s.ids + i) - lo;
+    if (r >= 0 && r < rows) atomicOr(present + (r >> 5), 1u << (r & 31));
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 31;
+  for (int r = threadIdx.x >> 5; r < rows; r += kSortWarps) {
+    if (present[r >> 5] >> (r & 31) & 1) continue;
+    O *row = out + (int64_t)(lo + r) * out_stride;
+    if constexpr (V * sizeof(O) == 16) {
+      for (int c = lane * V; c < hidden; c += 32 * V) *reinterpret_cast<uint4 *>(row + c) = make_uint4(0, 0, 0, 0);
+    } else {
+      for (int c = lane; c < hidden; c += 32) row[c] = O(0.0f);
+    }
+  }
+}
+
+struct SumArgs {
+  const uint2 *items;  // sorted
+  int n, vocab, hidden;
+  int64_t stride, out_stride;
+  float scale;
+  bool accumulate;
+  float *partial;  // [pieces][2][hidden]: of the run from the piece before, of the run into the next
+};
+
+// acc (fp32, as the columns of RowPart<., V, 8>) scaled, or added, into a row.
+template <typename O, int V>
+__device__ __forceinline__ void write_row(const float (&acc)[8], const SumArgs &a, O *row, int t,
+                                          int threads, int width) {
+  RowPart<O, V, 8> o;
+  if (a.accumulate) {
+    o.template load<true>(row, t, threads, width);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+      o.set2(e, fmaf(acc[e], a.scale, o.get(e)), fmaf(acc[e + 1], a.scale, o.get(e + 1)));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) o.set2(e, acc[e] * a.scale, acc[e + 1] * a.scale);
+  }
+  o.store(row, t, threads, width);
+}
+
+// A group of TPR threads sums a piece: runs inside it go to the table, its first
+// and last run to `partial` where they cross its border.
+template <typename T, typename O, int V, int TPR>
+__global__ void __launch_bounds__(kSumThreads)
+    embed_sum_kernel(const T *__restrict__ grad, SumArgs a, O *out) {
+  constexpr int kLoads = 4;
+  const int t = threadIdx.x % TPR;
+  const int piece = blockIdx.x * (kSumThreads / TPR) + threadIdx.x / TPR;
+  const int c0 = blockIdx.y * TPR * 8, width = a.hidden - c0;
+  pdl_wait_primary();
+  const int s = piece * kPiece;
+  if (s >= a.n) return;
+  const int end = min(s + kPiece, a.n);
+  const uint32_t before = s > 0 ? __ldcg(&a.items[s - 1].x) : ~0u;
+  const uint32_t after = end < a.n ? __ldcg(&a.items[end].x) : ~0u;
+  float acc[8];
+  uint32_t run = ~0u;
+  int start = s;
+  auto flush = [&](int stop) {
+    if (run >= (uint32_t)a.vocab) return;
+    if ((start == s && before == run) || (stop == end && after == run)) {
+      RowPart<float, V, 8> p;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) p.set2(e, acc[e], acc[e + 1]);
+      // (rows of `partial` are as far from 16 bytes as a row's length: by elements then)
+      float *row = a.partial + ((int64_t)piece * 2 + (start == s ? 0 : 1)) * a.hidden + c0;
+      p.store(row, t, TPR, width);
+    } else {
+      write_row<O, V>(acc, a, out + (int64_t)run * a.out_stride + c0, t, TPR, width);
+    }
+  };
+  for (int i = s; i < end; i += kLoads) {
+    uint2 it[kLoads];
+    RowPart<T, V, 8> p[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) it[j] = i + j < end ? __ldcg(a.items + i + j) : make_uint2(~0u, 0);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      if (it[j].x < (uint32_t)a.vocab) p[j].load(grad + (int64_t)it[j].y * a.stride + c0, t, TPR, width);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      if (it[j].x >= (uint32_t)a.vocab) continue;  // padding, sorted last
+      if (it[j].x != run) {
+        flush(i + j);
+        run = it[j].x;
+        start = i + j;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += p[j].get(e);
+    }
+  }
+  // (where padding follows the last run, `after` is its key and not the run's)
+  flush(end);
+}
+
+// A run that crosses pieces: the group of the piece where it begins adds the
+// pieces' sums in order.
+template <typename O, int V, int TPR>
+__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumArgs a, O *out) {
+  const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
+  const int piece = blockIdx.x * (kSumThreads / TPR) + threadIdx.x / TPR;
+  const int c0 = blockIdx.y * TPR * 8, width = a.hidden - c0;
+  pdl_wait_primary();
+  const int s = piece * kPiece, end = s + kPiece;
+  if (end >= a.n) return;
+  const uint32_t run = __ldcg(&a.items[end - 1].x);
+  if (run >= (uint32_t)a.vocab || __ldcg(&a.items[end].x) != run) return;
+  const bool whole = __ldcg(&a.items[s].x) == run;
+  if (whole && s > 0 && __ldcg(&a.items[s - 1].x) == run) return;  // begins before
+  // pieces that it reaches: those whose first position still is the run's
+  int last = piece;
+  for (bool more = true; more;) {
+    const int64_t at = (int64_t)(last + 1 + lane) * kPiece;
+    const uint32_t in = __ballot_sync(0xFFFFFFFFu, at < a.n && __ldcg(&a.items[at].x) == run);
+    const int n = in == 0xFFFFFFFFu ? 32 : __ffs(~in) - 1;
+    last += n;
+    more = n == 32;
+  }
+  float acc[8];
+  RowPart<float, V, 8> p;
+  p.template load<true>(a.partial + ((int64_t)piece * 2 + (whole ? 0 : 1)) * a.hidden + c0, t, TPR, width);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = p.get(e);
+#pragma unroll 4
+  for (int k = piece + 1; k <= last; ++k) {
+    p.template load<true>(a.partial + (int64_t)k * 2 * a.hidden + c0, t, TPR, width);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += p.get(e);
+  }
+  write_row<O, V>(acc, a, out + (int64_t)run * a.out_stride + c0, t, TPR, width);
+}
+
+size_t items_bytes(int rows) { return align_up((size_t)rows * sizeof(uint2), 256); }
+
+template <typename T, typename O, int V, int TPR>
+cudaError_t sum_pieces(const T *grad, const SumArgs &a, O *out, cudaStream_t stream) {
+  const int pieces = (a.n + kPiece - 1) / kPiece, groups = kSumThreads / TPR;
+  const dim3 grid((pieces + groups - 1) / groups, (a.hidden + TPR * 8 - 1) / (TPR * 8));
+  cudaError_t err = launch_chained(embed_sum_kernel<T, O, V, TPR>, grid, dim3(kSumThreads), 0, stream,
+                                   1, true, grad, a, out);
+  if (err != cudaSuccess || pieces < 2) return err;
+  return launch_chained(embed_join_kernel<O, V, TPR>, grid, dim3(kSumThreads), 0, stream, 1, true, a, out);
+}
+
+template <typename T, typename O, int V>
+cudaError_t sum_rows(const T *grad, const SumArgs &a, O *out, cudaStream_t stream) {
+  return a.hidden <= 256    ? sum_pieces<T, O, V, 32>(grad, a, out, stream)
+         : a.hidden <= 512  ? sum_pieces<T, O, V, 64>(grad, a, out, stream)
+         : a.hidden <= 1024 ? sum_pieces<T, O, V, 128>(grad, a, out, stream)
+                            : sum_pieces<T, O, V, 256>(grad, a, out, stream);
+}
+
+template <typename O, int V>
+cudaError_t sort_rows(const SortArgs &s, O *out, int hidden, int64_t out_stride, bool zero,
+                      cudaStream_t stream) {
+  auto kernel = embed_sort_kernel<O, V>;
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)sizeof(SortShared));
+  if (err != cudaSuccess) return err;
+  const int ctas = kSortCtas * (zero ? 1 + 2 * kSms / kSortCtas : 1);
+  return launch_chained(kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortShared), stream, kSortCtas,
+                        false, s, out, hidden, out_stride);
+}
+
+template <typename T, typename O>
+cudaError_t embed_grad(const T *grad, int rows, int hidden, int64_t stride, const int32_t *ids,
+                       float scale, O *out, int vocab, int64_t out_stride, bool accumulate,
+                       void *workspace, cudaStream_t stream) {
+  char *w = static_cast<char *>(workspace);
+  const SortArgs s = {ids, rows, vocab, reinterpret_cast<uint2 *>(w),
+                      reinterpret_cast<uint2 *>(w + items_bytes(rows))};
+  const SumArgs a = {s.a, rows, vocab, hidden, stride, out_stride, scale, accumulate,
+                     reinterpret_cast<float *>(w + 2 * items_bytes(rows))};
+  const void *base[1] = {out};
+  const int64_t strides[1] = {out_stride};
+  const int vo = row_vector(sizeof(O), hidden, 1, base, strides);
+  cudaError_t err = vo * sizeof(O) == 16
+                        ? sort_rows<O, 16 / sizeof(O)>(s, out, hidden, out_stride, !accumulate, stream)
+                        : sort_rows<O, 1>(s, out, hidden, out_stride, !accumulate, stream);
+  if (err != cudaSuccess || rows == 0) return err;
+  // one access for the gradient's rows, the table's and the sums': whole 16 bytes
+  // of the gradient's type, else element by element
+  const void *gbase[1] = {grad};
+  const int64_t gstrides[1] = {stride};
+  const int vg = row_vector(sizeof(T), hidden, 1, gbase, gstrides);
+  if (vg * sizeof(T) == 16 && vo * sizeof(O) == 16)
+    return sum_rows<T, O, 16 / sizeof(T)>(grad, a, out, stream);
+  return sum_rows<T, O, 1>(grad, a, out, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_embed(const void *table, int dtype, int vocab, int hidden, int64_t stride,
+                         const int32_t *ids, int rows, float scale, void *out, int64_t out_stride,
+                         cudaStream_t stream) {
+  const void *base[2] = {table, out};
+  const int64_t strides[2] = {stride, out_stride};
+  const int v = row_vector(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 2, base, strides);
+  auto go = [&](auto kernel, auto *tab, auto *o, int strip) {
+    const int64_t warps = (int64_t)rows * ((hidden + strip - 1) / strip);
+    const int64_t ctas = (warps + kLookupThreads / 32 - 1) / (kLookupThreads / 32);
+    const int64_t most = (int64_t)kSms * 64;
+    kernel<<<(unsigned)(ctas < most ? ctas : most), kLookupThreads, 0, stream>>>(
+        tab, vocab, hidden, stride, ids, rows, scale, o, out_stride);
+    return cudaGetLastError();
+  };
+  if (dtype == SLIMWISE_DTYPE_BF16) {
+    const auto *tab = static_cast<const __nv_bfloat16 *>(table);
+    auto *o = static_cast<__nv_bfloat16 *>(out);
+    if (v == 8) return go(embed_kernel<__nv_bfloat16, 8>, tab, o, 32 * 8 * kLookupLoads);
+    if (v == 2) return go(embed_kernel<__nv_bfloat16, 2>, tab, o, 32 * 2 * kLookupLoads);
+    return go(embed_kernel<__nv_bfloat16, 1>, tab, o, 32 * 2 * kLookupLoads);
+  }
+  const auto *tab = static_cast<const float *>(table);
+  auto *o = static_cast<float *>(out);
+  if (v == 4) return go(embed_kernel<float, 4>, tab, o, 32 * 4 * kLookupLoads);
+  return go(embed_kernel<float, 1>, tab, o, 32 * kLookupLoads);
+}
+
+size_t embed_grad_workspace(int rows, int hidden) {
+  const size_t pieces = ((size_t)rows + kPiece - 1) / kPiece;
+  return 2 * items_bytes(rows) + pieces * 2 * hidden * sizeof(float) + 256;
+}
+
+cudaError_t launch_embed_grad(const void *grad, int dtype, int rows, int hidden, int64_t stride,
+                              const int32_t *ids, float scale, void *out, int out_dtype, int vocab,
+                              int64_t out_stride, bool accumulate, void *workspace,
+                              cudaStream_t stream) {
+  auto go = [&](auto *g, auto *o) {
+    return embed_grad(g, rows, hidden, stride, ids, scale, o, vocab, out_stride, accumulate, workspace,
+                      stream);
+  };
+  const auto *gb = static_cast<const __nv_bfloat16 *>(grad);
+  const auto *gf = static_cast<const float *>(grad);
+  auto *ob = static_cast<__nv_bfloat16 *>(out);
+  auto *of = static_cast<float *>(out);
+  if (dtype == SLIMWISE_DTYPE_BF16) return out_dtype == SLIMWISE_DTYPE_BF16 ? go(gb, ob) : go(gb, of);
+  return out_dtype == SLIMWISE_DTYPE_BF16 ? go(gf, ob) : go(gf, of);
+}
+
+}  // namespace slimwise

@@ -1,0 +1,973 @@
+// linear_loss.cu -- cross entropy of a head's logits from the hidden rows and the
+// head's weight, with the gradients of both; the logits are not kept.
+//
+//   z = h W^T,  L_t = log sum_v exp z_tv - z_ty,  loss = sum_t w_t L_t
+//   dz_tv = w_t (softmax(z_t)_v - [v = y]),  dh = dz W,  dW = dz^T h
+//
+// Three matrix products of 2 T V H operations each, on the tensor cores.  A pass
+// over the logits for their sums and a second one for dz would make it four; this
+// needs one, because dz is a row factor times numbers that are known before the
+// sum: with the label's logit z_y as the row's reference (T dot products, first),
+//   e_tv = exp(z_tv - z_ty),  S_t = sum over v != y of e_tv,  L_t = log(1 + S_t)
+//   dz_tv = w_t / (1 + S_t) * (v = y ? -S_t : e_tv)
+// The first product's epilogue leaves e in bf16 and the sums of its columns; the
+// sums' kernel puts -S at the label and scales a copy of h by w / (1 + S).  Then
+//   dh = w / (1 + S) * (e W)   (the factor after the product)
+//   dW = e^T (w / (1 + S) h)
+// The label stays out of S, so that a nearly sure row's loss and gradient keep
+// their digits.  Two values are rounded to bf16 on the way, as the tensor cores
+// take them: e and, for dW, the scaled rows.
+//
+// z_y lies below log sum exp z, so e can grow: up to e^L.  Rows with L above
+// kMostLoss (a label of probability 1e-26) take the row's largest logit as the
+// reference instead, in a second run of the first product over their tiles.
+//
+// Rows without a label take part in nothing: the others are moved together first.
+// The matrix e, [rows, vocab] bf16, has at most kMostCells elements: more rows are
+// taken in chunks, and dW is then summed in fp32.
+//
+// The products (one kernel): a pair of CTAs per 256 x 256 tile, persistent; one warp
+// issues TMA copies of 64-deep slices into a ring of kStages, one the pair's MMAs
+// (M = N = 256, cta_group::2), eight read the accumulators, which are double
+// buffered in tensor memory.  Operands lie as they are, along the contraction (K-major)
+// or across it (MN-major): no transposed copies.
+#include <cudaTypedefs.h>
+
+#include <atomic>
+#include <cfloat>
+
+#include "train.cuh"
+
+namespace slimwise {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kMostLoss = 60.0f;
+constexpr int64_t kMostCells = 1ll << 30;
+constexpr int kTile = 256;       // rows and columns of a pair's tile
+constexpr int kHalf = 128;       // of a CTA's share of an operand
+constexpr int kDepth = 64;       // slice of the contraction: 128 bytes
+constexpr int kStages = 7;
+constexpr int kOperandBytes = kHalf * kDepth * 2;
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kEpiWarps = 8, kGemmThreads = 64 + 32 * kEpiWarps;
+constexpr int kMostPairs = kSms / 2;
+// Tiles of partial sums of dh: splits of the vocabulary are made while they fit.
+constexpr int kMostSplits = 96, kSplitTiles = 8 * kMostPairs;
+constexpr float kFloor = -FLT_MAX;  // stands in for -inf as a maximum
+
+enum Mode { kForward, kNumerators, kGradHidden, kGradWeight };
+enum Word { kLive = 0, kArrived = 1, kErr = kCtrlErr };
+
+struct Layout {
+  int rows_pad, chunk, chunks, vocab_tiles, hidden_tiles, split_tiles;
+  int64_t cells_stride;
+  size_t ctrl, orig, label, target, ref, scale, flags, rows, scaled, sums, cells, splits, acc, total;
+};
+
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_weight) {
+  Layout l;
+  const bool grad = grad_hidden || grad_weight;
+  l.rows_pad = ceil_div(rows, kTile) * kTile;
+  l.vocab_tiles = ceil_div(vocab, kTile);
+  l.hidden_tiles = ceil_div(hidden, kTile);
+  l.cells_stride = align_up((size_t)vocab, 64);
+  // (the forward pass keeps 16 bytes for each row and 256 columns)
+  int64_t most = grad ? kMostCells / l.cells_stride : ((int64_t)1 << 23) / l.vocab_tiles;
+  most = most / kTile * kTile;
+  if (most < kTile) most = kTile;
+  l.chunk = most < l.rows_pad ? (int)most : l.rows_pad;
+  l.chunks = ceil_div(l.rows_pad, l.chunk);
+  l.split_tiles = 0;
+  if (grad_hidden)
+    for (int m = 1; m <= l.chunk / kTile; ++m) {
+      const int tiles = m * l.hidden_tiles, kb = ceil_div(vocab, kDepth);
+      int s = kSplitTiles / tiles;
+      s = s < 1 ? 1 : s > kMostSplits ? kMostSplits : s;
+      s = s < kb ? s : kb;
+      if (s * tiles > l.split_tiles) l.split_tiles = s * tiles;
+    }
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    const size_t r = o;
+    o = align_up(o + bytes, 1024);
+    return r;
+  };
+  const size_t n = (size_t)l.rows_pad;
+  l.ctrl = take(kCtrlWords * 4);
+  l.orig = take(n * 4);
+  l.label = take(n * 4);
+  l.target = take(n * 4);
+  l.ref = take(n * 4);
+  l.scale = take(n * 4);
+  l.flags = take(n / kTile * 3 * 4);
+  l.rows = take(n * hidden * 2);
+  l.scaled = take(grad_weight ? (size_t)l.chunk * hidden * 2 : 0);
+  l.sums = take((size_t)l.vocab_tiles * 2 * l.chunk * sizeof(float2));
+  l.cells = take(grad ? (size_t)l.chunk * l.cells_stride * 2 : 0);
+  l.splits = take((size_t)l.split_tiles * kTile * kTile * 4);
+  l.acc = take(grad_weight && l.chunks > 1 ? (size_t)vocab * hidden * 4 : 0);
+  l.total = o;
+  return l;
+}
+
+// Device view of the workspace and the call.
+struct Call {
+  int T, H, V;
+  int rows_pad, chunk, vocab_tiles, hidden_tiles;
+  int64_t cells_stride;
+  int32_t *ctrl, *orig, *label;
+  int32_t *flags;  // [3][rows_pad / 256]: tiles to run again; their list; each chunk's number of them
+  float *target, *ref, *scale;
+  __nv_bfloat16 *rows, *scaled, *cells;
+  float2 *sums;   // [2 vocab_tiles][chunk]: sum of numerators, largest logit
+  float *splits;  // [tiles][256][256]
+  float *acc;     // [V][H], more than one chunk
+  const __nv_bfloat16 *hidden, *weight;
+  int64_t hidden_stride, weight_stride;
+  const int32_t *labels;
+  const float *row_weight;
+  float *row_loss, *loss;
+  __nv_bfloat16 *dh;
+  int64_t dh_stride;
+  void *dw;
+  int dw_fp32;
+  int64_t dw_stride;
+};
+
+__device__ __forceinline__ int chunk_rows(const Call &c, int chunk) {
+  const int left = __ldcg(c.ctrl + kLive) - chunk * c.chunk;
+  return left < 0 ? 0 : left < c.chunk ? left : c.chunk;
+}
+
+// Splits of dh's contraction: the fewest steps of 64 for the busiest pair, with a
+// tile's accumulators and its share of the joining pass counted as steps.  By one
+// warp, known to all its lanes.
+__device__ __forceinline__ int choose_splits(int tiles, int kb, int pairs) {
+  const int lane = threadIdx.x & 31;
+  int most = kSplitTiles / tiles;
+  most = max(1, min(min(most, kMostSplits), kb));
+  uint32_t best = ~0u;
+  for (int s = 1 + lane; s <= most; s += 32) {
+    const uint32_t steps = (uint32_t)((tiles * s + pairs - 1) / pairs) * ((kb + s - 1) / s + 3) +
+                           (uint32_t)(tiles * s) / 3;
+    best = min(best, steps << 7 | (uint32_t)s);
+  }
+  return (int)(__reduce_min_sync(0xFFFFFFFFu, best) & 127u);
+}
+
+// ---------------------------------------------------------------------------
+// rows with a label, moved together
+// ---------------------------------------------------------------------------
+__global__ void __launch_bounds__(1024) compact_kernel(Call c) {
+  __shared__ int part[32];
+  __shared__ int base;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_launch_dependents();
+  if (threadIdx.x < kCtrlWords) c.ctrl[threadIdx.x] = 0;
+  for (int i = threadIdx.x; i < c.rows_pad / kTile * 3; i += 1024) c.flags[i] = 0;
+  if (threadIdx.x == 0) base = 0;
+  __syncthreads();
+  for (int t0 = 0; t0 < c.rows_pad; t0 += 1024) {
+    const int t = t0 + threadIdx.x;
+    const int y = t < c.T ? __ldg(c.labels + t) : -1;
+    const uint32_t live = __ballot_sync(0xFFFFFFFFu, y >= 0);
+    if (lane == 0) part[warp] = __popc(live);
+    __syncthreads();
+    int at = base;
+    for (int w = 0; w < warp; ++w) at += part[w];
+    at += __popc(live & ((1u << lane) - 1));
+    if (y >= 0) {
+      c.orig[at] = t;
+      c.label[at] = y;
+    }
+    __syncthreads();
+    if (threadIdx.x == 1023) base = at + (y >= 0 ? 1 : 0);
+    __syncthreads();
+  }
+  const int n = base;
+  if (threadIdx.x == 0) c.ctrl[kLive] = n;
+  for (int i = n + threadIdx.x; i < c.rows_pad; i += 1024) c.label[i] = c.orig[i] = -1;
+}
+
+// A warp a row: row i of the labelled ones is copied and its label's logit
+// computed (fp32 sums of a lane's products, then over the lanes); row i of the
+// call gets the results of a row without a label where it has none.
+__global__ void __launch_bounds__(256) gather_kernel(Call c) {
+  const int lane = threadIdx.x & 31, i = blockIdx.x * 8 + (threadIdx.x >> 5);
+  pdl_wait_primary();
+  pdl_launch_dependents();
+  if (i >= c.rows_pad) return;
+  const int words = c.H / 8;
+  const int t = __ldcg(c.orig + i), y = __ldcg(c.label + i);
+  uint4 *to = reinterpret_cast<uint4 *>(c.rows + (int64_t)i * c.H);
+  if (t >= 0) {
+    const uint4 *from = reinterpret_cast<const uint4 *>(c.hidden + (int64_t)t * c.hidden_stride);
+    const bool known = y < c.V;
+    const uint4 *head = reinterpret_cast<const uint4 *>(c.weight + (int64_t)(known ? y : 0) * c.weight_stride);
+    float s = 0.0f;
+#pragma unroll 4
+    for (int k = lane; k < words; k += 32) {
+      const uint4 a = __ldg(from + k), b = __ldg(head + k);
+      to[k] = a;
+      const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        s = fmaf(__uint_as_float(av[q] << 16), __uint_as_float(bv[q] << 16), s);
+        s = fmaf(__uint_as_float(av[q] & 0xFFFF0000u), __uint_as_float(bv[q] & 0xFFFF0000u), s);
+      }
+    }
+    s = warp_sum(s);
+    if (!known) s = __int_as_float(0x7FC00000);  // a label outside the vocabulary: NaN
+    if (lane == 0) c.target[i] = c.ref[i] = s;
+  } else {
+    for (int k = lane; k < words; k += 32) to[k] = make_uint4(0, 0, 0, 0);
+  }
+  if (i < c.T && __ldg(c.labels + i) < 0) {
+    if (lane == 0) c.row_loss[i] = 0.0f;
+    if (c.dh) {
+      uint4 *row = reinterpret_cast<uint4 *>(c.dh + (int64_t)i * c.dh_stride);
+      for (int k = lane; k < words; k += 32) row[k] = make_uint4(0, 0, 0, 0);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// the products
+// ---------------------------------------------------------------------------
+struct Operands {
+  CUtensorMap a, b;
+};
+
+// Shared-memory descriptor of an MN-major operand with 128-byte swizzle: groups
+// of 64 elements across the contraction (128 bytes), `group` bytes apart, each of
+// 8-deep blocks of 1024 bytes along it.
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t saddr, uint32_t group) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(group >> 4) << 16;  // leading: to the next 64 elements
+  d |= (uint64_t)(1024 >> 4) << 32;   // stride: to the next 8 of the contraction
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// 32 accumulator columns of the thread's lane.
+__device__ __forceinline__ void tmem_ld_row(uint32_t taddr, float (&v)[32]) {
+  uint32_t *r = reinterpret_cast<uint32_t *>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+        "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
+        "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
+        "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+struct Unit {
+  int m, n, k0, k1;
+};
+
+template <Mode kMode>
+struct Work {
+  int mt, nt, kb, splits, units;
+  const int *list;  // kNumerators again: the tiles of rows to take
+  __device__ __forceinline__ Unit at(int u) const {
+    Unit r;
+    if constexpr (kMode == kForward || kMode == kNumerators) {
+      // the row tiles of a column tile next to each other: the head is read once
+      r.n = u / mt;
+      r.m = u - r.n * mt;
+      if (kMode == kNumerators && list) r.m = __ldcg(list + r.m);
+      r.k0 = 0;
+      r.k1 = kb;
+    } else if constexpr (kMode == kGradHidden) {
+      const int tiles = mt * nt, s = u / tiles, t = u - s * tiles;
+      r.m = t / nt;
+      r.n = t - r.m * nt;
+      r.k0 = (int)((int64_t)kb * s / splits);
+      r.k1 = (int)((int64_t)kb * (s + 1) / splits);
+    } else {
+      r.m = u / nt;
+      r.n = u - r.m * nt;
+      r.k0 = 0;
+      r.k1 = kb;
+    }
+    return r;
+  }
+};
+
+constexpr size_t kGemmSmem = (size_t)kStages * kStageBytes + 8 * (2 * kStages + 5) + 64 + 1024;
+
+// Sums of the columns' numerators and the P tile of 32 columns.
+template <Mode kMode>
+__device__ __forceinline__ void numerators(const float (&z)[32], float ref, int label, int valid,
+                                           float &sum, float &most, uint32_t (&packed)[16]) {
+  // label: the label's column here, or outside 0..31; valid: columns of the vocabulary
+  const bool plain = __all_sync(0xFFFFFFFFu, (unsigned)label >= 32u) && valid >= 32;
+  if constexpr (kMode == kForward) {
+    float m = most;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      if (plain || (j < valid && j != label)) m = fmaxf(m, z[j]);
+    }
+    sum *= ex2((most - m) * kLog2e);
+    most = m;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float e = ex2((z[j] - m) * kLog2e);
+      if (plain || (j < valid && j != label)) s[j & 3] += e;
+    }
+    sum += (s[0] + s[1]) + (s[2] + s[3]);
+  } else {
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) {
+      float e[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        e[q] = ex2((z[j + q] - ref) * kLog2e);
+        if (plain || (j + q < valid && j + q != label)) {
+          s[(j + q) & 3] += e[q];
+          most = fmaxf(most, z[j + q]);
+        }
+      }
+      packed[j / 2] = pack_bf16(e[0], e[1]);
+    }
+    sum += (s[0] + s[1]) + (s[2] + s[3]);
+  }
+}
+
+template <Mode kMode>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    product_kernel(const __grid_constant__ Operands maps, Call c, int chunk, int again,
+                   uint64_t timeout_ns) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char *smem = reinterpret_cast<unsigned char *>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t smem_base = smem_u32(smem);
+  const uint32_t bar0 = smem_base + kStages * kStageBytes;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
+  auto accf_bar = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
+  auto acce_bar = [&](int b) { return bar0 + 8u * (2 * kStages + 2 + b); };
+  const uint32_t drain_bar = bar0 + 8u * (2 * kStages + 4);
+  int *misc = reinterpret_cast<int *>(smem + kStages * kStageBytes + 8 * (2 * kStages + 5));
+  volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(misc);
+  volatile int *abort = misc + 1;
+  volatile int *consumed = misc + 2;
+  volatile int *n_splits = misc + 3;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t crank = cluster_ctarank();
+  const bool lead = crank == 0;
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+  pdl_wait_primary();
+  const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
+  Work<kMode> work;
+  work.list = nullptr;
+  work.splits = 1;
+  if constexpr (kMode == kForward || kMode == kNumerators) {
+    work.mt = (rows + kTile - 1) / kTile;
+    work.nt = c.vocab_tiles;
+    work.kb = (c.H + kDepth - 1) / kDepth;
+    if (kMode == kNumerators && again) {
+      // the tiles that the sums' kernel marked
+      const int tiles = c.rows_pad / kTile;
+      work.mt = __ldcg(c.flags + 2 * tiles + chunk);
+      work.list = c.flags + tiles + row0 / kTile;
+    }
+    work.units = work.mt * work.nt;
+  } else if constexpr (kMode == kGradHidden) {
+    work.mt = (rows + kTile - 1) / kTile;
+    work.nt = c.hidden_tiles;
+    work.kb = (c.V + kDepth - 1) / kDepth;
+    if (warp == 0 && rows > 0) {
+      const int s = choose_splits(work.mt * work.nt, work.kb, pairs);
+      if (lane == 0) *n_splits = s;
+    }
+    __syncthreads();
+    work.splits = rows > 0 ? *n_splits : 0;
+    work.units = work.mt * work.nt * work.splits;
+  } else {
+    work.mt = c.vocab_tiles;
+    work.nt = c.hidden_tiles;
+    work.kb = (rows + kDepth - 1) / kDepth;
+    work.units = rows > 0 ? work.mt * work.nt : 0;
+    if (rows == 0 && chunk == 0) {
+      // no labelled row at all: zeros (16 bytes are 8 elements, or 4)
+      const int words = c.H / (c.dw_fp32 ? 4 : 8);
+      const int64_t all = (int64_t)c.V * words;
+      for (int64_t i = (int64_t)blockIdx.x * kGemmThreads + threadIdx.x; i < all;
+           i += (int64_t)gridDim.x * kGemmThreads) {
+        const int64_t v = i / words, k = i - v * words;
+        char *row = static_cast<char *>(c.dw) + v * c.dw_stride * (c.dw_fp32 ? 4 : 2);
+        reinterpret_cast<uint4 *>(row)[k] = make_uint4(0, 0, 0, 0);
+      }
+    }
+  }
+  if (pair >= work.units) return;  // (both CTAs of a pair)
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(accf_bar(b), 1);
+      mbar_init(acce_bar(b), 2 * kEpiWarps);
+    }
+    mbar_init(drain_bar, 1);
+    *abort = 0;
+    *consumed = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&maps.a);
+    tma_prefetch_desc(&maps.b);
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32((const void *)tmem_slot), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  auto give_up = [&](int code) {
+    if (!*abort) {
+      *abort = 1;
+      atomicOr(c.ctrl + kErr, code);
+    }
+  };
+  if (threadIdx.x == 0 && !lead &&
+      ld_shared_cluster(mapa_shared(smem_u32((const void *)tmem_slot), 0u)) != tmem_base)
+    give_up(SLIMWISE_DEVERR_TMEM_PAIR);
+  // a bounded wait of the warp: whether it completed on every lane
+  auto all_ok = [&](bool ok) {
+    if (!ok) give_up(SLIMWISE_DEVERR_PIPELINE_TIMEOUT);
+    return __all_sync(0xFFFFFFFFu, ok) != 0;
+  };
+  // operands along the contraction (K-major) or across it
+  constexpr bool kAcrossA = kMode == kGradWeight;
+  constexpr bool kAcrossB = kMode == kGradHidden || kMode == kGradWeight;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ copies
+    int stage = 0, issued = 0;
+    uint32_t phase = 0;
+    const uint64_t policy = l2_policy_evict_last();
+    bool ok = true;
+    for (int u = pair; u < work.units && ok; u += pairs) {
+      const Unit w = work.at(u);
+      // first row (column) of this CTA's share of either operand
+      const int a0 = (kMode == kForward || kMode == kNumerators ? row0 : 0) + w.m * kTile + (int)crank * kHalf;
+      const int b0 = w.n * kTile + (int)crank * kHalf;
+      for (int k = w.k0; k < w.k1; ++k) {
+        if (!all_ok(mbar_wait_bounded(empty_bar(stage), phase ^ 1u, abort, timeout_ns))) {
+          ok = false;
+          break;
+        }
+        const uint32_t a = smem_base + (uint32_t)(stage * kStageBytes), b = a + kOperandBytes;
+        if (elect_one()) {
+          const uint32_t bar = mapa_shared(full_bar(stage), 0u);
+          if (lead) mbar_arrive_expect_tx(full_bar(stage), 2 * kStageBytes);
+          if constexpr (kAcrossA) {
+            tma_load_2d_pair(a, &maps.a, bar, a0, k * kDepth, policy);
+            tma_load_2d_pair(a + kOperandBytes / 2, &maps.a, bar, a0 + 64, k * kDepth, policy);
+          } else {
+            tma_load_2d_pair(a, &maps.a, bar, k * kDepth, a0, policy);
+          }
+          if constexpr (kAcrossB) {
+            tma_load_2d_pair(b, &maps.b, bar, b0, k * kDepth, policy);
+            tma_load_2d_pair(b + kOperandBytes / 2, &maps.b, bar, b0 + 64, k * kDepth, policy);
+          } else {
+            tma_load_2d_pair(b, &maps.b, bar, k * kDepth, b0, policy);
+          }
+        }
+        __syncwarp();
+        ++issued;
+        if (++stage == kStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    pdl_launch_dependents();
+    if (lane == 0) {
+      // until every stage still in the ring has been released (or, in the first
+      // CTA after an abort, its copies have landed): nothing is left on its way
+      // to this CTA's shared memory when it exits
+      const int from = issued > kStages ? issued - kStages : 0;
+      if (*abort && lead) {
+        for (int s = *consumed > from ? *consumed : from; s < issued; ++s)
+          mbar_wait_timeout(full_bar(s % kStages), (uint32_t)((s / kStages) & 1), 10000000ull);
+      } else {
+        for (int s = from; s < issued; ++s)
+          mbar_wait_timeout(empty_bar(s % kStages), (uint32_t)((s / kStages) & 1), 10000000ull);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMAs
+    if (lead) {
+      int stage = 0, local = 0, n_consumed = 0;
+      uint32_t phase = 0;
+      const uint32_t idesc = idesc_bf16_f32(kTile, kTile) | (kAcrossA ? 1u << 15 : 0u) |
+                             (kAcrossB ? 1u << 16 : 0u);
+      bool ok = true;
+      for (int u = pair; u < work.units && ok; u += pairs, ++local) {
+        const Unit w = work.at(u);
+        const int b = local & 1;
+        if (!all_ok(mbar_wait_cluster_bounded(acce_bar(b), ((uint32_t)(local >> 1) & 1u) ^ 1u, abort,
+                                              timeout_ns)))
+          break;
+        tc_fence_after();
+        const uint32_t d = tmem_base + (uint32_t)(b * kTile);
+        for (int k = w.k0; k < w.k1; ++k) {
+          if (!all_ok(mbar_wait_bounded(full_bar(stage), phase, abort, timeout_ns))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t as = smem_base + (uint32_t)(stage * kStageBytes), bs = as + kOperandBytes;
+          ++n_consumed;
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < kDepth / 16; ++kk)
+              tc_mma_bf16_pair(d,
+                               kAcrossA ? smem_desc_mn(as + kk * 2048, kOperandBytes / 2)
+                                        : smem_desc_sw128(as + kk * 32),
+                               kAcrossB ? smem_desc_mn(bs + kk * 2048, kOperandBytes / 2)
+                                        : smem_desc_sw128(bs + kk * 32),
+                               idesc, (k != w.k0 || kk != 0) ? 1u : 0u);
+            tc_commit_pair(empty_bar(stage), (uint16_t)3);
+            *consumed = n_consumed;
+          }
+          __syncwarp();
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        if (!ok) break;
+        if (elect_one()) tc_commit_pair(accf_bar(b), (uint16_t)3);
+        __syncwarp();
+      }
+      if (__any_sync(0xFFFFFFFFu, *abort != 0) && n_consumed > 0) {
+        if (elect_one()) tc_commit_pair(drain_bar, (uint16_t)1);
+        mbar_wait_timeout(drain_bar, 0, 10000000ull);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ accumulators
+    const int q = warp & 3, half = (warp - 2) >> 2;  // lanes 32 q.., columns 128 half..
+    const int in_tile = (int)crank * kHalf + 32 * q + lane;
+    int local = 0;
+    for (int u = pair; u < work.units; u += pairs, ++local) {
+      const Unit w = work.at(u);
+      const int b = local & 1;
+      if (!all_ok(mbar_wait_bounded(accf_bar(b), (uint32_t)(local >> 1) & 1u, abort, timeout_ns))) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(b * kTile + half * kHalf);
+      const int row = w.m * kTile + in_tile, col0 = w.n * kTile + half * kHalf;
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(mapa_shared(acce_bar(b), 0u));
+      };
+      if constexpr (kMode == kForward || kMode == kNumerators) {
+        const bool live = row < rows;
+        const float ref = live ? __ldcg(c.ref + row0 + row) : 0.0f;
+        const int label = live ? __ldcg(c.label + row0 + row) : -1;
+        float sum = 0.0f, most = kFloor;
+#pragma unroll 1
+        for (int k = 0; k < kHalf / 32; ++k) {
+          float z[32];
+          uint32_t packed[16];
+          tmem_ld_row(taddr + k * 32, z);
+          tmem_ld_wait();
+          if (k == kHalf / 32 - 1) release();
+          const int col = col0 + 32 * k;
+          numerators<kMode>(z, ref, label - col, c.V - col, sum, most, packed);
+          if constexpr (kMode == kNumerators) {
+            // rows past the last one: zeros (they are in the contraction of dW)
+            uint4 *to = reinterpret_cast<uint4 *>(c.cells + (int64_t)row * c.cells_stride + col);
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+              if (col + 8 * p < c.cells_stride)
+                to[p] = live ? make_uint4(packed[4 * p], packed[4 * p + 1], packed[4 * p + 2], packed[4 * p + 3])
+                             : make_uint4(0, 0, 0, 0);
+          }
+        }
+        c.sums[(int64_t)(w.n * 2 + half) * c.chunk + row] = make_float2(sum, most);
+      } else if constexpr (kMode == kGradHidden) {
+        float *to = c.splits + ((int64_t)u * kTile + in_tile) * kTile + half * kHalf;
+#pragma unroll 1
+        for (int k = 0; k < kHalf / 32; ++k) {
+          float z[32];
+          tmem_ld_row(taddr + k * 32, z);
+          tmem_ld_wait();
+          if (k == kHalf / 32 - 1) release();
+          if (row < rows && col0 + 32 * k < c.H)
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              *reinterpret_cast<float4 *>(to + 32 * k + j) = make_float4(z[j], z[j + 1], z[j + 2], z[j + 3]);
+        }
+      } else {
+        // chunks before the last leave fp32 sums; the last one adds them and rounds
+        const bool last = __ldcg(c.ctrl + kLive) <= row0 + c.chunk;
+        float *acc = c.acc + (int64_t)row * c.H;
+#pragma unroll 1
+        for (int k = 0; k < kHalf / 32; ++k) {
+          float z[32];
+          tmem_ld_row(taddr + k * 32, z);
+          tmem_ld_wait();
+          if (k == kHalf / 32 - 1) release();
+          if (row >= c.V) continue;
+#pragma unroll
+          for (int j = 0; j < 32; j += 8) {
+            const int col = col0 + 32 * k + j;
+            if (col >= c.H) continue;
+            if (chunk > 0) {
+              const float4 x = *reinterpret_cast<const float4 *>(acc + col);
+              const float4 y = *reinterpret_cast<const float4 *>(acc + col + 4);
+              z[j] += x.x; z[j + 1] += x.y; z[j + 2] += x.z; z[j + 3] += x.w;
+              z[j + 4] += y.x; z[j + 5] += y.y; z[j + 6] += y.z; z[j + 7] += y.w;
+            }
+            if (last && !c.dw_fp32) {
+              *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(c.dw) + (int64_t)row * c.dw_stride + col) =
+                  make_uint4(pack_bf16(z[j], z[j + 1]), pack_bf16(z[j + 2], z[j + 3]),
+                             pack_bf16(z[j + 4], z[j + 5]), pack_bf16(z[j + 6], z[j + 7]));
+            } else {
+              float *to = last ? static_cast<float *>(c.dw) + (int64_t)row * c.dw_stride + col : acc + col;
+              *reinterpret_cast<float4 *>(to) = make_float4(z[j], z[j + 1], z[j + 2], z[j + 3]);
+              *reinterpret_cast<float4 *>(to + 4) = make_float4(z[j + 4], z[j + 5], z[j + 6], z[j + 7]);
+            }
+          }
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// a row's sums
+// ---------------------------------------------------------------------------
+// 32 rows a CTA, a lane each; the column tiles' sums in 32 parts.  kForward: the
+// loss.  kNumerators: besides, the row's factor, the label's numerator and the
+// scaled row; `again`: only rows of the tiles that were run again (else a row whose
+// reference does not do marks its tile).  finish: the CTA that ends last adds up the
+// loss, in fp64 and in the order of the rows.
+template <Mode kMode>
+__global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again, int finish) {
+  __shared__ float part_sum[32][33], part_most[32][33];
+  __shared__ float row_scale[32];
+  __shared__ double total[32];
+  __shared__ int last;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_wait_primary();
+  pdl_launch_dependents();
+  const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
+  const int first = blockIdx.x * 32, row = first + lane;
+  const int tile = row0 / kTile + first / kTile;
+  const bool mine = first < (rows + kTile - 1) / kTile * kTile && (!again || __ldcg(c.flags + tile) != 0);
+  if (mine) {
+    float s = 0.0f, m = kFloor;
+    for (int i = warp; i < 2 * c.vocab_tiles; i += 32) {
+      const float2 v = __ldcg(c.sums + (int64_t)i * c.chunk + row);
+      if constexpr (kMode == kForward) {
+        const float to = fmaxf(m, v.y);
+        s = s * ex2((m - to) * kLog2e) + v.x * ex2((v.y - to) * kLog2e);
+        m = to;
+      } else {
+        s += v.x;
+        m = fmaxf(m, v.y);
+      }
+    }
+    part_sum[warp][lane] = s;
+    part_most[warp][lane] = m;
+    __syncthreads();
+    if (warp == 0) {
+      const int at = row0 + row;
+      const bool live = row < rows;
+      const float z = live ? __ldcg(c.target + at) : 0.0f;
+      float ref = live ? __ldcg(c.ref + at) : 0.0f, S = 0.0f, top = kFloor;
+      for (int k = 0; k < 32; ++k) top = fmaxf(top, part_most[k][lane]);
+      if constexpr (kMode == kForward) {
+        ref = fmaxf(top, z);
+        if (z != z) ref = z;
+        for (int k = 0; k < 32; ++k) S += part_sum[k][lane] * ex2((part_most[k][lane] - ref) * kLog2e);
+      } else {
+        for (int k = 0; k < 32; ++k) S += part_sum[k][lane];
+      }
+      float scale = 0.0f;
+      if (live) {
+        const int t = __ldcg(c.orig + at);
+        if (kMode == kNumerators && !again && S > expf(kMostLoss) && top < INFINITY) {
+          c.ref[at] = top;
+          const int tiles = c.rows_pad / kTile;
+          if (atomicExch(c.flags + tile, 1) == 0)
+            c.flags[tiles + row0 / kTile + atomicAdd(c.flags + 2 * tiles + chunk, 1)] = tile - row0 / kTile;
+        }
+        const float own = ref == z ? 1.0f : ex2((z - ref) * kLog2e);
+        const float loss = ref == z ? log1pf(S) : (ref - z) + logf(own + S);
+        c.row_loss[t] = loss;
+        if constexpr (kMode == kNumerators) {
+          scale = (c.row_weight ? __ldg(c.row_weight + t) : 1.0f) / (own + S);
+          c.scale[at] = scale;
+          const int y = __ldcg(c.label + at);
+          if (y < c.V) c.cells[(int64_t)row * c.cells_stride + y] = __float2bfloat16_rn(-S);
+        }
+      }
+      row_scale[lane] = scale;
+    }
+    if constexpr (kMode == kNumerators) {
+      __syncthreads();
+      if (c.scaled) {
+        const int r = first + warp;
+        const float scale = row_scale[warp];
+        const uint4 *from = reinterpret_cast<const uint4 *>(c.rows + (int64_t)(row0 + r) * c.H);
+        uint4 *to = reinterpret_cast<uint4 *>(c.scaled + (int64_t)r * c.H);
+        const bool live = r < rows;
+        for (int k = lane; k < c.H / 8; k += 32) {
+          uint4 v = live ? __ldcg(from + k) : make_uint4(0, 0, 0, 0);
+          uint32_t *x = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            x[q] = pack_bf16(__uint_as_float(x[q] << 16) * scale, __uint_as_float(x[q] & 0xFFFF0000u) * scale);
+          to[k] = v;
+        }
+      }
+    }
+  }
+  if (!finish || !c.loss) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(c.ctrl + kArrived, 1) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  double s = 0.0;
+  for (int t = threadIdx.x; t < c.T; t += 1024) {
+    const double l = (double)__ldcg(c.row_loss + t) * (c.row_weight ? (double)__ldg(c.row_weight + t) : 1.0);
+    s += __ldg(c.labels + t) >= 0 ? l : 0.0;
+  }
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  if (lane == 0) total[warp] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 32; ++w) s += total[w];
+    *c.loss = (float)s;
+  }
+}
+
+// dh: the splits' sums of a row in order, times its factor.
+__global__ void __launch_bounds__(256) join_kernel(Call c, int chunk, int pairs) {
+  __shared__ int n_splits;
+  pdl_wait_primary();
+  pdl_launch_dependents();
+  const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
+  const int mt = (rows + kTile - 1) / kTile, tiles = mt * c.hidden_tiles;
+  if (rows == 0) return;
+  if (threadIdx.x < 32) {
+    const int s = choose_splits(tiles, (c.V + kDepth - 1) / kDepth, pairs);
+    if (threadIdx.x == 0) n_splits = s;
+  }
+  __syncthreads();
+  const int splits = n_splits, words = c.H / 8;
+  const int64_t all = (int64_t)rows * words;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int row = (int)(i / words), col = (int)(i - (int64_t)row * words) * 8;
+    const int tile = row / kTile * c.hidden_tiles + col / kTile;
+    const float *from = c.splits + ((int64_t)tile * kTile + row % kTile) * kTile + col % kTile;
+    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      const float4 x = __ldcg(reinterpret_cast<const float4 *>(from));
+      const float4 y = __ldcg(reinterpret_cast<const float4 *>(from) + 1);
+      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+      v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+      from += (int64_t)tiles * kTile * kTile;
+    }
+    const float f = __ldcg(c.scale + row0 + row);
+    __nv_bfloat16 *to = c.dh + (int64_t)__ldcg(c.orig + row0 + row) * c.dh_stride + col;
+    *reinterpret_cast<uint4 *>(to) = make_uint4(pack_bf16(v[0] * f, v[1] * f), pack_bf16(v[2] * f, v[3] * f),
+                                                pack_bf16(v[4] * f, v[5] * f), pack_bf16(v[6] * f, v[7] * f));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+  static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> fn{nullptr};
+  PFN_cuTensorMapEncodeTiled_v12000 f = fn.load(std::memory_order_acquire);
+  if (!f) {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) !=
+            cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return nullptr;
+    f = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    fn.store(f, std::memory_order_release);
+  }
+  return f;
+}
+
+// A bf16 matrix of `rows` rows of `cols`, `stride` elements apart, in boxes of 64
+// columns and `box` rows; 128-byte swizzle, zeros outside.
+bool encode(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t stride, int box) {
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
+  cuuint32_t boxes[2] = {(cuuint32_t)kDepth, (cuuint32_t)box};
+  cuuint32_t steps[2] = {1, 1};
+  const auto f = encoder();
+  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, boxes,
+                steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Pairs that run at once (their CTAs' SMs lie in one cluster's reach); readies the
+// kernel on the current device.
+template <Mode kMode>
+cudaError_t resident_pairs(int *pairs) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  if (dev < 64 && (*pairs = known[dev].load(std::memory_order_acquire)) > 0) return cudaSuccess;
+  auto kernel = product_kernel<kMode>;
+  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmSmem);
+  if (err != cudaSuccess) return err;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2);
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = kGemmSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  err = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+  if (err != cudaSuccess) return err;
+  if (n < 1) return cudaErrorInvalidConfiguration;
+  *pairs = n < kMostPairs ? n : kMostPairs;
+  if (dev < 64) known[dev].store(*pairs, std::memory_order_release);
+  return cudaSuccess;
+}
+
+template <Mode kMode>
+cudaError_t run_product(const Operands &maps, const Call &c, int chunk, int again, cudaStream_t stream,
+                        int *used = nullptr) {
+  int pairs = 0;
+  const cudaError_t err = resident_pairs<kMode>(&pairs);
+  if (err != cudaSuccess) return err;
+  if (used) *used = pairs;
+  return launch_chained(product_kernel<kMode>, dim3(2 * pairs), dim3(kGemmThreads), kGemmSmem, stream, 2,
+                        true, maps, c, chunk, again, kDefaultWaitLimitNs);
+}
+
+}  // namespace
+
+size_t linear_loss_workspace(int rows, int hidden, int vocab, bool grad_hidden, bool grad_weight) {
+  return make_plan(rows, hidden, vocab, grad_hidden, grad_weight).total;
+}
+
+cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStream_t stream) {
+  const bool grad = a.grad_hidden || a.grad_weight;
+  const Layout l = make_plan(a.rows, a.width, a.vocab, a.grad_hidden != nullptr, a.grad_weight != nullptr);
+  char *w = static_cast<char *>(workspace);
+  Call c = {};
+  c.T = a.rows; c.H = a.width; c.V = a.vocab;
+  c.rows_pad = l.rows_pad; c.chunk = l.chunk;
+  c.vocab_tiles = l.vocab_tiles; c.hidden_tiles = l.hidden_tiles;
+  c.cells_stride = l.cells_stride;
+  c.ctrl = reinterpret_cast<int32_t *>(w + l.ctrl);
+  c.orig = reinterpret_cast<int32_t *>(w + l.orig);
+  c.label = reinterpret_cast<int32_t *>(w + l.label);
+  c.flags = reinterpret_cast<int32_t *>(w + l.flags);
+  c.target = reinterpret_cast<float *>(w + l.target);
+  c.ref = reinterpret_cast<float *>(w + l.ref);
+  c.scale = reinterpret_cast<float *>(w + l.scale);
+  c.rows = reinterpret_cast<__nv_bfloat16 *>(w + l.rows);
+  c.scaled = a.grad_weight ? reinterpret_cast<__nv_bfloat16 *>(w + l.scaled) : nullptr;
+  c.cells = reinterpret_cast<__nv_bfloat16 *>(w + l.cells);
+  c.sums = reinterpret_cast<float2 *>(w + l.sums);
+  c.splits = reinterpret_cast<float *>(w + l.splits);
+  c.acc = reinterpret_cast<float *>(w + l.acc);
+  c.hidden = static_cast<const __nv_bfloat16 *>(a.hidden);
+  c.weight = static_cast<const __nv_bfloat16 *>(a.weight);
+  c.hidden_stride = a.hidden_stride; c.weight_stride = a.weight_stride;
+  c.labels = a.labels; c.row_weight = a.row_weight; c.row_loss = a.row_loss; c.loss = a.loss;
+  c.dh = static_cast<__nv_bfloat16 *>(a.grad_hidden); c.dh_stride = a.grad_hidden_stride;
+  c.dw = a.grad_weight; c.dw_fp32 = a.grad_weight_dtype == SLIMWISE_DTYPE_FP32; c.dw_stride = a.grad_weight_stride;
+
+  Operands logits, dh, dw;
+  bool ok = encode(&logits.a, c.rows, l.rows_pad, c.H, c.H, kHalf) &&
+            encode(&logits.b, c.weight, c.V, c.H, c.weight_stride, kHalf);
+  if (a.grad_hidden)  // e along the vocabulary, the head across it
+    ok = ok && encode(&dh.a, c.cells, l.chunk, c.V, l.cells_stride, kHalf) &&
+         encode(&dh.b, c.weight, c.V, c.H, c.weight_stride, kDepth);
+  if (a.grad_weight)  // both across the rows
+    ok = ok && encode(&dw.a, c.cells, l.chunk, c.V, l.cells_stride, kDepth) &&
+         encode(&dw.b, c.scaled, l.chunk, c.H, c.H, kDepth);
+  if (!ok) return cudaErrorInvalidValue;
+
+  cudaError_t err = launch_chained(compact_kernel, dim3(1), dim3(1024), 0, stream, 1, false, c);
+  if (err == cudaSuccess)
+    err = launch_chained(gather_kernel, dim3((unsigned)((l.rows_pad + 7) / 8)), dim3(256), 0, stream, 1, true, c);
+  for (int k = 0; k < l.chunks && err == cudaSuccess; ++k) {
+    const dim3 sum_grid((unsigned)(l.chunk / 32));
+    const int finish = k == l.chunks - 1;
+    if (!grad) {
+      err = run_product<kForward>(logits, c, k, 0, stream);
+      if (err == cudaSuccess)
+        err = launch_chained(sums_kernel<kForward>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, 0, finish);
+      continue;
+    }
+    for (int again = 0; again < 2 && err == cudaSuccess; ++again) {
+      err = run_product<kNumerators>(logits, c, k, again, stream);
+      if (err == cudaSuccess)
+        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again,
+                             again && finish);
+    }
+    if (a.grad_hidden && err == cudaSuccess) {
+      int pairs = 0;
+      err = run_product<kGradHidden>(dh, c, k, 0, stream, &pairs);
+      if (err == cudaSuccess)
+        err = launch_chained(join_kernel, dim3(kSms * 8), dim3(256), 0, stream, 1, true, c, k, pairs);
+    }
+    if (a.grad_weight && err == cudaSuccess) err = run_product<kGradWeight>(dw, c, k, 0, stream);
+  }
+  return err;
+}
+
+}  // namespace slimwise
