@@ -589,6 +589,15 @@ def _matrix(t, name, dtype=None, shape=None, index=None):
     return args
 
 
+def _rows_out(out, name, like, shape, index, stream):
+    """(output, pointer, row stride): the given one, or a new one of `like`'s type."""
+    if out is None:
+        out = _new(stream, shape, like.dtype, like.device)
+        return out, out.data_ptr(), shape[1]
+    args = _matrix(out, name, like.dtype, shape, index)
+    return out, args[0], args[4]
+
+
 def _scratch(workspace, size, args, what, stream, device):
     """(workspace, pointer, bytes): the given one, or a new one in the stream's memory."""
     n = ctypes.c_size_t(0)
@@ -611,10 +620,8 @@ def slimwise_embed(table, ids, scale=1.0, out=None, stream=None):
         raise ValueError("ids must have one dimension")
     rows = ids.shape[0]
     p_ids = _vec(ids, _I32, (rows,), "ids", dev)
-    if out is None:
-        out = _new(stream, (rows, hidden), table.dtype, table.device)
-    o = _matrix(out, "out", table.dtype, (rows, hidden), dev)
-    _check(load().slimwise_embed(ptr, code, vocab, hidden, stride, p_ids, rows, scale, o[0], o[4],
+    out, o_ptr, o_stride = _rows_out(out, "out", table, (rows, hidden), dev, stream)
+    _check(load().slimwise_embed(ptr, code, vocab, hidden, stride, p_ids, rows, scale, o_ptr, o_stride,
                                  _stream(stream)), "slimwise_embed")
     return out
 
@@ -651,9 +658,7 @@ def slimwise_norm(x, weight, bias=None, layer=False, eps=1e-5, y=None, mean=None
     None for RMS norm, rstd fp32 [rows]); the last two are what the gradient needs."""
     ptr, code, rows, hidden, stride = _matrix(x, "x")
     dev, one, width = x.get_device(), (rows,), (hidden,)
-    if y is None:
-        y = _new(stream, (rows, hidden), x.dtype, x.device)
-    o = _matrix(y, "y", x.dtype, (rows, hidden), dev)
+    y, y_ptr, y_stride = _rows_out(y, "y", x, (rows, hidden), dev, stream)
     if rstd is None:
         rstd = _new(stream, one, _F32, x.device)
     if not layer:
@@ -663,7 +668,7 @@ def slimwise_norm(x, weight, bias=None, layer=False, eps=1e-5, y=None, mean=None
         mean = _new(stream, one, _F32, x.device)
     _check(load().slimwise_norm(
         ptr, code, rows, hidden, stride, _vec(weight, _F32, width, "weight", dev),
-        None if bias is None else _vec(bias, _F32, width, "bias", dev), int(bool(layer)), eps, o[0], o[4],
+        None if bias is None else _vec(bias, _F32, width, "bias", dev), int(bool(layer)), eps, y_ptr, y_stride,
         None if mean is None else _vec(mean, _F32, one, "mean", dev), _vec(rstd, _F32, one, "rstd", dev),
         _stream(stream)), "slimwise_norm")
     return y, mean, rstd
@@ -691,9 +696,7 @@ def slimwise_norm_grad(dy, x, weight, rstd, mean=None, grad_bias=None, dx=None, 
         raise ValueError("the bias has a gradient in layer norm alone")
     if dbias is not None and not grad_bias:
         raise ValueError("dbias is given, but not wanted")
-    if dx is None:
-        dx = _new(stream, (rows, hidden), x.dtype, x.device)
-    o = _matrix(dx, "dx", x.dtype, (rows, hidden), dev)
+    dx, dx_ptr, dx_stride = _rows_out(dx, "dx", x, (rows, hidden), dev, stream)
     if dweight is None:
         dweight = _new(stream, width, _F32, x.device)
     if grad_bias and dbias is None:
@@ -704,7 +707,7 @@ def slimwise_norm_grad(dy, x, weight, rstd, mean=None, grad_bias=None, dx=None, 
     _check(lib.slimwise_norm_grad(
         d[0], d[4], ptr, code, rows, hidden, stride, _vec(weight, _F32, width, "weight", dev),
         None if mean is None else _vec(mean, _F32, one, "mean", dev), _vec(rstd, _F32, one, "rstd", dev),
-        o[0], o[4], _vec(dweight, _F32, width, "dweight", dev),
+        dx_ptr, dx_stride, _vec(dweight, _F32, width, "dweight", dev),
         None if dbias is None else _vec(dbias, _F32, width, "dbias", dev), _stream(stream), w, n),
         "slimwise_norm_grad")
     if rows == 0:  # the sums over no rows are not computed by a kernel

@@ -11,7 +11,7 @@
 // in two or three passes, histograms in shared memory) while the other CTAs
 // write the zeros of the tokens that do not occur; each of those finds its
 // tokens' presence by reading all ids.  The next kernel sums the sorted rows in
-// pieces of kPiece positions: a token that lies inside a piece is written, one
+// pieces of some positions: a token that lies inside a piece is written, one
 // that crosses its border leaves fp32 sums, which a third kernel adds in order.
 // A token that occurs thousands of times is so spread over hundreds of CTAs.
 #include "train.cuh"
@@ -60,7 +60,9 @@ __global__ void __launch_bounds__(kLookupThreads)
 // ---------------------------------------------------------------------------
 constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
-constexpr int kPiece = 32;        // sorted positions that a group sums
+// Sorted positions that a group sums: enough pieces for all SMs where there are few,
+// and, where there are many, pieces that keep the joins of a frequent token short.
+constexpr int kLeastPiece = 4, kMostPiece = 256;
 constexpr int kSumThreads = 256;
 
 struct SortShared {
@@ -175,6 +177,7 @@ template <typename O, int V>
 __global__ void __launch_bounds__(kSortThreads)
     embed_sort_kernel(SortArgs s, O *__restrict__ out, int hidden, int64_t out_stride) {
   extern __shared__ __align__(16) unsigned char smem[];
+  pdl_launch_dependents();
   if (blockIdx.x < kSortCtas) {
     sort_by_id(s, *reinterpret_cast<SortShared *>(smem));
     return;
@@ -206,7 +209,7 @@ __global__ void __launch_bounds__(kSortThreads)
 
 struct SumArgs {
   const uint2 *items;  // sorted
-  int n, vocab, hidden;
+  int n, piece, vocab, hidden;
   int64_t stride, out_stride;
   float scale;
   bool accumulate;
@@ -240,9 +243,9 @@ __global__ void __launch_bounds__(kSumThreads)
   const int piece = blockIdx.x * (kSumThreads / TPR) + threadIdx.x / TPR;
   const int c0 = blockIdx.y * TPR * 8, width = a.hidden - c0;
   pdl_wait_primary();
-  const int s = piece * kPiece;
-  if (s >= a.n) return;
-  const int end = min(s + kPiece, a.n);
+  pdl_launch_dependents();
+  if ((int64_t)piece * a.piece >= a.n) return;
+  const int s = piece * a.piece, end = min(s + a.piece, a.n);
   const uint32_t before = s > 0 ? __ldcg(&a.items[s - 1].x) : ~0u;
   const uint32_t after = end < a.n ? __ldcg(&a.items[end].x) : ~0u;
   float acc[8];
@@ -290,13 +293,14 @@ __global__ void __launch_bounds__(kSumThreads)
 // A run that crosses pieces: the group of the piece where it begins adds the
 // pieces' sums in order.
 template <typename O, int V, int TPR>
-__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumArgs a, O *out) {
+__global__ void __launch_bounds__(kSumThreads, 1) embed_join_kernel(SumArgs a, O *out) {
   const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
   const int piece = blockIdx.x * (kSumThreads / TPR) + threadIdx.x / TPR;
   const int c0 = blockIdx.y * TPR * 8, width = a.hidden - c0;
   pdl_wait_primary();
-  const int s = piece * kPiece, end = s + kPiece;
-  if (end >= a.n) return;
+  pdl_launch_dependents();
+  if ((int64_t)(piece + 1) * a.piece >= a.n) return;
+  const int s = piece * a.piece, end = s + a.piece;
   const uint32_t run = __ldcg(&a.items[end - 1].x);
   if (run >= (uint32_t)a.vocab || __ldcg(&a.items[end].x) != run) return;
   const bool whole = __ldcg(&a.items[s].x) == run;
@@ -304,7 +308,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumArgs a, O *o
   // pieces that it reaches: those whose first position still is the run's
   int last = piece;
   for (bool more = true; more;) {
-    const int64_t at = (int64_t)(last + 1 + lane) * kPiece;
+    const int64_t at = (int64_t)(last + 1 + lane) * a.piece;
     const uint32_t in = __ballot_sync(0xFFFFFFFFu, at < a.n && __ldcg(&a.items[at].x) == run);
     const int n = in == 0xFFFFFFFFu ? 32 : __ffs(~in) - 1;
     last += n;
@@ -315,20 +319,49 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumArgs a, O *o
   p.template load<true>(a.partial + ((int64_t)piece * 2 + (whole ? 0 : 1)) * a.hidden + c0, t, TPR, width);
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = p.get(e);
-#pragma unroll 4
-  for (int k = piece + 1; k <= last; ++k) {
-    p.template load<true>(a.partial + (int64_t)k * 2 * a.hidden + c0, t, TPR, width);
+  // what it takes is the loads' latency: many at a time and without conditions (columns
+  // past the row's end read its last ones and are not stored; rows past the last
+  // piece read that one and are not added)
+  constexpr int kLoads = 12;
+  const float *row = a.partial + c0;
+  for (int k = piece + 1; k <= last; k += kLoads) {
+    float q[kLoads][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += p.get(e);
+    for (int j = 0; j < kLoads; ++j) {
+      const float *from = row + (int64_t)min(k + j, last) * 2 * a.hidden;
+#pragma unroll
+      for (int e = 0; e < 8; e += V) {
+        const float *at = from + min(RowPart<float, V, 8>::column(e, t, TPR), width - V);
+        if constexpr (V == 1) {
+          q[j][e] = __ldcg(at);
+        } else {
+#pragma unroll
+          for (int i = 0; i < V; i += 4) {
+            const float4 v = __ldcg(reinterpret_cast<const float4 *>(at + i));
+            q[j][e + i] = v.x; q[j][e + i + 1] = v.y; q[j][e + i + 2] = v.z; q[j][e + i + 3] = v.w;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += k + j <= last ? q[j][e] : 0.0f;
   }
   write_row<O, V>(acc, a, out + (int64_t)run * a.out_stride + c0, t, TPR, width);
+}
+
+int piece_rows(int rows) {
+  int p = kLeastPiece;
+  while (p < kMostPiece && (int64_t)p * kSms * 8 < rows) p *= 2;
+  return p;
 }
 
 size_t items_bytes(int rows) { return align_up((size_t)rows * sizeof(uint2), 256); }
 
 template <typename T, typename O, int V, int TPR>
 cudaError_t sum_pieces(const T *grad, const SumArgs &a, O *out, cudaStream_t stream) {
-  const int pieces = (a.n + kPiece - 1) / kPiece, groups = kSumThreads / TPR;
+  const int pieces = (a.n + a.piece - 1) / a.piece, groups = kSumThreads / TPR;
   const dim3 grid((pieces + groups - 1) / groups, (a.hidden + TPR * 8 - 1) / (TPR * 8));
   cudaError_t err = launch_chained(embed_sum_kernel<T, O, V, TPR>, grid, dim3(kSumThreads), 0, stream,
                                    1, true, grad, a, out);
@@ -363,7 +396,7 @@ cudaError_t embed_grad(const T *grad, int rows, int hidden, int64_t stride, cons
   char *w = static_cast<char *>(workspace);
   const SortArgs s = {ids, rows, vocab, reinterpret_cast<uint2 *>(w),
                       reinterpret_cast<uint2 *>(w + items_bytes(rows))};
-  const SumArgs a = {s.a, rows, vocab, hidden, stride, out_stride, scale, accumulate,
+  const SumArgs a = {s.a, rows, piece_rows(rows), vocab, hidden, stride, out_stride, scale, accumulate,
                      reinterpret_cast<float *>(w + 2 * items_bytes(rows))};
   const void *base[1] = {out};
   const int64_t strides[1] = {out_stride};
@@ -412,7 +445,7 @@ cudaError_t launch_embed(const void *table, int dtype, int vocab, int hidden, in
 }
 
 size_t embed_grad_workspace(int rows, int hidden) {
-  const size_t pieces = ((size_t)rows + kPiece - 1) / kPiece;
+  const size_t piece = (size_t)piece_rows(rows), pieces = ((size_t)rows + piece - 1) / piece;
   return 2 * items_bytes(rows) + pieces * 2 * hidden * sizeof(float) + 256;
 }
 

@@ -21,19 +21,9 @@ namespace slimwise {
 
 namespace {
 
-// Threads of a row and elements of a thread: rows up to 256, 1024, 2048, 4096,
-// 8192 and 16384 long.  CTAs hold eight rows' groups of a warp, else one row's.
-constexpr int kWarpRows = 8;
-template <int TPR>
-constexpr int kBlock = TPR == 32 ? 32 * kWarpRows : TPR;
-// Rows loaded at once by a group: 16 (32: the longest rows) KB of a tensor in
-// flight in 512 threads.
-template <typename T, int N>
-constexpr int kBatch = N >= 32 ? 1 : N == 16 ? (sizeof(T) == 2 ? 2 : 1) : (sizeof(T) == 2 ? 4 : 2);
-
-// Sums of K values over the group's threads, known to all of them.  `buf` holds
-// two sets of K values a warp, used in turn (`turn`), so that one barrier a
-// reduction is enough.
+// Sums of K values over a group of TPR threads, known to all of them.  `buf`: of
+// the group, two sets of K values a warp, used in turn (`turn`), so that one
+// barrier a reduction is enough.
 template <int TPR, int K>
 __device__ __forceinline__ void group_sum(float (&v)[K], float *buf, int &turn) {
 #pragma unroll
@@ -42,17 +32,17 @@ __device__ __forceinline__ void group_sum(float (&v)[K], float *buf, int &turn) 
     constexpr int W = TPR / 32;
     float *set = buf + turn * K * W;
     turn ^= 1;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x % TPR / 32, lane = threadIdx.x & 31;
     if (lane == 0)
 #pragma unroll
       for (int k = 0; k < K; ++k) set[k * W + warp] = v[k];
-    __syncthreads();
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / TPR), "n"(TPR) : "memory");
+    // (the W sums of a value by W lanes, the same way in every warp)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      float s = 0.0f;
+      v[k] = set[k * W + (lane & (W - 1))];
 #pragma unroll
-      for (int w = 0; w < W; ++w) s += set[k * W + w];
-      v[k] = s;
+      for (int o = W / 2; o >= 1; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
     }
   }
 }
@@ -65,80 +55,142 @@ struct NormArgs {
   float *mean, *rstd;
 };
 
-// R: rows that a group takes at once.
-template <typename T, int V, int TPR, int N, int R, bool kLayer>
-__global__ void __launch_bounds__(kBlock<TPR>)
+// Threads of a row (TPR) and elements of a thread (N): rows up to 256 (32, 8), 512,
+// 1024, .. 8192 (32 .. 512, 16) and 16384 (512, 32).  Groups are persistent: the weight
+// and bias of a thread's columns stay in its registers, and R rows are on their way while R
+// others are worked on.  16384 x 2048 bf16 layer norm, the kernel alone: with 8 elements
+// a thread 30 us, a row's sums costing as much as its elements; weights from the L1
+// cache for each row 36 us, L1 82 % busy.
+constexpr int kNormThreads = 256;
+template <int TPR>
+constexpr int kNormBlock = TPR > kNormThreads ? TPR : kNormThreads;
+template <typename T, int N>
+constexpr int kNormRows = N * (int)sizeof(T) >= 64 ? 1 : 64 / (N * (int)sizeof(T)) > 2 ? 2 : 64 / (N * (int)sizeof(T));
+
+template <typename T, int V, int TPR, int N, bool kLayer>
+__global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     norm_kernel(const T *__restrict__ x, NormArgs a, T *__restrict__ y) {
-  __shared__ float buf[2 * R * (TPR / 32)];
-  int turn = 0;
-  const int t = threadIdx.x % TPR;
-  const int groups = gridDim.x * (kBlock<TPR> / TPR);
+  constexpr int R = kNormRows<T, N>, P = N / V, W = TPR / 32, kGroups = kNormBlock<TPR> / TPR;
+  constexpr bool kHeld = N <= 16;
+  using Part = RowPart<T, V, N>;
+  __shared__ float2 buf[TPR > 32 ? 2 * R * kNormBlock<TPR> / 32 : 1];
+  const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv = 1.0f / (float)a.hidden;
-  for (int r0 = (blockIdx.x * (kBlock<TPR> / TPR) + threadIdx.x / TPR) * R; r0 < a.rows;
-       r0 += groups * R) {
-    RowPart<T, V, N> part[R];
+  // columns of this warp, and of the warp whose sums this lane joins
+  auto columns = [&](int warp) {
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < P; ++k) n += max(0, min(a.hidden - (k * TPR + 32 * warp) * V, 32 * V));
+    return (float)n;
+  };
+  const float warp_n = columns(t / 32), lane_n = columns(t & (W - 1));
+  const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f, lane_inv = lane_n > 0.0f ? 1.0f / lane_n : 0.0f;
+  auto pair = [&](const float *p, int e) {
+    const int c = Part::column(e, t, TPR), c1 = Part::column(e + 1, t, TPR);
+    return f2(p && c < a.hidden ? __ldg(p + c) : 0.0f, p && c1 < a.hidden ? __ldg(p + c1) : 0.0f);
+  };
+  F2 g[kHeld ? N / 2 : 1], o[kHeld ? N / 2 : 1];
+  if constexpr (kHeld)
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      g[e / 2] = pair(a.weight, e);
+      o[e / 2] = pair(a.bias, e);
+    }
+  auto fetch = [&](Part (&p)[R], int64_t r0) {
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (r0 + i < a.rows) part[i].load(x + (int64_t)(r0 + i) * a.stride, t, TPR, a.hidden);
+      p[i].load(x + (r0 + i < a.rows ? r0 + i : 0) * a.stride, t, TPR, r0 + i < a.rows ? a.hidden : 0);
+  };
+  const int64_t step = (int64_t)gridDim.x * kGroups * R;
+  int64_t r0 = ((int64_t)blockIdx.x * kGroups + group) * R;
+  int turn = 0;
+  Part p[R], next[kHeld ? R : 1];
+  if (kHeld && r0 < a.rows) fetch(p, r0);
+  for (; r0 < a.rows; r0 += step) {
+    if constexpr (kHeld) fetch(next, r0 + step);
+    else fetch(p, r0);
     float mu[R], q[R];
-    if constexpr (kLayer) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      mu[i] = 0.0f;
+      if constexpr (kLayer) {
+        F2 s = f2(0.0f);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) s = add2(s, p[i].get2(e));
+        const float2 h = halves(s);
+        mu[i] = warp_sum(h.x + h.y);
+      }
+    }
+    // the squares (layer norm: about the mean of the warp's columns)
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const F2 m = f2(-mu[i] * warp_inv);
+      F2 s = f2(0.0f);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) {
+        F2 d = p[i].get2(e);
+        if constexpr (kLayer) {
+          d = add2(d, m);
+          // (the last pieces may have columns past the row)
+          if (((e + 1) / V + 1) * TPR * V > a.hidden) {
+            const float2 h = halves(d);
+            d = f2(Part::column(e, t, TPR) < a.hidden ? h.x : 0.0f, Part::column(e + 1, t, TPR) < a.hidden ? h.y : 0.0f);
+          }
+        }
+        s = fma2(d, d, s);
+      }
+      const float2 h = halves(s);
+      q[i] = warp_sum(h.x + h.y);
+    }
+    if constexpr (TPR > 32) {
+      // of the row, a lane a warp: the warps' squares about their means, moved to the row's
+      // mean; two sets in turn, so that one barrier is enough
+      float2 *set = buf + (group * 2 + turn) * R * W;
+      turn ^= 1;
+      if ((t & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < R; ++i) set[i * W + t / 32] = make_float2(mu[i], q[i]);
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        mu[i] = 0.0f;
-        if (r0 + i < a.rows)
+        const float2 v = set[i * W + (t & (W - 1))];
+        q[i] = v.y;
+        if constexpr (kLayer) {
+          mu[i] = v.x;
 #pragma unroll
-          for (int e = 0; e < N; ++e) mu[i] += part[i].get(e);
+          for (int k = W / 2; k >= 1; k >>= 1) mu[i] += __shfl_xor_sync(0xFFFFFFFFu, mu[i], k);
+          mu[i] *= inv;
+          const float d = fmaf(v.x, lane_inv, -mu[i]);
+          q[i] = fmaf(lane_n * d, d, q[i]);
+        }
+#pragma unroll
+        for (int k = W / 2; k >= 1; k >>= 1) q[i] += __shfl_xor_sync(0xFFFFFFFFu, q[i], k);
       }
-      group_sum<TPR>(mu, buf, turn);
+    } else if constexpr (kLayer) {
 #pragma unroll
       for (int i = 0; i < R; ++i) mu[i] *= inv;
     }
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      q[i] = 0.0f;
-      if (r0 + i < a.rows)
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          float d = part[i].get(e);
-          if constexpr (kLayer)
-            d = RowPart<T, V, N>::column(e, t, TPR) < a.hidden ? d - mu[i] : 0.0f;
-          q[i] = fmaf(d, d, q[i]);
-        }
-    }
-    group_sum<TPR>(q, buf, turn);
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      q[i] = 1.0f / sqrtf(fmaf(q[i], inv, a.eps));
-      if (t == 0 && r0 + i < a.rows) {
-        a.rstd[r0 + i] = q[i];
-        if (kLayer && a.mean) a.mean[r0 + i] = mu[i];
+      if (r0 + i >= a.rows) continue;
+      const float rs = 1.0f / sqrtf(fmaf(q[i], inv, a.eps));
+      if (t == 0) {
+        a.rstd[r0 + i] = rs;
+        if constexpr (kLayer) a.mean[r0 + i] = mu[i];
       }
-    }
+      const F2 m = f2(-mu[i]), f = f2(rs);
 #pragma unroll
-    for (int e = 0; e < N; e += 2) {
-      float g[2], b[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int c = RowPart<T, V, N>::column(e + j, t, TPR);
-        g[j] = c < a.hidden ? __ldg(a.weight + c) : 0.0f;
-        b[j] = a.bias && c < a.hidden ? __ldg(a.bias + c) : 0.0f;
+      for (int e = 0; e < N; e += 2) {
+        F2 v = p[i].get2(e);
+        if constexpr (kLayer) v = add2(v, m);
+        if constexpr (kHeld) p[i].set2(e, fma2(mul2(v, f), g[e / 2], o[e / 2]));
+        else p[i].set2(e, fma2(mul2(v, f), pair(a.weight, e), pair(a.bias, e)));
       }
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
-        if (r0 + i >= a.rows) continue;
-        float n[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          n[j] = part[i].get(e + j);
-          if constexpr (kLayer) n[j] -= mu[i];
-          n[j] = fmaf(n[j] * q[i], g[j], b[j]);
-        }
-        part[i].set2(e, n[0], n[1]);
-      }
+      p[i].store(y + (r0 + i) * a.y_stride, t, TPR, a.hidden);
     }
+    if constexpr (kHeld)
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-      if (r0 + i < a.rows) part[i].store(y + (int64_t)(r0 + i) * a.y_stride, t, TPR, a.hidden);
+      for (int i = 0; i < R; ++i) p[i] = next[i];
   }
 }
 
@@ -149,91 +201,132 @@ struct GradArgs {
   float *partial;  // [CTAs][kLayer ? 2 : 1][hidden]
 };
 
+// Threads of a row (TPR) and elements of a thread (N): rows up to 256, 1024, 2048,
+// 4096, 8192 and 16384 long.  A CTA holds eight rows' groups of a warp, else one
+// row's.
+constexpr int kWarpRows = 8;
+template <int TPR>
+constexpr int kBlock = TPR == 32 ? 32 * kWarpRows : TPR;
+// Rows of a group at once; the next ones come into registers meanwhile where these
+// hold both.
+template <typename T, int N>
+constexpr int kBatch = N * (int)sizeof(T) >= 32 ? 1 : 32 / (N * (int)sizeof(T));
+template <int N>
+constexpr bool kAhead = N < 32;
+
 template <typename T, int V, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     norm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ x, GradArgs a,
                      T *__restrict__ dx) {
   constexpr int R = kBatch<T, N>, K = kLayer ? 2 * R : R;
   constexpr int kGroups = kBlock<TPR> / TPR;
-  constexpr bool kShared = N >= 32;
+  constexpr bool kShared = N >= 32;  // dg, db in shared memory; the weight is read for each row
   using Part = RowPart<T, V, N>;
+  struct Batch {
+    Part d[R], x[R];
+    float mu[R], rs[R];
+  };
   __shared__ float buf[2 * K * (TPR / 32)];
-  extern __shared__ float held[];  // kShared: dg [N][TPR], db [N][TPR]; groups of a warp: one group's sums
+  // kShared: dg [N][TPR], db [N][TPR]; groups of a warp: one group's sums
+  extern __shared__ __align__(16) float held[];
   int turn = 0;
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv = 1.0f / (float)a.hidden;
-  float g[N], dg[N], db[N];
+  auto read_weight = [&](int e) {
+    const int c = Part::column(e, t, TPR), c1 = Part::column(e + 1, t, TPR);
+    return f2(c < a.hidden ? __ldg(a.weight + c) : 0.0f, c1 < a.hidden ? __ldg(a.weight + c1) : 0.0f);
+  };
+  F2 g[kShared ? 1 : N / 2], dg[kShared ? 1 : N / 2], db[kShared ? 1 : N / 2];
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int c = Part::column(e, t, TPR);
-    g[e] = c < a.hidden ? __ldg(a.weight + c) : 0.0f;
-    dg[e] = db[e] = 0.0f;
+  for (int e = 0; e < N / 2; ++e) {
     if constexpr (kShared) {
-      held[e * TPR + t] = 0.0f;
-      if constexpr (kLayer) held[(N + e) * TPR + t] = 0.0f;
+      reinterpret_cast<F2 *>(held)[e * TPR + t] = f2(0.0f);
+      if constexpr (kLayer) reinterpret_cast<F2 *>(held)[(N / 2 + e) * TPR + t] = f2(0.0f);
+    } else {
+      g[e] = read_weight(2 * e);
+      dg[e] = db[e] = f2(0.0f);
     }
   }
-  for (int r0 = (blockIdx.x * kGroups + group) * R; r0 < a.rows; r0 += gridDim.x * kGroups * R) {
-    Part d[R], p[R];
-    float mu[R], rs[R], s[K];
+  auto weight = [&](int e) {
+    if constexpr (!kShared) return g[e / 2];
+    else return read_weight(e);
+  };
+  auto fetch = [&](Batch &b, int r0) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const bool in = r0 + i < a.rows;
-      if (in) {
-        d[i].load(dy + (int64_t)(r0 + i) * a.dy_stride, t, TPR, a.hidden);
-        p[i].load(x + (int64_t)(r0 + i) * a.stride, t, TPR, a.hidden);
-      } else {
-#pragma unroll
-        for (int k = 0; k < Part::kWords; ++k) d[i].w[k] = p[i].w[k] = 0u;
-      }
-      rs[i] = in ? __ldg(a.rstd + r0 + i) : 0.0f;
-      mu[i] = kLayer && in ? __ldg(a.mean + r0 + i) : 0.0f;
+      const int64_t r = in ? r0 + i : 0;
+      b.d[i].load(dy + r * a.dy_stride, t, TPR, in ? a.hidden : 0);
+      b.x[i].load(x + r * a.stride, t, TPR, in ? a.hidden : 0);
+      b.rs[i] = in ? __ldg(a.rstd + r) : 0.0f;
+      b.mu[i] = kLayer && in ? __ldg(a.mean + r) : 0.0f;
     }
+  };
+  const int step = gridDim.x * kGroups * R;
+  int r0 = (blockIdx.x * kGroups + group) * R;
+  Batch now, next;
+  if (kAhead<N> && r0 < a.rows) fetch(now, r0);
+  for (; r0 < a.rows; r0 += step) {
+    if constexpr (kAhead<N>) fetch(next, r0 + step < a.rows ? r0 + step : a.rows);
+    else fetch(now, r0);
+    float s[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) s[k] = 0.0f;
+    for (int i = 0; i < R; ++i) {
+      const F2 u = f2(-now.mu[i]), v = f2(now.rs[i]);
+      F2 sum = f2(0.0f), sum0 = f2(0.0f);
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        // (columns past the row: dy = 0 and g = 0)
-        const float de = d[i].get(e), n = (p[i].get(e) - mu[i]) * rs[i], ge = de * g[e];
-        s[i] = fmaf(n, ge, s[i]);
-        if constexpr (kLayer) s[R + i] += ge;
+      for (int e = 0; e < N; e += 2) {
+        // (columns past the row: dy = 0 and the weight 0)
+        F2 n = now.x[i].get2(e);
+        if constexpr (kLayer) n = add2(n, u);
+        n = mul2(n, v);
+        const F2 de = now.d[i].get2(e), ge = mul2(de, weight(e));
+        sum = fma2(n, ge, sum);
+        if constexpr (kLayer) sum0 = add2(sum0, ge);
         if constexpr (kShared) {
-          held[e * TPR + t] = fmaf(de, n, held[e * TPR + t]);
-          if constexpr (kLayer) held[(N + e) * TPR + t] += de;
+          F2 *at = reinterpret_cast<F2 *>(held) + (e / 2) * TPR + t;
+          *at = fma2(de, n, *at);
+          if constexpr (kLayer) at[N / 2 * TPR] = add2(at[N / 2 * TPR], de);
         } else {
-          dg[e] = fmaf(de, n, dg[e]);
-          if constexpr (kLayer) db[e] += de;
+          dg[e / 2] = fma2(de, n, dg[e / 2]);
+          if constexpr (kLayer) db[e / 2] = add2(db[e / 2], de);
         }
       }
+      const float2 h = halves(sum), h0 = halves(sum0);
+      s[i] = h.x + h.y;
+      if constexpr (kLayer) s[R + i] = h0.x + h0.y;
+    }
     group_sum<TPR>(s, buf, turn);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (r0 + i >= a.rows) continue;
-      const float m = s[i] * inv, m0 = kLayer ? s[R + i] * inv : 0.0f;
+      // dx = rs g - rs m0 - n rs m
+      const float rs = now.rs[i];
+      const F2 u = f2(-now.mu[i]), v = f2(rs), m = f2(-rs * (s[i] * inv)), m0 = f2(kLayer ? -rs * (s[R + i] * inv) : 0.0f);
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
-        float v[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float n = (p[i].get(e + j) - mu[i]) * rs[i];
-          v[j] = rs[i] * (fmaf(d[i].get(e + j), g[e + j], -m0) - n * m);
-        }
-        p[i].set2(e, v[0], v[1]);
+        F2 n = now.x[i].get2(e), ge = mul2(now.d[i].get2(e), weight(e));
+        if constexpr (kLayer) n = add2(n, u);
+        n = mul2(n, v);
+        ge = kLayer ? fma2(ge, v, m0) : mul2(ge, v);
+        now.x[i].set2(e, fma2(n, m, ge));
       }
-      p[i].store(dx + (int64_t)(r0 + i) * a.dx_stride, t, TPR, a.hidden);
+      now.x[i].store(dx + (int64_t)(r0 + i) * a.dx_stride, t, TPR, a.hidden);
     }
+    if constexpr (kAhead<N>) now = next;
   }
+  pdl_launch_dependents();
+  pdl_launch_dependents();
   // the CTA's sums: its groups' in turn
   float *out = a.partial + (int64_t)blockIdx.x * (kLayer ? 2 : 1) * a.hidden;
+  F2 *mine = reinterpret_cast<F2 *>(held);
   if constexpr (kGroups > 1) {
     for (int k = 0; k < kGroups; ++k) {
       if (group == k) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          held[e * TPR + t] = (k ? held[e * TPR + t] : 0.0f) + dg[e];
-          if constexpr (kLayer) held[(N + e) * TPR + t] = (k ? held[(N + e) * TPR + t] : 0.0f) + db[e];
+        for (int e = 0; e < N / 2; ++e) {
+          mine[e * TPR + t] = k ? add2(mine[e * TPR + t], dg[e]) : dg[e];
+          if constexpr (kLayer) mine[(N / 2 + e) * TPR + t] = k ? add2(mine[(N / 2 + e) * TPR + t], db[e]) : db[e];
         }
       }
       __syncthreads();
@@ -241,26 +334,224 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     if (group != 0) return;
   }
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int c = Part::column(e, t, TPR);
-    if (c >= a.hidden) continue;
-    out[c] = kShared || kGroups > 1 ? held[e * TPR + t] : dg[e];
-    if constexpr (kLayer) out[a.hidden + c] = kShared || kGroups > 1 ? held[(N + e) * TPR + t] : db[e];
+  for (int e = 0; e < N / 2; ++e) {
+    const float2 v = halves(kShared || kGroups > 1 ? mine[e * TPR + t] : dg[e]);
+    float2 b = make_float2(0.0f, 0.0f);
+    if constexpr (kLayer) b = halves(kShared || kGroups > 1 ? mine[(N / 2 + e) * TPR + t] : db[e]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int c = Part::column(2 * e + j, t, TPR);
+      if (c >= a.hidden) continue;
+      out[c] = j ? v.y : v.x;
+      if constexpr (kLayer) out[a.hidden + c] = j ? b.y : b.x;
+    }
   }
 }
 
-// The CTAs' sums of each column, in the order of the CTAs: eight parts of them,
-// each in order, then the parts.
+// Rows above 4096: the sums of a thread's columns leave no registers for rows.  These
+// pass through a ring in shared memory instead, where each thread copies its own
+// columns ahead (no barriers about data) and reads them twice: for the row's sums,
+// and for dx once these are known, which is one row later, so that the sums' way
+// through the warps and the barrier is hidden behind the row before.
+constexpr int kRingThreads = 512, kRingBytes = 200 * 1024;
+
+template <int B>
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool in) {
+  // (0 bytes of the source: zeros)
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(B), "r"(in ? B : 0)
+               : "memory");
+}
+
+template <typename T, int V, int N, bool kLayer>
+__global__ void __launch_bounds__(kRingThreads, 1)
+    norm_grad_ring_kernel(const T *__restrict__ dy, const T *__restrict__ x, GradArgs a, T *__restrict__ dx,
+                          int slots) {
+  constexpr int P = N / V, B = V * (int)sizeof(T), K = kLayer ? 2 : 1, W = kRingThreads / 32;
+  using Part = RowPart<T, V, V < 2 ? 2 : V>;  // a piece (V = 1: two)
+  constexpr int Q = V < 2 ? 2 : 1, E = V * Q;
+  extern __shared__ __align__(16) unsigned char ring[];  // [slots][2][pieces][threads][V]
+  __shared__ float sums[2][2][W];
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const int pieces = (a.hidden + kRingThreads * V - 1) / (kRingThreads * V);
+  const uint32_t slot_bytes = 2u * pieces * kRingThreads * B;
+  const float inv = 1.0f / (float)a.hidden;
+  auto column = [&](int p) { return (p * kRingThreads + t) * V; };
+  F2 g[N / 2], dg[N / 2], db[kLayer ? N / 2 : 1];
+#pragma unroll
+  for (int e = 0; e < N; e += 2) {
+    const int c = column(e / V) + e % V, c1 = column((e + 1) / V) + (e + 1) % V;
+    g[e / 2] = f2(c < a.hidden ? __ldg(a.weight + c) : 0.0f, c1 < a.hidden ? __ldg(a.weight + c1) : 0.0f);
+    dg[e / 2] = f2(0.0f);
+    if constexpr (kLayer) db[e / 2] = f2(0.0f);
+  }
+  // Only the last piece has threads without columns; theirs read column 0 into it,
+  // 0 bytes of it.  Addresses are a thread's and the piece's constant.
+  constexpr uint32_t kStep = kRingThreads * B;
+  const int last = column(pieces - 1);
+  const bool in_last = last < a.hidden;
+  const uint32_t ring_at = smem_u32(ring) + (uint32_t)t * B, half = (uint32_t)pieces * kStep;
+  auto send = [&](int slot, int64_t r) {
+    if (r < a.rows) {
+      const uint32_t to = ring_at + (uint32_t)slot * slot_bytes;
+      const T *d = dy + r * a.dy_stride + t * V, *v = x + r * a.stride + t * V;
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        if (p + 1 >= pieces) break;
+        copy_async<B>(to + p * kStep, d + p * kRingThreads * V, true);
+        copy_async<B>(to + half + p * kStep, v + p * kRingThreads * V, true);
+      }
+      const uint32_t end = to + (uint32_t)(pieces - 1) * kStep;
+      copy_async<B>(end, dy + r * a.dy_stride + (in_last ? last : 0), in_last);
+      copy_async<B>(end + half, x + r * a.stride + (in_last ? last : 0), in_last);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // E elements from piece p on of a row's half at `from`
+  auto take = [&](uint32_t from, int p) {
+    Part part;
+    if constexpr (B >= 16) {
+      const uint4 v = ld_shared_v4(from + p * kStep);
+      part.w[0] = v.x; part.w[1] = v.y; part.w[2] = v.z; part.w[3] = v.w;
+    } else {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        // (an odd number of pieces: what follows them is read, and not used)
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(part.w[q]) : "r"(from + (p + q) * kStep) : "memory");
+      }
+    }
+    return part;
+  };
+  const int64_t first = blockIdx.x, step = gridDim.x;
+  for (int k = 0; k < slots - 1; ++k) send(k, first + k * step);
+  // of the row whose sums are made, of the one before, whose dx is, and of the next
+  float mu = 0.0f, rs = 0.0f, mu0 = 0.0f, rs0 = 0.0f, m = 0.0f, m0 = 0.0f, mu1 = 0.0f, rs1 = 0.0f;
+  auto statistics = [&](int64_t r, float &u, float &v) {
+    v = r < a.rows ? __ldg(a.rstd + r) : 0.0f;
+    u = kLayer && r < a.rows ? __ldg(a.mean + r) : 0.0f;
+  };
+  statistics(first, mu1, rs1);
+  int slot = 0, before = slots - 1, turn = 0;
+  for (int64_t r = first; r - step < a.rows; r += step) {
+    mu = mu1;
+    rs = rs1;
+    statistics(r + step, mu1, rs1);
+    // groups of copies so far: slots - 1 and one a row; this row's is done with all but the newest ones
+    switch (slots) {
+      case 3: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+      case 4: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+      case 5: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+      default: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+    }
+    if (r < a.rows) {
+      F2 sum = f2(0.0f), sum0 = f2(0.0f);
+      const F2 u = f2(-mu), f = f2(rs);
+      const uint32_t from = ring_at + (uint32_t)slot * slot_bytes;
+#pragma unroll
+      for (int p = 0; p < P; p += Q) {
+        if (p >= pieces) break;
+        const Part d = take(from, p), v = take(from + half, p);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const int k = (p * V + e) / 2;
+          // (columns past the row: dy = 0 and the weight 0; a piece past the last: whatever it reads)
+          F2 n = v.get2(e), de = d.get2(e);
+          if (Q == 2 && p + 1 >= pieces) {
+            n = f2(v.get(0), 0.0f);
+            de = f2(d.get(0), 0.0f);
+          }
+          if constexpr (kLayer) n = add2(n, u);
+          n = mul2(n, f);
+          const F2 ge = mul2(de, g[k]);
+          sum = fma2(n, ge, sum);
+          dg[k] = fma2(de, n, dg[k]);
+          if constexpr (kLayer) {
+            sum0 = add2(sum0, ge);
+            db[k] = add2(db[k], de);
+          }
+        }
+      }
+      const float2 h = halves(sum), h0 = halves(sum0);
+      float s = h.x + h.y, s0 = h0.x + h0.y;
+      s = warp_sum(s);
+      if constexpr (kLayer) s0 = warp_sum(s0);
+      if (lane == 0) {
+        sums[turn][0][warp] = s;
+        if constexpr (kLayer) sums[turn][1][warp] = s0;
+      }
+    }
+    if (r > first) {
+      T *row = dx + (r - step) * a.dx_stride + t * V;
+      const uint32_t from = ring_at + (uint32_t)before * slot_bytes;
+      const F2 u = f2(-mu0), f = f2(rs0), a0 = f2(-rs0 * m0), a1 = f2(-rs0 * m);
+#pragma unroll
+      for (int p = 0; p < P; p += Q) {
+        if (p >= pieces) break;
+        const Part d = take(from, p), v = take(from + half, p);
+        Part o;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          F2 n = v.get2(e), ge = mul2(d.get2(e), g[(p * V + e) / 2]);
+          if constexpr (kLayer) n = add2(n, u);
+          n = mul2(n, f);
+          ge = kLayer ? fma2(ge, f, a0) : mul2(ge, f);
+          o.set2(e, fma2(n, a1, ge));
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          T *to = row + (p + q) * kRingThreads * V;
+          if (p + q + 1 < pieces || (p + q + 1 == pieces && in_last)) {
+            if constexpr (B >= 16) *reinterpret_cast<uint4 *>(to) = make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
+            else *reinterpret_cast<uint32_t *>(to) = o.w[q];
+          }
+        }
+      }
+    }
+    // the slot of the row before is free: the row `slots` after that one
+    send(before, r + (slots - 1) * step);
+    __syncthreads();
+    m = sums[turn][0][lane & (W - 1)];
+    if constexpr (kLayer) m0 = sums[turn][1][lane & (W - 1)];
+#pragma unroll
+    for (int o = W / 2; o >= 1; o >>= 1) {
+      m += __shfl_xor_sync(0xFFFFFFFFu, m, o);
+      if constexpr (kLayer) m0 += __shfl_xor_sync(0xFFFFFFFFu, m0, o);
+    }
+    m *= inv;
+    m0 *= inv;
+    turn ^= 1;
+    mu0 = mu;
+    rs0 = rs;
+    before = slot;
+    slot = slot + 1 < slots ? slot + 1 : 0;
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  pdl_launch_dependents();
+  float *out = a.partial + (int64_t)blockIdx.x * K * a.hidden;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const int c = column(e / V) + e % V;
+    if (c >= a.hidden) continue;
+    const float2 v = halves(dg[e / 2]);
+    out[c] = e & 1 ? v.y : v.x;
+    if constexpr (kLayer) {
+      const float2 b = halves(db[e / 2]);
+      out[a.hidden + c] = e & 1 ? b.y : b.x;
+    }
+  }
+}
+
+// The CTAs' sums of each column, in the order of the CTAs: 32 parts of them, each in
+// order, then the parts.
 // (`partial` is still written when this kernel starts: no __restrict__)
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
     norm_grad_sum_kernel(const float *partial, int ctas, int columns, int hidden, float *dweight,
                          float *dbias) {
-  __shared__ float part[8][32];
+  __shared__ float part[32][33];
   const int lane = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   pdl_wait_primary();
   float s = 0.0f;
   if (c < columns) {
-    const int per = (ctas + 7) / 8, end = min(ctas, (k + 1) * per);
+    const int per = (ctas + 31) / 32, end = min(ctas, (k + 1) * per);
 #pragma unroll 8
     for (int i = k * per; i < end; ++i) s += partial[(int64_t)i * columns + c];
   }
@@ -268,7 +559,7 @@ __global__ void __launch_bounds__(256)
   __syncthreads();
   if (k == 0 && c < columns) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += part[i][lane];
+    for (int i = 1; i < 32; ++i) s += part[i][lane];
     if (c < hidden) dweight[c] = s;
     else if (dbias) dbias[c - hidden] = s;
   }
@@ -284,59 +575,57 @@ int grad_ctas(int rows, int hidden) {
 
 template <typename T, int V, int TPR, int N, bool kLayer>
 cudaError_t norm_rows(const T *x, const NormArgs &a, T *y, cudaStream_t stream) {
-  constexpr int R = kBatch<T, N>, kGroups = kBlock<TPR> / TPR;
-  // few rows: one at a time, on as many SMs as there are
-  const int64_t most = (int64_t)kSms * (2048 / kBlock<TPR>);
-  if (R == 1 || a.rows < (int64_t)kSms * kGroups * R) {
-    const int64_t ctas = ((int64_t)a.rows + kGroups - 1) / kGroups;
-    norm_kernel<T, V, TPR, N, 1, kLayer>
-        <<<(unsigned)(ctas < most ? ctas : most), kBlock<TPR>, 0, stream>>>(x, a, y);
-  } else {
-    const int64_t ctas = ((int64_t)a.rows + kGroups * R - 1) / (kGroups * R);
-    norm_kernel<T, V, TPR, N, R, kLayer>
-        <<<(unsigned)(ctas < most ? ctas : most), kBlock<TPR>, 0, stream>>>(x, a, y);
-  }
+  // at least a row for every group
+  constexpr int kGroups = kNormBlock<TPR> / TPR;
+  const int most = kSms * (512 / kNormBlock<TPR>), ctas = (a.rows + kGroups - 1) / kGroups;
+  norm_kernel<T, V, TPR, N, kLayer><<<ctas < most ? ctas : most, kNormBlock<TPR>, 0, stream>>>(x, a, y);
   return cudaGetLastError();
 }
 
 template <typename T, int V, int TPR, int N, bool kLayer>
 cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *dweight,
                       float *dbias, cudaStream_t stream) {
-  constexpr bool kHeld = N >= 32 || kBlock<TPR> > TPR;
-  constexpr size_t smem = kHeld ? (size_t)(kLayer ? 2 : 1) * N * TPR * 4 : 0;
-  auto kernel = norm_grad_kernel<T, V, TPR, N, kLayer>;
-  if (smem > 48 * 1024) {
-    const cudaError_t err =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (err != cudaSuccess) return err;
-  }
   const int ctas = grad_ctas(a.rows, a.hidden);
-  kernel<<<ctas, kBlock<TPR>, smem, stream>>>(dy, x, a, dx);
+  // a row's two tensors, at least three times in a ring
+  constexpr int kPiece = kRingThreads * V * (int)sizeof(T);
+  const int row_bytes = 2 * ((a.hidden + kRingThreads * V - 1) / (kRingThreads * V)) * kPiece;
+  const int slots = kRingBytes / row_bytes < 6 ? kRingBytes / row_bytes : 6;
+  constexpr bool kRing = N >= 16 && N * sizeof(T) <= 64 && (V * sizeof(T) == 16 || (sizeof(T) == 4 && N == 16));
+  if (kRing && slots >= 3) {
+    if constexpr (kRing) {
+      auto kernel = norm_grad_ring_kernel<T, V, N, kLayer>;
+      const cudaError_t err =
+          cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               kRingBytes + kPiece);
+      if (err != cudaSuccess) return err;
+      kernel<<<ctas, kRingThreads, (size_t)slots * row_bytes + kPiece, stream>>>(dy, x, a, dx, slots);
+    }
+  } else {
+    constexpr bool kHeld = N >= 32 || kBlock<TPR> > TPR;
+    constexpr size_t smem = kHeld ? (size_t)(kLayer ? 2 : 1) * N * TPR * 4 : 0;
+    auto kernel = norm_grad_kernel<T, V, TPR, N, kLayer>;
+    if (smem > 48 * 1024) {
+      const cudaError_t err =
+          cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (err != cudaSuccess) return err;
+    }
+    kernel<<<ctas, kBlock<TPR>, smem, stream>>>(dy, x, a, dx);
+  }
   const cudaError_t err = cudaGetLastError();
   if (err != cudaSuccess) return err;
   const int columns = (kLayer ? 2 : 1) * a.hidden;
-  return launch_chained(norm_grad_sum_kernel, dim3((columns + 31) / 32), dim3(256), 0, stream, 1,
+  return launch_chained(norm_grad_sum_kernel, dim3((columns + 31) / 32), dim3(1024), 0, stream, 1,
                         true, a.partial, ctas, columns, a.hidden, dweight, dbias);
 }
 
-// Calls f.template operator()<T, V, TPR, N>() for a row's type, access and length.
+// Calls f.template run<T, V>() for a row's type and access.
 template <typename F>
-cudaError_t dispatch(int dtype, int v, int hidden, F &&f) {
-#define SLIMWISE_LENGTHS(T, V)                                        \
-  return hidden <= 256    ? f.template operator()<T, V, 32, 8>()      \
-         : hidden <= 1024 ? f.template operator()<T, V, 128, 8>()     \
-         : hidden <= 2048 ? f.template operator()<T, V, 256, 8>()     \
-         : hidden <= 4096 ? f.template operator()<T, V, 512, 8>()     \
-         : hidden <= 8192 ? f.template operator()<T, V, 512, 16>()    \
-                          : f.template operator()<T, V, 512, 32>()
-  if (dtype == SLIMWISE_DTYPE_BF16) {
-    if (v == 8) SLIMWISE_LENGTHS(__nv_bfloat16, 8);
-    if (v == 2) SLIMWISE_LENGTHS(__nv_bfloat16, 2);
-    SLIMWISE_LENGTHS(__nv_bfloat16, 1);
-  }
-  if (v == 4) SLIMWISE_LENGTHS(float, 4);
-  SLIMWISE_LENGTHS(float, 1);
-#undef SLIMWISE_LENGTHS
+cudaError_t dispatch(int dtype, int v, const F &f) {
+  if (dtype == SLIMWISE_DTYPE_BF16)
+    return v == 8   ? f.template run<__nv_bfloat16, 8>()
+           : v == 2 ? f.template run<__nv_bfloat16, 2>()
+                    : f.template run<__nv_bfloat16, 1>();
+  return v == 4 ? f.template run<float, 4>() : f.template run<float, 1>();
 }
 
 template <bool kLayer>
@@ -346,8 +635,18 @@ struct NormCall {
   void *y;
   cudaStream_t stream;
   template <typename T, int V, int TPR, int N>
-  cudaError_t operator()() const {
+  cudaError_t rows() const {
     return norm_rows<T, V, TPR, N, kLayer>(static_cast<const T *>(x), a, static_cast<T *>(y), stream);
+  }
+  template <typename T, int V>
+  cudaError_t run() const {
+    return a.hidden <= 256    ? rows<T, V, 32, 8>()
+           : a.hidden <= 512  ? rows<T, V, 32, 16>()
+           : a.hidden <= 1024 ? rows<T, V, 64, 16>()
+           : a.hidden <= 2048 ? rows<T, V, 128, 16>()
+           : a.hidden <= 4096 ? rows<T, V, 256, 16>()
+           : a.hidden <= 8192 ? rows<T, V, 512, 16>()
+                              : rows<T, V, 512, 32>();
   }
 };
 
@@ -359,9 +658,20 @@ struct GradCall {
   float *dweight, *dbias;
   cudaStream_t stream;
   template <typename T, int V, int TPR, int N>
-  cudaError_t operator()() const {
+  cudaError_t rows() const {
     return grad_rows<T, V, TPR, N, kLayer>(static_cast<const T *>(dy), static_cast<const T *>(x), a,
                                            static_cast<T *>(dx), dweight, dbias, stream);
+  }
+  template <typename T, int V>
+  cudaError_t run() const {
+    return a.hidden <= 256    ? rows<T, V, 32, 8>()
+           : a.hidden <= 1024 ? rows<T, V, 128, 8>()
+           : a.hidden <= 2048 ? rows<T, V, 256, 8>()
+           : a.hidden <= 4096 ? rows<T, V, 512, 8>()
+           : V < 4 && a.hidden <= 5120 ? rows<T, V, 512, V < 4 ? 10 : 16>()
+           : V < 8 && a.hidden <= 6144 ? rows<T, V, 512, V < 8 ? 12 : 16>()
+           : a.hidden <= 8192 ? rows<T, V, 512, 16>()
+                              : rows<T, V, 512, 32>();
   }
 };
 
@@ -374,8 +684,8 @@ cudaError_t launch_norm(const void *x, int dtype, int rows, int hidden, int64_t 
   const int64_t strides[2] = {stride, y_stride};
   const int v = row_vector(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 2, base, strides);
   const NormArgs a = {rows, hidden, stride, y_stride, weight, bias, eps, mean, rstd};
-  return layer ? dispatch(dtype, v, hidden, NormCall<true>{x, a, y, stream})
-               : dispatch(dtype, v, hidden, NormCall<false>{x, a, y, stream});
+  return layer ? dispatch(dtype, v, NormCall<true>{x, a, y, stream})
+               : dispatch(dtype, v, NormCall<false>{x, a, y, stream});
 }
 
 size_t norm_grad_workspace(int rows, int hidden) {
@@ -391,8 +701,8 @@ cudaError_t launch_norm_grad(const void *dy, int64_t dy_stride, const void *x, i
   const int v = row_vector(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 3, base, strides);
   const GradArgs a = {rows, hidden, dy_stride, stride, dx_stride, weight, mean, rstd,
                       static_cast<float *>(workspace)};
-  return mean ? dispatch(dtype, v, hidden, GradCall<true>{dy, x, a, dx, dweight, dbias, stream})
-              : dispatch(dtype, v, hidden, GradCall<false>{dy, x, a, dx, dweight, dbias, stream});
+  return mean ? dispatch(dtype, v, GradCall<true>{dy, x, a, dx, dweight, dbias, stream})
+              : dispatch(dtype, v, GradCall<false>{dy, x, a, dx, dweight, dbias, stream});
 }
 
 }  // namespace slimwise

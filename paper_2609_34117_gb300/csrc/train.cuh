@@ -108,6 +108,37 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t *>(&b);
 }
 
+// Two fp32 numbers in a register pair, and arithmetic on both at once.
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 f2(float a) { return f2(a, a); }
+__device__ __forceinline__ float2 halves(F2 a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+
 // A thread's part of a row: N elements of T in pieces of V, the row's pieces
 // dealt to `threads` threads in turn, as they lie in memory (a bf16 in half a
 // register).  Element e is column ((e / V) threads + t) V + e % V.
@@ -118,7 +149,7 @@ struct RowPart {
 
   template <bool kAfter, typename W>
   static __device__ __forceinline__ W read(const W *p) {
-    if constexpr (kAfter) return *p;
+    if constexpr (kAfter) return __ldcg(p);
     else return __ldg(p);
   }
   static __device__ __forceinline__ int column(int e, int t, int threads) {
@@ -158,6 +189,11 @@ struct RowPart {
     else return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
   }
   // Two neighbouring elements, e even.
+  __device__ __forceinline__ F2 get2(int e) const { return f2(get(e), get(e + 1)); }
+  __device__ __forceinline__ void set2(int e, F2 v) {
+    const float2 h = halves(v);
+    set2(e, h.x, h.y);
+  }
   __device__ __forceinline__ void set2(int e, float a, float b) {
     if constexpr (sizeof(T) == 4) {
       w[e] = __float_as_uint(a);

@@ -161,10 +161,10 @@ def _check_norm_grad(dy, x, w, layer, **kw):
     dx, dw, db = sw.slimwise_norm_grad(dy, x, w, rstd, mean=mean, **kw)
     wx, ww, wb, tol, sw_, sb = _grad_reference(dy, x, w, mean, rstd)
     _within(dx, wx, wx.abs() * _half(x.dtype) + tol * 1.01 + torch.finfo(x.dtype).tiny)
-    # a CTA's rows, its eight groups, an eighth of the CTAs' sums, the eighths; two roundings of a term
+    # a CTA's rows, its eight groups, a 32nd of the CTAs' sums, the 32 parts; two roundings of a term
     rows, hidden = x.shape
     ctas = 152 * (2 if hidden <= 256 else 4 if hidden <= 1024 else 2 if hidden <= 2048 else 1)
-    chain = (math.ceil(rows / min(ctas, max(rows, 1))) + 4 + 8 + math.ceil(ctas / 8) + 8 + 3) * 2.0 ** -24
+    chain = (math.ceil(rows / min(ctas, max(rows, 1))) + 4 + 8 + math.ceil(ctas / 32) + 32 + 3) * 2.0 ** -24
     _within(dw, ww, sw_ * chain + 1e-37)
     if layer and kw.get("grad_bias", True):
         _within(db, wb, sb * chain + 1e-37)
