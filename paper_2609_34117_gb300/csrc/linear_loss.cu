@@ -48,9 +48,11 @@ constexpr int64_t kMostCells = 1ll << 30;
 constexpr int kTile = 256;       // rows and columns of a pair's tile
 constexpr int kHalf = 128;       // of a CTA's share of an operand
 constexpr int kDepth = 64;       // slice of the contraction: 128 bytes
-constexpr int kStages = 7;
+constexpr int kStages = 6;
 constexpr int kOperandBytes = kHalf * kDepth * 2;
 constexpr int kStageBytes = 2 * kOperandBytes;
+// A warp's 32 rows x 64 columns of bf16 on their way out by TMA (128-byte swizzle).
+constexpr int kOutBytes = 32 * 128;
 constexpr int kEpiWarps = 8, kGemmThreads = 64 + 32 * kEpiWarps;
 constexpr int kMostPairs = kSms / 2;
 // Tiles of partial sums of dh: splits of the vocabulary are made while they fit.
@@ -58,12 +60,12 @@ constexpr int kMostSplits = 96, kSplitTiles = 8 * kMostPairs;
 constexpr float kFloor = -FLT_MAX;  // stands in for -inf as a maximum
 
 enum Mode { kForward, kNumerators, kGradHidden, kGradWeight };
-enum Word { kLive = 0, kArrived = 1, kErr = kCtrlErr };
+enum Word { kLive = 0, kArrived = 1, kArrivedAgain = 2, kErr = kCtrlErr };
 
 struct Layout {
   int rows_pad, chunk, chunks, vocab_tiles, hidden_tiles, split_tiles;
   int64_t cells_stride;
-  size_t ctrl, orig, label, target, ref, scale, flags, rows, scaled, sums, cells, splits, acc, total;
+  size_t ctrl, counts, orig, label, target, ref, scale, flags, rows, scaled, sums, cells, splits, acc, total;
 };
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
@@ -98,6 +100,7 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
   };
   const size_t n = (size_t)l.rows_pad;
   l.ctrl = take(kCtrlWords * 4);
+  l.counts = take((n + 1023) / 1024 * 4);
   l.orig = take(n * 4);
   l.label = take(n * 4);
   l.target = take(n * 4);
@@ -120,6 +123,7 @@ struct Call {
   int rows_pad, chunk, vocab_tiles, hidden_tiles;
   int64_t cells_stride;
   int32_t *ctrl, *orig, *label;
+  int32_t *counts;  // labelled rows of each 1024 (more than kCountedRows rows)
   int32_t *flags;  // [3][rows_pad / 256]: tiles to run again; their list; each chunk's number of them
   float *target, *ref, *scale;
   __nv_bfloat16 *rows, *scaled, *cells;
@@ -162,56 +166,59 @@ __device__ __forceinline__ int choose_splits(int tiles, int kb, int pairs) {
 // ---------------------------------------------------------------------------
 // rows with a label, moved together
 // ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(1024) compact_kernel(Call c) {
-  __shared__ int part[32];
-  __shared__ int base;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+constexpr int kGatherThreads = 1024, kGatherRows = kGatherThreads / 32;
+// More rows than this: the labels of each 1024 are counted first, and a CTA adds up
+// counts instead of reading all labels before its own.
+constexpr int kCountedRows = 32768;
+
+__global__ void __launch_bounds__(1024) count_kernel(Call c) {
   pdl_launch_dependents();
-  if (threadIdx.x < kCtrlWords) c.ctrl[threadIdx.x] = 0;
-  for (int i = threadIdx.x; i < c.rows_pad / kTile * 3; i += 1024) c.flags[i] = 0;
-  if (threadIdx.x == 0) base = 0;
-  __syncthreads();
-  for (int t0 = 0; t0 < c.rows_pad; t0 += 1024) {
-    const int t = t0 + threadIdx.x;
-    const int y = t < c.T ? __ldg(c.labels + t) : -1;
-    const uint32_t live = __ballot_sync(0xFFFFFFFFu, y >= 0);
-    if (lane == 0) part[warp] = __popc(live);
-    __syncthreads();
-    int at = base;
-    for (int w = 0; w < warp; ++w) at += part[w];
-    at += __popc(live & ((1u << lane) - 1));
-    if (y >= 0) {
-      c.orig[at] = t;
-      c.label[at] = y;
-    }
-    __syncthreads();
-    if (threadIdx.x == 1023) base = at + (y >= 0 ? 1 : 0);
-    __syncthreads();
-  }
-  const int n = base;
-  if (threadIdx.x == 0) c.ctrl[kLive] = n;
-  for (int i = n + threadIdx.x; i < c.rows_pad; i += 1024) c.label[i] = c.orig[i] = -1;
+  const int t = blockIdx.x * 1024 + threadIdx.x;
+  const int n = __syncthreads_count(t < c.T && __ldg(c.labels + t) >= 0);
+  if (threadIdx.x == 0) c.counts[blockIdx.x] = n;
 }
 
-// A warp a row: row i of the labelled ones is copied and its label's logit
-// computed (fp32 sums of a lane's products, then over the lanes); row i of the
-// call gets the results of a row without a label where it has none.
-__global__ void __launch_bounds__(256) gather_kernel(Call c) {
-  const int lane = threadIdx.x & 31, i = blockIdx.x * 8 + (threadIdx.x >> 5);
+// A warp a row: with a label, the row is copied to its place among those and its
+// label's logit computed (fp32 sums of a lane's products, then over the lanes);
+// without, it gets its results.
+__global__ void __launch_bounds__(kGatherThreads) gather_kernel(Call c, int counted) {
+  __shared__ int before_all, in_warp[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t0 = blockIdx.x * kGatherRows, t = t0 + warp;
+  if (threadIdx.x == 0) before_all = 0;
+  __syncthreads();
   pdl_wait_primary();
   pdl_launch_dependents();
-  if (i >= c.rows_pad) return;
+  if (blockIdx.x == 0) {
+    if (threadIdx.x != kLive && threadIdx.x < kCtrlWords) c.ctrl[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < c.rows_pad / kTile * 3; i += kGatherThreads) c.flags[i] = 0;
+  }
+  // labelled rows before the CTA's, in whole numbers
+  int n = 0;
+  const int from = counted ? t0 / 1024 * 1024 : 0;
+  if (counted)
+    for (int i = threadIdx.x; i < from / 1024; i += kGatherThreads) n += __ldcg(c.counts + i);
+#pragma unroll 8
+  for (int i = from + threadIdx.x; i < t0; i += kGatherThreads) n += __ldg(c.labels + i) >= 0 ? 1 : 0;
+  n = __reduce_add_sync(0xFFFFFFFFu, n);
+  if (lane == 0 && n) atomicAdd(&before_all, n);
+  const int y = t < c.T ? __ldg(c.labels + t) : -1;
+  if (lane == 0) in_warp[warp] = y >= 0 ? 1 : 0;
+  __syncthreads();
+  const uint32_t live = __ballot_sync(0xFFFFFFFFu, in_warp[lane] != 0);
+  const int at = before_all + __popc(live & ((1u << warp) - 1));
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) c.ctrl[kLive] = before_all + __popc(live);
+  if (t >= c.T) return;
   const int words = c.H / 8;
-  const int t = __ldcg(c.orig + i), y = __ldcg(c.label + i);
-  uint4 *to = reinterpret_cast<uint4 *>(c.rows + (int64_t)i * c.H);
-  if (t >= 0) {
-    const uint4 *from = reinterpret_cast<const uint4 *>(c.hidden + (int64_t)t * c.hidden_stride);
+  if (y >= 0) {
+    const uint4 *row = reinterpret_cast<const uint4 *>(c.hidden + (int64_t)t * c.hidden_stride);
     const bool known = y < c.V;
     const uint4 *head = reinterpret_cast<const uint4 *>(c.weight + (int64_t)(known ? y : 0) * c.weight_stride);
+    uint4 *to = reinterpret_cast<uint4 *>(c.rows + (int64_t)at * c.H);
     float s = 0.0f;
 #pragma unroll 4
     for (int k = lane; k < words; k += 32) {
-      const uint4 a = __ldg(from + k), b = __ldg(head + k);
+      const uint4 a = __ldg(row + k), b = __ldg(head + k);
       to[k] = a;
       const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -222,14 +229,15 @@ __global__ void __launch_bounds__(256) gather_kernel(Call c) {
     }
     s = warp_sum(s);
     if (!known) s = __int_as_float(0x7FC00000);  // a label outside the vocabulary: NaN
-    if (lane == 0) c.target[i] = c.ref[i] = s;
+    if (lane == 0) {
+      c.orig[at] = t;
+      c.label[at] = y;
+      c.target[at] = c.ref[at] = s;
+    }
   } else {
-    for (int k = lane; k < words; k += 32) to[k] = make_uint4(0, 0, 0, 0);
-  }
-  if (i < c.T && __ldg(c.labels + i) < 0) {
-    if (lane == 0) c.row_loss[i] = 0.0f;
+    if (lane == 0) c.row_loss[t] = 0.0f;
     if (c.dh) {
-      uint4 *row = reinterpret_cast<uint4 *>(c.dh + (int64_t)i * c.dh_stride);
+      uint4 *row = reinterpret_cast<uint4 *>(c.dh + (int64_t)t * c.dh_stride);
       for (int k = lane; k < words; k += 32) row[k] = make_uint4(0, 0, 0, 0);
     }
   }
@@ -240,6 +248,7 @@ __global__ void __launch_bounds__(256) gather_kernel(Call c) {
 // ---------------------------------------------------------------------------
 struct Operands {
   CUtensorMap a, b;
+  CUtensorMap out;  // bf16 results, boxes of 64 columns and 32 rows
 };
 
 // Shared-memory descriptor of an MN-major operand with 128-byte swizzle: groups
@@ -277,6 +286,39 @@ __device__ __forceinline__ float ex2(float x) {
   return r;
 }
 
+// A warp's 64 columns of 32 rows, two to a word, from the buffer of its lanes' rows.
+struct OutBuffer {
+  uint32_t at;  // shared address, 1024-byte aligned
+  // columns 32 h.. of this lane's row (h = 0, 1)
+  __device__ __forceinline__ void put(int lane, int h, const uint32_t (&w)[16]) const {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(
+                       at + (uint32_t)(lane * 128 + (((4 * h + c) ^ (lane & 7)) << 4))),
+                   "r"(w[4 * c]), "r"(w[4 * c + 1]), "r"(w[4 * c + 2]), "r"(w[4 * c + 3])
+                   : "memory");
+  }
+  // before it is written again: the last store has read it
+  __device__ __forceinline__ void wait(int lane) const {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+  }
+  __device__ __forceinline__ void send(int lane, const CUtensorMap *map, int x, int y) const {
+    fence_proxy_async_shared();
+    __syncwarp();
+    if (lane == 0) {
+      asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                       (uint64_t)map),
+                   "r"(x), "r"(y), "r"(at)
+                   : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+  __device__ __forceinline__ void finish(int lane) const {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+};
+
 struct Unit {
   int m, n, k0, k1;
 };
@@ -310,7 +352,8 @@ struct Work {
   }
 };
 
-constexpr size_t kGemmSmem = (size_t)kStages * kStageBytes + 8 * (2 * kStages + 5) + 64 + 1024;
+constexpr size_t kBars = (size_t)kStages * kStageBytes + kEpiWarps * kOutBytes;
+constexpr size_t kGemmSmem = kBars + 8 * (2 * kStages + 5) + 64 + 1024;
 
 // Sums of the columns' numerators and the P tile of 32 columns.
 template <Mode kMode>
@@ -360,13 +403,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   unsigned char *smem = reinterpret_cast<unsigned char *>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t smem_base = smem_u32(smem);
-  const uint32_t bar0 = smem_base + kStages * kStageBytes;
+  const uint32_t bar0 = smem_base + (uint32_t)kBars;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
   auto accf_bar = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
   auto acce_bar = [&](int b) { return bar0 + 8u * (2 * kStages + 2 + b); };
   const uint32_t drain_bar = bar0 + 8u * (2 * kStages + 4);
-  int *misc = reinterpret_cast<int *>(smem + kStages * kStageBytes + 8 * (2 * kStages + 5));
+  int *misc = reinterpret_cast<int *>(smem + kBars + 8 * (2 * kStages + 5));
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(misc);
   volatile int *abort = misc + 1;
   volatile int *consumed = misc + 2;
@@ -377,7 +420,39 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   const bool lead = crank == 0;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
-  pdl_wait_primary();
+  // The first product's second run has hardly ever anything to do: it looks first.
+  // All others get ready while the kernel before ends.
+  if (again) {
+    pdl_wait_primary();
+    if (__ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0) return;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(accf_bar(b), 1);
+      mbar_init(acce_bar(b), 2 * kEpiWarps);
+    }
+    mbar_init(drain_bar, 1);
+    *abort = 0;
+    *consumed = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&maps.a);
+    tma_prefetch_desc(&maps.b);
+    if constexpr (kMode == kNumerators || kMode == kGradWeight) tma_prefetch_desc(&maps.out);
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32((const void *)tmem_slot), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  if (!again) pdl_wait_primary();
   const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
   Work<kMode> work;
   work.list = nullptr;
@@ -421,33 +496,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
     }
   }
-  if (pair >= work.units) return;  // (both CTAs of a pair)
-
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(full_bar(s), 1);
-      mbar_init(empty_bar(s), 1);
-    }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(accf_bar(b), 1);
-      mbar_init(acce_bar(b), 2 * kEpiWarps);
-    }
-    mbar_init(drain_bar, 1);
-    *abort = 0;
-    *consumed = 0;
-    mbar_fence_init();
-    tma_prefetch_desc(&maps.a);
-    tma_prefetch_desc(&maps.b);
-  }
-  if (warp == 1) {
-    tmem_alloc_pair(smem_u32((const void *)tmem_slot), 512);
-    tmem_relinquish_pair();
-  }
-  tc_fence_before();
-  __syncthreads();
-  cluster_sync_all();
-  tc_fence_after();
-  const uint32_t tmem_base = *tmem_slot;
   auto give_up = [&](int code) {
     if (!*abort) {
       *abort = 1;
@@ -578,6 +626,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     // ------------------------------------------------------------ accumulators
     const int q = warp & 3, half = (warp - 2) >> 2;  // lanes 32 q.., columns 128 half..
     const int in_tile = (int)crank * kHalf + 32 * q + lane;
+    const OutBuffer out = {smem_base + (uint32_t)(kStages * kStageBytes + (warp - 2) * kOutBytes)};
     int local = 0;
     for (int u = pair; u < work.units; u += pairs, ++local) {
       const Unit w = work.at(u);
@@ -607,12 +656,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           numerators<kMode>(z, ref, label - col, c.V - col, sum, most, packed);
           if constexpr (kMode == kNumerators) {
             // rows past the last one: zeros (they are in the contraction of dW)
-            uint4 *to = reinterpret_cast<uint4 *>(c.cells + (int64_t)row * c.cells_stride + col);
+            if (!live)
 #pragma unroll
-            for (int p = 0; p < 4; ++p)
-              if (col + 8 * p < c.cells_stride)
-                to[p] = live ? make_uint4(packed[4 * p], packed[4 * p + 1], packed[4 * p + 2], packed[4 * p + 3])
-                             : make_uint4(0, 0, 0, 0);
+              for (int j = 0; j < 16; ++j) packed[j] = 0u;
+            if ((k & 1) == 0) out.wait(lane);
+            out.put(lane, k & 1, packed);
+            if ((k & 1) && col - 32 < c.cells_stride) out.send(lane, &maps.out, col - 32, row - lane);
           }
         }
         c.sums[(int64_t)(w.n * 2 + half) * c.chunk + row] = make_float2(sum, most);
@@ -639,30 +688,32 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           tmem_ld_row(taddr + k * 32, z);
           tmem_ld_wait();
           if (k == kHalf / 32 - 1) release();
-          if (row >= c.V) continue;
+          const int col = col0 + 32 * k;
+          if (chunk > 0 && row < c.V)
 #pragma unroll
-          for (int j = 0; j < 32; j += 8) {
-            const int col = col0 + 32 * k + j;
-            if (col >= c.H) continue;
-            if (chunk > 0) {
-              const float4 x = *reinterpret_cast<const float4 *>(acc + col);
-              const float4 y = *reinterpret_cast<const float4 *>(acc + col + 4);
-              z[j] += x.x; z[j + 1] += x.y; z[j + 2] += x.z; z[j + 3] += x.w;
-              z[j + 4] += y.x; z[j + 5] += y.y; z[j + 6] += y.z; z[j + 7] += y.w;
-            }
-            if (last && !c.dw_fp32) {
-              *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(c.dw) + (int64_t)row * c.dw_stride + col) =
-                  make_uint4(pack_bf16(z[j], z[j + 1]), pack_bf16(z[j + 2], z[j + 3]),
-                             pack_bf16(z[j + 4], z[j + 5]), pack_bf16(z[j + 6], z[j + 7]));
-            } else {
-              float *to = last ? static_cast<float *>(c.dw) + (int64_t)row * c.dw_stride + col : acc + col;
-              *reinterpret_cast<float4 *>(to) = make_float4(z[j], z[j + 1], z[j + 2], z[j + 3]);
-              *reinterpret_cast<float4 *>(to + 4) = make_float4(z[j + 4], z[j + 5], z[j + 6], z[j + 7]);
-            }
+            for (int j = 0; j < 32; j += 4)
+              if (col + j < c.H) {
+                const float4 x = *reinterpret_cast<const float4 *>(acc + col + j);
+                z[j] += x.x; z[j + 1] += x.y; z[j + 2] += x.z; z[j + 3] += x.w;
+              }
+          if (last && !c.dw_fp32) {
+            uint32_t packed[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) packed[j] = pack_bf16(z[2 * j], z[2 * j + 1]);
+            if ((k & 1) == 0) out.wait(lane);
+            out.put(lane, k & 1, packed);
+            if ((k & 1) && col - 32 < c.H && row - lane < c.V) out.send(lane, &maps.out, col - 32, row - lane);
+          } else if (row < c.V) {
+            float *to = last ? static_cast<float *>(c.dw) + (int64_t)row * c.dw_stride : acc;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              if (col + j < c.H)
+                *reinterpret_cast<float4 *>(to + col + j) = make_float4(z[j], z[j + 1], z[j + 2], z[j + 3]);
           }
         }
       }
     }
+    out.finish(lane);
   }
 
   tc_fence_before();
@@ -681,7 +732,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 // loss.  kNumerators: besides, the row's factor, the label's numerator and the
 // scaled row; `again`: only rows of the tiles that were run again (else a row whose
 // reference does not do marks its tile).  finish: the CTA that ends last adds up the
-// loss, in fp64 and in the order of the rows.
+// loss, in fp64 and in the order of the rows (the first run's, unless a tile is marked).
 template <Mode kMode>
 __global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again, int finish) {
   __shared__ float part_sum[32][33], part_most[32][33];
@@ -691,6 +742,7 @@ __global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait_primary();
   pdl_launch_dependents();
+  if (again && __ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0) return;
   const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
   const int first = blockIdx.x * 32, row = first + lane;
   const int tile = row0 / kTile + first / kTile;
@@ -737,10 +789,14 @@ __global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again
         const float loss = ref == z ? log1pf(S) : (ref - z) + logf(own + S);
         c.row_loss[t] = loss;
         if constexpr (kMode == kNumerators) {
-          scale = (c.row_weight ? __ldg(c.row_weight + t) : 1.0f) / (own + S);
+          // -S is the largest numerator: its rounding goes into the row's factor, and so to
+          // the others, whose products with the operands mostly cancel
+          const __nv_bfloat16 least = __float2bfloat16_rn(-S);
+          const float ratio = S / -__bfloat162float(least);
+          scale = (c.row_weight ? __ldg(c.row_weight + t) : 1.0f) / (own + S) * (ratio > 0.5f && ratio < 2.0f ? ratio : 1.0f);
           c.scale[at] = scale;
           const int y = __ldcg(c.label + at);
-          if (y < c.V) c.cells[(int64_t)row * c.cells_stride + y] = __float2bfloat16_rn(-S);
+          if (y < c.V) c.cells[(int64_t)row * c.cells_stride + y] = least;
         }
       }
       row_scale[lane] = scale;
@@ -767,7 +823,9 @@ __global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again
   if (!finish || !c.loss) return;
   __threadfence();
   __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(c.ctrl + kArrived, 1) == (int)gridDim.x - 1;
+  if (threadIdx.x == 0)
+    last = atomicAdd(c.ctrl + (again ? kArrivedAgain : kArrived), 1) == (int)gridDim.x - 1 &&
+           (again || __ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0);
   __syncthreads();
   if (!last) return;
   __threadfence();
@@ -799,25 +857,22 @@ __global__ void __launch_bounds__(256) join_kernel(Call c, int chunk, int pairs)
     if (threadIdx.x == 0) n_splits = s;
   }
   __syncthreads();
-  const int splits = n_splits, words = c.H / 8;
+  const int splits = n_splits, words = c.H / 4;
   const int64_t all = (int64_t)rows * words;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-    const int row = (int)(i / words), col = (int)(i - (int64_t)row * words) * 8;
+    const int row = (int)(i / words), col = (int)(i - (int64_t)row * words) * 4;
     const int tile = row / kTile * c.hidden_tiles + col / kTile;
     const float *from = c.splits + ((int64_t)tile * kTile + row % kTile) * kTile + col % kTile;
-    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
     for (int s = 0; s < splits; ++s) {
       const float4 x = __ldcg(reinterpret_cast<const float4 *>(from));
-      const float4 y = __ldcg(reinterpret_cast<const float4 *>(from) + 1);
       v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-      v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
       from += (int64_t)tiles * kTile * kTile;
     }
     const float f = __ldcg(c.scale + row0 + row);
     __nv_bfloat16 *to = c.dh + (int64_t)__ldcg(c.orig + row0 + row) * c.dh_stride + col;
-    *reinterpret_cast<uint4 *>(to) = make_uint4(pack_bf16(v[0] * f, v[1] * f), pack_bf16(v[2] * f, v[3] * f),
-                                                pack_bf16(v[4] * f, v[5] * f), pack_bf16(v[6] * f, v[7] * f));
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0] * f, v[1] * f), pack_bf16(v[2] * f, v[3] * f));
   }
 }
 
@@ -911,6 +966,7 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   c.vocab_tiles = l.vocab_tiles; c.hidden_tiles = l.hidden_tiles;
   c.cells_stride = l.cells_stride;
   c.ctrl = reinterpret_cast<int32_t *>(w + l.ctrl);
+  c.counts = reinterpret_cast<int32_t *>(w + l.counts);
   c.orig = reinterpret_cast<int32_t *>(w + l.orig);
   c.label = reinterpret_cast<int32_t *>(w + l.label);
   c.flags = reinterpret_cast<int32_t *>(w + l.flags);
@@ -930,20 +986,27 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   c.dh = static_cast<__nv_bfloat16 *>(a.grad_hidden); c.dh_stride = a.grad_hidden_stride;
   c.dw = a.grad_weight; c.dw_fp32 = a.grad_weight_dtype == SLIMWISE_DTYPE_FP32; c.dw_stride = a.grad_weight_stride;
 
-  Operands logits, dh, dw;
-  bool ok = encode(&logits.a, c.rows, l.rows_pad, c.H, c.H, kHalf) &&
+  Operands logits = {}, dh = {}, dw = {};
+  // (rows past the call's are zeros without being read)
+  bool ok = encode(&logits.a, c.rows, c.T, c.H, c.H, kHalf) &&
             encode(&logits.b, c.weight, c.V, c.H, c.weight_stride, kHalf);
+  if (grad) ok = ok && encode(&logits.out, c.cells, l.chunk, l.cells_stride, l.cells_stride, 32);
   if (a.grad_hidden)  // e along the vocabulary, the head across it
     ok = ok && encode(&dh.a, c.cells, l.chunk, c.V, l.cells_stride, kHalf) &&
          encode(&dh.b, c.weight, c.V, c.H, c.weight_stride, kDepth);
   if (a.grad_weight)  // both across the rows
     ok = ok && encode(&dw.a, c.cells, l.chunk, c.V, l.cells_stride, kDepth) &&
-         encode(&dw.b, c.scaled, l.chunk, c.H, c.H, kDepth);
+         encode(&dw.b, c.scaled, l.chunk, c.H, c.H, kDepth) &&
+         (c.dw_fp32 || encode(&dw.out, c.dw, c.V, c.H, c.dw_stride, 32));
   if (!ok) return cudaErrorInvalidValue;
 
-  cudaError_t err = launch_chained(compact_kernel, dim3(1), dim3(1024), 0, stream, 1, false, c);
+  const int counted = c.T > kCountedRows;
+  cudaError_t err = cudaSuccess;
+  if (counted)
+    err = launch_chained(count_kernel, dim3((unsigned)ceil_div(c.T, 1024)), dim3(1024), 0, stream, 1, false, c);
   if (err == cudaSuccess)
-    err = launch_chained(gather_kernel, dim3((unsigned)((l.rows_pad + 7) / 8)), dim3(256), 0, stream, 1, true, c);
+    err = launch_chained(gather_kernel, dim3((unsigned)ceil_div(c.T, kGatherRows)), dim3(kGatherThreads), 0, stream,
+                         1, counted != 0, c, counted);
   for (int k = 0; k < l.chunks && err == cudaSuccess; ++k) {
     const dim3 sum_grid((unsigned)(l.chunk / 32));
     const int finish = k == l.chunks - 1;
@@ -956,8 +1019,7 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
     for (int again = 0; again < 2 && err == cudaSuccess; ++again) {
       err = run_product<kNumerators>(logits, c, k, again, stream);
       if (err == cudaSuccess)
-        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again,
-                             again && finish);
+        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again, finish);
     }
     if (a.grad_hidden && err == cudaSuccess) {
       int pairs = 0;

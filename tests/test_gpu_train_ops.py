@@ -372,8 +372,9 @@ def _check_loss(hidden, weight, labels, row_weight, dh_out=True, dw_out=True, **
     p.scatter_(1, y, -others[:, None])
     dz = p * wt[:, None]
     b = 2.0 ** -8
-    # a numerator: rounded, and off by what its exponent and the row's sum are
-    off = dz.abs() * (b + 2 * sums)[:, None]
+    # a numerator: rounded (the label's: not, but the others then take over its rounding),
+    # and off by what its exponent and the row's sum are
+    off = dz.abs() * (2 * b + 2 * sums)[:, None]
     if dh is not None:
         want = dz @ w
         steps = (vocab / 16 + 128) * 2.0 ** -23
@@ -514,6 +515,14 @@ def test_linear_loss_in_chunks(labelled):
         _within(dh[a:a + 775], want, 2.0 ** -7 * want.abs() + (vocab / 16 + 128) * 2.0 ** -23 * dh_size[a:a + 775])
         total += part[3].double()
     _within(dw, total, 2.0 ** -8 * total.abs() + (rows / 16 + 32) * 2.0 ** -22 * dw_size + 1e-37)
+
+
+def test_linear_loss_of_many_rows():
+    # labels counted in blocks first
+    rows, width, vocab = 70001, 16, 300
+    hidden, weight, labels, wt = _head(rows, width, vocab, seed=8, ignored=0.3)
+    _check_loss(hidden, weight, labels, wt)
+    _check_loss(hidden, weight, labels, None, dh_out=False, dw_out=False)
 
 
 def test_linear_loss_is_the_same_every_time():
