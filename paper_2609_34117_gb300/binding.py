@@ -9,6 +9,7 @@ path: without the built library every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 
@@ -598,16 +599,22 @@ def _rows_out(out, name, like, shape, index, stream):
     return out, args[0], args[4]
 
 
-def _scratch(workspace, size, args, what, stream, device):
-    """(workspace, pointer, bytes): the given one, or a new one in the stream's memory."""
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(name, *sizes) -> int:
+    """What slimwise_<name>_workspace_size answers (a call's sizes hardly change)."""
     n = ctypes.c_size_t(0)
-    _check(size(*args, ctypes.byref(n)), what)
+    _check(getattr(load(), f"slimwise_{name}_workspace_size")(*sizes, ctypes.byref(n)), f"slimwise_{name}")
+    return int(n.value)
+
+
+def _scratch(workspace, nbytes, stream, device):
+    """(workspace, pointer, bytes): the given one, or a new one in the stream's memory."""
     if workspace is None:
-        workspace = _new(stream, (n.value,), _U8, device)
-    else:
-        _dev(workspace, _U8, "workspace")
-        if workspace.device != device:
-            raise ValueError(f"workspace must be on {device}")
+        workspace = _new(stream, nbytes, _U8, device)
+        return workspace, workspace.data_ptr(), nbytes
+    _dev(workspace, _U8, "workspace")
+    if workspace.device != device:
+        raise ValueError(f"workspace must be on {device}")
     return workspace, workspace.data_ptr(), workspace.numel()
 
 
@@ -627,10 +634,7 @@ def slimwise_embed(table, ids, scale=1.0, out=None, stream=None):
 
 
 def slimwise_embed_grad_workspace_size(rows: int, hidden: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check(load().slimwise_embed_grad_workspace_size(rows, hidden, ctypes.byref(n)),
-           "slimwise_embed_grad_workspace_size")
-    return int(n.value)
+    return _workspace_bytes("embed_grad", rows, hidden)
 
 
 def slimwise_embed_grad(grad, ids, out, scale=1.0, accumulate=False, workspace=None, stream=None):
@@ -645,8 +649,7 @@ def slimwise_embed_grad(grad, ids, out, scale=1.0, accumulate=False, workspace=N
         raise ValueError(f"out must have rows of {hidden}, got {o_hidden}")
     p_ids = _vec(ids, _I32, (rows,), "ids", dev)
     lib = load()
-    workspace, w, n = _scratch(workspace, lib.slimwise_embed_grad_workspace_size, (rows, hidden),
-                               "slimwise_embed_grad", stream, grad.device)
+    workspace, w, n = _scratch(workspace, _workspace_bytes("embed_grad", rows, hidden), stream, grad.device)
     _check(lib.slimwise_embed_grad(ptr, code, rows, hidden, stride, p_ids, scale, o_ptr, o_code, vocab,
                                    o_stride, int(accumulate), _stream(stream), w, n), "slimwise_embed_grad")
     return out
@@ -675,10 +678,7 @@ def slimwise_norm(x, weight, bias=None, layer=False, eps=1e-5, y=None, mean=None
 
 
 def slimwise_norm_grad_workspace_size(rows: int, hidden: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check(load().slimwise_norm_grad_workspace_size(rows, hidden, ctypes.byref(n)),
-           "slimwise_norm_grad_workspace_size")
-    return int(n.value)
+    return _workspace_bytes("norm_grad", rows, hidden)
 
 
 def slimwise_norm_grad(dy, x, weight, rstd, mean=None, grad_bias=None, dx=None, dweight=None, dbias=None,
@@ -702,8 +702,7 @@ def slimwise_norm_grad(dy, x, weight, rstd, mean=None, grad_bias=None, dx=None, 
     if grad_bias and dbias is None:
         dbias = _new(stream, width, _F32, x.device)
     lib = load()
-    workspace, w, n = _scratch(workspace, lib.slimwise_norm_grad_workspace_size, (rows, hidden),
-                               "slimwise_norm_grad", stream, x.device)
+    workspace, w, n = _scratch(workspace, _workspace_bytes("norm_grad", rows, hidden), stream, x.device)
     _check(lib.slimwise_norm_grad(
         d[0], d[4], ptr, code, rows, hidden, stride, _vec(weight, _F32, width, "weight", dev),
         None if mean is None else _vec(mean, _F32, one, "mean", dev), _vec(rstd, _F32, one, "rstd", dev),
@@ -720,11 +719,7 @@ def slimwise_norm_grad(dy, x, weight, rstd, mean=None, grad_bias=None, dx=None, 
 
 def slimwise_linear_loss_workspace_size(rows: int, hidden: int, vocab: int, grad_hidden=True,
                                         grad_weight=True) -> int:
-    n = ctypes.c_size_t(0)
-    _check(load().slimwise_linear_loss_workspace_size(rows, hidden, vocab, int(bool(grad_hidden)),
-                                                      int(bool(grad_weight)), ctypes.byref(n)),
-           "slimwise_linear_loss_workspace_size")
-    return int(n.value)
+    return _workspace_bytes("linear_loss", rows, hidden, vocab, int(bool(grad_hidden)), int(bool(grad_weight)))
 
 
 def slimwise_linear_loss(hidden, weight, labels, row_weight=None, grad_hidden=True, grad_weight=True,
@@ -762,9 +757,8 @@ def slimwise_linear_loss(hidden, weight, labels, row_weight=None, grad_hidden=Tr
     if loss is None:
         loss = _new(stream, (1,), _F32, hidden.device)
     lib = load()
-    workspace, ws, n = _scratch(workspace, lib.slimwise_linear_loss_workspace_size,
-                                (rows, width, vocab, int(dh is not None), int(dw is not None)),
-                                "slimwise_linear_loss", stream, hidden.device)
+    workspace, ws, n = _scratch(workspace, _workspace_bytes("linear_loss", rows, width, vocab, int(dh is not None),
+                                                            int(dw is not None)), stream, hidden.device)
     _check(lib.slimwise_linear_loss(
         h_ptr, h_stride, w_ptr, w_stride, rows, width, vocab, p_labels, p_weight,
         _vec(row_loss, _F32, one, "row_loss", dev), _vec(loss, _F32, (1,), "loss", dev), dh_ptr, dh_stride,

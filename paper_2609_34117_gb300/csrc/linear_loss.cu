@@ -54,13 +54,16 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 // A warp's 32 rows x 64 columns of bf16 on their way out by TMA (128-byte swizzle).
 constexpr int kOutBytes = 32 * 128;
 constexpr int kEpiWarps = 8, kGemmThreads = 64 + 32 * kEpiWarps;
+// Warps of the dW product that meanwhile join dh's splits: memory work beside the
+// tensor cores' (join: the number of pairs that dh's product ran with, 0: none).
+constexpr int kJoinThreads = 128;
 constexpr int kMostPairs = kSms / 2;
 // Tiles of partial sums of dh: splits of the vocabulary are made while they fit.
 constexpr int kMostSplits = 96, kSplitTiles = 8 * kMostPairs;
 constexpr float kFloor = -FLT_MAX;  // stands in for -inf as a maximum
 
 enum Mode { kForward, kNumerators, kGradHidden, kGradWeight };
-enum Word { kLive = 0, kArrived = 1, kArrivedAgain = 2, kErr = kCtrlErr };
+enum Word { kLive = 0, kArrived = 1, kErr = kCtrlErr };
 
 struct Layout {
   int rows_pad, chunk, chunks, vocab_tiles, hidden_tiles, split_tiles;
@@ -181,7 +184,7 @@ __global__ void __launch_bounds__(1024) count_kernel(Call c) {
 // A warp a row: with a label, the row is copied to its place among those and its
 // label's logit computed (fp32 sums of a lane's products, then over the lanes);
 // without, it gets its results.
-__global__ void __launch_bounds__(kGatherThreads) gather_kernel(Call c, int counted) {
+__global__ void __launch_bounds__(kGatherThreads, 1) gather_kernel(Call c, int counted) {
   __shared__ int before_all, in_warp[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = blockIdx.x * kGatherRows, t = t0 + warp;
@@ -353,7 +356,7 @@ struct Work {
 };
 
 constexpr size_t kBars = (size_t)kStages * kStageBytes + kEpiWarps * kOutBytes;
-constexpr size_t kGemmSmem = kBars + 8 * (2 * kStages + 5) + 64 + 1024;
+constexpr size_t kGemmSmem = kBars + 8 * (2 * kStages + 5) + 64 + 1024;  // barriers, words, alignment
 
 // Sums of the columns' numerators and the P tile of 32 columns.
 template <Mode kMode>
@@ -395,9 +398,55 @@ __device__ __forceinline__ void numerators(const float (&z)[32], float ref, int 
   }
 }
 
+// The loss over all rows, by N threads of a CTA: thread i adds its rows i, i + N, ...
+// in fp64 and in order, then a butterfly and the warps in turn.  Rows without a label
+// stay out whatever their weights (1 / the number of labelled rows may be 1 / 0).
+template <int N>
+__device__ __forceinline__ void total_loss(const Call &c, int thread, double *warps) {
+  double s = 0.0;
+#pragma unroll 4
+  for (int t = thread; t < c.T; t += N) {
+    const double l = (double)__ldcg(c.row_loss + t) * (c.row_weight ? (double)__ldg(c.row_weight + t) : 1.0);
+    s += __ldg(c.labels + t) >= 0 ? l : 0.0;
+  }
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  if ((thread & 31) == 0) warps[thread / 32] = s;
+  asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
+  if (thread == 0) {
+    for (int w = 1; w < N / 32; ++w) s += warps[w];
+    *c.loss = (float)s;
+  }
+}
+
+// dh: the splits' sums of a row in order, times its factor; by `threads` threads, in
+// whole warps.
+__device__ __forceinline__ void join_rows(const Call &c, int chunk, int pairs, int64_t thread, int64_t threads) {
+  const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
+  if (rows == 0) return;
+  const int tiles = (rows + kTile - 1) / kTile * c.hidden_tiles;
+  const int splits = choose_splits(tiles, (c.V + kDepth - 1) / kDepth, pairs), words = c.H / 4;
+  const int64_t all = (int64_t)rows * words;
+  for (int64_t i = thread; i < all; i += threads) {
+    const int row = (int)(i / words), col = (int)(i - (int64_t)row * words) * 4;
+    const int tile = row / kTile * c.hidden_tiles + col / kTile;
+    const float *from = c.splits + ((int64_t)tile * kTile + row % kTile) * kTile + col % kTile;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) {
+      const float4 x = __ldcg(reinterpret_cast<const float4 *>(from));
+      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+      from += (int64_t)tiles * kTile * kTile;
+    }
+    const float f = __ldcg(c.scale + row0 + row);
+    __nv_bfloat16 *to = c.dh + (int64_t)__ldcg(c.orig + row0 + row) * c.dh_stride + col;
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0] * f, v[1] * f), pack_bf16(v[2] * f, v[3] * f));
+  }
+}
+
 template <Mode kMode>
-__global__ void __launch_bounds__(kGemmThreads, 1)
-    product_kernel(const __grid_constant__ Operands maps, Call c, int chunk, int again,
+__global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinThreads : 0), 1)
+    product_kernel(const __grid_constant__ Operands maps, Call c, int chunk, int again, int join,
                    uint64_t timeout_ns) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char *smem = reinterpret_cast<unsigned char *>(
@@ -414,15 +463,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   volatile int *abort = misc + 1;
   volatile int *consumed = misc + 2;
   volatile int *n_splits = misc + 3;
+  double *warp_totals = reinterpret_cast<double *>(misc + 4);  // kGradWeight
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t crank = cluster_ctarank();
   const bool lead = crank == 0;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
-  // The first product's second run has hardly ever anything to do: it looks first.
+  // (again: the first product's second run; dW's product behind the last chunk)
+  // The second run has hardly ever anything to do: it looks first.
   // All others get ready while the kernel before ends.
-  if (again) {
+  if (kMode == kNumerators && again) {
     pdl_wait_primary();
     if (__ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0) return;
   }
@@ -452,7 +503,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  if (!again) pdl_wait_primary();
+  if (kMode != kNumerators || !again) pdl_wait_primary();
   const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
   Work<kMode> work;
   work.list = nullptr;
@@ -488,8 +539,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       // no labelled row at all: zeros (16 bytes are 8 elements, or 4)
       const int words = c.H / (c.dw_fp32 ? 4 : 8);
       const int64_t all = (int64_t)c.V * words;
-      for (int64_t i = (int64_t)blockIdx.x * kGemmThreads + threadIdx.x; i < all;
-           i += (int64_t)gridDim.x * kGemmThreads) {
+      for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all;
+           i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t v = i / words, k = i - v * words;
         char *row = static_cast<char *>(c.dw) + v * c.dw_stride * (c.dw_fp32 ? 4 : 2);
         reinterpret_cast<uint4 *>(row)[k] = make_uint4(0, 0, 0, 0);
@@ -622,6 +673,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
     }
     __syncwarp();
+  } else if (warp >= 2 + kEpiWarps) {
+    // ------------------------------------------------------------ dh's splits
+    // and, behind the last chunk, the loss
+    if (join)
+      join_rows(c, chunk, join, (int64_t)blockIdx.x * kJoinThreads + (threadIdx.x - kGemmThreads),
+                (int64_t)gridDim.x * kJoinThreads);
+    if (again && c.loss && blockIdx.x == 0) total_loss<kJoinThreads>(c, (int)threadIdx.x - kGemmThreads, warp_totals);
   } else {
     // ------------------------------------------------------------ accumulators
     const int q = warp & 3, half = (warp - 2) >> 2;  // lanes 32 q.., columns 128 half..
@@ -731,12 +789,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 // 32 rows a CTA, a lane each; the column tiles' sums in 32 parts.  kForward: the
 // loss.  kNumerators: besides, the row's factor, the label's numerator and the
 // scaled row; `again`: only rows of the tiles that were run again (else a row whose
-// reference does not do marks its tile).  finish: the CTA that ends last adds up the
-// loss, in fp64 and in the order of the rows (the first run's, unless a tile is marked).
+// reference does not do marks its tile).
 template <Mode kMode>
-__global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again, int finish) {
+__global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int again, int finish) {
   __shared__ float part_sum[32][33], part_most[32][33];
-  __shared__ float row_scale[32];
   __shared__ double total[32];
   __shared__ int last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -744,13 +800,22 @@ __global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again
   pdl_launch_dependents();
   if (again && __ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0) return;
   const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
-  const int first = blockIdx.x * 32, row = first + lane;
-  const int tile = row0 / kTile + first / kTile;
+  const int first = blockIdx.x * 32, tile = row0 / kTile + first / kTile;
   const bool mine = first < (rows + kTile - 1) / kTile * kTile && (!again || __ldcg(c.flags + tile) != 0);
   if (mine) {
+    // a warp's row and what is known of it
+    const int row = first + warp, at = row0 + row;
+    const bool live = row < rows;
+    const float z = live ? __ldcg(c.target + at) : 0.0f;
+    float ref = live ? __ldcg(c.ref + at) : 0.0f;
+    const int t = live ? __ldcg(c.orig + at) : 0, y = live ? __ldcg(c.label + at) : -1;
+    const float weight = live && c.row_weight ? __ldg(c.row_weight + t) : 1.0f;
+    // a lane a row: every 32nd part
     float s = 0.0f, m = kFloor;
+    const float2 *part = c.sums + first + lane;
+#pragma unroll 8
     for (int i = warp; i < 2 * c.vocab_tiles; i += 32) {
-      const float2 v = __ldcg(c.sums + (int64_t)i * c.chunk + row);
+      const float2 v = __ldcg(part + (int64_t)i * c.chunk);
       if constexpr (kMode == kForward) {
         const float to = fmaxf(m, v.y);
         s = s * ex2((m - to) * kLog2e) + v.x * ex2((v.y - to) * kLog2e);
@@ -763,52 +828,42 @@ __global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again
     part_sum[warp][lane] = s;
     part_most[warp][lane] = m;
     __syncthreads();
-    if (warp == 0) {
-      const int at = row0 + row;
-      const bool live = row < rows;
-      const float z = live ? __ldcg(c.target + at) : 0.0f;
-      float ref = live ? __ldcg(c.ref + at) : 0.0f, S = 0.0f, top = kFloor;
-      for (int k = 0; k < 32; ++k) top = fmaxf(top, part_most[k][lane]);
-      if constexpr (kMode == kForward) {
-        ref = fmaxf(top, z);
-        if (z != z) ref = z;
-        for (int k = 0; k < 32; ++k) S += part_sum[k][lane] * ex2((part_most[k][lane] - ref) * kLog2e);
-      } else {
-        for (int k = 0; k < 32; ++k) S += part_sum[k][lane];
-      }
-      float scale = 0.0f;
-      if (live) {
-        const int t = __ldcg(c.orig + at);
-        if (kMode == kNumerators && !again && S > expf(kMostLoss) && top < INFINITY) {
-          c.ref[at] = top;
-          const int tiles = c.rows_pad / kTile;
-          if (atomicExch(c.flags + tile, 1) == 0)
-            c.flags[tiles + row0 / kTile + atomicAdd(c.flags + 2 * tiles + chunk, 1)] = tile - row0 / kTile;
-        }
-        const float own = ref == z ? 1.0f : ex2((z - ref) * kLog2e);
-        const float loss = ref == z ? log1pf(S) : (ref - z) + logf(own + S);
-        c.row_loss[t] = loss;
-        if constexpr (kMode == kNumerators) {
-          // -S is the largest numerator: its rounding goes into the row's factor, and so to
-          // the others, whose products with the operands mostly cancel
-          const __nv_bfloat16 least = __float2bfloat16_rn(-S);
-          const float ratio = S / -__bfloat162float(least);
-          scale = (c.row_weight ? __ldg(c.row_weight + t) : 1.0f) / (own + S) * (ratio > 0.5f && ratio < 2.0f ? ratio : 1.0f);
+    float S = part_sum[lane][warp], top = part_most[lane][warp];
+    const float mine_most = top;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if constexpr (kMode == kForward) {
+      ref = z != z ? z : fmaxf(top, z);
+      S *= ex2((mine_most - ref) * kLog2e);
+    }
+    S = warp_sum(S);
+    const float own = ref == z ? 1.0f : ex2((z - ref) * kLog2e);
+    float scale = 0.0f;
+    if (live) {
+      if constexpr (kMode == kNumerators) {
+        // -S is the largest numerator: its rounding goes into the row's factor, and so to
+        // the others, whose products with the operands mostly cancel
+        const __nv_bfloat16 least = __float2bfloat16_rn(-S);
+        const float ratio = S / -__bfloat162float(least);
+        scale = weight / (own + S) * (ratio > 0.5f && ratio < 2.0f ? ratio : 1.0f);
+        if (lane == 0) {
           c.scale[at] = scale;
-          const int y = __ldcg(c.label + at);
           if (y < c.V) c.cells[(int64_t)row * c.cells_stride + y] = least;
+          if (!again && S > expf(kMostLoss) && top < INFINITY) {
+            c.ref[at] = top;
+            const int tiles = c.rows_pad / kTile;
+            if (atomicExch(c.flags + tile, 1) == 0)
+              c.flags[tiles + row0 / kTile + atomicAdd(c.flags + 2 * tiles + chunk, 1)] = tile - row0 / kTile;
+          }
         }
       }
-      row_scale[lane] = scale;
+      if (lane == 0) c.row_loss[t] = ref == z ? log1pf(S) : (ref - z) + logf(own + S);
     }
     if constexpr (kMode == kNumerators) {
-      __syncthreads();
       if (c.scaled) {
-        const int r = first + warp;
-        const float scale = row_scale[warp];
-        const uint4 *from = reinterpret_cast<const uint4 *>(c.rows + (int64_t)(row0 + r) * c.H);
-        uint4 *to = reinterpret_cast<uint4 *>(c.scaled + (int64_t)r * c.H);
-        const bool live = r < rows;
+        const uint4 *from = reinterpret_cast<const uint4 *>(c.rows + (int64_t)at * c.H);
+        uint4 *to = reinterpret_cast<uint4 *>(c.scaled + (int64_t)row * c.H);
+#pragma unroll 4
         for (int k = lane; k < c.H / 8; k += 32) {
           uint4 v = live ? __ldcg(from + k) : make_uint4(0, 0, 0, 0);
           uint32_t *x = reinterpret_cast<uint32_t *>(&v);
@@ -821,59 +876,24 @@ __global__ void __launch_bounds__(1024) sums_kernel(Call c, int chunk, int again
     }
   }
   if (!finish || !c.loss) return;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0)
-    last = atomicAdd(c.ctrl + (again ? kArrivedAgain : kArrived), 1) == (int)gridDim.x - 1 &&
-           (again || __ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0);
-  __syncthreads();
-  if (!last) return;
-  __threadfence();
-  double s = 0.0;
-  for (int t = threadIdx.x; t < c.T; t += 1024) {
-    const double l = (double)__ldcg(c.row_loss + t) * (c.row_weight ? (double)__ldg(c.row_weight + t) : 1.0);
-    s += __ldg(c.labels + t) >= 0 ? l : 0.0;
-  }
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-  if (lane == 0) total[warp] = s;
+  // the forward pass: the CTA that ends last adds up the loss
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < 32; ++w) s += total[w];
-    *c.loss = (float)s;
-  }
-}
-
-// dh: the splits' sums of a row in order, times its factor.
-__global__ void __launch_bounds__(256) join_kernel(Call c, int chunk, int pairs) {
-  __shared__ int n_splits;
-  pdl_wait_primary();
-  pdl_launch_dependents();
-  const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
-  const int mt = (rows + kTile - 1) / kTile, tiles = mt * c.hidden_tiles;
-  if (rows == 0) return;
-  if (threadIdx.x < 32) {
-    const int s = choose_splits(tiles, (c.V + kDepth - 1) / kDepth, pairs);
-    if (threadIdx.x == 0) n_splits = s;
+    __threadfence();
+    last = atomicAdd(c.ctrl + kArrived, 1) == (int)gridDim.x - 1;
+    __threadfence();
   }
   __syncthreads();
-  const int splits = n_splits, words = c.H / 4;
-  const int64_t all = (int64_t)rows * words;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-    const int row = (int)(i / words), col = (int)(i - (int64_t)row * words) * 4;
-    const int tile = row / kTile * c.hidden_tiles + col / kTile;
-    const float *from = c.splits + ((int64_t)tile * kTile + row % kTile) * kTile + col % kTile;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-    for (int s = 0; s < splits; ++s) {
-      const float4 x = __ldcg(reinterpret_cast<const float4 *>(from));
-      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-      from += (int64_t)tiles * kTile * kTile;
-    }
-    const float f = __ldcg(c.scale + row0 + row);
-    __nv_bfloat16 *to = c.dh + (int64_t)__ldcg(c.orig + row0 + row) * c.dh_stride + col;
-    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0] * f, v[1] * f), pack_bf16(v[2] * f, v[3] * f));
-  }
+  if (last) total_loss<1024>(c, threadIdx.x, total);
+}
+
+// By itself where dW is not wanted.
+__global__ void __launch_bounds__(256, 1) join_kernel(Call c, int chunk, int pairs, int finish) {
+  __shared__ double warp_totals[8];
+  pdl_wait_primary();
+  pdl_launch_dependents();
+  if (finish && c.loss && blockIdx.x == 0) total_loss<256>(c, threadIdx.x, warp_totals);
+  join_rows(c, chunk, pairs, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 
 // ---------------------------------------------------------------------------
@@ -922,7 +942,7 @@ cudaError_t resident_pairs(int *pairs) {
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
-  cfg.blockDim = dim3(kGemmThreads);
+  cfg.blockDim = dim3(kGemmThreads + (kMode == kGradWeight ? kJoinThreads : 0));
   cfg.dynamicSmemBytes = kGemmSmem;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -940,14 +960,15 @@ cudaError_t resident_pairs(int *pairs) {
 }
 
 template <Mode kMode>
-cudaError_t run_product(const Operands &maps, const Call &c, int chunk, int again, cudaStream_t stream,
+cudaError_t run_product(const Operands &maps, const Call &c, int chunk, int again, int join, cudaStream_t stream,
                         int *used = nullptr) {
+  constexpr int kThreads = kGemmThreads + (kMode == kGradWeight ? kJoinThreads : 0);
   int pairs = 0;
   const cudaError_t err = resident_pairs<kMode>(&pairs);
   if (err != cudaSuccess) return err;
   if (used) *used = pairs;
-  return launch_chained(product_kernel<kMode>, dim3(2 * pairs), dim3(kGemmThreads), kGemmSmem, stream, 2,
-                        true, maps, c, chunk, again, kDefaultWaitLimitNs);
+  return launch_chained(product_kernel<kMode>, dim3(2 * pairs), dim3(kThreads), kGemmSmem, stream, 2,
+                        true, maps, c, chunk, again, join, kDefaultWaitLimitNs);
 }
 
 }  // namespace
@@ -1011,23 +1032,23 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
     const dim3 sum_grid((unsigned)(l.chunk / 32));
     const int finish = k == l.chunks - 1;
     if (!grad) {
-      err = run_product<kForward>(logits, c, k, 0, stream);
+      err = run_product<kForward>(logits, c, k, 0, 0, stream);
       if (err == cudaSuccess)
         err = launch_chained(sums_kernel<kForward>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, 0, finish);
       continue;
     }
     for (int again = 0; again < 2 && err == cudaSuccess; ++again) {
-      err = run_product<kNumerators>(logits, c, k, again, stream);
+      err = run_product<kNumerators>(logits, c, k, again, 0, stream);
       if (err == cudaSuccess)
-        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again, finish);
+        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again, 0);
     }
+    int pairs = 0;
     if (a.grad_hidden && err == cudaSuccess) {
-      int pairs = 0;
-      err = run_product<kGradHidden>(dh, c, k, 0, stream, &pairs);
-      if (err == cudaSuccess)
-        err = launch_chained(join_kernel, dim3(kSms * 8), dim3(256), 0, stream, 1, true, c, k, pairs);
+      err = run_product<kGradHidden>(dh, c, k, 0, 0, stream, &pairs);
+      if (err == cudaSuccess && !a.grad_weight)
+        err = launch_chained(join_kernel, dim3(kSms * 8), dim3(256), 0, stream, 1, true, c, k, pairs, finish);
     }
-    if (a.grad_weight && err == cudaSuccess) err = run_product<kGradWeight>(dw, c, k, 0, stream);
+    if (a.grad_weight && err == cudaSuccess) err = run_product<kGradWeight>(dw, c, k, finish, pairs, stream);
   }
   return err;
 }
