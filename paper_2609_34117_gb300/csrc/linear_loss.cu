@@ -49,8 +49,15 @@ constexpr int kTile = 256;       // rows and columns of a pair's tile
 constexpr int kHalf = 128;       // of a CTA's share of an operand
 constexpr int kDepth = 64;       // slice of the contraction: 128 bytes
 constexpr int kStages = 6;
+// Few rows: the products' roles change.  The vocabulary (for dh: the width) is M, which
+// fills the tensor cores' rows and the accumulators' lanes, and the rows are N, 64 or 128 of
+// them.  With rows as M, 64 of them took a whole tile's time, and the two warps that can
+// read their lanes did all of the epilogue.
+constexpr int kFewRows = 128;
 constexpr int kOperandBytes = kHalf * kDepth * 2;
 constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kFewStages = 8, kFewStageBytes = kOperandBytes + kFewRows / 2 * kDepth * 2;
+static_assert(kFewStages * kFewStageBytes == kStages * kStageBytes, "the ring's room");
 // A warp's 32 rows x 64 columns of bf16 on their way out by TMA (128-byte swizzle).
 constexpr int kOutBytes = 32 * 128;
 constexpr int kEpiWarps = 8, kGemmThreads = 64 + 32 * kEpiWarps;
@@ -112,7 +119,7 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
   l.flags = take(n / kTile * 3 * 4);
   l.rows = take(n * hidden * 2);
   l.scaled = take(grad_weight ? (size_t)l.chunk * hidden * 2 : 0);
-  l.sums = take((size_t)l.vocab_tiles * 2 * l.chunk * sizeof(float2));
+  l.sums = take((size_t)(rows <= kFewRows ? kMostPairs * 8 : l.vocab_tiles * 2) * l.chunk * sizeof(float2));
   l.cells = take(grad ? (size_t)l.chunk * l.cells_stride * 2 : 0);
   l.splits = take((size_t)l.split_tiles * kTile * kTile * 4);
   l.acc = take(grad_weight && l.chunks > 1 ? (size_t)vocab * hidden * 4 : 0);
@@ -130,7 +137,7 @@ struct Call {
   int32_t *flags;  // [3][rows_pad / 256]: tiles to run again; their list; each chunk's number of them
   float *target, *ref, *scale;
   __nv_bfloat16 *rows, *scaled, *cells;
-  float2 *sums;   // [2 vocab_tiles][chunk]: sum of numerators, largest logit
+  float2 *sums;   // [2 vocab_tiles, or 8 a pair][chunk]: sum of numerators, largest logit
   float *splits;  // [tiles][256][256]
   float *acc;     // [V][H], more than one chunk
   const __nv_bfloat16 *hidden, *weight;
@@ -356,7 +363,9 @@ struct Work {
 };
 
 constexpr size_t kBars = (size_t)kStages * kStageBytes + kEpiWarps * kOutBytes;
-constexpr size_t kGemmSmem = kBars + 8 * (2 * kStages + 5) + 64 + 1024;  // barriers, words, alignment
+// barriers, words, the few rows' references and labels, alignment
+constexpr int kWords = 8 * (2 * kFewStages + 5);
+constexpr size_t kGemmSmem = kBars + kWords + 64 + kFewRows * 8 + 1024;
 
 // Sums of the columns' numerators and the P tile of 32 columns.
 template <Mode kMode>
@@ -396,6 +405,53 @@ __device__ __forceinline__ void numerators(const float (&z)[32], float ref, int 
     }
     sum += (s[0] + s[1]) + (s[2] + s[3]);
   }
+}
+
+__device__ __forceinline__ float warp_max_redux(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// 32 values of each lane reduced over the lanes: lane j gets value j's result.
+template <typename F>
+__device__ __forceinline__ float reduce_across(float (&x)[32], int lane, F op) {
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) {
+    const bool hi = (lane & o) != 0;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float other = __shfl_xor_sync(0xFFFFFFFFu, hi ? x[i] : x[i + o], o);
+      x[i] = op(hi ? x[i + o] : x[i], other);
+    }
+  }
+  return x[0];
+}
+
+// Few rows: 32 rows' logits z at the lane's word.  Leaves their numerators in bf16 at
+// `staged` (64 bytes a row, zeros for rows past `live`), and returns to lane j row j's
+// sum over the warp's words and largest logit.
+template <Mode kMode>
+__device__ __forceinline__ float2 few_numerators(float (&z)[32], const float *ref, const int *label, int word,
+                                                 bool known, int live, int lane, uint32_t staged) {
+  float top = kFloor;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const bool in = known && word != label[j];
+    const float most = warp_max_redux(in ? z[j] : kFloor);
+    if (lane == j) top = most;
+    const float r = kMode == kForward ? most : ref[j];
+    const float e = ex2((z[j] - r) * kLog2e);
+    if constexpr (kMode == kNumerators) {
+      const __nv_bfloat16 h = __float2bfloat16_rn(j < live ? e : 0.0f);
+      asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged + (uint32_t)(j * 64 + lane * 2)),
+                   "h"(*reinterpret_cast<const unsigned short *>(&h))
+                   : "memory");
+    }
+    z[j] = in ? e : 0.0f;
+  }
+  const float sum = reduce_across(z, lane, [](float a, float b) { return a + b; });
+  return make_float2(sum, top);
 }
 
 // The loss over all rows, by N threads of a CTA: thread i adds its rows i, i + N, ...
@@ -444,7 +500,7 @@ __device__ __forceinline__ void join_rows(const Call &c, int chunk, int pairs, i
   }
 }
 
-template <Mode kMode>
+template <Mode kMode, bool kFew>
 __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinThreads : 0), 1)
     product_kernel(const __grid_constant__ Operands maps, Call c, int chunk, int again, int join,
                    uint64_t timeout_ns) {
@@ -453,17 +509,22 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t smem_base = smem_u32(smem);
   const uint32_t bar0 = smem_base + (uint32_t)kBars;
+  constexpr int kRing = kFew ? kFewStages : kStages;
+  constexpr int kSlot = kFew ? kFewStageBytes : kStageBytes;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
-  auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
-  auto accf_bar = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
-  auto acce_bar = [&](int b) { return bar0 + 8u * (2 * kStages + 2 + b); };
-  const uint32_t drain_bar = bar0 + 8u * (2 * kStages + 4);
-  int *misc = reinterpret_cast<int *>(smem + kBars + 8 * (2 * kStages + 5));
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kRing + s); };
+  auto accf_bar = [&](int b) { return bar0 + 8u * (2 * kRing + b); };
+  auto acce_bar = [&](int b) { return bar0 + 8u * (2 * kRing + 2 + b); };
+  const uint32_t drain_bar = bar0 + 8u * (2 * kRing + 4);
+  int *misc = reinterpret_cast<int *>(smem + kBars + kWords);
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(misc);
   volatile int *abort = misc + 1;
   volatile int *consumed = misc + 2;
   volatile int *n_splits = misc + 3;
   double *warp_totals = reinterpret_cast<double *>(misc + 4);  // kGradWeight
+  float *few_ref = reinterpret_cast<float *>(misc + 16);
+  int *few_label = reinterpret_cast<int *>(few_ref + kFewRows);
+  const int few = c.T <= kFewRows / 2 ? kFewRows / 2 : kFewRows;  // N
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t crank = cluster_ctarank();
@@ -478,7 +539,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     if (__ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0) return;
   }
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < kRing; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
     }
@@ -492,7 +553,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     mbar_fence_init();
     tma_prefetch_desc(&maps.a);
     tma_prefetch_desc(&maps.b);
-    if constexpr (kMode == kNumerators || kMode == kGradWeight) tma_prefetch_desc(&maps.out);
+    if constexpr (kMode == kNumerators && !kFew) tma_prefetch_desc(&maps.out);
   }
   if (warp == 1) {
     tmem_alloc_pair(smem_u32((const void *)tmem_slot), 512);
@@ -519,6 +580,13 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       work.list = c.flags + tiles + row0 / kTile;
     }
     work.units = work.mt * work.nt;
+    if constexpr (kFew) {
+      for (int i = threadIdx.x; i < few; i += blockDim.x) {
+        few_ref[i] = i < rows ? __ldcg(c.ref + i) : 0.0f;
+        few_label[i] = i < rows ? __ldcg(c.label + i) : -1;
+      }
+      __syncthreads();
+    }
   } else if constexpr (kMode == kGradHidden) {
     work.mt = (rows + kTile - 1) / kTile;
     work.nt = c.hidden_tiles;
@@ -562,29 +630,32 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     return __all_sync(0xFFFFFFFFu, ok) != 0;
   };
   // operands along the contraction (K-major) or across it
-  constexpr bool kAcrossA = kMode == kGradWeight;
-  constexpr bool kAcrossB = kMode == kGradHidden || kMode == kGradWeight;
+  constexpr bool kAcrossA = kMode == kGradWeight || (kFew && kMode == kGradHidden);
+  constexpr bool kAcrossB = kMode == kGradWeight || (!kFew && kMode == kGradHidden);
 
   if (warp == 0) {
     // ------------------------------------------------------------ copies
     int stage = 0, issued = 0;
     uint32_t phase = 0;
     const uint64_t policy = l2_policy_evict_last();
+    fence_proxy_async_global();  // what the kernels before stored is read by TMA
     bool ok = true;
     for (int u = pair; u < work.units && ok; u += pairs) {
       const Unit w = work.at(u);
       // first row (column) of this CTA's share of either operand
-      const int a0 = (kMode == kForward || kMode == kNumerators ? row0 : 0) + w.m * kTile + (int)crank * kHalf;
-      const int b0 = w.n * kTile + (int)crank * kHalf;
+      const bool logits = kMode == kForward || kMode == kNumerators;
+      const int a0 = (kFew ? w.n * kTile : (logits ? row0 : 0) + w.m * kTile) + (int)crank * kHalf;
+      const int b0 = kFew ? (int)crank * few / 2 : w.n * kTile + (int)crank * kHalf;
       for (int k = w.k0; k < w.k1; ++k) {
         if (!all_ok(mbar_wait_bounded(empty_bar(stage), phase ^ 1u, abort, timeout_ns))) {
           ok = false;
           break;
         }
-        const uint32_t a = smem_base + (uint32_t)(stage * kStageBytes), b = a + kOperandBytes;
+        const uint32_t a = smem_base + (uint32_t)(stage * kSlot), b = a + kOperandBytes;
         if (elect_one()) {
           const uint32_t bar = mapa_shared(full_bar(stage), 0u);
-          if (lead) mbar_arrive_expect_tx(full_bar(stage), 2 * kStageBytes);
+          if (lead)
+            mbar_arrive_expect_tx(full_bar(stage), kFew ? 2 * kOperandBytes + few * kDepth * 2 : 2 * kStageBytes);
           if constexpr (kAcrossA) {
             tma_load_2d_pair(a, &maps.a, bar, a0, k * kDepth, policy);
             tma_load_2d_pair(a + kOperandBytes / 2, &maps.a, bar, a0 + 64, k * kDepth, policy);
@@ -600,7 +671,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
         }
         __syncwarp();
         ++issued;
-        if (++stage == kStages) {
+        if (++stage == kRing) {
           stage = 0;
           phase ^= 1u;
         }
@@ -611,13 +682,13 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       // until every stage still in the ring has been released (or, in the first
       // CTA after an abort, its copies have landed): nothing is left on its way
       // to this CTA's shared memory when it exits
-      const int from = issued > kStages ? issued - kStages : 0;
+      const int from = issued > kRing ? issued - kRing : 0;
       if (*abort && lead) {
         for (int s = *consumed > from ? *consumed : from; s < issued; ++s)
-          mbar_wait_timeout(full_bar(s % kStages), (uint32_t)((s / kStages) & 1), 10000000ull);
+          mbar_wait_timeout(full_bar(s % kRing), (uint32_t)((s / kRing) & 1), 10000000ull);
       } else {
         for (int s = from; s < issued; ++s)
-          mbar_wait_timeout(empty_bar(s % kStages), (uint32_t)((s / kStages) & 1), 10000000ull);
+          mbar_wait_timeout(empty_bar(s % kRing), (uint32_t)((s / kRing) & 1), 10000000ull);
       }
     }
     __syncwarp();
@@ -626,7 +697,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     if (lead) {
       int stage = 0, local = 0, n_consumed = 0;
       uint32_t phase = 0;
-      const uint32_t idesc = idesc_bf16_f32(kTile, kTile) | (kAcrossA ? 1u << 15 : 0u) |
+      const uint32_t idesc = idesc_bf16_f32(kTile, kFew ? few : kTile) | (kAcrossA ? 1u << 15 : 0u) |
                              (kAcrossB ? 1u << 16 : 0u);
       bool ok = true;
       for (int u = pair; u < work.units && ok; u += pairs, ++local) {
@@ -643,7 +714,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
             break;
           }
           tc_fence_after();
-          const uint32_t as = smem_base + (uint32_t)(stage * kStageBytes), bs = as + kOperandBytes;
+          const uint32_t as = smem_base + (uint32_t)(stage * kSlot), bs = as + kOperandBytes;
           ++n_consumed;
           if (elect_one()) {
 #pragma unroll
@@ -658,7 +729,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
             *consumed = n_consumed;
           }
           __syncwarp();
-          if (++stage == kStages) {
+          if (++stage == kRing) {
             stage = 0;
             phase ^= 1u;
           }
@@ -685,6 +756,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     const int q = warp & 3, half = (warp - 2) >> 2;  // lanes 32 q.., columns 128 half..
     const int in_tile = (int)crank * kHalf + 32 * q + lane;
     const OutBuffer out = {smem_base + (uint32_t)(kStages * kStageBytes + (warp - 2) * kOutBytes)};
+    float2 few_sums[2] = {make_float2(0.0f, kFloor), make_float2(0.0f, kFloor)};  // of the pair's tiles
     int local = 0;
     for (int u = pair; u < work.units; u += pairs, ++local) {
       const Unit w = work.at(u);
@@ -696,9 +768,58 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       auto release = [&]() {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(mapa_shared(acce_bar(b), 0u));
+        // (relaxed: what it hands over is tensor memory, ordered by the fence above; a release
+        // would wait for the tile before's stores)
+        if (lane == 0)
+          asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                           mapa_shared(acce_bar(b), 0u))
+                       : "memory");
       };
-      if constexpr (kMode == kForward || kMode == kNumerators) {
+      if constexpr (kFew) {
+        // this lane's word of the vocabulary (dh: column), all rows
+        const int mine = w.n * kTile + in_tile;
+        const uint32_t lanes = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(b * kTile);
+#pragma unroll 1
+        for (int t0 = half * (few / 2); t0 < (half + 1) * (few / 2); t0 += 32) {
+          float z[32];
+          tmem_ld_row(lanes + t0, z);
+          tmem_ld_wait();
+          if (t0 + 32 == (half + 1) * (few / 2)) release();
+          if constexpr (kMode == kGradHidden) {
+            float *to = c.splits + ((int64_t)u * kTile + t0) * kTile + in_tile;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (t0 + j < rows) to[j * kTile] = z[j];
+          } else {
+            const float2 sums = few_numerators<kMode>(z, few_ref + t0, few_label + t0, mine, mine < c.V, rows - t0,
+                                                      lane, out.at + (uint32_t)(t0 - half * (few / 2)) * 64);
+            float2 &kept = t0 == half * (few / 2) ? few_sums[0] : few_sums[1];
+            const float top = fmaxf(kept.y, sums.y);
+            if constexpr (kMode == kForward)
+              kept.x = kept.x * ex2((kept.y - top) * kLog2e) + sums.x * ex2((sums.y - top) * kLog2e);
+            else
+              kept.x += sums.x;
+            kept.y = top;
+          }
+        }
+        if constexpr (kMode == kNumerators) {
+          // the warp's 32 words of each row, 64 bytes
+          __syncwarp();
+          const int first = w.n * kTile + (int)crank * kHalf + 32 * q;
+          for (int i = lane; i < few / 2 * 4; i += 32) {
+            const int v = first + (i & 3) * 8;
+            const uint4 x = ld_shared_v4(out.at + (uint32_t)i * 16);
+            if (v < c.cells_stride)
+              *reinterpret_cast<uint4 *>(c.cells + (int64_t)(half * (few / 2) + (i >> 2)) * c.cells_stride + v) = x;
+          }
+          __syncwarp();
+        }
+      } else if constexpr (kMode == kForward || kMode == kNumerators) {
+        // nothing reads what rows past the last one, rounded up to dW's slices, would leave
+        if (row - lane >= (rows + kDepth - 1) / kDepth * kDepth) {
+          release();
+          continue;
+        }
         const bool live = row < rows;
         const float ref = live ? __ldcg(c.ref + row0 + row) : 0.0f;
         const int label = live ? __ldcg(c.label + row0 + row) : -1;
@@ -724,6 +845,10 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
         }
         c.sums[(int64_t)(w.n * 2 + half) * c.chunk + row] = make_float2(sum, most);
       } else if constexpr (kMode == kGradHidden) {
+        if (row - lane >= rows) {
+          release();
+          continue;
+        }
         float *to = c.splits + ((int64_t)u * kTile + in_tile) * kTile + half * kHalf;
 #pragma unroll 1
         for (int k = 0; k < kHalf / 32; ++k) {
@@ -772,6 +897,14 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       }
     }
     out.finish(lane);
+    if constexpr (kFew && kMode != kGradHidden) {
+      if (pair < work.units)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int t = half * (few / 2) + 32 * k + lane;
+          if (32 * k < few / 2 && t < rows) c.sums[(int64_t)((pair * 2 + (int)crank) * 4 + q) * c.chunk + t] = few_sums[k];
+        }
+    }
   }
 
   tc_fence_before();
@@ -789,9 +922,10 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
 // 32 rows a CTA, a lane each; the column tiles' sums in 32 parts.  kForward: the
 // loss.  kNumerators: besides, the row's factor, the label's numerator and the
 // scaled row; `again`: only rows of the tiles that were run again (else a row whose
-// reference does not do marks its tile).
+// reference does not do marks its tile).  pairs: those that the few rows' product ran
+// with (its sums are a pair's), else 0.
 template <Mode kMode>
-__global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int again, int finish) {
+__global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int again, int finish, int pairs) {
   __shared__ float part_sum[32][33], part_most[32][33];
   __shared__ double total[32];
   __shared__ int last;
@@ -811,10 +945,11 @@ __global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int ag
     const int t = live ? __ldcg(c.orig + at) : 0, y = live ? __ldcg(c.label + at) : -1;
     const float weight = live && c.row_weight ? __ldg(c.row_weight + t) : 1.0f;
     // a lane a row: every 32nd part
+    const int parts = pairs ? min(c.vocab_tiles, pairs) * 8 : c.vocab_tiles * 2;
     float s = 0.0f, m = kFloor;
     const float2 *part = c.sums + first + lane;
 #pragma unroll 8
-    for (int i = warp; i < 2 * c.vocab_tiles; i += 32) {
+    for (int i = warp; i < parts; i += 32) {
       const float2 v = __ldcg(part + (int64_t)i * c.chunk);
       if constexpr (kMode == kForward) {
         const float to = fmaxf(m, v.y);
@@ -930,14 +1065,14 @@ bool encode(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int6
 
 // Pairs that run at once (their CTAs' SMs lie in one cluster's reach); readies the
 // kernel on the current device.
-template <Mode kMode>
+template <Mode kMode, bool kFew>
 cudaError_t resident_pairs(int *pairs) {
   static std::atomic<int> known[64];
   int dev = 0;
   cudaError_t err = cudaGetDevice(&dev);
   if (err != cudaSuccess) return err;
   if (dev < 64 && (*pairs = known[dev].load(std::memory_order_acquire)) > 0) return cudaSuccess;
-  auto kernel = product_kernel<kMode>;
+  auto kernel = product_kernel<kMode, kFew>;
   err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmSmem);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
@@ -959,15 +1094,15 @@ cudaError_t resident_pairs(int *pairs) {
   return cudaSuccess;
 }
 
-template <Mode kMode>
+template <Mode kMode, bool kFew = false>
 cudaError_t run_product(const Operands &maps, const Call &c, int chunk, int again, int join, cudaStream_t stream,
                         int *used = nullptr) {
   constexpr int kThreads = kGemmThreads + (kMode == kGradWeight ? kJoinThreads : 0);
   int pairs = 0;
-  const cudaError_t err = resident_pairs<kMode>(&pairs);
+  const cudaError_t err = resident_pairs<kMode, kFew>(&pairs);
   if (err != cudaSuccess) return err;
   if (used) *used = pairs;
-  return launch_chained(product_kernel<kMode>, dim3(2 * pairs), dim3(kThreads), kGemmSmem, stream, 2,
+  return launch_chained(product_kernel<kMode, kFew>, dim3(2 * pairs), dim3(kThreads), kGemmSmem, stream, 2,
                         true, maps, c, chunk, again, join, kDefaultWaitLimitNs);
 }
 
@@ -1009,14 +1144,18 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
 
   Operands logits = {}, dh = {}, dw = {};
   // (rows past the call's are zeros without being read)
-  bool ok = encode(&logits.a, c.rows, c.T, c.H, c.H, kHalf) &&
-            encode(&logits.b, c.weight, c.V, c.H, c.weight_stride, kHalf);
-  if (grad) ok = ok && encode(&logits.out, c.cells, l.chunk, l.cells_stride, l.cells_stride, 32);
+  const bool few = c.T <= kFewRows;
+  const int few_half = (c.T <= kFewRows / 2 ? kFewRows / 2 : kFewRows) / 2;  // a CTA's rows of N
+  bool ok = encode(few ? &logits.b : &logits.a, c.rows, c.T, c.H, c.H, few ? few_half : kHalf) &&
+            encode(few ? &logits.a : &logits.b, c.weight, c.V, c.H, c.weight_stride, kHalf);
+  if (grad && !few) ok = ok && encode(&logits.out, c.cells, l.chunk, l.cells_stride, l.cells_stride, 32);
+  // (rows of the numerators past the call's, rounded up to dW's slices, are never written)
+  const int cell_rows = ceil_div(c.T, kDepth) * kDepth < l.chunk ? ceil_div(c.T, kDepth) * kDepth : l.chunk;
   if (a.grad_hidden)  // e along the vocabulary, the head across it
-    ok = ok && encode(&dh.a, c.cells, l.chunk, c.V, l.cells_stride, kHalf) &&
-         encode(&dh.b, c.weight, c.V, c.H, c.weight_stride, kDepth);
+    ok = ok && encode(few ? &dh.b : &dh.a, c.cells, cell_rows, c.V, l.cells_stride, few ? few_half : kHalf) &&
+         encode(few ? &dh.a : &dh.b, c.weight, c.V, c.H, c.weight_stride, kDepth);
   if (a.grad_weight)  // both across the rows
-    ok = ok && encode(&dw.a, c.cells, l.chunk, c.V, l.cells_stride, kDepth) &&
+    ok = ok && encode(&dw.a, c.cells, cell_rows, c.V, l.cells_stride, kDepth) &&
          encode(&dw.b, c.scaled, l.chunk, c.H, c.H, kDepth) &&
          (c.dw_fp32 || encode(&dw.out, c.dw, c.V, c.H, c.dw_stride, 32));
   if (!ok) return cudaErrorInvalidValue;
@@ -1031,20 +1170,24 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   for (int k = 0; k < l.chunks && err == cudaSuccess; ++k) {
     const dim3 sum_grid((unsigned)(l.chunk / 32));
     const int finish = k == l.chunks - 1;
+    int used = 0;
     if (!grad) {
-      err = run_product<kForward>(logits, c, k, 0, 0, stream);
+      err = few ? run_product<kForward, true>(logits, c, k, 0, 0, stream, &used)
+                : run_product<kForward>(logits, c, k, 0, 0, stream);
       if (err == cudaSuccess)
-        err = launch_chained(sums_kernel<kForward>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, 0, finish);
+        err = launch_chained(sums_kernel<kForward>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, 0, finish, used);
       continue;
     }
     for (int again = 0; again < 2 && err == cudaSuccess; ++again) {
-      err = run_product<kNumerators>(logits, c, k, again, 0, stream);
+      err = few ? run_product<kNumerators, true>(logits, c, k, again, 0, stream, &used)
+                : run_product<kNumerators>(logits, c, k, again, 0, stream);
       if (err == cudaSuccess)
-        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again, 0);
+        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again, 0, used);
     }
     int pairs = 0;
     if (a.grad_hidden && err == cudaSuccess) {
-      err = run_product<kGradHidden>(dh, c, k, 0, 0, stream, &pairs);
+      err = few ? run_product<kGradHidden, true>(dh, c, k, 0, 0, stream, &pairs)
+                : run_product<kGradHidden>(dh, c, k, 0, 0, stream, &pairs);
       if (err == cudaSuccess && !a.grad_weight)
         err = launch_chained(join_kernel, dim3(kSms * 8), dim3(256), 0, stream, 1, true, c, k, pairs, finish);
     }

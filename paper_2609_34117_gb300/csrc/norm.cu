@@ -15,6 +15,8 @@
 // The gradient of the weight: a thread keeps the same columns for all rows of
 // its CTA, so dg and db stay in its registers (32 columns of a thread: in shared
 // memory) until the CTA's last row; a second kernel adds the CTAs' sums in order.
+#include <type_traits>
+
 #include "train.cuh"
 
 namespace slimwise {
@@ -47,8 +49,16 @@ __device__ __forceinline__ void group_sum(float (&v)[K], float *buf, int &turn) 
   }
 }
 
+// Group g's barrier.
+template <int TPR>
+__device__ __forceinline__ void group_barrier(int g) {
+  if constexpr (TPR == 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "n"(TPR) : "memory");
+}
+
 struct NormArgs {
   int rows, hidden;
+  Extent x;
   int64_t stride, y_stride;
   const float *weight, *bias;
   float eps;
@@ -64,16 +74,18 @@ struct NormArgs {
 constexpr int kNormThreads = 256;
 template <int TPR>
 constexpr int kNormBlock = TPR > kNormThreads ? TPR : kNormThreads;
-template <typename T, int N>
-constexpr int kNormRows = N * (int)sizeof(T) >= 64 ? 1 : 64 / (N * (int)sizeof(T)) > 2 ? 2 : 64 / (N * (int)sizeof(T));
+template <typename T, bool kAny, int N>
+constexpr int kNormRows = kAny ? 1 : N * (int)sizeof(T) >= 64 ? 1 : 64 / (N * (int)sizeof(T)) > 2 ? 2 : 64 / (N * (int)sizeof(T));
 
-template <typename T, int V, int TPR, int N, bool kLayer>
+template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     norm_kernel(const T *__restrict__ x, NormArgs a, T *__restrict__ y) {
-  constexpr int R = kNormRows<T, N>, P = N / V, W = TPR / 32, kGroups = kNormBlock<TPR> / TPR;
+  constexpr int R = kNormRows<T, kAny, N>, P = N / V, W = TPR / 32, kGroups = kNormBlock<TPR> / TPR;
   constexpr bool kHeld = N <= 16;
   using Part = RowPart<T, V, N>;
   __shared__ float2 buf[TPR > 32 ? 2 * R * kNormBlock<TPR> / 32 : 1];
+  constexpr int kStaged = staged_elements<T>(TPR * N);
+  __shared__ __align__(16) unsigned char rows_out[kAny ? kGroups * R * kStaged * sizeof(T) : 16];
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv = 1.0f / (float)a.hidden;
   // columns of this warp, and of the warp whose sums this lane joins
@@ -96,19 +108,36 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
       g[e / 2] = pair(a.weight, e);
       o[e / 2] = pair(a.bias, e);
     }
-  auto fetch = [&](Part (&p)[R], int64_t r0) {
+  using Coming = typename std::conditional<kAny, Windows<T, kAny ? N : 16 / sizeof(T)>, Part>::type;
+  auto fetch = [&](Coming (&p)[R], int64_t r0) {
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-      p[i].load(x + (r0 + i < a.rows ? r0 + i : 0) * a.stride, t, TPR, r0 + i < a.rows ? a.hidden : 0);
+    for (int i = 0; i < R; ++i) {
+      const T *row = x + (r0 + i < a.rows ? r0 + i : 0) * a.stride;
+      const int width = r0 + i < a.rows ? a.hidden : 0;
+      if constexpr (kAny) p[i].load(row, t, TPR, width, a.x);
+      else p[i].load(row, t, TPR, width);
+    }
+  };
+  auto arrive = [&](Part (&p)[R], const Coming (&next)[R]) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if constexpr (kAny) p[i].take(next[i], t, TPR, a.hidden);
+      else p[i] = next[i];
+    }
   };
   const int64_t step = (int64_t)gridDim.x * kGroups * R;
   int64_t r0 = ((int64_t)blockIdx.x * kGroups + group) * R;
   int turn = 0;
-  Part p[R], next[kHeld ? R : 1];
-  if (kHeld && r0 < a.rows) fetch(p, r0);
+  T *staged = reinterpret_cast<T *>(rows_out) + (kAny ? group * R * kStaged : 0);
+  Part p[R];
+  Coming next[R];
+  if (kHeld && r0 < a.rows) {
+    fetch(next, r0);
+    arrive(p, next);
+  }
   for (; r0 < a.rows; r0 += step) {
-    if constexpr (kHeld) fetch(next, r0 + step);
-    else fetch(p, r0);
+    fetch(next, kHeld ? r0 + step : r0);
+    if constexpr (!kHeld) arrive(p, next);
     float mu[R], q[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -186,16 +215,24 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
         if constexpr (kHeld) p[i].set2(e, fma2(mul2(v, f), g[e / 2], o[e / 2]));
         else p[i].set2(e, fma2(mul2(v, f), pair(a.weight, e), pair(a.bias, e)));
       }
-      p[i].store(y + (r0 + i) * a.y_stride, t, TPR, a.hidden);
+      if constexpr (kAny) p[i].stage(staged + i * kStaged, t, TPR, a.hidden);
+      else p[i].store(y + (r0 + i) * a.y_stride, t, TPR, a.hidden);
     }
-    if constexpr (kHeld)
+    if constexpr (kAny) {
+      group_barrier<TPR>(group);
 #pragma unroll
-      for (int i = 0; i < R; ++i) p[i] = next[i];
+      for (int i = 0; i < R; ++i)
+        if (r0 + i < a.rows) store_any(staged + i * kStaged, y + (r0 + i) * a.y_stride, t, TPR, a.hidden);
+      // (the next rows are staged behind the barrier of their sums, or a warp's own)
+      if constexpr (TPR == 32) __syncwarp();
+    }
+    if constexpr (kHeld) arrive(p, next);
   }
 }
 
 struct GradArgs {
   int rows, hidden;
+  Extent dy, x;
   int64_t dy_stride, stride, dx_stride;
   const float *weight, *mean, *rstd;
   float *partial;  // [CTAs][kLayer ? 2 : 1][hidden]
@@ -211,10 +248,11 @@ constexpr int kBlock = TPR == 32 ? 32 * kWarpRows : TPR;
 // hold both.
 template <typename T, int N>
 constexpr int kBatch = N * (int)sizeof(T) >= 32 ? 1 : 32 / (N * (int)sizeof(T));
+// (windows take twice the registers on their way)
 template <int N>
 constexpr bool kAhead = N < 32;
 
-template <typename T, int V, int TPR, int N, bool kLayer>
+template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     norm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ x, GradArgs a,
                      T *__restrict__ dx) {
@@ -222,16 +260,24 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
   constexpr int kGroups = kBlock<TPR> / TPR;
   constexpr bool kShared = N >= 32;  // dg, db in shared memory; the weight is read for each row
   using Part = RowPart<T, V, N>;
+  using Coming = typename std::conditional<kAny, Windows<T, kAny ? N : 16 / sizeof(T)>, Part>::type;
   struct Batch {
     Part d[R], x[R];
     float mu[R], rs[R];
   };
+  struct ComingBatch {
+    Coming d[R], x[R];
+    float mu[R], rs[R];
+  };
   __shared__ float buf[2 * K * (TPR / 32)];
+  constexpr int kStaged = staged_elements<T>(TPR * N);
+  __shared__ __align__(16) unsigned char rows_out[kAny ? kGroups * R * kStaged * sizeof(T) : 16];
   // kShared: dg [N][TPR], db [N][TPR]; groups of a warp: one group's sums
   extern __shared__ __align__(16) float held[];
   int turn = 0;
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv = 1.0f / (float)a.hidden;
+  T *staged = reinterpret_cast<T *>(rows_out) + (kAny ? group * R * kStaged : 0);
   auto read_weight = [&](int e) {
     const int c = Part::column(e, t, TPR), c1 = Part::column(e + 1, t, TPR);
     return f2(c < a.hidden ? __ldg(a.weight + c) : 0.0f, c1 < a.hidden ? __ldg(a.weight + c1) : 0.0f);
@@ -251,24 +297,47 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     if constexpr (!kShared) return g[e / 2];
     else return read_weight(e);
   };
-  auto fetch = [&](Batch &b, int r0) {
+  auto fetch = [&](ComingBatch &b, int r0) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const bool in = r0 + i < a.rows;
       const int64_t r = in ? r0 + i : 0;
-      b.d[i].load(dy + r * a.dy_stride, t, TPR, in ? a.hidden : 0);
-      b.x[i].load(x + r * a.stride, t, TPR, in ? a.hidden : 0);
+      if constexpr (kAny) {
+        b.d[i].load(dy + r * a.dy_stride, t, TPR, in ? a.hidden : 0, a.dy);
+        b.x[i].load(x + r * a.stride, t, TPR, in ? a.hidden : 0, a.x);
+      } else {
+        b.d[i].load(dy + r * a.dy_stride, t, TPR, in ? a.hidden : 0);
+        b.x[i].load(x + r * a.stride, t, TPR, in ? a.hidden : 0);
+      }
       b.rs[i] = in ? __ldg(a.rstd + r) : 0.0f;
       b.mu[i] = kLayer && in ? __ldg(a.mean + r) : 0.0f;
     }
   };
   const int step = gridDim.x * kGroups * R;
   int r0 = (blockIdx.x * kGroups + group) * R;
-  Batch now, next;
-  if (kAhead<N> && r0 < a.rows) fetch(now, r0);
+  Batch now;
+  ComingBatch next;
+  auto arrive = [&]() {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if constexpr (kAny) {
+        now.d[i].take(next.d[i], t, TPR, a.hidden);
+        now.x[i].take(next.x[i], t, TPR, a.hidden);
+      } else {
+        now.d[i] = next.d[i];
+        now.x[i] = next.x[i];
+      }
+      now.mu[i] = next.mu[i];
+      now.rs[i] = next.rs[i];
+    }
+  };
+  if (kAhead<N> && r0 < a.rows) {
+    fetch(next, r0);
+    arrive();
+  }
   for (; r0 < a.rows; r0 += step) {
-    if constexpr (kAhead<N>) fetch(next, r0 + step < a.rows ? r0 + step : a.rows);
-    else fetch(now, r0);
+    fetch(next, !kAhead<N> ? r0 : r0 + step < a.rows ? r0 + step : a.rows);
+    if constexpr (!kAhead<N>) arrive();
     float s[K];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -311,9 +380,18 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
         ge = kLayer ? fma2(ge, v, m0) : mul2(ge, v);
         now.x[i].set2(e, fma2(n, m, ge));
       }
-      now.x[i].store(dx + (int64_t)(r0 + i) * a.dx_stride, t, TPR, a.hidden);
+      if constexpr (kAny) now.x[i].stage(staged + i * kStaged, t, TPR, a.hidden);
+      else now.x[i].store(dx + (int64_t)(r0 + i) * a.dx_stride, t, TPR, a.hidden);
     }
-    if constexpr (kAhead<N>) now = next;
+    if constexpr (kAny) {
+      group_barrier<TPR>(group);
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (r0 + i < a.rows)
+          store_any(staged + i * kStaged, dx + (int64_t)(r0 + i) * a.dx_stride, t, TPR, a.hidden);
+      if constexpr (TPR == 32) __syncwarp();
+    }
+    if constexpr (kAhead<N>) arrive();
   }
   pdl_launch_dependents();
   pdl_launch_dependents();
@@ -573,16 +651,16 @@ int grad_ctas(int rows, int hidden) {
   return ctas < most ? ctas : most;
 }
 
-template <typename T, int V, int TPR, int N, bool kLayer>
+template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
 cudaError_t norm_rows(const T *x, const NormArgs &a, T *y, cudaStream_t stream) {
   // at least a row for every group
   constexpr int kGroups = kNormBlock<TPR> / TPR;
   const int most = kSms * (512 / kNormBlock<TPR>), ctas = (a.rows + kGroups - 1) / kGroups;
-  norm_kernel<T, V, TPR, N, kLayer><<<ctas < most ? ctas : most, kNormBlock<TPR>, 0, stream>>>(x, a, y);
+  norm_kernel<T, V, kAny, TPR, N, kLayer><<<ctas < most ? ctas : most, kNormBlock<TPR>, 0, stream>>>(x, a, y);
   return cudaGetLastError();
 }
 
-template <typename T, int V, int TPR, int N, bool kLayer>
+template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
 cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *dweight,
                       float *dbias, cudaStream_t stream) {
   const int ctas = grad_ctas(a.rows, a.hidden);
@@ -590,7 +668,7 @@ cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *
   constexpr int kPiece = kRingThreads * V * (int)sizeof(T);
   const int row_bytes = 2 * ((a.hidden + kRingThreads * V - 1) / (kRingThreads * V)) * kPiece;
   const int slots = kRingBytes / row_bytes < 6 ? kRingBytes / row_bytes : 6;
-  constexpr bool kRing = N >= 16 && N * sizeof(T) <= 64 && (V * sizeof(T) == 16 || (sizeof(T) == 4 && N == 16));
+  constexpr bool kRing = !kAny && N >= 16 && N * sizeof(T) <= 64 && (V * sizeof(T) == 16 || (sizeof(T) == 4 && N == 16));
   if (kRing && slots >= 3) {
     if constexpr (kRing) {
       auto kernel = norm_grad_ring_kernel<T, V, N, kLayer>;
@@ -603,7 +681,7 @@ cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *
   } else {
     constexpr bool kHeld = N >= 32 || kBlock<TPR> > TPR;
     constexpr size_t smem = kHeld ? (size_t)(kLayer ? 2 : 1) * N * TPR * 4 : 0;
-    auto kernel = norm_grad_kernel<T, V, TPR, N, kLayer>;
+    auto kernel = norm_grad_kernel<T, V, kAny, TPR, N, kLayer>;
     if (smem > 48 * 1024) {
       const cudaError_t err =
           cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -618,14 +696,14 @@ cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *
                         true, a.partial, ctas, columns, a.hidden, dweight, dbias);
 }
 
-// Calls f.template run<T, V>() for a row's type and access.
+// Calls f.template run<T, V, kAny>() for a row's type and alignment: 16 bytes an access,
+// by windows where rows are not aligned (bf16), or an element an access (fp32, which
+// a warp's accesses take whole lines of all the same).
 template <typename F>
-cudaError_t dispatch(int dtype, int v, const F &f) {
+cudaError_t dispatch(int dtype, bool aligned, const F &f) {
   if (dtype == SLIMWISE_DTYPE_BF16)
-    return v == 8   ? f.template run<__nv_bfloat16, 8>()
-           : v == 2 ? f.template run<__nv_bfloat16, 2>()
-                    : f.template run<__nv_bfloat16, 1>();
-  return v == 4 ? f.template run<float, 4>() : f.template run<float, 1>();
+    return aligned ? f.template run<__nv_bfloat16, 8, false>() : f.template run<__nv_bfloat16, 8, true>();
+  return aligned ? f.template run<float, 4, false>() : f.template run<float, 1, false>();
 }
 
 template <bool kLayer>
@@ -634,19 +712,19 @@ struct NormCall {
   NormArgs a;
   void *y;
   cudaStream_t stream;
-  template <typename T, int V, int TPR, int N>
+  template <typename T, int V, bool kAny, int TPR, int N>
   cudaError_t rows() const {
-    return norm_rows<T, V, TPR, N, kLayer>(static_cast<const T *>(x), a, static_cast<T *>(y), stream);
+    return norm_rows<T, V, kAny, TPR, N, kLayer>(static_cast<const T *>(x), a, static_cast<T *>(y), stream);
   }
-  template <typename T, int V>
+  template <typename T, int V, bool kAny>
   cudaError_t run() const {
-    return a.hidden <= 256    ? rows<T, V, 32, 8>()
-           : a.hidden <= 512  ? rows<T, V, 32, 16>()
-           : a.hidden <= 1024 ? rows<T, V, 64, 16>()
-           : a.hidden <= 2048 ? rows<T, V, 128, 16>()
-           : a.hidden <= 4096 ? rows<T, V, 256, 16>()
-           : a.hidden <= 8192 ? rows<T, V, 512, 16>()
-                              : rows<T, V, 512, 32>();
+    return a.hidden <= 256    ? rows<T, V, kAny, 32, 8>()
+           : a.hidden <= 512  ? rows<T, V, kAny, 32, 16>()
+           : a.hidden <= 1024 ? rows<T, V, kAny, 64, 16>()
+           : a.hidden <= 2048 ? rows<T, V, kAny, 128, 16>()
+           : a.hidden <= 4096 ? rows<T, V, kAny, 256, 16>()
+           : a.hidden <= 8192 ? rows<T, V, kAny, 512, 16>()
+                              : rows<T, V, kAny, 512, 32>();
   }
 };
 
@@ -657,21 +735,21 @@ struct GradCall {
   void *dx;
   float *dweight, *dbias;
   cudaStream_t stream;
-  template <typename T, int V, int TPR, int N>
+  template <typename T, int V, bool kAny, int TPR, int N>
   cudaError_t rows() const {
-    return grad_rows<T, V, TPR, N, kLayer>(static_cast<const T *>(dy), static_cast<const T *>(x), a,
+    return grad_rows<T, V, kAny, TPR, N, kLayer>(static_cast<const T *>(dy), static_cast<const T *>(x), a,
                                            static_cast<T *>(dx), dweight, dbias, stream);
   }
-  template <typename T, int V>
+  template <typename T, int V, bool kAny>
   cudaError_t run() const {
-    return a.hidden <= 256    ? rows<T, V, 32, 8>()
-           : a.hidden <= 1024 ? rows<T, V, 128, 8>()
-           : a.hidden <= 2048 ? rows<T, V, 256, 8>()
-           : a.hidden <= 4096 ? rows<T, V, 512, 8>()
-           : V < 4 && a.hidden <= 5120 ? rows<T, V, 512, V < 4 ? 10 : 16>()
-           : V < 8 && a.hidden <= 6144 ? rows<T, V, 512, V < 8 ? 12 : 16>()
-           : a.hidden <= 8192 ? rows<T, V, 512, 16>()
-                              : rows<T, V, 512, 32>();
+    return a.hidden <= 256    ? rows<T, V, kAny, 32, 8>()
+           : a.hidden <= 1024 ? rows<T, V, kAny, 128, 8>()
+           : a.hidden <= 2048 ? rows<T, V, kAny, 256, 8>()
+           : a.hidden <= 4096 ? rows<T, V, kAny, 512, 8>()
+           : V < 4 && a.hidden <= 5120 ? rows<T, V, kAny, 512, V < 4 ? 10 : 16>()
+           : V < 8 && a.hidden <= 6144 ? rows<T, V, kAny, 512, V < 8 ? 12 : 16>()
+           : a.hidden <= 8192 ? rows<T, V, kAny, 512, 16>()
+                              : rows<T, V, kAny, 512, 32>();
   }
 };
 
@@ -682,8 +760,12 @@ cudaError_t launch_norm(const void *x, int dtype, int rows, int hidden, int64_t 
                         int64_t y_stride, float *mean, float *rstd, cudaStream_t stream) {
   const void *base[2] = {x, y};
   const int64_t strides[2] = {stride, y_stride};
-  const int v = row_vector(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 2, base, strides);
-  const NormArgs a = {rows, hidden, stride, y_stride, weight, bias, eps, mean, rstd};
+  const bool v = rows_aligned(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 2, base, strides);
+  const auto extent = [&](const void *p, int64_t step) {
+    return dtype == SLIMWISE_DTYPE_BF16 ? extent_of(static_cast<const __nv_bfloat16 *>(p), rows, step, hidden)
+                                        : extent_of(static_cast<const float *>(p), rows, step, hidden);
+  };
+  const NormArgs a = {rows, hidden, extent(x, stride), stride, y_stride, weight, bias, eps, mean, rstd};
   return layer ? dispatch(dtype, v, NormCall<true>{x, a, y, stream})
                : dispatch(dtype, v, NormCall<false>{x, a, y, stream});
 }
@@ -698,8 +780,12 @@ cudaError_t launch_norm_grad(const void *dy, int64_t dy_stride, const void *x, i
                              float *dbias, void *workspace, cudaStream_t stream) {
   const void *base[3] = {dy, x, dx};
   const int64_t strides[3] = {dy_stride, stride, dx_stride};
-  const int v = row_vector(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 3, base, strides);
-  const GradArgs a = {rows, hidden, dy_stride, stride, dx_stride, weight, mean, rstd,
+  const bool v = rows_aligned(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 3, base, strides);
+  const auto extent = [&](const void *p, int64_t step) {
+    return dtype == SLIMWISE_DTYPE_BF16 ? extent_of(static_cast<const __nv_bfloat16 *>(p), rows, step, hidden)
+                                        : extent_of(static_cast<const float *>(p), rows, step, hidden);
+  };
+  const GradArgs a = {rows, hidden, extent(dy, dy_stride), extent(x, stride), dy_stride, stride, dx_stride, weight, mean, rstd,
                       static_cast<float *>(workspace)};
   return mean ? dispatch(dtype, v, GradCall<true>{dy, x, a, dx, dweight, dbias, stream})
               : dispatch(dtype, v, GradCall<false>{dy, x, a, dx, dweight, dbias, stream});

@@ -60,6 +60,18 @@ inline int row_vector(int element_bytes, int hidden, int n, const void *const *b
   return v;
 }
 
+// Whether rows may be read and written 16 bytes at a time as they lie: all start on
+// 16-byte boundaries and are multiples of them long.  Else their kernels move windows
+// and shift (RowPart::load_any, store_any).
+inline bool rows_aligned(int element_bytes, int hidden, int n, const void *const *base,
+                         const int64_t *stride) {
+  const int v = 16 / element_bytes;
+  bool ok = hidden % v == 0;
+  for (int i = 0; i < n; ++i)
+    ok = ok && reinterpret_cast<uintptr_t>(base[i]) % 16 == 0 && stride[i] % v == 0;
+  return ok;
+}
+
 cudaError_t launch_norm(const void *x, int dtype, int rows, int hidden, int64_t stride,
                         const float *weight, const float *bias, bool layer, float eps, void *y,
                         int64_t y_stride, float *mean, float *rstd, cudaStream_t stream);
@@ -139,6 +151,114 @@ __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
   return r;
 }
 
+// Where a matrix's elements lie: reads of rows stay inside.
+struct Extent {
+  uintptr_t lo, hi;
+};
+template <typename T>
+__host__ __device__ inline Extent extent_of(const T *base, int64_t rows, int64_t stride, int hidden) {
+  const uintptr_t b = reinterpret_cast<uintptr_t>(base);
+  return {b, b + (rows ? (uintptr_t)((rows - 1) * stride + hidden) * sizeof(T) : 0)};
+}
+
+// A 16-byte window, element by element: what lies outside [lo, hi) is neither read
+// (but 0) nor written.
+template <typename T>
+__device__ __noinline__ uint4 read_edge(uintptr_t window, uintptr_t lo, uintptr_t hi) {
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uintptr_t a = window + 4 * i;
+    if constexpr (sizeof(T) == 4) {
+      if (a >= lo && a < hi) w[i] = __ldcg(reinterpret_cast<const uint32_t *>(a));
+    } else {
+      if (a >= lo && a < hi) w[i] = __ldcg(reinterpret_cast<const unsigned short *>(a));
+      if (a + 2 >= lo && a + 2 < hi) w[i] |= (uint32_t)__ldcg(reinterpret_cast<const unsigned short *>(a + 2)) << 16;
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __noinline__ void write_edge(uint4 v, uintptr_t window, uintptr_t lo, uintptr_t hi) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uintptr_t a = window + 4 * i;
+    if constexpr (sizeof(T) == 4) {
+      if (a >= lo && a < hi) *reinterpret_cast<uint32_t *>(a) = w[i];
+    } else {
+      if (a >= lo && a < hi) *reinterpret_cast<unsigned short *>(a) = (unsigned short)w[i];
+      if (a + 2 >= lo && a + 2 < hi) *reinterpret_cast<unsigned short *>(a + 2) = (unsigned short)(w[i] >> 16);
+    }
+  }
+}
+// 16 bytes from byte `by` (0..15, whole elements) of two windows.
+__device__ __forceinline__ uint4 shift_windows(uint4 a, uint4 b, int by) {
+  const uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  uint32_t y[6], z[5];
+#pragma unroll
+  for (int k = 0; k < 6; ++k) y[k] = by & 8 ? x[k + 2] : x[k];
+#pragma unroll
+  for (int k = 0; k < 5; ++k) z[k] = by & 4 ? y[k + 1] : y[k];
+  const uint32_t sel = by & 2 ? 0x5432u : 0x3210u;
+  return make_uint4(__byte_perm(z[0], z[1], sel), __byte_perm(z[1], z[2], sel), __byte_perm(z[2], z[3], sel),
+                    __byte_perm(z[3], z[4], sel));
+}
+
+// Rows staged in shared memory for store_any: element 0 behind a window, another
+// window behind the last.
+template <typename T>
+__host__ __device__ constexpr int staged_elements(int n) {
+  return n + 2 * 16 / (int)sizeof(T);
+}
+// Writes elements [0, width) of a staged row to `row`, which starts anywhere: whole
+// windows of it, read from the staged row shifted, the two at its ends by element.  By
+// `threads` threads, after a barrier.
+template <typename T>
+__device__ __forceinline__ void store_any(const T *staged, T *row, int t, int threads, int width) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(row), hi = lo + (uintptr_t)width * sizeof(T);
+  const int mis = (int)(lo & 15);
+  const uint4 *from = reinterpret_cast<const uint4 *>(staged);
+  for (uintptr_t w = lo - mis + 16 * (uintptr_t)t; w < hi; w += 16 * (uintptr_t)threads) {
+    const int k = (int)((w - (lo - mis)) >> 4);
+    // byte 0 of window k is byte 16 + 16 k - mis of the staged row
+    const uint4 v = mis ? shift_windows(from[k], from[k + 1], 16 - mis) : from[k + 1];
+    if (w >= lo && w + 16 <= hi) *reinterpret_cast<uint4 *>(w) = v;
+    else write_edge<T>(v, w, lo, hi);
+  }
+}
+
+// The two windows of each of a thread's accesses to a row, and where its elements
+// begin in the first.
+template <typename T, int N>
+struct Windows {
+  static constexpr int V = 16 / sizeof(T);
+  uint4 a[N / V], b[N / V];
+  int by;
+  __device__ __forceinline__ void load(const T *row, int t, int threads, int width, Extent x) {
+    // windows of a row reach up to 16 bytes beyond it: only the matrix's first and last
+    // rows have to look at each
+    const uintptr_t start = reinterpret_cast<uintptr_t>(row);
+    const bool inside = start >= x.lo + 16 && start + (uintptr_t)max(width, 0) * sizeof(T) + 32 <= x.hi;
+    by = (int)(start & 15);
+#pragma unroll
+    for (int p = 0; p < N / V; ++p) {
+      const int c = (p * threads + t) * V;
+      const uintptr_t at = start + (intptr_t)c * (int)sizeof(T) - by;
+      a[p] = b[p] = make_uint4(0, 0, 0, 0);
+      if (inside) {
+        if (c < width) {
+          a[p] = __ldg(reinterpret_cast<const uint4 *>(at));
+          b[p] = __ldg(reinterpret_cast<const uint4 *>(at) + 1);
+        }
+      } else if (c < width) {
+        a[p] = read_edge<T>(at, x.lo, x.hi);
+        b[p] = read_edge<T>(at + 16, x.lo, x.hi);
+      }
+    }
+  }
+};
+
 // A thread's part of a row: N elements of T in pieces of V, the row's pieces
 // dealt to `threads` threads in turn, as they lie in memory (a bf16 in half a
 // register).  Element e is column ((e / V) threads + t) V + e % V.
@@ -181,6 +301,42 @@ struct RowPart {
         const uint32_t v = in ? read<kAfter>(reinterpret_cast<const unsigned short *>(row + c)) : 0u;
         if (p & 1) w[p / 2] |= v << 16;
         else w[p / 2] = v;
+      }
+    }
+  }
+  // The same of a row that starts anywhere and of any width (V: 16 bytes): its windows
+  // on their way (load_windows), then shifted into place.
+  __device__ __forceinline__ void take(const Windows<T, N> &x, int t, int threads, int width) {
+    static_assert(V * sizeof(T) == 16, "windows");
+#pragma unroll
+    for (int p = 0; p < N / V; ++p) {
+      const int left = width - (p * threads + t) * V;
+      const uint4 v = shift_windows(x.a[p], x.b[p], x.by);
+      uint32_t *o = w + 4 * p;
+      o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+      if (left < V) {  // elements past the row: 0
+        const int bytes = left * (int)sizeof(T);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (4 * k >= bytes) o[k] = 0u;
+          else if (4 * k + 2 >= bytes) o[k] &= 0xFFFFu;
+        }
+      }
+    }
+  }
+  // Into a staged row (store_any).
+  __device__ __forceinline__ void stage(T *staged, int t, int threads, int width) const {
+#pragma unroll
+    for (int p = 0; p < N / V; ++p) {
+      const int c = (p * threads + t) * V;
+      if (c < width) {
+        constexpr int B = V * (int)sizeof(T);
+        static_assert(B % 16 == 0, "windows");
+#pragma unroll
+        for (int q = 0; q < B / 16; ++q) {
+          const uint32_t *o = w + (B / 4) * p + 4 * q;
+          reinterpret_cast<uint4 *>(staged + 16 / sizeof(T) + c)[q] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
       }
     }
   }

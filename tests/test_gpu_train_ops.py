@@ -389,6 +389,7 @@ def _check_loss(hidden, weight, labels, row_weight, dh_out=True, dw_out=True, **
 
 @pytest.mark.parametrize("rows,width,vocab", [
     (1, 8, 1), (1, 64, 2), (3, 16, 7), (5, 128, 255), (17, 72, 256), (64, 64, 257), (255, 136, 1000), (256, 256, 513),
+    (63, 40, 9), (64, 72, 511), (65, 200, 777), (128, 328, 1025), (129, 64, 600), (100, 2056, 130),
     (257, 264, 300), (300, 520, 2049), (513, 1032, 700), (64, 4096, 1500), (1021, 128, 5003), (40, 16384, 130)])
 def test_linear_loss(rows, width, vocab):
     _check_loss(*_head(rows, width, vocab, seed=rows + vocab))
@@ -460,6 +461,11 @@ def test_linear_loss_of_labels_that_are_sure_or_impossible():
     labels[:] = 7
     labels[300] = 2000
     _check_loss(hidden, weight, labels, wt)
+    # few rows
+    for rows in (7, 100):
+        labels[:rows] = 2000
+        _check_loss(hidden[:rows], weight, labels[:rows], wt[:rows])
+        _check_loss(hidden[:rows], weight, labels[:rows], wt[:rows], dh_out=False, dw_out=False)
 
 
 def test_linear_loss_of_what_is_no_number_and_of_labels_outside():
