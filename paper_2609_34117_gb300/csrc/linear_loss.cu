@@ -49,15 +49,15 @@ constexpr int kTile = 256;       // rows and columns of a pair's tile
 constexpr int kHalf = 128;       // of a CTA's share of an operand
 constexpr int kDepth = 64;       // slice of the contraction: 128 bytes
 constexpr int kStages = 6;
-// Few rows: the products' roles change.  The vocabulary (for dh: the width) is M, which
-// fills the tensor cores' rows and the accumulators' lanes, and the rows are N, 64 or 128 of
-// them.  With rows as M, 64 of them took a whole tile's time, and the two warps that can
-// read their lanes did all of the epilogue.
-constexpr int kFewRows = 128;
+// Roles swapped: the vocabulary (for dh: the width) is M, which fills the tensor cores'
+// rows and the accumulators' lanes, and tiles of `rows_tile` rows, a multiple of 32, are
+// N.  For few rows, of which a tile of 256 would be mostly empty and whose epilogue
+// only the warps of their lanes could do: 9 rows of 114316 words at 168 36 -> 24 us, and
+// for some hundred rows that tiles of 256 fit badly.
+constexpr int kSwapRows = 1024, kSwapAlways = 128, kSwapWidth = 512, kSwapStages = 8;
+constexpr int kRowData = kSwapRows * 8;  // the rows' references and labels, at the ring's end
 constexpr int kOperandBytes = kHalf * kDepth * 2;
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kFewStages = 8, kFewStageBytes = kOperandBytes + kFewRows / 2 * kDepth * 2;
-static_assert(kFewStages * kFewStageBytes == kStages * kStageBytes, "the ring's room");
 // A warp's 32 rows x 64 columns of bf16 on their way out by TMA (128-byte swizzle).
 constexpr int kOutBytes = 32 * 128;
 constexpr int kEpiWarps = 8, kGemmThreads = 64 + 32 * kEpiWarps;
@@ -74,15 +74,28 @@ enum Word { kLive = 0, kArrived = 1, kErr = kCtrlErr };
 
 struct Layout {
   int rows_pad, chunk, chunks, vocab_tiles, hidden_tiles, split_tiles;
+  int rows_tile;  // swapped_rows()
   int64_t cells_stride;
   size_t ctrl, counts, orig, label, target, ref, scale, flags, rows, scaled, sums, cells, splits, acc, total;
 };
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// N of the products with swapped roles, or 0: rows are M, in tiles of 256.  The swapped
+// epilogue takes twice the instructions: products along short rows keep the others
+// unless they have few of them.
+int swapped_rows(int rows, int hidden) {
+  if (rows > kSwapRows) return 0;
+  const int tiles = ceil_div(rows, kTile), n = ceil_div(ceil_div(rows, tiles), 32) * 32;
+  if (rows <= kSwapAlways) return n < 64 ? 64 : n;
+  return hidden >= kSwapWidth && n <= kTile * 7 / 8 ? n : 0;
+}
+
 Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_weight) {
   Layout l;
   const bool grad = grad_hidden || grad_weight;
+  l.rows_tile = swapped_rows(rows, hidden);
+  const int rows_tile = l.rows_tile ? l.rows_tile : kTile;
   l.rows_pad = ceil_div(rows, kTile) * kTile;
   l.vocab_tiles = ceil_div(vocab, kTile);
   l.hidden_tiles = ceil_div(hidden, kTile);
@@ -95,7 +108,7 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
   l.chunks = ceil_div(l.rows_pad, l.chunk);
   l.split_tiles = 0;
   if (grad_hidden)
-    for (int m = 1; m <= l.chunk / kTile; ++m) {
+    for (int m = 1; m <= ceil_div(l.chunk, rows_tile); ++m) {
       const int tiles = m * l.hidden_tiles, kb = ceil_div(vocab, kDepth);
       int s = kSplitTiles / tiles;
       s = s < 1 ? 1 : s > kMostSplits ? kMostSplits : s;
@@ -119,7 +132,7 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
   l.flags = take(n / kTile * 3 * 4);
   l.rows = take(n * hidden * 2);
   l.scaled = take(grad_weight ? (size_t)l.chunk * hidden * 2 : 0);
-  l.sums = take((size_t)(rows <= kFewRows ? kMostPairs * 8 : l.vocab_tiles * 2) * l.chunk * sizeof(float2));
+  l.sums = take((size_t)l.vocab_tiles * 2 * l.chunk * sizeof(float2));
   l.cells = take(grad ? (size_t)l.chunk * l.cells_stride * 2 : 0);
   l.splits = take((size_t)l.split_tiles * kTile * kTile * 4);
   l.acc = take(grad_weight && l.chunks > 1 ? (size_t)vocab * hidden * 4 : 0);
@@ -131,13 +144,14 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
 struct Call {
   int T, H, V;
   int rows_pad, chunk, vocab_tiles, hidden_tiles;
+  int rows_tile;  // of the first product and dh's
   int64_t cells_stride;
   int32_t *ctrl, *orig, *label;
   int32_t *counts;  // labelled rows of each 1024 (more than kCountedRows rows)
   int32_t *flags;  // [3][rows_pad / 256]: tiles to run again; their list; each chunk's number of them
   float *target, *ref, *scale;
   __nv_bfloat16 *rows, *scaled, *cells;
-  float2 *sums;   // [2 vocab_tiles, or 8 a pair][chunk]: sum of numerators, largest logit
+  float2 *sums;   // [2 vocab_tiles][chunk]: sum of numerators, largest logit
   float *splits;  // [tiles][256][256]
   float *acc;     // [V][H], more than one chunk
   const __nv_bfloat16 *hidden, *weight;
@@ -363,9 +377,9 @@ struct Work {
 };
 
 constexpr size_t kBars = (size_t)kStages * kStageBytes + kEpiWarps * kOutBytes;
-// barriers, words, the few rows' references and labels, alignment
-constexpr int kWords = 8 * (2 * kFewStages + 5);
-constexpr size_t kGemmSmem = kBars + kWords + 64 + kFewRows * 8 + 1024;
+// barriers, words, alignment
+constexpr int kWords = 8 * (2 * kSwapStages + 5);
+constexpr size_t kGemmSmem = kBars + kWords + 64 + 1024;
 
 // Sums of the columns' numerators and the P tile of 32 columns.
 template <Mode kMode>
@@ -428,11 +442,11 @@ __device__ __forceinline__ float reduce_across(float (&x)[32], int lane, F op) {
   return x[0];
 }
 
-// Few rows: 32 rows' logits z at the lane's word.  Leaves their numerators in bf16 at
+// Swapped roles: 32 rows' logits z at the lane's word.  Leaves their numerators in bf16 at
 // `staged` (64 bytes a row, zeros for rows past `live`), and returns to lane j row j's
 // sum over the warp's words and largest logit.
 template <Mode kMode>
-__device__ __forceinline__ float2 few_numerators(float (&z)[32], const float *ref, const int *label, int word,
+__device__ __forceinline__ float2 swapped_numerators(float (&z)[32], const float *ref, const int *label, int word,
                                                  bool known, int live, int lane, uint32_t staged) {
   float top = kFloor;
 #pragma unroll
@@ -452,6 +466,20 @@ __device__ __forceinline__ float2 few_numerators(float (&z)[32], const float *re
   }
   const float sum = reduce_across(z, lane, [](float a, float b) { return a + b; });
   return make_float2(sum, top);
+}
+
+// Whether all threads of the epilogue say so (one that gave up takes the others along).
+__device__ __forceinline__ bool epilogue_agrees(bool ok) {
+  int r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.and.pred q, 2, %2, p;\n\t"
+      "selp.s32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(ok ? 1 : 0), "n"(32 * kEpiWarps)
+      : "memory");
+  return r != 0;
 }
 
 // The loss over all rows, by N threads of a CTA: thread i adds its rows i, i + N, ...
@@ -480,27 +508,46 @@ __device__ __forceinline__ void total_loss(const Call &c, int thread, double *wa
 __device__ __forceinline__ void join_rows(const Call &c, int chunk, int pairs, int64_t thread, int64_t threads) {
   const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
   if (rows == 0) return;
-  const int tiles = (rows + kTile - 1) / kTile * c.hidden_tiles;
+  const int tiles = (rows + c.rows_tile - 1) / c.rows_tile * c.hidden_tiles;
   const int splits = choose_splits(tiles, (c.V + kDepth - 1) / kDepth, pairs), words = c.H / 4;
+  // four outputs at a time: their loads' latency is what this takes
+  constexpr int kItems = 4;
   const int64_t all = (int64_t)rows * words;
-  for (int64_t i = thread; i < all; i += threads) {
-    const int row = (int)(i / words), col = (int)(i - (int64_t)row * words) * 4;
-    const int tile = row / kTile * c.hidden_tiles + col / kTile;
-    const float *from = c.splits + ((int64_t)tile * kTile + row % kTile) * kTile + col % kTile;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-    for (int s = 0; s < splits; ++s) {
-      const float4 x = __ldcg(reinterpret_cast<const float4 *>(from));
-      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-      from += (int64_t)tiles * kTile * kTile;
+  for (int64_t i0 = thread; i0 < all; i0 += kItems * threads) {
+    const float *from[kItems];
+    float4 v[kItems];
+    int row[kItems], col[kItems];
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int64_t i = i0 + k * threads < all ? i0 + k * threads : i0;
+      row[k] = (int)(i / words);
+      col[k] = (int)(i - (int64_t)row[k] * words) * 4;
+      const int tile = row[k] / c.rows_tile * c.hidden_tiles + col[k] / kTile;
+      from[k] = c.splits + ((int64_t)tile * kTile + row[k] % c.rows_tile) * kTile + col[k] % kTile;
+      v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
-    const float f = __ldcg(c.scale + row0 + row);
-    __nv_bfloat16 *to = c.dh + (int64_t)__ldcg(c.orig + row0 + row) * c.dh_stride + col;
-    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0] * f, v[1] * f), pack_bf16(v[2] * f, v[3] * f));
+#pragma unroll 2
+    for (int s = 0; s < splits; ++s) {
+      float4 x[kItems];
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) x[k] = __ldcg(reinterpret_cast<const float4 *>(from[k]));
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) {
+        v[k].x += x[k].x; v[k].y += x[k].y; v[k].z += x[k].z; v[k].w += x[k].w;
+        from[k] += (int64_t)tiles * kTile * kTile;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      if (i0 + k * threads >= all) break;
+      const float f = __ldcg(c.scale + row0 + row[k]);
+      __nv_bfloat16 *to = c.dh + (int64_t)__ldcg(c.orig + row0 + row[k]) * c.dh_stride + col[k];
+      *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[k].x * f, v[k].y * f), pack_bf16(v[k].z * f, v[k].w * f));
+    }
   }
 }
 
-template <Mode kMode, bool kFew>
+template <Mode kMode, bool kSwapped>
 __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinThreads : 0), 1)
     product_kernel(const __grid_constant__ Operands maps, Call c, int chunk, int again, int join,
                    uint64_t timeout_ns) {
@@ -509,22 +556,23 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t smem_base = smem_u32(smem);
   const uint32_t bar0 = smem_base + (uint32_t)kBars;
-  constexpr int kRing = kFew ? kFewStages : kStages;
-  constexpr int kSlot = kFew ? kFewStageBytes : kStageBytes;
+  // N, a stage of the ring, and how many there are
+  const int n_rows = kSwapped ? c.rows_tile : kTile;
+  const int slot_bytes = kSwapped ? kOperandBytes + n_rows * kDepth : kStageBytes;
+  const int ring = kSwapped ? min(kSwapStages, (kStages * kStageBytes - kRowData) / slot_bytes) : kStages;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
-  auto empty_bar = [&](int s) { return bar0 + 8u * (kRing + s); };
-  auto accf_bar = [&](int b) { return bar0 + 8u * (2 * kRing + b); };
-  auto acce_bar = [&](int b) { return bar0 + 8u * (2 * kRing + 2 + b); };
-  const uint32_t drain_bar = bar0 + 8u * (2 * kRing + 4);
+  auto empty_bar = [&](int s) { return bar0 + 8u * (ring + s); };
+  auto accf_bar = [&](int b) { return bar0 + 8u * (2 * ring + b); };
+  auto acce_bar = [&](int b) { return bar0 + 8u * (2 * ring + 2 + b); };
+  const uint32_t drain_bar = bar0 + 8u * (2 * ring + 4);
   int *misc = reinterpret_cast<int *>(smem + kBars + kWords);
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(misc);
   volatile int *abort = misc + 1;
   volatile int *consumed = misc + 2;
   volatile int *n_splits = misc + 3;
   double *warp_totals = reinterpret_cast<double *>(misc + 4);  // kGradWeight
-  float *few_ref = reinterpret_cast<float *>(misc + 16);
-  int *few_label = reinterpret_cast<int *>(few_ref + kFewRows);
-  const int few = c.T <= kFewRows / 2 ? kFewRows / 2 : kFewRows;  // N
+  float *row_ref = reinterpret_cast<float *>(smem + kStages * kStageBytes - kRowData);  // kSwapped
+  int *row_label = reinterpret_cast<int *>(row_ref + kSwapRows);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t crank = cluster_ctarank();
@@ -539,7 +587,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     if (__ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0) return;
   }
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kRing; ++s) {
+    for (int s = 0; s < ring; ++s) {
       mbar_init(full_bar(s), 1);
       mbar_init(empty_bar(s), 1);
     }
@@ -553,7 +601,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     mbar_fence_init();
     tma_prefetch_desc(&maps.a);
     tma_prefetch_desc(&maps.b);
-    if constexpr (kMode == kNumerators && !kFew) tma_prefetch_desc(&maps.out);
+    if constexpr (kMode == kNumerators && !kSwapped) tma_prefetch_desc(&maps.out);
   }
   if (warp == 1) {
     tmem_alloc_pair(smem_u32((const void *)tmem_slot), 512);
@@ -570,25 +618,28 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
   work.list = nullptr;
   work.splits = 1;
   if constexpr (kMode == kForward || kMode == kNumerators) {
-    work.mt = (rows + kTile - 1) / kTile;
+    work.mt = (rows + n_rows - 1) / n_rows;
     work.nt = c.vocab_tiles;
     work.kb = (c.H + kDepth - 1) / kDepth;
     if (kMode == kNumerators && again) {
       // the tiles that the sums' kernel marked
-      const int tiles = c.rows_pad / kTile;
-      work.mt = __ldcg(c.flags + 2 * tiles + chunk);
-      work.list = c.flags + tiles + row0 / kTile;
+      // (roles swapped: all rows, whose tiles are others)
+      if constexpr (!kSwapped) {
+        const int tiles = c.rows_pad / kTile;
+        work.mt = __ldcg(c.flags + 2 * tiles + chunk);
+        work.list = c.flags + tiles + row0 / kTile;
+      }
     }
     work.units = work.mt * work.nt;
-    if constexpr (kFew) {
-      for (int i = threadIdx.x; i < few; i += blockDim.x) {
-        few_ref[i] = i < rows ? __ldcg(c.ref + i) : 0.0f;
-        few_label[i] = i < rows ? __ldcg(c.label + i) : -1;
+    if constexpr (kSwapped) {
+      for (int i = threadIdx.x; i < work.mt * n_rows; i += blockDim.x) {
+        row_ref[i] = i < rows ? __ldcg(c.ref + i) : 0.0f;
+        row_label[i] = i < rows ? __ldcg(c.label + i) : -1;
       }
       __syncthreads();
     }
   } else if constexpr (kMode == kGradHidden) {
-    work.mt = (rows + kTile - 1) / kTile;
+    work.mt = (rows + n_rows - 1) / n_rows;
     work.nt = c.hidden_tiles;
     work.kb = (c.V + kDepth - 1) / kDepth;
     if (warp == 0 && rows > 0) {
@@ -630,8 +681,8 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     return __all_sync(0xFFFFFFFFu, ok) != 0;
   };
   // operands along the contraction (K-major) or across it
-  constexpr bool kAcrossA = kMode == kGradWeight || (kFew && kMode == kGradHidden);
-  constexpr bool kAcrossB = kMode == kGradWeight || (!kFew && kMode == kGradHidden);
+  constexpr bool kAcrossA = kMode == kGradWeight || (kSwapped && kMode == kGradHidden);
+  constexpr bool kAcrossB = kMode == kGradWeight || (!kSwapped && kMode == kGradHidden);
 
   if (warp == 0) {
     // ------------------------------------------------------------ copies
@@ -644,18 +695,18 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       const Unit w = work.at(u);
       // first row (column) of this CTA's share of either operand
       const bool logits = kMode == kForward || kMode == kNumerators;
-      const int a0 = (kFew ? w.n * kTile : (logits ? row0 : 0) + w.m * kTile) + (int)crank * kHalf;
-      const int b0 = kFew ? (int)crank * few / 2 : w.n * kTile + (int)crank * kHalf;
+      const int a0 = (kSwapped ? w.n * kTile : (logits ? row0 : 0) + w.m * kTile) + (int)crank * kHalf;
+      const int b0 = kSwapped ? w.m * n_rows + (int)crank * n_rows / 2 : w.n * kTile + (int)crank * kHalf;
       for (int k = w.k0; k < w.k1; ++k) {
         if (!all_ok(mbar_wait_bounded(empty_bar(stage), phase ^ 1u, abort, timeout_ns))) {
           ok = false;
           break;
         }
-        const uint32_t a = smem_base + (uint32_t)(stage * kSlot), b = a + kOperandBytes;
+        const uint32_t a = smem_base + (uint32_t)(stage * slot_bytes), b = a + kOperandBytes;
         if (elect_one()) {
           const uint32_t bar = mapa_shared(full_bar(stage), 0u);
           if (lead)
-            mbar_arrive_expect_tx(full_bar(stage), kFew ? 2 * kOperandBytes + few * kDepth * 2 : 2 * kStageBytes);
+            mbar_arrive_expect_tx(full_bar(stage), 2 * slot_bytes);
           if constexpr (kAcrossA) {
             tma_load_2d_pair(a, &maps.a, bar, a0, k * kDepth, policy);
             tma_load_2d_pair(a + kOperandBytes / 2, &maps.a, bar, a0 + 64, k * kDepth, policy);
@@ -671,7 +722,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
         }
         __syncwarp();
         ++issued;
-        if (++stage == kRing) {
+        if (++stage == ring) {
           stage = 0;
           phase ^= 1u;
         }
@@ -682,13 +733,13 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       // until every stage still in the ring has been released (or, in the first
       // CTA after an abort, its copies have landed): nothing is left on its way
       // to this CTA's shared memory when it exits
-      const int from = issued > kRing ? issued - kRing : 0;
+      const int from = issued > ring ? issued - ring : 0;
       if (*abort && lead) {
         for (int s = *consumed > from ? *consumed : from; s < issued; ++s)
-          mbar_wait_timeout(full_bar(s % kRing), (uint32_t)((s / kRing) & 1), 10000000ull);
+          mbar_wait_timeout(full_bar(s % ring), (uint32_t)((s / ring) & 1), 10000000ull);
       } else {
         for (int s = from; s < issued; ++s)
-          mbar_wait_timeout(empty_bar(s % kRing), (uint32_t)((s / kRing) & 1), 10000000ull);
+          mbar_wait_timeout(empty_bar(s % ring), (uint32_t)((s / ring) & 1), 10000000ull);
       }
     }
     __syncwarp();
@@ -697,7 +748,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     if (lead) {
       int stage = 0, local = 0, n_consumed = 0;
       uint32_t phase = 0;
-      const uint32_t idesc = idesc_bf16_f32(kTile, kFew ? few : kTile) | (kAcrossA ? 1u << 15 : 0u) |
+      const uint32_t idesc = idesc_bf16_f32(kTile, n_rows) | (kAcrossA ? 1u << 15 : 0u) |
                              (kAcrossB ? 1u << 16 : 0u);
       bool ok = true;
       for (int u = pair; u < work.units && ok; u += pairs, ++local) {
@@ -714,7 +765,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
             break;
           }
           tc_fence_after();
-          const uint32_t as = smem_base + (uint32_t)(stage * kSlot), bs = as + kOperandBytes;
+          const uint32_t as = smem_base + (uint32_t)(stage * slot_bytes), bs = as + kOperandBytes;
           ++n_consumed;
           if (elect_one()) {
 #pragma unroll
@@ -729,7 +780,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
             *consumed = n_consumed;
           }
           __syncwarp();
-          if (++stage == kRing) {
+          if (++stage == ring) {
             stage = 0;
             phase ^= 1u;
           }
@@ -756,12 +807,34 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     const int q = warp & 3, half = (warp - 2) >> 2;  // lanes 32 q.., columns 128 half..
     const int in_tile = (int)crank * kHalf + 32 * q + lane;
     const OutBuffer out = {smem_base + (uint32_t)(kStages * kStageBytes + (warp - 2) * kOutBytes)};
-    float2 few_sums[2] = {make_float2(0.0f, kFloor), make_float2(0.0f, kFloor)};  // of the pair's tiles
+    // kSwapped: the four warps' sums of a row, [2 tiles in turn][4][256], joined a tile later,
+    // behind the barrier at which the warps agree on the next tile's wait
+    float2 *quarters = reinterpret_cast<float2 *>(smem + kStages * kStageBytes + kEpiWarps * kOutBytes / 2);
+    constexpr bool kSums = kSwapped && (kMode == kForward || kMode == kNumerators);
+    Unit joined = {0, -1, 0, 0};
+    auto join_quarters = [&](int parity) {
+      const int t = threadIdx.x - 64, row = joined.m * n_rows + t;
+      if (joined.n < 0 || t >= n_rows || row >= rows) return;
+      const float2 *at = quarters + parity * 4 * kTile + t;
+      float top = kFloor, sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = fmaxf(top, at[k * kTile].y);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        sum += kMode == kForward ? at[k * kTile].x * ex2((at[k * kTile].y - top) * kLog2e) : at[k * kTile].x;
+      c.sums[(int64_t)(joined.n * 2 + (int)crank) * c.chunk + row] = make_float2(sum, top);
+    };
     int local = 0;
     for (int u = pair; u < work.units; u += pairs, ++local) {
       const Unit w = work.at(u);
       const int b = local & 1;
-      if (!all_ok(mbar_wait_bounded(accf_bar(b), (uint32_t)(local >> 1) & 1u, abort, timeout_ns))) break;
+      bool ok = all_ok(mbar_wait_bounded(accf_bar(b), (uint32_t)(local >> 1) & 1u, abort, timeout_ns));
+      if constexpr (kSums) {
+        ok = epilogue_agrees(ok);
+        join_quarters((local & 1) ^ 1);
+        joined = w;
+      }
+      if (!ok) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(b * kTile + half * kHalf);
       const int row = w.m * kTile + in_tile, col0 = w.n * kTile + half * kHalf;
@@ -775,45 +848,46 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
                            mapa_shared(acce_bar(b), 0u))
                        : "memory");
       };
-      if constexpr (kFew) {
-        // this lane's word of the vocabulary (dh: column), all rows
-        const int mine = w.n * kTile + in_tile;
+      if constexpr (kSwapped) {
+        // this lane's word of the vocabulary (dh: column), the tile's rows in 32s, which the
+        // two halves of the warps take in turn
+        const int mine = w.n * kTile + in_tile, row_first = w.m * n_rows;
         const uint32_t lanes = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(b * kTile);
+        const uint32_t staged = smem_base + (uint32_t)(kStages * kStageBytes + (warp - 2) * kOutBytes / 2);
 #pragma unroll 1
-        for (int t0 = half * (few / 2); t0 < (half + 1) * (few / 2); t0 += 32) {
+        for (int t0 = 32 * half; t0 < n_rows; t0 += 64) {
           float z[32];
           tmem_ld_row(lanes + t0, z);
           tmem_ld_wait();
-          if (t0 + 32 == (half + 1) * (few / 2)) release();
+          if (t0 + 64 >= n_rows) release();
+          const int live = rows - row_first - t0;
           if constexpr (kMode == kGradHidden) {
             float *to = c.splits + ((int64_t)u * kTile + t0) * kTile + in_tile;
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-              if (t0 + j < rows) to[j * kTile] = z[j];
+              if (j < live) to[j * kTile] = z[j];
           } else {
-            const float2 sums = few_numerators<kMode>(z, few_ref + t0, few_label + t0, mine, mine < c.V, rows - t0,
-                                                      lane, out.at + (uint32_t)(t0 - half * (few / 2)) * 64);
-            float2 &kept = t0 == half * (few / 2) ? few_sums[0] : few_sums[1];
-            const float top = fmaxf(kept.y, sums.y);
-            if constexpr (kMode == kForward)
-              kept.x = kept.x * ex2((kept.y - top) * kLog2e) + sums.x * ex2((sums.y - top) * kLog2e);
-            else
-              kept.x += sums.x;
-            kept.y = top;
+            quarters[((local & 1) * 4 + q) * kTile + t0 + lane] =
+                swapped_numerators<kMode>(z, row_ref + row_first + t0, row_label + row_first + t0, mine, mine < c.V,
+                                          live, lane, staged);
+          }
+          if constexpr (kMode == kNumerators) {
+            // the warp's 32 words of each row, 64 bytes; as far as dW's slices read
+            __syncwarp();
+            const int first = w.n * kTile + (int)crank * kHalf + 32 * q;
+            const int needed = (rows + kDepth - 1) / kDepth * kDepth - row_first - t0;
+#pragma unroll
+            for (int i = lane; i < 128; i += 32) {
+              const int v = first + (i & 3) * 8;
+              const uint4 x = ld_shared_v4(staged + (uint32_t)i * 16);
+              if (v < c.cells_stride && (i >> 2) < needed)
+                *reinterpret_cast<uint4 *>(c.cells + (int64_t)(row_first + t0 + (i >> 2)) * c.cells_stride + v) = x;
+            }
+            __syncwarp();
           }
         }
-        if constexpr (kMode == kNumerators) {
-          // the warp's 32 words of each row, 64 bytes
-          __syncwarp();
-          const int first = w.n * kTile + (int)crank * kHalf + 32 * q;
-          for (int i = lane; i < few / 2 * 4; i += 32) {
-            const int v = first + (i & 3) * 8;
-            const uint4 x = ld_shared_v4(out.at + (uint32_t)i * 16);
-            if (v < c.cells_stride)
-              *reinterpret_cast<uint4 *>(c.cells + (int64_t)(half * (few / 2) + (i >> 2)) * c.cells_stride + v) = x;
-          }
-          __syncwarp();
-        }
+        // (a half without a 32 of its own)
+        if (32 * half >= n_rows) release();
       } else if constexpr (kMode == kForward || kMode == kNumerators) {
         // nothing reads what rows past the last one, rounded up to dW's slices, would leave
         if (row - lane >= (rows + kDepth - 1) / kDepth * kDepth) {
@@ -897,13 +971,8 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
       }
     }
     out.finish(lane);
-    if constexpr (kFew && kMode != kGradHidden) {
-      if (pair < work.units)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int t = half * (few / 2) + 32 * k + lane;
-          if (32 * k < few / 2 && t < rows) c.sums[(int64_t)((pair * 2 + (int)crank) * 4 + q) * c.chunk + t] = few_sums[k];
-        }
+    if constexpr (kSums) {
+      if (epilogue_agrees(!*abort)) join_quarters((local & 1) ^ 1);
     }
   }
 
@@ -921,11 +990,10 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
 // ---------------------------------------------------------------------------
 // 32 rows a CTA, a lane each; the column tiles' sums in 32 parts.  kForward: the
 // loss.  kNumerators: besides, the row's factor, the label's numerator and the
-// scaled row; `again`: only rows of the tiles that were run again (else a row whose
-// reference does not do marks its tile).  pairs: those that the few rows' product ran
-// with (its sums are a pair's), else 0.
+// scaled row; `again`: only rows of the tiles that were run again (roles swapped: all; else a row whose
+// reference does not do marks its tile).
 template <Mode kMode>
-__global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int again, int finish, int pairs) {
+__global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int again, int finish) {
   __shared__ float part_sum[32][33], part_most[32][33];
   __shared__ double total[32];
   __shared__ int last;
@@ -935,7 +1003,7 @@ __global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int ag
   if (again && __ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0) return;
   const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
   const int first = blockIdx.x * 32, tile = row0 / kTile + first / kTile;
-  const bool mine = first < (rows + kTile - 1) / kTile * kTile && (!again || __ldcg(c.flags + tile) != 0);
+  const bool mine = first < (rows + kTile - 1) / kTile * kTile && (!again || c.rows_tile != kTile || __ldcg(c.flags + tile) != 0);
   if (mine) {
     // a warp's row and what is known of it
     const int row = first + warp, at = row0 + row;
@@ -945,7 +1013,7 @@ __global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int ag
     const int t = live ? __ldcg(c.orig + at) : 0, y = live ? __ldcg(c.label + at) : -1;
     const float weight = live && c.row_weight ? __ldg(c.row_weight + t) : 1.0f;
     // a lane a row: every 32nd part
-    const int parts = pairs ? min(c.vocab_tiles, pairs) * 8 : c.vocab_tiles * 2;
+    const int parts = c.vocab_tiles * 2;
     float s = 0.0f, m = kFloor;
     const float2 *part = c.sums + first + lane;
 #pragma unroll 8
@@ -1065,14 +1133,14 @@ bool encode(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int6
 
 // Pairs that run at once (their CTAs' SMs lie in one cluster's reach); readies the
 // kernel on the current device.
-template <Mode kMode, bool kFew>
+template <Mode kMode, bool kSwapped>
 cudaError_t resident_pairs(int *pairs) {
   static std::atomic<int> known[64];
   int dev = 0;
   cudaError_t err = cudaGetDevice(&dev);
   if (err != cudaSuccess) return err;
   if (dev < 64 && (*pairs = known[dev].load(std::memory_order_acquire)) > 0) return cudaSuccess;
-  auto kernel = product_kernel<kMode, kFew>;
+  auto kernel = product_kernel<kMode, kSwapped>;
   err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmSmem);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
@@ -1094,15 +1162,15 @@ cudaError_t resident_pairs(int *pairs) {
   return cudaSuccess;
 }
 
-template <Mode kMode, bool kFew = false>
+template <Mode kMode, bool kSwapped = false>
 cudaError_t run_product(const Operands &maps, const Call &c, int chunk, int again, int join, cudaStream_t stream,
                         int *used = nullptr) {
   constexpr int kThreads = kGemmThreads + (kMode == kGradWeight ? kJoinThreads : 0);
   int pairs = 0;
-  const cudaError_t err = resident_pairs<kMode, kFew>(&pairs);
+  const cudaError_t err = resident_pairs<kMode, kSwapped>(&pairs);
   if (err != cudaSuccess) return err;
   if (used) *used = pairs;
-  return launch_chained(product_kernel<kMode, kFew>, dim3(2 * pairs), dim3(kThreads), kGemmSmem, stream, 2,
+  return launch_chained(product_kernel<kMode, kSwapped>, dim3(2 * pairs), dim3(kThreads), kGemmSmem, stream, 2,
                         true, maps, c, chunk, again, join, kDefaultWaitLimitNs);
 }
 
@@ -1120,6 +1188,7 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   c.T = a.rows; c.H = a.width; c.V = a.vocab;
   c.rows_pad = l.rows_pad; c.chunk = l.chunk;
   c.vocab_tiles = l.vocab_tiles; c.hidden_tiles = l.hidden_tiles;
+  c.rows_tile = l.rows_tile ? l.rows_tile : kTile;
   c.cells_stride = l.cells_stride;
   c.ctrl = reinterpret_cast<int32_t *>(w + l.ctrl);
   c.counts = reinterpret_cast<int32_t *>(w + l.counts);
@@ -1144,16 +1213,16 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
 
   Operands logits = {}, dh = {}, dw = {};
   // (rows past the call's are zeros without being read)
-  const bool few = c.T <= kFewRows;
-  const int few_half = (c.T <= kFewRows / 2 ? kFewRows / 2 : kFewRows) / 2;  // a CTA's rows of N
-  bool ok = encode(few ? &logits.b : &logits.a, c.rows, c.T, c.H, c.H, few ? few_half : kHalf) &&
-            encode(few ? &logits.a : &logits.b, c.weight, c.V, c.H, c.weight_stride, kHalf);
-  if (grad && !few) ok = ok && encode(&logits.out, c.cells, l.chunk, l.cells_stride, l.cells_stride, 32);
+  const bool swapped = l.rows_tile > 0;
+  const int half = c.rows_tile / 2;  // a CTA's rows of a tile
+  bool ok = encode(swapped ? &logits.b : &logits.a, c.rows, c.T, c.H, c.H, half) &&
+            encode(swapped ? &logits.a : &logits.b, c.weight, c.V, c.H, c.weight_stride, kHalf);
+  if (grad && !swapped) ok = ok && encode(&logits.out, c.cells, l.chunk, l.cells_stride, l.cells_stride, 32);
   // (rows of the numerators past the call's, rounded up to dW's slices, are never written)
   const int cell_rows = ceil_div(c.T, kDepth) * kDepth < l.chunk ? ceil_div(c.T, kDepth) * kDepth : l.chunk;
   if (a.grad_hidden)  // e along the vocabulary, the head across it
-    ok = ok && encode(few ? &dh.b : &dh.a, c.cells, cell_rows, c.V, l.cells_stride, few ? few_half : kHalf) &&
-         encode(few ? &dh.a : &dh.b, c.weight, c.V, c.H, c.weight_stride, kDepth);
+    ok = ok && encode(swapped ? &dh.b : &dh.a, c.cells, cell_rows, c.V, l.cells_stride, half) &&
+         encode(swapped ? &dh.a : &dh.b, c.weight, c.V, c.H, c.weight_stride, kDepth);
   if (a.grad_weight)  // both across the rows
     ok = ok && encode(&dw.a, c.cells, cell_rows, c.V, l.cells_stride, kDepth) &&
          encode(&dw.b, c.scaled, l.chunk, c.H, c.H, kDepth) &&
@@ -1170,23 +1239,22 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   for (int k = 0; k < l.chunks && err == cudaSuccess; ++k) {
     const dim3 sum_grid((unsigned)(l.chunk / 32));
     const int finish = k == l.chunks - 1;
-    int used = 0;
     if (!grad) {
-      err = few ? run_product<kForward, true>(logits, c, k, 0, 0, stream, &used)
+      err = swapped ? run_product<kForward, true>(logits, c, k, 0, 0, stream)
                 : run_product<kForward>(logits, c, k, 0, 0, stream);
       if (err == cudaSuccess)
-        err = launch_chained(sums_kernel<kForward>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, 0, finish, used);
+        err = launch_chained(sums_kernel<kForward>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, 0, finish);
       continue;
     }
     for (int again = 0; again < 2 && err == cudaSuccess; ++again) {
-      err = few ? run_product<kNumerators, true>(logits, c, k, again, 0, stream, &used)
+      err = swapped ? run_product<kNumerators, true>(logits, c, k, again, 0, stream)
                 : run_product<kNumerators>(logits, c, k, again, 0, stream);
       if (err == cudaSuccess)
-        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again, 0, used);
+        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again, 0);
     }
     int pairs = 0;
     if (a.grad_hidden && err == cudaSuccess) {
-      err = few ? run_product<kGradHidden, true>(dh, c, k, 0, 0, stream, &pairs)
+      err = swapped ? run_product<kGradHidden, true>(dh, c, k, 0, 0, stream, &pairs)
                 : run_product<kGradHidden>(dh, c, k, 0, 0, stream, &pairs);
       if (err == cudaSuccess && !a.grad_weight)
         err = launch_chained(join_kernel, dim3(kSms * 8), dim3(256), 0, stream, 1, true, c, k, pairs, finish);

@@ -390,6 +390,7 @@ def _check_loss(hidden, weight, labels, row_weight, dh_out=True, dw_out=True, **
 @pytest.mark.parametrize("rows,width,vocab", [
     (1, 8, 1), (1, 64, 2), (3, 16, 7), (5, 128, 255), (17, 72, 256), (64, 64, 257), (255, 136, 1000), (256, 256, 513),
     (63, 40, 9), (64, 72, 511), (65, 200, 777), (128, 328, 1025), (129, 64, 600), (100, 2056, 130),
+    (150, 520, 777), (640, 576, 1500), (890, 512, 300),
     (257, 264, 300), (300, 520, 2049), (513, 1032, 700), (64, 4096, 1500), (1021, 128, 5003), (40, 16384, 130)])
 def test_linear_loss(rows, width, vocab):
     _check_loss(*_head(rows, width, vocab, seed=rows + vocab))
@@ -443,18 +444,19 @@ def test_linear_loss_rows_without_labels():
     assert float(loss) == 0 and dh.shape == (0, 64) and bool((dw == 0).all())
 
 
-def test_linear_loss_of_labels_that_are_sure_or_impossible():
+@pytest.mark.parametrize("width,rows", [(64, 700), (512, 595)])
+def test_linear_loss_of_labels_that_are_sure_or_impossible(width, rows):
     # label's logit 40 above the others, as high as they, and 50, 70, 100 and 500 below the largest
-    width, vocab = 64, 3000
+    vocab = 3000
     weight = torch.zeros((vocab, width), dtype=BF16, device=DEV)
     weight[:, 1:] = (_randn(vocab, width - 1, seed=1) * 0.1).to(BF16)
     weight[5, 0], weight[2000, 0] = 1.0, -1.0
-    hidden = (_randn(700, width, seed=2) * 0.3).to(BF16)
-    scale = torch.tensor([40.0, 0.0, 25.0, 35.0, 50.0, 250.0, 3.0], device=DEV).repeat(100)
+    hidden = (_randn(rows, width, seed=2) * 0.3).to(BF16)
+    scale = torch.tensor([40.0, 0.0, 25.0, 35.0, 50.0, 250.0, 3.0], device=DEV).repeat(rows // 7)
     hidden[:, 0] = scale.to(BF16)
-    labels = torch.full((700,), 2000, dtype=torch.int32, device=DEV)
+    labels = torch.full((rows,), 2000, dtype=torch.int32, device=DEV)
     labels[::7] = 5
-    wt = 0.1 + torch.rand(700, generator=_gen(3), device=DEV)
+    wt = 0.1 + torch.rand(rows, generator=_gen(3), device=DEV)
     _check_loss(hidden, weight, labels, wt)
     _check_loss(hidden, weight, labels, wt, dh_out=False, dw_out=False)
     # one such row among others: only its tile is taken again
@@ -462,10 +464,10 @@ def test_linear_loss_of_labels_that_are_sure_or_impossible():
     labels[300] = 2000
     _check_loss(hidden, weight, labels, wt)
     # few rows
-    for rows in (7, 100):
-        labels[:rows] = 2000
-        _check_loss(hidden[:rows], weight, labels[:rows], wt[:rows])
-        _check_loss(hidden[:rows], weight, labels[:rows], wt[:rows], dh_out=False, dw_out=False)
+    for n in (7, 100):
+        labels[:n] = 2000
+        _check_loss(hidden[:n], weight, labels[:n], wt[:n])
+        _check_loss(hidden[:n], weight, labels[:n], wt[:n], dh_out=False, dw_out=False)
 
 
 def test_linear_loss_of_what_is_no_number_and_of_labels_outside():
