@@ -593,7 +593,11 @@ def _matrix(t, name, dtype=None, shape=None, index=None):
 def _rows_out(out, name, like, shape, index, stream):
     """(output, pointer, row stride): the given one, or a new one of `like`'s type."""
     if out is None:
-        out = _new(stream, shape, like.dtype, like.device)
+        # (empty_like takes half of empty's time)
+        if stream is None and like.shape == shape and like.is_contiguous():
+            out = torch.empty_like(like)
+        else:
+            out = _new(stream, shape, like.dtype, like.device)
         return out, out.data_ptr(), shape[1]
     args = _matrix(out, name, like.dtype, shape, index)
     return out, args[0], args[4]
@@ -741,17 +745,16 @@ def slimwise_linear_loss(hidden, weight, labels, row_weight=None, grad_hidden=Tr
     p_labels = _vec(labels, _I32, one, "labels", dev)
     p_weight = None if row_weight is None else _vec(row_weight, _F32, one, "row_weight", dev)
 
-    def gradient(g, shape, name, dtype):
-        if g is False or g is None:
-            return None, None, 0, 0
-        if g is True:
-            g = _new(stream, shape, bf16, hidden.device)
-            return g, g.data_ptr(), 0, width
-        ptr, code, _, _, stride = _matrix(g, name, dtype, shape, dev)
-        return g, ptr, code, stride
-
-    dh, dh_ptr, _, dh_stride = gradient(grad_hidden, (rows, width), "grad_hidden", bf16)
-    dw, dw_ptr, dw_code, dw_stride = gradient(grad_weight, (vocab, width), "grad_weight", None)
+    dh = dw = dh_ptr = dw_ptr = None
+    dh_stride = dw_stride = dw_code = 0
+    if grad_hidden is not False and grad_hidden is not None:
+        dh, dh_ptr, dh_stride = _rows_out(None if grad_hidden is True else grad_hidden, "grad_hidden", hidden,
+                                          (rows, width), dev, stream)
+    if grad_weight is True:
+        dw, dw_ptr, dw_stride = _rows_out(None, "grad_weight", weight, (vocab, width), dev, stream)
+    elif grad_weight is not False and grad_weight is not None:
+        dw = grad_weight
+        dw_ptr, dw_code, _, _, dw_stride = _matrix(dw, "grad_weight", None, (vocab, width), dev)
     if row_loss is None:
         row_loss = _new(stream, one, _F32, hidden.device)
     if loss is None:
