@@ -21,8 +21,18 @@ layer.  A step:
     dgamma   = sum over tokens of (dz head) * y / rms(y);  Adam
 
 and in the end the student answers: slimwise_sample draws each row's next token.
+evaluate() is the cross entropy of either model on given next tokens, without its
+logits (slimwise_norm, slimwise_linear_loss).
 
-    python -m paper_2609_34117_gb300.distill [--steps 30] [--vocab 32000]
+The model's ends can be trained on text first (pretrain(), --pretrain steps): the
+embedding, the norm and the head alone are a bigram model, whose gradients the
+library has in full:
+
+    h = slimwise_embed(tokens);  n = slimwise_norm(h)
+    loss, dn, dhead = slimwise_linear_loss(n, head, labels)
+    dh, dgamma = slimwise_norm_grad(dn);  dembed = slimwise_embed_grad(dh, tokens)
+
+    python -m paper_2609_34117_gb300.distill [--steps 30] [--vocab 32000] [--pretrain 0]
 """
 from __future__ import annotations
 
@@ -66,15 +76,19 @@ class Model:
     def normed(self, tokens, full):
         """y / rms(y) of the layer's output, fp32 [B, H]: the full pool's, or the
         retained pool's with the shared expert."""
-        h = self.embed[tokens]
+        y = self.output(tokens, full)
+        return y / y.square().mean(1, keepdim=True).sqrt()
+
+    def output(self, tokens, full):
+        """The layer's output with its residual, fp32 [B, H]."""
+        h = binding.slimwise_embed(self.embed, tokens.int())
         args = (h, self.router)
         if full:
             out = binding.slimwise_moe_decode_full(*args, self.w_gate_up, self.w_down, self.shape.top_k)
         else:
             out = binding.slimwise_moe_decode_shared(*args, self.retained, self.w_gate_up, self.w_down,
                                                      self.shape.top_k, *self.shared)
-        y = h.float() + out.float()
-        return y / y.square().mean(1, keepdim=True).sqrt()
+        return h.float() + out.float()
 
     def logits(self, normed, gamma):
         return (normed * gamma).to(torch.bfloat16) @ self.head.T
@@ -108,6 +122,46 @@ def distill(model: Model, steps=30, batch=256, k=64, alpha=0.1, temperature=1.0,
     return gamma, torch.cat(losses).tolist()
 
 
+def evaluate(model: Model, gamma, tokens, labels, full):
+    """Mean cross entropy of the full pool's or the retained pool's model at labels
+    (int32; negative: no label), fp32 [1]."""
+    n, _, _ = binding.slimwise_norm(model.output(tokens, full), gamma, eps=0.0)
+    weight = (labels >= 0).float() / (labels >= 0).sum()
+    return binding.slimwise_linear_loss(n.to(torch.bfloat16), model.head, labels, row_weight=weight,
+                                        grad_hidden=False, grad_weight=False)[0]
+
+
+def bigram_gradients(embed, gamma, head, tokens, labels, eps=1e-5):
+    """Loss and gradients of the model's ends without the layer: (loss fp32 [1],
+    gradients of the embedding fp32 [V, H], of gamma fp32 [H], of the head fp32 [V, H])."""
+    weight = (labels >= 0).float() / (labels >= 0).sum()
+    h = binding.slimwise_embed(embed, tokens)
+    n, _, rstd = binding.slimwise_norm(h, gamma, eps=eps)
+    fp32 = lambda t: torch.empty(t.shape, dtype=torch.float32, device=t.device)
+    loss, _, dn, dhead = binding.slimwise_linear_loss(n, head, labels, row_weight=weight, grad_weight=fp32(head))
+    dh, dgamma, _ = binding.slimwise_norm_grad(dn, h, gamma, rstd)
+    return loss, binding.slimwise_embed_grad(dh, tokens, fp32(embed)), dgamma, dhead
+
+
+def pretrain(model: Model, steps, batch=256, lr=0.5, seed=2):
+    """Trains the embedding, gamma and the head in place on a seeded text in which each
+    token has one successor; returns the loss of each step."""
+    dev = model.gamma.device
+    vocab = model.embed.shape[0]
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+    successor = torch.randperm(vocab, generator=g, device=dev).int()
+    losses = []
+    for _ in range(steps):
+        tokens = torch.randint(0, vocab, (batch,), generator=g, device=dev, dtype=torch.int32)
+        labels = successor[tokens.long()]
+        loss, dembed, dgamma, dhead = bigram_gradients(model.embed, model.gamma, model.head, tokens, labels)
+        for w, d in ((model.embed, dembed), (model.gamma, dgamma), (model.head, dhead)):
+            w.copy_(w.float() - lr * d)
+        losses.append(loss)
+    return torch.cat(losses).tolist() if losses else []
+
+
 def answer(model: Model, gamma, tokens, uniform, temperature=0.7, top_k=20, top_p=0.8):
     """The student's next token of each row, and its log-probability."""
     rows = tokens.shape[0]
@@ -122,13 +176,22 @@ def main():
     ap.add_argument("--steps", type=int, default=30)
     ap.add_argument("--batch", type=int, default=256)
     ap.add_argument("--vocab", type=int, default=32000)
+    ap.add_argument("--pretrain", type=int, default=0, help="steps of training the model's ends first")
     a = ap.parse_args()
     model = Model.random(vocab=a.vocab)
+    if a.pretrain:
+        first = pretrain(model, a.pretrain)
+        print(f"bigram loss {first[0]:.4f} ... {first[-1]:.4f}")
     gamma, losses = distill(model, a.steps, a.batch)
     print("loss", " ".join(f"{x:.4f}" for x in losses[::max(1, a.steps // 10)]), f"... {losses[-1]:.4f}")
     prompt = torch.arange(8, device="cuda")
     uniform = torch.rand(8, generator=torch.Generator(device="cuda").manual_seed(7), device="cuda")
     tokens, logprob = answer(model, gamma, prompt, uniform)
+    held_out = torch.arange(0, min(a.vocab, 4096), device="cuda")
+    likeliest = binding.slimwise_top_logits(model.logits(model.normed(held_out, True), model.gamma), 1)[0][:, 0]
+    entropy = lambda gamma, full: float(evaluate(model, gamma, held_out, likeliest.contiguous(), full))
+    print(f"cross entropy at the teacher's likeliest tokens: teacher {entropy(model.gamma, True):.4f}, student "
+          f"{entropy(model.gamma, False):.4f}, distilled {entropy(gamma, False):.4f}")
     print("answers", tokens.tolist(), "log-probabilities", [round(x, 3) for x in logprob.tolist()])
 
 
