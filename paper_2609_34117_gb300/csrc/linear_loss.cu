@@ -81,6 +81,13 @@ struct Layout {
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// bf16 parts of a scaled row in dW's contraction.  Its product with the label's exact
+// numerator is most of a row of dW, so that its rounding is most of dW's error.  Up to
+// 128 rows, where dW's product waits for memory, a second part holds the rest (for 64
+// rows of 32000 words at 1024 dW's error against 64 bits 0.0023 -> 0.0017, its rounding to
+// bf16 alone).
+__host__ __device__ inline int scaled_parts(int rows) { return rows <= 128 ? 2 : 1; }
+
 // N of the products with swapped roles, or 0: rows are M, in tiles of 256.  The swapped
 // epilogue takes twice the instructions: products along short rows keep the others
 // unless they have few of them.
@@ -131,7 +138,7 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
   l.scale = take(n * 4);
   l.flags = take(n / kTile * 3 * 4);
   l.rows = take(n * hidden * 2);
-  l.scaled = take(grad_weight ? (size_t)l.chunk * hidden * 2 : 0);
+  l.scaled = take(grad_weight ? (size_t)l.chunk * scaled_parts(rows) * hidden * 2 : 0);
   l.sums = take((size_t)l.vocab_tiles * 2 * l.chunk * sizeof(float2));
   l.cells = take(grad ? (size_t)l.chunk * l.cells_stride * 2 : 0);
   l.splits = take((size_t)l.split_tiles * kTile * kTile * 4);
@@ -652,7 +659,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
   } else {
     work.mt = c.vocab_tiles;
     work.nt = c.hidden_tiles;
-    work.kb = (rows + kDepth - 1) / kDepth;
+    work.kb = (rows + kDepth - 1) / kDepth * scaled_parts(c.T);
     work.units = rows > 0 ? work.mt * work.nt : 0;
     if (rows == 0 && chunk == 0) {
       // no labelled row at all: zeros (16 bytes are 8 elements, or 4)
@@ -703,19 +710,23 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
           break;
         }
         const uint32_t a = smem_base + (uint32_t)(stage * slot_bytes), b = a + kOperandBytes;
+        // (dW: the numerators again for the scaled rows' second part)
+        const int half_k = kMode == kGradWeight && scaled_parts(c.T) > 1 ? work.kb / 2 : work.kb;
+        const int ka = kMode == kGradWeight && k >= half_k ? k - half_k : k;
+        const int kb_row = ka * kDepth + (ka != k ? c.chunk : 0);
         if (elect_one()) {
           const uint32_t bar = mapa_shared(full_bar(stage), 0u);
           if (lead)
             mbar_arrive_expect_tx(full_bar(stage), 2 * slot_bytes);
           if constexpr (kAcrossA) {
-            tma_load_2d_pair(a, &maps.a, bar, a0, k * kDepth, policy);
-            tma_load_2d_pair(a + kOperandBytes / 2, &maps.a, bar, a0 + 64, k * kDepth, policy);
+            tma_load_2d_pair(a, &maps.a, bar, a0, ka * kDepth, policy);
+            tma_load_2d_pair(a + kOperandBytes / 2, &maps.a, bar, a0 + 64, ka * kDepth, policy);
           } else {
             tma_load_2d_pair(a, &maps.a, bar, k * kDepth, a0, policy);
           }
           if constexpr (kAcrossB) {
-            tma_load_2d_pair(b, &maps.b, bar, b0, k * kDepth, policy);
-            tma_load_2d_pair(b + kOperandBytes / 2, &maps.b, bar, b0 + 64, k * kDepth, policy);
+            tma_load_2d_pair(b, &maps.b, bar, b0, kb_row, policy);
+            tma_load_2d_pair(b + kOperandBytes / 2, &maps.b, bar, b0 + 64, kb_row, policy);
           } else {
             tma_load_2d_pair(b, &maps.b, bar, k * kDepth, b0, policy);
           }
@@ -1068,12 +1079,16 @@ __global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int ag
         uint4 *to = reinterpret_cast<uint4 *>(c.scaled + (int64_t)row * c.H);
 #pragma unroll 4
         for (int k = lane; k < c.H / 8; k += 32) {
-          uint4 v = live ? __ldcg(from + k) : make_uint4(0, 0, 0, 0);
-          uint32_t *x = reinterpret_cast<uint32_t *>(&v);
+          uint4 v = live ? __ldcg(from + k) : make_uint4(0, 0, 0, 0), rest;
+          uint32_t *x = reinterpret_cast<uint32_t *>(&v), *y2 = reinterpret_cast<uint32_t *>(&rest);
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            x[q] = pack_bf16(__uint_as_float(x[q] << 16) * scale, __uint_as_float(x[q] & 0xFFFF0000u) * scale);
+          for (int q = 0; q < 4; ++q) {
+            const float lo = __uint_as_float(x[q] << 16) * scale, hi = __uint_as_float(x[q] & 0xFFFF0000u) * scale;
+            x[q] = pack_bf16(lo, hi);
+            y2[q] = pack_bf16(lo - __uint_as_float(x[q] << 16), hi - __uint_as_float(x[q] & 0xFFFF0000u));
+          }
           to[k] = v;
+          if (scaled_parts(c.T) > 1) to[k + (int64_t)c.chunk * (c.H / 8)] = rest;
         }
       }
     }
@@ -1225,7 +1240,7 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
          encode(swapped ? &dh.a : &dh.b, c.weight, c.V, c.H, c.weight_stride, kDepth);
   if (a.grad_weight)  // both across the rows
     ok = ok && encode(&dw.a, c.cells, cell_rows, c.V, l.cells_stride, kDepth) &&
-         encode(&dw.b, c.scaled, l.chunk, c.H, c.H, kDepth) &&
+         encode(&dw.b, c.scaled, (int64_t)l.chunk * scaled_parts(c.T), c.H, c.H, kDepth) &&
          (c.dw_fp32 || encode(&dw.out, c.dw, c.V, c.H, c.dw_stride, 32));
   if (!ok) return cudaErrorInvalidValue;
 
