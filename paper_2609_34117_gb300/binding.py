@@ -583,7 +583,7 @@ def _matrix(t, name, dtype=None, shape=None, index=None):
     args = _logits(t, name)
     if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and t.shape != shape:
+    if shape is not None and (args[2], args[3]) != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if index is not None and t.get_device() != index:
         raise ValueError(f"{name} must be on cuda:{index}")
@@ -601,6 +601,18 @@ def _rows_out(out, name, like, shape, index, stream):
         return out, out.data_ptr(), shape[1]
     args = _matrix(out, name, like.dtype, shape, index)
     return out, args[0], args[4]
+
+
+def _vec_out(out, name, shape, index, stream, device, like=None):
+    """(fp32 vector, pointer): the given one, or a new one (where `like` has its shape
+    and type, by empty_like)."""
+    if out is not None:
+        return out, _vec(out, _F32, shape, name, index)
+    if like is not None and stream is None:
+        out = torch.empty_like(like)
+    else:
+        out = _new(stream, shape, _F32, device)
+    return out, out.data_ptr()
 
 
 @functools.lru_cache(maxsize=1024)
@@ -665,19 +677,17 @@ def slimwise_norm(x, weight, bias=None, layer=False, eps=1e-5, y=None, mean=None
     None for RMS norm, rstd fp32 [rows]); the last two are what the gradient needs."""
     ptr, code, rows, hidden, stride = _matrix(x, "x")
     dev, one, width = x.get_device(), (rows,), (hidden,)
+    p_weight = _vec(weight, _F32, width, "weight", dev)
+    p_bias = None if bias is None else _vec(bias, _F32, width, "bias", dev)
     y, y_ptr, y_stride = _rows_out(y, "y", x, (rows, hidden), dev, stream)
-    if rstd is None:
-        rstd = _new(stream, one, _F32, x.device)
-    if not layer:
-        if mean is not None:
-            raise ValueError("mean is layer norm's")
-    elif mean is None:
-        mean = _new(stream, one, _F32, x.device)
-    _check(load().slimwise_norm(
-        ptr, code, rows, hidden, stride, _vec(weight, _F32, width, "weight", dev),
-        None if bias is None else _vec(bias, _F32, width, "bias", dev), int(bool(layer)), eps, y_ptr, y_stride,
-        None if mean is None else _vec(mean, _F32, one, "mean", dev), _vec(rstd, _F32, one, "rstd", dev),
-        _stream(stream)), "slimwise_norm")
+    rstd, p_rstd = _vec_out(rstd, "rstd", one, dev, stream, x.device)
+    p_mean = None
+    if layer:
+        mean, p_mean = _vec_out(mean, "mean", one, dev, stream, x.device, rstd)
+    elif mean is not None:
+        raise ValueError("mean is layer norm's")
+    _check(load().slimwise_norm(ptr, code, rows, hidden, stride, p_weight, p_bias, 1 if layer else 0, eps, y_ptr,
+                                y_stride, p_mean, p_rstd, _stream(stream)), "slimwise_norm")
     return y, mean, rstd
 
 
@@ -700,19 +710,19 @@ def slimwise_norm_grad(dy, x, weight, rstd, mean=None, grad_bias=None, dx=None, 
         raise ValueError("the bias has a gradient in layer norm alone")
     if dbias is not None and not grad_bias:
         raise ValueError("dbias is given, but not wanted")
+    p_weight = _vec(weight, _F32, width, "weight", dev)
+    p_rstd = _vec(rstd, _F32, one, "rstd", dev)
+    p_mean = None if mean is None else _vec(mean, _F32, one, "mean", dev)
     dx, dx_ptr, dx_stride = _rows_out(dx, "dx", x, (rows, hidden), dev, stream)
-    if dweight is None:
-        dweight = _new(stream, width, _F32, x.device)
-    if grad_bias and dbias is None:
-        dbias = _new(stream, width, _F32, x.device)
+    dweight, p_dweight = _vec_out(dweight, "dweight", width, dev, stream, x.device, weight)
+    p_dbias = None
+    if grad_bias:
+        dbias, p_dbias = _vec_out(dbias, "dbias", width, dev, stream, x.device, weight)
     lib = load()
     workspace, w, n = _scratch(workspace, _workspace_bytes("norm_grad", rows, hidden), stream, x.device)
     _check(lib.slimwise_norm_grad(
-        d[0], d[4], ptr, code, rows, hidden, stride, _vec(weight, _F32, width, "weight", dev),
-        None if mean is None else _vec(mean, _F32, one, "mean", dev), _vec(rstd, _F32, one, "rstd", dev),
-        dx_ptr, dx_stride, _vec(dweight, _F32, width, "dweight", dev),
-        None if dbias is None else _vec(dbias, _F32, width, "dbias", dev), _stream(stream), w, n),
-        "slimwise_norm_grad")
+        d[0], d[4], ptr, code, rows, hidden, stride, p_weight, p_mean, p_rstd, dx_ptr, dx_stride, p_dweight,
+        p_dbias, _stream(stream), w, n), "slimwise_norm_grad")
     if rows == 0:  # the sums over no rows are not computed by a kernel
         with torch.cuda.stream(stream):
             dweight.zero_()
@@ -755,17 +765,14 @@ def slimwise_linear_loss(hidden, weight, labels, row_weight=None, grad_hidden=Tr
     elif grad_weight is not False and grad_weight is not None:
         dw = grad_weight
         dw_ptr, dw_code, _, _, dw_stride = _matrix(dw, "grad_weight", None, (vocab, width), dev)
-    if row_loss is None:
-        row_loss = _new(stream, one, _F32, hidden.device)
-    if loss is None:
-        loss = _new(stream, (1,), _F32, hidden.device)
+    row_loss, p_row_loss = _vec_out(row_loss, "row_loss", one, dev, stream, hidden.device, row_weight)
+    loss, p_loss = _vec_out(loss, "loss", (1,), dev, stream, hidden.device)
     lib = load()
     workspace, ws, n = _scratch(workspace, _workspace_bytes("linear_loss", rows, width, vocab, int(dh is not None),
                                                             int(dw is not None)), stream, hidden.device)
     _check(lib.slimwise_linear_loss(
-        h_ptr, h_stride, w_ptr, w_stride, rows, width, vocab, p_labels, p_weight,
-        _vec(row_loss, _F32, one, "row_loss", dev), _vec(loss, _F32, (1,), "loss", dev), dh_ptr, dh_stride,
-        dw_ptr, dw_code, dw_stride, _stream(stream), ws, n), "slimwise_linear_loss")
+        h_ptr, h_stride, w_ptr, w_stride, rows, width, vocab, p_labels, p_weight, p_row_loss, p_loss, dh_ptr,
+        dh_stride, dw_ptr, dw_code, dw_stride, _stream(stream), ws, n), "slimwise_linear_loss")
     if rows == 0:  # the sums over no rows are not computed by a kernel
         with torch.cuda.stream(stream):
             loss.zero_()
