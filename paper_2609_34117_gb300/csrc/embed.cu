@@ -8,12 +8,13 @@
 //
 // The gradient's order of summation must not depend on timing, so there are no
 // atomics on it.  One cluster sorts the positions by token (a stable radix sort
-// in two or three passes, histograms in shared memory) while the other CTAs
-// write the zeros of the tokens that do not occur; each of those finds its
-// tokens' presence by reading all ids.  The next kernel sums the sorted rows in
-// pieces of some positions: a token that lies inside a piece is written, one
-// that crosses its border leaves fp32 sums, which a third kernel adds in order.
-// A token that occurs thousands of times is so spread over hundreds of CTAs.
+// in two or three passes, histograms in shared memory).  The next kernel sums the
+// sorted rows in pieces of some positions: a token that lies inside a piece is
+// written, one that crosses its border leaves fp32 sums, which a third kernel adds
+// in order.  A token that occurs thousands of times is so spread over hundreds of
+// CTAs.  Most of the time is the zeros of the tokens that do not occur.  CTAs of the second
+// and third kernel write them, which find their tokens' presence by reading all ids
+// and wait for no kernel: they run beside the sort, the sums and the joins.
 #include "train.cuh"
 
 namespace slimwise {
@@ -171,40 +172,46 @@ __device__ void sort_by_id(const SortArgs &s, SortShared &sh) {
   }
 }
 
-// Cluster 0 sorts; the CTAs of the others share the table's rows and write the
-// zeros of those without a token (`zero`: else there are no others).
-template <typename O>
-__global__ void __launch_bounds__(kSortThreads)
-    embed_sort_kernel(SortArgs s, O *__restrict__ out, int hidden, int64_t out_stride) {
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs s) {
   extern __shared__ __align__(16) unsigned char smem[];
   pdl_launch_dependents();
-  if (blockIdx.x < kSortCtas) {
-    sort_by_id(s, *reinterpret_cast<SortShared *>(smem));
-    return;
-  }
-  uint32_t *present = reinterpret_cast<uint32_t *>(smem);
-  const int ctas = gridDim.x - kSortCtas, per = (s.vocab + ctas - 1) / ctas;
-  const int64_t first = (int64_t)(blockIdx.x - kSortCtas) * per;
-  const int lo = (int)(first < s.vocab ? first : s.vocab);
-  const int rows = min(per, s.vocab - lo);
-  for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) present[i] = 0u;
-  __syncthreads();
-#pragma unroll 8
-  for (int i = threadIdx.x; i < s.n; i += kSortThreads) {
-    const int r = __ldg(s.ids + i) - lo;
-    if (r >= 0 && r < rows) atomicOr(present + (r >> 5), 1u << (r & 31));
-  }
-  __syncthreads();
-  const int lane = threadIdx.x & 31;
-  for (int r = threadIdx.x >> 5; r < rows; r += kSortWarps) {
-    if (present[r >> 5] >> (r & 31) & 1) continue;
-    // whole windows of the row, its ends by element (by element alone 3.2 TB/s of bf16)
-    const uintptr_t start = reinterpret_cast<uintptr_t>(out + (int64_t)(lo + r) * out_stride);
-    const uintptr_t end = start + (uintptr_t)hidden * sizeof(O);
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    for (uintptr_t w = (start & ~(uintptr_t)15) + 16 * (uintptr_t)lane; w < end; w += 512) {
-      if (w >= start && w + 16 <= end) *reinterpret_cast<uint4 *>(w) = zero;
-      else write_edge<O>(zero, w, start, end);
+  sort_by_id(s, *reinterpret_cast<SortShared *>(smem));
+}
+
+// Zeros for the tokens of [from, to) that do not occur: the share of CTA `cta` of
+// `ctas`, kSumThreads threads each.
+constexpr int kZeroCtas = 2 * kSms, kZeroRows = 4096;
+struct ZeroArgs {
+  const int32_t *ids;
+  int ctas, from, to;  // 0 CTAs: none
+};
+template <typename O>
+__device__ void write_zeros(const ZeroArgs &z, int n, int hidden, O *out, int64_t out_stride) {
+  __shared__ uint32_t present[kZeroRows / 32];
+  const int lane = threadIdx.x & 31, per = (z.to - z.from + z.ctas - 1) / z.ctas;
+  const int64_t first = z.from + (int64_t)blockIdx.x * per;
+  const int end_row = (int)(first + per < z.to ? first + per : z.to);
+  for (int lo = (int)first; lo < end_row; lo += kZeroRows) {
+    const int rows = min(kZeroRows, end_row - lo);
+    __syncthreads();
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSumThreads) present[i] = 0u;
+    __syncthreads();
+#pragma unroll 16
+    for (int i = threadIdx.x; i < n; i += kSumThreads) {
+      const int r = __ldg(z.ids + i) - lo;
+      if (r >= 0 && r < rows) atomicOr(present + (r >> 5), 1u << (r & 31));
+    }
+    __syncthreads();
+    for (int r = threadIdx.x >> 5; r < rows; r += kSumThreads / 32) {
+      if (present[r >> 5] >> (r & 31) & 1) continue;
+      // whole windows of the row, its ends by element (by element alone 3.2 TB/s of bf16)
+      const uintptr_t start = reinterpret_cast<uintptr_t>(out + (int64_t)(lo + r) * out_stride);
+      const uintptr_t end = start + (uintptr_t)hidden * sizeof(O);
+      const uint4 zero = make_uint4(0, 0, 0, 0);
+      for (uintptr_t w = (start & ~(uintptr_t)15) + 16 * (uintptr_t)lane; w < end; w += 512) {
+        if (w >= start && w + 16 <= end) *reinterpret_cast<uint4 *>(w) = zero;
+        else write_edge<O>(zero, w, start, end);
+      }
     }
   }
 }
@@ -213,6 +220,7 @@ struct SumArgs {
   const uint2 *items;  // sorted
   int n, piece, vocab, hidden;
   int64_t stride, out_stride;
+  ZeroArgs zero;  // by the first CTAs of a kernel
   float scale;
   bool accumulate;
   float *partial;  // [pieces][2][hidden]: of the run from the piece before, of the run into the next
@@ -242,7 +250,12 @@ __global__ void __launch_bounds__(kSumThreads)
     embed_sum_kernel(const T *__restrict__ grad, SumArgs a, O *out) {
   constexpr int kLoads = 4;
   const int t = threadIdx.x % TPR;
-  const int piece = blockIdx.x * (kSumThreads / TPR) + threadIdx.x / TPR;
+  if ((int)blockIdx.x < a.zero.ctas) {
+    pdl_launch_dependents();
+    if (blockIdx.y == 0) write_zeros(a.zero, a.n, a.hidden, out, a.out_stride);
+    return;
+  }
+  const int piece = ((int)blockIdx.x - a.zero.ctas) * (kSumThreads / TPR) + threadIdx.x / TPR;
   const int c0 = blockIdx.y * TPR * 8, width = a.hidden - c0;
   pdl_wait_primary();
   pdl_launch_dependents();
@@ -297,7 +310,12 @@ __global__ void __launch_bounds__(kSumThreads)
 template <typename O, int V, int TPR>
 __global__ void __launch_bounds__(kSumThreads, 1) embed_join_kernel(SumArgs a, O *out) {
   const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
-  const int piece = blockIdx.x * (kSumThreads / TPR) + threadIdx.x / TPR;
+  if ((int)blockIdx.x < a.zero.ctas) {
+    pdl_launch_dependents();
+    if (blockIdx.y == 0) write_zeros(a.zero, a.n, a.hidden, out, a.out_stride);
+    return;
+  }
+  const int piece = ((int)blockIdx.x - a.zero.ctas) * (kSumThreads / TPR) + threadIdx.x / TPR;
   const int c0 = blockIdx.y * TPR * 8, width = a.hidden - c0;
   pdl_wait_primary();
   pdl_launch_dependents();
@@ -361,14 +379,31 @@ int piece_rows(int rows) {
 
 size_t items_bytes(int rows) { return align_up((size_t)rows * sizeof(uint2), 256); }
 
+// The tokens whose zeros the joining kernel writes, the last of the table: a few
+// microseconds' worth, as long as its joins wait for their loads, and none where many ids
+// would have to be read for them.
+int zeros_of_joins(int rows, int pieces, int hidden, int vocab, int element_bytes) {
+  if (pieces < 2 || rows > 65536) return 0;
+  const int64_t most = ((int64_t)40 << 20) / ((int64_t)hidden * element_bytes);
+  return (int)(most < vocab / 5 ? most : vocab / 5);
+}
+
 template <typename T, typename O, int V, int TPR>
-cudaError_t sum_pieces(const T *grad, const SumArgs &a, O *out, cudaStream_t stream) {
+cudaError_t sum_pieces(const T *grad, SumArgs a, O *out, cudaStream_t stream) {
   const int pieces = (a.n + a.piece - 1) / a.piece, groups = kSumThreads / TPR;
-  const dim3 grid((pieces + groups - 1) / groups, (a.hidden + TPR * 8 - 1) / (TPR * 8));
-  cudaError_t err = launch_chained(embed_sum_kernel<T, O, V, TPR>, grid, dim3(kSumThreads), 0, stream,
-                                   1, true, grad, a, out);
+  const unsigned blocks = (unsigned)((pieces + groups - 1) / groups), strips = (unsigned)((a.hidden + TPR * 8 - 1) / (TPR * 8));
+  const bool zero = a.zero.ctas > 0;
+  const int later = zero ? zeros_of_joins(a.n, pieces, a.hidden, a.vocab, sizeof(O)) : 0;
+  a.zero.to = a.vocab - later;
+  // (without rows the sort has not been launched: nothing to start beside)
+  cudaError_t err = launch_chained(embed_sum_kernel<T, O, V, TPR>, dim3(blocks + a.zero.ctas, strips),
+                                   dim3(kSumThreads), 0, stream, 1, a.n > 0, grad, a, out);
   if (err != cudaSuccess || pieces < 2) return err;
-  return launch_chained(embed_join_kernel<O, V, TPR>, grid, dim3(kSumThreads), 0, stream, 1, true, a, out);
+  a.zero.from = a.zero.to;
+  a.zero.to = a.vocab;
+  if (!later) a.zero.ctas = 0;
+  return launch_chained(embed_join_kernel<O, V, TPR>, dim3(blocks + a.zero.ctas, strips), dim3(kSumThreads), 0,
+                        stream, 1, true, a, out);
 }
 
 template <typename T, typename O, int V>
@@ -379,16 +414,12 @@ cudaError_t sum_rows(const T *grad, const SumArgs &a, O *out, cudaStream_t strea
                             : sum_pieces<T, O, V, 256>(grad, a, out, stream);
 }
 
-template <typename O>
-cudaError_t sort_rows(const SortArgs &s, O *out, int hidden, int64_t out_stride, bool zero,
-                      cudaStream_t stream) {
-  auto kernel = embed_sort_kernel<O>;
-  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+cudaError_t sort_rows(const SortArgs &s, cudaStream_t stream) {
+  const cudaError_t err = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                (int)sizeof(SortShared));
   if (err != cudaSuccess) return err;
-  const int ctas = kSortCtas * (zero ? 1 + 2 * kSms / kSortCtas : 1);
-  return launch_chained(kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortShared), stream, kSortCtas,
-                        false, s, out, hidden, out_stride);
+  return launch_chained(embed_sort_kernel, dim3(kSortCtas), dim3(kSortThreads), sizeof(SortShared), stream,
+                        kSortCtas, false, s);
 }
 
 template <typename T, typename O>
@@ -398,13 +429,16 @@ cudaError_t embed_grad(const T *grad, int rows, int hidden, int64_t stride, cons
   char *w = static_cast<char *>(workspace);
   const SortArgs s = {ids, rows, vocab, reinterpret_cast<uint2 *>(w),
                       reinterpret_cast<uint2 *>(w + items_bytes(rows))};
-  const SumArgs a = {s.a, rows, piece_rows(rows), vocab, hidden, stride, out_stride, scale, accumulate,
+  const SumArgs a = {s.a, rows, piece_rows(rows), vocab, hidden, stride, out_stride,
+                     {ids, accumulate ? 0 : kZeroCtas, 0, vocab}, scale, accumulate,
                      reinterpret_cast<float *>(w + 2 * items_bytes(rows))};
   const void *base[1] = {out};
   const int64_t strides[1] = {out_stride};
   const int vo = row_vector(sizeof(O), hidden, 1, base, strides);
-  const cudaError_t err = sort_rows<O>(s, out, hidden, out_stride, !accumulate, stream);
-  if (err != cudaSuccess || rows == 0) return err;
+  if (rows > 0) {
+    const cudaError_t err = sort_rows(s, stream);
+    if (err != cudaSuccess) return err;
+  }
   // one access for the gradient's rows, the table's and the sums': whole 16 bytes
   // of the gradient's type, else element by element
   const void *gbase[1] = {grad};
