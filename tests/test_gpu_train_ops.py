@@ -281,7 +281,8 @@ def _check_embed_grad(grad, ids, vocab, out, scale=1.0, accumulate=False):
 @pytest.mark.parametrize("odtype", TYPES)
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,hidden,vocab", [(1, 64, 10), (31, 8, 1), (33, 1000, 3), (700, 257, 501), (5000, 2048, 777),
-                                               (1021, 520, 40001), (64, 5001, 1000), (9000, 16, 262144)])
+                                               (1021, 520, 40001), (64, 5001, 1000), (9000, 16, 262144),
+                                               (500, 94, 30011), (500, 5, 30011), (100, 9, 5003), (2000, 333, 9001)])
 def test_embed_grad(rows, hidden, vocab, dtype, odtype, accumulate):
     grad = _randn(rows, hidden, seed=rows).to(dtype)
     out = _randn(vocab, hidden, seed=3).to(odtype)
