@@ -66,10 +66,14 @@ constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kLeastPiece = 4, kMostPiece = 256;
 constexpr int kSumThreads = 256;
 
+constexpr int kHalves = kSortThreads / kDigits;  // parts of the warps, in the sum over them
+constexpr int kHeldItems = 4;                     // of a lane, read once a pass
+static_assert(kSortWarps % kHalves == 0, "parts of the warps");
 struct SortShared {
-  uint32_t count[kSortWarps][kDigits];  // of a warp's items, then where its next item goes
+  uint32_t count[kSortWarps][kDigits];  // of a warp's items, then of those before it in its half
+  uint32_t start[kHalves][kDigits];     // a half's items, then where they go
   uint32_t total[kDigits];              // of the CTA's items
-  uint32_t scan[kSortWarps];
+  uint32_t scan[kDigits / 32];
 };
 // Bits of the largest key: vocab itself, the key of ids outside the table.
 __host__ __device__ inline int key_bits(int vocab) {
@@ -89,54 +93,101 @@ __device__ __forceinline__ uint32_t cluster_load(const uint32_t *p, uint32_t ran
   return ld_shared_cluster(mapa_shared(smem_u32(p), rank));
 }
 
+// Lanes whose digit is this lane's, of those that have one: a ballot a bit (a
+// match over the warp takes longer the more digits differ: 32768 ids 25 us with it).
+__device__ __forceinline__ uint32_t lanes_with(uint32_t d) {
+  uint32_t same = __ballot_sync(0xFFFFFFFFu, d < kDigits);
+#pragma unroll
+  for (int b = 0; b < kDigitBits; ++b) {
+    const bool set = (d >> b & 1u) != 0;
+    const uint32_t v = __ballot_sync(0xFFFFFFFFu, set);
+    same &= set ? v : ~v;
+  }
+  return same;
+}
+
 // Stable sort by key, one cluster.  A warp holds a run of the items; the digits
-// of its items are counted (pass 1 of the data), counts become the warps' first
-// places, digit by digit, and the items are moved in order (pass 2).
+// of its items are counted, counts become the warps' first places, digit by digit, and
+// the items are moved in order.  Up to kHeldItems a lane they stay in registers between.
 __device__ void sort_by_id(const SortArgs &s, SortShared &sh) {
-  const int cta = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int ctas = (int)gridDim.x, cta = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int bits = key_bits(s.vocab), passes = (bits + kDigitBits - 1) / kDigitBits;
   const int width = (bits + passes - 1) / passes;
   // items of a warp, a multiple of 32
-  const int per = ((s.n + kSortCtas * kSortWarps - 1) / (kSortCtas * kSortWarps) + 31) / 32 * 32;
+  const int per = ((s.n + ctas * kSortWarps - 1) / (ctas * kSortWarps) + 31) / 32 * 32;
   const int64_t first = (int64_t)(cta * kSortWarps + warp) * per;
   const int lo = (int)(first < s.n ? first : s.n), hi = (int)(first + per < s.n ? first + per : s.n);
+  const int digit = threadIdx.x & (kDigits - 1), half = threadIdx.x / kDigits;
+  constexpr int kPart = kSortWarps / kHalves, kBatch = 32 * kHeldItems;
   for (int pass = 0; pass < passes; ++pass) {
     // the last pass writes s.a
     const uint2 *src = (passes - pass) & 1 ? s.b : s.a;
     uint2 *dst = (passes - pass) & 1 ? s.a : s.b;
     const int shift = pass * width;
-    auto item = [&](int i) {
-      if (pass > 0) return __ldcg(src + i);
-      const int id = __ldg(s.ids + i);
-      return make_uint2(id >= 0 && id < s.vocab ? (uint32_t)id : (uint32_t)s.vocab, (uint32_t)i);
+    uint2 held[kHeldItems];
+    auto fetch = [&](int i0) {
+#pragma unroll
+      for (int k = 0; k < kHeldItems; ++k) {
+        const int i = i0 + 32 * k + lane;
+        held[k] = make_uint2(0u, 0u);
+        if (i >= hi) continue;
+        if (pass > 0) {
+          held[k] = __ldcg(src + i);
+        } else {
+          const int id = __ldg(s.ids + i);
+          held[k] = make_uint2(id >= 0 && id < s.vocab ? (uint32_t)id : (uint32_t)s.vocab, (uint32_t)i);
+        }
+      }
     };
-    for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0u;
+    auto digit_of = [&](int k, int i0) {
+      return i0 + 32 * k + lane < hi ? (held[k].x >> shift) & (kDigits - 1) : (uint32_t)kDigits;
+    };
+    fetch(lo);
+    for (int i = threadIdx.x; i < kSortWarps * kDigits / 4; i += kSortThreads)
+      reinterpret_cast<uint4 *>(&sh.count[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
-    for (int i = lo; i < hi; i += 32) {
-      const bool in = i + lane < hi;
-      const uint32_t d = in ? (item(i + lane).x >> shift) & (kDigits - 1) : kDigits;
-      const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
-      if (in && (same & ((1u << lane) - 1)) == 0) sh.count[warp][d] += __popc(same);
-      __syncwarp();
+    for (int i0 = lo; i0 < hi; i0 += kBatch) {
+      if (i0 > lo) fetch(i0);
+#pragma unroll
+      for (int k = 0; k < kHeldItems; ++k) {
+        if (i0 + 32 * k >= hi) break;
+        const uint32_t d = digit_of(k, i0);
+        const uint32_t same = lanes_with(d);
+        if (d < kDigits && (same & ((1u << lane) - 1)) == 0) sh.count[warp][d] += __popc(same);
+        __syncwarp();
+      }
     }
     __syncthreads();
+    {
+      uint32_t c[kPart], sum = 0;
+#pragma unroll
+      for (int w = 0; w < kPart; ++w) c[w] = sh.count[half * kPart + w][digit];
+#pragma unroll
+      for (int w = 0; w < kPart; ++w) {
+        sh.count[half * kPart + w][digit] = sum;
+        sum += c[w];
+      }
+      sh.start[half][digit] = sum;
+    }
+    __syncthreads();
+    uint32_t mine = 0;
     if (threadIdx.x < kDigits) {
-      uint32_t sum = 0;
-      for (int w = 0; w < kSortWarps; ++w) {
-        const uint32_t c = sh.count[w][threadIdx.x];
-        sh.count[w][threadIdx.x] = sum;
-        sum += c;
-      }
-      sh.total[threadIdx.x] = sum;
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) mine += sh.start[h][digit];
+      sh.total[digit] = mine;
     }
-    cluster_sync_all();
-    uint32_t before = 0, all = 0;  // this digit's items in earlier CTAs, in all
-    if (threadIdx.x < kDigits)
-      for (int c = 0; c < kSortCtas; ++c) {
-        const uint32_t v = cluster_load(&sh.total[threadIdx.x], (uint32_t)c);
-        before += c < cta ? v : 0u;
-        all += v;
+    uint32_t before = 0, all = mine;  // this digit's items in earlier CTAs, in all
+    if (ctas > 1) {
+      cluster_sync_all();
+      if (threadIdx.x < kDigits) {
+        all = 0;
+        for (int c = 0; c < ctas; ++c) {
+          const uint32_t v = cluster_load(&sh.total[digit], (uint32_t)c);
+          before += c < cta ? v : 0u;
+          all += v;
+        }
       }
+    }
     // exclusive scan of `all` over the digits
     uint32_t inc = all;
 #pragma unroll
@@ -144,31 +195,41 @@ __device__ void sort_by_id(const SortArgs &s, SortShared &sh) {
       const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
       if (lane >= o) inc += v;
     }
-    if (lane == 31) sh.scan[warp] = inc;
+    if (lane == 31 && threadIdx.x < kDigits) sh.scan[warp] = inc;
     __syncthreads();
     if (threadIdx.x < kDigits) {
       uint32_t base = before + inc - all;
-      for (int w = 0; w < warp; ++w) base += sh.scan[w];
-      for (int w = 0; w < kSortWarps; ++w) sh.count[w][threadIdx.x] += base;
+      const uint32_t earlier = lane < warp ? sh.scan[lane] : 0u;  // (as many warps as lanes at the most)
+      base += __reduce_add_sync(0xFFFFFFFFu, earlier);
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        const uint32_t n = sh.start[h][digit];
+        sh.start[h][digit] = base;
+        base += n;
+      }
     }
     __syncthreads();
-    for (int i = lo; i < hi; i += 32) {
-      const bool in = i + lane < hi;
-      const uint2 v = in ? item(i + lane) : make_uint2(0, 0);
-      const uint32_t d = in ? (v.x >> shift) & (kDigits - 1) : kDigits;
-      const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
-      const uint32_t rank = __popc(same & ((1u << lane) - 1));
-      const uint32_t place = in ? sh.count[warp][d] + rank : 0u;
-      __syncwarp();
-      if (in) {
-        dst[place] = v;
-        if (rank == 0) sh.count[warp][d] += __popc(same);
+    for (int i0 = lo; i0 < hi; i0 += kBatch) {
+      if (per > kBatch) fetch(i0);
+#pragma unroll
+      for (int k = 0; k < kHeldItems; ++k) {
+        if (i0 + 32 * k >= hi) break;
+        const uint32_t d = digit_of(k, i0);
+        const uint32_t same = lanes_with(d);
+        const uint32_t rank = __popc(same & ((1u << lane) - 1));
+        const bool in = d < kDigits;
+        const uint32_t place = in ? sh.start[warp / kPart][d] + sh.count[warp][d] + rank : 0u;
+        __syncwarp();
+        if (in) {
+          dst[place] = held[k];
+          if (rank == 0) sh.count[warp][d] += __popc(same);
+        }
+        __syncwarp();
       }
-      __syncwarp();
     }
     // the pass's items, written by all CTAs, are read by the next; totals are read no more
-    __threadfence();
-    cluster_sync_all();
+    if (ctas > 1) cluster_sync_all();
+    else __syncthreads();
   }
 }
 
@@ -438,8 +499,9 @@ cudaError_t sort_rows(const SortArgs &s, cudaStream_t stream) {
   const cudaError_t err = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                (int)sizeof(SortShared));
   if (err != cudaSuccess) return err;
-  return launch_chained(embed_sort_kernel, dim3(kSortCtas), dim3(kSortThreads), sizeof(SortShared), stream,
-                        kSortCtas, false, s);
+  // one CTA while its lanes hold all items
+  const int ctas = s.n <= kSortThreads * kHeldItems ? 1 : kSortCtas;
+  return launch_chained(embed_sort_kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortShared), stream, ctas, false, s);
 }
 
 template <typename T, typename O>
