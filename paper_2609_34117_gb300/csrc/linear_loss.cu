@@ -197,10 +197,10 @@ __device__ __forceinline__ int choose_splits(int tiles, int kb, int pairs) {
 // ---------------------------------------------------------------------------
 // rows with a label, moved together
 // ---------------------------------------------------------------------------
-constexpr int kGatherThreads = 1024, kGatherRows = kGatherThreads / 32;
+constexpr int kGatherThreads = 256, kGatherRows = kGatherThreads / 32;
 // More rows than this: the labels of each 1024 are counted first, and a CTA adds up
 // counts instead of reading all labels before its own.
-constexpr int kCountedRows = 32768;
+constexpr int kCountedRows = 8192;
 
 __global__ void __launch_bounds__(1024) count_kernel(Call c) {
   pdl_launch_dependents();
@@ -212,8 +212,8 @@ __global__ void __launch_bounds__(1024) count_kernel(Call c) {
 // A warp a row: with a label, the row is copied to its place among those and its
 // label's logit computed (fp32 sums of a lane's products, then over the lanes);
 // without, it gets its results.
-__global__ void __launch_bounds__(kGatherThreads, 1) gather_kernel(Call c, int counted) {
-  __shared__ int before_all, in_warp[32];
+__global__ void __launch_bounds__(kGatherThreads, 2) gather_kernel(Call c, int counted) {
+  __shared__ int before_all, in_warp[kGatherRows];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = blockIdx.x * kGatherRows, t = t0 + warp;
   if (threadIdx.x == 0) before_all = 0;
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kGatherThreads, 1) gather_kernel(Call c, int c
   const int y = t < c.T ? __ldg(c.labels + t) : -1;
   if (lane == 0) in_warp[warp] = y >= 0 ? 1 : 0;
   __syncthreads();
-  const uint32_t live = __ballot_sync(0xFFFFFFFFu, in_warp[lane] != 0);
+  const uint32_t live = __ballot_sync(0xFFFFFFFFu, lane < kGatherRows && in_warp[lane % kGatherRows] != 0);
   const int at = before_all + __popc(live & ((1u << warp) - 1));
   if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) c.ctrl[kLive] = before_all + __popc(live);
   if (t >= c.T) return;
@@ -999,21 +999,23 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
 // ---------------------------------------------------------------------------
 // a row's sums
 // ---------------------------------------------------------------------------
-// 32 rows a CTA, a lane each; the column tiles' sums in 32 parts.  kForward: the
+// Eight rows a CTA; the column tiles' sums of a row in 32 parts, four in a warp.  kForward: the
 // loss.  kNumerators: besides, the row's factor, the label's numerator and the
 // scaled row; `again`: only rows of the tiles that were run again (roles swapped: all; else a row whose
 // reference does not do marks its tile).
+constexpr int kSumRows = 8, kSumThreads = 32 * kSumRows;
+
 template <Mode kMode>
-__global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int again, int finish) {
-  __shared__ float part_sum[32][33], part_most[32][33];
-  __shared__ double total[32];
+__global__ void __launch_bounds__(kSumThreads, 2) sums_kernel(Call c, int chunk, int again, int finish) {
+  __shared__ float part_sum[32][kSumRows + 1], part_most[32][kSumRows + 1];
+  __shared__ double total[kSumThreads / 32];
   __shared__ int last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait_primary();
   pdl_launch_dependents();
   if (again && __ldcg(c.flags + 2 * (c.rows_pad / kTile) + chunk) == 0) return;
   const int rows = chunk_rows(c, chunk), row0 = chunk * c.chunk;
-  const int first = blockIdx.x * 32, tile = row0 / kTile + first / kTile;
+  const int first = blockIdx.x * kSumRows, tile = row0 / kTile + first / kTile;
   const bool mine = first < (rows + kTile - 1) / kTile * kTile && (!again || c.rows_tile != kTile || __ldcg(c.flags + tile) != 0);
   if (mine) {
     // a warp's row and what is known of it
@@ -1023,12 +1025,13 @@ __global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int ag
     float ref = live ? __ldcg(c.ref + at) : 0.0f;
     const int t = live ? __ldcg(c.orig + at) : 0, y = live ? __ldcg(c.label + at) : -1;
     const float weight = live && c.row_weight ? __ldg(c.row_weight + t) : 1.0f;
-    // a lane a row: every 32nd part
+    // every 32nd part of a row
+    const int mine_row = lane & (kSumRows - 1), share = warp * (32 / kSumRows) + lane / kSumRows;
     const int parts = c.vocab_tiles * 2;
     float s = 0.0f, m = kFloor;
-    const float2 *part = c.sums + first + lane;
+    const float2 *part = c.sums + first + mine_row;
 #pragma unroll 8
-    for (int i = warp; i < parts; i += 32) {
+    for (int i = share; i < parts; i += 32) {
       const float2 v = __ldcg(part + (int64_t)i * c.chunk);
       if constexpr (kMode == kForward) {
         const float to = fmaxf(m, v.y);
@@ -1039,8 +1042,8 @@ __global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int ag
         m = fmaxf(m, v.y);
       }
     }
-    part_sum[warp][lane] = s;
-    part_most[warp][lane] = m;
+    part_sum[share][mine_row] = s;
+    part_most[share][mine_row] = m;
     __syncthreads();
     float S = part_sum[lane][warp], top = part_most[lane][warp];
     const float mine_most = top;
@@ -1102,7 +1105,7 @@ __global__ void __launch_bounds__(1024, 1) sums_kernel(Call c, int chunk, int ag
     __threadfence();
   }
   __syncthreads();
-  if (last) total_loss<1024>(c, threadIdx.x, total);
+  if (last) total_loss<kSumThreads>(c, threadIdx.x, total);
 }
 
 // By itself where dW is not wanted.
@@ -1252,20 +1255,20 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
     err = launch_chained(gather_kernel, dim3((unsigned)ceil_div(c.T, kGatherRows)), dim3(kGatherThreads), 0, stream,
                          1, counted != 0, c, counted);
   for (int k = 0; k < l.chunks && err == cudaSuccess; ++k) {
-    const dim3 sum_grid((unsigned)(l.chunk / 32));
+    const dim3 sum_grid((unsigned)(l.chunk / kSumRows));
     const int finish = k == l.chunks - 1;
     if (!grad) {
       err = swapped ? run_product<kForward, true>(logits, c, k, 0, 0, stream)
                 : run_product<kForward>(logits, c, k, 0, 0, stream);
       if (err == cudaSuccess)
-        err = launch_chained(sums_kernel<kForward>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, 0, finish);
+        err = launch_chained(sums_kernel<kForward>, sum_grid, dim3(kSumThreads), 0, stream, 1, true, c, k, 0, finish);
       continue;
     }
     for (int again = 0; again < 2 && err == cudaSuccess; ++again) {
       err = swapped ? run_product<kNumerators, true>(logits, c, k, again, 0, stream)
                 : run_product<kNumerators>(logits, c, k, again, 0, stream);
       if (err == cudaSuccess)
-        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(1024), 0, stream, 1, true, c, k, again, 0);
+        err = launch_chained(sums_kernel<kNumerators>, sum_grid, dim3(kSumThreads), 0, stream, 1, true, c, k, again, 0);
     }
     int pairs = 0;
     if (a.grad_hidden && err == cudaSuccess) {

@@ -155,13 +155,14 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     for (int i = 0; i < R; ++i) {
       const F2 m = f2(-mu[i] * warp_inv);
       F2 s = f2(0.0f);
+      const bool full = a.hidden == TPR * N;
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
         F2 d = p[i].get2(e);
         if constexpr (kLayer) {
           d = add2(d, m);
           // (the last pieces may have columns past the row)
-          if (((e + 1) / V + 1) * TPR * V > a.hidden) {
+          if (!full && ((e + 1) / V + 1) * TPR * V > a.hidden) {
             const float2 h = halves(d);
             d = f2(Part::column(e, t, TPR) < a.hidden ? h.x : 0.0f, Part::column(e + 1, t, TPR) < a.hidden ? h.y : 0.0f);
           }
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (r0 + i >= a.rows) continue;
-      const float rs = 1.0f / sqrtf(fmaf(q[i], inv, a.eps));
+      const float rs = rsqrtf(fmaf(q[i], inv, a.eps));
       if (t == 0) {
         a.rstd[r0 + i] = rs;
         if constexpr (kLayer) a.mean[r0 + i] = mu[i];
