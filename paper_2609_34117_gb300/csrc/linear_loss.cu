@@ -44,6 +44,12 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMostLoss = 60.0f;
+// The tensor cores' fp32 sums are cut, not rounded, at each step of the contraction: a
+// logit is too small in magnitude by 1.03e-9 of itself for each element of the width
+// where it grows steadily, 0.9e-9 where it wanders (widths of 512 to 4096 alike), while
+// the label's, of plain sums, is not.  The expected loss is given back: a row's lse at
+// 4096 was 3.4e-6 of itself too small.
+constexpr float kTruncated = 1.0e-9f;
 constexpr int64_t kMostCells = 1ll << 30;
 constexpr int kTile = 256;       // rows and columns of a pair's tile
 constexpr int kHalf = 128;       // of a CTA's share of an operand
@@ -150,6 +156,7 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
 // Device view of the workspace and the call.
 struct Call {
   int T, H, V;
+  float unbias;  // of a logit: 1 + H kTruncated
   int rows_pad, chunk, vocab_tiles, hidden_tiles;
   int rows_tile;  // of the first product and dh's
   int64_t cells_stride;
@@ -390,7 +397,7 @@ constexpr size_t kGemmSmem = kBars + kWords + 64 + 1024;
 
 // Sums of the columns' numerators and the P tile of 32 columns.
 template <Mode kMode>
-__device__ __forceinline__ void numerators(const float (&z)[32], float ref, int label, int valid,
+__device__ __forceinline__ void numerators(const float (&z)[32], float unbias, float ref, int label, int valid,
                                            float &sum, float &most, uint32_t (&packed)[16]) {
   // label: the label's column here, or outside 0..31; valid: columns of the vocabulary
   const bool plain = __all_sync(0xFFFFFFFFu, (unsigned)label >= 32u) && valid >= 32;
@@ -405,7 +412,7 @@ __device__ __forceinline__ void numerators(const float (&z)[32], float ref, int 
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
-      const float e = ex2((z[j] - m) * kLog2e);
+      const float e = ex2(fmaf(z[j], unbias, -m) * kLog2e);
       if (plain || (j < valid && j != label)) s[j & 3] += e;
     }
     sum += (s[0] + s[1]) + (s[2] + s[3]);
@@ -416,7 +423,7 @@ __device__ __forceinline__ void numerators(const float (&z)[32], float ref, int 
       float e[2];
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        e[q] = ex2((z[j + q] - ref) * kLog2e);
+        e[q] = ex2(fmaf(z[j + q], unbias, -ref) * kLog2e);
         if (plain || (j + q < valid && j + q != label)) {
           s[(j + q) & 3] += e[q];
           most = fmaxf(most, z[j + q]);
@@ -453,7 +460,7 @@ __device__ __forceinline__ float reduce_across(float (&x)[32], int lane, F op) {
 // `staged` (64 bytes a row, zeros for rows past `live`), and returns to lane j row j's
 // sum over the warp's words and largest logit.
 template <Mode kMode>
-__device__ __forceinline__ float2 swapped_numerators(float (&z)[32], const float *ref, const int *label, int word,
+__device__ __forceinline__ float2 swapped_numerators(float (&z)[32], float unbias, const float *ref, const int *label, int word,
                                                  bool known, int live, int lane, uint32_t staged) {
   float top = kFloor;
 #pragma unroll
@@ -462,7 +469,7 @@ __device__ __forceinline__ float2 swapped_numerators(float (&z)[32], const float
     const float most = warp_max_redux(in ? z[j] : kFloor);
     if (lane == j) top = most;
     const float r = kMode == kForward ? most : ref[j];
-    const float e = ex2((z[j] - r) * kLog2e);
+    const float e = ex2(fmaf(z[j], unbias, -r) * kLog2e);
     if constexpr (kMode == kNumerators) {
       const __nv_bfloat16 h = __float2bfloat16_rn(j < live ? e : 0.0f);
       asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged + (uint32_t)(j * 64 + lane * 2)),
@@ -879,7 +886,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
               if (j < live) to[j * kTile] = z[j];
           } else {
             quarters[((local & 1) * 4 + q) * kTile + t0 + lane] =
-                swapped_numerators<kMode>(z, row_ref + row_first + t0, row_label + row_first + t0, mine, mine < c.V,
+                swapped_numerators<kMode>(z, c.unbias, row_ref + row_first + t0, row_label + row_first + t0, mine, mine < c.V,
                                           live, lane, staged);
           }
           if constexpr (kMode == kNumerators) {
@@ -917,7 +924,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
           tmem_ld_wait();
           if (k == kHalf / 32 - 1) release();
           const int col = col0 + 32 * k;
-          numerators<kMode>(z, ref, label - col, c.V - col, sum, most, packed);
+          numerators<kMode>(z, c.unbias, ref, label - col, c.V - col, sum, most, packed);
           if constexpr (kMode == kNumerators) {
             // rows past the last one: zeros (they are in the contraction of dW)
             if (!live)
@@ -1204,6 +1211,7 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   char *w = static_cast<char *>(workspace);
   Call c = {};
   c.T = a.rows; c.H = a.width; c.V = a.vocab;
+  c.unbias = 1.0f + (float)c.H * kTruncated;
   c.rows_pad = l.rows_pad; c.chunk = l.chunk;
   c.vocab_tiles = l.vocab_tiles; c.hidden_tiles = l.hidden_tiles;
   c.rows_tile = l.rows_tile ? l.rows_tile : kTile;
