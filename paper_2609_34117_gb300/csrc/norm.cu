@@ -68,9 +68,10 @@ struct NormArgs {
 // Threads of a row (TPR) and elements of a thread (N): rows up to 256 (32, 8), 512,
 // 1024, .. 8192 (32 .. 512, 16) and 16384 (512, 32).  Groups are persistent: the weight
 // and bias of a thread's columns stay in its registers, and R rows are on their way while R
-// others are worked on.  16384 x 2048 bf16 layer norm, the kernel alone: with 8 elements
-// a thread 30 us, a row's sums costing as much as its elements; weights from the L1
-// cache for each row 36 us, L1 82 % busy.
+// others are worked on.  Bound by instructions: 16384 x 2048 bf16 layer norm 26 us (a copy
+// of as many bytes 23); with 8 elements a thread 30, a row's sums costing as much as its
+// elements; weights from the L1 cache for each row 36, L1 82 % busy.  Rows that are
+// not aligned: 32768 x 4001 bf16 184 us, by element 230.
 constexpr int kNormThreads = 256;
 template <int TPR>
 constexpr int kNormBlock = TPR > kNormThreads ? TPR : kNormThreads;
@@ -239,9 +240,11 @@ struct GradArgs {
   float *partial;  // [CTAs][kLayer ? 2 : 1][hidden]
 };
 
-// Threads of a row (TPR) and elements of a thread (N): rows up to 256, 1024, 2048,
-// 4096, 8192 and 16384 long.  A CTA holds eight rows' groups of a warp, else one
-// row's.
+// Threads of a row (TPR) and elements of a thread (N): rows up to 256 (32, 8), 1024 (128,
+// 8), 2048 (256, 8), 4096 (512, 8), then 512 threads with 10, 12, 16 or 32.  A CTA holds
+// eight rows' groups of a warp, else one row's; 512 threads are on an SM.  Bound by
+// memory and a row's barrier: 16384 x 2048 bf16 RMS norm 36 us, 5.5 TB/s (a copy of as
+// many bytes 5.8); bf16 rows that are not aligned by their shifts: 32768 x 4001 325 us.
 constexpr int kWarpRows = 8;
 template <int TPR>
 constexpr int kBlock = TPR == 32 ? 32 * kWarpRows : TPR;
@@ -395,7 +398,6 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     if constexpr (kAhead<N>) arrive();
   }
   pdl_launch_dependents();
-  pdl_launch_dependents();
   // the CTA's sums: its groups' in turn
   float *out = a.partial + (int64_t)blockIdx.x * (kLayer ? 2 : 1) * a.hidden;
   F2 *mine = reinterpret_cast<F2 *>(held);
@@ -432,7 +434,12 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
 // columns ahead (no barriers about data) and reads them twice: for the row's sums,
 // and for dx once these are known, which is one row later, so that the sums' way
 // through the warps and the barrier is hidden behind the row before.
+// (Aligned rows, and fp32 ones by element; 32 columns of fp32 a thread would fill the ring
+// with one row.)  By element the copies are what takes the time: 4099 x 5001 fp32 67 us,
+// with the next row in registers, for which 10 columns a thread leave room, 42.
 constexpr int kRingThreads = 512, kRingBytes = 200 * 1024;
+template <typename T, int V, bool kAny, int N>
+constexpr bool kRing = !kAny && N >= 16 && N * sizeof(T) <= 64 && (V * sizeof(T) == 16 || sizeof(T) == 4);
 
 template <int B>
 __device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool in) {
@@ -665,20 +672,16 @@ template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
 cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *dweight,
                       float *dbias, cudaStream_t stream) {
   const int ctas = grad_ctas(a.rows, a.hidden);
-  // a row's two tensors, at least three times in a ring
-  constexpr int kPiece = kRingThreads * V * (int)sizeof(T);
-  const int row_bytes = 2 * ((a.hidden + kRingThreads * V - 1) / (kRingThreads * V)) * kPiece;
-  const int slots = kRingBytes / row_bytes < 6 ? kRingBytes / row_bytes : 6;
-  constexpr bool kRing = !kAny && N >= 16 && N * sizeof(T) <= 64 && (V * sizeof(T) == 16 || (sizeof(T) == 4 && N == 16));
-  if (kRing && slots >= 3) {
-    if constexpr (kRing) {
-      auto kernel = norm_grad_ring_kernel<T, V, N, kLayer>;
-      const cudaError_t err =
-          cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               kRingBytes + kPiece);
-      if (err != cudaSuccess) return err;
-      kernel<<<ctas, kRingThreads, (size_t)slots * row_bytes + kPiece, stream>>>(dy, x, a, dx, slots);
-    }
+  if constexpr (kRing<T, V, kAny, N>) {
+    // a row's two tensors, three to six times
+    constexpr int kPiece = kRingThreads * V * (int)sizeof(T);
+    const int row_bytes = 2 * ((a.hidden + kRingThreads * V - 1) / (kRingThreads * V)) * kPiece;
+    const int slots = kRingBytes / row_bytes < 6 ? kRingBytes / row_bytes : 6;
+    auto kernel = norm_grad_ring_kernel<T, V, N, kLayer>;
+    const cudaError_t err =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + kPiece);
+    if (err != cudaSuccess) return err;
+    kernel<<<ctas, kRingThreads, (size_t)slots * row_bytes + kPiece, stream>>>(dy, x, a, dx, slots);
   } else {
     constexpr bool kHeld = N >= 32 || kBlock<TPR> > TPR;
     constexpr size_t smem = kHeld ? (size_t)(kLayer ? 2 : 1) * N * TPR * 4 : 0;

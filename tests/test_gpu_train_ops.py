@@ -542,3 +542,56 @@ def test_linear_loss_is_the_same_every_time():
     got = sw.slimwise_linear_loss(*head[:3], row_weight=head[3], workspace=ws)
     assert all(torch.equal(a, b) for a, b in zip(runs[0], got))
     assert sw.slimwise_moe_device_status(ws) == 0
+
+
+# ---------------------------------------------------------------------------
+# offsets past 32 bits
+# ---------------------------------------------------------------------------
+def test_embed_offsets_past_32_bits():
+    vocab, hidden = 300000, 8192  # 2.4e9 elements
+    table = torch.zeros((vocab, hidden), dtype=BF16, device=DEV)
+    table[-3:] = _randn(3, hidden, seed=1).to(BF16)
+    ids = torch.tensor([vocab - 1, 0, vocab - 3, -1, vocab - 1], dtype=torch.int32, device=DEV)
+    out = sw.slimwise_embed(table, ids)
+    assert torch.equal(out[[0, 2, 4]], table[[vocab - 1, vocab - 3, vocab - 1]]) and bool((out[[1, 3]] == 0).all())
+    grad = out.clone()
+    table.fill_(NAN)
+    sw.slimwise_embed_grad(grad, ids, table)
+    assert torch.equal(table[-1], (2 * grad[0].float()).to(BF16)) and torch.equal(table[-3], grad[2])
+    assert bool((table[:-3] == 0).all()) and bool((table[-2] == 0).all())
+
+
+def test_norm_offsets_past_32_bits():
+    rows, hidden = 300000, 8192
+    x = torch.ones((rows, hidden), dtype=BF16, device=DEV)
+    x[-4:] = _randn(4, hidden, seed=1).to(BF16)
+    w = 1 + 0.1 * _randn(hidden, seed=2)
+    y, _, rstd = sw.slimwise_norm(x, w)
+    few = sw.slimwise_norm(x[-4:].clone(), w)
+    assert torch.equal(y[-4:], few[0]) and torch.equal(rstd[-4:], few[2])
+    dx = sw.slimwise_norm_grad(x, x, w, rstd, dx=y)[0]
+    assert torch.equal(dx[-4:], sw.slimwise_norm_grad(x[-4:].clone(), x[-4:].clone(), w, few[2])[0])
+
+
+def test_linear_loss_offsets_past_32_bits():
+    vocab, width = 393216, 8192
+    weight = torch.zeros((vocab, width), dtype=BF16, device=DEV)
+    weight[-700:] = (_randn(700, width, seed=1) * 0.05).to(BF16)
+    hidden = _randn(3, width, seed=2).to(BF16)
+    labels = torch.tensor([vocab - 1, vocab - 500, 7], dtype=torch.int32, device=DEV)
+    dw = torch.full((vocab, width), NAN, dtype=BF16, device=DEV)
+    loss, row, dh, _ = sw.slimwise_linear_loss(hidden, weight, labels, grad_weight=dw)
+    z = torch.zeros((3, vocab), dtype=torch.float64, device=DEV)
+    z[:, -700:] = hidden.double() @ weight[-700:].double().T
+    p = torch.softmax(z, 1)
+    want = torch.logsumexp(z, 1) - z.gather(1, labels.long()[:, None])[:, 0]
+    # logits of up to 25, off by 2^-17 of themselves
+    assert bool(((row.double() - want).abs() <= 25 * 2.0 ** -17).all())
+    p[torch.arange(3), labels.long()] -= 1
+    for v in (7, vocab - 1, vocab - 500, vocab - 2, 12345):
+        ref = p[:, v] @ hidden.double()
+        size = p[:, v].abs() @ hidden.double().abs()
+        assert bool(((dw[v].double() - ref).abs() <= 3 * 2.0 ** -8 * size).all())
+    ref = p[:, -700:] @ weight[-700:].double()
+    size = p[:, -700:].abs() @ weight[-700:].double().abs()
+    assert bool(((dh.double() - ref).abs() <= 4 * 2.0 ** -8 * size).all())
