@@ -906,6 +906,17 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
         }
         // (a half without a 32 of its own)
         if (32 * half >= n_rows) release();
+        if constexpr (kMode == kNumerators) {
+          // zeros between the last tile and the end of dW's slices, which may lie further
+          const int covered = row_first + n_rows, end = (rows + kDepth - 1) / kDepth * kDepth;
+          if (half == 0 && w.m == work.mt - 1)
+            for (int i = lane; i < (end - covered) * 4; i += 32) {
+              const int v = w.n * kTile + (int)crank * kHalf + 32 * q + (i & 3) * 8;
+              if (v < c.cells_stride)
+                *reinterpret_cast<uint4 *>(c.cells + (int64_t)(covered + (i >> 2)) * c.cells_stride + v) =
+                    make_uint4(0, 0, 0, 0);
+            }
+        }
       } else if constexpr (kMode == kForward || kMode == kNumerators) {
         // nothing reads what rows past the last one, rounded up to dW's slices, would leave
         if (row - lane >= (rows + kDepth - 1) / kDepth * kDepth) {

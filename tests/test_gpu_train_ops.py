@@ -595,3 +595,48 @@ def test_linear_loss_offsets_past_32_bits():
     ref = p[:, -700:] @ weight[-700:].double()
     size = p[:, -700:].abs() @ weight[-700:].double().abs()
     assert bool(((dh.double() - ref).abs() <= 4 * 2.0 ** -8 * size).all())
+
+
+def _workspaces(nbytes):
+    """The same number of bytes holding zeros, NaN in bf16 and fp32, and infinities in
+    bf16, each before bytes that no call may touch."""
+    for fill in (0x0000, 0xFFFF, 0x7F80):
+        words = torch.full(((nbytes + 4096) // 2,), fill, dtype=torch.int32, device=DEV).to(torch.int16)
+        raw = words.view(torch.uint8)
+        yield raw[:nbytes], lambda raw=raw, fill=fill: bool(((raw[nbytes:].view(torch.int16).int() & 0xFFFF) == fill).all())
+
+
+@pytest.mark.parametrize("labelled", [1.0, 0.86, 0.5, 0.02])
+@pytest.mark.parametrize("width,vocab", [(1024, 2003), (264, 300)])
+@pytest.mark.parametrize("rows", [1, 31, 64, 65, 90, 96, 97, 128, 129, 150, 290, 300, 417, 500, 700, 870, 1000])
+def test_linear_loss_does_not_depend_on_what_the_workspace_holds(rows, width, vocab, labelled):
+    hidden, weight, labels, row_weight = _head(rows, width, vocab, seed=rows)
+    labels = torch.where(labels < 0, 0, labels)
+    labels[int(math.ceil(rows * labelled)):] = -1
+    labels = labels[torch.randperm(rows, generator=_gen(rows), device=DEV)].contiguous()
+    for dh, dw in ((True, True), (False, True), (True, False), (False, False)):
+        first = None
+        for ws, untouched in _workspaces(sw.slimwise_linear_loss_workspace_size(rows, width, vocab, dh, dw)):
+            got = sw.slimwise_linear_loss(hidden, weight, labels, row_weight, grad_hidden=dh, grad_weight=dw, workspace=ws)
+            got = [t.clone() for t in got if t is not None]
+            first = first or got
+            assert untouched()
+            assert all(torch.equal(x, y) and bool(x.isfinite().all()) for x, y in zip(got, first))
+
+
+@pytest.mark.parametrize("rows,hidden,vocab", [(1, 8, 3), (100, 64, 50), (700, 257, 501), (5000, 1000, 777)])
+def test_embed_and_norm_gradients_do_not_depend_on_what_the_workspace_holds(rows, hidden, vocab):
+    grad, x = _randn(rows, hidden, seed=1).to(BF16), _randn(rows, hidden, seed=2).to(BF16)
+    w, ids = _randn(hidden, seed=3), _ids(rows, vocab, seed=4)
+    _, mean, rstd = sw.slimwise_norm(x, w, layer=True)
+    first = None
+    for ws, untouched in _workspaces(sw.slimwise_embed_grad_workspace_size(rows, hidden)):
+        out = torch.empty((vocab, hidden), device=DEV)
+        sw.slimwise_embed_grad(grad, ids, out, workspace=ws)
+        first = out if first is None else first
+        assert untouched() and torch.equal(out, first)
+    first = None
+    for ws, untouched in _workspaces(sw.slimwise_norm_grad_workspace_size(rows, hidden)):
+        got = sw.slimwise_norm_grad(grad, x, w, rstd, mean, workspace=ws)
+        first = first or got
+        assert untouched() and all(torch.equal(a, b) for a, b in zip(got, first))
