@@ -562,7 +562,9 @@ int slimwise_norm_grad(const void *dy, int64_t dy_stride, const void *x, int32_t
  *   grad_weight  grad_weight_dtype [vocab, width], NULL to skip
  *   workspace    256-byte aligned, slimwise_linear_loss_workspace_size() bytes for
  *                the gradients asked for: 2 bytes for each row and token, at most
- *                2^31 of them, and less beside
+ *                2^31 of them, and a 32nd of that; up to 8 for each element of
+ *                hidden; 160 MB for sums of a split product; and, where the rows
+ *                come in chunks, 4 for each element of weight
  * A row with a label >= vocab, a NaN or a logit of +inf has NaN loss and gradient,
  * and grad_weight is then NaN where the formula has it.  dz's numerators (which the
  * products take) and the rows scaled by their weights are rounded to bf16.  A device

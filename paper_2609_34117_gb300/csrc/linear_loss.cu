@@ -979,7 +979,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
 #pragma unroll
             for (int j = 0; j < 32; j += 4)
               if (col + j < c.H) {
-                const float4 x = *reinterpret_cast<const float4 *>(acc + col + j);
+                const float4 x = __ldcg(reinterpret_cast<const float4 *>(acc + col + j));
                 z[j] += x.x; z[j + 1] += x.y; z[j + 2] += x.z; z[j + 3] += x.w;
               }
           if (last && !c.dw_fp32) {
