@@ -49,6 +49,46 @@ __device__ __forceinline__ void group_sum(float (&v)[K], float *buf, int &turn) 
   }
 }
 
+// How rows lie: on 16-byte boundaries and a multiple of 16 bytes long (or an element an
+// access, V = 1); anywhere; or anywhere, but a call's tensors alike, a row's start as
+// far behind a boundary in each.
+enum Form { kAligned, kAnywhere, kAlike };
+// kAlike: every eighth row starts at the same distance from a boundary, so a CTA takes
+// the rows of one class, r = class + 8 k.  Of such a row the `body` is whole windows
+// behind `head` elements; those before and behind it, 14 at the most, are held one more by the
+// first threads of a group (column `own`, else -1): no shifts, no windows in part.  Where
+// tensors do not lie so, windows are shifted into place on their way in and out.
+constexpr int kClasses = 8;
+template <bool kSame>
+struct RowsOf {
+  int cls, units, ctas, cta;  // rows of the class, and CTAs; this one
+  int head, body, ends, own;
+  // (t: of a group's threads; base: of a tensor with rows of `size` bytes an element)
+  __device__ __forceinline__ RowsOf(int rows, int hidden, const void *base, int64_t stride, int size, int t) {
+    cls = kSame ? (int)blockIdx.x % kClasses : 0;
+    units = kSame ? (rows - cls + kClasses - 1) / kClasses : rows;
+    ctas = kSame ? ((int)gridDim.x - cls + kClasses - 1) / kClasses : (int)gridDim.x;
+    cta = kSame ? (int)blockIdx.x / kClasses : (int)blockIdx.x;
+    const int v = 16 / size;
+    const uintptr_t start = reinterpret_cast<uintptr_t>(base) + (uintptr_t)(cls * stride * size);
+    head = kSame ? min((int)(-start & 15) / size, hidden) : 0;
+    body = kSame ? (hidden - head) / v * v : hidden;
+    ends = hidden - body;
+    own = !kSame || t >= ends ? -1 : t < head ? t : body + t;
+  }
+  __device__ __forceinline__ int64_t row(int64_t unit) const { return kSame ? cls + kClasses * unit : unit; }
+};
+// Element `own` of a row, or 0, as it lies (bf16).
+template <typename T>
+__device__ __forceinline__ uint32_t read_own(const T *row, int own) {
+  return own >= 0 ? (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(row + own)) : 0u;
+}
+__device__ __forceinline__ float own_value(uint32_t bits) { return __uint_as_float(bits << 16); }
+template <typename T>
+__device__ __forceinline__ void write_own(T *row, int own, float v) {
+  if (own >= 0) *reinterpret_cast<unsigned short *>(row + own) = (unsigned short)pack_bf16(v, 0.0f);
+}
+
 // Group g's barrier.
 template <int TPR>
 __device__ __forceinline__ void group_barrier(int g) {
@@ -78,9 +118,10 @@ constexpr int kNormBlock = TPR > kNormThreads ? TPR : kNormThreads;
 template <typename T, bool kAny, int N>
 constexpr int kNormRows = kAny ? 1 : N * (int)sizeof(T) >= 64 ? 1 : 64 / (N * (int)sizeof(T)) > 2 ? 2 : 64 / (N * (int)sizeof(T));
 
-template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
+template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     norm_kernel(const T *__restrict__ x, NormArgs a, T *__restrict__ y) {
+  constexpr bool kAny = kForm == kAnywhere, kSame = kForm == kAlike;
   constexpr int R = kNormRows<T, kAny, N>, P = N / V, W = TPR / 32, kGroups = kNormBlock<TPR> / TPR;
   constexpr bool kHeld = N <= 16;
   using Part = RowPart<T, V, N>;
@@ -89,19 +130,22 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
   __shared__ __align__(16) unsigned char rows_out[kAny ? kGroups * R * kStaged * sizeof(T) : 16];
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv = 1.0f / (float)a.hidden;
+  const RowsOf<kSame> rows(a.rows, a.hidden, x, a.stride, (int)sizeof(T), t);
   // columns of this warp, and of the warp whose sums this lane joins
   auto columns = [&](int warp) {
     int n = 0;
 #pragma unroll
-    for (int k = 0; k < P; ++k) n += max(0, min(a.hidden - (k * TPR + 32 * warp) * V, 32 * V));
-    return (float)n;
+    for (int k = 0; k < P; ++k) n += max(0, min(rows.body - (k * TPR + 32 * warp) * V, 32 * V));
+    return (float)(n + (warp == 0 ? rows.ends : 0));
   };
   const float warp_n = columns(t / 32), lane_n = columns(t & (W - 1));
   const float warp_inv = warp_n > 0.0f ? 1.0f / warp_n : 0.0f, lane_inv = lane_n > 0.0f ? 1.0f / lane_n : 0.0f;
   auto pair = [&](const float *p, int e) {
     const int c = Part::column(e, t, TPR), c1 = Part::column(e + 1, t, TPR);
-    return f2(p && c < a.hidden ? __ldg(p + c) : 0.0f, p && c1 < a.hidden ? __ldg(p + c1) : 0.0f);
+    return f2(p && c < rows.body ? __ldg(p + rows.head + c) : 0.0f, p && c1 < rows.body ? __ldg(p + rows.head + c1) : 0.0f);
   };
+  const float own_g = kSame && rows.own >= 0 ? __ldg(a.weight + rows.own) : 0.0f;
+  const float own_o = kSame && rows.own >= 0 && a.bias ? __ldg(a.bias + rows.own) : 0.0f;
   F2 g[kHeld ? N / 2 : 1], o[kHeld ? N / 2 : 1];
   if constexpr (kHeld)
 #pragma unroll
@@ -110,13 +154,15 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
       o[e / 2] = pair(a.bias, e);
     }
   using Coming = typename std::conditional<kAny, Windows<T, kAny ? N : 16 / sizeof(T)>, Part>::type;
+  uint32_t own[R], own_next[R];  // kAlike: this thread's element beside the body
   auto fetch = [&](Coming (&p)[R], int64_t r0) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const T *row = x + (r0 + i < a.rows ? r0 + i : 0) * a.stride;
-      const int width = r0 + i < a.rows ? a.hidden : 0;
+      const T *row = x + (r0 + i < rows.units ? rows.row(r0 + i) : 0) * a.stride;
+      const int width = r0 + i < rows.units ? rows.body : 0;
       if constexpr (kAny) p[i].load(row, t, TPR, width, a.x);
-      else p[i].load(row, t, TPR, width);
+      else p[i].load(row + rows.head, t, TPR, width);
+      if (kSame && t < 32) own_next[i] = read_own(row, rows.own);
     }
   };
   auto arrive = [&](Part (&p)[R], const Coming (&next)[R]) {
@@ -124,19 +170,20 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     for (int i = 0; i < R; ++i) {
       if constexpr (kAny) p[i].take(next[i], t, TPR, a.hidden);
       else p[i] = next[i];
+      if constexpr (kSame) own[i] = own_next[i];
     }
   };
-  const int64_t step = (int64_t)gridDim.x * kGroups * R;
-  int64_t r0 = ((int64_t)blockIdx.x * kGroups + group) * R;
+  const int64_t step = (int64_t)rows.ctas * kGroups * R;
+  int64_t r0 = ((int64_t)rows.cta * kGroups + group) * R;
   int turn = 0;
   T *staged = reinterpret_cast<T *>(rows_out) + (kAny ? group * R * kStaged : 0);
   Part p[R];
   Coming next[R];
-  if (kHeld && r0 < a.rows) {
+  if (kHeld && r0 < rows.units) {
     fetch(next, r0);
     arrive(p, next);
   }
-  for (; r0 < a.rows; r0 += step) {
+  for (; r0 < rows.units; r0 += step) {
     fetch(next, kHeld ? r0 + step : r0);
     if constexpr (!kHeld) arrive(p, next);
     float mu[R], q[R];
@@ -148,7 +195,9 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
 #pragma unroll
         for (int e = 0; e < N; e += 2) s = add2(s, p[i].get2(e));
         const float2 h = halves(s);
-        mu[i] = warp_sum(h.x + h.y);
+        mu[i] = h.x + h.y;
+        if (kSame && t < 32) mu[i] += own_value(own[i]);
+        mu[i] = warp_sum(mu[i]);
       }
     }
     // the squares (layer norm: about the mean of the warp's columns)
@@ -163,15 +212,20 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
         if constexpr (kLayer) {
           d = add2(d, m);
           // (the last pieces may have columns past the row)
-          if (!full && ((e + 1) / V + 1) * TPR * V > a.hidden) {
+          if (!full && ((e + 1) / V + 1) * TPR * V > rows.body) {
             const float2 h = halves(d);
-            d = f2(Part::column(e, t, TPR) < a.hidden ? h.x : 0.0f, Part::column(e + 1, t, TPR) < a.hidden ? h.y : 0.0f);
+            d = f2(Part::column(e, t, TPR) < rows.body ? h.x : 0.0f, Part::column(e + 1, t, TPR) < rows.body ? h.y : 0.0f);
           }
         }
         s = fma2(d, d, s);
       }
       const float2 h = halves(s);
-      q[i] = warp_sum(h.x + h.y);
+      q[i] = h.x + h.y;
+      if (kSame && t < 32) {
+        const float d = rows.own >= 0 ? own_value(own[i]) - (kLayer ? mu[i] * warp_inv : 0.0f) : 0.0f;
+        q[i] = fmaf(d, d, q[i]);
+      }
+      q[i] = warp_sum(q[i]);
     }
     if constexpr (TPR > 32) {
       // of the row, a lane a warp: the warps' squares about their means, moved to the row's
@@ -203,11 +257,12 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     }
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      if (r0 + i >= a.rows) continue;
+      if (r0 + i >= rows.units) continue;
+      const int64_t r = rows.row(r0 + i);
       const float rs = rsqrtf(fmaf(q[i], inv, a.eps));
       if (t == 0) {
-        a.rstd[r0 + i] = rs;
-        if constexpr (kLayer) a.mean[r0 + i] = mu[i];
+        a.rstd[r] = rs;
+        if constexpr (kLayer) a.mean[r] = mu[i];
       }
       const F2 m = f2(-mu[i]), f = f2(rs);
 #pragma unroll
@@ -218,7 +273,9 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
         else p[i].set2(e, fma2(mul2(v, f), pair(a.weight, e), pair(a.bias, e)));
       }
       if constexpr (kAny) p[i].stage(staged + i * kStaged, t, TPR, a.hidden);
-      else p[i].store(y + (r0 + i) * a.y_stride, t, TPR, a.hidden);
+      else p[i].store(y + r * a.y_stride + rows.head, t, TPR, rows.body);
+      if (kSame && t < 32)
+        write_own(y + r * a.y_stride, rows.own, fmaf((own_value(own[i]) - (kLayer ? mu[i] : 0.0f)) * rs, own_g, own_o));
     }
     if constexpr (kAny) {
       group_barrier<TPR>(group);
@@ -256,12 +313,15 @@ constexpr int kBatch = N * (int)sizeof(T) >= 32 ? 1 : 32 / (N * (int)sizeof(T));
 template <int N>
 constexpr bool kAhead = N < 32;
 
-template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
+template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     norm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ x, GradArgs a,
                      T *__restrict__ dx) {
+  constexpr bool kAny = kForm == kAnywhere, kSame = kForm == kAlike;
   constexpr int R = kBatch<T, N>, K = kLayer ? 2 * R : R;
   constexpr int kGroups = kBlock<TPR> / TPR;
+  // (kAlike: the registers do not hold the weights too)
+  constexpr bool kStored = kSame && kLayer && N == 16;
   constexpr bool kShared = N >= 32;  // dg, db in shared memory; the weight is read for each row
   using Part = RowPart<T, V, N>;
   using Coming = typename std::conditional<kAny, Windows<T, kAny ? N : 16 / sizeof(T)>, Part>::type;
@@ -282,43 +342,56 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv = 1.0f / (float)a.hidden;
   T *staged = reinterpret_cast<T *>(rows_out) + (kAny ? group * R * kStaged : 0);
+  const RowsOf<kSame> rows(a.rows, a.hidden, x, a.stride, (int)sizeof(T), t);
   auto read_weight = [&](int e) {
     const int c = Part::column(e, t, TPR), c1 = Part::column(e + 1, t, TPR);
-    return f2(c < a.hidden ? __ldg(a.weight + c) : 0.0f, c1 < a.hidden ? __ldg(a.weight + c1) : 0.0f);
+    return f2(c < rows.body ? __ldg(a.weight + rows.head + c) : 0.0f,
+              c1 < rows.body ? __ldg(a.weight + rows.head + c1) : 0.0f);
   };
-  F2 g[kShared ? 1 : N / 2], dg[kShared ? 1 : N / 2], db[kShared ? 1 : N / 2];
+  // kAlike: this thread's element beside the body, of x and above it of dy
+  uint32_t own[R], own_next[R];
+  const float own_g = kSame && rows.own >= 0 ? __ldg(a.weight + rows.own) : 0.0f;
+  float own_dg = 0.0f, own_db = 0.0f;
+  auto own_x = [](uint32_t v) { return own_value(v); };
+  auto own_dy = [](uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); };
+  __shared__ F2 weights[kStored ? N / 2 * TPR : 1];
+  F2 g[kShared || kStored ? 1 : N / 2], dg[kShared ? 1 : N / 2], db[kShared ? 1 : N / 2];
 #pragma unroll
   for (int e = 0; e < N / 2; ++e) {
     if constexpr (kShared) {
       reinterpret_cast<F2 *>(held)[e * TPR + t] = f2(0.0f);
       if constexpr (kLayer) reinterpret_cast<F2 *>(held)[(N / 2 + e) * TPR + t] = f2(0.0f);
     } else {
-      g[e] = read_weight(2 * e);
+      if constexpr (kStored) weights[e * TPR + t] = read_weight(2 * e);
+      else g[e] = read_weight(2 * e);
       dg[e] = db[e] = f2(0.0f);
     }
   }
   auto weight = [&](int e) {
-    if constexpr (!kShared) return g[e / 2];
+    if constexpr (kStored) return weights[e / 2 * TPR + t];
+    else if constexpr (!kShared) return g[e / 2];
     else return read_weight(e);
   };
   auto fetch = [&](ComingBatch &b, int r0) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const bool in = r0 + i < a.rows;
-      const int64_t r = in ? r0 + i : 0;
+      const bool in = r0 + i < rows.units;
+      const int64_t r = in ? rows.row(r0 + i) : 0;
       if constexpr (kAny) {
         b.d[i].load(dy + r * a.dy_stride, t, TPR, in ? a.hidden : 0, a.dy);
         b.x[i].load(x + r * a.stride, t, TPR, in ? a.hidden : 0, a.x);
       } else {
-        b.d[i].load(dy + r * a.dy_stride, t, TPR, in ? a.hidden : 0);
-        b.x[i].load(x + r * a.stride, t, TPR, in ? a.hidden : 0);
+        b.d[i].load(dy + r * a.dy_stride + rows.head, t, TPR, in ? rows.body : 0);
+        b.x[i].load(x + r * a.stride + rows.head, t, TPR, in ? rows.body : 0);
       }
+      if constexpr (kSame)
+        own_next[i] = read_own(x + r * a.stride, in ? rows.own : -1) | read_own(dy + r * a.dy_stride, in ? rows.own : -1) << 16;
       b.rs[i] = in ? __ldg(a.rstd + r) : 0.0f;
       b.mu[i] = kLayer && in ? __ldg(a.mean + r) : 0.0f;
     }
   };
-  const int step = gridDim.x * kGroups * R;
-  int r0 = (blockIdx.x * kGroups + group) * R;
+  const int step = rows.ctas * kGroups * R;
+  int r0 = (rows.cta * kGroups + group) * R;
   Batch now;
   ComingBatch next;
   auto arrive = [&]() {
@@ -331,16 +404,17 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
         now.d[i] = next.d[i];
         now.x[i] = next.x[i];
       }
+      if constexpr (kSame) own[i] = own_next[i];
       now.mu[i] = next.mu[i];
       now.rs[i] = next.rs[i];
     }
   };
-  if (kAhead<N> && r0 < a.rows) {
+  if (kAhead<N> && r0 < rows.units) {
     fetch(next, r0);
     arrive();
   }
-  for (; r0 < a.rows; r0 += step) {
-    fetch(next, !kAhead<N> ? r0 : r0 + step < a.rows ? r0 + step : a.rows);
+  for (; r0 < rows.units; r0 += step) {
+    fetch(next, !kAhead<N> ? r0 : r0 + step < rows.units ? r0 + step : rows.units);
     if constexpr (!kAhead<N>) arrive();
     float s[K];
 #pragma unroll
@@ -368,11 +442,20 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
       const float2 h = halves(sum), h0 = halves(sum0);
       s[i] = h.x + h.y;
       if constexpr (kLayer) s[R + i] = h0.x + h0.y;
+      if (kSame && t < 32) {
+        const float n = (own_x(own[i]) - now.mu[i]) * now.rs[i], d = own_dy(own[i]);
+        s[i] = fmaf(n, d * own_g, s[i]);
+        own_dg = fmaf(d, n, own_dg);
+        if constexpr (kLayer) {
+          s[R + i] += d * own_g;
+          own_db += d;
+        }
+      }
     }
     group_sum<TPR>(s, buf, turn);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      if (r0 + i >= a.rows) continue;
+      if (r0 + i >= rows.units) continue;
       // dx = rs g - rs m0 - n rs m
       const float rs = now.rs[i];
       const F2 u = f2(-now.mu[i]), v = f2(rs), m = f2(-rs * (s[i] * inv)), m0 = f2(kLayer ? -rs * (s[R + i] * inv) : 0.0f);
@@ -385,7 +468,11 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
         now.x[i].set2(e, fma2(n, m, ge));
       }
       if constexpr (kAny) now.x[i].stage(staged + i * kStaged, t, TPR, a.hidden);
-      else now.x[i].store(dx + (int64_t)(r0 + i) * a.dx_stride, t, TPR, a.hidden);
+      else now.x[i].store(dx + rows.row(r0 + i) * a.dx_stride + rows.head, t, TPR, rows.body);
+      if (kSame && t < 32) {
+        const float n = (own_x(own[i]) - now.mu[i]) * rs, k = -rs * (s[i] * inv), k0 = kLayer ? -rs * (s[R + i] * inv) : 0.0f;
+        write_own(dx + rows.row(r0 + i) * a.dx_stride, rows.own, fmaf(n, k, fmaf(own_dy(own[i]) * own_g, rs, k0)));
+      }
     }
     if constexpr (kAny) {
       group_barrier<TPR>(group);
@@ -402,8 +489,16 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
   float *out = a.partial + (int64_t)blockIdx.x * (kLayer ? 2 : 1) * a.hidden;
   F2 *mine = reinterpret_cast<F2 *>(held);
   if constexpr (kGroups > 1) {
+    __shared__ float2 own_sum[kSame ? TPR : 1];
     for (int k = 0; k < kGroups; ++k) {
       if (group == k) {
+        if constexpr (kSame) {
+          if (k) {
+            own_dg += own_sum[t].x;
+            own_db += own_sum[t].y;
+          }
+          own_sum[t] = make_float2(own_dg, own_db);
+        }
 #pragma unroll
         for (int e = 0; e < N / 2; ++e) {
           mine[e * TPR + t] = k ? add2(mine[e * TPR + t], dg[e]) : dg[e];
@@ -413,6 +508,14 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
       __syncthreads();
     }
     if (group != 0) return;
+    if constexpr (kSame) {
+      own_dg = own_sum[t].x;
+      own_db = own_sum[t].y;
+    }
+  }
+  if (kSame && rows.own >= 0) {
+    out[rows.own] = own_dg;
+    if constexpr (kLayer) out[a.hidden + rows.own] = own_db;
   }
 #pragma unroll
   for (int e = 0; e < N / 2; ++e) {
@@ -421,207 +524,11 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     if constexpr (kLayer) b = halves(kShared || kGroups > 1 ? mine[(N / 2 + e) * TPR + t] : db[e]);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int c = Part::column(2 * e + j, t, TPR);
-      if (c >= a.hidden) continue;
+      int c = Part::column(2 * e + j, t, TPR);
+      if (c >= rows.body) continue;
+      c += rows.head;
       out[c] = j ? v.y : v.x;
       if constexpr (kLayer) out[a.hidden + c] = j ? b.y : b.x;
-    }
-  }
-}
-
-// Rows above 4096: the sums of a thread's columns leave no registers for rows.  These
-// pass through a ring in shared memory instead, where each thread copies its own
-// columns ahead (no barriers about data) and reads them twice: for the row's sums,
-// and for dx once these are known, which is one row later, so that the sums' way
-// through the warps and the barrier is hidden behind the row before.
-// (Aligned rows, and fp32 ones by element; 32 columns of fp32 a thread would fill the ring
-// with one row.)  By element the copies are what takes the time: 4099 x 5001 fp32 67 us,
-// with the next row in registers, for which 10 columns a thread leave room, 42.
-constexpr int kRingThreads = 512, kRingBytes = 200 * 1024;
-template <typename T, int V, bool kAny, int N>
-constexpr bool kRing = !kAny && N >= 16 && N * sizeof(T) <= 64 && (V * sizeof(T) == 16 || sizeof(T) == 4);
-
-template <int B>
-__device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool in) {
-  // (0 bytes of the source: zeros)
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(B), "r"(in ? B : 0)
-               : "memory");
-}
-
-template <typename T, int V, int N, bool kLayer>
-__global__ void __launch_bounds__(kRingThreads, 1)
-    norm_grad_ring_kernel(const T *__restrict__ dy, const T *__restrict__ x, GradArgs a, T *__restrict__ dx,
-                          int slots) {
-  constexpr int P = N / V, B = V * (int)sizeof(T), K = kLayer ? 2 : 1, W = kRingThreads / 32;
-  using Part = RowPart<T, V, V < 2 ? 2 : V>;  // a piece (V = 1: two)
-  constexpr int Q = V < 2 ? 2 : 1, E = V * Q;
-  extern __shared__ __align__(16) unsigned char ring[];  // [slots][2][pieces][threads][V]
-  __shared__ float sums[2][2][W];
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const int pieces = (a.hidden + kRingThreads * V - 1) / (kRingThreads * V);
-  const uint32_t slot_bytes = 2u * pieces * kRingThreads * B;
-  const float inv = 1.0f / (float)a.hidden;
-  auto column = [&](int p) { return (p * kRingThreads + t) * V; };
-  F2 g[N / 2], dg[N / 2], db[kLayer ? N / 2 : 1];
-#pragma unroll
-  for (int e = 0; e < N; e += 2) {
-    const int c = column(e / V) + e % V, c1 = column((e + 1) / V) + (e + 1) % V;
-    g[e / 2] = f2(c < a.hidden ? __ldg(a.weight + c) : 0.0f, c1 < a.hidden ? __ldg(a.weight + c1) : 0.0f);
-    dg[e / 2] = f2(0.0f);
-    if constexpr (kLayer) db[e / 2] = f2(0.0f);
-  }
-  // Only the last piece has threads without columns; theirs read column 0 into it,
-  // 0 bytes of it.  Addresses are a thread's and the piece's constant.
-  constexpr uint32_t kStep = kRingThreads * B;
-  const int last = column(pieces - 1);
-  const bool in_last = last < a.hidden;
-  const uint32_t ring_at = smem_u32(ring) + (uint32_t)t * B, half = (uint32_t)pieces * kStep;
-  auto send = [&](int slot, int64_t r) {
-    if (r < a.rows) {
-      const uint32_t to = ring_at + (uint32_t)slot * slot_bytes;
-      const T *d = dy + r * a.dy_stride + t * V, *v = x + r * a.stride + t * V;
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        if (p + 1 >= pieces) break;
-        copy_async<B>(to + p * kStep, d + p * kRingThreads * V, true);
-        copy_async<B>(to + half + p * kStep, v + p * kRingThreads * V, true);
-      }
-      const uint32_t end = to + (uint32_t)(pieces - 1) * kStep;
-      copy_async<B>(end, dy + r * a.dy_stride + (in_last ? last : 0), in_last);
-      copy_async<B>(end + half, x + r * a.stride + (in_last ? last : 0), in_last);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  // E elements from piece p on of a row's half at `from`
-  auto take = [&](uint32_t from, int p) {
-    Part part;
-    if constexpr (B >= 16) {
-      const uint4 v = ld_shared_v4(from + p * kStep);
-      part.w[0] = v.x; part.w[1] = v.y; part.w[2] = v.z; part.w[3] = v.w;
-    } else {
-#pragma unroll
-      for (int q = 0; q < Q; ++q) {
-        // (an odd number of pieces: what follows them is read, and not used)
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(part.w[q]) : "r"(from + (p + q) * kStep) : "memory");
-      }
-    }
-    return part;
-  };
-  const int64_t first = blockIdx.x, step = gridDim.x;
-  for (int k = 0; k < slots - 1; ++k) send(k, first + k * step);
-  // of the row whose sums are made, of the one before, whose dx is, and of the next
-  float mu = 0.0f, rs = 0.0f, mu0 = 0.0f, rs0 = 0.0f, m = 0.0f, m0 = 0.0f, mu1 = 0.0f, rs1 = 0.0f;
-  auto statistics = [&](int64_t r, float &u, float &v) {
-    v = r < a.rows ? __ldg(a.rstd + r) : 0.0f;
-    u = kLayer && r < a.rows ? __ldg(a.mean + r) : 0.0f;
-  };
-  statistics(first, mu1, rs1);
-  int slot = 0, before = slots - 1, turn = 0;
-  for (int64_t r = first; r - step < a.rows; r += step) {
-    mu = mu1;
-    rs = rs1;
-    statistics(r + step, mu1, rs1);
-    // groups of copies so far: slots - 1 and one a row; this row's is done with all but the newest ones
-    switch (slots) {
-      case 3: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-      case 4: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-      case 5: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-      default: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
-    }
-    if (r < a.rows) {
-      F2 sum = f2(0.0f), sum0 = f2(0.0f);
-      const F2 u = f2(-mu), f = f2(rs);
-      const uint32_t from = ring_at + (uint32_t)slot * slot_bytes;
-#pragma unroll
-      for (int p = 0; p < P; p += Q) {
-        if (p >= pieces) break;
-        const Part d = take(from, p), v = take(from + half, p);
-#pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const int k = (p * V + e) / 2;
-          // (columns past the row: dy = 0 and the weight 0; a piece past the last: whatever it reads)
-          F2 n = v.get2(e), de = d.get2(e);
-          if (Q == 2 && p + 1 >= pieces) {
-            n = f2(v.get(0), 0.0f);
-            de = f2(d.get(0), 0.0f);
-          }
-          if constexpr (kLayer) n = add2(n, u);
-          n = mul2(n, f);
-          const F2 ge = mul2(de, g[k]);
-          sum = fma2(n, ge, sum);
-          dg[k] = fma2(de, n, dg[k]);
-          if constexpr (kLayer) {
-            sum0 = add2(sum0, ge);
-            db[k] = add2(db[k], de);
-          }
-        }
-      }
-      const float2 h = halves(sum), h0 = halves(sum0);
-      float s = h.x + h.y, s0 = h0.x + h0.y;
-      s = warp_sum(s);
-      if constexpr (kLayer) s0 = warp_sum(s0);
-      if (lane == 0) {
-        sums[turn][0][warp] = s;
-        if constexpr (kLayer) sums[turn][1][warp] = s0;
-      }
-    }
-    if (r > first) {
-      T *row = dx + (r - step) * a.dx_stride + t * V;
-      const uint32_t from = ring_at + (uint32_t)before * slot_bytes;
-      const F2 u = f2(-mu0), f = f2(rs0), a0 = f2(-rs0 * m0), a1 = f2(-rs0 * m);
-#pragma unroll
-      for (int p = 0; p < P; p += Q) {
-        if (p >= pieces) break;
-        const Part d = take(from, p), v = take(from + half, p);
-        Part o;
-#pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          F2 n = v.get2(e), ge = mul2(d.get2(e), g[(p * V + e) / 2]);
-          if constexpr (kLayer) n = add2(n, u);
-          n = mul2(n, f);
-          ge = kLayer ? fma2(ge, f, a0) : mul2(ge, f);
-          o.set2(e, fma2(n, a1, ge));
-        }
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-          T *to = row + (p + q) * kRingThreads * V;
-          if (p + q + 1 < pieces || (p + q + 1 == pieces && in_last)) {
-            if constexpr (B >= 16) *reinterpret_cast<uint4 *>(to) = make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]);
-            else *reinterpret_cast<uint32_t *>(to) = o.w[q];
-          }
-        }
-      }
-    }
-    // the slot of the row before is free: the row `slots` after that one
-    send(before, r + (slots - 1) * step);
-    __syncthreads();
-    m = sums[turn][0][lane & (W - 1)];
-    if constexpr (kLayer) m0 = sums[turn][1][lane & (W - 1)];
-#pragma unroll
-    for (int o = W / 2; o >= 1; o >>= 1) {
-      m += __shfl_xor_sync(0xFFFFFFFFu, m, o);
-      if constexpr (kLayer) m0 += __shfl_xor_sync(0xFFFFFFFFu, m0, o);
-    }
-    m *= inv;
-    m0 *= inv;
-    turn ^= 1;
-    mu0 = mu;
-    rs0 = rs;
-    before = slot;
-    slot = slot + 1 < slots ? slot + 1 : 0;
-  }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-  pdl_launch_dependents();
-  float *out = a.partial + (int64_t)blockIdx.x * K * a.hidden;
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int c = column(e / V) + e % V;
-    if (c >= a.hidden) continue;
-    const float2 v = halves(dg[e / 2]);
-    out[c] = e & 1 ? v.y : v.x;
-    if constexpr (kLayer) {
-      const float2 b = halves(db[e / 2]);
-      out[a.hidden + c] = e & 1 ? b.y : b.x;
     }
   }
 }
@@ -651,48 +558,37 @@ __global__ void __launch_bounds__(1024)
   }
 }
 
-int grad_ctas(int rows, int hidden) {
-  const int tpr = hidden <= 256 ? 32 : hidden <= 1024 ? 128 : hidden <= 2048 ? 256 : 512;
+int grad_ctas(int rows, int tpr) {
   const int groups = tpr == 32 ? kWarpRows : 1, most = kSms * (512 / (tpr * groups));
-  // (at least a row for every group)
-  const int ctas = (rows + groups - 1) / groups;
-  return ctas < most ? ctas : most;
+  // (at least a row for every group, and a CTA for every class of rows)
+  const int least = rows < kClasses ? rows : kClasses, ctas = (rows + groups - 1) / groups;
+  return ctas < least ? least : ctas < most ? ctas : most;
 }
 
-template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
+template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 cudaError_t norm_rows(const T *x, const NormArgs &a, T *y, cudaStream_t stream) {
   // at least a row for every group
   constexpr int kGroups = kNormBlock<TPR> / TPR;
-  const int most = kSms * (512 / kNormBlock<TPR>), ctas = (a.rows + kGroups - 1) / kGroups;
-  norm_kernel<T, V, kAny, TPR, N, kLayer><<<ctas < most ? ctas : most, kNormBlock<TPR>, 0, stream>>>(x, a, y);
+  const int most = kSms * (512 / kNormBlock<TPR>), least = a.rows < kClasses ? a.rows : kClasses;
+  int ctas = (a.rows + kGroups - 1) / kGroups;
+  ctas = kForm == kAlike && ctas < least ? least : ctas < most ? ctas : most;
+  norm_kernel<T, V, kForm, TPR, N, kLayer><<<ctas, kNormBlock<TPR>, 0, stream>>>(x, a, y);
   return cudaGetLastError();
 }
 
-template <typename T, int V, bool kAny, int TPR, int N, bool kLayer>
+template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *dweight,
                       float *dbias, cudaStream_t stream) {
-  const int ctas = grad_ctas(a.rows, a.hidden);
-  if constexpr (kRing<T, V, kAny, N>) {
-    // a row's two tensors, three to six times
-    constexpr int kPiece = kRingThreads * V * (int)sizeof(T);
-    const int row_bytes = 2 * ((a.hidden + kRingThreads * V - 1) / (kRingThreads * V)) * kPiece;
-    const int slots = kRingBytes / row_bytes < 6 ? kRingBytes / row_bytes : 6;
-    auto kernel = norm_grad_ring_kernel<T, V, N, kLayer>;
+  const int ctas = grad_ctas(a.rows, TPR);
+  constexpr bool kHeld = N >= 32 || kBlock<TPR> > TPR;
+  constexpr size_t smem = kHeld ? (size_t)(kLayer ? 2 : 1) * N * TPR * 4 : 0;
+  auto kernel = norm_grad_kernel<T, V, kForm, TPR, N, kLayer>;
+  if (smem > 48 * 1024) {
     const cudaError_t err =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + kPiece);
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (err != cudaSuccess) return err;
-    kernel<<<ctas, kRingThreads, (size_t)slots * row_bytes + kPiece, stream>>>(dy, x, a, dx, slots);
-  } else {
-    constexpr bool kHeld = N >= 32 || kBlock<TPR> > TPR;
-    constexpr size_t smem = kHeld ? (size_t)(kLayer ? 2 : 1) * N * TPR * 4 : 0;
-    auto kernel = norm_grad_kernel<T, V, kAny, TPR, N, kLayer>;
-    if (smem > 48 * 1024) {
-      const cudaError_t err =
-          cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (err != cudaSuccess) return err;
-    }
-    kernel<<<ctas, kBlock<TPR>, smem, stream>>>(dy, x, a, dx);
   }
+  kernel<<<ctas, kBlock<TPR>, smem, stream>>>(dy, x, a, dx);
   const cudaError_t err = cudaGetLastError();
   if (err != cudaSuccess) return err;
   const int columns = (kLayer ? 2 : 1) * a.hidden;
@@ -700,14 +596,26 @@ cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *
                         true, a.partial, ctas, columns, a.hidden, dweight, dbias);
 }
 
-// Calls f.template run<T, V, kAny>() for a row's type and alignment: 16 bytes an access,
+// Calls f.template run<T, V, form>() for a row's type and alignment: 16 bytes an access,
 // by windows where rows are not aligned (bf16), or an element an access (fp32, which
 // a warp's accesses take whole lines of all the same).
 template <typename F>
-cudaError_t dispatch(int dtype, bool aligned, const F &f) {
+cudaError_t dispatch(int dtype, bool aligned, bool alike, const F &f) {
   if (dtype == SLIMWISE_DTYPE_BF16)
-    return aligned ? f.template run<__nv_bfloat16, 8, false>() : f.template run<__nv_bfloat16, 8, true>();
-  return aligned ? f.template run<float, 4, false>() : f.template run<float, 1, false>();
+    return aligned ? f.template run<__nv_bfloat16, 8, kAligned>()
+           : alike ? f.template run<__nv_bfloat16, 8, kAlike>()
+                   : f.template run<__nv_bfloat16, 8, kAnywhere>();
+  return aligned ? f.template run<float, 4, kAligned>() : f.template run<float, 1, kAligned>();
+}
+
+// Whether each row starts at one distance from a 16-byte boundary in all n tensors.
+bool rows_alike(int element_bytes, int n, const void *const *base, const int64_t *stride) {
+  const int v = 16 / element_bytes;
+  bool ok = true;
+  for (int i = 1; i < n; ++i)
+    ok = ok && (reinterpret_cast<uintptr_t>(base[i]) - reinterpret_cast<uintptr_t>(base[0])) % 16 == 0 &&
+         (stride[i] - stride[0]) % v == 0;
+  return ok;
 }
 
 template <bool kLayer>
@@ -716,19 +624,19 @@ struct NormCall {
   NormArgs a;
   void *y;
   cudaStream_t stream;
-  template <typename T, int V, bool kAny, int TPR, int N>
+  template <typename T, int V, Form kForm, int TPR, int N>
   cudaError_t rows() const {
-    return norm_rows<T, V, kAny, TPR, N, kLayer>(static_cast<const T *>(x), a, static_cast<T *>(y), stream);
+    return norm_rows<T, V, kForm, TPR, N, kLayer>(static_cast<const T *>(x), a, static_cast<T *>(y), stream);
   }
-  template <typename T, int V, bool kAny>
+  template <typename T, int V, Form kForm>
   cudaError_t run() const {
-    return a.hidden <= 256    ? rows<T, V, kAny, 32, 8>()
-           : a.hidden <= 512  ? rows<T, V, kAny, 32, 16>()
-           : a.hidden <= 1024 ? rows<T, V, kAny, 64, 16>()
-           : a.hidden <= 2048 ? rows<T, V, kAny, 128, 16>()
-           : a.hidden <= 4096 ? rows<T, V, kAny, 256, 16>()
-           : a.hidden <= 8192 ? rows<T, V, kAny, 512, 16>()
-                              : rows<T, V, kAny, 512, 32>();
+    return a.hidden <= 256    ? rows<T, V, kForm, 32, 8>()
+           : a.hidden <= 512  ? rows<T, V, kForm, 32, 16>()
+           : a.hidden <= 1024 ? rows<T, V, kForm, 64, 16>()
+           : a.hidden <= 2048 ? rows<T, V, kForm, 128, 16>()
+           : a.hidden <= 4096 ? rows<T, V, kForm, 256, 16>()
+           : a.hidden <= 8192 ? rows<T, V, kForm, 512, 16>()
+                              : rows<T, V, kForm, 512, 32>();
   }
 };
 
@@ -739,21 +647,21 @@ struct GradCall {
   void *dx;
   float *dweight, *dbias;
   cudaStream_t stream;
-  template <typename T, int V, bool kAny, int TPR, int N>
+  template <typename T, int V, Form kForm, int TPR, int N>
   cudaError_t rows() const {
-    return grad_rows<T, V, kAny, TPR, N, kLayer>(static_cast<const T *>(dy), static_cast<const T *>(x), a,
+    return grad_rows<T, V, kForm, TPR, N, kLayer>(static_cast<const T *>(dy), static_cast<const T *>(x), a,
                                            static_cast<T *>(dx), dweight, dbias, stream);
   }
-  template <typename T, int V, bool kAny>
+  template <typename T, int V, Form kForm>
   cudaError_t run() const {
-    return a.hidden <= 256    ? rows<T, V, kAny, 32, 8>()
-           : a.hidden <= 1024 ? rows<T, V, kAny, 128, 8>()
-           : a.hidden <= 2048 ? rows<T, V, kAny, 256, 8>()
-           : a.hidden <= 4096 ? rows<T, V, kAny, 512, 8>()
-           : V < 4 && a.hidden <= 5120 ? rows<T, V, kAny, 512, V < 4 ? 10 : 16>()
-           : V < 8 && a.hidden <= 6144 ? rows<T, V, kAny, 512, V < 8 ? 12 : 16>()
-           : a.hidden <= 8192 ? rows<T, V, kAny, 512, 16>()
-                              : rows<T, V, kAny, 512, 32>();
+    return a.hidden <= 256    ? rows<T, V, kForm, 32, 8>()
+           : a.hidden <= 1024 ? rows<T, V, kForm, 128, 8>()
+           : a.hidden <= 2048 ? rows<T, V, kForm, 256, 8>()
+           : a.hidden <= 4096 ? rows<T, V, kForm, V == 8 ? 256 : 512, V == 8 ? 16 : 8>()
+           : V < 4 && a.hidden <= 5120 ? rows<T, V, kForm, 512, V < 4 ? 10 : 16>()
+           : V < 8 && a.hidden <= 6144 ? rows<T, V, kForm, 512, V < 8 ? 12 : 16>()
+           : a.hidden <= 8192 ? rows<T, V, kForm, 512, 16>()
+                              : rows<T, V, kForm, 512, 32>();
   }
 };
 
@@ -765,17 +673,20 @@ cudaError_t launch_norm(const void *x, int dtype, int rows, int hidden, int64_t 
   const void *base[2] = {x, y};
   const int64_t strides[2] = {stride, y_stride};
   const bool v = rows_aligned(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 2, base, strides);
+  const bool alike = rows_alike(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, 2, base, strides);
   const auto extent = [&](const void *p, int64_t step) {
     return dtype == SLIMWISE_DTYPE_BF16 ? extent_of(static_cast<const __nv_bfloat16 *>(p), rows, step, hidden)
                                         : extent_of(static_cast<const float *>(p), rows, step, hidden);
   };
   const NormArgs a = {rows, hidden, extent(x, stride), stride, y_stride, weight, bias, eps, mean, rstd};
-  return layer ? dispatch(dtype, v, NormCall<true>{x, a, y, stream})
-               : dispatch(dtype, v, NormCall<false>{x, a, y, stream});
+  return layer ? dispatch(dtype, v, alike, NormCall<true>{x, a, y, stream})
+               : dispatch(dtype, v, alike, NormCall<false>{x, a, y, stream});
 }
 
 size_t norm_grad_workspace(int rows, int hidden) {
-  return (size_t)grad_ctas(rows, hidden) * 2 * hidden * sizeof(float);
+  // (fp32 rows of 2049 to 4096 have half the CTAs)
+  return (size_t)grad_ctas(rows, hidden <= 256 ? 32 : hidden <= 1024 ? 128 : hidden <= 4096 ? 256 : 512) * 2 * hidden *
+         sizeof(float);
 }
 
 cudaError_t launch_norm_grad(const void *dy, int64_t dy_stride, const void *x, int dtype, int rows,
@@ -785,14 +696,15 @@ cudaError_t launch_norm_grad(const void *dy, int64_t dy_stride, const void *x, i
   const void *base[3] = {dy, x, dx};
   const int64_t strides[3] = {dy_stride, stride, dx_stride};
   const bool v = rows_aligned(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, hidden, 3, base, strides);
+  const bool alike = rows_alike(dtype == SLIMWISE_DTYPE_BF16 ? 2 : 4, 3, base, strides);
   const auto extent = [&](const void *p, int64_t step) {
     return dtype == SLIMWISE_DTYPE_BF16 ? extent_of(static_cast<const __nv_bfloat16 *>(p), rows, step, hidden)
                                         : extent_of(static_cast<const float *>(p), rows, step, hidden);
   };
   const GradArgs a = {rows, hidden, extent(dy, dy_stride), extent(x, stride), dy_stride, stride, dx_stride, weight, mean, rstd,
                       static_cast<float *>(workspace)};
-  return mean ? dispatch(dtype, v, GradCall<true>{dy, x, a, dx, dweight, dbias, stream})
-              : dispatch(dtype, v, GradCall<false>{dy, x, a, dx, dweight, dbias, stream});
+  return mean ? dispatch(dtype, v, alike, GradCall<true>{dy, x, a, dx, dweight, dbias, stream})
+              : dispatch(dtype, v, alike, GradCall<false>{dy, x, a, dx, dweight, dbias, stream});
 }
 
 }  // namespace slimwise

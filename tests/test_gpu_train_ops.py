@@ -640,3 +640,32 @@ def test_embed_and_norm_gradients_do_not_depend_on_what_the_workspace_holds(rows
         got = sw.slimwise_norm_grad(grad, x, w, rstd, mean, workspace=ws)
         first = first or got
         assert untouched() and all(torch.equal(a, b) for a, b in zip(got, first))
+
+
+@pytest.mark.parametrize("layer", [False, True])
+@pytest.mark.parametrize("pad,start", [(0, 0), (0, 3), (1, 0), (2, 5), (5, 7), (8, 1)])
+@pytest.mark.parametrize("rows,hidden", [
+    (1, 1), (1, 15), (2, 3), (7, 5), (8, 7), (9, 9), (20, 13), (63, 17), (64, 250), (65, 255), (300, 257), (3000, 99),
+    (11, 511), (700, 513), (40, 1001), (333, 1023), (17, 2047), (700, 2041), (30, 4001), (9, 4095), (400, 4093),
+    (21, 5001), (200, 8191), (33, 8193), (310, 16383), (5, 16381)])
+def test_norm_of_rows_that_start_alike_in_all_tensors(rows, hidden, pad, start, layer):
+    make = lambda values: _rows(values, BF16, pad=pad, start=start)
+    x, dy = make(_randn(rows, hidden, seed=1) * 2 + 0.5)[0], make(_randn(rows, hidden, seed=2))[0]
+    w, b = 1 + 0.2 * _randn(hidden, seed=3), 0.1 * _randn(hidden, seed=4)
+    (y, around), (dx, beside) = make(torch.zeros(rows, hidden, device=DEV)), make(torch.zeros(rows, hidden, device=DEV))
+    outside = int(torch.isnan(around).sum())
+    _check_norm(x, w, b, layer, y=y)
+    _check_norm_grad(dy, x, w, layer, dx=dx)
+    assert int(torch.isnan(around).sum()) == outside and int(torch.isnan(beside).sum()) == outside
+    again = sw.slimwise_norm(x, w, b, layer)[0]  # (the output elsewhere: other widths may round otherwise)
+    assert float((again.float() - y.float()).abs().max()) <= 2.0 ** -7 * float(y.float().abs().max())
+
+
+def test_norm_of_rows_that_start_alike_keeps_nan_and_infinities_in_their_rows():
+    x = _rows(_randn(70, 1003, seed=1), BF16)[0]
+    good = sw.slimwise_norm(x, torch.ones(1003, device=DEV), layer=True)[0].clone()
+    x[3, 0], x[10, 1002], x[33, 500] = NAN, math.inf, -math.inf
+    y = sw.slimwise_norm(x, torch.ones(1003, device=DEV), layer=True)[0]
+    bad = torch.zeros(70, dtype=torch.bool, device=DEV)
+    bad[[3, 10, 33]] = True
+    assert torch.equal(y[~bad], good[~bad]) and bool(y[bad].isnan().any(1).all())
