@@ -146,13 +146,15 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
   };
   const float own_g = kSame && rows.own >= 0 ? __ldg(a.weight + rows.own) : 0.0f;
   const float own_o = kSame && rows.own >= 0 && a.bias ? __ldg(a.bias + rows.own) : 0.0f;
+  // (32 elements a thread: in shared memory, [N / 2][TPR] of the weight, then of the bias)
   F2 g[kHeld ? N / 2 : 1], o[kHeld ? N / 2 : 1];
-  if constexpr (kHeld)
+  extern __shared__ __align__(16) float held[];
+  F2 *stored = reinterpret_cast<F2 *>(held) + t;
 #pragma unroll
-    for (int e = 0; e < N; e += 2) {
-      g[e / 2] = pair(a.weight, e);
-      o[e / 2] = pair(a.bias, e);
-    }
+  for (int e = 0; e < N; e += 2) {
+    (kHeld ? g[kHeld ? e / 2 : 0] : stored[e / 2 * TPR]) = pair(a.weight, e);
+    (kHeld ? o[kHeld ? e / 2 : 0] : stored[(N / 2 + e / 2) * TPR]) = pair(a.bias, e);
+  }
   using Coming = typename std::conditional<kAny, Windows<T, kAny ? N : 16 / sizeof(T)>, Part>::type;
   uint32_t own[R], own_next[R];  // kAlike: this thread's element beside the body
   auto fetch = [&](Coming (&p)[R], int64_t r0) {
@@ -179,13 +181,12 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
   T *staged = reinterpret_cast<T *>(rows_out) + (kAny ? group * R * kStaged : 0);
   Part p[R];
   Coming next[R];
-  if (kHeld && r0 < rows.units) {
+  if (r0 < rows.units) {
     fetch(next, r0);
     arrive(p, next);
   }
   for (; r0 < rows.units; r0 += step) {
-    fetch(next, kHeld ? r0 + step : r0);
-    if constexpr (!kHeld) arrive(p, next);
+    fetch(next, r0 + step);
     float mu[R], q[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -270,7 +271,7 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
         F2 v = p[i].get2(e);
         if constexpr (kLayer) v = add2(v, m);
         if constexpr (kHeld) p[i].set2(e, fma2(mul2(v, f), g[e / 2], o[e / 2]));
-        else p[i].set2(e, fma2(mul2(v, f), pair(a.weight, e), pair(a.bias, e)));
+        else p[i].set2(e, fma2(mul2(v, f), stored[e / 2 * TPR], stored[(N / 2 + e / 2) * TPR]));
       }
       if constexpr (kAny) p[i].stage(staged + i * kStaged, t, TPR, a.hidden);
       else p[i].store(y + r * a.y_stride + rows.head, t, TPR, rows.body);
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
       // (the next rows are staged behind the barrier of their sums, or a warp's own)
       if constexpr (TPR == 32) __syncwarp();
     }
-    if constexpr (kHeld) arrive(p, next);
+    arrive(p, next);
   }
 }
 
@@ -309,9 +310,18 @@ constexpr int kBlock = TPR == 32 ? 32 * kWarpRows : TPR;
 // hold both.
 template <typename T, int N>
 constexpr int kBatch = N * (int)sizeof(T) >= 32 ? 1 : 32 / (N * (int)sizeof(T));
-// (windows take twice the registers on their way)
-template <int N>
-constexpr bool kAhead = N < 32;
+// What of a thread does not stay in registers: the next row where it would take 64 of them
+// (windows take twice as many on their way); the columns' sums where these, the rows and
+// the next ones take 96 and more (aligned rows alone have room for 96); the weights of 24 columns
+// and more (and 16 where the rows' ends are held besides).  Sums and weights are then in shared
+// memory.
+template <typename T, Form kForm, int N>
+constexpr bool kAhead = N * (int)sizeof(T) <= (kForm == kAnywhere ? 48 : 96);
+template <typename T, Form kForm, int N, bool kLayer>
+constexpr bool kSumsShared = (kLayer ? 2 : 1) * N + N * (int)sizeof(T) / 2 *
+                             (1 + (kAhead<T, kForm, N> ? kForm == kAnywhere ? 2 : 1 : 0)) > (kForm == kAligned ? 96 : 95);
+template <Form kForm, int N, bool kLayer>
+constexpr bool kWeightsShared = N >= 24 || (kForm == kAlike && kLayer && N == 16);
 
 template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
@@ -320,9 +330,8 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
   constexpr bool kAny = kForm == kAnywhere, kSame = kForm == kAlike;
   constexpr int R = kBatch<T, N>, K = kLayer ? 2 * R : R;
   constexpr int kGroups = kBlock<TPR> / TPR;
-  // (kAlike: the registers do not hold the weights too)
-  constexpr bool kStored = kSame && kLayer && N == 16;
-  constexpr bool kShared = N >= 32;  // dg, db in shared memory; the weight is read for each row
+  constexpr bool kStored = kWeightsShared<kForm, N, kLayer>, kShared = kSumsShared<T, kForm, N, kLayer>;
+  constexpr bool kNext = kAhead<T, kForm, N>;
   using Part = RowPart<T, V, N>;
   using Coming = typename std::conditional<kAny, Windows<T, kAny ? N : 16 / sizeof(T)>, Part>::type;
   struct Batch {
@@ -336,7 +345,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
   __shared__ float buf[2 * K * (TPR / 32)];
   constexpr int kStaged = staged_elements<T>(TPR * N);
   __shared__ __align__(16) unsigned char rows_out[kAny ? kGroups * R * kStaged * sizeof(T) : 16];
-  // kShared: dg [N][TPR], db [N][TPR]; groups of a warp: one group's sums
+  // kShared: dg [N][TPR], db [N][TPR]; groups of a warp: one group's sums; kStored: weights [N][TPR]
   extern __shared__ __align__(16) float held[];
   int turn = 0;
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
@@ -354,23 +363,22 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
   float own_dg = 0.0f, own_db = 0.0f;
   auto own_x = [](uint32_t v) { return own_value(v); };
   auto own_dy = [](uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); };
-  __shared__ F2 weights[kStored ? N / 2 * TPR : 1];
-  F2 g[kShared || kStored ? 1 : N / 2], dg[kShared ? 1 : N / 2], db[kShared ? 1 : N / 2];
+  F2 *weights = reinterpret_cast<F2 *>(held) + (kShared ? (kLayer ? 2 : 1) * (N / 2) * TPR : 0);
+  F2 g[kStored ? 1 : N / 2], dg[kShared ? 1 : N / 2], db[kShared ? 1 : N / 2];
 #pragma unroll
   for (int e = 0; e < N / 2; ++e) {
+    if constexpr (kStored) weights[e * TPR + t] = read_weight(2 * e);
+    else g[e] = read_weight(2 * e);
     if constexpr (kShared) {
       reinterpret_cast<F2 *>(held)[e * TPR + t] = f2(0.0f);
       if constexpr (kLayer) reinterpret_cast<F2 *>(held)[(N / 2 + e) * TPR + t] = f2(0.0f);
     } else {
-      if constexpr (kStored) weights[e * TPR + t] = read_weight(2 * e);
-      else g[e] = read_weight(2 * e);
       dg[e] = db[e] = f2(0.0f);
     }
   }
   auto weight = [&](int e) {
     if constexpr (kStored) return weights[e / 2 * TPR + t];
-    else if constexpr (!kShared) return g[e / 2];
-    else return read_weight(e);
+    else return g[e / 2];
   };
   auto fetch = [&](ComingBatch &b, int r0) {
 #pragma unroll
@@ -409,13 +417,13 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
       now.rs[i] = next.rs[i];
     }
   };
-  if (kAhead<N> && r0 < rows.units) {
+  if (kNext && r0 < rows.units) {
     fetch(next, r0);
     arrive();
   }
   for (; r0 < rows.units; r0 += step) {
-    fetch(next, !kAhead<N> ? r0 : r0 + step < rows.units ? r0 + step : rows.units);
-    if constexpr (!kAhead<N>) arrive();
+    fetch(next, !kNext ? r0 : r0 + step < rows.units ? r0 + step : rows.units);
+    if constexpr (!kNext) arrive();
     float s[K];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -482,7 +490,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
           store_any(staged + i * kStaged, dx + (int64_t)(r0 + i) * a.dx_stride, t, TPR, a.hidden);
       if constexpr (TPR == 32) __syncwarp();
     }
-    if constexpr (kAhead<N>) arrive();
+    if constexpr (kNext) arrive();
   }
   pdl_launch_dependents();
   // the CTA's sums: its groups' in turn
@@ -572,7 +580,13 @@ cudaError_t norm_rows(const T *x, const NormArgs &a, T *y, cudaStream_t stream) 
   const int most = kSms * (512 / kNormBlock<TPR>), least = a.rows < kClasses ? a.rows : kClasses;
   int ctas = (a.rows + kGroups - 1) / kGroups;
   ctas = kForm == kAlike && ctas < least ? least : ctas < most ? ctas : most;
-  norm_kernel<T, V, kForm, TPR, N, kLayer><<<ctas, kNormBlock<TPR>, 0, stream>>>(x, a, y);
+  constexpr int kStored = N > 16 ? 2 * N * TPR * 4 : 0;
+  auto kernel = norm_kernel<T, V, kForm, TPR, N, kLayer>;
+  if (kStored) {
+    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStored);
+    if (err != cudaSuccess) return err;
+  }
+  kernel<<<ctas, kNormBlock<TPR>, kStored, stream>>>(x, a, y);
   return cudaGetLastError();
 }
 
@@ -580,10 +594,10 @@ template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *dweight,
                       float *dbias, cudaStream_t stream) {
   const int ctas = grad_ctas(a.rows, TPR);
-  constexpr bool kHeld = N >= 32 || kBlock<TPR> > TPR;
-  constexpr size_t smem = kHeld ? (size_t)(kLayer ? 2 : 1) * N * TPR * 4 : 0;
+  constexpr bool kHeld = kSumsShared<T, kForm, N, kLayer> || kBlock<TPR> > TPR;
+  constexpr size_t smem = (size_t)((kHeld ? kLayer ? 2 : 1 : 0) + (kWeightsShared<kForm, N, kLayer> ? 1 : 0)) * N * TPR * 4;
   auto kernel = norm_grad_kernel<T, V, kForm, TPR, N, kLayer>;
-  if (smem > 48 * 1024) {
+  if (N >= 16 && smem) {  // (with the static arrays it may be above 48 KB)
     const cudaError_t err =
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (err != cudaSuccess) return err;
@@ -635,8 +649,9 @@ struct NormCall {
            : a.hidden <= 1024 ? rows<T, V, kForm, 64, 16>()
            : a.hidden <= 2048 ? rows<T, V, kForm, 128, 16>()
            : a.hidden <= 4096 ? rows<T, V, kForm, 256, 16>()
-           : a.hidden <= 8192 ? rows<T, V, kForm, 512, 16>()
-                              : rows<T, V, kForm, 512, 32>();
+           : a.hidden <= 8192  ? rows<T, V, kForm, 512, 16>()
+           : a.hidden <= 12288 ? rows<T, V, kForm, 512, 24>()
+                               : rows<T, V, kForm, 512, 32>();
   }
 };
 
@@ -660,8 +675,9 @@ struct GradCall {
            : a.hidden <= 4096 ? rows<T, V, kForm, V == 8 ? 256 : 512, V == 8 ? 16 : 8>()
            : V < 4 && a.hidden <= 5120 ? rows<T, V, kForm, 512, V < 4 ? 10 : 16>()
            : V < 8 && a.hidden <= 6144 ? rows<T, V, kForm, 512, V < 8 ? 12 : 16>()
-           : a.hidden <= 8192 ? rows<T, V, kForm, 512, 16>()
-                              : rows<T, V, kForm, 512, 32>();
+           : a.hidden <= 8192  ? rows<T, V, kForm, 512, 16>()
+           : a.hidden <= 12288 ? rows<T, V, kForm, 512, 24>()
+                               : rows<T, V, kForm, 512, 32>();
   }
 };
 
