@@ -13,7 +13,7 @@
 // spread costs nothing of it.
 //
 // The gradient of the weight: a thread keeps the same columns for all rows of
-// its CTA, so dg and db stay in its registers (32 columns of a thread: in shared
+// its CTA, so dg and db stay in its registers (many columns of a thread: in its shared
 // memory) until the CTA's last row; a second kernel adds the CTAs' sums in order.
 #include <type_traits>
 
@@ -106,12 +106,13 @@ struct NormArgs {
 };
 
 // Threads of a row (TPR) and elements of a thread (N): rows up to 256 (32, 8), 512,
-// 1024, .. 8192 (32 .. 512, 16) and 16384 (512, 32).  Groups are persistent: the weight
-// and bias of a thread's columns stay in its registers, and R rows are on their way while R
-// others are worked on.  Bound by instructions: 16384 x 2048 bf16 layer norm 26 us (a copy
-// of as many bytes 23); with 8 elements a thread 30, a row's sums costing as much as its
-// elements; weights from the L1 cache for each row 36, L1 82 % busy.  Rows that are
-// not aligned: 32768 x 4001 bf16 184 us, by element 230.
+// 1024, .. 8192 (32 .. 512, 16), 12288 (512, 24) and 16384 (512, 32).  Groups are persistent:
+// the weight and bias of a thread's columns stay in its registers (24 and 32 elements: in
+// shared memory; 2000 x 16000 bf16 35 us, read from the caches for each row 94), and R
+// rows are on their way while R others are worked on.  Bound by memory and instructions:
+// 16384 x 2048 bf16 layer norm 26 us, by itself 23 (a copy of as many bytes 23); with 8
+// elements a thread 30, a row's sums costing as much as its elements.  bf16 rows of 4001,
+// 32768 of them: alike in x and y 98 us, anywhere 182, by element 230.
 constexpr int kNormThreads = 256;
 template <int TPR>
 constexpr int kNormBlock = TPR > kNormThreads ? TPR : kNormThreads;
@@ -298,14 +299,16 @@ struct GradArgs {
   float *partial;  // [CTAs][kLayer ? 2 : 1][hidden]
 };
 
-// Threads of a row (TPR) and elements of a thread (N): rows up to 256 (32, 8), 1024 (128,
-// 8), 2048 (256, 8), 4096 (512, 8), then 512 threads with 10, 12, 16 or 32.  A CTA holds
-// eight rows' groups of a warp, else one row's; 512 threads are on an SM.  Bound by
-// memory and a row's barrier: 16384 x 2048 bf16 RMS norm 36 us, 5.5 TB/s (a copy of as
-// many bytes 5.8); bf16 rows that are not aligned by their shifts: 32768 x 4001 325 us.
-constexpr int kWarpRows = 8;
+// Threads of a row (TPR) and elements of a thread (N): bf16 rows up to 256 (32, 8), 512
+// (32, 16), 1024 (128, 8), 2048 (256, 8), 4096 (256, 16), 8192 (512, 16), 12288 (512, 24)
+// and 16384 (512, 32); fp32 with more threads between, and 10 and 12 elements.  512 threads
+// are on an SM, several groups to a CTA, whose sums are joined before they leave: as many
+// CTAs as groups cost 4 us at 32768 x 1000.  Bound by memory and a row's barrier: 16384 x 2048
+// bf16 RMS norm 36 us, 5.5 TB/s (a copy of as many bytes 5.8).  A ring of asynchronous copies
+// in place of the next row in registers took 133 us for 6000 x 7168 fp32, this 96.  bf16
+// rows of 4001, 32768 of them: alike in all tensors 162, anywhere 283.
 template <int TPR>
-constexpr int kBlock = TPR == 32 ? 32 * kWarpRows : TPR;
+constexpr int kBlock = TPR == 32 ? 256 : 512;
 // Rows of a group at once; the next ones come into registers meanwhile where these
 // hold both.
 template <typename T, int N>
@@ -342,7 +345,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     Coming d[R], x[R];
     float mu[R], rs[R];
   };
-  __shared__ float buf[2 * K * (TPR / 32)];
+  __shared__ float buf[kGroups][2 * K * (TPR / 32)];
   constexpr int kStaged = staged_elements<T>(TPR * N);
   __shared__ __align__(16) unsigned char rows_out[kAny ? kGroups * R * kStaged * sizeof(T) : 16];
   // kShared: dg [N][TPR], db [N][TPR]; groups of a warp: one group's sums; kStored: weights [N][TPR]
@@ -363,7 +366,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
   float own_dg = 0.0f, own_db = 0.0f;
   auto own_x = [](uint32_t v) { return own_value(v); };
   auto own_dy = [](uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); };
-  F2 *weights = reinterpret_cast<F2 *>(held) + (kShared ? (kLayer ? 2 : 1) * (N / 2) * TPR : 0);
+  F2 *weights = reinterpret_cast<F2 *>(held) + (kShared || kGroups > 1 ? (kLayer ? 2 : 1) * (N / 2) * TPR : 0);
   F2 g[kStored ? 1 : N / 2], dg[kShared ? 1 : N / 2], db[kShared ? 1 : N / 2];
 #pragma unroll
   for (int e = 0; e < N / 2; ++e) {
@@ -460,7 +463,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
         }
       }
     }
-    group_sum<TPR>(s, buf, turn);
+    group_sum<TPR>(s, buf[group], turn);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (r0 + i >= rows.units) continue;
@@ -567,7 +570,7 @@ __global__ void __launch_bounds__(1024)
 }
 
 int grad_ctas(int rows, int tpr) {
-  const int groups = tpr == 32 ? kWarpRows : 1, most = kSms * (512 / (tpr * groups));
+  const int block = tpr == 32 ? kBlock<32> : kBlock<64>, groups = block / tpr, most = kSms * (512 / block);
   // (at least a row for every group, and a CTA for every class of rows)
   const int least = rows < kClasses ? rows : kClasses, ctas = (rows + groups - 1) / groups;
   return ctas < least ? least : ctas < most ? ctas : most;
@@ -670,6 +673,7 @@ struct GradCall {
   template <typename T, int V, Form kForm>
   cudaError_t run() const {
     return a.hidden <= 256    ? rows<T, V, kForm, 32, 8>()
+           : V == 8 && a.hidden <= 512 ? rows<T, V, kForm, 32, V == 8 ? 16 : 8>()
            : a.hidden <= 1024 ? rows<T, V, kForm, 128, 8>()
            : a.hidden <= 2048 ? rows<T, V, kForm, 256, 8>()
            : a.hidden <= 4096 ? rows<T, V, kForm, V == 8 ? 256 : 512, V == 8 ? 16 : 8>()
@@ -700,9 +704,9 @@ cudaError_t launch_norm(const void *x, int dtype, int rows, int hidden, int64_t 
 }
 
 size_t norm_grad_workspace(int rows, int hidden) {
-  // (fp32 rows of 2049 to 4096 have half the CTAs)
-  return (size_t)grad_ctas(rows, hidden <= 256 ? 32 : hidden <= 1024 ? 128 : hidden <= 4096 ? 256 : 512) * 2 * hidden *
-         sizeof(float);
+  // (of either type; groups of 512 threads have the most CTAs but for those of a warp)
+  const int narrow = hidden <= 512 ? grad_ctas(rows, 32) : 0, wide = grad_ctas(rows, 512);
+  return (size_t)(narrow > wide ? narrow : wide) * 2 * hidden * sizeof(float);
 }
 
 cudaError_t launch_norm_grad(const void *dy, int64_t dy_stride, const void *x, int dtype, int rows,
