@@ -49,15 +49,16 @@ __device__ __forceinline__ void group_sum(float (&v)[K], float *buf, int &turn) 
   }
 }
 
-// How rows lie: on 16-byte boundaries and a multiple of 16 bytes long (or an element an
-// access, V = 1); anywhere; or anywhere, but a call's tensors alike, a row's start as
-// far behind a boundary in each.
+// How bf16 rows lie: on 16-byte boundaries and a multiple of 16 bytes long; anywhere; or
+// anywhere, but a call's tensors alike, a row's start as far behind a boundary in each.
+// (fp32 rows: 16 bytes an access, or an element, which costs them little.)
 enum Form { kAligned, kAnywhere, kAlike };
-// kAlike: every eighth row starts at the same distance from a boundary, so a CTA takes
-// the rows of one class, r = class + 8 k.  Of such a row the `body` is whole windows
-// behind `head` elements; those before and behind it, 14 at the most, are held one more by the
-// first threads of a group (column `own`, else -1): no shifts, no windows in part.  Where
-// tensors do not lie so, windows are shifted into place on their way in and out.
+// Rows that are not aligned: every eighth starts at the same distance from a boundary, so a
+// CTA takes the rows of one class, r = class + 8 k.  Of such a row of the output, `body`
+// elements behind the first `head` are whole windows; those before and behind it, 14 at
+// the most, are held by the first threads of a group, one more element each (column `own`,
+// else -1).  kAlike: the inputs' windows are the same, nothing is shifted.  kAnywhere:
+// each access reads the two windows that its elements lie in, and shifts them.
 constexpr int kClasses = 8;
 template <bool kSame>
 struct RowsOf {
@@ -89,13 +90,6 @@ __device__ __forceinline__ void write_own(T *row, int own, float v) {
   if (own >= 0) *reinterpret_cast<unsigned short *>(row + own) = (unsigned short)pack_bf16(v, 0.0f);
 }
 
-// Group g's barrier.
-template <int TPR>
-__device__ __forceinline__ void group_barrier(int g) {
-  if constexpr (TPR == 32) __syncwarp();
-  else asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "n"(TPR) : "memory");
-}
-
 struct NormArgs {
   int rows, hidden;
   Extent x;
@@ -112,7 +106,8 @@ struct NormArgs {
 // rows are on their way while R others are worked on.  Bound by memory and instructions:
 // 16384 x 2048 bf16 layer norm 26 us, by itself 23 (a copy of as many bytes 23); with 8
 // elements a thread 30, a row's sums costing as much as its elements.  bf16 rows of 4001,
-// 32768 of them: alike in x and y 98 us, anywhere 182, by element 230.
+// 32768 of them: alike in x and y 98 us, anywhere 133 (written through
+// shared memory as whole windows 182, by element 230).
 constexpr int kNormThreads = 256;
 template <int TPR>
 constexpr int kNormBlock = TPR > kNormThreads ? TPR : kNormThreads;
@@ -122,16 +117,14 @@ constexpr int kNormRows = kAny ? 1 : N * (int)sizeof(T) >= 64 ? 1 : 64 / (N * (i
 template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     norm_kernel(const T *__restrict__ x, NormArgs a, T *__restrict__ y) {
-  constexpr bool kAny = kForm == kAnywhere, kSame = kForm == kAlike;
+  constexpr bool kAny = kForm == kAnywhere, kSame = kForm != kAligned;
   constexpr int R = kNormRows<T, kAny, N>, P = N / V, W = TPR / 32, kGroups = kNormBlock<TPR> / TPR;
   constexpr bool kHeld = N <= 16;
   using Part = RowPart<T, V, N>;
   __shared__ float2 buf[TPR > 32 ? 2 * R * kNormBlock<TPR> / 32 : 1];
-  constexpr int kStaged = staged_elements<T>(TPR * N);
-  __shared__ __align__(16) unsigned char rows_out[kAny ? kGroups * R * kStaged * sizeof(T) : 16];
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv = 1.0f / (float)a.hidden;
-  const RowsOf<kSame> rows(a.rows, a.hidden, x, a.stride, (int)sizeof(T), t);
+  const RowsOf<kSame> rows(a.rows, a.hidden, y, a.y_stride, (int)sizeof(T), t);
   // columns of this warp, and of the warp whose sums this lane joins
   auto columns = [&](int warp) {
     int n = 0;
@@ -163,7 +156,7 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     for (int i = 0; i < R; ++i) {
       const T *row = x + (r0 + i < rows.units ? rows.row(r0 + i) : 0) * a.stride;
       const int width = r0 + i < rows.units ? rows.body : 0;
-      if constexpr (kAny) p[i].load(row, t, TPR, width, a.x);
+      if constexpr (kAny) p[i].load(row + rows.head, t, TPR, width, a.x);
       else p[i].load(row + rows.head, t, TPR, width);
       if (kSame && t < 32) own_next[i] = read_own(row, rows.own);
     }
@@ -171,7 +164,7 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
   auto arrive = [&](Part (&p)[R], const Coming (&next)[R]) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      if constexpr (kAny) p[i].take(next[i], t, TPR, a.hidden);
+      if constexpr (kAny) p[i].take(next[i], t, TPR, rows.body);
       else p[i] = next[i];
       if constexpr (kSame) own[i] = own_next[i];
     }
@@ -179,7 +172,6 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
   const int64_t step = (int64_t)rows.ctas * kGroups * R;
   int64_t r0 = ((int64_t)rows.cta * kGroups + group) * R;
   int turn = 0;
-  T *staged = reinterpret_cast<T *>(rows_out) + (kAny ? group * R * kStaged : 0);
   Part p[R];
   Coming next[R];
   if (r0 < rows.units) {
@@ -274,18 +266,9 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
         if constexpr (kHeld) p[i].set2(e, fma2(mul2(v, f), g[e / 2], o[e / 2]));
         else p[i].set2(e, fma2(mul2(v, f), stored[e / 2 * TPR], stored[(N / 2 + e / 2) * TPR]));
       }
-      if constexpr (kAny) p[i].stage(staged + i * kStaged, t, TPR, a.hidden);
-      else p[i].store(y + r * a.y_stride + rows.head, t, TPR, rows.body);
+      p[i].store(y + r * a.y_stride + rows.head, t, TPR, rows.body);
       if (kSame && t < 32)
         write_own(y + r * a.y_stride, rows.own, fmaf((own_value(own[i]) - (kLayer ? mu[i] : 0.0f)) * rs, own_g, own_o));
-    }
-    if constexpr (kAny) {
-      group_barrier<TPR>(group);
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-        if (r0 + i < a.rows) store_any(staged + i * kStaged, y + (r0 + i) * a.y_stride, t, TPR, a.hidden);
-      // (the next rows are staged behind the barrier of their sums, or a warp's own)
-      if constexpr (TPR == 32) __syncwarp();
     }
     arrive(p, next);
   }
@@ -306,7 +289,7 @@ struct GradArgs {
 // CTAs as groups cost 4 us at 32768 x 1000.  Bound by memory and a row's barrier: 16384 x 2048
 // bf16 RMS norm 36 us, 5.5 TB/s (a copy of as many bytes 5.8).  A ring of asynchronous copies
 // in place of the next row in registers took 133 us for 6000 x 7168 fp32, this 96.  bf16
-// rows of 4001, 32768 of them: alike in all tensors 162, anywhere 283.
+// rows of 4001, 32768 of them: alike in all tensors 162, anywhere 258.
 template <int TPR>
 constexpr int kBlock = TPR == 32 ? 256 : 512;
 // Rows of a group at once; the next ones come into registers meanwhile where these
@@ -316,21 +299,21 @@ constexpr int kBatch = N * (int)sizeof(T) >= 32 ? 1 : 32 / (N * (int)sizeof(T));
 // What of a thread does not stay in registers: the next row where it would take 64 of them
 // (windows take twice as many on their way); the columns' sums where these, the rows and
 // the next ones take 96 and more (aligned rows alone have room for 96); the weights of 24 columns
-// and more (and 16 where the rows' ends are held besides).  Sums and weights are then in shared
-// memory.
+// and more (of fewer where the rows' ends are held besides: with windows, or 16 of layer norm).
+// Sums and weights are then in shared memory.
 template <typename T, Form kForm, int N>
 constexpr bool kAhead = N * (int)sizeof(T) <= (kForm == kAnywhere ? 48 : 96);
 template <typename T, Form kForm, int N, bool kLayer>
 constexpr bool kSumsShared = (kLayer ? 2 : 1) * N + N * (int)sizeof(T) / 2 *
                              (1 + (kAhead<T, kForm, N> ? kForm == kAnywhere ? 2 : 1 : 0)) > (kForm == kAligned ? 96 : 95);
 template <Form kForm, int N, bool kLayer>
-constexpr bool kWeightsShared = N >= 24 || (kForm == kAlike && kLayer && N == 16);
+constexpr bool kWeightsShared = N >= 24 || kForm == kAnywhere || (kForm == kAlike && kLayer && N == 16);
 
 template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     norm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ x, GradArgs a,
                      T *__restrict__ dx) {
-  constexpr bool kAny = kForm == kAnywhere, kSame = kForm == kAlike;
+  constexpr bool kAny = kForm == kAnywhere, kSame = kForm != kAligned;
   constexpr int R = kBatch<T, N>, K = kLayer ? 2 * R : R;
   constexpr int kGroups = kBlock<TPR> / TPR;
   constexpr bool kStored = kWeightsShared<kForm, N, kLayer>, kShared = kSumsShared<T, kForm, N, kLayer>;
@@ -346,15 +329,12 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     float mu[R], rs[R];
   };
   __shared__ float buf[kGroups][2 * K * (TPR / 32)];
-  constexpr int kStaged = staged_elements<T>(TPR * N);
-  __shared__ __align__(16) unsigned char rows_out[kAny ? kGroups * R * kStaged * sizeof(T) : 16];
   // kShared: dg [N][TPR], db [N][TPR]; groups of a warp: one group's sums; kStored: weights [N][TPR]
   extern __shared__ __align__(16) float held[];
   int turn = 0;
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float inv = 1.0f / (float)a.hidden;
-  T *staged = reinterpret_cast<T *>(rows_out) + (kAny ? group * R * kStaged : 0);
-  const RowsOf<kSame> rows(a.rows, a.hidden, x, a.stride, (int)sizeof(T), t);
+  const RowsOf<kSame> rows(a.rows, a.hidden, dx, a.dx_stride, (int)sizeof(T), t);
   auto read_weight = [&](int e) {
     const int c = Part::column(e, t, TPR), c1 = Part::column(e + 1, t, TPR);
     return f2(c < rows.body ? __ldg(a.weight + rows.head + c) : 0.0f,
@@ -389,8 +369,8 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
       const bool in = r0 + i < rows.units;
       const int64_t r = in ? rows.row(r0 + i) : 0;
       if constexpr (kAny) {
-        b.d[i].load(dy + r * a.dy_stride, t, TPR, in ? a.hidden : 0, a.dy);
-        b.x[i].load(x + r * a.stride, t, TPR, in ? a.hidden : 0, a.x);
+        b.d[i].load(dy + r * a.dy_stride + rows.head, t, TPR, in ? rows.body : 0, a.dy);
+        b.x[i].load(x + r * a.stride + rows.head, t, TPR, in ? rows.body : 0, a.x);
       } else {
         b.d[i].load(dy + r * a.dy_stride + rows.head, t, TPR, in ? rows.body : 0);
         b.x[i].load(x + r * a.stride + rows.head, t, TPR, in ? rows.body : 0);
@@ -409,8 +389,8 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if constexpr (kAny) {
-        now.d[i].take(next.d[i], t, TPR, a.hidden);
-        now.x[i].take(next.x[i], t, TPR, a.hidden);
+        now.d[i].take(next.d[i], t, TPR, rows.body);
+        now.x[i].take(next.x[i], t, TPR, rows.body);
       } else {
         now.d[i] = next.d[i];
         now.x[i] = next.x[i];
@@ -478,20 +458,11 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
         ge = kLayer ? fma2(ge, v, m0) : mul2(ge, v);
         now.x[i].set2(e, fma2(n, m, ge));
       }
-      if constexpr (kAny) now.x[i].stage(staged + i * kStaged, t, TPR, a.hidden);
-      else now.x[i].store(dx + rows.row(r0 + i) * a.dx_stride + rows.head, t, TPR, rows.body);
+      now.x[i].store(dx + rows.row(r0 + i) * a.dx_stride + rows.head, t, TPR, rows.body);
       if (kSame && t < 32) {
         const float n = (own_x(own[i]) - now.mu[i]) * rs, k = -rs * (s[i] * inv), k0 = kLayer ? -rs * (s[R + i] * inv) : 0.0f;
         write_own(dx + rows.row(r0 + i) * a.dx_stride, rows.own, fmaf(n, k, fmaf(own_dy(own[i]) * own_g, rs, k0)));
       }
-    }
-    if constexpr (kAny) {
-      group_barrier<TPR>(group);
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-        if (r0 + i < a.rows)
-          store_any(staged + i * kStaged, dx + (int64_t)(r0 + i) * a.dx_stride, t, TPR, a.hidden);
-      if constexpr (TPR == 32) __syncwarp();
     }
     if constexpr (kNext) arrive();
   }
@@ -582,7 +553,7 @@ cudaError_t norm_rows(const T *x, const NormArgs &a, T *y, cudaStream_t stream) 
   constexpr int kGroups = kNormBlock<TPR> / TPR;
   const int most = kSms * (512 / kNormBlock<TPR>), least = a.rows < kClasses ? a.rows : kClasses;
   int ctas = (a.rows + kGroups - 1) / kGroups;
-  ctas = kForm == kAlike && ctas < least ? least : ctas < most ? ctas : most;
+  ctas = kForm != kAligned && ctas < least ? least : ctas < most ? ctas : most;
   constexpr int kStored = N > 16 ? 2 * N * TPR * 4 : 0;
   auto kernel = norm_kernel<T, V, kForm, TPR, N, kLayer>;
   if (kStored) {

@@ -61,8 +61,7 @@ inline int row_vector(int element_bytes, int hidden, int n, const void *const *b
 }
 
 // Whether rows may be read and written 16 bytes at a time as they lie: all start on
-// 16-byte boundaries and are multiples of them long.  Else their kernels move windows
-// and shift (RowPart::load_any, store_any).
+// 16-byte boundaries and are multiples of them long.
 inline bool rows_aligned(int element_bytes, int hidden, int n, const void *const *base,
                          const int64_t *stride) {
   const int v = 16 / element_bytes;
@@ -205,29 +204,6 @@ __device__ __forceinline__ uint4 shift_windows(uint4 a, uint4 b, int by) {
                     __byte_perm(z[3], z[4], sel));
 }
 
-// Rows staged in shared memory for store_any: element 0 behind a window, another
-// window behind the last.
-template <typename T>
-__host__ __device__ constexpr int staged_elements(int n) {
-  return n + 2 * 16 / (int)sizeof(T);
-}
-// Writes elements [0, width) of a staged row to `row`, which starts anywhere: whole
-// windows of it, read from the staged row shifted, the two at its ends by element.  By
-// `threads` threads, after a barrier.
-template <typename T>
-__device__ __forceinline__ void store_any(const T *staged, T *row, int t, int threads, int width) {
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(row), hi = lo + (uintptr_t)width * sizeof(T);
-  const int mis = (int)(lo & 15);
-  const uint4 *from = reinterpret_cast<const uint4 *>(staged);
-  for (uintptr_t w = lo - mis + 16 * (uintptr_t)t; w < hi; w += 16 * (uintptr_t)threads) {
-    const int k = (int)((w - (lo - mis)) >> 4);
-    // byte 0 of window k is byte 16 + 16 k - mis of the staged row
-    const uint4 v = mis ? shift_windows(from[k], from[k + 1], 16 - mis) : from[k + 1];
-    if (w >= lo && w + 16 <= hi) *reinterpret_cast<uint4 *>(w) = v;
-    else write_edge<T>(v, w, lo, hi);
-  }
-}
-
 // The two windows of each of a thread's accesses to a row, and where its elements
 // begin in the first.
 template <typename T, int N>
@@ -305,7 +281,7 @@ struct RowPart {
     }
   }
   // The same of a row that starts anywhere and of any width (V: 16 bytes): its windows
-  // on their way (load_windows), then shifted into place.
+  // on their way (Windows), then shifted into place.
   __device__ __forceinline__ void take(const Windows<T, N> &x, int t, int threads, int width) {
     static_assert(V * sizeof(T) == 16, "windows");
 #pragma unroll
@@ -320,22 +296,6 @@ struct RowPart {
         for (int k = 0; k < 4; ++k) {
           if (4 * k >= bytes) o[k] = 0u;
           else if (4 * k + 2 >= bytes) o[k] &= 0xFFFFu;
-        }
-      }
-    }
-  }
-  // Into a staged row (store_any).
-  __device__ __forceinline__ void stage(T *staged, int t, int threads, int width) const {
-#pragma unroll
-    for (int p = 0; p < N / V; ++p) {
-      const int c = (p * threads + t) * V;
-      if (c < width) {
-        constexpr int B = V * (int)sizeof(T);
-        static_assert(B % 16 == 0, "windows");
-#pragma unroll
-        for (int q = 0; q < B / 16; ++q) {
-          const uint32_t *o = w + (B / 4) * p + 4 * q;
-          reinterpret_cast<uint4 *>(staged + 16 / sizeof(T) + c)[q] = make_uint4(o[0], o[1], o[2], o[3]);
         }
       }
     }
