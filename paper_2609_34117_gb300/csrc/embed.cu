@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kSumThreads)
 // A run that crosses pieces: the group of the piece where it begins adds the
 // pieces' sums in order.
 template <typename O, int V, int TPR>
-__global__ void __launch_bounds__(kSumThreads, 1) embed_join_kernel(SumArgs a, O *out) {
+__global__ void __launch_bounds__(kSumThreads, 3) embed_join_kernel(SumArgs a, O *out) {
   const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
   if ((int)blockIdx.x < a.zero.ctas) {
     pdl_launch_dependents();
@@ -401,29 +401,36 @@ __global__ void __launch_bounds__(kSumThreads, 1) embed_join_kernel(SumArgs a, O
   pdl_wait_primary();
   pdl_launch_dependents();
   if ((int64_t)(piece + 1) * a.piece >= a.n) return;
+  // (the keys around the piece and where the next 32 begin at once: their latency, with the
+  // sums', is what a join of two pieces takes)
   const int s = piece * a.piece, end = s + a.piece;
-  const uint32_t run = __ldcg(&a.items[end - 1].x);
-  if (run >= (uint32_t)a.vocab || __ldcg(&a.items[end].x) != run) return;
-  const bool whole = __ldcg(&a.items[s].x) == run;
-  if (whole && s > 0 && __ldcg(&a.items[s - 1].x) == run) return;  // begins before
+  const int64_t starts = (int64_t)(piece + 1 + lane) * a.piece;
+  const uint32_t run = __ldcg(&a.items[end - 1].x), first = __ldcg(&a.items[s].x);
+  const uint32_t before = s > 0 ? __ldcg(&a.items[s - 1].x) : ~0u;
+  uint32_t in = __ballot_sync(0xFFFFFFFFu, starts < a.n && __ldcg(&a.items[starts < a.n ? starts : s].x) == run);
+  if (run >= (uint32_t)a.vocab || (in & 1u) == 0) return;
+  const bool whole = first == run;
+  if (whole && before == run) return;  // begins before
   // pieces that it reaches: those whose first position still is the run's
   int last = piece;
-  for (bool more = true; more;) {
-    const int64_t at = (int64_t)(last + 1 + lane) * a.piece;
-    const uint32_t in = __ballot_sync(0xFFFFFFFFu, at < a.n && __ldcg(&a.items[at].x) == run);
+  for (;;) {
     const int n = in == 0xFFFFFFFFu ? 32 : __ffs(~in) - 1;
     last += n;
-    more = n == 32;
+    if (n < 32) break;
+    const int64_t at = (int64_t)(last + 1 + lane) * a.piece;
+    in = __ballot_sync(0xFFFFFFFFu, at < a.n && __ldcg(&a.items[at].x) == run);
   }
   float acc[8];
   RowPart<float, V, 8> p;
   p.template load<true>(a.partial + ((int64_t)piece * 2 + (whole ? 0 : 1)) * a.hidden + c0, t, TPR, width);
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = p.get(e);
-  // what it takes is the loads' latency: many at a time and without conditions (columns
+  // what it takes is the loads' latency: several at a time, with room for three CTAs on an SM
+  // (28042 ids of 8232 tokens, 1088 fp32: all of the gradient 59 us; 12 at a time and two CTAs
+  // 68, but 32768 times the same token, 1024 bf16, 100 in place of 123), without conditions (columns
   // past the row's end read its last ones and are not stored; rows past the last
   // piece read that one and are not added)
-  constexpr int kLoads = 12;
+  constexpr int kLoads = 6;
   const float *row = a.partial + c0;
   for (int k = piece + 1; k <= last; k += kLoads) {
     float q[kLoads][8];
