@@ -146,13 +146,14 @@ __device__ void sort_by_id(const SortArgs &s, SortShared &sh) {
     for (int i = threadIdx.x; i < kSortWarps * kDigits / 4; i += kSortThreads)
       reinterpret_cast<uint4 *>(&sh.count[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
+    uint32_t alike[kHeldItems];  // of the held items: lanes of the same digit
     for (int i0 = lo; i0 < hi; i0 += kBatch) {
       if (i0 > lo) fetch(i0);
 #pragma unroll
       for (int k = 0; k < kHeldItems; ++k) {
         if (i0 + 32 * k >= hi) break;
         const uint32_t d = digit_of(k, i0);
-        const uint32_t same = lanes_with(d);
+        const uint32_t same = alike[k] = lanes_with(d);
         if (d < kDigits && (same & ((1u << lane) - 1)) == 0) sh.count[warp][d] += __popc(same);
         __syncwarp();
       }
@@ -215,7 +216,7 @@ __device__ void sort_by_id(const SortArgs &s, SortShared &sh) {
       for (int k = 0; k < kHeldItems; ++k) {
         if (i0 + 32 * k >= hi) break;
         const uint32_t d = digit_of(k, i0);
-        const uint32_t same = lanes_with(d);
+        const uint32_t same = per > kBatch ? lanes_with(d) : alike[k];
         const uint32_t rank = __popc(same & ((1u << lane) - 1));
         const bool in = d < kDigits;
         const uint32_t place = in ? sh.start[warp / kPart][d] + sh.count[warp][d] + rank : 0u;
