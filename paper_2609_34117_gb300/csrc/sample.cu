@@ -62,7 +62,7 @@ constexpr float kWeightOne = 1099511627776.0f;  // 2^40, the largest element's w
 //        base; of the weights twice (the quotient 1 / T is the same in both)
 //     8  exp2's and exp's own
 //   290  58 changes of a sum's reference, a factor of exp2 and a product: 4 at
-//        refreshes, 48 at cuts of a warp's list (3072 units of it, 64 between two
+//        refreshes, 48 at cuts of a warp's list (3 x 1024 units of it, 64 between two
 //        cuts), 6 in most_of_many() and the join
 //   217  additions of units that are dropped from the list: their factor, and four to
 //        a lane at each refresh and cut and at the row's end
