@@ -504,8 +504,8 @@ cudaError_t sum_rows(const T *grad, const SumArgs &a, O *out, cudaStream_t strea
 }
 
 cudaError_t sort_rows(const SortArgs &s, cudaStream_t stream) {
-  const cudaError_t err = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (int)sizeof(SortShared));
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t err = allow_shared(ready, (const void *)embed_sort_kernel, (int)sizeof(SortShared));
   if (err != cudaSuccess) return err;
   // one CTA while its lanes hold all items
   const int ctas = s.n <= kSortThreads * kHeldItems ? 1 : kSortCtas;

@@ -567,7 +567,8 @@ cudaError_t norm_rows(const T *x, const NormArgs &a, T *y, cudaStream_t stream) 
   constexpr int kStored = N > 16 ? 2 * N * TPR * 4 : 0;
   auto kernel = norm_kernel<T, V, kForm, TPR, N, kLayer>;
   if (kStored) {
-    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStored);
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t err = allow_shared(ready, (const void *)kernel, kStored);
     if (err != cudaSuccess) return err;
   }
   kernel<<<ctas, kNormBlock<TPR>, kStored, stream>>>(x, a, y);
@@ -582,8 +583,8 @@ cudaError_t grad_rows(const T *dy, const T *x, const GradArgs &a, T *dx, float *
   constexpr size_t smem = (size_t)((kHeld ? kLayer ? 2 : 1 : 0) + (kWeightsShared<kForm, N, kLayer> ? 1 : 0)) * N * TPR * 4;
   auto kernel = norm_grad_kernel<T, V, kForm, TPR, N, kLayer>;
   if (N >= 16 && smem) {  // (with the static arrays it may be above 48 KB)
-    const cudaError_t err =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t err = allow_shared(ready, (const void *)kernel, (int)smem);
     if (err != cudaSuccess) return err;
   }
   kernel<<<ctas, kBlock<TPR>, smem, stream>>>(dy, x, a, dx);

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace slimwise {
@@ -41,6 +43,19 @@ inline cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, s
   cfg.attrs = attr;
   cfg.numAttrs = (unsigned)n;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
+// Lets `kernel` have `bytes` of dynamic shared memory on the current device, once for each
+// device that `devices` has no bit of yet.
+inline cudaError_t allow_shared(std::atomic<uint64_t> &devices, const void *kernel, int bytes) {
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (devices.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (err == cudaSuccess) devices.fetch_or(bit, std::memory_order_release);
+  return err;
 }
 
 // Elements that one access of rows may take: 16 bytes of them where every row
