@@ -292,10 +292,11 @@ struct GradArgs {
 // rows of 4001, 32768 of them: alike in all tensors 162, anywhere 258.
 template <int TPR>
 constexpr int kBlock = TPR == 32 ? 256 : 512;
-// Rows of a group at once; the next ones come into registers meanwhile where these
-// hold both.
-template <typename T, int N>
-constexpr int kBatch = N * (int)sizeof(T) >= 32 ? 1 : 32 / (N * (int)sizeof(T));
+// Rows of a group at once; the next ones come into registers meanwhile where these hold
+// both.  Of 8 elements a thread three bf16 rows where they are aligned (16384 x 2048 41.0 -> 37.9
+// us, four spill), else two (fp32 8192 x 4096 82 -> 71); of more, one.
+template <typename T, Form kForm, int N>
+constexpr int kBatch = N != 8 ? 1 : sizeof(T) == 2 && kForm == kAligned ? 3 : 2;
 // What of a thread does not stay in registers: the next row where it would take 64 of them
 // (windows take twice as many on their way); the columns' sums where these, the rows and
 // the next ones take 96 and more (aligned rows alone have room for 96); the weights of 24 columns
@@ -314,7 +315,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, 512 / kBlock<TPR>)
     norm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ x, GradArgs a,
                      T *__restrict__ dx) {
   constexpr bool kAny = kForm == kAnywhere, kSame = kForm != kAligned;
-  constexpr int R = kBatch<T, N>, K = kLayer ? 2 * R : R;
+  constexpr int R = kBatch<T, kForm, N>, K = kLayer ? 2 * R : R;
   constexpr int kGroups = kBlock<TPR> / TPR;
   constexpr bool kStored = kWeightsShared<kForm, N, kLayer>, kShared = kSumsShared<T, kForm, N, kLayer>;
   constexpr bool kNext = kAhead<T, kForm, N>;
