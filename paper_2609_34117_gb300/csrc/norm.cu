@@ -111,14 +111,15 @@ struct NormArgs {
 constexpr int kNormThreads = 256;
 template <int TPR>
 constexpr int kNormBlock = TPR > kNormThreads ? TPR : kNormThreads;
-template <typename T, bool kAny, int N>
-constexpr int kNormRows = kAny ? 1 : N * (int)sizeof(T) >= 64 ? 1 : 64 / (N * (int)sizeof(T)) > 2 ? 2 : 64 / (N * (int)sizeof(T));
+// (two fp32 rows of 16 in place of one: 8192 x 8192 92 -> 90 us, 32768 x 1000 49 -> 47)
+template <bool kAny, int N>
+constexpr int kNormRows = !kAny && N <= 16 ? 2 : 1;
 
 template <typename T, int V, Form kForm, int TPR, int N, bool kLayer>
 __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     norm_kernel(const T *__restrict__ x, NormArgs a, T *__restrict__ y) {
   constexpr bool kAny = kForm == kAnywhere, kSame = kForm != kAligned;
-  constexpr int R = kNormRows<T, kAny, N>, P = N / V, W = TPR / 32, kGroups = kNormBlock<TPR> / TPR;
+  constexpr int R = kNormRows<kAny, N>, P = N / V, W = TPR / 32, kGroups = kNormBlock<TPR> / TPR;
   constexpr bool kHeld = N <= 16;
   using Part = RowPart<T, V, N>;
   __shared__ float2 buf[TPR > 32 ? 2 * R * kNormBlock<TPR> / 32 : 1];
@@ -287,7 +288,7 @@ struct GradArgs {
 // and 16384 (512, 32); fp32 with more threads between, and 10 and 12 elements.  512 threads
 // are on an SM, several groups to a CTA, whose sums are joined before they leave: as many
 // CTAs as groups cost 4 us at 32768 x 1000.  Bound by memory and a row's barrier: 16384 x 2048
-// bf16 RMS norm 36 us, 5.5 TB/s (a copy of as many bytes 5.8).  A ring of asynchronous copies
+// bf16 RMS norm 33 us by itself, 6.1 TB/s.  A ring of asynchronous copies
 // in place of the next row in registers took 133 us for 6000 x 7168 fp32, this 96.  bf16
 // rows of 4001, 32768 of them: alike in all tensors 162, anywhere 258.
 template <int TPR>
