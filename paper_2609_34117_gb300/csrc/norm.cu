@@ -200,7 +200,8 @@ __global__ void __launch_bounds__(kNormBlock<TPR>, 512 / kNormBlock<TPR>)
     for (int i = 0; i < R; ++i) {
       const F2 m = f2(-mu[i] * warp_inv);
       F2 s = f2(0.0f);
-      const bool full = a.hidden == TPR * N;
+      // (not the row's width: of rows that start anywhere the ends are no columns of the threads)
+      const bool full = rows.body == TPR * N;
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
         F2 d = p[i].get2(e);
