@@ -1072,6 +1072,8 @@ __global__ void __launch_bounds__(kSumThreads, 2) sums_kernel(Call c, int chunk,
       S *= ex2((mine_most - ref) * kLog2e);
     }
     S = warp_sum(S);
+    // an infinite logit of the label: all other exponentials are 0, where the formula has no number
+    if (z == INFINITY) S = __int_as_float(0x7FC00000);
     const float own = ref == z ? 1.0f : ex2((z - ref) * kLog2e);
     float scale = 0.0f;
     if (live) {

@@ -1,9 +1,12 @@
-"""Edges of the operators around the layer: where variants meet alignment."""
+"""Edges of the operators around the layer: where variants meet alignment, and infinite
+logits."""
+import math
+
 import pytest
 import torch
 
 import paper_2609_34117_gb300 as sw
-from tests.test_gpu_train_ops import BF16, _check_norm, _grad_reference, _half, _randn, _rows, _within
+from tests.test_gpu_train_ops import BF16, DEV, _check_norm, _grad_reference, _half, _head, _randn, _rows, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +43,49 @@ def test_norm_of_whole_widths_into_rows_that_start_anywhere(hidden, alike, layer
         want, _, _, tol, _, _ = _grad_reference(dy, x, w, mean, rstd)
         _within(got, want, want.abs() * _half(BF16) + tol * 1.01 + torch.finfo(BF16).tiny)
         assert int(torch.isnan(around).sum()) == outside and int(torch.isnan(beside).sum()) == outside
+
+
+# ---------------------------------------------------------------------------
+# the head's cross entropy: infinite logits
+# ---------------------------------------------------------------------------
+# rows few enough for tiles of them (vocabulary and rows in changed roles), in tiles of 256,
+# and of several tiles
+SIZES = [(40, 64, 700), (300, 64, 700), (300, 520, 2049), (700, 136, 1000)]
+PARTS = [(True, True), (True, False), (False, True), (False, False)]
+HUGE = 2.0 ** 127  # its square is past every type's range
+
+
+def _infinite(rows, width, vocab, infinite):
+    """A head whose logits of column V0 are what `infinite` says in rows with a huge (or 1)
+    first element, and whose others do not see that element."""
+    hidden, weight, labels, wt = _head(rows, width, vocab, seed=rows + width, ignored=0.0)
+    labels = torch.where(labels == 11, 12, labels).int()
+    weight[:, 0], hidden[:, 0] = 0.0, 0.0
+    weight[11, 0] = infinite
+    return hidden, weight, labels, wt
+
+
+@pytest.mark.parametrize("at_label", [True])
+@pytest.mark.parametrize("infinite", [HUGE, math.inf])
+@pytest.mark.parametrize("rows,width,vocab", SIZES)
+def test_linear_loss_of_a_logit_of_plus_infinity(rows, width, vocab, infinite, at_label):
+    hidden, weight, labels, wt = _infinite(rows, width, vocab, infinite)
+    if math.isinf(infinite):
+        hidden[:, 0] = -1.0  # the others' logits of that word: -inf
+    bad = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    bad[[7, rows - 1]] = True
+    labels[bad] = 11 if at_label else 5
+    usual = labels.clone()
+    usual[bad] = 5
+    clean = sw.slimwise_linear_loss(hidden, weight, usual, wt)
+    assert bool(clean[1].isfinite().all())
+    hidden[bad, 0] = HUGE
+    for dh, dw in PARTS:
+        loss, row, gh, gw = sw.slimwise_linear_loss(hidden, weight, labels, wt, grad_hidden=dh, grad_weight=dw)
+        assert bool(loss.isnan().all()) and torch.equal(row.isnan(), bad)
+        if dh:
+            assert bool(gh[bad].isnan().all()) and torch.equal(gh[~bad, 1:], clean[2][~bad, 1:])
+        if dw:
+            assert bool(gw.isnan().all())
+        if dh or dw:
+            assert torch.equal(row[~bad], clean[1][~bad])
