@@ -1072,8 +1072,9 @@ __global__ void __launch_bounds__(kSumThreads, 2) sums_kernel(Call c, int chunk,
       S *= ex2((mine_most - ref) * kLog2e);
     }
     S = warp_sum(S);
-    // an infinite logit of the label: all other exponentials are 0, where the formula has no number
-    if (z == INFINITY) S = __int_as_float(0x7FC00000);
+    // a logit of +inf: the formula has no number, but the others' exponentials are 0 where it is the
+    // label's, and the sum's inverse is 0 where it is another's
+    if (z == INFINITY || top == INFINITY) S = __int_as_float(0x7FC00000);
     const float own = ref == z ? 1.0f : ex2((z - ref) * kLog2e);
     float scale = 0.0f;
     if (live) {
@@ -1086,7 +1087,7 @@ __global__ void __launch_bounds__(kSumThreads, 2) sums_kernel(Call c, int chunk,
         if (lane == 0) {
           c.scale[at] = scale;
           if (y < c.V) c.cells[(int64_t)row * c.cells_stride + y] = least;
-          if (!again && S > expf(kMostLoss) && top < INFINITY) {
+          if (!again && S > expf(kMostLoss)) {
             c.ref[at] = top;
             const int tiles = c.rows_pad / kTile;
             if (atomicExch(c.flags + tile, 1) == 0)

@@ -65,7 +65,7 @@ def _infinite(rows, width, vocab, infinite):
     return hidden, weight, labels, wt
 
 
-@pytest.mark.parametrize("at_label", [True])
+@pytest.mark.parametrize("at_label", [True, False])
 @pytest.mark.parametrize("infinite", [HUGE, math.inf])
 @pytest.mark.parametrize("rows,width,vocab", SIZES)
 def test_linear_loss_of_a_logit_of_plus_infinity(rows, width, vocab, infinite, at_label):
