@@ -566,7 +566,8 @@ int slimwise_norm_grad(const void *dy, int64_t dy_stride, const void *x, int32_t
  *                hidden; 160 MB for sums of a split product; and, where the rows
  *                come in chunks, 4 for each element of weight
  * A row with a label >= vocab, a NaN or a logit of +inf has NaN loss and gradient,
- * and grad_weight is then NaN where the formula has it.  dz's numerators (which the
+ * and grad_weight is then NaN where the formula has it; a label's logit of -inf has
+ * loss +inf and the formula's gradient (NaN where all logits are -inf).  dz's numerators (which the
  * products take) and the rows scaled by their weights are rounded to bf16.  A device
  * wait that gave up is reported by slimwise_moe_device_status(workspace, ...).
  */

@@ -1087,7 +1087,8 @@ __global__ void __launch_bounds__(kSumThreads, 2) sums_kernel(Call c, int chunk,
         if (lane == 0) {
           c.scale[at] = scale;
           if (y < c.V) c.cells[(int64_t)row * c.cells_stride + y] = least;
-          if (!again && S > expf(kMostLoss)) {
+          // (a label's logit of -inf: S is no number where another one is -inf too, unless all are)
+          if (!again && (S > expf(kMostLoss) || (z == -INFINITY && top > kFloor && top < INFINITY))) {
             c.ref[at] = top;
             const int tiles = c.rows_pad / kTile;
             if (atomicExch(c.flags + tile, 1) == 0)

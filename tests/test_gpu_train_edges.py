@@ -89,3 +89,27 @@ def test_linear_loss_of_a_logit_of_plus_infinity(rows, width, vocab, infinite, a
             assert bool(gw.isnan().all())
         if dh or dw:
             assert torch.equal(row[~bad], clean[1][~bad])
+
+
+@pytest.mark.parametrize("rows,width,vocab", SIZES)
+def test_linear_loss_of_logits_of_minus_infinity(rows, width, vocab):
+    # the label's and another one's: the loss is infinite, the gradient is not.  It is what it is
+    # where both are so low that their exponentials are 0.
+    hidden, weight, labels, wt = _infinite(rows, width, vocab, -HUGE)
+    weight[13, 0] = -HUGE
+    low = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    low[[0, 9, rows - 2]] = True
+    labels[low] = 11
+    labels[9] = 5  # not at the label
+    finite_w, finite_h = weight.clone(), hidden.clone()
+    finite_w[:, 0] /= HUGE / 16
+    finite_h[low, 0], hidden[low, 0] = 16.0, HUGE
+    impossible = low & (labels == 11)
+    for dh, dw in PARTS:
+        want = sw.slimwise_linear_loss(finite_h, finite_w, labels, wt, grad_hidden=dh, grad_weight=dw)
+        _, row, gh, gw = sw.slimwise_linear_loss(hidden, weight, labels, wt, grad_hidden=dh, grad_weight=dw)
+        assert bool((row[impossible] == math.inf).all()) and torch.equal(row[~impossible], want[1][~impossible])
+        if dh:
+            assert torch.equal(gh[:, 1:], want[2][:, 1:])
+        if dw:
+            assert torch.equal(gw[:, 1:], want[3][:, 1:])
