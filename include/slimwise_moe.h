@@ -567,9 +567,10 @@ int slimwise_norm_grad(const void *dy, int64_t dy_stride, const void *x, int32_t
  *                come in chunks, 4 for each element of weight
  * A row with a label >= vocab, a NaN or a logit of +inf has NaN loss and gradient,
  * and grad_weight is then NaN where the formula has it; a label's logit of -inf has
- * loss +inf and the formula's gradient (NaN where all logits are -inf).  dz's numerators (which the
- * products take) and the rows scaled by their weights are rounded to bf16.  A device
- * wait that gave up is reported by slimwise_moe_device_status(workspace, ...).
+ * loss +inf and the formula's gradient (NaN where all logits are -inf).  dz's
+ * numerators (which the products take) and the rows scaled by their weights are
+ * rounded to bf16.  A device wait that gave up is reported by
+ * slimwise_moe_device_status(workspace, ...).
  */
 int slimwise_linear_loss_workspace_size(int32_t rows, int32_t width, int32_t vocab,
                                         int32_t grad_hidden, int32_t grad_weight, size_t *bytes);

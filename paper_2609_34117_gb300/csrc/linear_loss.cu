@@ -44,11 +44,14 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMostLoss = 60.0f;
-// The tensor cores' fp32 sums are cut, not rounded, at each step of the contraction: a
-// logit is too small in magnitude by 1.03e-9 of itself for each element of the width
-// where it grows steadily, 0.9e-9 where it wanders (widths of 512 to 4096 alike), while
-// the label's, of plain sums, is not.  The expected loss is given back: a row's lse at
-// 4096 was 3.4e-6 of itself too small.
+// The tensor cores' fp32 sums are cut, not rounded, at each step of the contraction that
+// adds something: a logit of a dense row is too small in magnitude by 1.03e-9 of itself
+// for each element of the width where it grows steadily, 0.9e-9 where it wanders (widths of
+// 512 to 16384 alike), while the label's, of plain sums, is not.  The expected loss is given
+// back, by the pieces of 8 elements of the row that are not all zeros: mean error of 300 row
+// losses (10 to 16) at 8192 3e-7 in place of -1.1e-5, of 200 at 16384 under 1e-7 in place
+// of -2.1e-5.  It is an expectation: a sum that happens to be exact gets its share all the same,
+// 1e-9 of the logit for each element.
 constexpr float kTruncated = 1.0e-9f;
 constexpr int64_t kMostCells = 1ll << 30;
 constexpr int kTile = 256;       // rows and columns of a pair's tile
@@ -60,10 +63,13 @@ constexpr int kStages = 6;
 // N.  For few rows, of which a tile of 256 would be mostly empty and whose epilogue
 // only the warps of their lanes could do: 9 rows of 114316 words at 168 36 -> 24 us, and
 // for some hundred rows that tiles of 256 fit badly.
-constexpr int kSwapRows = 1024, kSwapAlways = 128, kSwapWidth = 512, kSwapStages = 8;
-constexpr int kRowData = kSwapRows * 8;  // the rows' references and labels, at the ring's end
+constexpr int kSwapRows = 896, kSwapAlways = 128, kSwapWidth = 512, kSwapStages = 8;
+// the rows' references, factors and labels, at the ring's end
+constexpr int kRowData = kSwapRows * 12;
 constexpr int kOperandBytes = kHalf * kDepth * 2;
 constexpr int kStageBytes = 2 * kOperandBytes;
+// (with room for the rows' data behind as many stages: 7 for tiles of 160 rows)
+constexpr int kRingBytes = kStages * kStageBytes + 1024;
 // A warp's 32 rows x 64 columns of bf16 on their way out by TMA (128-byte swizzle).
 constexpr int kOutBytes = 32 * 128;
 constexpr int kEpiWarps = 8, kGemmThreads = 64 + 32 * kEpiWarps;
@@ -82,7 +88,7 @@ struct Layout {
   int rows_pad, chunk, chunks, vocab_tiles, hidden_tiles, split_tiles;
   int rows_tile;  // swapped_rows()
   int64_t cells_stride;
-  size_t ctrl, counts, orig, label, target, ref, scale, flags, rows, scaled, sums, cells, splits, acc, total;
+  size_t ctrl, counts, orig, label, target, ref, unbias, scale, flags, rows, scaled, sums, cells, splits, acc, total;
 };
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
@@ -141,6 +147,7 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
   l.label = take(n * 4);
   l.target = take(n * 4);
   l.ref = take(n * 4);
+  l.unbias = take(n * 4);
   l.scale = take(n * 4);
   l.flags = take(n / kTile * 3 * 4);
   l.rows = take(n * hidden * 2);
@@ -156,7 +163,6 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
 // Device view of the workspace and the call.
 struct Call {
   int T, H, V;
-  float unbias;  // of a logit: 1 + H kTruncated
   int rows_pad, chunk, vocab_tiles, hidden_tiles;
   int rows_tile;  // of the first product and dh's
   int64_t cells_stride;
@@ -164,6 +170,7 @@ struct Call {
   int32_t *counts;  // labelled rows of each 1024 (more than kCountedRows rows)
   int32_t *flags;  // [3][rows_pad / 256]: tiles to run again; their list; each chunk's number of them
   float *target, *ref, *scale;
+  float *unbias;  // of a row's logits: 1 + kTruncated for each element that is added
   __nv_bfloat16 *rows, *scaled, *cells;
   float2 *sums;   // [2 vocab_tiles][chunk]: sum of numerators, largest logit
   float *splits;  // [tiles][256][256]
@@ -254,10 +261,12 @@ __global__ void __launch_bounds__(kGatherThreads, 2) gather_kernel(Call c, int c
     const uint4 *head = reinterpret_cast<const uint4 *>(c.weight + (int64_t)(known ? y : 0) * c.weight_stride);
     uint4 *to = reinterpret_cast<uint4 *>(c.rows + (int64_t)at * c.H);
     float s = 0.0f;
+    int added = 0;  // pieces that are not all zeros
 #pragma unroll 4
     for (int k = lane; k < words; k += 32) {
       const uint4 a = __ldg(row + k), b = __ldg(head + k);
       to[k] = a;
+      added += ((a.x | a.y | a.z | a.w) & 0x7FFF7FFFu) != 0u ? 1 : 0;
       const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -266,8 +275,10 @@ __global__ void __launch_bounds__(kGatherThreads, 2) gather_kernel(Call c, int c
       }
     }
     s = warp_sum(s);
+    added = __reduce_add_sync(0xFFFFFFFFu, added);
     if (!known) s = __int_as_float(0x7FC00000);  // a label outside the vocabulary: NaN
     if (lane == 0) {
+      c.unbias[at] = 1.0f + (float)(8 * added) * kTruncated;
       c.orig[at] = t;
       c.label[at] = y;
       c.target[at] = c.ref[at] = s;
@@ -390,7 +401,7 @@ struct Work {
   }
 };
 
-constexpr size_t kBars = (size_t)kStages * kStageBytes + kEpiWarps * kOutBytes;
+constexpr size_t kBars = (size_t)kRingBytes + kEpiWarps * kOutBytes;
 // barriers, words, alignment
 constexpr int kWords = 8 * (2 * kSwapStages + 5);
 constexpr size_t kGemmSmem = kBars + kWords + 64 + 1024;
@@ -456,20 +467,22 @@ __device__ __forceinline__ float reduce_across(float (&x)[32], int lane, F op) {
   return x[0];
 }
 
-// Swapped roles: 32 rows' logits z at the lane's word.  Leaves their numerators in bf16 at
+// Swapped roles: 32 rows' logits z at the lane's word; ref: the rows' references and
+// factors.  Leaves their numerators in bf16 at
 // `staged` (64 bytes a row, zeros for rows past `live`), and returns to lane j row j's
 // sum over the warp's words and largest logit.
 template <Mode kMode>
-__device__ __forceinline__ float2 swapped_numerators(float (&z)[32], float unbias, const float *ref, const int *label, int word,
-                                                 bool known, int live, int lane, uint32_t staged) {
+__device__ __forceinline__ float2 swapped_numerators(float (&z)[32], const float2 *ref, const int *label, int word, bool known,
+                                                  int live, int lane, uint32_t staged) {
   float top = kFloor;
 #pragma unroll
   for (int j = 0; j < 32; ++j) {
     const bool in = known && word != label[j];
     const float most = warp_max_redux(in ? z[j] : kFloor);
     if (lane == j) top = most;
-    const float r = kMode == kForward ? most : ref[j];
-    const float e = ex2(fmaf(z[j], unbias, -r) * kLog2e);
+    const float2 of_row = ref[j];
+    const float r = kMode == kForward ? most : of_row.x;
+    const float e = ex2(fmaf(z[j], of_row.y, -r) * kLog2e);
     if constexpr (kMode == kNumerators) {
       const __nv_bfloat16 h = __float2bfloat16_rn(j < live ? e : 0.0f);
       asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged + (uint32_t)(j * 64 + lane * 2)),
@@ -573,7 +586,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
   // N, a stage of the ring, and how many there are
   const int n_rows = kSwapped ? c.rows_tile : kTile;
   const int slot_bytes = kSwapped ? kOperandBytes + n_rows * kDepth : kStageBytes;
-  const int ring = kSwapped ? min(kSwapStages, (kStages * kStageBytes - kRowData) / slot_bytes) : kStages;
+  const int ring = kSwapped ? min(kSwapStages, (kRingBytes - kRowData) / slot_bytes) : kStages;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (ring + s); };
   auto accf_bar = [&](int b) { return bar0 + 8u * (2 * ring + b); };
@@ -585,7 +598,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
   volatile int *consumed = misc + 2;
   volatile int *n_splits = misc + 3;
   double *warp_totals = reinterpret_cast<double *>(misc + 4);  // kGradWeight
-  float *row_ref = reinterpret_cast<float *>(smem + kStages * kStageBytes - kRowData);  // kSwapped
+  float2 *row_ref = reinterpret_cast<float2 *>(smem + kRingBytes - kRowData);  // kSwapped: reference, factor
   int *row_label = reinterpret_cast<int *>(row_ref + kSwapRows);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -647,7 +660,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     work.units = work.mt * work.nt;
     if constexpr (kSwapped) {
       for (int i = threadIdx.x; i < work.mt * n_rows; i += blockDim.x) {
-        row_ref[i] = i < rows ? __ldcg(c.ref + i) : 0.0f;
+        row_ref[i] = i < rows ? make_float2(__ldcg(c.ref + i), __ldcg(c.unbias + i)) : make_float2(0.0f, 1.0f);
         row_label[i] = i < rows ? __ldcg(c.label + i) : -1;
       }
       __syncthreads();
@@ -824,10 +837,10 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     // ------------------------------------------------------------ accumulators
     const int q = warp & 3, half = (warp - 2) >> 2;  // lanes 32 q.., columns 128 half..
     const int in_tile = (int)crank * kHalf + 32 * q + lane;
-    const OutBuffer out = {smem_base + (uint32_t)(kStages * kStageBytes + (warp - 2) * kOutBytes)};
+    const OutBuffer out = {smem_base + (uint32_t)(kRingBytes + (warp - 2) * kOutBytes)};
     // kSwapped: the four warps' sums of a row, [2 tiles in turn][4][256], joined a tile later,
     // behind the barrier at which the warps agree on the next tile's wait
-    float2 *quarters = reinterpret_cast<float2 *>(smem + kStages * kStageBytes + kEpiWarps * kOutBytes / 2);
+    float2 *quarters = reinterpret_cast<float2 *>(smem + kRingBytes + kEpiWarps * kOutBytes / 2);
     constexpr bool kSums = kSwapped && (kMode == kForward || kMode == kNumerators);
     Unit joined = {0, -1, 0, 0};
     auto join_quarters = [&](int parity) {
@@ -871,7 +884,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
         // two halves of the warps take in turn
         const int mine = w.n * kTile + in_tile, row_first = w.m * n_rows;
         const uint32_t lanes = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(b * kTile);
-        const uint32_t staged = smem_base + (uint32_t)(kStages * kStageBytes + (warp - 2) * kOutBytes / 2);
+        const uint32_t staged = smem_base + (uint32_t)(kRingBytes + (warp - 2) * kOutBytes / 2);
 #pragma unroll 1
         for (int t0 = 32 * half; t0 < n_rows; t0 += 64) {
           float z[32];
@@ -886,7 +899,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
               if (j < live) to[j * kTile] = z[j];
           } else {
             quarters[((local & 1) * 4 + q) * kTile + t0 + lane] =
-                swapped_numerators<kMode>(z, c.unbias, row_ref + row_first + t0, row_label + row_first + t0, mine, mine < c.V,
+                swapped_numerators<kMode>(z, row_ref + row_first + t0, row_label + row_first + t0, mine, mine < c.V,
                                           live, lane, staged);
           }
           if constexpr (kMode == kNumerators) {
@@ -926,6 +939,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
         const bool live = row < rows;
         const float ref = live ? __ldcg(c.ref + row0 + row) : 0.0f;
         const int label = live ? __ldcg(c.label + row0 + row) : -1;
+        const float unbias = live ? __ldcg(c.unbias + row0 + row) : 1.0f;
         float sum = 0.0f, most = kFloor;
 #pragma unroll 1
         for (int k = 0; k < kHalf / 32; ++k) {
@@ -935,7 +949,7 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
           tmem_ld_wait();
           if (k == kHalf / 32 - 1) release();
           const int col = col0 + 32 * k;
-          numerators<kMode>(z, c.unbias, ref, label - col, c.V - col, sum, most, packed);
+          numerators<kMode>(z, unbias, ref, label - col, c.V - col, sum, most, packed);
           if constexpr (kMode == kNumerators) {
             // rows past the last one: zeros (they are in the contraction of dW)
             if (!live)
@@ -1226,7 +1240,6 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   char *w = static_cast<char *>(workspace);
   Call c = {};
   c.T = a.rows; c.H = a.width; c.V = a.vocab;
-  c.unbias = 1.0f + (float)c.H * kTruncated;
   c.rows_pad = l.rows_pad; c.chunk = l.chunk;
   c.vocab_tiles = l.vocab_tiles; c.hidden_tiles = l.hidden_tiles;
   c.rows_tile = l.rows_tile ? l.rows_tile : kTile;
@@ -1238,6 +1251,7 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   c.flags = reinterpret_cast<int32_t *>(w + l.flags);
   c.target = reinterpret_cast<float *>(w + l.target);
   c.ref = reinterpret_cast<float *>(w + l.ref);
+  c.unbias = reinterpret_cast<float *>(w + l.unbias);
   c.scale = reinterpret_cast<float *>(w + l.scale);
   c.rows = reinterpret_cast<__nv_bfloat16 *>(w + l.rows);
   c.scaled = a.grad_weight ? reinterpret_cast<__nv_bfloat16 *>(w + l.scaled) : nullptr;

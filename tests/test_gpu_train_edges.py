@@ -1,12 +1,12 @@
-"""Edges of the operators around the layer: where variants meet alignment, and infinite
-logits."""
+"""Edges of the operators around the layer: where variants meet alignment, infinite
+logits, and logits whose sums are exact or dense."""
 import math
 
 import pytest
 import torch
 
 import paper_2609_34117_gb300 as sw
-from tests.test_gpu_train_ops import BF16, DEV, _check_norm, _grad_reference, _half, _head, _randn, _rows, _within
+from tests.test_gpu_train_ops import BF16, DEV, _check_norm, _gen, _grad_reference, _half, _head, _randn, _rows, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +113,64 @@ def test_linear_loss_of_logits_of_minus_infinity(rows, width, vocab):
             assert torch.equal(gh[:, 1:], want[2][:, 1:])
         if dw:
             assert torch.equal(gw[:, 1:], want[3][:, 1:])
+
+
+# ---------------------------------------------------------------------------
+# the head's cross entropy: what the tensor cores cut off a logit
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("grad", [True, False])
+@pytest.mark.parametrize("kind", ["one element", "sums that cancel"])
+@pytest.mark.parametrize("rows", [40, 250])
+@pytest.mark.parametrize("width", [64, 4096, 8192, 16384])
+def test_linear_loss_of_exact_logits(width, rows, kind, grad):
+    vocab, g = 600, _gen(width)
+    hidden = torch.zeros((rows, width), device=DEV)
+    if kind == "one element":
+        # one product a logit, up to 64
+        at = torch.randint(0, width, (rows, 1), generator=g, device=DEV)
+        hidden.scatter_(1, at, 16.0)
+        weight = torch.randint(-512, 513, (vocab, width), generator=g, device=DEV) / 128.0
+    else:
+        # multiples of 1/8 that wander up to a few hundred and back: every partial sum is a
+        # whole number of them below 2^24
+        hidden.copy_(torch.randint(0, 2, hidden.shape, generator=g, device=DEV) * 2.0 - 1.0)
+        weight = torch.randint(-1, 2, (vocab, width), generator=g, device=DEV) / 8.0
+        weight[:, width // 2:] += 2.0 * weight[:, width // 2:].sign() * (width >= 4096)
+        weight[:, width // 2 + width // 4:] = -weight[:, width // 2:width // 2 + width // 4]
+        hidden[:, width // 2 + width // 4:] = hidden[:, width // 2:width // 2 + width // 4]
+    hidden, weight = hidden.to(BF16), weight.to(BF16)
+    labels = torch.randint(0, vocab, (rows,), generator=g, device=DEV).int()
+    _, row, _, _ = sw.slimwise_linear_loss(hidden, weight, labels, grad_hidden=grad, grad_weight=False)
+    z = hidden.double() @ weight.double().T
+    y = labels.long()[:, None]
+    over = torch.logsumexp(z.scatter(1, y, -math.inf), 1) - z.gather(1, y)[:, 0]
+    want = over.clamp(min=0) + torch.log1p(torch.exp(-over.abs()))
+    # the logits are exact.  A difference of logits d is rounded, then times log2 e: its exponential
+    # is off by 2 |d| 2^-24 of itself and 2^-22; sums of 128 + 64 + 64 terms; the logarithm's and
+    # the last sum's roundings
+    d = (z - z.gather(1, y)).abs().amax(1)
+    off = d * 2.0 ** -23 + 2.0 ** -21 + 300 * 2.0 ** -24
+    if kind == "sums that cancel":
+        # nothing is cut off, but what is expected to be is given back: 1e-9 of a logit for each
+        # element (of one element less than a rounding)
+        off = off + 1.01e-9 * width * z.abs().amax(1)
+    _within(row, want, off * want.clamp(max=1.0) + want * 2.0 ** -22)
+
+
+@pytest.mark.parametrize("grad", [True, False])
+@pytest.mark.parametrize("rows", [40, 250])
+@pytest.mark.parametrize("width", [2048, 4096, 8192, 16384])
+def test_linear_loss_of_dense_rows_is_not_too_small(width, rows, grad):
+    # another word's logit is about 15 and grows steadily: uncorrected, it and the loss are too
+    # small by 1e-9 of it for each element; a tenth of that differs with how the sums grow
+    vocab, g = 2000, _gen(width + rows)
+    weight = (torch.randn((vocab, width), generator=g, device=DEV) * (1.5 / math.sqrt(width))).to(BF16)
+    other = torch.randint(1000, vocab, (rows,), generator=g, device=DEV)
+    hidden = (torch.randn((rows, width), generator=g, device=DEV) + 15 / 2.25 * weight[other].float()).to(BF16)
+    labels = torch.randint(0, 1000, (rows,), generator=g, device=DEV).int()
+    _, row, _, _ = sw.slimwise_linear_loss(hidden, weight, labels, grad_hidden=grad, grad_weight=False)
+    z = hidden.double() @ weight.double().T
+    p = torch.softmax(z, 1)
+    cut = 1e-9 * width * float((p * z).sum(1).mean())
+    error = float((row.double() - (torch.logsumexp(z, 1) - z.gather(1, labels.long()[:, None])[:, 0])).mean())
+    assert cut > 2e-5 and abs(error) <= 0.25 * cut + 2.0 ** -21
