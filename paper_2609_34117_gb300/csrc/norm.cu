@@ -286,12 +286,13 @@ struct GradArgs {
 
 // Threads of a row (TPR) and elements of a thread (N): bf16 rows up to 256 (32, 8), 512
 // (32, 16), 1024 (128, 8), 2048 (256, 8), 4096 (256, 16), 8192 (512, 16), 12288 (512, 24)
-// and 16384 (512, 32); fp32 with more threads between, and 10 and 12 elements.  512 threads
-// are on an SM, several groups to a CTA, whose sums are joined before they leave: as many
-// CTAs as groups cost 4 us at 32768 x 1000.  Bound by memory and a row's barrier: 16384 x 2048
-// bf16 RMS norm 33 us by itself, 6.1 TB/s.  A ring of asynchronous copies
-// in place of the next row in registers took 133 us for 6000 x 7168 fp32, this 96.  bf16
-// rows of 4001, 32768 of them: alike in all tensors 162, anywhere 258.
+// and 16384 (512, 32); fp32 with more threads between, and 12 elements up to 6144 (10 up to
+// 5120 take as long: 4099 x 5001 55.4 us with either, 20000 x 5001 214 against 212.6 with
+// 12, behind a cold cache).  512 threads are on an SM, several groups to a CTA, whose sums
+// are joined before they leave: as many CTAs as groups cost 4 us at 32768 x 1000.  Bound by
+// memory and a row's barrier: 16384 x 2048 bf16 RMS norm 33 us by itself, 6.1 TB/s.  A ring
+// of asynchronous copies in place of the next row in registers took 133 us for 6000 x 7168
+// fp32, this 96.  bf16 rows of 4001, 32768 of them: alike in all tensors 162, anywhere 258.
 template <int TPR>
 constexpr int kBlock = TPR == 32 ? 256 : 512;
 // Rows of a group at once; the next ones come into registers meanwhile where these hold
@@ -665,7 +666,6 @@ struct GradCall {
            : a.hidden <= 1024 ? rows<T, V, kForm, 128, 8>()
            : a.hidden <= 2048 ? rows<T, V, kForm, 256, 8>()
            : a.hidden <= 4096 ? rows<T, V, kForm, V == 8 ? 256 : 512, V == 8 ? 16 : 8>()
-           : V < 4 && a.hidden <= 5120 ? rows<T, V, kForm, 512, V < 4 ? 10 : 16>()
            : V < 8 && a.hidden <= 6144 ? rows<T, V, kForm, 512, V < 8 ? 12 : 16>()
            : a.hidden <= 8192  ? rows<T, V, kForm, 512, 16>()
            : a.hidden <= 12288 ? rows<T, V, kForm, 512, 24>()
