@@ -1,12 +1,12 @@
 """Edges of the operators around the layer: where variants meet alignment, infinite
-logits, and logits whose sums are exact or dense."""
+logits, logits whose sums are exact or dense, and long lists of ids."""
 import math
 
 import pytest
 import torch
 
 import paper_2609_34117_gb300 as sw
-from tests.test_gpu_train_ops import BF16, DEV, _check_norm, _gen, _grad_reference, _half, _head, _randn, _rows, _within
+from tests.test_gpu_train_ops import BF16, DEV, F32, NAN, _check_norm, _gen, _grad_reference, _half, _head, _randn, _rows, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -174,3 +174,40 @@ def test_linear_loss_of_dense_rows_is_not_too_small(width, rows, grad):
     cut = 1e-9 * width * float((p * z).sum(1).mean())
     error = float((row.double() - (torch.logsumexp(z, 1) - z.gather(1, labels.long()[:, None])[:, 0])).mean())
     assert cut > 2e-5 and abs(error) <= 0.25 * cut + 2.0 ** -21
+
+
+# ---------------------------------------------------------------------------
+# the table's gradient: long lists
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,odtype", [(BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("kind", ["one token", "few tokens", "log-uniform", "all different"])
+@pytest.mark.parametrize("rows,hidden", [(70001, 16), (131072, 9), (200003, 8), (1 << 20, 8)])
+def test_embed_grad_of_long_lists(rows, hidden, kind, dtype, odtype):
+    vocab, g = 1 << 20 if kind == "all different" else 100003, _gen(rows)
+    if kind == "one token":
+        ids = torch.full((rows,), 77, device=DEV)
+    elif kind == "few tokens":
+        ids = torch.randint(0, 5, (rows,), generator=g, device=DEV) * 25000
+    elif kind == "log-uniform":
+        ids = (vocab ** torch.rand(rows, generator=g, device=DEV)).long().clamp(max=vocab) - 1
+    else:
+        ids = torch.randperm(vocab, generator=g, device=DEV)[:rows]
+    ids = ids.int()
+    if kind != "all different":
+        ids[::16], ids[5::977] = -1, vocab
+    grad = torch.randn((rows, hidden), generator=g, device=DEV).to(dtype)
+    out = torch.full((vocab, hidden), NAN, dtype=odtype, device=DEV)
+    sw.slimwise_embed_grad(grad, ids, out, scale=2.0)
+    live = (ids >= 0) & (ids < vocab)
+    at, v = ids[live].long(), grad[live].double()
+    zeros = torch.zeros((vocab, hidden), dtype=torch.float64, device=DEV)
+    want, sizes = zeros.index_add(0, at, v) * 2.0, zeros.index_add(0, at, v.abs()) * 2.0
+    count = torch.bincount(at, minlength=vocab).double()
+    # a token's positions are summed in pieces of 256 at most (4 at least), which are then added in
+    # order: a chain of 256 additions and one a piece, of 64 at least where the list is this long
+    chain = (256.0 + count / 64 + 2.0).clamp(max=float(1 << 20)).minimum(count + 2.0)[:, None] * 2.0 ** -24
+    _within(out, want, want.abs() * (_half(odtype) + 2.0 ** -23) + sizes * chain)
+    assert bool((out[count == 0] == 0).all())
+    again = torch.empty_like(out)
+    sw.slimwise_embed_grad(grad, ids, again, scale=2.0)
+    assert torch.equal(out, again)
