@@ -1087,8 +1087,9 @@ __global__ void __launch_bounds__(kSumThreads, 2) sums_kernel(Call c, int chunk,
     }
     S = warp_sum(S);
     // a logit of +inf: the formula has no number, but the others' exponentials are 0 where it is the
-    // label's, and the sum's inverse is 0 where it is another's
-    if (z == INFINITY || top == INFINITY) S = __int_as_float(0x7FC00000);
+    // label's, and the sum's inverse is 0 where it is another's.  Nor where the label's is the only
+    // one and -inf.
+    if (z == INFINITY || top == INFINITY || (z == -INFINITY && S == 0.0f)) S = __int_as_float(0x7FC00000);
     const float own = ref == z ? 1.0f : ex2((z - ref) * kLog2e);
     float scale = 0.0f;
     if (live) {

@@ -115,6 +115,20 @@ def test_linear_loss_of_logits_of_minus_infinity(rows, width, vocab):
             assert torch.equal(gw[:, 1:], want[3][:, 1:])
 
 
+@pytest.mark.parametrize("vocab", [1, 2, 300])
+@pytest.mark.parametrize("rows", [3, 200])
+def test_linear_loss_where_all_logits_are_minus_infinity(rows, vocab):
+    hidden, weight = torch.zeros((rows, 64), dtype=BF16, device=DEV), torch.zeros((vocab, 64), dtype=BF16, device=DEV)
+    weight[:, 3], hidden[::2, 3] = -HUGE, HUGE
+    labels = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    bad = torch.arange(rows, device=DEV) % 2 == 0
+    for dh, dw in PARTS:
+        _, row, gh, gw = sw.slimwise_linear_loss(hidden, weight, labels, grad_hidden=dh, grad_weight=dw)
+        assert torch.equal(row.isnan(), bad) and bool(((row[~bad] - math.log(vocab)).abs() <= 1e-5).all())
+        assert gh is None or bool(gh[bad].isnan().all())
+        assert gw is None or bool(gw.isnan().all())
+
+
 # ---------------------------------------------------------------------------
 # the head's cross entropy: what the tensor cores cut off a logit
 # ---------------------------------------------------------------------------
