@@ -545,8 +545,9 @@ int slimwise_norm_grad(const void *dy, int64_t dy_stride, const void *x, int32_t
                        void *stream, void *workspace, size_t workspace_bytes);
 
 /*
- * Cross entropy of the logits z = hidden weight^T, which are not kept, and its
- * gradients:
+ * Cross entropy of the logits z = hidden weight^T, and its gradients.  The loss
+ * alone keeps no logits; with a gradient their exponentials are kept in bf16, in the
+ * workspace, in chunks of rows:
  *   L_t  = log sum_v exp z_tv - z_t[label_t],   loss = sum_t row_weight[t] L_t
  *   grad_hidden = dz weight,  grad_weight = dz^T hidden,
  *   dz_tv = row_weight[t] (softmax(z_t)_v - [v = label_t])
@@ -561,15 +562,19 @@ int slimwise_norm_grad(const void *dy, int64_t dy_stride, const void *x, int32_t
  *   grad_hidden  bf16 [rows, width], NULL to skip
  *   grad_weight  grad_weight_dtype [vocab, width], NULL to skip
  *   workspace    256-byte aligned, slimwise_linear_loss_workspace_size() bytes for
- *                the gradients asked for: 2 bytes for each row and token, at most
- *                2^31 of them, and a 32nd of that; up to 8 for each element of
- *                hidden; 160 MB for sums of a split product; and, where the rows
- *                come in chunks, 4 for each element of weight
+ *                the gradients asked for: 2 bytes for each row and token (as many as
+ *                bf16 logits), at most 2^31 of them, and a 32nd of that; up to 8 for
+ *                each element of hidden; 160 MB for sums of a split product; and,
+ *                where the rows come in chunks, 4 for each element of weight.
+ *                Without gradients: 16 for each row and 256 tokens, and 2 for each
+ *                element of hidden
  * A row with a label >= vocab, a NaN or a logit of +inf has NaN loss and gradient,
  * and grad_weight is then NaN where the formula has it; a label's logit of -inf has
  * loss +inf and the formula's gradient (NaN where all logits are -inf).  dz's
- * numerators (which the products take) and the rows scaled by their weights are
- * rounded to bf16.  A device wait that gave up is reported by
+ * numerators (which the products take) and, above 128 rows, the rows scaled by
+ * their weights are rounded to bf16, whatever grad_weight's type: an fp32
+ * grad_weight is then 1.6e-3 of its norm off (to 128 rows 4e-5), a bf16 one, rounded
+ * besides, 2.3e-3.  A device wait that gave up is reported by
  * slimwise_moe_device_status(workspace, ...).
  */
 int slimwise_linear_loss_workspace_size(int32_t rows, int32_t width, int32_t vocab,

@@ -739,8 +739,9 @@ def slimwise_linear_loss_workspace_size(rows: int, hidden: int, vocab: int, grad
 def slimwise_linear_loss(hidden, weight, labels, row_weight=None, grad_hidden=True, grad_weight=True,
                          row_loss=None, loss=None, workspace=None, stream=None):
     """Cross entropy of the head's logits hidden @ weight.T (bf16 [rows, width] and
-    [vocab, width]) at labels int32 [rows] (negative: the row is left out), without
-    keeping the logits, and its gradients.  row_weight fp32 [rows], e.g. 1 / the
+    [vocab, width]) at labels int32 [rows] (negative: the row is left out), and its
+    gradients.  The loss alone keeps no logits; with a gradient the workspace holds
+    their exponentials in bf16 (as large as bf16 logits, at most 2 GiB).  row_weight fp32 [rows], e.g. 1 / the
     number of labelled rows; None: 1 each.  grad_hidden, grad_weight: True to
     allocate that gradient, False to leave it out, or the tensor to write (the
     weight's in bf16 or fp32).  Returns (loss fp32 [1], row losses fp32 [rows],

@@ -1,5 +1,6 @@
 // linear_loss.cu -- cross entropy of a head's logits from the hidden rows and the
-// head's weight, with the gradients of both; the logits are not kept.
+// head's weight, with the gradients of both.  The loss alone keeps no logits; the
+// gradients keep their exponentials in bf16, in the workspace.
 //
 //   z = h W^T,  L_t = log sum_v exp z_tv - z_ty,  loss = sum_t w_t L_t
 //   dz_tv = w_t (softmax(z_t)_v - [v = y]),  dh = dz W,  dW = dz^T h
@@ -47,11 +48,11 @@ constexpr float kMostLoss = 60.0f;
 // The tensor cores' fp32 sums are cut, not rounded, at each step of the contraction that
 // adds something: a logit of a dense row is too small in magnitude by 1.03e-9 of itself
 // for each element of the width where it grows steadily, 0.9e-9 where it wanders (widths of
-// 512 to 16384 alike), while the label's, of plain sums, is not.  The expected loss is given
-// back, by the pieces of 8 elements of the row that are not all zeros: mean error of 300 row
-// losses (10 to 16) at 8192 3e-7 in place of -1.1e-5, of 200 at 16384 under 1e-7 in place
-// of -2.1e-5.  It is an expectation: a sum that happens to be exact gets its share all the same,
-// 1e-9 of the logit for each element.
+// 512 to 4096 alike), while the label's, of plain sums, is not.  The expected loss is given
+// back, by the pieces of 8 elements of the row that are not all zeros.  It holds beyond: mean
+// error of 300 row losses (10 to 16) at 8192 3e-7 in place of -1.1e-5, of 200 at 16384
+// under 1e-7 in place of -2.1e-5.  It is an expectation: a sum that happens to be exact gets
+// its share all the same, 1e-9 of the logit for each element.
 constexpr float kTruncated = 1.0e-9f;
 constexpr int64_t kMostCells = 1ll << 30;
 constexpr int kTile = 256;       // rows and columns of a pair's tile
@@ -97,7 +98,10 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // numerator is most of a row of dW, so that its rounding is most of dW's error.  Up to
 // 128 rows, where dW's product waits for memory, a second part holds the rest (for 64
 // rows of 32000 words at 1024 dW's error against 64 bits 0.0023 -> 0.0017, its rounding to
-// bf16 alone).
+// bf16 alone).  Above, it would double a product that the tensor cores bound: 1021 x 65537
+// at 2048 478 -> 593 us, 4096 x 131072 3.11 -> 4.1 ms, for 0.0023 -> 0.0017 in bf16 and 0.0016
+// -> 4e-5 in fp32; a bf16 program's dz is rounded alike.  (One rule for both types: dW in
+// bf16 is the fp32 one rounded.)
 __host__ __device__ inline int scaled_parts(int rows) { return rows <= 128 ? 2 : 1; }
 
 // N of the products with swapped roles, or 0: rows are M, in tiles of 256.  The swapped
