@@ -54,6 +54,7 @@ constexpr float kMostLoss = 60.0f;
 // under 1e-7 in place of -2.1e-5.  It is an expectation: a sum that happens to be exact gets
 // its share all the same, 1e-9 of the logit for each element.
 constexpr float kTruncated = 1.0e-9f;
+__host__ __device__ inline float given_back(int elements) { return fmaf((float)elements, kTruncated, 1.0f); }
 constexpr int64_t kMostCells = 1ll << 30;
 constexpr int kTile = 256;       // rows and columns of a pair's tile
 constexpr int kHalf = 128;       // of a CTA's share of an operand
@@ -167,6 +168,7 @@ Layout make_plan(int rows, int hidden, int vocab, bool grad_hidden, bool grad_we
 // Device view of the workspace and the call.
 struct Call {
   int T, H, V;
+  float dense;  // given_back() of rows without a piece of zeros
   int rows_pad, chunk, vocab_tiles, hidden_tiles;
   int rows_tile;  // of the first product and dh's
   int64_t cells_stride;
@@ -282,7 +284,7 @@ __global__ void __launch_bounds__(kGatherThreads, 2) gather_kernel(Call c, int c
     added = __reduce_add_sync(0xFFFFFFFFu, added);
     if (!known) s = __int_as_float(0x7FC00000);  // a label outside the vocabulary: NaN
     if (lane == 0) {
-      c.unbias[at] = 1.0f + (float)(8 * added) * kTruncated;
+      c.unbias[at] = given_back(8 * added);
       c.orig[at] = t;
       c.label[at] = y;
       c.target[at] = c.ref[at] = s;
@@ -471,22 +473,20 @@ __device__ __forceinline__ float reduce_across(float (&x)[32], int lane, F op) {
   return x[0];
 }
 
-// Swapped roles: 32 rows' logits z at the lane's word; ref: the rows' references and
-// factors.  Leaves their numerators in bf16 at
-// `staged` (64 bytes a row, zeros for rows past `live`), and returns to lane j row j's
-// sum over the warp's words and largest logit.
+// Swapped roles: 32 rows' logits z at the lane's word; unbias: their common factor.  Leaves
+// their numerators in bf16 at `staged` (64 bytes a row, zeros for rows past `live`), and
+// returns to lane j row j's sum over the warp's words and largest logit.
 template <Mode kMode>
-__device__ __forceinline__ float2 swapped_numerators(float (&z)[32], const float2 *ref, const int *label, int word, bool known,
-                                                  int live, int lane, uint32_t staged) {
+__device__ __forceinline__ float2 swapped_numerators(float (&z)[32], float unbias, const float *ref, const int *label, int word,
+                                                 bool known, int live, int lane, uint32_t staged) {
   float top = kFloor;
 #pragma unroll
   for (int j = 0; j < 32; ++j) {
     const bool in = known && word != label[j];
     const float most = warp_max_redux(in ? z[j] : kFloor);
     if (lane == j) top = most;
-    const float2 of_row = ref[j];
-    const float r = kMode == kForward ? most : of_row.x;
-    const float e = ex2(fmaf(z[j], of_row.y, -r) * kLog2e);
+    const float r = kMode == kForward ? most : ref[j];
+    const float e = ex2(fmaf(z[j], unbias, -r) * kLog2e);
     if constexpr (kMode == kNumerators) {
       const __nv_bfloat16 h = __float2bfloat16_rn(j < live ? e : 0.0f);
       asm volatile("st.shared.b16 [%0], %1;" ::"r"(staged + (uint32_t)(j * 64 + lane * 2)),
@@ -602,8 +602,9 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
   volatile int *consumed = misc + 2;
   volatile int *n_splits = misc + 3;
   double *warp_totals = reinterpret_cast<double *>(misc + 4);  // kGradWeight
-  float2 *row_ref = reinterpret_cast<float2 *>(smem + kRingBytes - kRowData);  // kSwapped: reference, factor
-  int *row_label = reinterpret_cast<int *>(row_ref + kSwapRows);
+  float *row_ref = reinterpret_cast<float *>(smem + kRingBytes - kRowData);  // kSwapped
+  float *row_unbias = row_ref + kSwapRows;
+  int *row_label = reinterpret_cast<int *>(row_unbias + kSwapRows);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t crank = cluster_ctarank();
@@ -664,7 +665,8 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
     work.units = work.mt * work.nt;
     if constexpr (kSwapped) {
       for (int i = threadIdx.x; i < work.mt * n_rows; i += blockDim.x) {
-        row_ref[i] = i < rows ? make_float2(__ldcg(c.ref + i), __ldcg(c.unbias + i)) : make_float2(0.0f, 1.0f);
+        row_ref[i] = i < rows ? __ldcg(c.ref + i) : 0.0f;
+        row_unbias[i] = i < rows ? __ldcg(c.unbias + i) : c.dense;
         row_label[i] = i < rows ? __ldcg(c.label + i) : -1;
       }
       __syncthreads();
@@ -891,20 +893,27 @@ __global__ void __launch_bounds__(kGemmThreads + (kMode == kGradWeight ? kJoinTh
         const uint32_t staged = smem_base + (uint32_t)(kRingBytes + (warp - 2) * kOutBytes / 2);
 #pragma unroll 1
         for (int t0 = 32 * half; t0 < n_rows; t0 += 64) {
+          const int live = rows - row_first - t0;
           float z[32];
           tmem_ld_row(lanes + t0, z);
           tmem_ld_wait();
           if (t0 + 64 >= n_rows) release();
-          const int live = rows - row_first - t0;
           if constexpr (kMode == kGradHidden) {
             float *to = c.splits + ((int64_t)u * kTile + t0) * kTile + in_tile;
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               if (j < live) to[j * kTile] = z[j];
           } else {
+            // (rows that are not dense: in advance, which rounds the logits once more.  Factors that
+            // are read row by row in all cases cost 3 % of the product.)
+            const float *unbias = row_unbias + row_first + t0;
+            const bool dense = __all_sync(0xFFFFFFFFu, unbias[lane] == c.dense);
+            if (!dense)
+#pragma unroll
+              for (int j = 0; j < 32; ++j) z[j] *= unbias[j];
             quarters[((local & 1) * 4 + q) * kTile + t0 + lane] =
-                swapped_numerators<kMode>(z, row_ref + row_first + t0, row_label + row_first + t0, mine, mine < c.V,
-                                          live, lane, staged);
+                swapped_numerators<kMode>(z, dense ? c.dense : 1.0f, row_ref + row_first + t0, row_label + row_first + t0,
+                                          mine, mine < c.V, live, lane, staged);
           }
           if constexpr (kMode == kNumerators) {
             // the warp's 32 words of each row, 64 bytes; as far as dW's slices read
@@ -1245,6 +1254,7 @@ cudaError_t launch_linear_loss(const LinearLossArgs &a, void *workspace, cudaStr
   char *w = static_cast<char *>(workspace);
   Call c = {};
   c.T = a.rows; c.H = a.width; c.V = a.vocab;
+  c.dense = given_back(c.H);
   c.rows_pad = l.rows_pad; c.chunk = l.chunk;
   c.vocab_tiles = l.vocab_tiles; c.hidden_tiles = l.hidden_tiles;
   c.rows_tile = l.rows_tile ? l.rows_tile : kTile;

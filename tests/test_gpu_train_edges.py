@@ -172,6 +172,24 @@ def test_linear_loss_of_exact_logits(width, rows, kind, grad):
 
 
 @pytest.mark.parametrize("grad", [True, False])
+@pytest.mark.parametrize("rows", [40, 250, 600])
+def test_linear_loss_of_dense_rows_among_others(rows, grad):
+    width, vocab, g = 4096, 900, _gen(rows)
+    hidden, weight, labels, wt = _head(rows, width, vocab, seed=rows, ignored=0.0)
+    some = torch.rand(rows, generator=g, device=DEV) < 0.2
+    alone = sw.slimwise_linear_loss(hidden, weight, torch.where(some, -1, labels).int(), wt, grad_hidden=grad, grad_weight=False)
+    hidden[some] = 0.0
+    hidden[some, 17] = 30.0
+    row = sw.slimwise_linear_loss(hidden, weight, labels, wt, grad_hidden=grad, grad_weight=False)[1]
+    z = hidden.double() @ weight.double().T
+    # a logit of a dense row may be rounded once more, and then the difference to the label's
+    largest = z.abs().amax(1)
+    _within(row[~some], alone[1][~some].double(), (largest * 2.0 ** -22 + 2.0 ** -21 * alone[1].abs())[~some])
+    want = torch.logsumexp(z, 1) - z.gather(1, labels.long()[:, None])[:, 0]
+    _within(row[some], want[some], (2 * largest * 2.0 ** -23 + 2.0 ** -21 + 300 * 2.0 ** -24 + want * 2.0 ** -22)[some])
+
+
+@pytest.mark.parametrize("grad", [True, False])
 @pytest.mark.parametrize("rows", [40, 250])
 @pytest.mark.parametrize("width", [2048, 4096, 8192, 16384])
 def test_linear_loss_of_dense_rows_is_not_too_small(width, rows, grad):
